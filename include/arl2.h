@@ -47,7 +47,8 @@ typedef enum {
     ARL2_ERR_UNSUPPORTED = -2, /* shape / dtype combination with no kernel                  */
     ARL2_ERR_CUDA = -3,        /* a CUDA runtime or driver call failed                      */
     ARL2_ERR_TIMEOUT = -4,     /* a bounded wait inside a kernel expired (device status)    */
-    ARL2_ERR_WORKSPACE = -5    /* workspace too small or misaligned                         */
+    ARL2_ERR_WORKSPACE = -5,   /* workspace too small or misaligned                         */
+    ARL2_ERR_RANGE = -6        /* a page number, length or position outside of a cache (device status) */
 } arl2_status;
 
 typedef enum {
@@ -265,6 +266,85 @@ int arl2_project_in(arl2_ctx* ctx, const void* d_x, void* d_q, void* d_k, void* 
                     void* stream);
 int arl2_project_out(arl2_ctx* ctx, const void* d_o, void* d_y, void* stream);
 
+/*
+ * A paged key/value cache held in 4 bits, for the softmax layers of a stack (Eq. 1 over a growing cache): append rotates new
+ * keys and rounds keys and values on the way, attend is softmax attention over what is held.  The cache belongs to a context,
+ * whose B, H, D, I/O type, softmax scale, status word and launch counter it shares; the context must outlive it.
+ *
+ * Format.  A cached row (one token, one key head) is cut into groups of 64 channels; a group is held as two fp16 numbers,
+ * its minimum and a step, and one 4-bit code per channel, which stands for  minimum + step * code:
+ *   minimum = fp16(min x),  step = fp16((max x - min x) / 15),  code = round((x - minimum) / step), held to 0 .. 15
+ * (in fp32, the divisions as products with fp32 reciprocals; a step of zero gives codes of zero).  Magnitudes above 61440 are
+ * held as 61440; a NaN makes its group's values NaN.
+ * A page holds `page_tokens` tokens of one stream for all kv_heads: [kv_heads] units of
+ *   K codes [page_tokens, D/2] bytes | V codes, the same | K parameters [page_tokens, D/64] of (minimum, step) | V parameters
+ * with the even channel of a pair in the low half of its byte.  The page table [B, max_pages] int32 names the pages of each
+ * stream in order; entries past a stream's length are not looked at, and several streams may name the same page.
+ *
+ *   kv_heads     key/value heads; divides H, and query head h reads key head h / (H / kv_heads)
+ *   page_tokens  16, 32, 64, 128 or 256
+ *   num_pages    pages in the pool, max_pages pages per stream (page_tokens * max_pages <= 2^30)
+ *   rope_rows    positions in the rotary tables, 0 = no rotation
+ */
+typedef struct arl2_cache arl2_cache; /* opaque, host memory owned by the library */
+typedef struct {
+    uint32_t struct_size;
+    int32_t kv_heads;
+    int32_t page_tokens;
+    int32_t num_pages;
+    int32_t max_pages;
+    int32_t rope_rows;
+} arl2_cache_config;
+
+/* Bytes of one page, and of the scratch that a cache needs (256-byte aligned base).  0 for an invalid configuration. */
+size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg);
+size_t arl2_cache_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg);
+
+/*
+ *   d_pages       [num_pages, arl2_cache_page_bytes] bytes, 128-byte aligned; not cleared
+ *   d_page_table  [B, max_pages] int32, may be rewritten between calls in stream order
+ *   d_rope_cos, d_rope_sin  [rope_rows, D/2] fp32, 16-byte aligned; both NULL where rope_rows is 0
+ *   d_workspace   private to this cache until arl2_cache_destroy
+ * All stay the caller's.  Launches one small kernel on `stream`.  Calls on one cache are ordered by the caller (one stream, or
+ * events between streams): they share the workspace.  Calls may be captured and replayed.
+ */
+int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d_pages, const int32_t* d_page_table,
+                      const float* d_rope_cos, const float* d_rope_sin, void* d_workspace, size_t workspace_bytes,
+                      void* stream, arl2_cache** out);
+
+/*
+ * Tokens start[b] .. start[b] + tokens - 1 of each stream, written to their places (over whatever is there, as a block is
+ * written anew at every denoising step):
+ *   K row of position t = RoPE_t(k[b, t - start[b], h]),  V row = v[b, t - start[b], h],  both rounded to the format above.
+ *   d_k, d_v      [B, tokens, kv_heads, D] of the I/O type; heads and channels contiguous, batch and token strides in elements
+ *   d_start       [B] int32; a negative entry marks an idle stream, for which nothing is written
+ *   d_k_held, d_v_held  [B, tokens, kv_heads, D] of the I/O type, each may be NULL: the values that the cache now stands for
+ *                 (zeros where nothing was written)
+ * A token past the table, in a page that the pool does not have, or past the rotary tables is left out, and arl2_sync_status
+ * reports ARL2_ERR_RANGE.
+ */
+int arl2_cache_append(arl2_cache* cache, const void* d_k, int64_t k_batch_stride, int64_t k_token_stride,
+                      const void* d_v, int64_t v_batch_stride, int64_t v_token_stride, int32_t tokens,
+                      const int32_t* d_start, void* d_k_held, void* d_v_held, void* stream);
+
+/*
+ * Softmax attention of `queries` new rows per stream over the first lengths[b] tokens that the cache holds:
+ *   d_out[b,i,h,:] = softmax_j(<RoPE_t(q[b,i,h]), K_j> scale) V_j,   t = q_start[b] + i,
+ * j = 0 .. lengths[b] - 1, with ARL2_CACHE_CAUSAL only j <= t.  A row that sees no key is zero.
+ *   d_q        [B, queries, H, D] of the I/O type, strides as in arl2_cache_append; d_out the same, contiguous
+ *   d_lengths  [B] int32, 0 allowed; d_q_start [B] int32 or NULL: the queries are the last tokens held, lengths[b] - queries
+ * Positions before the first row of the rotary tables count as the first row.  A length past the table, a page that the pool
+ * does not have, or a position past the rotary tables counts as the last there is (a page: as not visible), and
+ * arl2_sync_status reports ARL2_ERR_RANGE.  bf16 I/O: fp16 operands on tensor cores, fp32 softmax and sums; fp32 I/O: each
+ * fp32 operand as two fp16 numbers (the codes are exact), to fp32's accuracy.  Bitwise reproducible.
+ */
+#define ARL2_CACHE_CAUSAL 1u
+int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride, int64_t q_token_stride, int32_t queries,
+                      const int32_t* d_lengths, const int32_t* d_q_start, uint32_t flags, void* d_out, void* stream);
+
+/* Frees the host object only; no device buffer is touched and nothing is synchronised. */
+void arl2_cache_destroy(arl2_cache* cache);
+
 /* S <- 0 for stream `stream_index` (0..B-1) or all streams (-1): Algorithm 1, first line. */
 int arl2_reset(arl2_ctx* ctx, int32_t stream_index, void* stream);
 
@@ -278,7 +358,8 @@ int arl2_set_state(arl2_ctx* ctx, const float* src, void* stream);
 /*
  * Synchronise `stream` and return the device status word: ARL2_OK, or ARL2_ERR_TIMEOUT
  * if a bounded wait inside a kernel expired (the kernel then returned early; its output
- * is undefined, the context stays usable).  The word is cleared by the call.
+ * is undefined, the context stays usable), or else ARL2_ERR_RANGE if a cache call met a page, length or position
+ * outside of its bounds.  The word is cleared by the call.
  */
 int arl2_sync_status(arl2_ctx* ctx, void* stream);
 

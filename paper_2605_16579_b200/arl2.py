@@ -21,6 +21,7 @@ ARL2_FLAG_TOKEN_GATES = 2
 ARL2_FLAG_GATE_SCALAR = 4
 ARL2_FLAG_GATE_ELEMENTWISE = 8
 ARL2_FLAG_DELTA_DECAYED_PREDICTION = 32
+ARL2_CACHE_CAUSAL = 1
 
 
 def ARL2_FLAG_DEBUG_WAIT_LIMIT(polls: int) -> int:
@@ -32,6 +33,7 @@ EXPORTS = (
     "arl2_set_profile_events", "arl2_commit_static_scratch", "arl2_commit_delta", "arl2_commit_tokens", "arl2_teacher_step", "arl2_commit_decay_tokens",
     "arl2_step_kernel_name", "arl2_destroy", "arl2_last_error", "arl2_version", "arl2_debug_set_wait_limit", "arl2_debug_set_walk_wait_limit", "arl2_clean_pass", "arl2_denoise_step_token_level",
     "arl2_projection_workspace_bytes", "arl2_set_projections", "arl2_project_in", "arl2_project_out",
+    "arl2_cache_page_bytes", "arl2_cache_workspace_bytes", "arl2_cache_create", "arl2_cache_append", "arl2_cache_attend", "arl2_cache_destroy",
 )
 
 
@@ -46,6 +48,14 @@ class arl2_config(ctypes.Structure):
         ("io_dtype", ctypes.c_int32),
         ("softmax_scale", ctypes.c_float), ("l2_eps", ctypes.c_float),
         ("commit_rule", ctypes.c_int32), ("flags", ctypes.c_uint32),
+    ]
+
+
+class arl2_cache_config(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("kv_heads", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("rope_rows", ctypes.c_int32),
     ]
 
 
@@ -114,6 +124,19 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.arl2_set_profile_events.argtypes = [vp, vp, vp]
     lib.arl2_commit_static_scratch.restype = ctypes.c_int
     lib.arl2_commit_static_scratch.argtypes = [cp] + [vp] * 9
+    ccp, i32, i64, u32 = ctypes.POINTER(arl2_cache_config), ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32
+    lib.arl2_cache_page_bytes.restype = ctypes.c_size_t
+    lib.arl2_cache_page_bytes.argtypes = [cp, ccp]
+    lib.arl2_cache_workspace_bytes.restype = ctypes.c_size_t
+    lib.arl2_cache_workspace_bytes.argtypes = [cp, ccp]
+    lib.arl2_cache_create.restype = ctypes.c_int
+    lib.arl2_cache_create.argtypes = [vp, ccp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]
+    lib.arl2_cache_append.restype = ctypes.c_int
+    lib.arl2_cache_append.argtypes = [vp, vp, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp]
+    lib.arl2_cache_attend.restype = ctypes.c_int
+    lib.arl2_cache_attend.argtypes = [vp, vp, i64, i64, i32, vp, vp, u32, vp, vp]
+    lib.arl2_cache_destroy.restype = None
+    lib.arl2_cache_destroy.argtypes = [vp]
     lib.arl2_launch_count.restype = ctypes.c_uint64
     lib.arl2_launch_count.argtypes = [vp]
     lib.arl2_step_kernel_name.restype = ctypes.c_char_p
@@ -421,6 +444,110 @@ class Layer:
                 and tuple(t.shape) == tuple(shape) and t.dtype == dtype):
             raise Arl2Error(f"{what}: expected a contiguous CUDA tensor {tuple(shape)} {dtype}, got "
                             f"{tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+class Cache:
+    """A paged key/value cache held in 4 bits (the arl2_cache_* entry points), of a layer's B, H, D and dtype.
+
+    ``page_table`` ([B, max_pages] int32) says which pages of the pool hold a stream's tokens, in order; the caller hands them
+    out.  ``pages`` (uint8 [num_pages, page_bytes], uncleared) and ``page_table`` (filled with -1) are made here unless they
+    are handed in.  Rotary tables: [positions, D/2] fp32, both or neither.  Calls on one cache are for one stream at a time.
+    """
+
+    def __init__(self, layer, num_pages, max_pages, kv_heads=None, page_tokens=64, rope_cos=None, rope_sin=None, pages=None, page_table=None):
+        lib = load()
+        self._lib, self._cache = lib, None
+        self.layer, self.device, self.dtype = layer, layer.device, layer.dtype
+        self.kv_heads = layer.H if kv_heads is None else kv_heads
+        rows = 0 if rope_cos is None else int(rope_cos.shape[0])
+        self.cfg = arl2_cache_config(ctypes.sizeof(arl2_cache_config), self.kv_heads, page_tokens, num_pages, max_pages, rows)
+        self.page_bytes = lib.arl2_cache_page_bytes(ctypes.byref(layer.cfg), ctypes.byref(self.cfg))
+        if self.page_bytes == 0:
+            raise Arl2Error("arl2_cache_page_bytes: " + lib.arl2_last_error().decode())
+        n = lib.arl2_cache_workspace_bytes(ctypes.byref(layer.cfg), ctypes.byref(self.cfg))
+        for t in (rope_cos, rope_sin):
+            if t is not None:
+                layer._want(t, (rows, layer.D // 2), torch.float32, "rope table")
+        with torch.cuda.device(self.device):
+            if pages is None:
+                pages = torch.empty(num_pages, self.page_bytes, dtype=torch.uint8, device=self.device)
+            if page_table is None:
+                page_table = torch.full((layer.B, max_pages), -1, dtype=torch.int32, device=self.device)
+            layer._want(pages, (num_pages, self.page_bytes), torch.uint8, "pages")
+            layer._want(page_table, (layer.B, max_pages), torch.int32, "page_table")
+            self.pages, self.page_table, self._rope = pages, page_table, (rope_cos, rope_sin)
+            self._workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+            handle = ctypes.c_void_p()
+            _check(lib.arl2_cache_create(layer._ctx, ctypes.byref(self.cfg), _ptr(pages), _ptr(page_table), _ptr(rope_cos), _ptr(rope_sin),
+                                         _ptr(self._workspace), n, _stream(), ctypes.byref(handle)), "arl2_cache_create")
+        self._cache = handle
+
+    def append(self, k, v, start, held=False):
+        """Rows k, v [B, T, kv_heads, D] of tokens start[b] .. start[b] + T - 1 (start: int32 [B], negative: idle stream), keys
+        rotated to their positions.  ``held=True`` returns (k, v) as the cache now holds them, which may also be given as a pair
+        of tensors to write to."""
+        layer = self.layer
+        shape = (layer.B, int(k.shape[1]), self.kv_heads, layer.D)
+        ks, vs = self._rows(k, shape, "k"), self._rows(v, shape, "v")
+        layer._want(start, (layer.B,), torch.int32, "start")
+        kh = vh = None
+        if held is not False:
+            kh, vh = (torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(2)) if held is True else held
+            layer._want(kh, shape, self.dtype, "held keys")
+            layer._want(vh, shape, self.dtype, "held values")
+        self._run("arl2_cache_append", k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], shape[1], start.data_ptr(), _ptr(kh), _ptr(vh))
+        return None if kh is None else (kh, vh)
+
+    def attend(self, q, lengths, q_start=None, causal=False, out=None):
+        """Attention of q [B, T, H, D] over the first lengths[b] tokens held (int32 [B]); q is rotated to its positions
+        q_start[b] + i, by default those of the last T tokens.  ``causal``: query i sees the tokens up to its own position."""
+        layer = self.layer
+        shape = (layer.B, int(q.shape[1]), layer.H, layer.D)
+        qs = self._rows(q, shape, "q")
+        layer._want(lengths, (layer.B,), torch.int32, "lengths")
+        if q_start is not None:
+            layer._want(q_start, (layer.B,), torch.int32, "q_start")
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        else:
+            layer._want(out, shape, self.dtype, "out")
+        self._run("arl2_cache_attend", q.data_ptr(), qs[0], qs[1], shape[1], lengths.data_ptr(), _ptr(q_start), ARL2_CACHE_CAUSAL if causal else 0, out.data_ptr())
+        return out
+
+    def close(self):
+        if self._cache is not None:
+            self._lib.arl2_cache_destroy(self._cache)
+            self._cache = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- helpers -----------------------------------------------------------------------
+    def _rows(self, t, shape, what):
+        """The batch and token strides of a tensor whose heads and channels are contiguous."""
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is self.dtype and t.shape == shape:
+            st = t.stride()
+            if (st[3] == 1 or shape[3] == 1) and (st[2] == shape[3] or shape[2] == 1):
+                # (a dimension of one element may have any stride)
+                return st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else shape[2] * shape[3]
+        raise Arl2Error(f"{what}: expected a CUDA tensor {tuple(shape)} {self.dtype} with contiguous heads and channels, got "
+                        f"{tuple(t.shape)} {t.dtype} with strides {tuple(t.stride())} on {t.device}")
+
+    def _run(self, name, *args):
+        if self.layer._ctx is None:
+            raise Arl2Error(f"{name}: the cache's layer has been closed")
+        current = torch.cuda.current_device()
+        index = self.device.index
+        if index is None or index == current:
+            status = getattr(self._lib, name)(self._cache, *args, _raw_stream(current))
+        else:
+            with torch.cuda.device(index):
+                status = getattr(self._lib, name)(self._cache, *args, _raw_stream(index))
+        if status != 0:
+            _check(status, name)
 
 
 STATIC_SCRATCH_BYTES = 8 << 20

@@ -1065,7 +1065,7 @@ int arl2_sync_status(arl2_ctx* ctx, void* stream)
 {
     if (!check_ctx(ctx)) return ARL2_ERR_INVALID_ARG;
     cudaStream_t st = as_stream(stream);
-    uint32_t words[2] = {0, 0};
+    uint32_t words[kStatusRangeWhere + 1] = {0};
     cudaError_t e = cudaMemcpyAsync(words, ctx->ws + ctx->lay.status, sizeof(words),
                                     cudaMemcpyDeviceToHost, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
@@ -1079,8 +1079,222 @@ int arl2_sync_status(arl2_ctx* ctx, void* stream)
         if (r != ARL2_OK) return r;
         return ARL2_ERR_TIMEOUT;
     }
+    if (words[kStatusRange] != 0) {
+        static const char* const what[] = {"", "a length or token outside of the page table", "a page that the pool does not have",
+                                           "a position outside of the rotary tables"};
+        set_error("a cache call met %s (stream %u)", what[words[kStatusRange] & 3u], words[kStatusRangeWhere]);
+        int r = account(ctx, fill_zero(ctx->ws + ctx->lay.status, kStatusWords * sizeof(uint32_t), st));
+        if (r != ARL2_OK) return r;
+        return ARL2_ERR_RANGE;
+    }
     return ARL2_OK;
 }
+
+namespace {
+
+// Scratch of a cache: tickets of the items that several CTAs share, their rows' statistics, their rows
+struct CacheLayout {
+    size_t tickets, part_ml, part_o, total;
+};
+CacheLayout cache_layout(int D)
+{
+    CacheLayout l;
+    size_t off = 0;
+    l.tickets = off; off += align_up((size_t)kCacheCtas * sizeof(uint32_t));
+    l.part_ml = off; off += align_up((size_t)kCachePartRows * 2 * sizeof(float));
+    l.part_o = off;  off += align_up((size_t)kCachePartRows * D * sizeof(float));
+    l.total = off;
+    return l;
+}
+
+bool valid_cache_config(const arl2_config* cfg, const arl2_cache_config* c)
+{
+    if (!valid_config(cfg)) return false;
+    if (c == nullptr) { set_error("cache config is NULL"); return false; }
+    if (c->struct_size != sizeof(arl2_cache_config)) {
+        set_error("cache config.struct_size is %u, this library expects %zu", c->struct_size, sizeof(arl2_cache_config));
+        return false;
+    }
+    if (c->kv_heads < 1 || cfg->H % c->kv_heads != 0) {
+        set_error("kv_heads must divide H = %d (got %d)", cfg->H, c->kv_heads);
+        return false;
+    }
+    if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1)) != 0) {
+        set_error("page_tokens must be 16, 32, 64, 128 or 256 (got %d)", c->page_tokens);
+        return false;
+    }
+    if (c->num_pages < 1 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens > ((int64_t)1 << 30)) {
+        set_error("num_pages and max_pages must be >= 1, and a stream at most 2^30 tokens (got %d pages, %d per stream of %d tokens)",
+                  c->num_pages, c->max_pages, c->page_tokens);
+        return false;
+    }
+    if (c->rope_rows < 0) { set_error("rope_rows must be >= 0 (got %d)", c->rope_rows); return false; }
+    return true;
+}
+
+size_t cache_unit_bytes(const arl2_config* cfg, const arl2_cache_config* c)
+{
+    return (size_t)c->page_tokens * (cfg->D + cfg->D / 64 * 8);
+}
+
+// Strides of a [B, tokens, heads, D] tensor whose heads and channels are contiguous.
+bool check_strides(const char* who, int64_t batch, int64_t token, int heads, int D)
+{
+    if (batch >= 0 && token >= (int64_t)heads * D && batch < ((int64_t)1 << 40) && token < ((int64_t)1 << 40)) return true;
+    set_error("%s: strides must be in [0, 2^40), a token's at least heads * D (got %lld and %lld)", who, (long long)batch, (long long)token);
+    return false;
+}
+
+bool rows_are_wide(const void* p, int64_t batch, int64_t token, int elem)
+{
+    return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(batch * elem) | (uintptr_t)(token * elem)) % 16 == 0;
+}
+
+}  // namespace
+
+struct arl2_cache {
+    arl2_ctx* ctx;
+    arl2_cache_config cfg;
+    CacheView view;
+    float* part_o;
+    float* part_ml;
+    uint32_t* tickets;
+};
+
+size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
+{
+    if (!valid_cache_config(cfg, cache_cfg)) return 0;
+    return cache_unit_bytes(cfg, cache_cfg) * cache_cfg->kv_heads;
+}
+
+size_t arl2_cache_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
+{
+    if (!valid_cache_config(cfg, cache_cfg)) return 0;
+    return cache_layout(cfg->D).total;
+}
+
+int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d_pages, const int32_t* d_page_table,
+                      const float* d_rope_cos, const float* d_rope_sin, void* d_workspace, size_t workspace_bytes,
+                      void* stream, arl2_cache** out)
+{
+    if (out == nullptr) { set_error("out is NULL"); return ARL2_ERR_INVALID_ARG; }
+    *out = nullptr;
+    if (!check_ctx(ctx) || !valid_cache_config(&ctx->cfg, cache_cfg)) return ARL2_ERR_INVALID_ARG;
+    if (d_pages == nullptr || d_page_table == nullptr || d_workspace == nullptr) {
+        set_error("cache_create: pages, page_table and workspace must not be NULL");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if ((d_rope_cos != nullptr) != (cache_cfg->rope_rows > 0) || (d_rope_sin != nullptr) != (cache_cfg->rope_rows > 0)) {
+        set_error("cache_create: rotary tables must be given where rope_rows > 0, and be NULL where it is 0");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (reinterpret_cast<uintptr_t>(d_pages) % 128 != 0 || reinterpret_cast<uintptr_t>(d_page_table) % 4 != 0 ||
+        reinterpret_cast<uintptr_t>(d_rope_cos) % 16 != 0 || reinterpret_cast<uintptr_t>(d_rope_sin) % 16 != 0) {
+        set_error("cache_create: pages must be 128-byte, rotary tables 16-byte and the page table 4-byte aligned");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    const CacheLayout lay = cache_layout(ctx->cfg.D);
+    if (workspace_bytes < lay.total || reinterpret_cast<uintptr_t>(d_workspace) % kAlign != 0) {
+        set_error("cache_create: the workspace needs %zu bytes, 256-byte aligned (got %zu)", lay.total, workspace_bytes);
+        return ARL2_ERR_WORKSPACE;
+    }
+    arl2_cache* c = new (std::nothrow) arl2_cache();
+    if (c == nullptr) { set_error("out of host memory"); return ARL2_ERR_INVALID_ARG; }
+    uint8_t* ws = static_cast<uint8_t*>(d_workspace);
+    c->ctx = ctx;
+    c->cfg = *cache_cfg;
+    c->view.pages = static_cast<uint8_t*>(d_pages);
+    c->view.table = d_page_table;
+    c->view.kv_heads = cache_cfg->kv_heads;
+    c->view.page_shift = 0;
+    while ((1 << c->view.page_shift) < cache_cfg->page_tokens) ++c->view.page_shift;
+    c->view.num_pages = cache_cfg->num_pages;
+    c->view.max_pages = cache_cfg->max_pages;
+    c->view.unit_bytes = cache_unit_bytes(&ctx->cfg, cache_cfg);
+    c->view.rope_cos = d_rope_cos;
+    c->view.rope_sin = d_rope_sin;
+    c->view.rope_rows = cache_cfg->rope_rows;
+    c->view.status = reinterpret_cast<uint32_t*>(ctx->ws + ctx->lay.status);
+    c->tickets = reinterpret_cast<uint32_t*>(ws + lay.tickets);
+    c->part_ml = reinterpret_cast<float*>(ws + lay.part_ml);
+    c->part_o = reinterpret_cast<float*>(ws + lay.part_o);
+    const int r = account(ctx, fill_zero(c->tickets, kCacheCtas * sizeof(uint32_t), as_stream(stream)));
+    if (r != ARL2_OK) { delete c; return r; }
+    *out = c;
+    return ARL2_OK;
+}
+
+int arl2_cache_append(arl2_cache* cache, const void* d_k, int64_t k_batch_stride, int64_t k_token_stride, const void* d_v,
+                      int64_t v_batch_stride, int64_t v_token_stride, int32_t tokens, const int32_t* d_start, void* d_k_held,
+                      void* d_v_held, void* stream)
+{
+    if (cache == nullptr) { set_error("cache is NULL"); return ARL2_ERR_INVALID_ARG; }
+    const arl2_config& cfg = cache->ctx->cfg;
+    if (!d_k || !d_v || !d_start) { set_error("cache_append: k, v and start must not be NULL"); return ARL2_ERR_INVALID_ARG; }
+    if (tokens < 1) { set_error("cache_append: tokens must be >= 1 (got %d)", tokens); return ARL2_ERR_INVALID_ARG; }
+    const int heads = cache->cfg.kv_heads, elem = cfg.io_dtype == ARL2_FP32 ? 4 : 2;
+    if (!check_strides("cache_append: k", k_batch_stride, k_token_stride, heads, cfg.D) ||
+        !check_strides("cache_append: v", v_batch_stride, v_token_stride, heads, cfg.D))
+        return ARL2_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(d_k) | reinterpret_cast<uintptr_t>(d_v) | reinterpret_cast<uintptr_t>(d_k_held) |
+         reinterpret_cast<uintptr_t>(d_v_held)) % elem != 0 || reinterpret_cast<uintptr_t>(d_start) % 4 != 0) {
+        set_error("cache_append: tensors must be aligned to their elements");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (d_k_held == d_k || d_v_held == d_v || d_k_held == d_v || d_v_held == d_k || (d_k_held != nullptr && d_k_held == d_v_held)) {
+        set_error("cache_append: the held values must not alias an input or each other");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    CacheAppendArgs a;
+    a.c = cache->view;
+    a.B = cfg.B; a.D = cfg.D; a.tokens = tokens;
+    a.k = d_k; a.v = d_v;
+    a.k_batch = k_batch_stride; a.k_token = k_token_stride;
+    a.v_batch = v_batch_stride; a.v_token = v_token_stride;
+    a.start = d_start;
+    a.k_held = d_k_held; a.v_held = d_v_held;
+    a.wide = rows_are_wide(d_k, k_batch_stride, k_token_stride, elem) && rows_are_wide(d_v, v_batch_stride, v_token_stride, elem) &&
+             rows_are_wide(d_k_held, 0, 0, 1) && rows_are_wide(d_v_held, 0, 0, 1);
+    return account(cache->ctx, cache_append(a, cfg.io_dtype, as_stream(stream)));
+}
+
+int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride, int64_t q_token_stride, int32_t queries,
+                      const int32_t* d_lengths, const int32_t* d_q_start, uint32_t flags, void* d_out, void* stream)
+{
+    if (cache == nullptr) { set_error("cache is NULL"); return ARL2_ERR_INVALID_ARG; }
+    const arl2_config& cfg = cache->ctx->cfg;
+    if (!d_q || !d_lengths || !d_out) { set_error("cache_attend: q, lengths and out must not be NULL"); return ARL2_ERR_INVALID_ARG; }
+    if (d_out == d_q) { set_error("cache_attend: out must not alias q"); return ARL2_ERR_INVALID_ARG; }
+    if (queries < 1 || (int64_t)queries * (cfg.H / cache->cfg.kv_heads) > ((int64_t)1 << 30)) {
+        set_error("cache_attend: queries must be >= 1, and at most 2^30 rows per key head (got %d)", queries);
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if ((flags & ~ARL2_CACHE_CAUSAL) != 0) { set_error("cache_attend: unknown flags 0x%x", flags); return ARL2_ERR_INVALID_ARG; }
+    if (!check_strides("cache_attend: q", q_batch_stride, q_token_stride, cfg.H, cfg.D)) return ARL2_ERR_INVALID_ARG;
+    const int elem = cfg.io_dtype == ARL2_FP32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out)) % elem != 0 ||
+        (reinterpret_cast<uintptr_t>(d_lengths) | reinterpret_cast<uintptr_t>(d_q_start)) % 4 != 0) {
+        set_error("cache_attend: tensors must be aligned to their elements");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    CacheAttendArgs a;
+    a.c = cache->view;
+    a.s_B = cfg.B; a.H = cfg.H; a.D = cfg.D; a.queries = queries;
+    a.rep = cfg.H / cache->cfg.kv_heads;
+    a.row_blocks = a.min_share = 0;
+    a.q = d_q;
+    a.q_batch = q_batch_stride; a.q_token = q_token_stride;
+    a.lengths = d_lengths; a.q_start = d_q_start;
+    a.causal = (flags & ARL2_CACHE_CAUSAL) ? 1 : 0;
+    a.scale_log2 = cache->ctx->shape.scale_log2;
+    a.out = d_out;
+    a.part_o = cache->part_o; a.part_ml = cache->part_ml; a.tickets = cache->tickets;
+    a.wide = rows_are_wide(d_q, q_batch_stride, q_token_stride, elem) && rows_are_wide(d_out, 0, 0, 1);
+    a.wait_limit = cache->ctx->wait_limit;
+    return account(cache->ctx, cache_attend(a, cfg.io_dtype, as_stream(stream)));
+}
+
+void arl2_cache_destroy(arl2_cache* cache) { delete cache; }
 
 uint64_t arl2_launch_count(const arl2_ctx* ctx) { return ctx ? ctx->launches : 0; }
 

@@ -1,0 +1,859 @@
+// The paged 4-bit key/value cache: appending rows, and attention by warp-level matrix instructions.
+//
+// Append.  Each lane holds 8 channels of a row (16 lanes a row of 128), rotates them, finds minimum and maximum of its group of
+// 64 channels with its 7 neighbours, and writes one word of 8 codes.  Bound by HBM: 4 D bytes (bf16) are read per token and head and
+// 9/8 D written.  A row group takes several heads of one token, so that the token's row of the rotary tables is fetched once for
+// them and their loads are in flight together.
+//
+// Attention (one query per stream up to a few dozen rows; any number in fp32 and with D = 64).  Keys are the M side of the
+// matrix instruction and query rows the N side, so that 8 rows fill it:  S^T = K Q^T, then  O^T = V^T P^T.  Codes go into the
+// instruction as they are: four bits of a word, masked out where they stand, are the fp16 denormal code * 2^-24 (bits 0-3 of a
+// half) or code * 2^-20 (bits 4-7), both exact.  With minimum lo and step st per key and group g of channels,
+//   s_j = sum_g  st_jg (sum_c q_c code_jc) + lo_jg (sum_c q_c),        o_c = sum_j (p_j st_jg) code_jc + sum_j p_j lo_jg,
+// so a key costs a few fp32 operations per group and its 256 values cost one AND each pair, and nothing of a value is rounded.
+// Rows of q are scaled by a power of two into fp16's range (1024 <= max < 2048), p st by a power of two per group, which
+// grows like the softmax's reference maximum.  fp32 I/O: q and p st as two fp16 numbers each, twice the instructions, and codes
+// less 8 as whole numbers (an addition per pair): with unsigned ones the sums of 64 products, from which the minimum's part is
+// subtracted, lost five bits (errors of 3e-6 to 9e-6 of the output, now 1e-7).
+#include <cuda_bf16.h>
+
+#include <atomic>
+
+#include "cache_common.cuh"
+
+namespace arl2 {
+namespace {
+
+constexpr int kMaxDevices = 64;
+constexpr float kHoldLimit = 61440.0f;     // minimum + 15 steps stays finite in fp16
+
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float d;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// ------------------------------------------------------------------------------------------------ append
+// 8 consecutive values of a row; `wide`: they start on a 16-byte boundary
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool wide, float (&x)[8])
+{
+    if (wide) {
+        const uint4 r = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, bool wide, float (&x)[8])
+{
+    if (wide) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, bool wide, const float (&x)[8])
+{
+    if (wide) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
+    }
+}
+__device__ __forceinline__ void store8(float* p, bool wide, const float (&x)[8])
+{
+    if (wide) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = x[i];
+    }
+}
+
+// 8 of a group's 64 channels -> one word of codes and the group's (minimum, step); x becomes what these stand for.  Every
+// operation is a single fp32 one, so that the codes are those of the formula whoever evaluates it.
+__device__ __forceinline__ void hold8(float (&x)[8], uint32_t& codes, uint32_t& params)
+{
+    float lo = kHoldLimit, hi = -kHoldLimit;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = max_nan(min_nan(x[i], kHoldLimit), -kHoldLimit);
+        lo = min_nan(lo, x[i]);
+        hi = max_nan(hi, x[i]);
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+    }
+    const __half step_h = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), lo_h = __float2half_rn(lo);
+    const float step = __half2float(step_h), base = __half2float(lo_h);
+    const float inverse = step > 0.0f ? __frcp_rn(step) : 0.0f;
+    codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float code = fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], base), inverse)), 0.0f), 15.0f);   // (NaN: 0)
+        codes |= (uint32_t)code << (4 * i);
+        x[i] = fmaf(step, code, base);
+    }
+    params = (uint32_t)__half_as_ushort(lo_h) | ((uint32_t)__half_as_ushort(step_h) << 16);
+}
+
+constexpr int kAppendThreads = 256;
+
+// kHeads heads of one token per row group
+template <int D, typename IO, int kHeads>
+__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const CacheAppendArgs p)
+{
+    using U = Unit<D>;
+    constexpr int kLanes = D / 8;
+    grid_dependency_sync();
+    const int head_blocks = (p.c.kv_heads + kHeads - 1) / kHeads;
+    const long long group = ((long long)blockIdx.x * kAppendThreads + threadIdx.x) / kLanes;
+    const int lr = threadIdx.x % kLanes;
+    const long long rows = (long long)p.B * p.tokens;
+    long long row = group / head_blocks;
+    const int h0 = (int)(group - row * head_blocks) * kHeads;
+    const bool there = row < rows;       // (the lanes of a warp stay together: they shuffle)
+    if (!there) row = rows - 1;
+    const int b = (int)(row / p.tokens), i = (int)(row - (long long)b * p.tokens);
+
+    const int begin = p.start[b];
+    const long long pos = (long long)begin + i;
+    // what cannot be stored is left out, and recorded by one lane
+    bool stored = there && begin >= 0;
+    CacheRange wrong = kRangeNone;
+    int page = 0;
+    if (stored) {
+        if ((pos >> p.c.page_shift) >= p.c.max_pages) wrong = kRangeLength;
+        else {
+            page = p.c.table[(long long)b * p.c.max_pages + (pos >> p.c.page_shift)];
+            if (page < 0 || page >= p.c.num_pages) wrong = kRangePage;
+            else if (p.c.rope_cos != nullptr && pos >= p.c.rope_rows) wrong = kRangePosition;
+        }
+        if (wrong != kRangeNone) {
+            stored = false;
+            if (lr == 0 && h0 == 0) range_error(p.c.status, wrong, b);
+        }
+    }
+    const bool rotate = stored && p.c.rope_cos != nullptr;
+    float cs[4] = {1.0f, 1.0f, 1.0f, 1.0f}, sn[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (rotate) {
+        const float4 c4 = *reinterpret_cast<const float4*>(p.c.rope_cos + pos * (D / 2) + lr * 4);
+        const float4 s4 = *reinterpret_cast<const float4*>(p.c.rope_sin + pos * (D / 2) + lr * 4);
+        cs[0] = c4.x; cs[1] = c4.y; cs[2] = c4.z; cs[3] = c4.w;
+        sn[0] = s4.x; sn[1] = s4.y; sn[2] = s4.z; sn[3] = s4.w;
+    }
+    const IO* k = static_cast<const IO*>(p.k) + b * p.k_batch + i * p.k_token + lr * 8;
+    const IO* v = static_cast<const IO*>(p.v) + b * p.v_batch + i * p.v_token + lr * 8;
+    float x[2][kHeads][8];
+#pragma unroll
+    for (int n = 0; n < kHeads; ++n) {
+        const int h = min(h0 + n, p.c.kv_heads - 1);
+        load8(k + (size_t)h * D, p.wide, x[0][n]);
+        load8(v + (size_t)h * D, p.wide, x[1][n]);
+    }
+    const int slot = (int)(pos & ((1 << p.c.page_shift) - 1)), page_tokens = 1 << p.c.page_shift;
+    uint8_t* unit = p.c.pages + ((size_t)page * p.c.kv_heads + h0) * p.c.unit_bytes;
+#pragma unroll
+    for (int n = 0; n < kHeads; ++n) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (t == 0 && rotate) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const float a = x[0][n][2 * m], c = x[0][n][2 * m + 1];
+                    x[0][n][2 * m] = __fsub_rn(__fmul_rn(a, cs[m]), __fmul_rn(c, sn[m]));
+                    x[0][n][2 * m + 1] = __fadd_rn(__fmul_rn(a, sn[m]), __fmul_rn(c, cs[m]));
+                }
+            }
+            uint32_t codes, params;
+            hold8(x[t][n], codes, params);
+            const bool mine = h0 + n < p.c.kv_heads;
+            if (stored && mine) {
+                uint8_t* at = unit + n * p.c.unit_bytes;
+                *reinterpret_cast<uint32_t*>(at + (t ? U::v_codes(page_tokens) : 0) + slot * U::kRow + lr * 4) = codes;
+                if ((lr & 7) == 0)
+                    *reinterpret_cast<uint32_t*>(at + (t ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + (lr >> 3) * 4) = params;
+            }
+            void* held = t ? p.v_held : p.k_held;
+            if (held != nullptr && there && mine) {
+                if (!stored) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[t][n][e] = 0.0f;
+                }
+                store8(static_cast<IO*>(held) + ((size_t)row * p.c.kv_heads + h0 + n) * D + lr * 8, p.wide, x[t][n]);
+            }
+        }
+    }
+}
+
+// --------------------------------------------------------------------------------------------- attention
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kKeys = 16;                  // keys of a matrix instruction, a warp's step
+constexpr int kChunk = kWarps * kKeys;     // keys of a CTA's step
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+// codes i and i + 4 of a word as a pair of fp16 denormals: code * 2^-24 for even i, code * 2^-20 for odd i
+__device__ __forceinline__ uint32_t code_pair(uint32_t word, int i)
+{
+    return ((i & 2) ? word >> 8 : word) & ((i & 1) ? 0x00F000F0u : 0x000F000Fu);
+}
+// the same codes less 8, as whole numbers: the products of signed codes nearly cancel instead of summing to 7.5 times the sum
+// of the other operand, of which the instruction's sums (which are cut off, not rounded) then lose bits
+__device__ __forceinline__ uint32_t signed_pair(uint32_t word, int i)
+{
+    const uint32_t x = code_pair(word, i) | ((i & 1) ? 0x54005400u : 0x64006400u);     // 64 + code, 1024 + code
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&x), (i & 1) ? __half2half2(__ushort_as_half(0x5480)) : __half2half2(__ushort_as_half(0x6408)));
+    return *reinterpret_cast<const uint32_t*>(&d);
+}
+template <bool kSigned>
+__device__ __forceinline__ uint32_t operand_pair(uint32_t word, int i) { return kSigned ? signed_pair(word, i) : code_pair(word, i); }
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// (cached rows are read once, by one SM)
+__device__ __forceinline__ uint32_t load_once(const uint32_t* p)
+{
+    uint32_t v;
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 load_once(const uint2* p)
+{
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+
+// What a lane reads of 16 keys.  Keys: channels [16 tig, 16 tig + 16) of each group of keys gid and gid + 8 (gid = lane / 4,
+// tig = lane % 4); values: channels [8 gid, 8 gid + 8) of each group of tokens 2 tig, 2 tig + 1, 2 tig + 8 and 2 tig + 9;
+// parameters of keys gid and gid + 8.
+template <int G>
+struct Raw {
+    uint2 k[2][G];
+    uint32_t v[4][G];
+    uint32_t kp[2][G], vp[2][G];
+};
+template <int D>
+__device__ __forceinline__ void load_raw(Raw<D / 64>& r, const uint8_t* unit, int page_tokens, int slot, int gid, int tig)
+{
+    using U = Unit<D>;
+    constexpr int G = U::kGroups;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int at = slot + gid + 8 * e;
+#pragma unroll
+        for (int g = 0; g < G; ++g) r.k[e][g] = load_once(reinterpret_cast<const uint2*>(unit + at * U::kRow + g * 32 + tig * 8));
+        const uint8_t* kp = unit + U::k_par(page_tokens) + at * U::kPar;
+        const uint8_t* vp = unit + U::v_par(page_tokens) + at * U::kPar;
+        if constexpr (G == 2) {
+            const uint2 a = load_once(reinterpret_cast<const uint2*>(kp)), b = load_once(reinterpret_cast<const uint2*>(vp));
+            r.kp[e][0] = a.x; r.kp[e][1] = a.y;
+            r.vp[e][0] = b.x; r.vp[e][1] = b.y;
+        } else {
+            r.kp[e][0] = load_once(reinterpret_cast<const uint32_t*>(kp));
+            r.vp[e][0] = load_once(reinterpret_cast<const uint32_t*>(vp));
+        }
+    }
+    const uint8_t* vc = unit + U::v_codes(page_tokens);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int at = slot + 2 * tig + (e & 1) + 8 * (e >> 1);
+#pragma unroll
+        for (int g = 0; g < G; ++g) r.v[e][g] = load_once(reinterpret_cast<const uint32_t*>(vc + at * U::kRow + g * 32 + gid * 4));
+    }
+}
+
+// kRows query rows of one key head; kSplit: operands as two fp16 numbers (fp32 I/O)
+template <int D, int kTiles, bool kSplit>
+struct RowsConfig {
+    static constexpr int G = D / kCacheGroup;
+    static constexpr int kRows = 8 * kTiles;
+    static constexpr int kParts = kSplit ? 2 : 1;
+    static constexpr int kLd = D + 1;
+    // shared memory: the query operand, then (over it) the warps' rows; per row its factor, its sums per group, the keys it sees
+    static constexpr int kQBytes = kParts * kRows * D * 2;
+    static constexpr int kMergeBytes = kWarps * kRows * (kLd + 2) * 4;
+    static constexpr int kInfo = (kQBytes > kMergeBytes ? kQBytes : kMergeBytes);
+    static constexpr int kBytes = kInfo + kRows * (1 + G + 1) * 4 + 128;
+};
+
+template <int D, typename IO, int kTiles>
+__global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAttendArgs p)
+{
+    constexpr bool kSplit = sizeof(IO) == 4;
+    using C = RowsConfig<D, kTiles, kSplit>;
+    using U = Unit<D>;
+    constexpr int G = C::G, kRows = C::kRows, kParts = C::kParts;
+    // slack of the reference maximum (log2 units) and the place of p * step in fp16's range: at most 2^14
+    constexpr float kSlack = kSplit ? 0.0f : 8.0f;
+    constexpr float kPlace = kSplit ? 16384.0f : 64.0f;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __half* q_frag = reinterpret_cast<__half*>(smem);          // [part][tile][group][k-step][lane][4]
+    float* merge_o = reinterpret_cast<float*>(smem);           // [warp][row][kLd]
+    float* merge_ml = merge_o + kWarps * kRows * C::kLd;       // [warp][row][2]
+    float* row_scale = reinterpret_cast<float*>(smem + C::kInfo);   // [row]
+    float* row_sum = row_scale + kRows;                        // [row][group]
+    int* row_seen = reinterpret_cast<int*>(row_sum + kRows * G);    // [row]
+    __shared__ long long scratch[kWarps + 8];
+    __shared__ int last_part;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+    const int page_tokens = 1 << p.c.page_shift;
+    grid_dependency_sync();
+    const Cut cut = cut_work<kRows, kChunk, kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
+    int b = cut.b, rb = cut.rb, h = cut.h;
+    long long item_begin = cut.item_begin;
+
+    for (long long at = cut.begin; at < cut.end;) {
+        const int have = stream_tokens(p, b, rb == 0 && h == 0 && at == item_begin);
+        const int first = first_position(p, b, have);
+        const int seen = keys_seen(p, have, first, (rb + 1) * kRows);
+        const int chunks = max(1, (seen + kChunk - 1) / kChunk);
+        const int c0 = (int)(at - item_begin);
+        const int c1 = (int)min((long long)chunks, c0 + (cut.end - at));
+        const int rows = min(kRows, p.queries * p.rep - rb * kRows);
+
+        // ---- the query rows: rotated, scaled into fp16's range, laid out as the instruction's second operand
+        __syncthreads();
+        for (int r = warp; r < kRows; r += kWarps) {
+            constexpr int kPer = D / 32;       // channels of a lane
+            float x[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
+            int sees = 0;
+            if (r < rows) {
+                const int flat = rb * kRows + r, i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
+                const IO* src = static_cast<const IO*>(p.q) + b * p.q_batch + i * p.q_token + (size_t)head * D + lane * kPer;
+                const long long pos = (long long)first + i;
+                sees = p.causal ? (int)max(0LL, min((long long)have, pos + 1)) : have;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) x[e] = static_cast<float>(src[e]);
+                if (p.c.rope_cos != nullptr) {
+                    long long t = max(pos, 0LL);
+                    if (t >= p.c.rope_rows) {
+                        if (lane == 0 && at == item_begin) range_error(p.c.status, kRangePosition, b);
+                        t = p.c.rope_rows - 1;
+                    }
+#pragma unroll
+                    for (int m = 0; m < kPer / 2; ++m) {
+                        const float cs = p.c.rope_cos[t * (D / 2) + lane * (kPer / 2) + m], sn = p.c.rope_sin[t * (D / 2) + lane * (kPer / 2) + m];
+                        const float u = x[2 * m], w = x[2 * m + 1];
+                        x[2 * m] = u * cs - w * sn;
+                        x[2 * m + 1] = u * sn + w * cs;
+                    }
+                }
+            }
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) most = max_nan(most, fabsf(x[e]));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
+            // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
+            const bool finite = most <= 3.402823466e38f;
+            int e2 = 0;
+            if (most > 0.0f && finite) e2 = min(10 - ilogbf(most), 126);
+            const float up = scalbnf(1.0f, e2 >> 1), up2 = scalbnf(1.0f, e2 - (e2 >> 1));
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                x[e] = finite ? x[e] * up * up2 : 0.0f;
+                sum += x[e];
+            }
+            // sums over a group's lanes
+#pragma unroll
+            for (int d = 1; d < 32 / G; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (lane == 0) {
+                row_scale[r] = finite ? p.scale_log2 / up / up2 : __int_as_float(0x7fc00000);
+                row_seen[r] = sees;
+            }
+            if ((lane % (32 / G)) == 0) row_sum[r * G + lane / (32 / G)] = sum;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                // channel c of its group: lane quarter c / 16, word (c / 8) % 2, code c % 8 of the word
+                const int c = lane * kPer + e, cg = c & 63, g = c >> 6;
+                const int quarter = cg >> 4, word = (cg >> 3) & 1, i = cg & 3, upper = (cg >> 2) & 1;
+                const int step = 2 * word + (i >> 1), reg = i & 1;
+                const float y = reg && !kSplit ? x[e] * 0.0625f : x[e];      // (odd codes are 2^4 larger)
+                const __half hi = __float2half_rn(y);
+                const size_t to = (((((size_t)(r >> 3)) * G + g) * 4 + step) * 32 + (r & 7) * 4 + quarter) * 4 + reg * 2 + upper;
+                q_frag[to] = hi;
+                if constexpr (kSplit) q_frag[(size_t)kTiles * G * 4 * 32 * 4 + to] = __float2half_rn(y - __half2float(hi));
+            }
+        }
+        __syncthreads();
+
+        auto q_operand = [&](int part, int t, int g, int s) {
+            return *reinterpret_cast<const uint2*>(q_frag + ((((size_t)(part * kTiles + t) * G + g) * 4 + s) * 32 + lane) * 4);
+        };
+        // few rows: kept in registers
+        constexpr bool kKeep = kTiles * kParts == 1;
+        uint2 kept[kKeep ? G : 1][4];
+        if constexpr (kKeep) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) kept[g][s] = q_operand(0, 0, g, s);
+        }
+        // this lane's query rows: 8 t + 2 tig + e
+        float scale[kTiles][2], sums[kTiles][2][G];
+        int sees[kTiles][2];
+        int fewest = have;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * t + 2 * tig + e;
+                scale[t][e] = row_scale[r];
+                sees[t][e] = row_seen[r];
+#pragma unroll
+                for (int g = 0; g < G; ++g) sums[t][e][g] = row_sum[r * G + g];
+            }
+        for (int r = 0; r < rows; ++r) fewest = min(fewest, row_seen[r]);
+
+        float o[G][4][kTiles][4];     // [group][channel tile][row tile]
+        float m_ref[kTiles][2], l[kTiles][2], lows[kTiles][2][G];
+        float v_top[G];               // a power of two that no step so far exceeds
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            v_top[g] = 0.0f;
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[g][m][t][e] = 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                m_ref[t][e] = -INFINITY;
+                l[t][e] = 0.0f;
+#pragma unroll
+                for (int g = 0; g < G; ++g) lows[t][e][g] = 0.0f;
+            }
+
+        // Key tiles of this warp: chunk * kWarps + warp.  A lane holds the page of one of the next 32 of them; -1: none, or
+        // one that the pool does not have.
+        const int32_t* table = p.c.table + (size_t)b * p.c.max_pages;
+        auto page_of = [&](int c) {
+            const int key = (c * kWarps + warp) * kKeys;
+            if (c >= c1 || key >= seen) return -1;
+            const int page = table[key >> p.c.page_shift];
+            if (page >= 0 && page < p.c.num_pages) return page;
+            range_error(p.c.status, kRangePage, b);
+            return -1;
+        };
+        int pages_from = c0, my_page = page_of(c0 + lane);
+        auto fetch = [&](int c, Raw<G>& raw) {      // whether there is anything to do for this warp in chunk c
+            if (c - pages_from == 32) {
+                pages_from = c;
+                my_page = page_of(c + lane);
+            }
+            const int page = __shfl_sync(0xffffffffu, my_page, c - pages_from);
+            if (page < 0) return false;
+            const int key = (c * kWarps + warp) * kKeys;
+            load_raw<D>(raw, p.c.pages + ((size_t)page * p.c.kv_heads + h) * p.c.unit_bytes, page_tokens, key & (page_tokens - 1), gid, tig);
+            return true;
+        };
+
+        Raw<G> next;
+        bool have_next = fetch(c0, next);
+#pragma unroll 1
+        for (int c = c0; c < c1; ++c) {
+            const Raw<G> cur = next;
+            const bool todo = have_next;
+            have_next = c + 1 < c1 ? fetch(c + 1, next) : false;
+            if (!todo) continue;
+            const int key0 = (c * kWarps + warp) * kKeys;
+
+            // ---- sums of q * code per group
+            float acc[G][kTiles][4], rest[kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[g][t][e] = rest[kSplit ? g : 0][t][e] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const uint32_t w0 = (s & 2) ? cur.k[0][g].y : cur.k[0][g].x, w1 = (s & 2) ? cur.k[1][g].y : cur.k[1][g].x;
+                    const int i = 2 * (s & 1);
+                    const uint32_t a[4] = {operand_pair<kSplit>(w0, i), operand_pair<kSplit>(w1, i), operand_pair<kSplit>(w0, i + 1), operand_pair<kSplit>(w1, i + 1)};
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+                        for (int part = 0; part < kParts; ++part) {
+                            uint2 q;
+                            if constexpr (kKeep) q = kept[g][s];
+                            else q = q_operand(part, t, g, s);
+                            mma16816(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                        }
+                    }
+                }
+            }
+            // ---- scores in log2 units: keys gid (x[t][0 .. 1]) and gid + 8 (x[t][2 .. 3])
+            float kl[2][G], ks[2][G], vl[2][G], vs[2][G];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const float2 a = unpack_half(cur.kp[e][g]), v = unpack_half(cur.vp[e][g]);
+                    kl[e][g] = kSplit ? fmaf(8.0f, a.y, a.x) : a.x;
+                    ks[e][g] = kSplit ? a.y : a.y * 16777216.0f;
+                    vl[e][g] = kSplit ? fmaf(8.0f, v.y, v.x) : v.x;
+                    vs[e][g] = v.y;
+                }
+            float x[kTiles][4];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float s = 0.0f;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) s = fmaf(kSplit ? acc[g][t][e] + rest[kSplit ? g : 0][t][e] : acc[g][t][e], ks[e >> 1][g], fmaf(kl[e >> 1][g], sums[t][e & 1][g], s));
+                    x[t][e] = s * scale[t][e & 1];
+                }
+            const bool edge = key0 + kKeys > fewest;     // some row does not see some of these keys
+            if (edge) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int key = key0 + gid + 8 * e;
+                    if (key >= have) {                   // nothing is there: whatever the memory holds stays out of the sums
+#pragma unroll
+                        for (int g = 0; g < G; ++g) vl[e][g] = vs[e][g] = 0.0f;
+                    }
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int f = 0; f < 2; ++f)
+                            if (key >= sees[t][f]) x[t][2 * e + f] = -INFINITY;
+                }
+            }
+            // ---- reference maximum and the values' scale: renewed only where they have to be
+            bool renew = false;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) renew |= x[t][e] > m_ref[t][e & 1] + kSlack;
+#pragma unroll
+            for (int g = 0; g < G; ++g) renew |= vs[0][g] > v_top[g] || vs[1][g] > v_top[g];
+            if (__any_sync(0xffffffffu, renew)) {
+                float down[kTiles][2];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        float mx = fmaxf(x[t][f], x[t][2 + f]);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                        const float m_new = fmaxf(m_ref[t][f], mx);
+                        down[t][f] = m_new == m_ref[t][f] ? 1.0f : exp2_fast(m_ref[t][f] - m_new);
+                        m_ref[t][f] = m_new;
+                        l[t][f] *= down[t][f];
+#pragma unroll
+                        for (int g = 0; g < G; ++g) lows[t][f][g] *= down[t][f];
+                    }
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    float top = fmaxf(vs[0][g], vs[1][g]);
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    float shrink = 1.0f;
+                    if (top > v_top[g]) {   // the next power of two: the exponent field of twice the step
+                        const float up = __uint_as_float((__float_as_uint(2.0f * top)) & 0x7f800000u);
+                        shrink = v_top[g] / up;
+                        v_top[g] = up;
+                    }
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[g][m][t][e] *= down[t][e & 1] * shrink;
+                }
+            }
+            // ---- p, and p * step per group as the instruction's second operand
+            float scaled[2][G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const float f = v_top[g] > 0.0f ? kPlace / v_top[g] : 1.0f;
+                scaled[0][g] = vs[0][g] * f;
+                scaled[1][g] = vs[1][g] * f;
+            }
+            uint32_t pb[kParts][kTiles][G][2];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                float pr[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float m = m_ref[t][e & 1] == -INFINITY ? 0.0f : m_ref[t][e & 1];
+                    pr[e] = exp2_fast(x[t][e] - m);
+                    l[t][e & 1] += pr[e];
+                }
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float y0 = pr[2 * e] * scaled[e][g], y1 = pr[2 * e + 1] * scaled[e][g];
+                        float a0 = pr[2 * e] * vl[e][g], a1 = pr[2 * e + 1] * vl[e][g];
+                        if (edge) {      // a NaN or an infinity that a row does not see is not to reach it as 0 * NaN
+                            if (x[t][2 * e] == -INFINITY) y0 = a0 = 0.0f;
+                            if (x[t][2 * e + 1] == -INFINITY) y1 = a1 = 0.0f;
+                        }
+                        lows[t][0][g] += a0;
+                        lows[t][1][g] += a1;
+                        const uint32_t hi = pack_half(y0, y1);
+                        pb[0][t][g][e] = transpose8x8(hi);
+                        if constexpr (kSplit) {
+                            const float2 back = unpack_half(hi);
+                            pb[1][t][g][e] = transpose8x8(pack_half(y0 - back.x, y1 - back.y));
+                        }
+                    }
+            }
+            // ---- O^T += V^T P^T, 16 channels at a time: rows gid and gid + 8 are channels 8 gid + m and 8 gid + 4 + m of the group
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const uint32_t a_lo = __byte_perm(cur.v[0][g], cur.v[1][g], 0x5410), a_hi = __byte_perm(cur.v[0][g], cur.v[1][g], 0x7632);
+                const uint32_t b_lo = __byte_perm(cur.v[2][g], cur.v[3][g], 0x5410), b_hi = __byte_perm(cur.v[2][g], cur.v[3][g], 0x7632);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const uint32_t a[4] = {operand_pair<kSplit>(a_lo, m), operand_pair<kSplit>(a_hi, m), operand_pair<kSplit>(b_lo, m), operand_pair<kSplit>(b_hi, m)};
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        if constexpr (kSplit) {     // added up by fp32 additions, which round
+                            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                            mma16816(sum, a, pb[kParts - 1][t][g][0], pb[kParts - 1][t][g][1]);
+                            mma16816(sum, a, pb[0][t][g][0], pb[0][t][g][1]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[g][m][t][e] += sum[e];
+                        } else {
+                            mma16816(o[g][m][t], a, pb[0][t][g][0], pb[0][t][g][1]);
+                        }
+                    }
+                }
+            }
+        }
+
+        // ---- the warps' rows meet in shared memory
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    l[t][f] += __shfl_xor_sync(0xffffffffu, l[t][f], d);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) lows[t][f][g] += __shfl_xor_sync(0xffffffffu, lows[t][f][g], d);
+                }
+        __syncthreads();       // (the query operand has been read)
+        {
+            float* mine = merge_o + warp * kRows * C::kLd;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const float back = v_top[g] * ((kSplit ? 1.0f : 16777216.0f) / kPlace);
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int r = 8 * t + 2 * tig + (e & 1), ch = g * 64 + gid * 8 + m + (e >> 1) * 4;
+                            mine[r * C::kLd + ch] = fmaf(o[g][m][t][e], (m & 1) && !kSplit ? back * 0.0625f : back, lows[t][e & 1][g]);
+                        }
+            }
+            if (gid == 0) {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const int r = 8 * t + 2 * tig + f;
+                        merge_ml[(warp * kRows + r) * 2] = m_ref[t][f];
+                        merge_ml[(warp * kRows + r) * 2 + 1] = l[t][f];
+                    }
+            }
+        }
+        __syncthreads();
+        const Parts parts = item_parts(cut, item_begin, chunks);
+        auto write_row = [&](int r, int ch, float value) {
+            const int flat = rb * kRows + r, i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
+            static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + head) * D + ch] = static_cast<IO>(value);
+        };
+        const int slot = parts.slot((int)blockIdx.x);
+        for (int x = tid; x < rows * D; x += kThreads) {
+            const int r = x / D, ch = x - r * D;
+            float m = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) m = fmaxf(m, merge_ml[(w * kRows + r) * 2]);
+            const float m_use = m == -INFINITY ? 0.0f : m;
+            float sum = 0.0f, total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = exp2_fast(merge_ml[(w * kRows + r) * 2] - m_use);
+                sum = fmaf(merge_o[(w * kRows + r) * C::kLd + ch], f, sum);
+                total = fmaf(merge_ml[(w * kRows + r) * 2 + 1], f, total);
+            }
+            if (parts.count == 1) write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
+            else {
+                p.part_o[((size_t)slot * kRows + r) * D + ch] = sum;
+                if (ch == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)slot * kRows + r) * 2) = make_float2(m, total);
+            }
+        }
+        if (parts.count > 1) {
+            // whoever is the last of the item's CTAs joins their rows, in the order of the CTAs
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                __threadfence();
+                last_part = atomicAdd(p.tickets + parts.first, 1u) == (uint32_t)parts.count - 1;
+            }
+            __syncthreads();
+            if (last_part) {
+                __threadfence();
+                if (tid == 0) p.tickets[parts.first] = 0;      // as it was found
+                for (int x = tid; x < rows * D; x += kThreads) {
+                    const int r = x / D, ch = x - r * D;
+                    float m = -INFINITY;
+                    for (int w = 0; w < parts.count; ++w) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)parts.slot(parts.first + w) * kRows + r) * 2));
+                    const float m_use = m == -INFINITY ? 0.0f : m;
+                    float sum = 0.0f, total = 0.0f;
+                    for (int w = 0; w < parts.count; ++w) {
+                        const size_t s = (size_t)parts.slot(parts.first + w) * kRows + r;
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + s * 2));
+                        const float f = exp2_fast(ml.x - m_use);
+                        sum = fmaf(__ldcg(p.part_o + s * D + ch), f, sum);
+                        total = fmaf(ml.y, f, total);
+                    }
+                    write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
+                }
+            }
+        }
+
+        at += c1 - c0;
+        item_begin += chunks;
+        if (++h == p.c.kv_heads) {
+            h = 0;
+            if (++rb == p.row_blocks) { rb = 0; ++b; }
+        }
+    }
+}
+
+template <int D, typename IO>
+int launch_append(const CacheAppendArgs& a, cudaStream_t st)
+{
+    constexpr int kLanes = D / 8;
+    const long long rows = (long long)a.B * a.tokens;
+    auto blocks = [&](int heads) { return (rows * ((a.c.kv_heads + heads - 1) / heads) * kLanes + kAppendThreads - 1) / kAppendThreads; };
+    // one head per row group while that does not fill the device
+    const bool few = blocks(4) < 148 * 2;
+    const long long grid = blocks(few ? 1 : 4);
+    if (grid > 0x7fffffffLL) { set_error("cache_append: too many rows"); return ARL2_ERR_UNSUPPORTED; }
+    const cudaError_t e = launch_kernel(few ? cache_append_kernel<D, IO, 1> : cache_append_kernel<D, IO, 4>, dim3((unsigned)grid), kAppendThreads, 0, st, a);
+    if (e != cudaSuccess) { set_error("launch of cache_append_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    return 1;
+}
+
+template <int D, typename IO, int kTiles>
+int launch_attend(CacheAttendArgs& a, cudaStream_t st)
+{
+    using C = RowsConfig<D, kTiles, sizeof(IO) == 4>;
+    auto kernel = cache_attend_kernel<D, IO, kTiles>;
+    // CTAs that the device holds at once, per device; found once (whoever finds it finds the same)
+    static std::atomic<int> resident[kMaxDevices];
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || dev < 0 || dev >= kMaxDevices) { set_error("cannot identify the current device (%s)", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    int ctas = resident[dev].load(std::memory_order_relaxed);
+    if (ctas == 0) {
+        int sms = 0, per_sm = 0;
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, C::kBytes);
+        if (e != cudaSuccess || sms * per_sm < 1) {
+            cudaGetLastError();
+            set_error("cache_attend: cannot set up the kernel: %s", cudaGetErrorString(e));
+            return ARL2_ERR_CUDA;
+        }
+        ctas = sms * per_sm;
+        resident[dev].store(ctas, std::memory_order_relaxed);
+    }
+    a.row_blocks = (a.queries * a.rep + C::kRows - 1) / C::kRows;
+    a.min_share = 2;
+    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * ((((long long)a.c.max_pages << a.c.page_shift) + kChunk - 1) / kChunk);
+    long long grid = ctas;
+    if (grid > kCacheCtas) grid = kCacheCtas;
+    if (grid > most) grid = most;
+    e = launch_kernel(kernel, dim3((unsigned)grid), kThreads, C::kBytes, st, a);
+    if (e != cudaSuccess) { set_error("launch of cache_attend_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    return 1;
+}
+
+template <int D>
+int attend_any(CacheAttendArgs& a, int dtype, cudaStream_t st)
+{
+    const int rows = a.queries * a.rep;
+    if (dtype == ARL2_FP32) return rows <= 8 ? launch_attend<D, float, 1>(a, st) : launch_attend<D, float, 2>(a, st);
+    return rows <= 8 ? launch_attend<D, __nv_bfloat16, 1>(a, st) : rows <= 16 ? launch_attend<D, __nv_bfloat16, 2>(a, st) : launch_attend<D, __nv_bfloat16, 4>(a, st);
+}
+
+}  // namespace
+
+int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
+{
+    if (a.D == 128) return dtype == ARL2_FP32 ? launch_append<128, float>(a, st) : launch_append<128, __nv_bfloat16>(a, st);
+    return dtype == ARL2_FP32 ? launch_append<64, float>(a, st) : launch_append<64, __nv_bfloat16>(a, st);
+}
+
+int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)
+{
+    return a.D == 128 ? attend_any<128>(a, dtype, st) : attend_any<64>(a, dtype, st);
+}
+
+}  // namespace arl2

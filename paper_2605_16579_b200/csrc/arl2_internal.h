@@ -15,8 +15,11 @@ enum StatusWord : int {
     kStatusError = 0,    // first error code a kernel recorded (0 = none)
     kStatusWhere = 1,    // which wait gave up (kernel-specific tag)
     kStatusSched = 2,    // two item counters of the persistent step kernel (words 2 and 3)
+    kStatusRange = 4,    // first CacheRange that a cache kernel met (0 = none); a word of its own: it stops no later kernel
+    kStatusRangeWhere = 5,   // ... and the stream it was met in
     kStatusWords = 64
 };
+enum CacheRange : int { kRangeNone = 0, kRangeLength = 1, kRangePage = 2, kRangePosition = 3 };
 
 constexpr int kCommitChunk = 512;  // tokens per partial sum of the commit reduction
 // Key-range split of the step kernel's last wave: at most kMaxSplit parts per item, and room for
@@ -183,6 +186,57 @@ struct GemmArgs {
     uint32_t wait_limit = 0;
 };
 int tc_gemm(const GemmArgs& a, cudaStream_t st);
+
+// ---- the paged 4-bit key/value cache (arl2_cache.cu, arl2_tc_cache.cu) ---------------------
+struct CacheView {
+    uint8_t* pages;
+    const int32_t* table;    // [B, max_pages]
+    int kv_heads, page_shift, num_pages, max_pages;   // pages of 1 << page_shift tokens
+    size_t unit_bytes;       // one head's part of a page
+    const float* rope_cos;   // [rope_rows, D/2] or nullptr
+    const float* rope_sin;
+    int rope_rows;
+    uint32_t* status;
+};
+struct CacheAppendArgs {
+    CacheView c;
+    int B, D, tokens;
+    const void* k;
+    const void* v;
+    int64_t k_batch, k_token, v_batch, v_token;   // strides in elements
+    const int32_t* start;
+    void* k_held;            // or nullptr
+    void* v_held;
+    bool wide;               // every row of the tensors starts on a 16-byte boundary
+};
+// Room for the partial rows of attention over a cache: two slots per CTA (item_parts), kCachePartRows rows each, and a ticket
+// per CTA; sized for a device of 148 SMs (with more, the launchers take fewer CTAs).
+constexpr int kCacheCtas = 4 * 148;        // most CTAs of the warp-level kernel, of at most 32 rows
+constexpr int kCacheTcCtas = 148;          // most CTAs of the tcgen05 kernel, of 256 rows
+constexpr int kCachePartRows = 2 * kCacheTcCtas * 256;
+static_assert(2 * kCacheCtas * 32 <= kCachePartRows, "the partial rows of both kernels have the same room");
+struct CacheAttendArgs {
+    CacheView c;
+    int s_B, H, D, queries;
+    int rep;                 // query heads that share a key head
+    int row_blocks;          // blocks of query rows per key head (set by the launcher)
+    int min_share;           // fewest key chunks that a CTA is given (set by the launcher)
+    const void* q;
+    int64_t q_batch, q_token;
+    const int32_t* lengths;
+    const int32_t* q_start;  // or nullptr
+    int causal;
+    float scale_log2;
+    void* out;
+    float* part_o;           // [kCachePartRows, D] unnormalised rows
+    float* part_ml;          // [kCachePartRows, 2] reference maximum (log2 units), row sum
+    uint32_t* tickets;       // [kCacheCtas], zero between calls
+    bool wide;               // as in CacheAppendArgs, for q and out
+    uint32_t wait_limit = 0; // as in StepArgs
+};
+int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st);
+// attention by warp-level matrix instructions: every shape and type
+int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st);
 
 void set_error(const char* fmt, ...);
 
