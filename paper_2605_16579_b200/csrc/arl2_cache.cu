@@ -341,24 +341,21 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
     float* row_scale = reinterpret_cast<float*>(smem + C::kInfo);   // [row]
     float* row_sum = row_scale + kRows;                        // [row][group]
     int* row_seen = reinterpret_cast<int*>(row_sum + kRows * G);    // [row]
-    __shared__ long long scratch[kWarps + 8];
+    __shared__ long long scratch[kWarps + 3];
     __shared__ int last_part;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const int page_tokens = 1 << p.c.page_shift;
     grid_dependency_sync();
     const Cut cut = cut_work<kRows, kChunk, kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
-    int b = cut.b, rb = cut.rb, h = cut.h;
-    long long item_begin = cut.item_begin;
+    if (cut.begin >= cut.end) return;
+    Walk<kRows, kChunk> walk{locate<kRows, kChunk, kThreads>(p, cut.begin, scratch), cut.begin, cut.end};
 
-    for (long long at = cut.begin; at < cut.end;) {
-        const int have = stream_tokens(p, b, rb == 0 && h == 0 && at == item_begin);
-        const int first = first_position(p, b, have);
-        const int seen = keys_seen(p, have, first, (rb + 1) * kRows);
-        const int chunks = max(1, (seen + kChunk - 1) / kChunk);
-        const int c0 = (int)(at - item_begin);
-        const int c1 = (int)min((long long)chunks, c0 + (cut.end - at));
-        const int rows = min(kRows, p.queries * p.rep - rb * kRows);
+    Segment seg;
+    while (walk.next(p, seg)) {
+        const int b = seg.at.b, rb = seg.at.rb, h = seg.at.h;
+        const int have = seg.have, first = seg.first, seen = seg.seen, rows = seg.rows, c0 = seg.c0, c1 = seg.c1;
+        if (tid == 0 && seg.opens) (void)stream_tokens(p, b, true);
 
         // ---- the query rows: rotated, scaled into fp16's range, laid out as the instruction's second operand
         __syncthreads();
@@ -378,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
                 if (p.c.rope_cos != nullptr) {
                     long long t = max(pos, 0LL);
                     if (t >= p.c.rope_rows) {
-                        if (lane == 0 && at == item_begin) range_error(p.c.status, kRangePosition, b);
+                        if (lane == 0) range_error(p.c.status, kRangePosition, b);
                         t = p.c.rope_rows - 1;
                     }
 #pragma unroll
@@ -721,7 +718,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
             }
         }
         __syncthreads();
-        const Parts parts = item_parts(cut, item_begin, chunks);
+        const Parts parts = item_parts(cut.share, seg.at.item_begin, seg.chunks);
         auto write_row = [&](int r, int ch, float value) {
             const int flat = rb * kRows + r, i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
             static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + head) * D + ch] = static_cast<IO>(value);
@@ -774,13 +771,6 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
                     write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
                 }
             }
-        }
-
-        at += c1 - c0;
-        item_begin += chunks;
-        if (++h == p.c.kv_heads) {
-            h = 0;
-            if (++rb == p.row_blocks) { rb = 0; ++b; }
         }
     }
 }
@@ -853,6 +843,7 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
 
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)
 {
+    if (a.D == 128 && dtype == ARL2_BF16 && a.queries * a.rep > 32) return tc_cache_attend(a, st);
     return a.D == 128 ? attend_any<128>(a, dtype, st) : attend_any<64>(a, dtype, st);
 }
 

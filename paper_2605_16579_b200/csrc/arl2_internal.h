@@ -237,6 +237,8 @@ struct CacheAttendArgs {
 int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st);
 // attention by warp-level matrix instructions: every shape and type
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st);
+// attention by tcgen05: bf16 I/O, D = 128, many rows
+int tc_cache_attend(CacheAttendArgs a, cudaStream_t st);
 
 void set_error(const char* fmt, ...);
 

@@ -29,11 +29,11 @@ struct Unit {
     __host__ __device__ static constexpr int v_par(int page_tokens) { return page_tokens * (2 * kRow + kPar); }
 };
 
-// Tokens of stream b that there are; a length past the table is recorded once per stream by the caller that says so.
+// Tokens of stream b that there are.  A length past the table is recorded by whoever says so.
 __device__ __forceinline__ int stream_tokens(const CacheAttendArgs& p, int b, bool report)
 {
     const int have = p.lengths[b], most = p.c.max_pages << p.c.page_shift;
-    if (have > most && report) range_error(p.c.status, kRangeLength, b);
+    if (report && have > most) range_error(p.c.status, kRangeLength, b);
     return max(0, min(have, most));
 }
 
@@ -56,11 +56,13 @@ __device__ __forceinline__ int keys_seen(const CacheAttendArgs& p, int have, int
 // Attention work is one sequence of key chunks: by stream, block of query rows, key head, and chunk.  Every CTA takes an equal
 // share of it, wherever that begins and ends; an item (one block of rows of one head) that more than one CTA works on is
 // joined from partial rows.  The cut follows from the lengths alone, so that results do not depend on timing.
+struct Place {
+    int b, rb, h;             // an item
+    long long item_begin;     // its first chunk in the sequence
+};
 struct Cut {
-    long long share;          // chunks per CTA
+    long long share, total;   // chunks per CTA, and of all
     long long begin, end;     // this CTA's
-    int b, rb, h;             // the item that holds `begin`
-    long long item_begin;     // where that item starts
 };
 
 // Chunks of (stream, block of rows); never none, so that rows without keys are written too.
@@ -73,34 +75,38 @@ __device__ __forceinline__ int unit_chunks(const CacheAttendArgs& p, int unit)
     return max(1, (seen + kChunk - 1) / kChunk);
 }
 
-// All threads of a CTA of kThreads; `scratch` holds kThreads / 32 + 8 words of 64 bits of shared memory.
+// The share of a CTA.  All threads of a CTA of kThreads; `scratch`: kThreads / 32 + 3 words of 64 bits of shared memory.
 template <int kRows, int kChunk, int kThreads>
 __device__ __forceinline__ Cut cut_work(const CacheAttendArgs& p, int cta, int ctas, long long* scratch)
 {
     constexpr int kWarps = kThreads / 32;
-    const int units = p.s_B * p.row_blocks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    long long* sums = scratch;
-    long long* found = scratch + kWarps;   // unit, its first chunk, chunks per head
-    // chunks of all units, and of those before each round of kThreads
+    const int units = p.s_B * p.row_blocks, tid = threadIdx.x;
     long long mine = 0;
     for (int u = tid; u < units; u += kThreads) mine += (long long)unit_chunks<kRows, kChunk>(p, u) * p.c.kv_heads;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-    if (lane == 0) sums[warp] = mine;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) total += sums[w];
+    if ((tid & 31) == 0) scratch[tid >> 5] = mine;
     __syncthreads();
     Cut c;
-    c.share = max((long long)p.min_share, (total + ctas - 1) / ctas);
-    c.begin = c.share * cta;
-    c.end = min(total, c.begin + c.share);
-    c.b = c.rb = c.h = 0;
-    c.item_begin = 0;
-    if (c.begin >= total) return c;
+    c.total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) c.total += scratch[w];
+    __syncthreads();
+    c.share = max((long long)p.min_share, (c.total + ctas - 1) / ctas);
+    c.begin = min(c.total, c.share * cta);
+    c.end = min(c.total, c.begin + c.share);
+    return c;
+}
+
+// The item that holds chunk `at` (below the total).  All threads, as above.
+template <int kRows, int kChunk, int kThreads>
+__device__ __forceinline__ Place locate(const CacheAttendArgs& p, long long at, long long* scratch)
+{
+    constexpr int kWarps = kThreads / 32;
+    const int units = p.s_B * p.row_blocks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    long long* found = scratch + kWarps;   // unit, its first chunk, chunks per head
     long long before = 0;
-    for (int u0 = 0; u0 < units; u0 += kThreads) {
+    for (int u0 = 0; u0 < units && before <= at; u0 += kThreads) {
         const int u = u0 + tid, each = u < units ? unit_chunks<kRows, kChunk>(p, u) : 0;
         const long long size = (long long)each * p.c.kv_heads;
         long long upto = size;
@@ -109,31 +115,69 @@ __device__ __forceinline__ Cut cut_work(const CacheAttendArgs& p, int cta, int c
             const long long x = __shfl_up_sync(0xffffffffu, upto, d);
             if (lane >= d) upto += x;
         }
-        if (lane == 31) sums[warp] = upto;
+        if (lane == 31) scratch[warp] = upto;
         __syncthreads();
         long long round = 0;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) upto += sums[w];
-            round += sums[w];
+            if (w < warp) upto += scratch[w];
+            round += scratch[w];
         }
-        const long long at = before + upto - size;
-        if (u < units && at <= c.begin && c.begin < at + size) {
+        const long long from = before + upto - size;
+        if (u < units && from <= at && at < from + size) {
             found[0] = u;
-            found[1] = at;
+            found[1] = from;
             found[2] = each;
         }
         before += round;
         __syncthreads();
-        if (c.begin < before) break;
     }
     const int u = (int)found[0];
-    c.b = u / p.row_blocks;
-    c.rb = u - c.b * p.row_blocks;
-    c.h = (int)((c.begin - found[1]) / found[2]);
-    c.item_begin = found[1] + (long long)c.h * found[2];
-    return c;
+    Place q;
+    q.b = u / p.row_blocks;
+    q.rb = u - q.b * p.row_blocks;
+    q.h = (int)((at - found[1]) / found[2]);
+    q.item_begin = found[1] + (long long)q.h * found[2];
+    return q;
 }
+
+// What a CTA does of one item: key chunks [c0, c1) of `chunks`.
+struct Segment {
+    Place at;
+    int have, first;          // tokens of the stream, position of its first query
+    int seen;                 // keys that some row of the item sees
+    int rows;                 // rows of the item that there are
+    int chunks, c0, c1;
+    bool opens;               // the item's first chunk is among them
+};
+// A CTA's segments one after the other.
+template <int kRows, int kChunk>
+struct Walk {
+    Place place;
+    long long at, end;
+    __device__ __forceinline__ bool next(const CacheAttendArgs& p, Segment& s)
+    {
+        if (at >= end) return false;
+        s.at = place;
+        s.have = stream_tokens(p, place.b, false);
+        s.first = first_position(p, place.b, s.have);
+        s.seen = keys_seen(p, s.have, s.first, (place.rb + 1) * kRows);
+        s.rows = min(kRows, p.queries * p.rep - place.rb * kRows);
+        s.chunks = max(1, (s.seen + kChunk - 1) / kChunk);
+        s.c0 = (int)(at - place.item_begin);
+        s.c1 = (int)min((long long)s.chunks, s.c0 + (end - at));
+        s.opens = s.c0 == 0;
+        at += s.c1 - s.c0;
+        if (s.c1 == s.chunks) {
+            place.item_begin += s.chunks;
+            if (++place.h == p.c.kv_heads) {
+                place.h = 0;
+                if (++place.rb == p.row_blocks) { place.rb = 0; ++place.b; }
+            }
+        }
+        return true;
+    }
+};
 
 // The CTAs that share an item, and where each of them leaves its rows: an item begins as the last thing that its first CTA
 // does, and goes on as the first thing that every other one does.
@@ -141,11 +185,11 @@ struct Parts {
     int first, count;
     __device__ __forceinline__ int slot(int cta) const { return 2 * cta + (cta == first ? 1 : 0); }
 };
-__device__ __forceinline__ Parts item_parts(const Cut& c, long long item_begin, int chunks)
+__device__ __forceinline__ Parts item_parts(long long share, long long item_begin, int chunks)
 {
     Parts q;
-    q.first = (int)(item_begin / c.share);
-    q.count = (int)((item_begin + chunks - 1) / c.share) - q.first + 1;
+    q.first = (int)(item_begin / share);
+    q.count = (int)((item_begin + chunks - 1) / share) - q.first + 1;
     return q;
 }
 
