@@ -333,9 +333,9 @@ int arl2_cache_append(arl2_cache* cache, const void* d_k, int64_t k_batch_stride
  * j = 0 .. lengths[b] - 1, with ARL2_CACHE_CAUSAL only j <= t.  A row that sees no key is zero.
  *   d_q        [B, queries, H, D] of the I/O type, strides as in arl2_cache_append; d_out the same, contiguous
  *   d_lengths  [B] int32, 0 allowed; d_q_start [B] int32 or NULL: the queries are the last tokens held, lengths[b] - queries
- * Positions before the first row of the rotary tables count as the first row.  A length past the table, a page that the pool
- * does not have, or a position past the rotary tables counts as the last there is (a page: as not visible), and
- * arl2_sync_status reports ARL2_ERR_RANGE.  bf16 I/O: fp16 operands on tensor cores, fp32 softmax and sums; fp32 I/O: each
+ * Positions before the first row of the rotary tables count as the first row.  A length past the table or a position past the
+ * rotary tables counts as the last there is, a page that the pool does not have reads as zeros, and arl2_sync_status reports
+ * ARL2_ERR_RANGE.  bf16 I/O: fp16 operands on tensor cores, fp32 softmax and sums; fp32 I/O: each
  * fp32 operand as two fp16 numbers (the codes are exact), to fp32's accuracy.  Bitwise reproducible.
  */
 #define ARL2_CACHE_CAUSAL 1u

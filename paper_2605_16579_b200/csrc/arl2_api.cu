@@ -1094,15 +1094,23 @@ namespace {
 
 // Scratch of a cache: tickets of the items that several CTAs share, their rows' statistics, their rows
 struct CacheLayout {
-    size_t tickets, part_ml, part_o, total;
+    size_t tickets, part_items, part_ml, part_o, marks, unpacked, total;
+    int unpack_pairs;
 };
-CacheLayout cache_layout(int D)
+CacheLayout cache_layout(const arl2_config& cfg, const arl2_cache_config& c)
 {
     CacheLayout l;
+    const int D = cfg.D;
     size_t off = 0;
     l.tickets = off; off += align_up((size_t)kCacheCtas * sizeof(uint32_t));
+    l.part_items = off; off += align_up((size_t)kCacheTcCtas * sizeof(int4));
     l.part_ml = off; off += align_up((size_t)kCachePartRows * 2 * sizeof(float));
     l.part_o = off;  off += align_up((size_t)kCachePartRows * D * sizeof(float));
+    // operand tiles of all the keys that there may be, or of as many as that is worth
+    const int64_t tiles = ((int64_t)c.max_pages * c.page_tokens + 127) / 128 * c.kv_heads * cfg.B;
+    l.unpack_pairs = !tc_supported(cfg) ? 0 : (int)(tiles < kUnpackMost ? tiles : kUnpackMost);
+    l.marks = off;    off += align_up((size_t)l.unpack_pairs * kUnpackMarks * sizeof(uint32_t));
+    l.unpacked = off; off += (size_t)l.unpack_pairs * kUnpackPair;
     l.total = off;
     return l;
 }
@@ -1159,6 +1167,10 @@ struct arl2_cache {
     float* part_o;
     float* part_ml;
     uint32_t* tickets;
+    int4* part_items;
+    uint8_t* unpacked;
+    uint32_t* unpack_marks;
+    int unpack_pairs;
 };
 
 size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
@@ -1170,7 +1182,7 @@ size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* ca
 size_t arl2_cache_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
 {
     if (!valid_cache_config(cfg, cache_cfg)) return 0;
-    return cache_layout(cfg->D).total;
+    return cache_layout(*cfg, *cache_cfg).total;
 }
 
 int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d_pages, const int32_t* d_page_table,
@@ -1193,7 +1205,7 @@ int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d
         set_error("cache_create: pages must be 128-byte, rotary tables 16-byte and the page table 4-byte aligned");
         return ARL2_ERR_INVALID_ARG;
     }
-    const CacheLayout lay = cache_layout(ctx->cfg.D);
+    const CacheLayout lay = cache_layout(ctx->cfg, *cache_cfg);
     if (workspace_bytes < lay.total || reinterpret_cast<uintptr_t>(d_workspace) % kAlign != 0) {
         set_error("cache_create: the workspace needs %zu bytes, 256-byte aligned (got %zu)", lay.total, workspace_bytes);
         return ARL2_ERR_WORKSPACE;
@@ -1216,8 +1228,12 @@ int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d
     c->view.rope_rows = cache_cfg->rope_rows;
     c->view.status = reinterpret_cast<uint32_t*>(ctx->ws + ctx->lay.status);
     c->tickets = reinterpret_cast<uint32_t*>(ws + lay.tickets);
+    c->part_items = reinterpret_cast<int4*>(ws + lay.part_items);
     c->part_ml = reinterpret_cast<float*>(ws + lay.part_ml);
     c->part_o = reinterpret_cast<float*>(ws + lay.part_o);
+    c->unpacked = ws + lay.unpacked;
+    c->unpack_marks = reinterpret_cast<uint32_t*>(ws + lay.marks);
+    c->unpack_pairs = lay.unpack_pairs;
     const int r = account(ctx, fill_zero(c->tickets, kCacheCtas * sizeof(uint32_t), as_stream(stream)));
     if (r != ARL2_OK) { delete c; return r; }
     *out = c;
@@ -1289,6 +1305,9 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
     a.scale_log2 = cache->ctx->shape.scale_log2;
     a.out = d_out;
     a.part_o = cache->part_o; a.part_ml = cache->part_ml; a.tickets = cache->tickets;
+    a.part_items = cache->part_items;
+    a.unpacked = cache->unpacked; a.unpack_marks = cache->unpack_marks; a.unpack_pairs = cache->unpack_pairs;
+    a.tensor_cores = cache->ctx->use_tc;
     a.wide = rows_are_wide(d_q, q_batch_stride, q_token_stride, elem) && rows_are_wide(d_out, 0, 0, 1);
     a.wait_limit = cache->ctx->wait_limit;
     return account(cache->ctx, cache_attend(a, cfg.io_dtype, as_stream(stream)));

@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
     grid_dependency_sync();
     const Cut cut = cut_work<kRows, kChunk, kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
     if (cut.begin >= cut.end) return;
-    Walk<kRows, kChunk> walk{locate<kRows, kChunk, kThreads>(p, cut.begin, scratch), cut.begin, cut.end};
+    Walk<kRows, kChunk, false> walk{locate<kRows, kChunk, kThreads>(p, cut.begin, scratch), cut.begin, cut.end};
 
     Segment seg;
     while (walk.next(p, seg)) {
@@ -477,8 +477,8 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
                 for (int g = 0; g < G; ++g) lows[t][e][g] = 0.0f;
             }
 
-        // Key tiles of this warp: chunk * kWarps + warp.  A lane holds the page of one of the next 32 of them; -1: none, or
-        // one that the pool does not have.
+        // Key tiles of this warp: chunk * kWarps + warp.  A lane holds the page of one of the next 32 of them; -1: nothing to see,
+        // -2: one that the pool does not have.
         const int32_t* table = p.c.table + (size_t)b * p.c.max_pages;
         auto page_of = [&](int c) {
             const int key = (c * kWarps + warp) * kKeys;
@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
             const int page = table[key >> p.c.page_shift];
             if (page >= 0 && page < p.c.num_pages) return page;
             range_error(p.c.status, kRangePage, b);
-            return -1;
+            return -2;
         };
         int pages_from = c0, my_page = page_of(c0 + lane);
         auto fetch = [&](int c, Raw<G>& raw) {      // whether there is anything to do for this warp in chunk c
@@ -495,7 +495,11 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
                 my_page = page_of(c + lane);
             }
             const int page = __shfl_sync(0xffffffffu, my_page, c - pages_from);
-            if (page < 0) return false;
+            if (page == -1) return false;
+            if (page < 0) {      // reads as zeros
+                raw = Raw<G>();
+                return true;
+            }
             const int key = (c * kWarps + warp) * kKeys;
             load_raw<D>(raw, p.c.pages + ((size_t)page * p.c.kv_heads + h) * p.c.unit_bytes, page_tokens, key & (page_tokens - 1), gid, tig);
             return true;
@@ -843,7 +847,7 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
 
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)
 {
-    if (a.D == 128 && dtype == ARL2_BF16 && a.queries * a.rep > 32) return tc_cache_attend(a, st);
+    if (a.tensor_cores && a.queries * a.rep > 32) return tc_cache_attend(a, st);
     return a.D == 128 ? attend_any<128>(a, dtype, st) : attend_any<64>(a, dtype, st);
 }
 

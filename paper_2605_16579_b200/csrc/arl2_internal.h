@@ -215,6 +215,11 @@ constexpr int kCacheCtas = 4 * 148;        // most CTAs of the warp-level kernel
 constexpr int kCacheTcCtas = 148;          // most CTAs of the tcgen05 kernel, of 256 rows
 constexpr int kCachePartRows = 2 * kCacheTcCtas * 256;
 static_assert(2 * kCacheCtas * 32 <= kCachePartRows, "the partial rows of both kernels have the same room");
+// ... and for keys and values of the tcgen05 kernel turned into operand tiles ahead of it: a K and a V tile of 128 keys of a head
+constexpr size_t kUnpackPair = 2 * 128 * 128 * 2;
+constexpr int kUnpackMost = 4096;          // pairs at most (256 MB)
+constexpr int kUnpackMarks = 16;           // words beside a pair: what is special about its keys
+constexpr int kUnpackStreams = 128;        // most streams
 struct CacheAttendArgs {
     CacheView c;
     int s_B, H, D, queries;
@@ -231,7 +236,13 @@ struct CacheAttendArgs {
     float* part_o;           // [kCachePartRows, D] unnormalised rows
     float* part_ml;          // [kCachePartRows, 2] reference maximum (log2 units), row sum
     uint32_t* tickets;       // [kCacheCtas], zero between calls
+    int4* part_items;        // [kCacheTcCtas] the item that a CTA of the tcgen05 kernel began and others went on with: parts, stream, block of rows, key head
+    uint8_t* unpacked = nullptr;       // [unpack_pairs] pairs of operand tiles, and
+    uint32_t* unpack_marks = nullptr;  // [unpack_pairs, kUnpackMarks]
+    int unpack_pairs = 0;
+    int either = 0;          // the lengths decide whether the tiles are unpacked ahead (set by the launcher)
     bool wide;               // as in CacheAppendArgs, for q and out
+    bool tensor_cores;       // the context is one of the tcgen05 kernels (bf16 I/O, D = 128, not asked to do without)
     uint32_t wait_limit = 0; // as in StepArgs
 };
 int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st);

@@ -1,17 +1,20 @@
 // Attention over the paged 4-bit cache on tcgen05 / TMEM, for many query rows (bf16 I/O, D = 128).
 //
 // One CTA per SM.  An item is two 128-row tiles of query rows of one key head against the keys that they see; the items' key
-// tiles of 128 form one sequence that is cut evenly over the CTAs (cache_common.cuh).  Roles of the 16 warps:
+// tiles of 128 form one sequence that is cut evenly over the CTAs (cache_common.cuh).  Roles:
 //   warps 0-3 / 4-7   softmax group of tile 0 / 1, one thread per query row.  It also writes its tile's Q operand: rows rotated in
 //                     fp32, scaled by a power of two into fp16's range, rounded to fp16 once.
-//   warps 8-11        K and V: codes and parameters of a tile from global memory into registers, one tile ahead, from there as
-//                     minimum + step * code in fp16 into a ring of 32 KB operand tiles.  (fp16: the codes are exact in it, and
-//                     its rounding, 2^-12, is a sixteenth of bf16's.)
-//   warps 12 / 13     MMA issuer of tile 0 / 1:  S_t = Q_t K_j^T and O_t += P_t V_j into TMEM
+//   two warps         MMA issuer of tile 0 / 1:  S_t = Q_t K_j^T and O_t += P_t V_j into TMEM
+//   K and V           into a ring of 32 KB operand tiles of minimum + step * code in fp16 (in which the codes are exact; its rounding,
+//                     2^-12, is an eighth of bf16's), in one of two ways:
+//     unpacked ahead  cache_unpack_kernel writes the operand tiles of all keys to the workspace, as they stand in shared memory,
+//                     and one thread copies them in.  Costs 512 bytes per key and head written and read again, once per call.
+//     on the way      four warps read codes and parameters, one tile ahead, and write the operand tiles themselves: no workspace, but
+//                     every item converts its keys anew, beside two softmax groups that want the same issue slots.
 // TMEM (512 columns): S_0 | S_1 | O_0 | O_1, the fp16 probabilities over the first 64 columns of S_t.
 // The codes i and i + 4 of a 32-bit word come out of it as a pair, so that operand columns stand in the order 0 4 1 5 2 6 3 7 in every
 // eight: the Q operand is written in the same order, and the output's columns are put back in order when they are read.
-// Keys that are not there (past the length, in a page that the pool does not have) are written as zeros and masked in the scores.
+// Keys past the length are written as zeros and masked in the scores; a page that the pool does not have reads as zeros.
 //
 // An item that several CTAs work on leaves unnormalised fp32 rows, which cache_join_kernel puts together.
 // Every wait is bounded, as in the step kernel.
@@ -24,10 +27,21 @@ namespace {
 constexpr int kD = 128;
 constexpr int kItemRows = 2 * kTile;
 constexpr int kStages = 5;
-constexpr int kThreads = 512;
-// setmaxnreg moves registers within what the CTA was launched with: 512 threads x 128
-constexpr int kRegsSoftmax = 192, kRegsHold = 88, kRegsIssue = 40;
-static_assert(256 * kRegsSoftmax + 128 * kRegsHold + 128 * kRegsIssue <= kThreads * 128, "register pool");
+// Warps and registers of the two ways.  setmaxnreg moves registers within what the CTA was launched with (threads x launch registers).
+template <bool kUnpacked>
+struct Roles;
+template <>
+struct Roles<true> {
+    static constexpr int kThreads = 384, kIssuer = 9;          // warp 8 copies
+    static constexpr int kRegsSoftmax = 232, kRegsOther = 40;
+    static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * 168, "register pool");
+};
+template <>
+struct Roles<false> {
+    static constexpr int kThreads = 512, kIssuer = 12;         // warps 8-11 convert
+    static constexpr int kRegsSoftmax = 192, kRegsHold = 88, kRegsOther = 40;
+    static_assert(256 * kRegsSoftmax + 128 * kRegsHold + 128 * kRegsOther <= kThreads * 128, "register pool");
+};
 constexpr float kRescaleThreshold = 8.0f;   // log2 units of slack before O is rescaled: p <= 2^8
 
 constexpr int kOffQ = 0;
@@ -35,9 +49,10 @@ constexpr int kOffRing = kOffQ + 2 * kTileBytes;
 constexpr int kOffBars = kOffRing + kStages * kTileBytes;
 constexpr int kSpecials = 16;               // key tiles whose marks are kept (more than are ever under way)
 constexpr int kOffMarks = kOffBars + 256;   // [kSpecials][kMarkWords]
-constexpr int kMarkWords = 10;              // any; keys by 16 without a page (bits 0-7); keys with a NaN value, per group [2][4]
+constexpr int kMarkWords = 9;               // whether a value is not finite; the keys of those, per group [2][4]
+static_assert(kMarkWords <= kUnpackMarks, "marks");
 constexpr int kSmemBytes = kOffMarks + kSpecials * kMarkWords * 4 + 1024;   // + alignment slack
-static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 20 * 8 <= 227 * 1024, "shared memory, with what the kernel declares itself");
 
 enum Bar : int {
     kBarQ0 = 0, kBarQ1,                         // softmax group t -> issuer t: the Q operand is written
@@ -51,6 +66,18 @@ enum Bar : int {
     kNumBars
 };
 static_assert(kNumBars * 8 + 8 <= 256, "barrier block");
+
+// bytes (a multiple of 16, both addresses on 16) into this CTA's shared memory
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void st_shared_zero(uint32_t addr)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0) : "memory");
+}
 
 // fp16 x fp16 -> fp32
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn)
@@ -66,11 +93,56 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 // operand column c holds channel channel_of(c); column of channel: the inverse, per eight 0 2 4 6 1 3 5 7
 __host__ __device__ constexpr int column_of(int channel) { return (channel & ~7) | ((channel & 3) << 1) | ((channel >> 2) & 1); }
 
-using ItemWalk = Walk<kItemRows, kTile>;
+using ItemWalk = Walk<kItemRows, kTile, true>;
 
-// ---- one thread per query row
+// Operand tiles unpacked ahead: pair (first[b] + j) * kv_heads + h holds K and V of key tile j.  All threads of the CTA.
+// Whether all of them have room; `first`: kUnpackStreams + 1 words of shared memory.
+__device__ __forceinline__ bool place_tiles(const CacheAttendArgs& p, int* first)
+{
+    // (fewer streams than threads: a scan by one warp)
+    if (threadIdx.x < 32) {
+        int before = 0;
+        for (int b0 = 0; b0 < p.s_B; b0 += 32) {
+            const int b = b0 + (int)threadIdx.x;
+            const int tiles = b < p.s_B ? (stream_tokens(p, b, false) + kTile - 1) / kTile : 0;
+            int upto = tiles;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, upto, d);
+                if ((int)threadIdx.x >= d) upto += x;
+            }
+            if (b < p.s_B) first[b] = before + upto - tiles;
+            // (past the room, where it is only compared with: no overflow)
+            before = min(before + __shfl_sync(0xffffffffu, upto, 31), kUnpackMost + 1);
+        }
+        if (threadIdx.x == 0) first[p.s_B] = before;
+    }
+    __syncthreads();
+    return (long long)first[p.s_B] * p.c.kv_heads <= p.unpack_pairs;
+}
+
+__device__ __forceinline__ bool not_finite(uint32_t params) { return (params & 0x7c00u) == 0x7c00u || (params & 0x7c000000u) == 0x7c000000u; }
+
+// 8 channels of a row: one word of codes -> 16 bytes of an operand row, in the order 0 4 1 5 2 6 3 7
+__device__ __forceinline__ uint4 hold_word(uint32_t codes, __half2 low, __half2 step)
+{
+    uint32_t v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint32_t word = (c & 2) ? codes >> 8 : codes;
+        const uint32_t x = (c & 1) ? (word & 0x00F000F0u) | 0x54005400u : (word & 0x000F000Fu) | 0x64006400u;   // 64 + code, 1024 + code
+        const __half2 code = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2half2(__ushort_as_half((c & 1) ? 0x5400 : 0x6400)));
+        const __half2 y = __hfma2(code, step, low);
+        v[c] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// ---- one thread per query row.  marks: what is special about the key tiles, in shared memory by key tiles so far, or
+// beside the tiles unpacked ahead (first: place_tiles)
+template <bool kUnpacked>
 __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* smem, uint32_t bars, uint32_t tmem_base, const Abort& ab,
-                                             const volatile uint32_t* marks, ItemWalk walk, long long share, int t, int r, int warp_in_group)
+                                             const volatile uint32_t* marks, const int* first, ItemWalk walk, const Cut& cut, int t, int r, int warp_in_group)
 {
     const uint32_t lane_base = tmem_base + ((uint32_t)(warp_in_group * 32) << 16);
     const uint32_t s_addr = lane_base + (uint32_t)(t * kTile);
@@ -78,6 +150,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
     const uint32_t bar_s = bars + 8 * (kBarS0 + t), bar_p = bars + 8 * (kBarP0 + t);
     uint32_t s_cnt = 0, o_cnt = 0, tile_cnt = 0;   // phases consumed; key tiles so far, whichever group has work in them
     uint32_t sreg[128];
+    int4 begun = make_int4(0, 0, 0, 0);     // the item that this CTA began and others went on with
 
     Segment seg;
     while (walk.next(p, seg)) {
@@ -160,8 +233,23 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         const uint64_t c2x2 = pack2(c2, c2);
         float m_ref = -INFINITY;
         uint64_t l2 = pack2(0.0f, 0.0f);
-        uint32_t poison = 0;      // groups of channels that a NaN reaches this row in
-        for (int jj = 0; jj < n; ++jj, ++tile_cnt) {
+        // groups of channels that a NaN reaches this row in.  (With causality only: a row that does not see a key is not to meet it as
+        // 0 * NaN, so such values are taken out of V and marked.)
+        uint32_t poison = 0;
+        const uint32_t* pair_marks = p.unpack_marks;
+        const size_t mark_stride = (size_t)p.c.kv_heads * kUnpackMarks;
+        if (kUnpacked && p.causal) pair_marks += ((size_t)(first[seg.at.b] + seg.c0) * p.c.kv_heads + seg.at.h) * kUnpackMarks;
+        auto poison_of = [&](int jj) {
+            const int visible_keys = sees - (seg.c0 + jj) * kTile;
+            auto word = [&](int i) { return kUnpacked ? pair_marks[jj * mark_stride + i] : marks[((tile_cnt + jj) % kSpecials) * kMarkWords + i]; };
+            if (word(0) == 0) return;
+            for (int i = 0; i < 8; ++i) {
+                const int left = visible_keys - (i & 3) * 32;      // keys of this word that the row sees
+                const uint32_t visible = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+                if (word(1 + i) & visible) poison |= 1u << (i >> 2);
+            }
+        };
+        for (int jj = 0; jj < n; ++jj) {
             const int key0 = (seg.c0 + jj) * kTile;
             (void)wait_bar(bar_s, s_cnt & 1, ab, 120 + t);   // (where it expired, the loop goes on over whatever is there)
             ++s_cnt;
@@ -175,19 +263,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
                 for (int c = 0; c < 128; ++c)
                     if (c >= n_valid) sreg[c] = __float_as_uint(-INFINITY);
             }
-            const volatile uint32_t* mark = marks + (tile_cnt % kSpecials) * kMarkWords;
-            if (mark[0] != 0) {      // (rare)
-                const uint32_t gone = mark[1];
-#pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if ((gone >> (c >> 4)) & 1) sreg[c] = __float_as_uint(-INFINITY);
-                for (int g = 0; g < 2; ++g)
-                    for (int w = 0; w < 4; ++w) {
-                        const int left = n_valid - w * 32;      // keys of this word that the row sees
-                        const uint32_t visible = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
-                        if (mark[2 + g * 4 + w] & visible) poison |= 1u << g;
-                    }
-            }
+            if (p.causal && jj > 0) poison_of(jj - 1);     // (V of the tile before is there: P V has been computed)
             float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int c = 0; c < 128; c += 8) {
@@ -242,7 +318,10 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         if (!wait_bar_warp(bars + 8 * (kBarO0 + t), o_cnt & 1, ab, 140 + t)) return;
         ++o_cnt;
         tc_fence_after();
-        const Parts parts = item_parts(share, seg.at.item_begin, seg.chunks);
+        if (p.causal && seg.seen > 0) poison_of(n - 1);
+        tile_cnt += n;
+        const Parts parts = item_parts(cut.share, seg.at.item_begin - cut.base, seg.chunks);
+        if (parts.count > 1 && parts.first == (int)blockIdx.x) begun = make_int4(parts.count, seg.at.b, seg.at.rb, seg.at.h);
         const float nan = __int_as_float(0x7fc00000);
         if (parts.count > 1) {
             const size_t row = (size_t)parts.slot((int)blockIdx.x) * kItemRows + in_item;
@@ -298,131 +377,145 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         }
         tc_fence_before();
     }
+    if (t == 0 && r == 0) p.part_items[blockIdx.x] = begun;
 }
 
-// ---- 128 threads that bring K and V: four threads a row of codes, 16 bytes each
+// ---- two warps that bring K, two that bring V: four threads a row of codes, 16 bytes each
+constexpr int kHoldRows = 8;        // rows of a thread
 struct HeldRows {
-    uint4 codes[4];
-    uint32_t params[4];     // fp16 (minimum, step); zero where no key is
+    uint4 codes[kHoldRows];
+    uint32_t params[kHoldRows];     // fp16 (minimum, step); zero where no key is
 };
-__device__ __forceinline__ bool not_finite(uint32_t params) { return (params & 0x7c00u) == 0x7c00u || (params & 0x7c000000u) == 0x7c000000u; }
-
-__device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t* marks, ItemWalk walk, int tid)
+__device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t* marks, ItemWalk walk, int which, int tid)
 {
-    const int page_tokens = 1 << p.c.page_shift, quarter = tid & 3, lane = tid & 31;
     using U = Unit<kD>;
-    // Rows of this thread: base + 32 i.  The two upper quarters take the row two further (^ 2) at the same time: with it the eight
+    const int page_tokens = 1 << p.c.page_shift, quarter = tid & 3, lane = tid & 31;
+    const int codes_at = (which ? U::v_codes(page_tokens) : 0) + quarter * 16;
+    const int params_at = (which ? U::v_par(page_tokens) : U::k_par(page_tokens)) + (quarter >> 1) * 4;
+    // Rows of this thread: row0 + 16 i.  The two upper quarters take the row two further (^ 2) at the same time: with it the eight
     // threads of a store's phase fall into eight different 16-byte columns of the swizzled tile.
     const int row0 = (tid >> 2) ^ ((quarter & 2) ? 2 : 0);
-    uint32_t n = 0, tile_cnt = 0;
+    uint32_t entry = which, tile_cnt = 0;     // this role's next ring entry; key tiles so far
     bool ok = true;
 
     Segment seg;
-    // pages of this thread's rows of a key tile; -1: no key there
-    auto look_up = [&](const Segment& s, int tile, int (&page)[4]) {
-        const int32_t* table = p.c.table + (size_t)s.at.b * p.c.max_pages;
+    // pages of this thread's rows of a key tile; -1: no key there.  (16 rows that begin at a multiple of 16 have one page.)
+    auto look_up = [&](int tile, int (&page)[kHoldRows]) {
+        const int32_t* table = p.c.table + (size_t)seg.at.b * p.c.max_pages;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int key = tile * kTile + row0 + 32 * i;
-            page[i] = key < s.seen && tile < s.c1 ? table[key >> p.c.page_shift] : -1;
+        for (int i = 0; i < kHoldRows; ++i) {
+            const int key = tile * kTile + row0 + 16 * i;
+            page[i] = key < seg.seen && tile < seg.c1 ? table[key >> p.c.page_shift] : -1;
         }
     };
-    auto fetch = [&](const Segment& s, int tile, const int (&page)[4], int which, HeldRows& r) {
+    auto fetch = [&](int tile, const int (&page)[kHoldRows], HeldRows& r) {
+        const uint8_t* head = p.c.pages + seg.at.h * p.c.unit_bytes;
+        const size_t page_bytes = p.c.unit_bytes * p.c.kv_heads;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kHoldRows; ++i) {
             r.codes[i] = make_uint4(0, 0, 0, 0);
             r.params[i] = 0;
-            if (page[i] >= 0 && page[i] < p.c.num_pages) {
-                const int slot = (tile * kTile + row0 + 32 * i) & (page_tokens - 1);
-                const uint8_t* unit = p.c.pages + ((size_t)page[i] * p.c.kv_heads + s.at.h) * p.c.unit_bytes;
-                r.codes[i] = *reinterpret_cast<const uint4*>(unit + (which ? U::v_codes(page_tokens) : 0) + slot * U::kRow + quarter * 16);
-                r.params[i] = *reinterpret_cast<const uint32_t*>(unit + (which ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + (quarter >> 1) * 4);
+            if ((uint32_t)page[i] < (uint32_t)p.c.num_pages) {
+                const int slot = (tile * kTile + row0 + 16 * i) & (page_tokens - 1);
+                const uint8_t* unit = head + (uint32_t)page[i] * page_bytes;
+                r.codes[i] = *reinterpret_cast<const uint4*>(unit + codes_at + slot * U::kRow);
+                r.params[i] = *reinterpret_cast<const uint32_t*>(unit + params_at + slot * U::kPar);
             }
         }
     };
-    // what softmax has to know of a tile, before its keys go out
-    auto mark = [&](const Segment& s, int tile, const int (&page)[4], const HeldRows& k, HeldRows& v) {
+    // what softmax has to know of a tile, and the caller (rare)
+    auto mark = [&](int tile, const int (&page)[kHoldRows], HeldRows& r) {
         uint32_t* m = marks + (tile_cnt % kSpecials) * kMarkWords;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 32 * i, key = tile * kTile + row;
-            if (key < s.seen && (page[i] < 0 || page[i] >= p.c.num_pages)) {
-                range_error(p.c.status, kRangePage, s.at.b);
-                atomicOr(m + 1, 1u << (row >> 4));
-                m[0] = 1;
-            }
-            // a value that is not finite would reach rows that do not see it as 0 * NaN: it is taken out, and softmax told
-            if (p.causal && not_finite(v.params[i])) {
-                v.params[i] = 0;
-                atomicOr(m + 2 + (quarter >> 1) * 4 + (row >> 5), 1u << (row & 31));
+        for (int i = 0; i < kHoldRows; ++i) {
+            const int row = row0 + 16 * i;
+            if (which == 0) {
+                if (tile * kTile + row < seg.seen && (uint32_t)page[i] >= (uint32_t)p.c.num_pages) range_error(p.c.status, kRangePage, seg.at.b);
+            } else if (p.causal && not_finite(r.params[i])) {
+                r.params[i] = 0;
+                atomicOr(m + 1 + (quarter >> 1) * 4 + (row >> 5), 1u << (row & 31));
                 m[0] = 1;
             }
         }
-        (void)k;
     };
-    auto clear_mark = [&](uint32_t tile) {
-        if (tid < kMarkWords) marks[(tile % kSpecials) * kMarkWords + tid] = 0;
-    };
-    // a ring slot's worth: out of registers, as fp16 values, into the swizzled operand tile
+    // a ring entry: out of registers, as fp16 values, into the swizzled operand tile
     auto put = [&](const HeldRows& r) {
-        const uint32_t slot = n % kStages;
-        if (n >= (uint32_t)kStages) ok = wait_bar_warp(bars + 8 * (kBarEmpty0 + slot), ((n / kStages) - 1) & 1, ab, 151);
+        const uint32_t slot = entry % kStages;
+        if (entry >= (uint32_t)kStages) ok = wait_bar_warp(bars + 8 * (kBarEmpty0 + slot), ((entry / kStages) - 1) & 1, ab, 151 + which);
         if (!ok) return;
         uint8_t* tile = smem + kOffRing + slot * kTileBytes + (quarter >> 1) * kHalfBytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 32 * i;
+        for (int i = 0; i < kHoldRows; ++i) {
+            const int row = row0 + 16 * i;
             const uint32_t w[4] = {r.codes[i].x, r.codes[i].y, r.codes[i].z, r.codes[i].w};
             const __half2 both = *reinterpret_cast<const __half2*>(&r.params[i]);
             const __half2 low = __low2half2(both), step = __high2half2(both);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                uint32_t v[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t word = (c & 2) ? w[k] >> 8 : w[k];
-                    const uint32_t x = (c & 1) ? (word & 0x00F000F0u) | 0x54005400u : (word & 0x000F000Fu) | 0x64006400u;   // 64 + code, 1024 + code
-                    const __half2 code = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2half2(__ushort_as_half((c & 1) ? 0x5400 : 0x6400)));
-                    const __half2 y = __hfma2(code, step, low);
-                    v[c] = *reinterpret_cast<const uint32_t*>(&y);
-                }
                 const int chunk = (quarter & 1) * 4 + k;
-                *reinterpret_cast<uint4*>(tile + row * 128 + ((chunk ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<uint4*>(tile + row * 128 + ((chunk ^ (row & 7)) << 4)) = hold_word(w[k], low, step);
             }
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (kBarFull0 + slot));
-        ++n;
+        entry += 2;
     };
 
     while (ok && walk.next(p, seg)) {
-        if (tid == 0 && seg.opens) (void)stream_tokens(p, seg.at.b, true);
-        // entries: K_0 V_0 K_1 V_1 ...; a tile's codes are fetched while the tile before is written
-        int page[4], next_page[4];
-        HeldRows k, v;
-        look_up(seg, seg.c0, page);
-        fetch(seg, seg.c0, page, 0, k);
-        fetch(seg, seg.c0, page, 1, v);
-        look_up(seg, seg.c0 + 1, next_page);
+        if (tid == 0 && which == 0 && seg.opens) (void)stream_tokens(p, seg.at.b, true);
+        // entries: K_0 V_0 K_1 V_1 ...; a tile's codes are fetched while the tile before is waited for and its pages looked up one earlier
+        int page[kHoldRows], next_page[kHoldRows];
+        HeldRows r;
+        look_up(seg.c0, page);
+        look_up(seg.c0 + 1, next_page);
+        fetch(seg.c0, page, r);
         for (int j = seg.c0; j < seg.c1 && ok; ++j, ++tile_cnt) {
-            clear_mark(tile_cnt + kSpecials / 2);
-            mark(seg, j, page, k, v);
-            put(k);
-            if (!ok) break;
-            if (j + 1 < seg.c1) fetch(seg, j + 1, next_page, 0, k);
-            put(v);
-            if (!ok) break;
-            if (j + 1 < seg.c1) fetch(seg, j + 1, next_page, 1, v);
+            if (which == 1 && tid < kMarkWords) marks[((tile_cnt + kSpecials / 2) % kSpecials) * kMarkWords + tid] = 0;
+            mark(j, page, r);
+            put(r);
+            if (!ok || j + 1 == seg.c1) continue;
+            fetch(j + 1, next_page, r);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) page[i] = next_page[i];
-            look_up(seg, j + 2, next_page);
+            for (int i = 0; i < kHoldRows; ++i) page[i] = next_page[i];
+            look_up(j + 2, next_page);
         }
     }
 }
 
-__global__ void __launch_bounds__(kThreads, 1) tc_cache_attend_kernel(const CacheAttendArgs p)
+// ---- one thread that copies the tiles unpacked ahead.  Returns the ring entries that it has sent for.
+__device__ __forceinline__ uint32_t copy_role(const CacheAttendArgs& p, uint32_t smem_base, uint32_t bars, const Abort& ab, const int* first, ItemWalk walk)
 {
+    uint32_t n = 0;
+    Segment seg;
+    while (walk.next(p, seg)) {
+        if (seg.opens) (void)stream_tokens(p, seg.at.b, true);
+        // (an item without keys has one tile of which every score is masked: any tile will do, and there need not be one)
+        const bool none = seg.seen == 0;
+        const uint8_t* src = p.unpacked + ((size_t)(first[seg.at.b] + (none ? 0 : seg.c0)) * p.c.kv_heads + seg.at.h) * kUnpackPair;
+        const size_t step = (size_t)p.c.kv_heads * kUnpackPair;
+        for (int e = 0; e < 2 * (seg.c1 - seg.c0); ++e, ++n) {
+            const uint32_t slot = n % kStages;
+            const bool ok = n < (uint32_t)kStages || wait_bar(bars + 8 * (kBarEmpty0 + slot), ((n / kStages) - 1) & 1, ab, 150);
+            if (!ok) return n;
+            const uint32_t bar = bars + 8 * (kBarFull0 + slot);
+            if (none) {
+                for (int i = 0; i < kTileBytes / 16; ++i) st_shared_zero(smem_base + kOffRing + slot * kTileBytes + i * 16);
+                fence_proxy_async_smem();
+                mbar_arrive(bar);
+            } else {
+                mbar_expect_tx(bar, kTileBytes);
+                bulk_load(smem_base + kOffRing + slot * kTileBytes, src + (size_t)(e >> 1) * step + (e & 1) * kTileBytes, kTileBytes, bar);
+            }
+        }
+    }
+    return n;
+}
+
+template <bool kUnpacked>
+__global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend_kernel(const CacheAttendArgs p)
+{
+    using R = Roles<kUnpacked>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t bars = smem_u32(smem) + kOffBars;
@@ -431,14 +524,15 @@ __global__ void __launch_bounds__(kThreads, 1) tc_cache_attend_kernel(const Cach
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kOffMarks);
     const Abort ab{abort_flag, p.c.status, p.wait_limit ? p.wait_limit - 1 : kSpinLimit};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    __shared__ long long scratch[kThreads / 32 + 3];
+    __shared__ long long scratch[R::kThreads / 32 + 3];
+    __shared__ int first[kUnpackStreams + 1];
 
     if (tid == 0) {
         mbar_init(bars + 8 * kBarQ0, 128);
         mbar_init(bars + 8 * kBarQ1, 128);
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(bars + 8 * (kBarFull0 + s), 4);    // the four warps that write a tile
-            mbar_init(bars + 8 * (kBarEmpty0 + s), 2);   // both issuers
+            mbar_init(bars + 8 * (kBarFull0 + s), kUnpacked ? 1 : 2);    // the copying thread, or the two warps that write a tile
+            mbar_init(bars + 8 * (kBarEmpty0 + s), 2);                   // both issuers
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(bars + 8 * (kBarS0 + t), 1);
@@ -451,8 +545,9 @@ __global__ void __launch_bounds__(kThreads, 1) tc_cache_attend_kernel(const Cach
         fence_barrier_init();
         fence_proxy_async_smem();
     }
-    for (int i = tid; i < kSpecials * kMarkWords; i += kThreads) marks[i] = 0;
-    if (warp == 12) {
+    if constexpr (!kUnpacked)
+        for (int i = tid; i < kSpecials * kMarkWords; i += R::kThreads) marks[i] = 0;
+    if (warp == R::kIssuer) {
         tmem_alloc(smem_u32(tmem_slot), 512);
         tmem_relinquish();
     }
@@ -462,24 +557,39 @@ __global__ void __launch_bounds__(kThreads, 1) tc_cache_attend_kernel(const Cach
     const uint32_t tmem_base = *tmem_slot;
     grid_dependency_sync();
 
-    const Cut cut = cut_work<kItemRows, kTile, kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
-    ItemWalk walk{{0, 0, 0, 0}, cut.begin, cut.end};
-    if (cut.begin < cut.end) walk.place = locate<kItemRows, kTile, kThreads>(p, cut.begin, scratch);
+    // Where the lengths decide on the way, the other kernel is there, too.
+    bool mine = true;
+    if (kUnpacked || p.either) {
+        const bool room = place_tiles(p, first);
+        mine = !p.either || room == kUnpacked;
+    }
+    const Cut cut = cut_whole_first<kItemRows, kTile, R::kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
+    ItemWalk walk{{0, 0, 0, 0}, cut.begin, mine ? cut.end : cut.begin, mine ? cut.whole : 0, (int)blockIdx.x, (int)gridDim.x};
+    if (cut.begin < cut.end) walk.place = locate_by_head<kItemRows, kTile, R::kThreads>(p, cut.begin, scratch);
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        softmax_role(p, smem, bars, tmem_base, ab, marks, walk, cut.share, warp >> 2, (warp & 3) * 32 + lane, warp & 3);
-    } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsHold));
-        hold_role(p, smem, bars, ab, marks, walk, tid - 256);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kRegsSoftmax));
+        softmax_role<kUnpacked>(p, smem, bars, tmem_base, ab, marks, first, walk, cut, warp >> 2, (warp & 3) * 32 + lane, warp & 3);
+    } else if constexpr (!kUnpacked) {
+        if (warp < 12) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsHold));
+            hold_role(p, smem, bars, ab, marks, walk, (warp - 8) >> 1, tid & 63);
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsOther));
+        }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsOther));
+        if (warp == 8 && lane == 0) {
+            const uint32_t n = copy_role(p, smem_u32(smem), bars, ab, first, walk);
+            // copies into this CTA's shared memory are waited for, whatever became of the waits
+            for (uint32_t m = (n > (uint32_t)kStages ? n - kStages : 0); m < n; ++m) drain_bar(bars + 8 * (kBarFull0 + m % kStages), (m / kStages) & 1);
+        }
     }
-    if (warp == 12 || warp == 13) {
+    if (warp == R::kIssuer || warp == R::kIssuer + 1) {
         // ---- MMA issuers, as in the step kernel: the whole warp walks the loop, one elected lane issues, and the two take turns on
         // the tensor pipe
         const uint32_t lead = elect_one();
-        const int t = __shfl_sync(0xffffffffu, warp - 12, 0);
+        const int t = __shfl_sync(0xffffffffu, warp - R::kIssuer, 0);
         const uint32_t smem_base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
         const uint32_t bars = smem_base + kOffBars;
         const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
@@ -567,55 +677,133 @@ __global__ void __launch_bounds__(kThreads, 1) tc_cache_attend_kernel(const Cach
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == R::kIssuer) {
         tc_fence_after();
         tmem_dealloc(tmem_base, 512);
     }
 }
 
-// ---- rows of the items that several CTAs share.  CTA x of a launch of ctas x kJoinBlocks looks after the item that CTA
-// x / kJoinBlocks began and did not end, if there is one: a warp per row, the parts in the order of their CTAs.
-constexpr int kJoinBlocks = 16, kJoinThreads = 256;
-__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAttendArgs p, int ctas)
+// ---- K and V of every key tile of every stream as operand tiles in the workspace, pair by pair.  Bound by writing them: 512 bytes
+// per key and head.  A thread takes 32 channels of a row at a time and writes them as two whole 32-byte sectors.
+constexpr int kUnpackThreads = 256;
+__global__ void __launch_bounds__(kUnpackThreads) cache_unpack_kernel(const CacheAttendArgs p)
 {
-    __shared__ long long scratch[kJoinThreads / 32 + 3];
+    using U = Unit<kD>;
+    __shared__ int first[kUnpackStreams + 1];
+    __shared__ uint32_t marks[kUnpackMarks];
+    const int tid = threadIdx.x, quarter = tid & 3, page_tokens = 1 << p.c.page_shift;
+    grid_dependency_sync();
+    if (!place_tiles(p, first)) return;
+    const int pairs = first[p.s_B] * p.c.kv_heads;
+    int b = 0;
+    for (int pair = (int)blockIdx.x; pair < pairs; pair += (int)gridDim.x) {
+        const int at = pair / p.c.kv_heads, h = pair - at * p.c.kv_heads;
+        while (first[b + 1] <= at) ++b;      // (pairs only grow)
+        const int tile = at - first[b], have = stream_tokens(p, b, false);
+        if (tid < kUnpackMarks) marks[tid] = 0;
+        __syncthreads();
+        uint4 codes[2][2];
+        uint32_t params[2][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = (tid >> 2) + 64 * e, key = tile * kTile + row;
+            const int page = key < have ? p.c.table[(size_t)b * p.c.max_pages + (key >> p.c.page_shift)] : -1;
+            const bool there = (uint32_t)page < (uint32_t)p.c.num_pages;
+            if (key < have && !there) range_error(p.c.status, kRangePage, b);
+            const int slot = key & (page_tokens - 1);
+            const uint8_t* unit = p.c.pages + ((size_t)(there ? page : 0) * p.c.kv_heads + h) * p.c.unit_bytes;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                codes[e][w] = make_uint4(0, 0, 0, 0);
+                params[e][w] = 0;
+                if (there) {
+                    codes[e][w] = *reinterpret_cast<const uint4*>(unit + (w ? U::v_codes(page_tokens) : 0) + slot * U::kRow + quarter * 16);
+                    params[e][w] = *reinterpret_cast<const uint32_t*>(unit + (w ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + (quarter >> 1) * 4);
+                }
+            }
+            if (p.causal && not_finite(params[e][1])) {     // (taken out, and softmax told)
+                params[e][1] = 0;
+                atomicOr(marks + 1 + (quarter >> 1) * 4 + (row >> 5), 1u << (row & 31));
+                marks[0] = 1;
+            }
+        }
+        uint8_t* out = p.unpacked + (size_t)pair * kUnpackPair + (quarter >> 1) * kHalfBytes;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = (tid >> 2) + 64 * e;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const __half2 both = *reinterpret_cast<const __half2*>(&params[e][w]);
+                const __half2 low = __low2half2(both), step = __high2half2(both);
+                const uint32_t c[4] = {codes[e][w].x, codes[e][w].y, codes[e][w].z, codes[e][w].w};
+#pragma unroll
+                for (int k = 0; k < 4; k += 2) {
+                    // chunks 2 m and 2 m + 1 of the swizzled row share a sector, in the order that the row's lowest bit gives
+                    const uint4 x = hold_word(c[k], low, step), y = hold_word(c[k + 1], low, step);
+                    const bool swap = (row & 1) != 0;
+                    const uint4 lo = swap ? y : x, hi = swap ? x : y;
+                    const uint32_t words[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                    const int chunk = ((quarter & 1) * 4 + k) ^ (row & 6);
+                    store_row32(out + w * kTileBytes + row * 128 + (chunk << 4), words);
+                }
+            }
+        }
+        __syncthreads();
+        if (tid < kUnpackMarks) p.unpack_marks[(size_t)pair * kUnpackMarks + tid] = marks[tid];
+    }
+}
+
+// ---- rows of the items that several CTAs share.  Block x of a launch of ctas x kJoinBlocks looks after part of the item that CTA
+// x / kJoinBlocks began and did not end, if there is one: a warp per row, the parts in the order of their CTAs.
+constexpr int kJoinBlocks = 8, kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAttendArgs p)
+{
     const int cta = (int)blockIdx.x / kJoinBlocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_sync();
-    const Cut cut = cut_work<kItemRows, kTile, kJoinThreads>(p, cta, ctas, scratch);
-    if (cut.begin >= cut.end || p.c.status[kStatusError] != 0u) return;
-    ItemWalk walk{locate<kItemRows, kTile, kJoinThreads>(p, cut.end - 1, scratch), 0, cut.total};
-    walk.at = walk.place.item_begin;
-    Segment seg;
-    (void)walk.next(p, seg);
-    const Parts parts = item_parts(cut.share, seg.at.item_begin, seg.chunks);
-    if (parts.count == 1 || parts.first != cta) return;
+    const int4 item = p.part_items[cta];       // parts, stream, block of rows, key head
+    if (item.x < 2 || p.c.status[kStatusError] != 0u) return;
     constexpr int kRowsEach = kItemRows / kJoinBlocks / (kJoinThreads / 32);
+    const int rows = min(kItemRows, p.queries * p.rep - item.z * kItemRows);
     const int r0 = ((int)blockIdx.x % kJoinBlocks) * (kItemRows / kJoinBlocks) + warp * kRowsEach;
+    if (r0 >= rows) return;
+    const Parts parts{cta, item.x};
+    // rows that are not there are computed from whatever the workspace holds, and not written
+    float m[kRowsEach], total[kRowsEach];
+    float4 acc[kRowsEach];
 #pragma unroll
     for (int x = 0; x < kRowsEach; ++x) {
-        const int r = r0 + x;
-        if (r >= seg.rows) break;
-        float m = -INFINITY;
-        for (int w = 0; w < parts.count; ++w) m = fmaxf(m, p.part_ml[((size_t)parts.slot(parts.first + w) * kItemRows + r) * 2]);
-        const float m_use = m == -INFINITY ? 0.0f : m;
-        float total = 0.0f;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int w = 0; w < parts.count; ++w) {
-            const size_t row = (size_t)parts.slot(parts.first + w) * kItemRows + r;
-            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + row * 2);
-            const float4 o = *reinterpret_cast<const float4*>(p.part_o + row * kD + lane * 4);
-            const float f = ex2_approx(ml.x - m_use);
-            total = fmaf(f, ml.y, total);
-            acc.x = fmaf(f, o.x, acc.x);
-            acc.y = fmaf(f, o.y, acc.y);
-            acc.z = fmaf(f, o.z, acc.z);
-            acc.w = fmaf(f, o.w, acc.w);
+        m[x] = -INFINITY;
+        total[x] = 0.0f;
+        acc[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    for (int w = 0; w < parts.count; ++w) {
+        const size_t row = (size_t)parts.slot(cta + w) * kItemRows + r0;
+        float2 ml[kRowsEach];
+        float4 o[kRowsEach];
+#pragma unroll
+        for (int x = 0; x < kRowsEach; ++x) {
+            ml[x] = *reinterpret_cast<const float2*>(p.part_ml + (row + x) * 2);
+            o[x] = *reinterpret_cast<const float4*>(p.part_o + (row + x) * kD + lane * 4);
         }
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-        const int flat = seg.at.rb * kItemRows + r, i = flat / p.rep, head = seg.at.h * p.rep + flat - i * p.rep;
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)seg.at.b * p.queries + i) * p.H + head) * kD + lane * 4;
-        const uint32_t w0 = pack_bf16(acc.x * inv, acc.y * inv), w1 = pack_bf16(acc.z * inv, acc.w * inv);
+#pragma unroll
+        for (int x = 0; x < kRowsEach; ++x) {
+            const float m_new = fmaxf(m[x], ml[x].x), m_use = m_new == -INFINITY ? 0.0f : m_new;
+            const float f = ex2_approx(m[x] - m_use), g = ex2_approx(ml[x].x - m_use);
+            m[x] = m_new;
+            total[x] = total[x] * f + ml[x].y * g;
+            acc[x].x = acc[x].x * f + o[x].x * g;
+            acc[x].y = acc[x].y * f + o[x].y * g;
+            acc[x].z = acc[x].z * f + o[x].z * g;
+            acc[x].w = acc[x].w * f + o[x].w * g;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < kRowsEach; ++x) {
+        if (r0 + x >= rows) break;
+        const float inv = total[x] == 0.0f ? 0.0f : 1.0f / total[x];
+        const int flat = item.z * kItemRows + r0 + x, i = flat / p.rep, head = item.w * p.rep + flat - i * p.rep;
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)item.y * p.queries + i) * p.H + head) * kD + lane * 4;
+        const uint32_t w0 = pack_bf16(acc[x].x * inv, acc[x].y * inv), w1 = pack_bf16(acc[x].z * inv, acc[x].w * inv);
         if (p.wide) *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
         else {
             dst[0] = __ushort_as_bfloat16((unsigned short)(w0 & 0xffffu));
@@ -629,22 +817,53 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
 std::mutex g_setup_mutex;
 DeviceSetup g_setup[kMaxDevices];
 
+// Rows per key head from which on unpacking ahead pays for itself.
+constexpr int kUnpackRows = 512;
+
+int launch_tc_attend(bool unpacked, const CacheAttendArgs& a, int grid, cudaStream_t st)
+{
+    const cudaError_t e = unpacked ? launch_kernel(tc_cache_attend_kernel<true>, dim3((unsigned)grid), Roles<true>::kThreads, kSmemBytes, st, a)
+                                   : launch_kernel(tc_cache_attend_kernel<false>, dim3((unsigned)grid), Roles<false>::kThreads, kSmemBytes, st, a);
+    if (e != cudaSuccess) { set_error("launch of tc_cache_attend_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    return 1;
+}
+
 }  // namespace
 
 int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
 {
     int num_sms = 0;
-    if (int r = device_setup_once(g_setup_mutex, g_setup, [] { return opt_in_smem(tc_cache_attend_kernel, kSmemBytes); }, &num_sms)) return r;
+    if (int r = device_setup_once(g_setup_mutex, g_setup, [] {
+            const cudaError_t e = opt_in_smem(tc_cache_attend_kernel<true>, kSmemBytes);
+            return e == cudaSuccess ? opt_in_smem(tc_cache_attend_kernel<false>, kSmemBytes) : e;
+        }, &num_sms)) return r;
     a.row_blocks = (a.queries * a.rep + kItemRows - 1) / kItemRows;
     a.min_share = 4;
-    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * ((((long long)a.c.max_pages << a.c.page_shift) + kTile - 1) / kTile);
+    const long long tiles = (((long long)a.c.max_pages << a.c.page_shift) + kTile - 1) / kTile;   // of a stream and head, at most
+    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * tiles;
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;
     if (grid > most) grid = most;
-    cudaError_t e = launch_kernel(tc_cache_attend_kernel, dim3((unsigned)grid), kThreads, kSmemBytes, st, a);
-    if (e != cudaSuccess) { set_error("launch of tc_cache_attend_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
-    e = launch_kernel(cache_join_kernel, dim3((unsigned)grid * kJoinBlocks), kJoinThreads, 0, st, a, (int)grid);
+    const bool ahead = a.queries * a.rep >= kUnpackRows && a.unpack_pairs > 0 && a.s_B <= kUnpackStreams;
+    const long long pairs = (long long)a.s_B * a.c.kv_heads * tiles;
+    // where the workspace may be too small for the lengths, which only the device knows, both kernels go out, and one returns at once
+    a.either = ahead && pairs > a.unpack_pairs;
+    int launched = 0;
+    if (ahead) {
+        const long long ctas = pairs < num_sms * 4 ? pairs : num_sms * 4;
+        const cudaError_t e = launch_kernel(cache_unpack_kernel, dim3((unsigned)ctas), kUnpackThreads, 0, st, a);
+        if (e != cudaSuccess) { set_error("launch of cache_unpack_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+        const int r = launch_tc_attend(true, a, (int)grid, st);
+        if (r < 0) return r;
+        launched += 1 + r;
+    }
+    if (!ahead || a.either) {
+        const int r = launch_tc_attend(false, a, (int)grid, st);
+        if (r < 0) return r;
+        launched += r;
+    }
+    const cudaError_t e = launch_kernel(cache_join_kernel, dim3((unsigned)grid * kJoinBlocks), kJoinThreads, 0, st, a);
     if (e != cudaSuccess) { set_error("launch of cache_join_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
-    return 2;
+    return launched + 1;
 }
 
 }  // namespace arl2
