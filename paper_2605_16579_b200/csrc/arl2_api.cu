@@ -1094,7 +1094,7 @@ namespace {
 
 // Scratch of a cache: tickets of the items that several CTAs share, their rows' statistics, their rows
 struct CacheLayout {
-    size_t tickets, part_items, part_ml, part_o, marks, unpacked, total;
+    size_t tickets, part_items, part_ml, part_o, marks, q_scale, unpacked, total;
     int unpack_pairs;
 };
 CacheLayout cache_layout(const arl2_config& cfg, const arl2_cache_config& c)
@@ -1106,10 +1106,12 @@ CacheLayout cache_layout(const arl2_config& cfg, const arl2_cache_config& c)
     l.part_items = off; off += align_up((size_t)kCacheTcCtas * sizeof(int4));
     l.part_ml = off; off += align_up((size_t)kCachePartRows * 2 * sizeof(float));
     l.part_o = off;  off += align_up((size_t)kCachePartRows * D * sizeof(float));
-    // operand tiles of all the keys that there may be, or of as many as that is worth
-    const int64_t tiles = ((int64_t)c.max_pages * c.page_tokens + 127) / 128 * c.kv_heads * cfg.B;
-    l.unpack_pairs = !tc_supported(cfg) ? 0 : (int)(tiles < kUnpackMost ? tiles : kUnpackMost);
+    // operand tiles of all the keys that there may be and of a block of queries, or of as many as that is worth
+    const int64_t rows = (int64_t)cfg.L * (cfg.H / c.kv_heads);
+    const int64_t pairs = (((int64_t)c.max_pages * c.page_tokens + 127) / 128 + (rows + 255) / 256) * c.kv_heads * cfg.B;
+    l.unpack_pairs = !tc_supported(cfg) ? 0 : (int)(pairs < kUnpackMost ? pairs : kUnpackMost);
     l.marks = off;    off += align_up((size_t)l.unpack_pairs * kUnpackMarks * sizeof(uint32_t));
+    l.q_scale = off;  off += align_up((size_t)l.unpack_pairs * 256 * sizeof(float));
     l.unpacked = off; off += (size_t)l.unpack_pairs * kUnpackPair;
     l.total = off;
     return l;
@@ -1170,6 +1172,7 @@ struct arl2_cache {
     int4* part_items;
     uint8_t* unpacked;
     uint32_t* unpack_marks;
+    float* q_scale;
     int unpack_pairs;
 };
 
@@ -1233,6 +1236,7 @@ int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d
     c->part_o = reinterpret_cast<float*>(ws + lay.part_o);
     c->unpacked = ws + lay.unpacked;
     c->unpack_marks = reinterpret_cast<uint32_t*>(ws + lay.marks);
+    c->q_scale = reinterpret_cast<float*>(ws + lay.q_scale);
     c->unpack_pairs = lay.unpack_pairs;
     const int r = account(ctx, fill_zero(c->tickets, kCacheCtas * sizeof(uint32_t), as_stream(stream)));
     if (r != ARL2_OK) { delete c; return r; }
@@ -1306,7 +1310,7 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
     a.out = d_out;
     a.part_o = cache->part_o; a.part_ml = cache->part_ml; a.tickets = cache->tickets;
     a.part_items = cache->part_items;
-    a.unpacked = cache->unpacked; a.unpack_marks = cache->unpack_marks; a.unpack_pairs = cache->unpack_pairs;
+    a.unpacked = cache->unpacked; a.unpack_marks = cache->unpack_marks; a.unpack_pairs = cache->unpack_pairs; a.q_scale = cache->q_scale;
     a.tensor_cores = cache->ctx->use_tc;
     a.wide = rows_are_wide(d_q, q_batch_stride, q_token_stride, elem) && rows_are_wide(d_out, 0, 0, 1);
     a.wait_limit = cache->ctx->wait_limit;

@@ -325,7 +325,7 @@ struct RowsConfig {
 };
 
 template <int D, typename IO, int kTiles>
-__global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAttendArgs p)
+__global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_constant__ CacheAttendArgs p)
 {
     constexpr bool kSplit = sizeof(IO) == 4;
     using C = RowsConfig<D, kTiles, kSplit>;
@@ -341,15 +341,16 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
     float* row_scale = reinterpret_cast<float*>(smem + C::kInfo);   // [row]
     float* row_sum = row_scale + kRows;                        // [row][group]
     int* row_seen = reinterpret_cast<int*>(row_sum + kRows * G);    // [row]
-    __shared__ long long scratch[kWarps + 3];
+    __shared__ long long scratch[kWarps + 4];
+    __shared__ Streams streams;
+    __shared__ Cut slow;
     __shared__ int last_part;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const int page_tokens = 1 << p.c.page_shift;
     grid_dependency_sync();
-    const Cut cut = cut_work<kRows, kChunk, kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
-    if (cut.begin >= cut.end) return;
-    Walk<kRows, kChunk, false> walk{locate<kRows, kChunk, kThreads>(p, cut.begin, scratch), cut.begin, cut.end};
+    const Cut cut = Planner<kRows, kChunk, false, kThreads>::cut(p, streams, (int)blockIdx.x, (int)gridDim.x, scratch, &slow);
+    Walk<kRows, kChunk, false> walk(streams, cut, (int)blockIdx.x, (int)gridDim.x, true);
 
     Segment seg;
     while (walk.next(p, seg)) {
@@ -722,7 +723,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const CacheAtten
             }
         }
         __syncthreads();
-        const Parts parts = item_parts(cut.share, seg.at.item_begin, seg.chunks);
+        const Parts parts = item_parts(cut, seg);
         auto write_row = [&](int r, int ch, float value) {
             const int flat = rb * kRows + r, i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
             static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + head) * D + ch] = static_cast<IO>(value);

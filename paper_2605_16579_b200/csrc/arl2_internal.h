@@ -215,11 +215,12 @@ constexpr int kCacheCtas = 4 * 148;        // most CTAs of the warp-level kernel
 constexpr int kCacheTcCtas = 148;          // most CTAs of the tcgen05 kernel, of 256 rows
 constexpr int kCachePartRows = 2 * kCacheTcCtas * 256;
 static_assert(2 * kCacheCtas * 32 <= kCachePartRows, "the partial rows of both kernels have the same room");
-// ... and for keys and values of the tcgen05 kernel turned into operand tiles ahead of it: a K and a V tile of 128 keys of a head
+// ... and for the operands of the tcgen05 kernel, made ahead of it: 64 KB are a K and a V tile of 128 keys of a head (from the front),
+// or the Q tiles of 256 query rows of a key head (from the back)
 constexpr size_t kUnpackPair = 2 * 128 * 128 * 2;
 constexpr int kUnpackMost = 4096;          // pairs at most (256 MB)
-constexpr int kUnpackMarks = 16;           // words beside a pair: what is special about its keys
-constexpr int kUnpackStreams = 128;        // most streams
+constexpr int kUnpackMarks = 16;           // words beside a pair of K and V: what is special about its keys
+constexpr int kUnpackStreams = 64;         // most streams
 struct CacheAttendArgs {
     CacheView c;
     int s_B, H, D, queries;
@@ -239,6 +240,7 @@ struct CacheAttendArgs {
     int4* part_items;        // [kCacheTcCtas] the item that a CTA of the tcgen05 kernel began and others went on with: parts, stream, block of rows, key head
     uint8_t* unpacked = nullptr;       // [unpack_pairs] pairs of operand tiles, and
     uint32_t* unpack_marks = nullptr;  // [unpack_pairs, kUnpackMarks]
+    float* q_scale = nullptr;          // [unpack_pairs, 256] factors of the rows' scores
     int unpack_pairs = 0;
     int either = 0;          // the lengths decide whether the tiles are unpacked ahead (set by the launcher)
     bool wide;               // as in CacheAppendArgs, for q and out

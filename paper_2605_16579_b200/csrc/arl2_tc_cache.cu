@@ -2,15 +2,15 @@
 //
 // One CTA per SM.  An item is two 128-row tiles of query rows of one key head against the keys that they see; the items' key
 // tiles of 128 form one sequence that is cut evenly over the CTAs (cache_common.cuh).  Roles:
-//   warps 0-3 / 4-7   softmax group of tile 0 / 1, one thread per query row.  It also writes its tile's Q operand: rows rotated in
-//                     fp32, scaled by a power of two into fp16's range, rounded to fp16 once.
+//   warps 0-3 / 4-7   softmax group of tile 0 / 1, one thread per query row
 //   two warps         MMA issuer of tile 0 / 1:  S_t = Q_t K_j^T and O_t += P_t V_j into TMEM
-//   K and V           into a ring of 32 KB operand tiles of minimum + step * code in fp16 (in which the codes are exact; its rounding,
-//                     2^-12, is an eighth of bf16's), in one of two ways:
-//     unpacked ahead  cache_unpack_kernel writes the operand tiles of all keys to the workspace, as they stand in shared memory,
-//                     and one thread copies them in.  Costs 512 bytes per key and head written and read again, once per call.
-//     on the way      four warps read codes and parameters, one tile ahead, and write the operand tiles themselves: no workspace, but
-//                     every item converts its keys anew, beside two softmax groups that want the same issue slots.
+// The operands are tiles of 32 KB: Q's rows, rotated in fp32, scaled by a power of two into fp16's range and rounded to fp16; K and V
+// as minimum + step * code in fp16 (in which the codes are exact; its rounding, 2^-12, is an eighth of bf16's), through a ring.  They
+// are made in one of two ways:
+//     ahead       cache_unpack_kernel writes all of them to the workspace, as they stand in shared memory, and one thread copies them
+//                 in.  Costs 512 bytes per key and head written and read again, once per call.
+//     on the way  four warps read codes and parameters, one tile ahead, and write the tiles of K and V, the softmax groups those of Q:
+//                 less to move, but every item converts its keys anew, beside two softmax groups that want the same issue slots.
 // TMEM (512 columns): S_0 | S_1 | O_0 | O_1, the fp16 probabilities over the first 64 columns of S_t.
 // The codes i and i + 4 of a 32-bit word come out of it as a pair, so that operand columns stand in the order 0 4 1 5 2 6 3 7 in every
 // eight: the Q operand is written in the same order, and the output's columns are put back in order when they are read.
@@ -52,10 +52,11 @@ constexpr int kOffMarks = kOffBars + 256;   // [kSpecials][kMarkWords]
 constexpr int kMarkWords = 9;               // whether a value is not finite; the keys of those, per group [2][4]
 static_assert(kMarkWords <= kUnpackMarks, "marks");
 constexpr int kSmemBytes = kOffMarks + kSpecials * kMarkWords * 4 + 1024;   // + alignment slack
-static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 20 * 8 <= 227 * 1024, "shared memory, with what the kernel declares itself");
+static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 20 * 8 + (int)sizeof(Streams) + (int)sizeof(Cut) <= 227 * 1024, "shared memory, with what the kernel declares itself");
 
 enum Bar : int {
-    kBarQ0 = 0, kBarQ1,                         // softmax group t -> issuer t: the Q operand is written
+    kBarQ0 = 0, kBarQ1,                         // -> issuer t: its Q tile is there
+    kBarQFree0, kBarQFree1,                     // issuer t -> copying thread: it has been read
     kBarFull0,                                  // kStages of them
     kBarEmpty0 = kBarFull0 + kStages,           // kStages of them
     kBarS0 = kBarEmpty0 + kStages, kBarS1,
@@ -96,6 +97,7 @@ __host__ __device__ constexpr int column_of(int channel) { return (channel & ~7)
 using ItemWalk = Walk<kItemRows, kTile, true>;
 
 // Operand tiles unpacked ahead: pair (first[b] + j) * kv_heads + h holds K and V of key tile j.  All threads of the CTA.
+// Block rb of query rows of head h: pair unpack_pairs - 1 - ((b * kv_heads + h) * row_blocks + rb).
 // Whether all of them have room; `first`: kUnpackStreams + 1 words of shared memory.
 __device__ __forceinline__ bool place_tiles(const CacheAttendArgs& p, int* first)
 {
@@ -118,7 +120,11 @@ __device__ __forceinline__ bool place_tiles(const CacheAttendArgs& p, int* first
         if (threadIdx.x == 0) first[p.s_B] = before;
     }
     __syncthreads();
-    return (long long)first[p.s_B] * p.c.kv_heads <= p.unpack_pairs;
+    return ((long long)first[p.s_B] + (long long)p.s_B * p.row_blocks) * p.c.kv_heads <= p.unpack_pairs;
+}
+__device__ __forceinline__ size_t q_pair(const CacheAttendArgs& p, const Place& at)
+{
+    return (size_t)p.unpack_pairs - 1 - (((size_t)at.b * p.c.kv_heads + at.h) * p.row_blocks + at.rb);
 }
 
 __device__ __forceinline__ bool not_finite(uint32_t params) { return (params & 0x7c00u) == 0x7c00u || (params & 0x7c000000u) == 0x7c000000u; }
@@ -138,6 +144,91 @@ __device__ __forceinline__ uint4 hold_word(uint32_t codes, __half2 low, __half2 
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// ---- the Q operand of kWarpRows rows, from row `row0` of block rb of (b, h) on: rotated in fp32, scaled by a power of two into fp16's
+// range, rounded to fp16.  `first`: the position of the stream's first query, rows: the block's.  A row at a time by the whole warp,
+// kBatch rows' loads in flight.  Lane l gets the factor of row l's scores.
+template <int kWarpRows, int kBatch>
+__device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb, int h, int first, int rows, uint8_t* tile, int row0, int lane)
+{
+    int own_e2 = 0;
+    bool own_finite = true;
+    // lane l: where row l's channels are, and its row of the rotary tables
+    const int own_flat = rb * kItemRows + min(row0 + (lane & (kWarpRows - 1)), rows - 1);
+    const int own_i = own_flat / p.rep, own_head = h * p.rep + own_flat - own_i * p.rep;
+    const __nv_bfloat16* own_src = static_cast<const __nv_bfloat16*>(p.q) + b * p.q_batch + own_i * p.q_token + (size_t)own_head * kD;
+    long long own_at = max((long long)first + own_i, 0LL);
+    if (p.c.rope_cos != nullptr && own_at >= p.c.rope_rows) {
+        range_error(p.c.status, kRangePosition, b);
+        own_at = p.c.rope_rows - 1;
+    }
+#pragma unroll 1
+    for (int r0 = 0; r0 < kWarpRows; r0 += kBatch) {
+        // (no branch and nothing that is written among the loads: they would wait for one another)
+        float x[kBatch][4];
+        float2 cs[kBatch], sn[kBatch];
+        if (p.wide) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own_src), r0 + k));
+                const uint2 v = reinterpret_cast<const uint2*>(src)[lane];
+                x[k][0] = __uint_as_float(v.x << 16);
+                x[k][1] = __uint_as_float(v.x & 0xFFFF0000u);
+                x[k][2] = __uint_as_float(v.y << 16);
+                x[k][3] = __uint_as_float(v.y & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own_src), r0 + k));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[k][e] = __bfloat162float(src[lane * 4 + e]);
+            }
+        }
+        if (p.c.rope_cos != nullptr) {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int at = __shfl_sync(0xffffffffu, (int)own_at, r0 + k);
+                cs[k] = reinterpret_cast<const float2*>(p.c.rope_cos + (size_t)at * (kD / 2))[lane];
+                sn[k] = reinterpret_cast<const float2*>(p.c.rope_sin + (size_t)at * (kD / 2))[lane];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                cs[k] = make_float2(1.0f, 1.0f);
+                sn[k] = make_float2(0.0f, 0.0f);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const float a0 = x[k][0] * cs[k].x - x[k][1] * sn[k].x, a1 = x[k][0] * sn[k].x + x[k][1] * cs[k].x;
+            const float a2 = x[k][2] * cs[k].y - x[k][3] * sn[k].y, a3 = x[k][2] * sn[k].y + x[k][3] * cs[k].y;
+            // (as whole numbers the magnitudes are in the same order, infinities and NaN above all others)
+            uint32_t most = max(max(__float_as_uint(a0) & 0x7fffffffu, __float_as_uint(a1) & 0x7fffffffu),
+                                max(__float_as_uint(a2) & 0x7fffffffu, __float_as_uint(a3) & 0x7fffffffu));
+            most = __reduce_max_sync(0xffffffffu, most);
+            // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
+            const bool finite = most < 0x7f800000u;
+            const int e2 = most == 0 ? 0 : min(137 - (int)(most >> 23), 126);
+            const float up = __uint_as_float((uint32_t)(127 + (e2 >> 1)) << 23), up2 = __uint_as_float((uint32_t)(127 + e2 - (e2 >> 1)) << 23);
+            if (lane == r0 + k) {
+                own_e2 = e2;
+                own_finite = finite;
+            }
+            const bool zero = !finite || row0 + r0 + k >= rows;
+            const uint32_t w0 = zero ? 0u : pack_f16(a0 * up * up2, a1 * up * up2), w1 = zero ? 0u : pack_f16(a2 * up * up2, a3 * up * up2);
+            // channels 8 c + 0 .. 3 are in even lanes, 4 .. 7 in odd ones; columns hold 0 4 1 5 | 2 6 3 7: an even lane writes the first four
+            const uint32_t give = (lane & 1) ? w0 : w1, got = __shfl_xor_sync(0xffffffffu, give, 1);
+            const uint32_t lo = (lane & 1) ? got : w0, hi = (lane & 1) ? w1 : got;     // channels m, m + 1 and m + 4, m + 5
+            const int row = (row0 & (kTile - 1)) + r0 + k, c = lane >> 1;
+            *reinterpret_cast<uint2*>(tile + (c >> 3) * kHalfBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4) + (lane & 1) * 8) =
+                make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+        }
+    }
+    // (both factors have exponents that a float has)
+    const float down = __uint_as_float((uint32_t)(127 - (own_e2 >> 1)) << 23), down2 = __uint_as_float((uint32_t)(127 - own_e2 + (own_e2 >> 1)) << 23);
+    return own_finite ? p.scale_log2 * down * down2 : __int_as_float(0x7fc00000);
+}
+
 // ---- one thread per query row.  marks: what is special about the key tiles, in shared memory by key tiles so far, or
 // beside the tiles unpacked ahead (first: place_tiles)
 template <bool kUnpacked>
@@ -151,6 +242,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
     uint32_t s_cnt = 0, o_cnt = 0, tile_cnt = 0;   // phases consumed; key tiles so far, whichever group has work in them
     uint32_t sreg[128];
     int4 begun = make_int4(0, 0, 0, 0);     // the item that this CTA began and others went on with
+    if constexpr (kUnpacked) grid_dependency_wait();
 
     Segment seg;
     while (walk.next(p, seg)) {
@@ -162,70 +254,12 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         const int i = flat / p.rep, head = seg.at.h * p.rep + flat - i * p.rep;
         const long long pos = (long long)seg.first + i;
         const int sees = !p.causal ? seg.have : (int)max(0LL, min((long long)seg.have, pos + 1));
-
-        // ---- the row of Q: rotated, scaled, rounded to fp16.  (Every MMA that read the item before's has ended: its last
-        // scores have been here.)
-        float c2 = p.scale_log2;
-        {
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + seg.at.b * p.q_batch + i * p.q_token + (size_t)head * kD;
-            if (p.wide) {
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const uint4 v = reinterpret_cast<const uint4*>(src)[c];
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        sreg[c * 8 + 2 * m] = w[m] << 16;
-                        sreg[c * 8 + 2 * m + 1] = w[m] & 0xFFFF0000u;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < kD; ++c) sreg[c] = __float_as_uint(__bfloat162float(src[c]));
-            }
-            if (p.c.rope_cos != nullptr) {
-                long long at = max(pos, 0LL);
-                if (at >= p.c.rope_rows) {
-                    if (valid) range_error(p.c.status, kRangePosition, seg.at.b);
-                    at = p.c.rope_rows - 1;
-                }
-                const float4* cos4 = reinterpret_cast<const float4*>(p.c.rope_cos + at * (kD / 2));
-                const float4* sin4 = reinterpret_cast<const float4*>(p.c.rope_sin + at * (kD / 2));
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    const float4 c4 = cos4[c], s4 = sin4[c];
-                    const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const float a = __uint_as_float(sreg[c * 8 + 2 * m]), b = __uint_as_float(sreg[c * 8 + 2 * m + 1]);
-                        sreg[c * 8 + 2 * m] = __float_as_uint(a * cs[m] - b * sn[m]);
-                        sreg[c * 8 + 2 * m + 1] = __float_as_uint(a * sn[m] + b * cs[m]);
-                    }
-                }
-            }
-            float most = 0.0f;
-            bool finite = true;
-#pragma unroll
-            for (int c = 0; c < kD; ++c) {
-                const float a = fabsf(__uint_as_float(sreg[c]));
-                finite = finite && a <= 3.402823466e38f;
-                most = fmaxf(most, a);
-            }
-            // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
-            int e2 = 0;
-            if (most > 0.0f && finite) e2 = min(10 - ilogbf(most), 126);
-            const float up = finite ? scalbnf(1.0f, e2 >> 1) : 0.0f, up2 = scalbnf(1.0f, e2 - (e2 >> 1));
-            c2 = finite ? p.scale_log2 / up / up2 : __int_as_float(0x7fc00000);
-            const bool zero = !valid || !finite;
-            uint8_t* tile = smem + kOffQ + t * kTileBytes;
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-                uint32_t w[4];
-#pragma unroll
-                for (int m = 0; m < 4; ++m)     // columns 2 m and 2 m + 1: channels m and m + 4
-                    w[m] = zero ? 0u : pack_f16(__uint_as_float(sreg[c * 8 + m]) * up * up2, __uint_as_float(sreg[c * 8 + m + 4]) * up * up2);
-                *reinterpret_cast<uint4*>(tile + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+        float c2;
+        if constexpr (kUnpacked) {
+            c2 = p.q_scale[q_pair(p, seg.at) * kItemRows + in_item];
+        } else {
+            // (Every MMA that read the item before's Q has ended: its last scores have been here.)
+            c2 = write_q<32, 8>(p, seg.at.b, seg.at.rb, seg.at.h, seg.first, seg.rows, smem + kOffQ + t * kTileBytes, t * kTile + warp_in_group * 32, r & 31);
             fence_proxy_async_smem();
             mbar_arrive(bars + 8 * (kBarQ0 + t));
         }
@@ -320,7 +354,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         tc_fence_after();
         if (p.causal && seg.seen > 0) poison_of(n - 1);
         tile_cnt += n;
-        const Parts parts = item_parts(cut.share, seg.at.item_begin - cut.base, seg.chunks);
+        const Parts parts = item_parts(cut, seg);
         if (parts.count > 1 && parts.first == (int)blockIdx.x) begun = make_int4(parts.count, seg.at.b, seg.at.rb, seg.at.h);
         const float nan = __int_as_float(0x7fc00000);
         if (parts.count > 1) {
@@ -483,37 +517,51 @@ __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* sme
     }
 }
 
-// ---- one thread that copies the tiles unpacked ahead.  Returns the ring entries that it has sent for.
-__device__ __forceinline__ uint32_t copy_role(const CacheAttendArgs& p, uint32_t smem_base, uint32_t bars, const Abort& ab, const int* first, ItemWalk walk)
+// ---- one thread that copies the tiles made ahead, and waits for what it has sent for
+__device__ __forceinline__ void copy_role(const CacheAttendArgs& p, uint32_t smem_base, uint32_t bars, const Abort& ab, const int* first, ItemWalk walk)
 {
-    uint32_t n = 0;
+    uint32_t n = 0, q_cnt[2] = {0, 0};      // ring entries and Q tiles so far
+    bool ok = true;
     Segment seg;
-    while (walk.next(p, seg)) {
+    while (ok && walk.next(p, seg)) {
         if (seg.opens) (void)stream_tokens(p, seg.at.b, true);
-        // (an item without keys has one tile of which every score is masked: any tile will do, and there need not be one)
+        const uint8_t* q = p.unpacked + q_pair(p, seg.at) * kUnpackPair;
+        for (int t = 0; t < 2 && ok && t * kTile < seg.rows; ++t) {
+            if (q_cnt[t] > 0) ok = wait_bar(bars + 8 * (kBarQFree0 + t), (q_cnt[t] - 1) & 1, ab, 152 + t);
+            if (!ok) break;
+            const uint32_t bar = bars + 8 * (kBarQ0 + t);
+            mbar_expect_tx(bar, kTileBytes);
+            bulk_load(smem_base + kOffQ + t * kTileBytes, q + t * kTileBytes, kTileBytes, bar);
+            ++q_cnt[t];
+        }
+        // (an item without keys has one tile, of which every score is masked)
         const bool none = seg.seen == 0;
-        const uint8_t* src = p.unpacked + ((size_t)(first[seg.at.b] + (none ? 0 : seg.c0)) * p.c.kv_heads + seg.at.h) * kUnpackPair;
+        const uint8_t* src = p.unpacked + ((size_t)(first[seg.at.b] + seg.c0) * p.c.kv_heads + seg.at.h) * kUnpackPair;
         const size_t step = (size_t)p.c.kv_heads * kUnpackPair;
-        for (int e = 0; e < 2 * (seg.c1 - seg.c0); ++e, ++n) {
+        for (int e = 0; e < 2 * (seg.c1 - seg.c0) && ok; ++e) {
             const uint32_t slot = n % kStages;
-            const bool ok = n < (uint32_t)kStages || wait_bar(bars + 8 * (kBarEmpty0 + slot), ((n / kStages) - 1) & 1, ab, 150);
-            if (!ok) return n;
-            const uint32_t bar = bars + 8 * (kBarFull0 + slot);
+            if (n >= (uint32_t)kStages) ok = wait_bar(bars + 8 * (kBarEmpty0 + slot), ((n / kStages) - 1) & 1, ab, 150);
+            if (!ok) break;
+            const uint32_t bar = bars + 8 * (kBarFull0 + slot), dst = smem_base + kOffRing + slot * kTileBytes;
             if (none) {
-                for (int i = 0; i < kTileBytes / 16; ++i) st_shared_zero(smem_base + kOffRing + slot * kTileBytes + i * 16);
+                for (int i = 0; i < kTileBytes / 16; ++i) st_shared_zero(dst + i * 16);
                 fence_proxy_async_smem();
                 mbar_arrive(bar);
             } else {
                 mbar_expect_tx(bar, kTileBytes);
-                bulk_load(smem_base + kOffRing + slot * kTileBytes, src + (size_t)(e >> 1) * step + (e & 1) * kTileBytes, kTileBytes, bar);
+                bulk_load(dst, src + (size_t)(e >> 1) * step + (e & 1) * kTileBytes, kTileBytes, bar);
             }
+            ++n;
         }
     }
-    return n;
+    // copies into this CTA's shared memory are waited for, whatever became of the waits
+    for (int t = 0; t < 2; ++t)
+        if (q_cnt[t] > 0) drain_bar(bars + 8 * (kBarQ0 + t), (q_cnt[t] - 1) & 1);
+    for (uint32_t m = (n > (uint32_t)kStages ? n - kStages : 0); m < n; ++m) drain_bar(bars + 8 * (kBarFull0 + m % kStages), (m / kStages) & 1);
 }
 
 template <bool kUnpacked>
-__global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend_kernel(const CacheAttendArgs p)
+__global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend_kernel(const __grid_constant__ CacheAttendArgs p)
 {
     using R = Roles<kUnpacked>;
     extern __shared__ uint8_t smem_raw[];
@@ -524,12 +572,16 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kOffMarks);
     const Abort ab{abort_flag, p.c.status, p.wait_limit ? p.wait_limit - 1 : kSpinLimit};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    __shared__ long long scratch[R::kThreads / 32 + 3];
+    __shared__ long long scratch[R::kThreads / 32 + 4];
+    __shared__ Streams streams;
+    __shared__ Cut slow;
     __shared__ int first[kUnpackStreams + 1];
 
     if (tid == 0) {
-        mbar_init(bars + 8 * kBarQ0, 128);
-        mbar_init(bars + 8 * kBarQ1, 128);
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(bars + 8 * (kBarQ0 + t), kUnpacked ? 1 : 128);     // the copying thread, or the softmax group
+            mbar_init(bars + 8 * (kBarQFree0 + t), 1);
+        }
         for (int s = 0; s < kStages; ++s) {
             mbar_init(bars + 8 * (kBarFull0 + s), kUnpacked ? 1 : 2);    // the copying thread, or the two warps that write a tile
             mbar_init(bars + 8 * (kBarEmpty0 + s), 2);                   // both issuers
@@ -555,7 +607,8 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    grid_dependency_sync();
+    // After the unpacking kernel, which waited for all before it, the cut of the work runs beside its end.
+    if constexpr (!kUnpacked) grid_dependency_sync();
 
     // Where the lengths decide on the way, the other kernel is there, too.
     bool mine = true;
@@ -563,9 +616,8 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
         const bool room = place_tiles(p, first);
         mine = !p.either || room == kUnpacked;
     }
-    const Cut cut = cut_whole_first<kItemRows, kTile, R::kThreads>(p, (int)blockIdx.x, (int)gridDim.x, scratch);
-    ItemWalk walk{{0, 0, 0, 0}, cut.begin, mine ? cut.end : cut.begin, mine ? cut.whole : 0, (int)blockIdx.x, (int)gridDim.x};
-    if (cut.begin < cut.end) walk.place = locate_by_head<kItemRows, kTile, R::kThreads>(p, cut.begin, scratch);
+    const Cut cut = Planner<kItemRows, kTile, true, R::kThreads>::cut(p, streams, (int)blockIdx.x, (int)gridDim.x, scratch, &slow);
+    ItemWalk walk(streams, cut, (int)blockIdx.x, (int)gridDim.x, mine);
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kRegsSoftmax));
@@ -580,9 +632,8 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsOther));
         if (warp == 8 && lane == 0) {
-            const uint32_t n = copy_role(p, smem_u32(smem), bars, ab, first, walk);
-            // copies into this CTA's shared memory are waited for, whatever became of the waits
-            for (uint32_t m = (n > (uint32_t)kStages ? n - kStages : 0); m < n; ++m) drain_bar(bars + 8 * (kBarFull0 + m % kStages), (m / kStages) & 1);
+            grid_dependency_sync();
+            copy_role(p, smem_u32(smem), bars, ab, first, walk);
         }
     }
     if (warp == R::kIssuer || warp == R::kIssuer + 1) {
@@ -644,6 +695,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
             issue_qk(slot_addr(cons));
             mma_commit_if(lead, bar_s);
             release(cons, alone);
+            if (kUnpacked && n == 1) mma_commit_if(lead, bars + 8 * (kBarQFree0 + t));
             for (int j = 0; j < n; ++j) {
                 const uint32_t e_v = cons + 2 * j + 1, e_k = e_v + 1;
                 const bool last = j + 1 == n;
@@ -661,6 +713,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
                 if (!last) {
                     issue_qk(slot_addr(e_k));
                     mma_commit_if(lead, bar_s);
+                    if (kUnpacked && j + 2 == n) mma_commit_if(lead, bars + 8 * (kBarQFree0 + t));     // the last read of Q
                 } else {
                     mma_commit_if(lead, bars + 8 * (kBarO0 + t));
                 }
@@ -683,10 +736,11 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
     }
 }
 
-// ---- K and V of every key tile of every stream as operand tiles in the workspace, pair by pair.  Bound by writing them: 512 bytes
-// per key and head.  A thread takes 32 channels of a row at a time and writes them as two whole 32-byte sectors.
+// ---- the operand tiles of a call in the workspace: blocks of query rows, then K and V of every key tile of every stream, pair by pair.
+// Bound by writing them: 512 bytes per key and head.  A thread takes 32 channels of a cached row at a time and writes them as two
+// whole 32-byte sectors.
 constexpr int kUnpackThreads = 256;
-__global__ void __launch_bounds__(kUnpackThreads) cache_unpack_kernel(const CacheAttendArgs p)
+__global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const CacheAttendArgs p)
 {
     using U = Unit<kD>;
     __shared__ int first[kUnpackStreams + 1];
@@ -694,9 +748,24 @@ __global__ void __launch_bounds__(kUnpackThreads) cache_unpack_kernel(const Cach
     const int tid = threadIdx.x, quarter = tid & 3, page_tokens = 1 << p.c.page_shift;
     grid_dependency_sync();
     if (!place_tiles(p, first)) return;
-    const int pairs = first[p.s_B] * p.c.kv_heads;
+    const int pairs = first[p.s_B] * p.c.kv_heads, q_blocks = p.s_B * p.c.kv_heads * p.row_blocks;
+    int work = (int)blockIdx.x;
+    for (; work < q_blocks; work += (int)gridDim.x) {
+        const int bh = work / p.row_blocks;
+        Place at;
+        at.rb = work - bh * p.row_blocks;
+        at.b = bh / p.c.kv_heads;
+        at.h = bh - at.b * p.c.kv_heads;
+        const size_t pair = q_pair(p, at);
+        int have, position;
+        Streams::look_up(p, at.b, have, position);
+        const int row0 = (tid >> 5) * 32, lane = tid & 31;      // (8 warps of 32 rows)
+        const float scale = write_q<32, 4>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
+                                        p.unpacked + pair * kUnpackPair + (row0 / kTile) * kTileBytes, row0, lane);
+        p.q_scale[pair * kItemRows + row0 + lane] = scale;
+    }
     int b = 0;
-    for (int pair = (int)blockIdx.x; pair < pairs; pair += (int)gridDim.x) {
+    for (int pair = work - q_blocks; pair < pairs; pair += (int)gridDim.x) {
         const int at = pair / p.c.kv_heads, h = pair - at * p.c.kv_heads;
         while (first[b + 1] <= at) ++b;      // (pairs only grow)
         const int tile = at - first[b], have = stream_tokens(p, b, false);
@@ -844,7 +913,7 @@ int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;
     if (grid > most) grid = most;
     const bool ahead = a.queries * a.rep >= kUnpackRows && a.unpack_pairs > 0 && a.s_B <= kUnpackStreams;
-    const long long pairs = (long long)a.s_B * a.c.kv_heads * tiles;
+    const long long pairs = (long long)a.s_B * a.c.kv_heads * (tiles + a.row_blocks);
     // where the workspace may be too small for the lengths, which only the device knows, both kernels go out, and one returns at once
     a.either = ahead && pairs > a.unpack_pairs;
     int launched = 0;

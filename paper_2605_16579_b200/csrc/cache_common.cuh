@@ -37,11 +37,26 @@ __device__ __forceinline__ int stream_tokens(const CacheAttendArgs& p, int b, bo
     return max(0, min(have, most));
 }
 
-// position of the stream's first query (it may be negative: fewer tokens than queries)
-__device__ __forceinline__ int first_position(const CacheAttendArgs& p, int b, int have)
-{
-    return p.q_start != nullptr ? p.q_start[b] : have - p.queries;
-}
+// A CTA's own copy of what the streams' lengths say; streams past the copies are looked up.
+constexpr int kPlanStreams = 64;
+struct Streams {
+    int have[kPlanStreams];     // tokens that there are
+    int first[kPlanStreams];    // position of the first query (it may be negative: fewer tokens than queries)
+    __device__ __forceinline__ void get(const CacheAttendArgs& p, int b, int& tokens, int& position) const
+    {
+        if (b < kPlanStreams) {
+            tokens = have[b];
+            position = first[b];
+        } else {
+            look_up(p, b, tokens, position);
+        }
+    }
+    static __device__ __forceinline__ void look_up(const CacheAttendArgs& p, int b, int& tokens, int& position)
+    {
+        tokens = stream_tokens(p, b, false);
+        position = p.q_start != nullptr ? p.q_start[b] : tokens - p.queries;
+    }
+};
 
 // The keys that the query rows [.., row_end) of a block of rows see between them.  Rows of a key head are ordered by
 // token, then by the query head among the H / kv_heads that share it.
@@ -56,165 +71,158 @@ __device__ __forceinline__ int keys_seen(const CacheAttendArgs& p, int have, int
 // Attention work is one sequence of key chunks: by stream, block of query rows, key head, and chunk (kByHead: by stream, key head,
 // block of query rows and chunk, so that CTAs side by side read the same keys).  Every CTA takes an equal
 // share of it, wherever that begins and ends; an item (one block of rows of one head) that more than one CTA works on is
-// joined from partial rows.  The cut follows from the lengths alone, so that results do not depend on timing.
+// joined from partial rows.  Where all items are alike and there are more of them than CTAs (kByHead), each CTA first does as many
+// as there are for all whole, side by side from the first key on, and only the rest is cut: CTAs that read the same keys then read
+// them at the same time, and few rows are exchanged.
+// The cut follows from the lengths alone, so that results do not depend on timing.
 struct Place {
     int b, rb, h;             // an item
     long long item_begin;     // its first chunk in the sequence
 };
 struct Cut {
-    long long share, total;   // chunks per CTA, and of all
+    long long share;          // chunks per CTA
     long long begin, end;     // this CTA's
-    long long base;           // chunks of the items that CTAs do whole, before the shares (cut_whole_first)
+    long long base;           // chunks of the items that CTAs do whole, which are the first
     int whole;                // such items per CTA
+    Place place;              // the item that holds `begin`, where begin < end
 };
 
-// Chunks of (stream, block of rows); never none, so that rows without keys are written too.
-template <int kRows, int kChunk>
-__device__ __forceinline__ int unit_chunks(const CacheAttendArgs& p, int unit)
-{
-    const int b = unit / p.row_blocks, rb = unit - b * p.row_blocks;
-    const int have = stream_tokens(p, b, false);
-    const int seen = keys_seen(p, have, first_position(p, b, have), (rb + 1) * kRows);
-    return max(1, (seen + kChunk - 1) / kChunk);
-}
+template <int kRows, int kChunk, bool kByHead, int kThreads>
+struct Planner {
+    static constexpr int kWarps = kThreads / 32;
 
-// The share of a CTA.  All threads of a CTA of kThreads; `scratch`: kThreads / 32 + 3 words of 64 bits of shared memory.
-template <int kRows, int kChunk, int kThreads>
-__device__ __forceinline__ Cut cut_work(const CacheAttendArgs& p, int cta, int ctas, long long* scratch)
-{
-    constexpr int kWarps = kThreads / 32;
-    const int units = p.s_B * p.row_blocks, tid = threadIdx.x;
-    long long mine = 0;
-    for (int u = tid; u < units; u += kThreads) mine += (long long)unit_chunks<kRows, kChunk>(p, u) * p.c.kv_heads;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-    if ((tid & 31) == 0) scratch[tid >> 5] = mine;
-    __syncthreads();
-    Cut c;
-    c.total = c.base = 0;
-    c.whole = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) c.total += scratch[w];
-    __syncthreads();
-    c.share = max((long long)p.min_share, (c.total + ctas - 1) / ctas);
-    c.begin = min(c.total, c.share * cta);
-    c.end = min(c.total, c.begin + c.share);
-    return c;
-}
+    // Chunks of (stream, block of rows); never none, so that rows without keys are written too.
+    static __device__ __forceinline__ int chunks_of(int seen) { return max(1, (seen + kChunk - 1) / kChunk); }
+    static __device__ __forceinline__ int unit_chunks(const CacheAttendArgs& p, const Streams& st, int b, int rb)
+    {
+        int have, first;
+        st.get(p, b, have, first);
+        return chunks_of(keys_seen(p, have, first, (rb + 1) * kRows));
+    }
 
-// Where all items are alike and there are more of them than CTAs, each CTA does as many as there are for all whole, side by side from
-// the first key on, and only the rest is cut: CTAs that read the same keys then read them at the same time, and few rows are exchanged.
-template <int kRows, int kChunk, int kThreads>
-__device__ __forceinline__ Cut cut_whole_first(const CacheAttendArgs& p, int cta, int ctas, long long* scratch)
-{
-    Cut c = cut_work<kRows, kChunk, kThreads>(p, cta, ctas, scratch);
-    const long long items = (long long)p.s_B * p.row_blocks * p.c.kv_heads;
-    const int each = unit_chunks<kRows, kChunk>(p, 0);
-    bool alike = !p.causal;
-    for (int b = threadIdx.x; b < p.s_B; b += kThreads) alike = alike && unit_chunks<kRows, kChunk>(p, b * p.row_blocks) == each;
-    if (!__syncthreads_and(alike) || items < ctas) return c;
-    c.whole = (int)(items / ctas);
-    c.base = (long long)c.whole * ctas * each;
-    c.share = max((long long)p.min_share, (c.total - c.base + ctas - 1) / ctas);
-    c.begin = min(c.total, c.base + c.share * cta);
-    c.end = min(c.total, c.begin + c.share);
-    return c;
-}
-
-// The item that holds chunk `at` (below the total).  All threads, as above.
-template <int kRows, int kChunk, int kThreads>
-__device__ __forceinline__ Place locate(const CacheAttendArgs& p, long long at, long long* scratch)
-{
-    constexpr int kWarps = kThreads / 32;
-    const int units = p.s_B * p.row_blocks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    long long* found = scratch + kWarps;   // unit, its first chunk, chunks per head
-    long long before = 0;
-    for (int u0 = 0; u0 < units && before <= at; u0 += kThreads) {
-        const int u = u0 + tid, each = u < units ? unit_chunks<kRows, kChunk>(p, u) : 0;
-        const long long size = (long long)each * p.c.kv_heads;
-        long long upto = size;
+    // Work of any shape: sums over the streams and blocks of rows.  All threads; `scratch`: kWarps + 4 words of shared memory.
+    // (A function of its own: what calls of one length, the usual ones, do not reach should not stand in their way.)
+    static __device__ __noinline__ void general(const CacheAttendArgs& p, const Streams& st, int cta, int ctas, long long* scratch, Cut* out)
+    {
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        // entities: (stream, block of rows), or streams, whose few blocks of rows a thread adds up by itself
+        const int entities = kByHead ? p.s_B : p.s_B * p.row_blocks;
+        auto size_of = [&](int e) {
+            if (!kByHead) return (long long)unit_chunks(p, st, e / p.row_blocks, e % p.row_blocks);
+            long long sum = 0;
+            for (int rb = 0; rb < p.row_blocks; ++rb) sum += unit_chunks(p, st, e, rb);
+            return sum;
+        };
+        long long mine = 0;
+        for (int e = tid; e < entities; e += kThreads) mine += size_of(e) * p.c.kv_heads;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += x;
-        }
-        if (lane == 31) scratch[warp] = upto;
+        for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+        if (lane == 0) scratch[warp] = mine;
         __syncthreads();
-        long long round = 0;
+        long long total = 0;
+        for (int w = 0; w < kWarps; ++w) total += scratch[w];
+        __syncthreads();
+        Cut c;
+        c.base = 0;
+        c.whole = 0;
+        c.share = max((long long)p.min_share, (total + ctas - 1) / ctas);
+        c.begin = min(total, c.share * cta);
+        c.end = min(total, c.begin + c.share);
+        c.place = Place{0, 0, 0, 0};
+        if (c.begin < c.end) {
+            long long* found = scratch + kWarps;   // entity, its first chunk, chunks per head
+            long long before = 0;
+            for (int e0 = 0; e0 < entities && before <= c.begin; e0 += kThreads) {
+                const int e = e0 + tid;
+                const long long each = e < entities ? size_of(e) : 0, size = each * p.c.kv_heads;
+                long long upto = size;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) upto += scratch[w];
-            round += scratch[w];
+                for (int d = 1; d < 32; d <<= 1) {
+                    const long long x = __shfl_up_sync(0xffffffffu, upto, d);
+                    if (lane >= d) upto += x;
+                }
+                if (lane == 31) scratch[warp] = upto;
+                __syncthreads();
+                long long round = 0;
+                for (int w = 0; w < kWarps; ++w) {
+                    if (w < warp) upto += scratch[w];
+                    round += scratch[w];
+                }
+                const long long from = before + upto - size;
+                if (e < entities && from <= c.begin && c.begin < from + size) {
+                    found[0] = e;
+                    found[1] = from;
+                    found[2] = each;
+                }
+                before += round;
+                __syncthreads();
+            }
+            const int e = (int)found[0];
+            c.place.h = (int)((c.begin - found[1]) / found[2]);
+            c.place.item_begin = found[1] + (long long)c.place.h * found[2];
+            if (kByHead) {
+                c.place.b = e;
+                for (c.place.rb = 0; c.place.rb + 1 < p.row_blocks; ++c.place.rb) {
+                    const int chunks = unit_chunks(p, st, e, c.place.rb);
+                    if (c.begin < c.place.item_begin + chunks) break;
+                    c.place.item_begin += chunks;
+                }
+            } else {
+                c.place.b = e / p.row_blocks;
+                c.place.rb = e - c.place.b * p.row_blocks;
+            }
         }
-        const long long from = before + upto - size;
-        if (u < units && from <= at && at < from + size) {
-            found[0] = u;
-            found[1] = from;
-            found[2] = each;
-        }
-        before += round;
+        if (tid == 0) *out = c;
         __syncthreads();
     }
-    const int u = (int)found[0];
-    Place q;
-    q.b = u / p.row_blocks;
-    q.rb = u - q.b * p.row_blocks;
-    q.h = (int)((at - found[1]) / found[2]);
-    q.item_begin = found[1] + (long long)q.h * found[2];
-    return q;
-}
 
-// The same where the sequence is ordered by head: few blocks of rows, which a thread adds up by itself.
-template <int kRows, int kChunk, int kThreads>
-__device__ __forceinline__ Place locate_by_head(const CacheAttendArgs& p, long long at, long long* scratch)
-{
-    constexpr int kWarps = kThreads / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    long long* found = scratch + kWarps;   // stream, its first chunk, chunks per head
-    long long before = 0;
-    for (int b0 = 0; b0 < p.s_B && before <= at; b0 += kThreads) {
-        const int b = b0 + tid;
-        long long each = 0;
-        if (b < p.s_B) {
-            if (!p.causal) each = (long long)unit_chunks<kRows, kChunk>(p, b * p.row_blocks) * p.row_blocks;
-            else
-                for (int rb = 0; rb < p.row_blocks; ++rb) each += unit_chunks<kRows, kChunk>(p, b * p.row_blocks + rb);
+    // This CTA's share.  All threads; st, scratch and `slow` in shared memory.
+    static __device__ __forceinline__ Cut cut(const CacheAttendArgs& p, Streams& st, int cta, int ctas, long long* scratch, Cut* slow)
+    {
+        // all streams alike: a few divisions (in 32 bits, where the chunks can be counted in them)
+        int have0, first0;
+        Streams::look_up(p, 0, have0, first0);
+        bool alike = !p.causal;
+        for (int b = threadIdx.x; b < p.s_B; b += kThreads) {
+            int have, first;
+            Streams::look_up(p, b, have, first);
+            if (b < kPlanStreams) {
+                st.have[b] = have;
+                st.first[b] = first;
+            }
+            alike = alike && have == have0;
         }
-        const long long size = each * p.c.kv_heads;
-        long long upto = size;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += x;
+        const int each = chunks_of(have0);
+        const long long all = (long long)p.s_B * p.row_blocks * p.c.kv_heads;
+        alike = alike && all * each < (1LL << 31) && (long long)p.min_share * ctas < (1LL << 31);
+        if (!__syncthreads_and(alike)) {
+            general(p, st, cta, ctas, scratch, slow);
+            return *slow;
         }
-        if (lane == 31) scratch[warp] = upto;
-        __syncthreads();
-        long long round = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) upto += scratch[w];
-            round += scratch[w];
-        }
-        const long long from = before + upto - size;
-        if (b < p.s_B && from <= at && at < from + size) {
-            found[0] = b;
-            found[1] = from;
-            found[2] = each;
-        }
-        before += round;
-        __syncthreads();
+        const uint32_t items = (uint32_t)all, total = items * (uint32_t)each;
+        Cut c;
+        c.whole = kByHead ? (int)(items / (uint32_t)ctas) : 0;
+        const uint32_t base = (uint32_t)c.whole * (uint32_t)ctas * (uint32_t)each;
+        const uint32_t share = max((uint32_t)p.min_share, (total - base + (uint32_t)ctas - 1) / (uint32_t)ctas);
+        const uint32_t begin = (uint32_t)min((long long)total, (long long)base + (long long)share * cta);
+        c.base = base;
+        c.share = share;
+        c.begin = begin;
+        c.end = min(total, begin + share);
+        const uint32_t item = begin / (uint32_t)each;
+        c.place = split(p, item);
+        c.place.item_begin = (long long)item * each;
+        return c;
     }
-    Place q;
-    q.b = (int)found[0];
-    q.h = (int)((at - found[1]) / found[2]);
-    q.item_begin = found[1] + (long long)q.h * found[2];
-    for (q.rb = 0; q.rb + 1 < p.row_blocks; ++q.rb) {
-        const int chunks = unit_chunks<kRows, kChunk>(p, q.b * p.row_blocks + q.rb);
-        if (at < q.item_begin + chunks) break;
-        q.item_begin += chunks;
+    // item number -> stream, block of rows, head
+    static __device__ __forceinline__ Place split(const CacheAttendArgs& p, uint32_t item)
+    {
+        const uint32_t inner = kByHead ? p.row_blocks : p.c.kv_heads, outer = kByHead ? p.c.kv_heads : p.row_blocks;
+        const uint32_t x = item / inner, y = x / outer;
+        const int in = (int)(item - x * inner), out = (int)(x - y * outer);
+        return Place{(int)y, kByHead ? in : out, kByHead ? out : in, 0};
     }
-    return q;
-}
+};
 
 // What a CTA does of one item: key chunks [c0, c1) of `chunks`.
 struct Segment {
@@ -225,31 +233,37 @@ struct Segment {
     int chunks, c0, c1;
     bool opens;               // the item's first chunk is among them
 };
-// A CTA's segments one after the other: its whole items (kByHead only), then its share from `place` on.
+// A CTA's segments one after the other: its whole items, then its share from `place` on.
 template <int kRows, int kChunk, bool kByHead>
 struct Walk {
+    using Plan = Planner<kRows, kChunk, kByHead, 32>;
+    const Streams* st;
     Place place;
     long long at, end;
-    int whole = 0, item = 0, ctas = 0;     // whole items to go, the next one, and the step to the one after
+    int whole, item, ctas;     // whole items to go, the next one, and the step to the one after
+    __device__ __forceinline__ Walk(const Streams& streams, const Cut& c, int cta, int of, bool any)
+        : st(&streams), place(c.place), at(c.begin), end(any ? c.end : c.begin), whole(any ? c.whole : 0), item(cta), ctas(of) {}
     __device__ __forceinline__ bool next(const CacheAttendArgs& p, Segment& s)
     {
-        if (kByHead && whole > 0) {
-            --whole;
-            const int bh = item / p.row_blocks;
-            s.at.rb = item - bh * p.row_blocks;
-            s.at.b = bh / p.c.kv_heads;
-            s.at.h = bh - s.at.b * p.c.kv_heads;
+        const bool entire = kByHead && whole > 0;
+        if (!entire && at >= end) return false;
+        s.at = place;
+        if (entire) {
+            s.at = Plan::split(p, (uint32_t)item);
             s.at.item_begin = -1;
+        }
+        st->get(p, s.at.b, s.have, s.first);
+        s.seen = keys_seen(p, s.have, s.first, (s.at.rb + 1) * kRows);
+        s.rows = min(kRows, p.queries * p.rep - s.at.rb * kRows);
+        s.chunks = Plan::chunks_of(s.seen);
+        if (entire) {
+            --whole;
             item += ctas;
-            describe(p, s);
             s.c0 = 0;
             s.c1 = s.chunks;
             s.opens = true;
             return true;
         }
-        if (at >= end) return false;
-        s.at = place;
-        describe(p, s);
         s.c0 = (int)(at - place.item_begin);
         s.c1 = (int)min((long long)s.chunks, s.c0 + (end - at));
         s.opens = s.c0 == 0;
@@ -268,14 +282,6 @@ struct Walk {
         }
         return true;
     }
-    __device__ __forceinline__ void describe(const CacheAttendArgs& p, Segment& s) const
-    {
-        s.have = stream_tokens(p, s.at.b, false);
-        s.first = first_position(p, s.at.b, s.have);
-        s.seen = keys_seen(p, s.have, s.first, (s.at.rb + 1) * kRows);
-        s.rows = min(kRows, p.queries * p.rep - s.at.rb * kRows);
-        s.chunks = max(1, (s.seen + kChunk - 1) / kChunk);
-    }
 };
 
 // The CTAs that share an item, and where each of them leaves its rows: an item begins as the last thing that its first CTA
@@ -284,12 +290,18 @@ struct Parts {
     int first, count;
     __device__ __forceinline__ int slot(int cta) const { return 2 * cta + (cta == first ? 1 : 0); }
 };
-// (item_begin counted from the base; a whole item is below it)
-__device__ __forceinline__ Parts item_parts(long long share, long long item_begin, int chunks)
+__device__ __forceinline__ Parts item_parts(const Cut& c, const Segment& s)
 {
-    Parts q;
-    q.first = (int)(item_begin / share);
-    q.count = item_begin < 0 ? 1 : (int)((item_begin + chunks - 1) / share) - q.first + 1;
+    Parts q{(int)blockIdx.x, 1};
+    if (s.c0 == 0 && s.c1 == s.chunks) return q;      // all of it is this CTA's
+    const long long begin = s.at.item_begin - c.base, last = begin + s.chunks - 1;
+    if (last < (1LL << 31) && c.share < (1LL << 31)) {
+        q.first = (int)((uint32_t)begin / (uint32_t)c.share);
+        q.count = (int)((uint32_t)last / (uint32_t)c.share) - q.first + 1;
+    } else {
+        q.first = (int)(begin / c.share);
+        q.count = (int)(last / c.share) - q.first + 1;
+    }
     return q;
 }
 
