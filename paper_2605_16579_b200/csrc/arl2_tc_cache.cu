@@ -748,77 +748,93 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
     const int tid = threadIdx.x, quarter = tid & 3, page_tokens = 1 << p.c.page_shift;
     grid_dependency_sync();
     if (!place_tiles(p, first)) return;
-    const int pairs = first[p.s_B] * p.c.kv_heads, q_blocks = p.s_B * p.c.kv_heads * p.row_blocks;
+    constexpr int kQParts = 4;      // of a block of query rows
+    const int pairs = first[p.s_B] * p.c.kv_heads, q_works = p.s_B * p.c.kv_heads * p.row_blocks * kQParts;
     int work = (int)blockIdx.x;
-    for (; work < q_blocks; work += (int)gridDim.x) {
-        const int bh = work / p.row_blocks;
+    for (; work < q_works; work += (int)gridDim.x) {
+        const int block = work / kQParts, bh = block / p.row_blocks;
         Place at;
-        at.rb = work - bh * p.row_blocks;
+        at.rb = block - bh * p.row_blocks;
         at.b = bh / p.c.kv_heads;
         at.h = bh - at.b * p.c.kv_heads;
         const size_t pair = q_pair(p, at);
         int have, position;
         Streams::look_up(p, at.b, have, position);
-        const int row0 = (tid >> 5) * 32, lane = tid & 31;      // (8 warps of 32 rows)
-        const float scale = write_q<32, 4>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
+        constexpr int kWarpRows = kItemRows / kQParts / (kUnpackThreads / 32);
+        const int row0 = (work % kQParts) * (kItemRows / kQParts) + (tid >> 5) * kWarpRows, lane = tid & 31;
+        const float scale = write_q<kWarpRows, 8>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
                                         p.unpacked + pair * kUnpackPair + (row0 / kTile) * kTileBytes, row0, lane);
-        p.q_scale[pair * kItemRows + row0 + lane] = scale;
+        if (lane < kWarpRows) p.q_scale[pair * kItemRows + row0 + lane] = scale;
     }
-    int b = 0;
-    for (int pair = work - q_blocks; pair < pairs; pair += (int)gridDim.x) {
-        const int at = pair / p.c.kv_heads, h = pair - at * p.c.kv_heads;
-        while (first[b + 1] <= at) ++b;      // (pairs only grow)
-        const int tile = at - first[b], have = stream_tokens(p, b, false);
-        if (tid < kUnpackMarks) marks[tid] = 0;
-        __syncthreads();
-        uint4 codes[2][2];
-        uint32_t params[2][2];
+    // Then tiles, K (even) and V (odd) of a pair.  A thread has rows tid / 4 and 64 further of a tile; the next tile's are fetched while
+    // this one's are written.
+    struct Rows {
+        uint4 codes[2];
+        uint32_t params[2];
+    };
+    int fetch_b = 0;      // (tiles only grow)
+    auto fetch = [&](int tile_no, Rows& r) {
+        const int w = tile_no & 1, at = (tile_no >> 1) / p.c.kv_heads, h = (tile_no >> 1) - at * p.c.kv_heads;
+        while (first[fetch_b + 1] <= at) ++fetch_b;
+        const int tile = at - first[fetch_b], have = stream_tokens(p, fetch_b, false);
+        const int32_t* table = p.c.table + (size_t)fetch_b * p.c.max_pages;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int row = (tid >> 2) + 64 * e, key = tile * kTile + row;
-            const int page = key < have ? p.c.table[(size_t)b * p.c.max_pages + (key >> p.c.page_shift)] : -1;
-            const bool there = (uint32_t)page < (uint32_t)p.c.num_pages;
-            if (key < have && !there) range_error(p.c.status, kRangePage, b);
-            const int slot = key & (page_tokens - 1);
-            const uint8_t* unit = p.c.pages + ((size_t)(there ? page : 0) * p.c.kv_heads + h) * p.c.unit_bytes;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                codes[e][w] = make_uint4(0, 0, 0, 0);
-                params[e][w] = 0;
-                if (there) {
-                    codes[e][w] = *reinterpret_cast<const uint4*>(unit + (w ? U::v_codes(page_tokens) : 0) + slot * U::kRow + quarter * 16);
-                    params[e][w] = *reinterpret_cast<const uint32_t*>(unit + (w ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + (quarter >> 1) * 4);
+            const int key = tile * kTile + (tid >> 2) + 64 * e;
+            r.codes[e] = make_uint4(0, 0, 0, 0);
+            r.params[e] = 0;
+            if (key < have) {
+                const int page = table[key >> p.c.page_shift];
+                if ((uint32_t)page < (uint32_t)p.c.num_pages) {
+                    const int slot = key & (page_tokens - 1);
+                    const uint8_t* unit = p.c.pages + ((size_t)page * p.c.kv_heads + h) * p.c.unit_bytes;
+                    r.codes[e] = *reinterpret_cast<const uint4*>(unit + (w ? U::v_codes(page_tokens) : 0) + slot * U::kRow + quarter * 16);
+                    r.params[e] = *reinterpret_cast<const uint32_t*>(unit + (w ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + (quarter >> 1) * 4);
+                } else {
+                    range_error(p.c.status, kRangePage, fetch_b);
                 }
             }
-            if (p.causal && not_finite(params[e][1])) {     // (taken out, and softmax told)
-                params[e][1] = 0;
+        }
+    };
+    int tile_no = work - q_works;
+    Rows next;
+    if (tile_no < 2 * pairs) fetch(tile_no, next);
+    for (; tile_no < 2 * pairs; tile_no += (int)gridDim.x) {
+        Rows cur = next;
+        if (tile_no + (int)gridDim.x < 2 * pairs) fetch(tile_no + (int)gridDim.x, next);
+        if (p.causal && (tile_no & 1)) {      // values that are not finite are taken out, and softmax told
+            __syncthreads();
+            if (tid < kUnpackMarks) marks[tid] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = (tid >> 2) + 64 * e;
+                if (!not_finite(cur.params[e])) continue;
+                cur.params[e] = 0;
                 atomicOr(marks + 1 + (quarter >> 1) * 4 + (row >> 5), 1u << (row & 31));
                 marks[0] = 1;
             }
+            __syncthreads();
+            if (tid < kUnpackMarks) p.unpack_marks[(size_t)(tile_no >> 1) * kUnpackMarks + tid] = marks[tid];
         }
-        uint8_t* out = p.unpacked + (size_t)pair * kUnpackPair + (quarter >> 1) * kHalfBytes;
+        uint8_t* out = p.unpacked + (size_t)tile_no * kTileBytes + (quarter >> 1) * kHalfBytes;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int row = (tid >> 2) + 64 * e;
+            const __half2 both = *reinterpret_cast<const __half2*>(&cur.params[e]);
+            const __half2 low = __low2half2(both), step = __high2half2(both);
+            const uint32_t c[4] = {cur.codes[e].x, cur.codes[e].y, cur.codes[e].z, cur.codes[e].w};
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const __half2 both = *reinterpret_cast<const __half2*>(&params[e][w]);
-                const __half2 low = __low2half2(both), step = __high2half2(both);
-                const uint32_t c[4] = {codes[e][w].x, codes[e][w].y, codes[e][w].z, codes[e][w].w};
-#pragma unroll
-                for (int k = 0; k < 4; k += 2) {
-                    // chunks 2 m and 2 m + 1 of the swizzled row share a sector, in the order that the row's lowest bit gives
-                    const uint4 x = hold_word(c[k], low, step), y = hold_word(c[k + 1], low, step);
-                    const bool swap = (row & 1) != 0;
-                    const uint4 lo = swap ? y : x, hi = swap ? x : y;
-                    const uint32_t words[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                    const int chunk = ((quarter & 1) * 4 + k) ^ (row & 6);
-                    store_row32(out + w * kTileBytes + row * 128 + (chunk << 4), words);
-                }
+            for (int k = 0; k < 4; k += 2) {
+                // chunks 2 m and 2 m + 1 of the swizzled row share a sector, in the order that the row's lowest bit gives
+                const uint4 x = hold_word(c[k], low, step), y = hold_word(c[k + 1], low, step);
+                const bool swap = (row & 1) != 0;
+                const uint4 lo = swap ? y : x, hi = swap ? x : y;
+                const uint32_t words[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                const int chunk = ((quarter & 1) * 4 + k) ^ (row & 6);
+                store_row32(out + row * 128 + (chunk << 4), words);
             }
         }
-        __syncthreads();
-        if (tid < kUnpackMarks) p.unpack_marks[(size_t)pair * kUnpackMarks + tid] = marks[tid];
     }
 }
 
@@ -918,7 +934,7 @@ int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
     a.either = ahead && pairs > a.unpack_pairs;
     int launched = 0;
     if (ahead) {
-        const long long ctas = pairs < num_sms * 4 ? pairs : num_sms * 4;
+        const long long ctas = pairs < num_sms * 4 ? pairs : num_sms * 4;   // (all of them at once)
         const cudaError_t e = launch_kernel(cache_unpack_kernel, dim3((unsigned)ctas), kUnpackThreads, 0, st, a);
         if (e != cudaSuccess) { set_error("launch of cache_unpack_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
         const int r = launch_tc_attend(true, a, (int)grid, st);
