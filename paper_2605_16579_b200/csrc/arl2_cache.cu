@@ -18,6 +18,7 @@
 #include <cuda_bf16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "cache_common.cuh"
 
@@ -224,6 +225,13 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// the same with nothing to add to
+__device__ __forceinline__ void mma16816_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
 {
     uint32_t d;
@@ -257,58 +265,74 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-// (cached rows are read once, by one SM)
-__device__ __forceinline__ uint32_t load_once(const uint32_t* p)
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b)
 {
-    uint32_t v;
-    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
+    const __half2 d = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&d);
 }
-__device__ __forceinline__ uint2 load_once(const uint2* p)
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// 16 bytes to shared memory in the background
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
 {
-    uint2 v;
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 // What a lane reads of 16 keys.  Keys: channels [16 tig, 16 tig + 16) of each group of keys gid and gid + 8 (gid = lane / 4,
 // tig = lane % 4); values: channels [8 gid, 8 gid + 8) of each group of tokens 2 tig, 2 tig + 1, 2 tig + 8 and 2 tig + 9;
 // parameters of keys gid and gid + 8.
-template <int G>
-struct Raw {
-    uint2 k[2][G];
-    uint32_t v[4][G];
-    uint32_t kp[2][G], vp[2][G];
-};
+//
+// 16 keys on their way through shared memory, a warp's own: rows of K codes, with 16-byte pieces exchanged so that the eight
+// lanes that read at once meet different banks; rows of V codes, 16 bytes apart for the same reason; parameters of K and of V.
 template <int D>
-__device__ __forceinline__ void load_raw(Raw<D / 64>& r, const uint8_t* unit, int page_tokens, int slot, int gid, int tig)
-{
+struct Stage {
     using U = Unit<D>;
-    constexpr int G = U::kGroups;
+    static constexpr int G = U::kGroups;
+    static constexpr int kPieces = U::kRow / 16;                // of a row
+    static constexpr int kLdV = U::kRow + 16;
+    static constexpr int kOffV = kKeys * U::kRow;
+    static constexpr int kOffKP = kOffV + kKeys * kLdV;
+    static constexpr int kOffVP = kOffKP + kKeys * U::kPar;
+    static constexpr int kBytes = kOffVP + kKeys * U::kPar;
+    static __device__ __forceinline__ int k_piece(int row, int piece) { return row * U::kRow + (piece ^ (D == 128 ? (row & 2) : 0)) * 16; }
+
+    // A lane's part of the copying: where its pieces go in a stage, and where they come from in a unit.
+    struct Copier {
+        uint32_t to_k, to_v, to_p;
+        uint32_t from_v, from_p;
+    };
+    static constexpr int kParPieces = kKeys * U::kPar / 16;       // of K's parameters, and of V's
+    static __device__ __forceinline__ Copier copier(int page_tokens, int lane)
+    {
+        const int row = lane / kPieces, piece = lane % kPieces, which = (lane / kParPieces) & 1, part = lane % kParPieces;
+        Copier c;
+        c.to_k = k_piece(row, piece);
+        c.to_v = kOffV + row * kLdV + piece * 16;
+        c.to_p = (which ? kOffVP : kOffKP) + part * 16;
+        c.from_v = U::v_codes(page_tokens);
+        c.from_p = (which ? U::v_par(page_tokens) : U::k_par(page_tokens)) + part * 16;
+        return c;
+    }
+    // unit: the head's part of the page, slot: the first key's place in it
+    static __device__ __forceinline__ void copy(const Copier& c, uint32_t to, const uint8_t* unit, int slot, int lane)
+    {
+        const uint8_t* k = unit + (uint32_t)(slot * U::kRow + lane * 16);
+        const uint8_t* v = k + c.from_v;
+        constexpr int kRounds = kKeys * kPieces / 32, kRowsEach = kKeys / kRounds;     // (the same piece of rows kRowsEach further)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int at = slot + gid + 8 * e;
-#pragma unroll
-        for (int g = 0; g < G; ++g) r.k[e][g] = load_once(reinterpret_cast<const uint2*>(unit + at * U::kRow + g * 32 + tig * 8));
-        const uint8_t* kp = unit + U::k_par(page_tokens) + at * U::kPar;
-        const uint8_t* vp = unit + U::v_par(page_tokens) + at * U::kPar;
-        if constexpr (G == 2) {
-            const uint2 a = load_once(reinterpret_cast<const uint2*>(kp)), b = load_once(reinterpret_cast<const uint2*>(vp));
-            r.kp[e][0] = a.x; r.kp[e][1] = a.y;
-            r.vp[e][0] = b.x; r.vp[e][1] = b.y;
-        } else {
-            r.kp[e][0] = load_once(reinterpret_cast<const uint32_t*>(kp));
-            r.vp[e][0] = load_once(reinterpret_cast<const uint32_t*>(vp));
+        for (int i = 0; i < kRounds; ++i) {
+            copy16(to + c.to_k + i * kRowsEach * U::kRow, k + 512 * i);
+            copy16(to + c.to_v + i * kRowsEach * kLdV, v + 512 * i);
         }
+        if (lane < 2 * kParPieces) copy16(to + c.to_p, unit + (uint32_t)(slot * U::kPar) + c.from_p);
     }
-    const uint8_t* vc = unit + U::v_codes(page_tokens);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int at = slot + 2 * tig + (e & 1) + 8 * (e >> 1);
-#pragma unroll
-        for (int g = 0; g < G; ++g) r.v[e][g] = load_once(reinterpret_cast<const uint32_t*>(vc + at * U::kRow + g * 32 + gid * 4));
+    static __device__ __forceinline__ void zero(uint8_t* to, int lane)
+    {
+        for (int i = lane * 16; i < kBytes; i += 512) *reinterpret_cast<uint4*>(to + i) = make_uint4(0, 0, 0, 0);
     }
-}
+};
 
 // kRows query rows of one key head; kSplit: operands as two fp16 numbers (fp32 I/O)
 template <int D, int kTiles, bool kSplit>
@@ -316,24 +340,30 @@ struct RowsConfig {
     static constexpr int G = D / kCacheGroup;
     static constexpr int kRows = 8 * kTiles;
     static constexpr int kParts = kSplit ? 2 : 1;
+    static constexpr int kStages = 3;
     static constexpr int kLd = D + 1;
-    // shared memory: the query operand, then (over it) the warps' rows; per row its factor, its sums per group, the keys it sees
+    // CTAs that an SM is to hold: by the registers of the output's fragments
+    static constexpr int kPerSm = D * kTiles <= 128 ? (kSplit ? 3 : 4) : D * kTiles <= 256 ? (kSplit ? 2 : 3) : 2;
+    // shared memory: the query operand and the keys on their way, then (over them) the warps' rows; per row its factor, its sums per
+    // group, the keys it sees
     static constexpr int kQBytes = kParts * kRows * D * 2;
+    static constexpr int kStageAt = kQBytes;
+    static constexpr int kLoopBytes = kStageAt + kWarps * kStages * Stage<D>::kBytes;
     static constexpr int kMergeBytes = kWarps * kRows * (kLd + 2) * 4;
-    static constexpr int kInfo = (kQBytes > kMergeBytes ? kQBytes : kMergeBytes);
-    static constexpr int kBytes = kInfo + kRows * (1 + G + 1) * 4 + 128;
+    static constexpr int kInfo = (kLoopBytes > kMergeBytes ? kLoopBytes : kMergeBytes);
+    static constexpr int kBytes = kInfo + kRows * (1 + G + 1) * 4;
 };
 
 template <int D, typename IO, int kTiles>
-__global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_constant__ CacheAttendArgs p)
+__global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 4>::kPerSm) cache_attend_kernel(const __grid_constant__ CacheAttendArgs p)
 {
     constexpr bool kSplit = sizeof(IO) == 4;
     using C = RowsConfig<D, kTiles, kSplit>;
-    using U = Unit<D>;
+    using S = Stage<D>;
     constexpr int G = C::G, kRows = C::kRows, kParts = C::kParts;
-    // slack of the reference maximum (log2 units) and the place of p * step in fp16's range: at most 2^14
-    constexpr float kSlack = kSplit ? 0.0f : 8.0f;
-    constexpr float kPlace = kSplit ? 16384.0f : 64.0f;
+    // The place of p * step in fp16's range: at most 2^14.  The reference maximum follows every larger score, so that the largest p is
+    // exactly 1: its p * step then has no rounding against its p * minimum, which it nearly cancels with where the value is small.
+    constexpr float kPlace = 16384.0f;
     extern __shared__ __align__(16) uint8_t smem[];
     __half* q_frag = reinterpret_cast<__half*>(smem);          // [part][tile][group][k-step][lane][4]
     float* merge_o = reinterpret_cast<float*>(smem);           // [warp][row][kLd]
@@ -341,13 +371,16 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
     float* row_scale = reinterpret_cast<float*>(smem + C::kInfo);   // [row]
     float* row_sum = row_scale + kRows;                        // [row][group]
     int* row_seen = reinterpret_cast<int*>(row_sum + kRows * G);    // [row]
-    __shared__ long long scratch[kWarps + 4];
+    __shared__ long long scratch[2 * kWarps + 4];
     __shared__ Streams streams;
     __shared__ Cut slow;
     __shared__ int last_part;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const int page_tokens = 1 << p.c.page_shift;
+    uint8_t* stages = smem + C::kStageAt + warp * C::kStages * S::kBytes;
+    const uint32_t stages_at = static_cast<uint32_t>(__cvta_generic_to_shared(stages));
+    const typename S::Copier copier = S::copier(page_tokens, lane);
     grid_dependency_sync();
     const Cut cut = Planner<kRows, kChunk, false, kThreads>::cut(p, streams, (int)blockIdx.x, (int)gridDim.x, scratch, &slow);
     Walk<kRows, kChunk, false> walk(streams, cut, (int)blockIdx.x, (int)gridDim.x, true);
@@ -357,72 +390,113 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
         const int b = seg.at.b, rb = seg.at.rb, h = seg.at.h;
         const int have = seg.have, first = seg.first, seen = seg.seen, rows = seg.rows, c0 = seg.c0, c1 = seg.c1;
         if (tid == 0 && seg.opens) (void)stream_tokens(p, b, true);
+        __syncthreads();     // (shared memory of the item before has been read)
+
+        // ---- keys on their way.  Key tiles of this warp: chunk * kWarps + warp, up to c_end.  A lane holds where one of the next 32 is.
+        const int32_t* table = p.c.table + (size_t)b * p.c.max_pages;
+        const uint8_t* head = p.c.pages + (size_t)h * p.c.unit_bytes;
+        const int c_end = min(c1, (seen - warp * kKeys + kChunk - 1) / kChunk);
+        auto unit_of = [&](int c) {
+            if (c >= c_end) return (const uint8_t*)nullptr;
+            const uint32_t page = table[(c * kChunk + warp * kKeys) >> p.c.page_shift];
+            if (page < (uint32_t)p.c.num_pages) return head + (size_t)page * ((size_t)p.c.kv_heads * p.c.unit_bytes);
+            range_error(p.c.status, kRangePage, b);
+            return (const uint8_t*)nullptr;          // (reads as zeros)
+        };
+        int turn = 0, stage_in = 0;                  // of the lane whose tile is next; byte offset of the stage it goes to
+        const uint8_t* my_unit = unit_of(c0 + lane);
+        int fetch_c = c0;
+        auto fetch = [&]() {
+            if (fetch_c < c_end) {
+                const uint8_t* unit = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_unit), turn));
+                if (unit != nullptr) S::copy(copier, stages_at + stage_in, unit, (fetch_c * kChunk + warp * kKeys) & (page_tokens - 1), lane);
+                else S::zero(stages + stage_in, lane);
+                ++fetch_c;
+                if (++turn == 32) {
+                    turn = 0;
+                    my_unit = unit_of(fetch_c + lane);
+                }
+            }
+            copies_commit();
+            stage_in = stage_in == (C::kStages - 1) * S::kBytes ? 0 : stage_in + S::kBytes;
+        };
+#pragma unroll
+        for (int i = 0; i < C::kStages - 1; ++i) fetch();
 
         // ---- the query rows: rotated, scaled into fp16's range, laid out as the instruction's second operand
-        __syncthreads();
-        for (int r = warp; r < kRows; r += kWarps) {
+        {
             constexpr int kPer = D / 32;       // channels of a lane
-            float x[kPer];
+            constexpr int kEach = kRows / kWarps;
+            float x[kEach][kPer], cs[kEach][kPer / 2], sn[kEach][kPer / 2];
+            long long pos[kEach];
+            bool past = false;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
-            int sees = 0;
-            if (r < rows) {
-                const int flat = rb * kRows + r, i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
-                const IO* src = static_cast<const IO*>(p.q) + b * p.q_batch + i * p.q_token + (size_t)head * D + lane * kPer;
-                const long long pos = (long long)first + i;
-                sees = p.causal ? (int)max(0LL, min((long long)have, pos + 1)) : have;
+            for (int k = 0; k < kEach; ++k) {      // (all loads before anything that waits for one)
+                const int flat = rb * kRows + min(warp + kWarps * k, rows - 1), i = flat / p.rep, q_head = h * p.rep + flat - i * p.rep;
+                const IO* src = static_cast<const IO*>(p.q) + b * p.q_batch + i * p.q_token + (size_t)q_head * D + lane * kPer;
+                pos[k] = (long long)first + i;
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) x[e] = static_cast<float>(src[e]);
+                for (int e = 0; e < kPer; ++e) x[k][e] = static_cast<float>(src[e]);
                 if (p.c.rope_cos != nullptr) {
-                    long long t = max(pos, 0LL);
-                    if (t >= p.c.rope_rows) {
-                        if (lane == 0) range_error(p.c.status, kRangePosition, b);
-                        t = p.c.rope_rows - 1;
-                    }
+                    const long long t = min(max(pos[k], 0LL), (long long)p.c.rope_rows - 1);
+                    past |= pos[k] >= p.c.rope_rows;
 #pragma unroll
                     for (int m = 0; m < kPer / 2; ++m) {
-                        const float cs = p.c.rope_cos[t * (D / 2) + lane * (kPer / 2) + m], sn = p.c.rope_sin[t * (D / 2) + lane * (kPer / 2) + m];
-                        const float u = x[2 * m], w = x[2 * m + 1];
-                        x[2 * m] = u * cs - w * sn;
-                        x[2 * m + 1] = u * sn + w * cs;
+                        cs[k][m] = p.c.rope_cos[t * (D / 2) + lane * (kPer / 2) + m];
+                        sn[k][m] = p.c.rope_sin[t * (D / 2) + lane * (kPer / 2) + m];
                     }
                 }
             }
-            float most = 0.0f;
+            if (past && lane == 0) range_error(p.c.status, kRangePosition, b);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) most = max_nan(most, fabsf(x[e]));
+            for (int k = 0; k < kEach; ++k) {
+                const int r = warp + kWarps * k;
+                uint32_t most = 0;
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
-            // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
-            const bool finite = most <= 3.402823466e38f;
-            int e2 = 0;
-            if (most > 0.0f && finite) e2 = min(10 - ilogbf(most), 126);
-            const float up = scalbnf(1.0f, e2 >> 1), up2 = scalbnf(1.0f, e2 - (e2 >> 1));
-            float sum = 0.0f;
+                for (int m = 0; m < kPer / 2; ++m) {
+                    float u = x[k][2 * m], w = x[k][2 * m + 1];
+                    if (p.c.rope_cos != nullptr) {
+                        const float a = u * cs[k][m] - w * sn[k][m];
+                        w = u * sn[k][m] + w * cs[k][m];
+                        u = a;
+                    }
+                    if (r >= rows) u = w = 0.0f;
+                    x[k][2 * m] = u;
+                    x[k][2 * m + 1] = w;
+                    // (as whole numbers the magnitudes are in the same order, infinities and NaN above all others)
+                    most = max(most, max(__float_as_uint(u) & 0x7fffffffu, __float_as_uint(w) & 0x7fffffffu));
+                }
+                most = __reduce_max_sync(0xffffffffu, most);
+                // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
+                const bool finite = most < 0x7f800000u;
+                const int e2 = !finite || most == 0 ? 0 : min(137 - (int)(most >> 23), 126);
+                const float up = pow2(e2 >> 1), up2 = pow2(e2 - (e2 >> 1));
+                float sum = 0.0f;
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                x[e] = finite ? x[e] * up * up2 : 0.0f;
-                sum += x[e];
-            }
-            // sums over a group's lanes
+                for (int e = 0; e < kPer; ++e) {
+                    x[k][e] = finite ? x[k][e] * up * up2 : 0.0f;
+                    sum += x[k][e];
+                }
+                // sums over a group's lanes
 #pragma unroll
-            for (int d = 1; d < 32 / G; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if (lane == 0) {
-                row_scale[r] = finite ? p.scale_log2 / up / up2 : __int_as_float(0x7fc00000);
-                row_seen[r] = sees;
-            }
-            if ((lane % (32 / G)) == 0) row_sum[r * G + lane / (32 / G)] = sum;
+                for (int d = 1; d < 32 / G; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                if (lane == 0) {
+                    row_scale[r] = finite ? p.scale_log2 * pow2(-(e2 >> 1)) * pow2((e2 >> 1) - e2) : __int_as_float(0x7fc00000);
+                    row_seen[r] = r >= rows ? 0 : p.causal ? (int)max(0LL, min((long long)have, pos[k] + 1)) : have;
+                }
+                if ((lane % (32 / G)) == 0) row_sum[r * G + lane / (32 / G)] = sum;
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                // channel c of its group: lane quarter c / 16, word (c / 8) % 2, code c % 8 of the word
-                const int c = lane * kPer + e, cg = c & 63, g = c >> 6;
-                const int quarter = cg >> 4, word = (cg >> 3) & 1, i = cg & 3, upper = (cg >> 2) & 1;
-                const int step = 2 * word + (i >> 1), reg = i & 1;
-                const float y = reg && !kSplit ? x[e] * 0.0625f : x[e];      // (odd codes are 2^4 larger)
-                const __half hi = __float2half_rn(y);
-                const size_t to = (((((size_t)(r >> 3)) * G + g) * 4 + step) * 32 + (r & 7) * 4 + quarter) * 4 + reg * 2 + upper;
-                q_frag[to] = hi;
-                if constexpr (kSplit) q_frag[(size_t)kTiles * G * 4 * 32 * 4 + to] = __float2half_rn(y - __half2float(hi));
+                for (int e = 0; e < kPer; ++e) {
+                    // channel c of its group: lane quarter c / 16, word (c / 8) % 2, code c % 8 of the word
+                    const int c = lane * kPer + e, cg = c & 63, g = c >> 6;
+                    const int quarter = cg >> 4, word = (cg >> 3) & 1, i = cg & 3, upper = (cg >> 2) & 1;
+                    const int step = 2 * word + (i >> 1), reg = i & 1;
+                    const float y = reg && !kSplit ? x[k][e] * 0.0625f : x[k][e];      // (odd codes are 2^4 larger)
+                    const __half hi = __float2half_rn(y);
+                    const size_t to = (((((size_t)(r >> 3)) * G + g) * 4 + step) * 32 + (r & 7) * 4 + quarter) * 4 + reg * 2 + upper;
+                    q_frag[to] = hi;
+                    if constexpr (kSplit) q_frag[(size_t)kTiles * G * 4 * 32 * 4 + to] = __float2half_rn(y - __half2float(hi));
+                }
             }
         }
         __syncthreads();
@@ -441,7 +515,6 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
         }
         // this lane's query rows: 8 t + 2 tig + e
         float scale[kTiles][2], sums[kTiles][2][G];
-        int sees[kTiles][2];
         int fewest = have;
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
@@ -449,18 +522,22 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
             for (int e = 0; e < 2; ++e) {
                 const int r = 8 * t + 2 * tig + e;
                 scale[t][e] = row_scale[r];
-                sees[t][e] = row_seen[r];
 #pragma unroll
                 for (int g = 0; g < G; ++g) sums[t][e][g] = row_sum[r * G + g];
             }
-        for (int r = 0; r < rows; ++r) fewest = min(fewest, row_seen[r]);
+        if (p.causal) fewest = min(have, max(0, (int)max(-1LL, min((long long)have, (long long)first + (rb * kRows) / p.rep)) + 1));   // the first row's
 
         float o[G][4][kTiles][4];     // [group][channel tile][row tile]
-        float m_ref[kTiles][2], l[kTiles][2], lows[kTiles][2][G];
-        float v_top[G];               // a power of two that no step so far exceeds
+        // reference maximum: in the scores' own units, and times the row's factor
+        float top[kTiles][2], m_ref[kTiles][2], l[kTiles][2], lows[kTiles][2][G];
+        // what p * step is multiplied by per group, as a pair of fp16 (bf16 I/O), and the parameters above which it has to shrink
+        float v_mul[G];
+        uint32_t v_mul2[G], v_limit[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            v_top[g] = 0.0f;
+            v_mul[g] = 32768.0f;
+            v_mul2[g] = 0x78007800u;
+            v_limit[g] = 0x0000ffffu;      // a step of zero; then the power of two below which steps are
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -472,61 +549,35 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                m_ref[t][e] = -INFINITY;
-                l[t][e] = 0.0f;
+                top[t][e] = -INFINITY;
+                m_ref[t][e] = l[t][e] = 0.0f;
 #pragma unroll
                 for (int g = 0; g < G; ++g) lows[t][e][g] = 0.0f;
             }
 
-        // Key tiles of this warp: chunk * kWarps + warp.  A lane holds the page of one of the next 32 of them; -1: nothing to see,
-        // -2: one that the pool does not have.
-        const int32_t* table = p.c.table + (size_t)b * p.c.max_pages;
-        auto page_of = [&](int c) {
-            const int key = (c * kWarps + warp) * kKeys;
-            if (c >= c1 || key >= seen) return -1;
-            const int page = table[key >> p.c.page_shift];
-            if (page >= 0 && page < p.c.num_pages) return page;
-            range_error(p.c.status, kRangePage, b);
-            return -2;
-        };
-        int pages_from = c0, my_page = page_of(c0 + lane);
-        auto fetch = [&](int c, Raw<G>& raw) {      // whether there is anything to do for this warp in chunk c
-            if (c - pages_from == 32) {
-                pages_from = c;
-                my_page = page_of(c + lane);
-            }
-            const int page = __shfl_sync(0xffffffffu, my_page, c - pages_from);
-            if (page == -1) return false;
-            if (page < 0) {      // reads as zeros
-                raw = Raw<G>();
-                return true;
-            }
-            const int key = (c * kWarps + warp) * kKeys;
-            load_raw<D>(raw, p.c.pages + ((size_t)page * p.c.kv_heads + h) * p.c.unit_bytes, page_tokens, key & (page_tokens - 1), gid, tig);
-            return true;
-        };
-
-        Raw<G> next;
-        bool have_next = fetch(c0, next);
+        int stage_out = 0;
 #pragma unroll 1
-        for (int c = c0; c < c1; ++c) {
-            const Raw<G> cur = next;
-            const bool todo = have_next;
-            have_next = c + 1 < c1 ? fetch(c + 1, next) : false;
-            if (!todo) continue;
-            const int key0 = (c * kWarps + warp) * kKeys;
+        for (int c = c0; c < c_end; ++c) {
+            copies_wait<C::kStages - 2>();
+            __syncwarp();
+            const uint8_t* stage = stages + stage_out;
+            stage_out = stage_out == (C::kStages - 1) * S::kBytes ? 0 : stage_out + S::kBytes;
+            const int key0 = c * kChunk + warp * kKeys;
+            fetch();     // (into the stage that was read in the step before, by all lanes)
 
             // ---- sums of q * code per group
             float acc[G][kTiles][4], rest[kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
 #pragma unroll
             for (int g = 0; g < G; ++g) {
+                uint2 kw[2];
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[g][t][e] = rest[kSplit ? g : 0][t][e] = 0.0f;
+                for (int e = 0; e < 2; ++e) {
+                    const int row = gid + 8 * e;
+                    kw[e] = *reinterpret_cast<const uint2*>(stage + S::k_piece(row, g * 2 + (tig >> 1)) + (tig & 1) * 8);
+                }
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    const uint32_t w0 = (s & 2) ? cur.k[0][g].y : cur.k[0][g].x, w1 = (s & 2) ? cur.k[1][g].y : cur.k[1][g].x;
+                    const uint32_t w0 = (s & 2) ? kw[0].y : kw[0].x, w1 = (s & 2) ? kw[1].y : kw[1].x;
                     const int i = 2 * (s & 1);
                     const uint32_t a[4] = {operand_pair<kSplit>(w0, i), operand_pair<kSplit>(w1, i), operand_pair<kSplit>(w0, i + 1), operand_pair<kSplit>(w1, i + 1)};
 #pragma unroll
@@ -536,33 +587,51 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
                             uint2 q;
                             if constexpr (kKeep) q = kept[g][s];
                             else q = q_operand(part, t, g, s);
-                            mma16816(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                            if (s == 0) mma16816_new(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                            else mma16816(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
                         }
                     }
                 }
             }
-            // ---- scores in log2 units: keys gid (x[t][0 .. 1]) and gid + 8 (x[t][2 .. 3])
-            float kl[2][G], ks[2][G], vl[2][G], vs[2][G];
+            // ---- parameters of keys gid and gid + 8; rows' scores x[t][0 .. 1] and x[t][2 .. 3] (still to be multiplied by the row's factor)
+            uint32_t kp[2][G], vp[2][G];
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const float2 a = unpack_half(cur.kp[e][g]), v = unpack_half(cur.vp[e][g]);
-                    kl[e][g] = kSplit ? fmaf(8.0f, a.y, a.x) : a.x;
-                    ks[e][g] = kSplit ? a.y : a.y * 16777216.0f;
-                    vl[e][g] = kSplit ? fmaf(8.0f, v.y, v.x) : v.x;
-                    vs[e][g] = v.y;
+            for (int e = 0; e < 2; ++e) {
+                const uint8_t* at = stage + S::kOffKP + (gid + 8 * e) * S::U::kPar;
+                if constexpr (G == 2) {
+                    const uint2 a = *reinterpret_cast<const uint2*>(at), v = *reinterpret_cast<const uint2*>(at + S::kOffVP - S::kOffKP);
+                    kp[e][0] = a.x; kp[e][1] = a.y;
+                    vp[e][0] = v.x; vp[e][1] = v.y;
+                } else {
+                    kp[e][0] = *reinterpret_cast<const uint32_t*>(at);
+                    vp[e][0] = *reinterpret_cast<const uint32_t*>(at + S::kOffVP - S::kOffKP);
                 }
+            }
             float x[kTiles][4];
+            {
+                float kl[2][G], ks[2][G];
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float s = 0.0f;
+                    for (int g = 0; g < G; ++g) {
+                        const float2 a = unpack_half(kp[e][g]);
+                        kl[e][g] = kSplit ? fmaf(8.0f, a.y, a.x) : a.x;
+                        ks[e][g] = a.y;
+                    }
 #pragma unroll
-                    for (int g = 0; g < G; ++g) s = fmaf(kSplit ? acc[g][t][e] + rest[kSplit ? g : 0][t][e] : acc[g][t][e], ks[e >> 1][g], fmaf(kl[e >> 1][g], sums[t][e & 1][g], s));
-                    x[t][e] = s * scale[t][e & 1];
-                }
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float low = kl[e >> 1][0] * sums[t][e & 1][0], s = 0.0f;
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            if (g > 0) low = fmaf(kl[e >> 1][g], sums[t][e & 1][g], low);
+                            const float a = kSplit ? acc[g][t][e] + rest[kSplit ? g : 0][t][e] : acc[g][t][e];
+                            s = g == 0 ? a * ks[e >> 1][g] : fmaf(a, ks[e >> 1][g], s);
+                        }
+                        x[t][e] = fmaf(s, kSplit ? 1.0f : 16777216.0f, low);
+                    }
+            }
             const bool edge = key0 + kKeys > fewest;     // some row does not see some of these keys
             if (edge) {
 #pragma unroll
@@ -570,13 +639,13 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
                     const int key = key0 + gid + 8 * e;
                     if (key >= have) {                   // nothing is there: whatever the memory holds stays out of the sums
 #pragma unroll
-                        for (int g = 0; g < G; ++g) vl[e][g] = vs[e][g] = 0.0f;
+                        for (int g = 0; g < G; ++g) vp[e][g] = 0;
                     }
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                         for (int f = 0; f < 2; ++f)
-                            if (key >= sees[t][f]) x[t][2 * e + f] = -INFINITY;
+                            if (key >= row_seen[8 * t + 2 * tig + f]) x[t][2 * e + f] = -INFINITY;
                 }
             }
             // ---- reference maximum and the values' scale: renewed only where they have to be
@@ -584,9 +653,9 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) renew |= x[t][e] > m_ref[t][e & 1] + kSlack;
+                for (int e = 0; e < 4; ++e) renew |= x[t][e] > top[t][e & 1];
 #pragma unroll
-            for (int g = 0; g < G; ++g) renew |= vs[0][g] > v_top[g] || vs[1][g] > v_top[g];
+            for (int g = 0; g < G; ++g) renew |= max(vp[0][g], vp[1][g]) > v_limit[g];      // (the step is the upper half, and not negative)
             if (__any_sync(0xffffffffu, renew)) {
                 float down[kTiles][2];
 #pragma unroll
@@ -596,23 +665,31 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
                         float mx = fmaxf(x[t][f], x[t][2 + f]);
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                        const float m_new = fmaxf(m_ref[t][f], mx);
-                        down[t][f] = m_new == m_ref[t][f] ? 1.0f : exp2_fast(m_ref[t][f] - m_new);
-                        m_ref[t][f] = m_new;
+                        down[t][f] = 1.0f;
+                        if (mx > top[t][f]) {
+                            const float m_new = __fmul_rn(mx, scale[t][f]);
+                            down[t][f] = top[t][f] == -INFINITY ? 0.0f : exp2_fast(m_ref[t][f] - m_new);
+                            top[t][f] = mx;
+                            m_ref[t][f] = m_new;
+                        }
                         l[t][f] *= down[t][f];
 #pragma unroll
                         for (int g = 0; g < G; ++g) lows[t][f][g] *= down[t][f];
                     }
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    float top = fmaxf(vs[0][g], vs[1][g]);
-#pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    uint32_t most = __reduce_max_sync(0xffffffffu, max(vp[0][g], vp[1][g])) >> 16;
                     float shrink = 1.0f;
-                    if (top > v_top[g]) {   // the next power of two: the exponent field of twice the step
-                        const float up = __uint_as_float((__float_as_uint(2.0f * top)) & 0x7f800000u);
-                        shrink = v_top[g] / up;
-                        v_top[g] = up;
+                    if (most > (v_limit[g] >> 16) && most < 0x7c00u) {
+                        // kPlace over the next power of two above the step, as far as fp16 goes
+                        const float step = __half2float(__ushort_as_half((unsigned short)most));
+                        const float above = __uint_as_float(__float_as_uint(2.0f * step) & 0x7f800000u);
+                        const float mul = fminf(kPlace / above, 32768.0f);
+                        v_limit[g] = ((uint32_t)__half_as_ushort(__float2half_rn(above)) << 16) | 0xffffu;
+                        shrink = mul / v_mul[g];
+                        v_mul[g] = mul;
+                        const uint32_t m16 = __half_as_ushort(__float2half_rn(mul));
+                        v_mul2[g] = m16 | (m16 << 16);
                     }
 #pragma unroll
                     for (int m = 0; m < 4; ++m)
@@ -623,48 +700,61 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
                 }
             }
             // ---- p, and p * step per group as the instruction's second operand
-            float scaled[2][G];
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const float f = v_top[g] > 0.0f ? kPlace / v_top[g] : 1.0f;
-                scaled[0][g] = vs[0][g] * f;
-                scaled[1][g] = vs[1][g] * f;
-            }
             uint32_t pb[kParts][kTiles][G][2];
+            auto weigh = [&](auto masked) {
+                constexpr bool kMasked = decltype(masked)::value;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                float pr[4];
+                for (int t = 0; t < kTiles; ++t) {
+                    float pr[4];
+                    bool hidden[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float m = m_ref[t][e & 1] == -INFINITY ? 0.0f : m_ref[t][e & 1];
-                    pr[e] = exp2_fast(x[t][e] - m);
-                    l[t][e & 1] += pr[e];
-                }
-#pragma unroll
-                for (int g = 0; g < G; ++g)
+                    for (int e = 0; e < 4; ++e) {
+                        // (with a fused product the largest would not be 1)
+                        pr[e] = exp2_fast(__fsub_rn(__fmul_rn(x[t][e], scale[t][e & 1]), m_ref[t][e & 1]));
+                        hidden[e] = kMasked && x[t][e] == -INFINITY;
+                        if (kMasked && hidden[e]) pr[e] = 0.0f;          // (its factor may be NaN)
+                        l[t][e & 1] += pr[e];
+                    }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float y0 = pr[2 * e] * scaled[e][g], y1 = pr[2 * e + 1] * scaled[e][g];
-                        float a0 = pr[2 * e] * vl[e][g], a1 = pr[2 * e + 1] * vl[e][g];
-                        if (edge) {      // a NaN or an infinity that a row does not see is not to reach it as 0 * NaN
-                            if (x[t][2 * e] == -INFINITY) y0 = a0 = 0.0f;
-                            if (x[t][2 * e + 1] == -INFINITY) y1 = a1 = 0.0f;
-                        }
-                        lows[t][0][g] += a0;
-                        lows[t][1][g] += a1;
-                        const uint32_t hi = pack_half(y0, y1);
-                        pb[0][t][g][e] = transpose8x8(hi);
-                        if constexpr (kSplit) {
-                            const float2 back = unpack_half(hi);
-                            pb[1][t][g][e] = transpose8x8(pack_half(y0 - back.x, y1 - back.y));
+                        const uint32_t p2 = kSplit ? 0u : pack_half(pr[2 * e], pr[2 * e + 1]);
+                        // a NaN or an infinity that a row does not see is not to reach it as 0 * NaN
+                        const uint32_t keep = (hidden[2 * e] ? 0u : 0xffffu) | (hidden[2 * e + 1] ? 0u : 0xffff0000u);
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            const float2 v = unpack_half(vp[e][g]);
+                            const float vl = kSplit ? fmaf(8.0f, v.y, v.x) : v.x;
+                            uint32_t hi, lo = 0;
+                            if constexpr (kSplit) {
+                                const float s = v.y * v_mul[g], y0 = pr[2 * e] * s, y1 = pr[2 * e + 1] * s;
+                                hi = pack_half(y0, y1);
+                                const float2 back = unpack_half(hi);
+                                lo = pack_half(y0 - back.x, y1 - back.y);
+                            } else {
+                                hi = mul_half2(p2, mul_half2(__byte_perm(vp[e][g], 0, 0x3232), v_mul2[g]));
+                            }
+                            if (!(kMasked && hidden[2 * e])) lows[t][0][g] = fmaf(pr[2 * e], vl, lows[t][0][g]);
+                            if (!(kMasked && hidden[2 * e + 1])) lows[t][1][g] = fmaf(pr[2 * e + 1], vl, lows[t][1][g]);
+                            if (kMasked) {
+                                hi &= keep;
+                                lo &= keep;
+                            }
+                            pb[0][t][g][e] = transpose8x8(hi);
+                            if constexpr (kSplit) pb[kParts - 1][t][g][e] = transpose8x8(lo);
                         }
                     }
-            }
+                }
+            };
+            if (edge) weigh(std::true_type());
+            else weigh(std::false_type());
             // ---- O^T += V^T P^T, 16 channels at a time: rows gid and gid + 8 are channels 8 gid + m and 8 gid + 4 + m of the group
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const uint32_t a_lo = __byte_perm(cur.v[0][g], cur.v[1][g], 0x5410), a_hi = __byte_perm(cur.v[0][g], cur.v[1][g], 0x7632);
-                const uint32_t b_lo = __byte_perm(cur.v[2][g], cur.v[3][g], 0x5410), b_hi = __byte_perm(cur.v[2][g], cur.v[3][g], 0x7632);
+                uint32_t vw[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(stage + S::kOffV + (2 * tig + (e & 1) + 8 * (e >> 1)) * S::kLdV + g * 32 + gid * 4);
+                const uint32_t a_lo = __byte_perm(vw[0], vw[1], 0x5410), a_hi = __byte_perm(vw[0], vw[1], 0x7632);
+                const uint32_t b_lo = __byte_perm(vw[2], vw[3], 0x5410), b_hi = __byte_perm(vw[2], vw[3], 0x7632);
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     const uint32_t a[4] = {operand_pair<kSplit>(a_lo, m), operand_pair<kSplit>(a_hi, m), operand_pair<kSplit>(b_lo, m), operand_pair<kSplit>(b_hi, m)};
@@ -683,6 +773,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
                 }
             }
         }
+        copies_wait<0>();
 
         // ---- the warps' rows meet in shared memory
 #pragma unroll
@@ -695,12 +786,12 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
 #pragma unroll
                     for (int g = 0; g < G; ++g) lows[t][f][g] += __shfl_xor_sync(0xffffffffu, lows[t][f][g], d);
                 }
-        __syncthreads();       // (the query operand has been read)
+        __syncthreads();       // (the query operand and all keys have been read)
         {
             float* mine = merge_o + warp * kRows * C::kLd;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const float back = v_top[g] * ((kSplit ? 1.0f : 16777216.0f) / kPlace);
+                const float back = (kSplit ? 1.0f : 16777216.0f) / v_mul[g];
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -717,7 +808,7 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
                         const int r = 8 * t + 2 * tig + f;
-                        merge_ml[(warp * kRows + r) * 2] = m_ref[t][f];
+                        merge_ml[(warp * kRows + r) * 2] = top[t][f] == -INFINITY ? -INFINITY : m_ref[t][f];
                         merge_ml[(warp * kRows + r) * 2 + 1] = l[t][f];
                     }
             }
@@ -725,8 +816,8 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
         __syncthreads();
         const Parts parts = item_parts(cut, seg);
         auto write_row = [&](int r, int ch, float value) {
-            const int flat = rb * kRows + r, i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
-            static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + head) * D + ch] = static_cast<IO>(value);
+            const int flat = rb * kRows + r, i = flat / p.rep, q_head = h * p.rep + flat - i * p.rep;
+            static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + q_head) * D + ch] = static_cast<IO>(value);
         };
         const int slot = parts.slot((int)blockIdx.x);
         for (int x = tid; x < rows * D; x += kThreads) {
@@ -760,18 +851,50 @@ __global__ void __launch_bounds__(kThreads) cache_attend_kernel(const __grid_con
             if (last_part) {
                 __threadfence();
                 if (tid == 0) p.tickets[parts.first] = 0;      // as it was found
-                for (int x = tid; x < rows * D; x += kThreads) {
-                    const int r = x / D, ch = x - r * D;
+                // their common reference maximum, then each warp a fourth of the parts, several rows asked for at once, and the warps' sums
+                for (int r = warp; r < rows; r += kWarps) {
                     float m = -INFINITY;
-                    for (int w = 0; w < parts.count; ++w) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)parts.slot(parts.first + w) * kRows + r) * 2));
-                    const float m_use = m == -INFINITY ? 0.0f : m;
-                    float sum = 0.0f, total = 0.0f;
-                    for (int w = 0; w < parts.count; ++w) {
+                    for (int w = lane; w < parts.count; w += 32) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)parts.slot(parts.first + w) * kRows + r) * 2));
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                    if (lane == 0) row_scale[r] = m == -INFINITY ? 0.0f : m;
+                }
+                __syncthreads();
+                constexpr int kPer = D / 32;
+                for (int r = 0; r < rows; ++r) {
+                    const float m = row_scale[r];
+                    float sum[kPer], total = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
+#pragma unroll 8
+                    for (int w = warp; w < parts.count; w += kWarps) {
                         const size_t s = (size_t)parts.slot(parts.first + w) * kRows + r;
                         const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + s * 2));
-                        const float f = exp2_fast(ml.x - m_use);
-                        sum = fmaf(__ldcg(p.part_o + s * D + ch), f, sum);
+                        float x[kPer];
+                        if constexpr (kPer == 4) {
+                            const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + s * D) + lane);
+                            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+                        } else {
+                            const float2 v = __ldcg(reinterpret_cast<const float2*>(p.part_o + s * D) + lane);
+                            x[0] = v.x; x[1] = v.y;
+                        }
+                        const float f = exp2_fast(ml.x - m);
                         total = fmaf(ml.y, f, total);
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) sum[e] = fmaf(x[e], f, sum[e]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) merge_o[(warp * kRows + r) * C::kLd + lane * kPer + e] = sum[e];
+                    if (lane == 0) merge_ml[(warp * kRows + r) * 2 + 1] = total;
+                }
+                __syncthreads();
+                for (int x = tid; x < rows * D; x += kThreads) {
+                    const int r = x / D, ch = x - r * D;
+                    float sum = 0.0f, total = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        sum += merge_o[(w * kRows + r) * C::kLd + ch];
+                        total += merge_ml[(w * kRows + r) * 2 + 1];
                     }
                     write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
                 }
@@ -821,6 +944,7 @@ int launch_attend(CacheAttendArgs& a, cudaStream_t st)
     }
     a.row_blocks = (a.queries * a.rep + C::kRows - 1) / C::kRows;
     a.min_share = 2;
+    a.max_parts = kTiles == 1 ? 64 : kTiles == 2 ? 32 : 16;
     const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * ((((long long)a.c.max_pages << a.c.page_shift) + kChunk - 1) / kChunk);
     long long grid = ctas;
     if (grid > kCacheCtas) grid = kCacheCtas;

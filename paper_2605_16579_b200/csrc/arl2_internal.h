@@ -226,7 +226,8 @@ struct CacheAttendArgs {
     int s_B, H, D, queries;
     int rep;                 // query heads that share a key head
     int row_blocks;          // blocks of query rows per key head (set by the launcher)
-    int min_share;           // fewest key chunks that a CTA is given (set by the launcher)
+    int min_share;           // fewest key chunks that a CTA is given, and most CTAs that an item is cut into (set by the launcher)
+    int max_parts;
     const void* q;
     int64_t q_batch, q_token;
     const int32_t* lengths;

@@ -52,7 +52,7 @@ constexpr int kOffMarks = kOffBars + 256;   // [kSpecials][kMarkWords]
 constexpr int kMarkWords = 9;               // whether a value is not finite; the keys of those, per group [2][4]
 static_assert(kMarkWords <= kUnpackMarks, "marks");
 constexpr int kSmemBytes = kOffMarks + kSpecials * kMarkWords * 4 + 1024;   // + alignment slack
-static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 20 * 8 + (int)sizeof(Streams) + (int)sizeof(Cut) <= 227 * 1024, "shared memory, with what the kernel declares itself");
+static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 36 * 8 + (int)sizeof(Streams) + (int)sizeof(Cut) <= 227 * 1024, "shared memory, with what the kernel declares itself");
 
 enum Bar : int {
     kBarQ0 = 0, kBarQ1,                         // -> issuer t: its Q tile is there
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kOffMarks);
     const Abort ab{abort_flag, p.c.status, p.wait_limit ? p.wait_limit - 1 : kSpinLimit};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    __shared__ long long scratch[R::kThreads / 32 + 4];
+    __shared__ long long scratch[2 * (R::kThreads / 32) + 4];
     __shared__ Streams streams;
     __shared__ Cut slow;
     __shared__ int first[kUnpackStreams + 1];
@@ -924,6 +924,7 @@ int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
         }, &num_sms)) return r;
     a.row_blocks = (a.queries * a.rep + kItemRows - 1) / kItemRows;
     a.min_share = 4;
+    a.max_parts = 32;
     const long long tiles = (((long long)a.c.max_pages << a.c.page_shift) + kTile - 1) / kTile;   // of a stream and head, at most
     const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * tiles;
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;

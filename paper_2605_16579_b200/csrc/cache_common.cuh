@@ -100,7 +100,7 @@ struct Planner {
         return chunks_of(keys_seen(p, have, first, (rb + 1) * kRows));
     }
 
-    // Work of any shape: sums over the streams and blocks of rows.  All threads; `scratch`: kWarps + 4 words of shared memory.
+    // Work of any shape: sums over the streams and blocks of rows.  All threads; `scratch`: 2 kWarps + 4 words of shared memory.
     // (A function of its own: what calls of one length, the usual ones, do not reach should not stand in their way.)
     static __device__ __noinline__ void general(const CacheAttendArgs& p, const Streams& st, int cta, int ctas, long long* scratch, Cut* out)
     {
@@ -114,18 +114,30 @@ struct Planner {
             return sum;
         };
         long long mine = 0;
-        for (int e = tid; e < entities; e += kThreads) mine += size_of(e) * p.c.kv_heads;
+        int longest = 0;
+        for (int e = tid; e < entities; e += kThreads) {
+            const long long size = size_of(e);
+            mine += size * p.c.kv_heads;
+            longest = max(longest, unit_chunks(p, st, kByHead ? e : e / p.row_blocks, kByHead ? p.row_blocks - 1 : e % p.row_blocks));
+        }
+        longest = __reduce_max_sync(0xffffffffu, longest);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-        if (lane == 0) scratch[warp] = mine;
+        if (lane == 0) {
+            scratch[warp] = mine;
+            scratch[kWarps + 4 + warp] = longest;
+        }
         __syncthreads();
         long long total = 0;
-        for (int w = 0; w < kWarps; ++w) total += scratch[w];
+        for (int w = 0; w < kWarps; ++w) {
+            total += scratch[w];
+            longest = max(longest, (int)scratch[kWarps + 4 + w]);
+        }
         __syncthreads();
         Cut c;
         c.base = 0;
         c.whole = 0;
-        c.share = max((long long)p.min_share, (total + ctas - 1) / ctas);
+        c.share = max(max((long long)p.min_share, (total + ctas - 1) / ctas), (long long)(longest + p.max_parts - 1) / p.max_parts);
         c.begin = min(total, c.share * cta);
         c.end = min(total, c.begin + c.share);
         c.place = Place{0, 0, 0, 0};
@@ -194,7 +206,7 @@ struct Planner {
         }
         const int each = chunks_of(have0);
         const long long all = (long long)p.s_B * p.row_blocks * p.c.kv_heads;
-        alike = alike && all * each < (1LL << 31) && (long long)p.min_share * ctas < (1LL << 31);
+        alike = alike && all * each < (1LL << 31);
         if (!__syncthreads_and(alike)) {
             general(p, st, cta, ctas, scratch, slow);
             return *slow;
@@ -203,7 +215,8 @@ struct Planner {
         Cut c;
         c.whole = kByHead ? (int)(items / (uint32_t)ctas) : 0;
         const uint32_t base = (uint32_t)c.whole * (uint32_t)ctas * (uint32_t)each;
-        const uint32_t share = max((uint32_t)p.min_share, (total - base + (uint32_t)ctas - 1) / (uint32_t)ctas);
+        const uint32_t fewest = max((uint32_t)p.min_share, ((uint32_t)each + p.max_parts - 1) / p.max_parts);
+        const uint32_t share = max(fewest, (total - base + (uint32_t)ctas - 1) / (uint32_t)ctas);
         const uint32_t begin = (uint32_t)min((long long)total, (long long)base + (long long)share * cta);
         c.base = base;
         c.share = share;
