@@ -216,8 +216,10 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Cach
 // --------------------------------------------------------------------------------------------- attention
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kKeys = 16;                  // keys of a matrix instruction, a warp's step
-constexpr int kChunk = kWarps * kKeys;     // keys of a CTA's step
+constexpr int kKeys = 16;                  // keys of a matrix instruction
+
+// What a page that the pool does not have reads as.
+__device__ uint4 g_no_page[Unit<128>::bytes(256) / 16];
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -271,66 +273,71 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b)
     return *reinterpret_cast<const uint32_t*>(&d);
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
-// 16 bytes to shared memory in the background
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
+// (cached rows are read once, by one SM)
+__device__ __forceinline__ uint32_t load_once(const uint32_t* p)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    uint32_t v;
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ uint2 load_once(const uint2* p)
+{
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
 
-// What a lane reads of 16 keys.  Keys: channels [16 tig, 16 tig + 16) of each group of keys gid and gid + 8 (gid = lane / 4,
-// tig = lane % 4); values: channels [8 gid, 8 gid + 8) of each group of tokens 2 tig, 2 tig + 1, 2 tig + 8 and 2 tig + 9;
-// parameters of keys gid and gid + 8.
-//
-// 16 keys on their way through shared memory, a warp's own: rows of K codes, with 16-byte pieces exchanged so that the eight
-// lanes that read at once meet different banks; rows of V codes, 16 bytes apart for the same reason; parameters of K and of V.
+// What a lane reads of 16 keys (gid = lane / 4, tig = lane % 4).  K: channels [16 tig, 16 tig + 16) of each group of keys gid and
+// gid + 8, and their parameters.  V: channels [8 gid, 8 gid + 8) of each group of tokens 2 tig, 2 tig + 1, 2 tig + 8 and 2 tig + 9, and
+// the parameters of keys gid and gid + 8.  Straight into registers: the next tile's K once this one's has been multiplied, its V at the end.
+// (Through shared memory by asynchronous copies the same took a hundred instructions more per tile, of which the kernel is short.)
 template <int D>
-struct Stage {
+struct Reader {
     using U = Unit<D>;
     static constexpr int G = U::kGroups;
-    static constexpr int kPieces = U::kRow / 16;                // of a row
-    static constexpr int kLdV = U::kRow + 16;
-    static constexpr int kOffV = kKeys * U::kRow;
-    static constexpr int kOffKP = kOffV + kKeys * kLdV;
-    static constexpr int kOffVP = kOffKP + kKeys * U::kPar;
-    static constexpr int kBytes = kOffVP + kKeys * U::kPar;
-    static __device__ __forceinline__ int k_piece(int row, int piece) { return row * U::kRow + (piece ^ (D == 128 ? (row & 2) : 0)) * 16; }
-
-    // A lane's part of the copying: where its pieces go in a stage, and where they come from in a unit.
-    struct Copier {
-        uint32_t to_k, to_v, to_p;
-        uint32_t from_v, from_p;
+    uint2 k[2][G];
+    uint32_t kp[2][G], v[4][G], vp[2][G];
+    // where a lane's parts are in a unit
+    struct Offsets {
+        uint32_t k, v, kp, vp;
     };
-    static constexpr int kParPieces = kKeys * U::kPar / 16;       // of K's parameters, and of V's
-    static __device__ __forceinline__ Copier copier(int page_tokens, int lane)
+    static __device__ __forceinline__ Offsets offsets(int page_tokens, int lane)
     {
-        const int row = lane / kPieces, piece = lane % kPieces, which = (lane / kParPieces) & 1, part = lane % kParPieces;
-        Copier c;
-        c.to_k = k_piece(row, piece);
-        c.to_v = kOffV + row * kLdV + piece * 16;
-        c.to_p = (which ? kOffVP : kOffKP) + part * 16;
-        c.from_v = U::v_codes(page_tokens);
-        c.from_p = (which ? U::v_par(page_tokens) : U::k_par(page_tokens)) + part * 16;
-        return c;
+        const int gid = lane >> 2, tig = lane & 3;
+        return Offsets{(uint32_t)(gid * U::kRow + tig * 8), (uint32_t)(U::v_codes(page_tokens) + 2 * tig * U::kRow + gid * 4),
+                       (uint32_t)(U::k_par(page_tokens) + gid * U::kPar), (uint32_t)(U::v_par(page_tokens) + gid * U::kPar)};
     }
-    // unit: the head's part of the page, slot: the first key's place in it
-    static __device__ __forceinline__ void copy(const Copier& c, uint32_t to, const uint8_t* unit, int slot, int lane)
+    __device__ __forceinline__ void load_k(const Offsets& o, const uint8_t* unit, int slot)
     {
-        const uint8_t* k = unit + (uint32_t)(slot * U::kRow + lane * 16);
-        const uint8_t* v = k + c.from_v;
-        constexpr int kRounds = kKeys * kPieces / 32, kRowsEach = kKeys / kRounds;     // (the same piece of rows kRowsEach further)
+        const uint8_t* at = unit + (o.k + (uint32_t)slot * U::kRow);
+        const uint8_t* par = unit + (o.kp + (uint32_t)slot * U::kPar);
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
-            copy16(to + c.to_k + i * kRowsEach * U::kRow, k + 512 * i);
-            copy16(to + c.to_v + i * kRowsEach * kLdV, v + 512 * i);
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) k[e][g] = load_once(reinterpret_cast<const uint2*>(at + 8 * e * U::kRow + g * 32));
+            params(par + 8 * e * U::kPar, kp[e]);
         }
-        if (lane < 2 * kParPieces) copy16(to + c.to_p, unit + (uint32_t)(slot * U::kPar) + c.from_p);
     }
-    static __device__ __forceinline__ void zero(uint8_t* to, int lane)
+    __device__ __forceinline__ void load_v(const Offsets& o, const uint8_t* unit, int slot)
     {
-        for (int i = lane * 16; i < kBytes; i += 512) *reinterpret_cast<uint4*>(to + i) = make_uint4(0, 0, 0, 0);
+        const uint8_t* at = unit + (o.v + (uint32_t)slot * U::kRow);
+        const uint8_t* par = unit + (o.vp + (uint32_t)slot * U::kPar);
+        params(par, vp[0]);
+        params(par + 8 * U::kPar, vp[1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int g = 0; g < G; ++g) v[e][g] = load_once(reinterpret_cast<const uint32_t*>(at + ((e & 1) + 8 * (e >> 1)) * U::kRow + g * 32));
+    }
+    static __device__ __forceinline__ void params(const uint8_t* at, uint32_t (&to)[G])
+    {
+        if constexpr (G == 2) {
+            const uint2 x = load_once(reinterpret_cast<const uint2*>(at));
+            to[0] = x.x;
+            to[1] = x.y;
+        } else {
+            to[0] = load_once(reinterpret_cast<const uint32_t*>(at));
+        }
     }
 };
 
@@ -339,18 +346,17 @@ template <int D, int kTiles, bool kSplit>
 struct RowsConfig {
     static constexpr int G = D / kCacheGroup;
     static constexpr int kRows = 8 * kTiles;
+    // key tiles of a warp's step, while there are registers for two: what a step costs beside them is then shared by 32 keys
+    static constexpr int kSteps = kTiles == 1 && !kSplit ? 2 : 1;
+    static constexpr int kChunk = kWarps * kSteps * kKeys;     // keys of a CTA's step
     static constexpr int kParts = kSplit ? 2 : 1;
-    static constexpr int kStages = 3;
     static constexpr int kLd = D + 1;
     // CTAs that an SM is to hold: by the registers of the output's fragments
-    static constexpr int kPerSm = D * kTiles <= 128 ? (kSplit ? 3 : 4) : D * kTiles <= 256 ? (kSplit ? 2 : 3) : 2;
-    // shared memory: the query operand and the keys on their way, then (over them) the warps' rows; per row its factor, its sums per
-    // group, the keys it sees
+    static constexpr int kPerSm = D * kTiles <= 128 ? 3 : 2;
+    // shared memory: the query operand, then (over it) the warps' rows; per row its factor, its sums per group, the keys it sees
     static constexpr int kQBytes = kParts * kRows * D * 2;
-    static constexpr int kStageAt = kQBytes;
-    static constexpr int kLoopBytes = kStageAt + kWarps * kStages * Stage<D>::kBytes;
     static constexpr int kMergeBytes = kWarps * kRows * (kLd + 2) * 4;
-    static constexpr int kInfo = (kLoopBytes > kMergeBytes ? kLoopBytes : kMergeBytes);
+    static constexpr int kInfo = (kQBytes > kMergeBytes ? kQBytes : kMergeBytes);
     static constexpr int kBytes = kInfo + kRows * (1 + G + 1) * 4;
 };
 
@@ -359,8 +365,8 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 {
     constexpr bool kSplit = sizeof(IO) == 4;
     using C = RowsConfig<D, kTiles, kSplit>;
-    using S = Stage<D>;
-    constexpr int G = C::G, kRows = C::kRows, kParts = C::kParts;
+    using Rd = Reader<D>;
+    constexpr int G = C::G, kRows = C::kRows, kParts = C::kParts, kSteps = C::kSteps, kChunk = C::kChunk;
     // The place of p * step in fp16's range: at most 2^14.  The reference maximum follows every larger score, so that the largest p is
     // exactly 1: its p * step then has no rounding against its p * minimum, which it nearly cancels with where the value is small.
     constexpr float kPlace = 16384.0f;
@@ -378,9 +384,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const int page_tokens = 1 << p.c.page_shift;
-    uint8_t* stages = smem + C::kStageAt + warp * C::kStages * S::kBytes;
-    const uint32_t stages_at = static_cast<uint32_t>(__cvta_generic_to_shared(stages));
-    const typename S::Copier copier = S::copier(page_tokens, lane);
+    const typename Rd::Offsets offsets = Rd::offsets(page_tokens, lane);
     grid_dependency_sync();
     const Cut cut = Planner<kRows, kChunk, false, kThreads>::cut(p, streams, (int)blockIdx.x, (int)gridDim.x, scratch, &slow);
     Walk<kRows, kChunk, false> walk(streams, cut, (int)blockIdx.x, (int)gridDim.x, true);
@@ -392,36 +396,43 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
         if (tid == 0 && seg.opens) (void)stream_tokens(p, b, true);
         __syncthreads();     // (shared memory of the item before has been read)
 
-        // ---- keys on their way.  Key tiles of this warp: chunk * kWarps + warp, up to c_end.  A lane holds where one of the next 32 is.
+        // ---- keys.  A warp's steps: chunk by chunk, kSteps tiles from key (c * kWarps + warp) * kSteps * kKeys on, up to c_end.  A lane holds
+        // where the tiles of one of 32 steps are, from step `held` on.
         const int32_t* table = p.c.table + (size_t)b * p.c.max_pages;
         const uint8_t* head = p.c.pages + (size_t)h * p.c.unit_bytes;
-        const int c_end = min(c1, (seen - warp * kKeys + kChunk - 1) / kChunk);
-        auto unit_of = [&](int c) {
-            if (c >= c_end) return (const uint8_t*)nullptr;
-            const uint32_t page = table[(c * kChunk + warp * kKeys) >> p.c.page_shift];
+        const int warp_key = warp * kSteps * kKeys;
+        const int c_end = min(c1, (seen - warp_key + kChunk - 1) / kChunk);
+        auto unit_of = [&](int key) {
+            if (key >= seen || key >= c1 * kChunk) return reinterpret_cast<const uint8_t*>(g_no_page);
+            const uint32_t page = table[key >> p.c.page_shift];
             if (page < (uint32_t)p.c.num_pages) return head + (size_t)page * ((size_t)p.c.kv_heads * p.c.unit_bytes);
             range_error(p.c.status, kRangePage, b);
-            return (const uint8_t*)nullptr;          // (reads as zeros)
+            return reinterpret_cast<const uint8_t*>(g_no_page);
         };
-        int turn = 0, stage_in = 0;                  // of the lane whose tile is next; byte offset of the stage it goes to
-        const uint8_t* my_unit = unit_of(c0 + lane);
-        int fetch_c = c0;
-        auto fetch = [&]() {
-            if (fetch_c < c_end) {
-                const uint8_t* unit = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_unit), turn));
-                if (unit != nullptr) S::copy(copier, stages_at + stage_in, unit, (fetch_c * kChunk + warp * kKeys) & (page_tokens - 1), lane);
-                else S::zero(stages + stage_in, lane);
-                ++fetch_c;
-                if (++turn == 32) {
-                    turn = 0;
-                    my_unit = unit_of(fetch_c + lane);
-                }
-            }
-            copies_commit();
-            stage_in = stage_in == (C::kStages - 1) * S::kBytes ? 0 : stage_in + S::kBytes;
-        };
+        int held = c0;
+        const uint8_t* my_unit[kSteps];
+        auto hold_units = [&]() {
 #pragma unroll
-        for (int i = 0; i < C::kStages - 1; ++i) fetch();
+            for (int u = 0; u < kSteps; ++u) my_unit[u] = unit_of((held + lane) * kChunk + warp_key + u * kKeys);
+        };
+        hold_units();
+        Rd raw[kSteps];
+        const uint8_t* unit[kSteps];
+        int slot[kSteps];
+        auto find = [&](int c) {       // where step c's tiles are
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u) {
+                unit[u] = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_unit[u]), c - held));
+                slot[u] = (c * kChunk + warp_key + u * kKeys) & (page_tokens - 1);
+            }
+        };
+        if (c0 < c_end) {
+            find(c0);
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u) raw[u].load_k(offsets, unit[u], slot[u]);
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u) raw[u].load_v(offsets, unit[u], slot[u]);
+        }
 
         // ---- the query rows: rotated, scaled into fp16's range, laid out as the instruction's second operand
         {
@@ -555,66 +566,42 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                 for (int g = 0; g < G; ++g) lows[t][e][g] = 0.0f;
             }
 
-        int stage_out = 0;
 #pragma unroll 1
         for (int c = c0; c < c_end; ++c) {
-            copies_wait<C::kStages - 2>();
-            __syncwarp();
-            const uint8_t* stage = stages + stage_out;
-            stage_out = stage_out == (C::kStages - 1) * S::kBytes ? 0 : stage_out + S::kBytes;
-            const int key0 = c * kChunk + warp * kKeys;
-            fetch();     // (into the stage that was read in the step before, by all lanes)
+            const int key0 = c * kChunk + warp_key;
 
-            // ---- sums of q * code per group
-            float acc[G][kTiles][4], rest[kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
+            // ---- scores of keys gid (x[u][t][0 .. 1]) and gid + 8 (x[u][t][2 .. 3]), still to be multiplied by the row's factor
+            float x[kSteps][kTiles][4];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                uint2 kw[2];
+            for (int u = 0; u < kSteps; ++u) {
+                // sums of q * code per group
+                float acc[G][kTiles][4], rest[kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int row = gid + 8 * e;
-                    kw[e] = *reinterpret_cast<const uint2*>(stage + S::k_piece(row, g * 2 + (tig >> 1)) + (tig & 1) * 8);
-                }
+                for (int g = 0; g < G; ++g) {
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const uint32_t w0 = (s & 2) ? kw[0].y : kw[0].x, w1 = (s & 2) ? kw[1].y : kw[1].x;
-                    const int i = 2 * (s & 1);
-                    const uint32_t a[4] = {operand_pair<kSplit>(w0, i), operand_pair<kSplit>(w1, i), operand_pair<kSplit>(w0, i + 1), operand_pair<kSplit>(w1, i + 1)};
+                    for (int s = 0; s < 4; ++s) {
+                        const uint32_t w0 = (s & 2) ? raw[u].k[0][g].y : raw[u].k[0][g].x, w1 = (s & 2) ? raw[u].k[1][g].y : raw[u].k[1][g].x;
+                        const int i = 2 * (s & 1);
+                        const uint32_t a[4] = {operand_pair<kSplit>(w0, i), operand_pair<kSplit>(w1, i), operand_pair<kSplit>(w0, i + 1), operand_pair<kSplit>(w1, i + 1)};
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
+                        for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
-                        for (int part = 0; part < kParts; ++part) {
-                            uint2 q;
-                            if constexpr (kKeep) q = kept[g][s];
-                            else q = q_operand(part, t, g, s);
-                            if (s == 0) mma16816_new(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
-                            else mma16816(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                            for (int part = 0; part < kParts; ++part) {
+                                uint2 q;
+                                if constexpr (kKeep) q = kept[g][s];
+                                else q = q_operand(part, t, g, s);
+                                if (s == 0) mma16816_new(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                                else mma16816(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                            }
                         }
                     }
                 }
-            }
-            // ---- parameters of keys gid and gid + 8; rows' scores x[t][0 .. 1] and x[t][2 .. 3] (still to be multiplied by the row's factor)
-            uint32_t kp[2][G], vp[2][G];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint8_t* at = stage + S::kOffKP + (gid + 8 * e) * S::U::kPar;
-                if constexpr (G == 2) {
-                    const uint2 a = *reinterpret_cast<const uint2*>(at), v = *reinterpret_cast<const uint2*>(at + S::kOffVP - S::kOffKP);
-                    kp[e][0] = a.x; kp[e][1] = a.y;
-                    vp[e][0] = v.x; vp[e][1] = v.y;
-                } else {
-                    kp[e][0] = *reinterpret_cast<const uint32_t*>(at);
-                    vp[e][0] = *reinterpret_cast<const uint32_t*>(at + S::kOffVP - S::kOffKP);
-                }
-            }
-            float x[kTiles][4];
-            {
                 float kl[2][G], ks[2][G];
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float2 a = unpack_half(kp[e][g]);
+                        const float2 a = unpack_half(raw[u].kp[e][g]);
                         kl[e][g] = kSplit ? fmaf(8.0f, a.y, a.x) : a.x;
                         ks[e][g] = a.y;
                     }
@@ -629,40 +616,65 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                             const float a = kSplit ? acc[g][t][e] + rest[kSplit ? g : 0][t][e] : acc[g][t][e];
                             s = g == 0 ? a * ks[e >> 1][g] : fmaf(a, ks[e >> 1][g], s);
                         }
-                        x[t][e] = fmaf(s, kSplit ? 1.0f : 16777216.0f, low);
+                        x[u][t][e] = fmaf(s, kSplit ? 1.0f : 16777216.0f, low);
                     }
             }
-            const bool edge = key0 + kKeys > fewest;     // some row does not see some of these keys
+            const bool more = c + 1 < c_end;
+            if (more) {
+                if (c + 1 - held == 32) {
+                    held = c + 1;
+                    hold_units();
+                }
+                find(c + 1);
+#pragma unroll
+                for (int u = 0; u < kSteps; ++u) raw[u].load_k(offsets, unit[u], slot[u]);
+            }
+            const bool edge = key0 + kSteps * kKeys > fewest;     // some row does not see some of these keys
             if (edge) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int key = key0 + gid + 8 * e;
-                    if (key >= have) {                   // nothing is there: whatever the memory holds stays out of the sums
+                for (int u = 0; u < kSteps; ++u)
 #pragma unroll
-                        for (int g = 0; g < G; ++g) vp[e][g] = 0;
+                    for (int e = 0; e < 2; ++e) {
+                        const int key = key0 + u * kKeys + gid + 8 * e;
+                        if (key >= have) {                   // nothing is there: whatever the memory holds stays out of the sums
+#pragma unroll
+                            for (int g = 0; g < G; ++g) raw[u].vp[e][g] = 0;
+                        }
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                            for (int f = 0; f < 2; ++f)
+                                if (key >= row_seen[8 * t + 2 * tig + f]) x[u][t][2 * e + f] = -INFINITY;
                     }
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                        for (int f = 0; f < 2; ++f)
-                            if (key >= row_seen[8 * t + 2 * tig + f]) x[t][2 * e + f] = -INFINITY;
-                }
             }
             // ---- reference maximum and the values' scale: renewed only where they have to be
             bool renew = false;
+            uint32_t v_most[G];      // (the step is the upper half, and not negative)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                v_most[g] = max(raw[0].vp[0][g], raw[0].vp[1][g]);
+#pragma unroll
+                for (int u = 1; u < kSteps; ++u) v_most[g] = max(v_most[g], max(raw[u].vp[0][g], raw[u].vp[1][g]));
+                renew |= v_most[g] > v_limit[g];
+            }
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) renew |= x[t][e] > top[t][e & 1];
+                for (int f = 0; f < 2; ++f) {
+                    float mx = fmaxf(x[0][t][f], x[0][t][2 + f]);
 #pragma unroll
-            for (int g = 0; g < G; ++g) renew |= max(vp[0][g], vp[1][g]) > v_limit[g];      // (the step is the upper half, and not negative)
+                    for (int u = 1; u < kSteps; ++u) mx = fmaxf(mx, fmaxf(x[u][t][f], x[u][t][2 + f]));
+                    renew |= mx > top[t][f];
+                }
             if (__any_sync(0xffffffffu, renew)) {
                 float down[kTiles][2];
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
-                        float mx = fmaxf(x[t][f], x[t][2 + f]);
+                        float mx = fmaxf(x[0][t][f], x[0][t][2 + f]);
+#pragma unroll
+                        for (int u = 1; u < kSteps; ++u) mx = fmaxf(mx, fmaxf(x[u][t][f], x[u][t][2 + f]));
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                         down[t][f] = 1.0f;
@@ -678,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                     }
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    uint32_t most = __reduce_max_sync(0xffffffffu, max(vp[0][g], vp[1][g])) >> 16;
+                    const uint32_t most = __reduce_max_sync(0xffffffffu, v_most[g]) >> 16;
                     float shrink = 1.0f;
                     if (most > (v_limit[g] >> 16) && most < 0x7c00u) {
                         // kPlace over the next power of two above the step, as far as fp16 goes
@@ -700,80 +712,84 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                 }
             }
             // ---- p, and p * step per group as the instruction's second operand
-            uint32_t pb[kParts][kTiles][G][2];
+            uint32_t pb[kSteps][kParts][kTiles][G][2];
             auto weigh = [&](auto masked) {
                 constexpr bool kMasked = decltype(masked)::value;
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    float pr[4];
-                    bool hidden[4];
+                for (int u = 0; u < kSteps; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        // (with a fused product the largest would not be 1)
-                        pr[e] = exp2_fast(__fsub_rn(__fmul_rn(x[t][e], scale[t][e & 1]), m_ref[t][e & 1]));
-                        hidden[e] = kMasked && x[t][e] == -INFINITY;
-                        if (kMasked && hidden[e]) pr[e] = 0.0f;          // (its factor may be NaN)
-                        l[t][e & 1] += pr[e];
-                    }
+                    for (int t = 0; t < kTiles; ++t) {
+                        float pr[4];
+                        bool hidden[4];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t p2 = kSplit ? 0u : pack_half(pr[2 * e], pr[2 * e + 1]);
-                        // a NaN or an infinity that a row does not see is not to reach it as 0 * NaN
-                        const uint32_t keep = (hidden[2 * e] ? 0u : 0xffffu) | (hidden[2 * e + 1] ? 0u : 0xffff0000u);
+                        for (int e = 0; e < 4; ++e) {
+                            // (with a fused product the largest would not be 1)
+                            pr[e] = exp2_fast(__fsub_rn(__fmul_rn(x[u][t][e], scale[t][e & 1]), m_ref[t][e & 1]));
+                            hidden[e] = kMasked && x[u][t][e] == -INFINITY;
+                            if (kMasked && hidden[e]) pr[e] = 0.0f;          // (its factor may be NaN)
+                            l[t][e & 1] += pr[e];
+                        }
 #pragma unroll
-                        for (int g = 0; g < G; ++g) {
-                            const float2 v = unpack_half(vp[e][g]);
-                            const float vl = kSplit ? fmaf(8.0f, v.y, v.x) : v.x;
-                            uint32_t hi, lo = 0;
-                            if constexpr (kSplit) {
-                                const float s = v.y * v_mul[g], y0 = pr[2 * e] * s, y1 = pr[2 * e + 1] * s;
-                                hi = pack_half(y0, y1);
-                                const float2 back = unpack_half(hi);
-                                lo = pack_half(y0 - back.x, y1 - back.y);
-                            } else {
-                                hi = mul_half2(p2, mul_half2(__byte_perm(vp[e][g], 0, 0x3232), v_mul2[g]));
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t p2 = kSplit ? 0u : pack_half(pr[2 * e], pr[2 * e + 1]);
+                            // a NaN or an infinity that a row does not see is not to reach it as 0 * NaN
+                            const uint32_t keep = (hidden[2 * e] ? 0u : 0xffffu) | (hidden[2 * e + 1] ? 0u : 0xffff0000u);
+#pragma unroll
+                            for (int g = 0; g < G; ++g) {
+                                const float2 v = unpack_half(raw[u].vp[e][g]);
+                                const float vl = kSplit ? fmaf(8.0f, v.y, v.x) : v.x;
+                                uint32_t hi, lo = 0;
+                                if constexpr (kSplit) {
+                                    const float s = v.y * v_mul[g], y0 = pr[2 * e] * s, y1 = pr[2 * e + 1] * s;
+                                    hi = pack_half(y0, y1);
+                                    const float2 back = unpack_half(hi);
+                                    lo = pack_half(y0 - back.x, y1 - back.y);
+                                } else {
+                                    hi = mul_half2(p2, mul_half2(__byte_perm(raw[u].vp[e][g], 0, 0x3232), v_mul2[g]));
+                                }
+                                if (!(kMasked && hidden[2 * e])) lows[t][0][g] = fmaf(pr[2 * e], vl, lows[t][0][g]);
+                                if (!(kMasked && hidden[2 * e + 1])) lows[t][1][g] = fmaf(pr[2 * e + 1], vl, lows[t][1][g]);
+                                if (kMasked) {
+                                    hi &= keep;
+                                    lo &= keep;
+                                }
+                                pb[u][0][t][g][e] = transpose8x8(hi);
+                                if constexpr (kSplit) pb[u][kParts - 1][t][g][e] = transpose8x8(lo);
                             }
-                            if (!(kMasked && hidden[2 * e])) lows[t][0][g] = fmaf(pr[2 * e], vl, lows[t][0][g]);
-                            if (!(kMasked && hidden[2 * e + 1])) lows[t][1][g] = fmaf(pr[2 * e + 1], vl, lows[t][1][g]);
-                            if (kMasked) {
-                                hi &= keep;
-                                lo &= keep;
-                            }
-                            pb[0][t][g][e] = transpose8x8(hi);
-                            if constexpr (kSplit) pb[kParts - 1][t][g][e] = transpose8x8(lo);
                         }
                     }
-                }
             };
             if (edge) weigh(std::true_type());
             else weigh(std::false_type());
             // ---- O^T += V^T P^T, 16 channels at a time: rows gid and gid + 8 are channels 8 gid + m and 8 gid + 4 + m of the group
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                uint32_t vw[4];
+            for (int u = 0; u < kSteps; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(stage + S::kOffV + (2 * tig + (e & 1) + 8 * (e >> 1)) * S::kLdV + g * 32 + gid * 4);
-                const uint32_t a_lo = __byte_perm(vw[0], vw[1], 0x5410), a_hi = __byte_perm(vw[0], vw[1], 0x7632);
-                const uint32_t b_lo = __byte_perm(vw[2], vw[3], 0x5410), b_hi = __byte_perm(vw[2], vw[3], 0x7632);
+                for (int g = 0; g < G; ++g) {
+                    const uint32_t a_lo = __byte_perm(raw[u].v[0][g], raw[u].v[1][g], 0x5410), a_hi = __byte_perm(raw[u].v[0][g], raw[u].v[1][g], 0x7632);
+                    const uint32_t b_lo = __byte_perm(raw[u].v[2][g], raw[u].v[3][g], 0x5410), b_hi = __byte_perm(raw[u].v[2][g], raw[u].v[3][g], 0x7632);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const uint32_t a[4] = {operand_pair<kSplit>(a_lo, m), operand_pair<kSplit>(a_hi, m), operand_pair<kSplit>(b_lo, m), operand_pair<kSplit>(b_hi, m)};
+                    for (int m = 0; m < 4; ++m) {
+                        const uint32_t a[4] = {operand_pair<kSplit>(a_lo, m), operand_pair<kSplit>(a_hi, m), operand_pair<kSplit>(b_lo, m), operand_pair<kSplit>(b_hi, m)};
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
-                        if constexpr (kSplit) {     // added up by fp32 additions, which round
-                            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                            mma16816(sum, a, pb[kParts - 1][t][g][0], pb[kParts - 1][t][g][1]);
-                            mma16816(sum, a, pb[0][t][g][0], pb[0][t][g][1]);
+                        for (int t = 0; t < kTiles; ++t) {
+                            if constexpr (kSplit) {     // added up by fp32 additions, which round
+                                float sum[4];
+                                mma16816_new(sum, a, pb[u][kParts - 1][t][g][0], pb[u][kParts - 1][t][g][1]);
+                                mma16816(sum, a, pb[u][0][t][g][0], pb[u][0][t][g][1]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[g][m][t][e] += sum[e];
-                        } else {
-                            mma16816(o[g][m][t], a, pb[0][t][g][0], pb[0][t][g][1]);
+                                for (int e = 0; e < 4; ++e) o[g][m][t][e] += sum[e];
+                            } else {
+                                mma16816(o[g][m][t], a, pb[u][0][t][g][0], pb[u][0][t][g][1]);
+                            }
                         }
                     }
                 }
+            if (more) {
+#pragma unroll
+                for (int u = 0; u < kSteps; ++u) raw[u].load_v(offsets, unit[u], slot[u]);
             }
         }
-        copies_wait<0>();
 
         // ---- the warps' rows meet in shared memory
 #pragma unroll
@@ -819,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             const int flat = rb * kRows + r, i = flat / p.rep, q_head = h * p.rep + flat - i * p.rep;
             static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + q_head) * D + ch] = static_cast<IO>(value);
         };
-        const int slot = parts.slot((int)blockIdx.x);
+        const int part_slot = parts.slot((int)blockIdx.x);
         for (int x = tid; x < rows * D; x += kThreads) {
             const int r = x / D, ch = x - r * D;
             float m = -INFINITY;
@@ -835,8 +851,8 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             }
             if (parts.count == 1) write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
             else {
-                p.part_o[((size_t)slot * kRows + r) * D + ch] = sum;
-                if (ch == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)slot * kRows + r) * 2) = make_float2(m, total);
+                p.part_o[((size_t)part_slot * kRows + r) * D + ch] = sum;
+                if (ch == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)part_slot * kRows + r) * 2) = make_float2(m, total);
             }
         }
         if (parts.count > 1) {
@@ -851,42 +867,54 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             if (last_part) {
                 __threadfence();
                 if (tid == 0) p.tickets[parts.first] = 0;      // as it was found
-                // their common reference maximum, then each warp a fourth of the parts, several rows asked for at once, and the warps' sums
-                for (int r = warp; r < rows; r += kWarps) {
+                // The common reference maximum of a row, then its parts.  With few rows each warp takes a fourth of the parts; with more, a row.
+                constexpr int kPer = D / 32;
+                const int shared_by = rows < kWarps ? kWarps : 1, lead = shared_by == 1 ? 0 : warp;
+                for (int r = shared_by == 1 ? warp : 0; r < rows; r += shared_by == 1 ? kWarps : 1) {
                     float m = -INFINITY;
                     for (int w = lane; w < parts.count; w += 32) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)parts.slot(parts.first + w) * kRows + r) * 2));
 #pragma unroll
                     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                    if (lane == 0) row_scale[r] = m == -INFINITY ? 0.0f : m;
-                }
-                __syncthreads();
-                constexpr int kPer = D / 32;
-                for (int r = 0; r < rows; ++r) {
-                    const float m = row_scale[r];
+                    if (m == -INFINITY) m = 0.0f;
                     float sum[kPer], total = 0.0f;
 #pragma unroll
                     for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
-#pragma unroll 8
-                    for (int w = warp; w < parts.count; w += kWarps) {
-                        const size_t s = (size_t)parts.slot(parts.first + w) * kRows + r;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + s * 2));
-                        float x[kPer];
-                        if constexpr (kPer == 4) {
-                            const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + s * D) + lane);
-                            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-                        } else {
-                            const float2 v = __ldcg(reinterpret_cast<const float2*>(p.part_o + s * D) + lane);
-                            x[0] = v.x; x[1] = v.y;
+                    constexpr int kBatch = 8;       // parts asked for at once
+                    for (int w0 = lead; w0 < parts.count; w0 += kBatch * shared_by) {
+                        float2 ml[kBatch];
+                        float x[kBatch][kPer];
+#pragma unroll
+                        for (int k = 0; k < kBatch; ++k) {
+                            const int w = min(w0 + k * shared_by, parts.count - 1);
+                            const size_t s = (size_t)parts.slot(parts.first + w) * kRows + r;
+                            ml[k] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + s * 2));
+                            if constexpr (kPer == 4) {
+                                const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + s * D) + lane);
+                                x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
+                            } else {
+                                const float2 v = __ldcg(reinterpret_cast<const float2*>(p.part_o + s * D) + lane);
+                                x[k][0] = v.x; x[k][1] = v.y;
+                            }
                         }
-                        const float f = exp2_fast(ml.x - m);
-                        total = fmaf(ml.y, f, total);
 #pragma unroll
-                        for (int e = 0; e < kPer; ++e) sum[e] = fmaf(x[e], f, sum[e]);
+                        for (int k = 0; k < kBatch; ++k) {
+                            if (w0 + k * shared_by >= parts.count) break;
+                            const float f = exp2_fast(ml[k].x - m);
+                            total = fmaf(ml[k].y, f, total);
+#pragma unroll
+                            for (int e = 0; e < kPer; ++e) sum[e] = fmaf(x[k][e], f, sum[e]);
+                        }
                     }
+                    if (shared_by == 1) {
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e) merge_o[(warp * kRows + r) * C::kLd + lane * kPer + e] = sum[e];
-                    if (lane == 0) merge_ml[(warp * kRows + r) * 2 + 1] = total;
+                        for (int e = 0; e < kPer; ++e) write_row(r, lane * kPer + e, total == 0.0f ? 0.0f : sum[e] / total);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) merge_o[(warp * kRows + r) * C::kLd + lane * kPer + e] = sum[e];
+                        if (lane == 0) merge_ml[(warp * kRows + r) * 2 + 1] = total;
+                    }
                 }
+                if (shared_by == 1) continue;
                 __syncthreads();
                 for (int x = tid; x < rows * D; x += kThreads) {
                     const int r = x / D, ch = x - r * D;
@@ -944,8 +972,8 @@ int launch_attend(CacheAttendArgs& a, cudaStream_t st)
     }
     a.row_blocks = (a.queries * a.rep + C::kRows - 1) / C::kRows;
     a.min_share = 2;
-    a.max_parts = kTiles == 1 ? 64 : kTiles == 2 ? 32 : 16;
-    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * ((((long long)a.c.max_pages << a.c.page_shift) + kChunk - 1) / kChunk);
+    a.max_parts = kTiles == 1 ? 64 : 32;
+    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * ((((long long)a.c.max_pages << a.c.page_shift) + C::kChunk - 1) / C::kChunk);
     long long grid = ctas;
     if (grid > kCacheCtas) grid = kCacheCtas;
     if (grid > most) grid = most;
@@ -959,7 +987,7 @@ int attend_any(CacheAttendArgs& a, int dtype, cudaStream_t st)
 {
     const int rows = a.queries * a.rep;
     if (dtype == ARL2_FP32) return rows <= 8 ? launch_attend<D, float, 1>(a, st) : launch_attend<D, float, 2>(a, st);
-    return rows <= 8 ? launch_attend<D, __nv_bfloat16, 1>(a, st) : rows <= 16 ? launch_attend<D, __nv_bfloat16, 2>(a, st) : launch_attend<D, __nv_bfloat16, 4>(a, st);
+    return rows <= 8 ? launch_attend<D, __nv_bfloat16, 1>(a, st) : launch_attend<D, __nv_bfloat16, 2>(a, st);
 }
 
 }  // namespace
@@ -972,7 +1000,7 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
 
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)
 {
-    if (a.tensor_cores && a.queries * a.rep > 32) return tc_cache_attend(a, st);
+    if (a.tensor_cores && a.queries * a.rep > 16) return tc_cache_attend(a, st);
     return a.D == 128 ? attend_any<128>(a, dtype, st) : attend_any<64>(a, dtype, st);
 }
 
