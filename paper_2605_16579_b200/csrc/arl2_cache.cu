@@ -273,70 +273,96 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b)
     return *reinterpret_cast<const uint32_t*>(&d);
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
-// (cached rows are read once, by one SM)
-__device__ __forceinline__ uint32_t load_once(const uint32_t* p)
+// 16 bytes to shared memory in the background
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
 {
-    uint32_t v;
-    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ uint2 load_once(const uint2* p)
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+// four 8 x 8 matrices of 16-bit words; the lanes of each eight name the rows of one
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at)
 {
-    uint2 v;
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load_matrices_transposed(uint32_t (&r)[4], uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 
-// What a lane reads of 16 keys (gid = lane / 4, tig = lane % 4).  K: channels [16 tig, 16 tig + 16) of each group of keys gid and
-// gid + 8, and their parameters.  V: channels [8 gid, 8 gid + 8) of each group of tokens 2 tig, 2 tig + 1, 2 tig + 8 and 2 tig + 9, and
-// the parameters of keys gid and gid + 8.  Straight into registers: the next tile's K once this one's has been multiplied, its V at the end.
-// (Through shared memory by asynchronous copies the same took a hundred instructions more per tile, of which the kernel is short.)
+// 16 keys of a warp in shared memory: K codes | V codes | parameters of K | of V.  A row of codes is kPieces 16-byte pieces, exchanged by
+// the row's number so that eight rows' pieces lie in different banks.  Read as 8 x 8 matrices of 16-bit words (gid = lane / 4, tig =
+// lane % 4), K gives a lane the words tig of all pieces of keys gid and gid + 8, and V, transposed, the words gid of tokens 2 tig and
+// 2 tig + 1 side by side, as the second product wants them.
 template <int D>
-struct Reader {
+struct Tile {
     using U = Unit<D>;
     static constexpr int G = U::kGroups;
-    uint2 k[2][G];
-    uint32_t kp[2][G], v[4][G], vp[2][G];
-    // where a lane's parts are in a unit
-    struct Offsets {
-        uint32_t k, v, kp, vp;
-    };
-    static __device__ __forceinline__ Offsets offsets(int page_tokens, int lane)
+    static constexpr int kPieces = U::kRow / 16;
+    static constexpr int kCodes = kKeys * U::kRow, kParams = kKeys * U::kPar;
+    static constexpr int kBytes = 2 * kCodes + 2 * kParams;
+    static_assert(kBytes % 128 == 0, "pieces of a tile keep their banks");
+    static __device__ __forceinline__ uint32_t piece_at(int row, int piece)
     {
-        const int gid = lane >> 2, tig = lane & 3;
-        return Offsets{(uint32_t)(gid * U::kRow + tig * 8), (uint32_t)(U::v_codes(page_tokens) + 2 * tig * U::kRow + gid * 4),
-                       (uint32_t)(U::k_par(page_tokens) + gid * U::kPar), (uint32_t)(U::v_par(page_tokens) + gid * U::kPar)};
+        return row * U::kRow + ((piece ^ (kPieces == 4 ? (row >> 1) & 3 : (row >> 2) & 1)) << 4);
     }
-    __device__ __forceinline__ void load_k(const Offsets& o, const uint8_t* unit, int slot)
+    // a lane's part: where its pieces come from and go to, and the rows that it names when matrices are read
+    struct Lane {
+        uint32_t from_v, from_p, to, to_p, read;
+    };
+    static __device__ __forceinline__ Lane lane_part(int page_tokens, int lane)
     {
-        const uint8_t* at = unit + (o.k + (uint32_t)slot * U::kRow);
-        const uint8_t* par = unit + (o.kp + (uint32_t)slot * U::kPar);
+        constexpr int kParPieces = kParams / 16;
+        Lane x;
+        x.to = piece_at(lane / kPieces, lane % kPieces);
+        x.from_v = U::v_codes(page_tokens);
+        x.from_p = (lane < kParPieces ? U::k_par(page_tokens) : U::v_par(page_tokens)) + (lane % kParPieces) * 16;
+        x.to_p = 2 * kCodes + lane * 16;
+        // matrices: the pieces of rows 0 .. 7 (and, where a row has two, of rows 8 .. 15)
+        x.read = kPieces == 4 ? piece_at(lane & 7, lane >> 3) : piece_at((lane & 7) + 8 * (lane >> 4), (lane >> 3) & 1);
+        return x;
+    }
+    // unit: the head's part of the page, slot: the first key's place in it
+    static __device__ __forceinline__ void copy(const Lane& x, uint32_t to, const uint8_t* unit, int slot, int lane)
+    {
+        const uint8_t* k = unit + (uint32_t)(slot * U::kRow + lane * 16);
+        const uint8_t* v = k + x.from_v;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int i = 0; i < kCodes / 512; ++i) {      // (the next 32 pieces: eight rows on, exchanged in the same way)
+            copy16(to + x.to + 512 * i, k + 512 * i);
+            copy16(to + x.to + kCodes + 512 * i, v + 512 * i);
+        }
+        if (lane < 2 * kParams / 16) copy16(to + x.to_p, unit + (uint32_t)(slot * U::kPar) + x.from_p);
+    }
+    // K: word j of group g of keys gid (e = 0) and gid + 8; V: w[e][g][upper] of tokens 8 e + 2 tig, + 1
+    static __device__ __forceinline__ void codes(uint32_t (&w)[2][G][2], const Lane& x, uint32_t at, bool transposed)
+    {
+        uint32_t r[4];
+        if constexpr (kPieces == 4) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) k[e][g] = load_once(reinterpret_cast<const uint2*>(at + 8 * e * U::kRow + g * 32));
-            params(par + 8 * e * U::kPar, kp[e]);
+            for (int e = 0; e < 2; ++e) {
+                if (transposed) load_matrices_transposed(r, at + x.read + 8 * e * U::kRow);
+                else load_matrices(r, at + x.read + 8 * e * U::kRow);
+                w[e][0][0] = r[0]; w[e][0][1] = r[1];
+                w[e][G - 1][0] = r[2]; w[e][G - 1][1] = r[3];
+            }
+        } else {
+            if (transposed) load_matrices_transposed(r, at + x.read);
+            else load_matrices(r, at + x.read);
+            w[0][0][0] = r[0]; w[0][0][1] = r[1];
+            w[1][0][0] = r[2]; w[1][0][1] = r[3];
         }
     }
-    __device__ __forceinline__ void load_v(const Offsets& o, const uint8_t* unit, int slot)
+    static __device__ __forceinline__ void params(uint32_t (&to)[G], const uint8_t* tile, int which, int key)
     {
-        const uint8_t* at = unit + (o.v + (uint32_t)slot * U::kRow);
-        const uint8_t* par = unit + (o.vp + (uint32_t)slot * U::kPar);
-        params(par, vp[0]);
-        params(par + 8 * U::kPar, vp[1]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int g = 0; g < G; ++g) v[e][g] = load_once(reinterpret_cast<const uint32_t*>(at + ((e & 1) + 8 * (e >> 1)) * U::kRow + g * 32));
-    }
-    static __device__ __forceinline__ void params(const uint8_t* at, uint32_t (&to)[G])
-    {
+        const uint8_t* at = tile + 2 * kCodes + which * kParams + key * U::kPar;
         if constexpr (G == 2) {
-            const uint2 x = load_once(reinterpret_cast<const uint2*>(at));
+            const uint2 x = *reinterpret_cast<const uint2*>(at);
             to[0] = x.x;
-            to[1] = x.y;
+            to[G - 1] = x.y;
         } else {
-            to[0] = load_once(reinterpret_cast<const uint32_t*>(at));
+            to[0] = *reinterpret_cast<const uint32_t*>(at);
         }
     }
 };
@@ -353,10 +379,12 @@ struct RowsConfig {
     static constexpr int kLd = D + 1;
     // CTAs that an SM is to hold: by the registers of the output's fragments
     static constexpr int kPerSm = D * kTiles <= 128 ? 3 : 2;
-    // shared memory: the query operand, then (over it) the warps' rows; per row its factor, its sums per group, the keys it sees
+    static constexpr int kStages = 3;         // steps of keys on their way or being read
+    // shared memory: the query operand and the keys, then (over them) the warps' rows; per row its factor, its sums per group, the keys it sees
     static constexpr int kQBytes = kParts * kRows * D * 2;
+    static constexpr int kLoopBytes = kQBytes + kWarps * kStages * kSteps * Tile<D>::kBytes;
     static constexpr int kMergeBytes = kWarps * kRows * (kLd + 2) * 4;
-    static constexpr int kInfo = (kQBytes > kMergeBytes ? kQBytes : kMergeBytes);
+    static constexpr int kInfo = (kLoopBytes > kMergeBytes ? kLoopBytes : kMergeBytes);
     static constexpr int kBytes = kInfo + kRows * (1 + G + 1) * 4;
 };
 
@@ -365,12 +393,12 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 {
     constexpr bool kSplit = sizeof(IO) == 4;
     using C = RowsConfig<D, kTiles, kSplit>;
-    using Rd = Reader<D>;
+    using T = Tile<D>;
     constexpr int G = C::G, kRows = C::kRows, kParts = C::kParts, kSteps = C::kSteps, kChunk = C::kChunk;
     // The place of p * step in fp16's range: at most 2^14.  The reference maximum follows every larger score, so that the largest p is
     // exactly 1: its p * step then has no rounding against its p * minimum, which it nearly cancels with where the value is small.
     constexpr float kPlace = 16384.0f;
-    extern __shared__ __align__(16) uint8_t smem[];
+    extern __shared__ __align__(128) uint8_t smem[];
     __half* q_frag = reinterpret_cast<__half*>(smem);          // [part][tile][group][k-step][lane][4]
     float* merge_o = reinterpret_cast<float*>(smem);           // [warp][row][kLd]
     float* merge_ml = merge_o + kWarps * kRows * C::kLd;       // [warp][row][2]
@@ -384,7 +412,10 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const int page_tokens = 1 << p.c.page_shift;
-    const typename Rd::Offsets offsets = Rd::offsets(page_tokens, lane);
+    constexpr int kStepBytes = kSteps * T::kBytes;
+    const typename T::Lane mine = T::lane_part(page_tokens, lane);
+    uint8_t* keys = smem + C::kQBytes + warp * C::kStages * kStepBytes;
+    const uint32_t keys_at = static_cast<uint32_t>(__cvta_generic_to_shared(keys));
     grid_dependency_sync();
     const Cut cut = Planner<kRows, kChunk, false, kThreads>::cut(p, streams, (int)blockIdx.x, (int)gridDim.x, scratch, &slow);
     Walk<kRows, kChunk, false> walk(streams, cut, (int)blockIdx.x, (int)gridDim.x, true);
@@ -416,23 +447,25 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             for (int u = 0; u < kSteps; ++u) my_unit[u] = unit_of((held + lane) * kChunk + warp_key + u * kKeys);
         };
         hold_units();
-        Rd raw[kSteps];
-        const uint8_t* unit[kSteps];
-        int slot[kSteps];
-        auto find = [&](int c) {       // where step c's tiles are
+        int fetched = c0, stage_in = 0;      // the next step to ask for, and where it goes
+        auto fetch = [&]() {
+            if (fetched < c_end) {
+                if (fetched - held == 32) {
+                    held = fetched;
+                    hold_units();
+                }
 #pragma unroll
-            for (int u = 0; u < kSteps; ++u) {
-                unit[u] = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_unit[u]), c - held));
-                slot[u] = (c * kChunk + warp_key + u * kKeys) & (page_tokens - 1);
+                for (int u = 0; u < kSteps; ++u) {
+                    const uint8_t* unit = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_unit[u]), fetched - held));
+                    T::copy(mine, keys_at + stage_in + u * T::kBytes, unit, (fetched * kChunk + warp_key + u * kKeys) & (page_tokens - 1), lane);
+                }
+                ++fetched;
+                stage_in = stage_in == (C::kStages - 1) * kStepBytes ? 0 : stage_in + kStepBytes;
             }
+            copies_commit();
         };
-        if (c0 < c_end) {
-            find(c0);
 #pragma unroll
-            for (int u = 0; u < kSteps; ++u) raw[u].load_k(offsets, unit[u], slot[u]);
-#pragma unroll
-            for (int u = 0; u < kSteps; ++u) raw[u].load_v(offsets, unit[u], slot[u]);
-        }
+        for (int i = 0; i < C::kStages - 1; ++i) fetch();
 
         // ---- the query rows: rotated, scaled into fp16's range, laid out as the instruction's second operand
         {
@@ -498,9 +531,9 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                 if ((lane % (32 / G)) == 0) row_sum[r * G + lane / (32 / G)] = sum;
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
-                    // channel c of its group: lane quarter c / 16, word (c / 8) % 2, code c % 8 of the word
+                    // channel c of its group: lane tig = (c / 8) % 4, word c / 32, code c % 8 of the word
                     const int c = lane * kPer + e, cg = c & 63, g = c >> 6;
-                    const int quarter = cg >> 4, word = (cg >> 3) & 1, i = cg & 3, upper = (cg >> 2) & 1;
+                    const int quarter = (cg >> 3) & 3, word = cg >> 5, i = cg & 3, upper = (cg >> 2) & 1;
                     const int step = 2 * word + (i >> 1), reg = i & 1;
                     const float y = reg && !kSplit ? x[k][e] * 0.0625f : x[k][e];      // (odd codes are 2^4 larger)
                     const __half hi = __float2half_rn(y);
@@ -566,21 +599,32 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                 for (int g = 0; g < G; ++g) lows[t][e][g] = 0.0f;
             }
 
+        int stage_out = 0;
 #pragma unroll 1
         for (int c = c0; c < c_end; ++c) {
             const int key0 = c * kChunk + warp_key;
+            copies_wait<C::kStages - 2>();
+            __syncwarp();
+            fetch();     // (to where the step before was, which all lanes have read)
+            const uint32_t step_at = keys_at + stage_out;
+            const uint8_t* step = keys + stage_out;
+            stage_out = stage_out == (C::kStages - 1) * kStepBytes ? 0 : stage_out + kStepBytes;
 
             // ---- scores of keys gid (x[u][t][0 .. 1]) and gid + 8 (x[u][t][2 .. 3]), still to be multiplied by the row's factor
             float x[kSteps][kTiles][4];
 #pragma unroll
             for (int u = 0; u < kSteps; ++u) {
+                uint32_t kw[2][G][2], kp[2][G];
+                T::codes(kw, mine, step_at + u * T::kBytes, false);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) T::params(kp[e], step + u * T::kBytes, 0, gid + 8 * e);
                 // sums of q * code per group
                 float acc[G][kTiles][4], rest[kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        const uint32_t w0 = (s & 2) ? raw[u].k[0][g].y : raw[u].k[0][g].x, w1 = (s & 2) ? raw[u].k[1][g].y : raw[u].k[1][g].x;
+                        const uint32_t w0 = kw[0][g][s >> 1], w1 = kw[1][g][s >> 1];
                         const int i = 2 * (s & 1);
                         const uint32_t a[4] = {operand_pair<kSplit>(w0, i), operand_pair<kSplit>(w1, i), operand_pair<kSplit>(w0, i + 1), operand_pair<kSplit>(w1, i + 1)};
 #pragma unroll
@@ -601,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float2 a = unpack_half(raw[u].kp[e][g]);
+                        const float2 a = unpack_half(kp[e][g]);
                         kl[e][g] = kSplit ? fmaf(8.0f, a.y, a.x) : a.x;
                         ks[e][g] = a.y;
                     }
@@ -619,16 +663,11 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                         x[u][t][e] = fmaf(s, kSplit ? 1.0f : 16777216.0f, low);
                     }
             }
-            const bool more = c + 1 < c_end;
-            if (more) {
-                if (c + 1 - held == 32) {
-                    held = c + 1;
-                    hold_units();
-                }
-                find(c + 1);
+            uint32_t vp[kSteps][2][G];
 #pragma unroll
-                for (int u = 0; u < kSteps; ++u) raw[u].load_k(offsets, unit[u], slot[u]);
-            }
+            for (int u = 0; u < kSteps; ++u)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) T::params(vp[u][e], step + u * T::kBytes, 1, gid + 8 * e);
             const bool edge = key0 + kSteps * kKeys > fewest;     // some row does not see some of these keys
             if (edge) {
 #pragma unroll
@@ -638,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                         const int key = key0 + u * kKeys + gid + 8 * e;
                         if (key >= have) {                   // nothing is there: whatever the memory holds stays out of the sums
 #pragma unroll
-                            for (int g = 0; g < G; ++g) raw[u].vp[e][g] = 0;
+                            for (int g = 0; g < G; ++g) vp[u][e][g] = 0;
                         }
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t)
@@ -652,9 +691,9 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             uint32_t v_most[G];      // (the step is the upper half, and not negative)
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                v_most[g] = max(raw[0].vp[0][g], raw[0].vp[1][g]);
+                v_most[g] = max(vp[0][0][g], vp[0][1][g]);
 #pragma unroll
-                for (int u = 1; u < kSteps; ++u) v_most[g] = max(v_most[g], max(raw[u].vp[0][g], raw[u].vp[1][g]));
+                for (int u = 1; u < kSteps; ++u) v_most[g] = max(v_most[g], max(vp[u][0][g], vp[u][1][g]));
                 renew |= v_most[g] > v_limit[g];
             }
 #pragma unroll
@@ -736,7 +775,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                             const uint32_t keep = (hidden[2 * e] ? 0u : 0xffffu) | (hidden[2 * e + 1] ? 0u : 0xffff0000u);
 #pragma unroll
                             for (int g = 0; g < G; ++g) {
-                                const float2 v = unpack_half(raw[u].vp[e][g]);
+                                const float2 v = unpack_half(vp[u][e][g]);
                                 const float vl = kSplit ? fmaf(8.0f, v.y, v.x) : v.x;
                                 uint32_t hi, lo = 0;
                                 if constexpr (kSplit) {
@@ -745,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                                     const float2 back = unpack_half(hi);
                                     lo = pack_half(y0 - back.x, y1 - back.y);
                                 } else {
-                                    hi = mul_half2(p2, mul_half2(__byte_perm(raw[u].vp[e][g], 0, 0x3232), v_mul2[g]));
+                                    hi = mul_half2(p2, mul_half2(__byte_perm(vp[u][e][g], 0, 0x3232), v_mul2[g]));
                                 }
                                 if (!(kMasked && hidden[2 * e])) lows[t][0][g] = fmaf(pr[2 * e], vl, lows[t][0][g]);
                                 if (!(kMasked && hidden[2 * e + 1])) lows[t][1][g] = fmaf(pr[2 * e + 1], vl, lows[t][1][g]);
@@ -761,16 +800,16 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             };
             if (edge) weigh(std::true_type());
             else weigh(std::false_type());
-            // ---- O^T += V^T P^T, 16 channels at a time: rows gid and gid + 8 are channels 8 gid + m and 8 gid + 4 + m of the group
+            // ---- O^T += V^T P^T, 16 channels at a time: rows gid and gid + 8 are channels 4 gid + m and 32 + 4 gid + m of the group
 #pragma unroll
-            for (int u = 0; u < kSteps; ++u)
+            for (int u = 0; u < kSteps; ++u) {
+                uint32_t vw[2][G][2];
+                T::codes(vw, mine, step_at + u * T::kBytes + T::kCodes, true);
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const uint32_t a_lo = __byte_perm(raw[u].v[0][g], raw[u].v[1][g], 0x5410), a_hi = __byte_perm(raw[u].v[0][g], raw[u].v[1][g], 0x7632);
-                    const uint32_t b_lo = __byte_perm(raw[u].v[2][g], raw[u].v[3][g], 0x5410), b_hi = __byte_perm(raw[u].v[2][g], raw[u].v[3][g], 0x7632);
+                for (int g = 0; g < G; ++g)
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
-                        const uint32_t a[4] = {operand_pair<kSplit>(a_lo, m), operand_pair<kSplit>(a_hi, m), operand_pair<kSplit>(b_lo, m), operand_pair<kSplit>(b_hi, m)};
+                        const uint32_t a[4] = {operand_pair<kSplit>(vw[0][g][0], m), operand_pair<kSplit>(vw[0][g][1], m), operand_pair<kSplit>(vw[1][g][0], m), operand_pair<kSplit>(vw[1][g][1], m)};
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t) {
                             if constexpr (kSplit) {     // added up by fp32 additions, which round
@@ -784,12 +823,9 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                             }
                         }
                     }
-                }
-            if (more) {
-#pragma unroll
-                for (int u = 0; u < kSteps; ++u) raw[u].load_v(offsets, unit[u], slot[u]);
             }
         }
+        copies_wait<0>();
 
         // ---- the warps' rows meet in shared memory
 #pragma unroll
@@ -814,7 +850,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int r = 8 * t + 2 * tig + (e & 1), ch = g * 64 + gid * 8 + m + (e >> 1) * 4;
+                            const int r = 8 * t + 2 * tig + (e & 1), ch = g * 64 + (e >> 1) * 32 + gid * 4 + m;
                             mine[r * C::kLd + ch] = fmaf(o[g][m][t][e], (m & 1) && !kSplit ? back * 0.0625f : back, lows[t][e & 1][g]);
                         }
             }
