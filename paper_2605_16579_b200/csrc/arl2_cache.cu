@@ -95,14 +95,36 @@ __device__ __forceinline__ void store8(float* p, bool wide, const float (&x)[8])
     }
 }
 
+// two fp32 operations in one instruction, each rounded
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // 8 of a group's 64 channels -> one word of codes and the group's (minimum, step); x becomes what these stand for.  Every
 // operation is a single fp32 one, so that the codes are those of the formula whoever evaluates it.
+// (Magnitudes above the limit need no clamp of their own: their codes are the ends' anyway.  Rounding to whole numbers is an addition
+// of 1.5 * 2^23, and codes come together as digits of a whole number in fp32: conversions and rint have a quarter of the rate.)
 __device__ __forceinline__ void hold8(float (&x)[8], uint32_t& codes, uint32_t& params)
 {
-    float lo = kHoldLimit, hi = -kHoldLimit;
+    float lo = min_nan(x[0], x[1]), hi = max_nan(x[0], x[1]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = max_nan(min_nan(x[i], kHoldLimit), -kHoldLimit);
+    for (int i = 2; i < 8; ++i) {
         lo = min_nan(lo, x[i]);
         hi = max_nan(hi, x[i]);
     }
@@ -111,16 +133,25 @@ __device__ __forceinline__ void hold8(float (&x)[8], uint32_t& codes, uint32_t& 
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
+    lo = max_nan(min_nan(lo, kHoldLimit), -kHoldLimit);
+    hi = max_nan(min_nan(hi, kHoldLimit), -kHoldLimit);
     const __half step_h = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), lo_h = __float2half_rn(lo);
     const float step = __half2float(step_h), base = __half2float(lo_h);
     const float inverse = step > 0.0f ? __frcp_rn(step) : 0.0f;
-    codes = 0;
+    const uint64_t base2 = pair(-base, -base), inverse2 = pair(inverse, inverse);
+    constexpr float kMagic = 12582912.0f;
+    float c[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float code = fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], base), inverse)), 0.0f), 15.0f);   // (NaN: 0)
-        codes |= (uint32_t)code << (4 * i);
-        x[i] = fmaf(step, code, base);
+    for (int i = 0; i < 8; i += 2) {
+        unpair(mul_pair(add_pair(pair(x[i], x[i + 1]), base2), inverse2), c[i], c[i + 1]);
+        c[i] = fminf(fmaxf(c[i], 0.0f), 15.0f);              // (NaN: 0)
+        c[i + 1] = fminf(fmaxf(c[i + 1], 0.0f), 15.0f);
+        unpair(add_pair(add_pair(pair(c[i], c[i + 1]), pair(kMagic, kMagic)), pair(-kMagic, -kMagic)), c[i], c[i + 1]);
     }
+    const float low4 = fmaf(16.0f, fmaf(16.0f, fmaf(16.0f, c[3], c[2]), c[1]), c[0]), high4 = fmaf(16.0f, fmaf(16.0f, fmaf(16.0f, c[7], c[6]), c[5]), c[4]);
+    codes = __byte_perm(__float_as_uint(low4 + kMagic), __float_as_uint(high4 + kMagic), 0x5410);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(step, c[i], base);
     params = (uint32_t)__half_as_ushort(lo_h) | ((uint32_t)__half_as_ushort(step_h) << 16);
 }
 
@@ -187,6 +218,7 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Cach
             if (t == 0 && rotate) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
+                    // every operation rounded (of a packed product and sum the compiler makes one with a single rounding)
                     const float a = x[0][n][2 * m], c = x[0][n][2 * m + 1];
                     x[0][n][2 * m] = __fsub_rn(__fmul_rn(a, cs[m]), __fmul_rn(c, sn[m]));
                     x[0][n][2 * m + 1] = __fadd_rn(__fmul_rn(a, sn[m]), __fmul_rn(c, cs[m]));
@@ -223,21 +255,21 @@ __device__ uint4 g_no_page[Unit<128>::bytes(256) / 16];
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // the same with nothing to add to
 __device__ __forceinline__ void mma16816_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
 {
     uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
 // codes i and i + 4 of a word as a pair of fp16 denormals: code * 2^-24 for even i, code * 2^-20 for odd i
@@ -379,7 +411,7 @@ struct RowsConfig {
     static constexpr int kLd = D + 1;
     // CTAs that an SM is to hold: by the registers of the output's fragments
     static constexpr int kPerSm = D * kTiles <= 128 ? 3 : 2;
-    static constexpr int kStages = 3;         // steps of keys on their way or being read
+    static constexpr int kStages = 2;         // steps of keys on their way or being read
     // shared memory: the query operand and the keys, then (over them) the warps' rows; per row its factor, its sums per group, the keys it sees
     static constexpr int kQBytes = kParts * kRows * D * 2;
     static constexpr int kLoopBytes = kQBytes + kWarps * kStages * kSteps * Tile<D>::kBytes;
@@ -612,40 +644,44 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 
             // ---- scores of keys gid (x[u][t][0 .. 1]) and gid + 8 (x[u][t][2 .. 3]), still to be multiplied by the row's factor
             float x[kSteps][kTiles][4];
+            uint32_t kw[kSteps][2][G][2], kp[kSteps][2][G];
 #pragma unroll
             for (int u = 0; u < kSteps; ++u) {
-                uint32_t kw[2][G][2], kp[2][G];
-                T::codes(kw, mine, step_at + u * T::kBytes, false);
+                T::codes(kw[u], mine, step_at + u * T::kBytes, false);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) T::params(kp[e], step + u * T::kBytes, 0, gid + 8 * e);
-                // sums of q * code per group
-                float acc[G][kTiles][4], rest[kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
+                for (int e = 0; e < 2; ++e) T::params(kp[u][e], step + u * T::kBytes, 0, gid + 8 * e);
+            }
+            // sums of q * code per group.  (Step by step of all of them: a sum's own steps wait for one another.)
+            float acc[kSteps][G][kTiles][4], rest[kSplit ? kSteps : 1][kSplit ? G : 1][kTiles][4];   // (the low parts' sums apart: they would be cut off)
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const uint32_t w0 = kw[0][g][s >> 1], w1 = kw[1][g][s >> 1];
+                for (int u = 0; u < kSteps; ++u)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const uint32_t w0 = kw[u][0][g][s >> 1], w1 = kw[u][1][g][s >> 1];
                         const int i = 2 * (s & 1);
                         const uint32_t a[4] = {operand_pair<kSplit>(w0, i), operand_pair<kSplit>(w1, i), operand_pair<kSplit>(w0, i + 1), operand_pair<kSplit>(w1, i + 1)};
 #pragma unroll
-                        for (int t = 0; t < kTiles; ++t) {
+                        for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                             for (int part = 0; part < kParts; ++part) {
                                 uint2 q;
                                 if constexpr (kKeep) q = kept[g][s];
                                 else q = q_operand(part, t, g, s);
-                                if (s == 0) mma16816_new(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
-                                else mma16816(part == 0 ? acc[g][t] : rest[kSplit ? g : 0][t], a, q.x, q.y);
+                                float (&to)[4] = part == 0 ? acc[u][g][t] : rest[kSplit ? u : 0][kSplit ? g : 0][t];
+                                if (s == 0) mma16816_new(to, a, q.x, q.y);
+                                else mma16816(to, a, q.x, q.y);
                             }
-                        }
                     }
-                }
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u) {
                 float kl[2][G], ks[2][G];
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float2 a = unpack_half(kp[e][g]);
+                        const float2 a = unpack_half(kp[u][e][g]);
                         kl[e][g] = kSplit ? fmaf(8.0f, a.y, a.x) : a.x;
                         ks[e][g] = a.y;
                     }
@@ -657,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 #pragma unroll
                         for (int g = 0; g < G; ++g) {
                             if (g > 0) low = fmaf(kl[e >> 1][g], sums[t][e & 1][g], low);
-                            const float a = kSplit ? acc[g][t][e] + rest[kSplit ? g : 0][t][e] : acc[g][t][e];
+                            const float a = kSplit ? acc[u][g][t][e] + rest[kSplit ? u : 0][kSplit ? g : 0][t][e] : acc[u][g][t][e];
                             s = g == 0 ? a * ks[e >> 1][g] : fmaf(a, ks[e >> 1][g], s);
                         }
                         x[u][t][e] = fmaf(s, kSplit ? 1.0f : 16777216.0f, low);
