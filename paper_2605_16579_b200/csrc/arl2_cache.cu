@@ -1,8 +1,9 @@
 // The paged 4-bit key/value cache: appending rows, and attention by warp-level matrix instructions.
 //
-// Append.  Each lane holds 8 channels of a row (16 lanes a row of 128), rotates them, finds minimum and maximum of its group of
-// 64 channels with its 7 neighbours, and writes one word of 8 codes.  Bound by HBM: 4 D bytes (bf16) are read per token and head and
-// 9/8 D written.  A row group takes several heads of one token, so that the token's row of the rotary tables is fetched once for
+// Append.  Each lane holds 16 channels of a row (8 lanes a row of 128), rotates them, finds minimum and maximum of its group of
+// 64 channels with its 3 neighbours, and writes two words of 8 codes.  4 D bytes (bf16) are read per token and head and 9/8 D written,
+// but what bounds it is the instructions: about 18 a value, of which minimum, maximum, quotient and clamp are on the half-rate pipe.
+// A row group takes two heads of one token, so that the token's row of the rotary tables is fetched once for
 // them and their loads are in flight together.
 //
 // Attention (one query per stream up to a few dozen rows; any number in fp32 and with D = 64).  Keys are the M side of the
@@ -42,56 +43,65 @@ __device__ __forceinline__ float max_nan(float a, float b)
 }
 
 // ------------------------------------------------------------------------------------------------ append
-// 8 consecutive values of a row; `wide`: they start on a 16-byte boundary
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool wide, float (&x)[8])
+constexpr int kLaneValues = 16;
+// consecutive values of a row; `wide`: they start on a 16-byte boundary
+__device__ __forceinline__ void load_values(const __nv_bfloat16* p, bool wide, float (&x)[kLaneValues])
 {
     if (wide) {
-        const uint4 r = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        for (int h = 0; h < kLaneValues / 8; ++h) {
+            const uint4 r = reinterpret_cast<const uint4*>(p)[h];
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[8 * h + 2 * i] = __uint_as_float(w[i] << 16);
+                x[8 * h + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+        for (int i = 0; i < kLaneValues; ++i) x[i] = __bfloat162float(p[i]);
     }
 }
-__device__ __forceinline__ void load8(const float* p, bool wide, float (&x)[8])
+__device__ __forceinline__ void load_values(const float* p, bool wide, float (&x)[kLaneValues])
 {
     if (wide) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = p[i];
-    }
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* p, bool wide, const float (&x)[8])
-{
-    if (wide) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        for (int h = 0; h < kLaneValues / 4; ++h) {
+            const float4 a = reinterpret_cast<const float4*>(p)[h];
+            x[4 * h] = a.x; x[4 * h + 1] = a.y; x[4 * h + 2] = a.z; x[4 * h + 3] = a.w;
         }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
+        for (int i = 0; i < kLaneValues; ++i) x[i] = p[i];
     }
 }
-__device__ __forceinline__ void store8(float* p, bool wide, const float (&x)[8])
+__device__ __forceinline__ void store_values(__nv_bfloat16* p, bool wide, const float (&x)[kLaneValues])
 {
     if (wide) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+        for (int h = 0; h < kLaneValues / 8; ++h) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 y = __floats2bfloat162_rn(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            reinterpret_cast<uint4*>(p)[h] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = x[i];
+        for (int i = 0; i < kLaneValues; ++i) p[i] = __float2bfloat16_rn(x[i]);
+    }
+}
+__device__ __forceinline__ void store_values(float* p, bool wide, const float (&x)[kLaneValues])
+{
+    if (wide) {
+#pragma unroll
+        for (int h = 0; h < kLaneValues / 4; ++h) reinterpret_cast<float4*>(p)[h] = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLaneValues; ++i) p[i] = x[i];
     }
 }
 
@@ -116,42 +126,65 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
     return d;
 }
 
-// 8 of a group's 64 channels -> one word of codes and the group's (minimum, step); x becomes what these stand for.  Every
+__device__ __forceinline__ float min3_nan(float a, float b, float c)
+{
+    float d;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// 16 of a group's 64 channels -> two words of codes and the group's (minimum, step); x becomes what these stand for.  Every
 // operation is a single fp32 one, so that the codes are those of the formula whoever evaluates it.
 // (Magnitudes above the limit need no clamp of their own: their codes are the ends' anyway.  Rounding to whole numbers is an addition
-// of 1.5 * 2^23, and codes come together as digits of a whole number in fp32: conversions and rint have a quarter of the rate.)
-__device__ __forceinline__ void hold8(float (&x)[8], uint32_t& codes, uint32_t& params)
+// of 1.5 * 2^23, and codes come together as digits of a whole number in fp32: conversions and rint have a quarter of the rate.
+// The quotients are clamped only where the roundings of minimum and step let the ends' fall outside.)
+__device__ __forceinline__ void hold_values(float (&x)[kLaneValues], uint32_t (&codes)[2], uint32_t& params)
 {
     float lo = min_nan(x[0], x[1]), hi = max_nan(x[0], x[1]);
 #pragma unroll
-    for (int i = 2; i < 8; ++i) {
-        lo = min_nan(lo, x[i]);
-        hi = max_nan(hi, x[i]);
+    for (int i = 2; i < kLaneValues; i += 2) {
+        lo = min3_nan(lo, x[i], x[i + 1]);
+        hi = max3_nan(hi, x[i], x[i + 1]);
     }
 #pragma unroll
-    for (int d = 1; d < 8; d <<= 1) {
+    for (int d = 1; d < kCacheGroup / kLaneValues; d <<= 1) {
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
     lo = max_nan(min_nan(lo, kHoldLimit), -kHoldLimit);
+    const float end = hi;
     hi = max_nan(min_nan(hi, kHoldLimit), -kHoldLimit);
     const __half step_h = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), lo_h = __float2half_rn(lo);
     const float step = __half2float(step_h), base = __half2float(lo_h);
     const float inverse = step > 0.0f ? __frcp_rn(step) : 0.0f;
+    // the ends' quotients, between which the others' are (of an infinity or a NaN among the values: not so)
+    const bool inside = __fmul_rn(__fsub_rn(lo, base), inverse) >= -0.5f && __fmul_rn(__fsub_rn(end, base), inverse) < 15.5f && end >= lo;
+    const bool clamp = !__all_sync(0xffffffffu, inside);
     const uint64_t base2 = pair(-base, -base), inverse2 = pair(inverse, inverse);
     constexpr float kMagic = 12582912.0f;
-    float c[8];
+    float c[kLaneValues];
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        unpair(mul_pair(add_pair(pair(x[i], x[i + 1]), base2), inverse2), c[i], c[i + 1]);
-        c[i] = fminf(fmaxf(c[i], 0.0f), 15.0f);              // (NaN: 0)
-        c[i + 1] = fminf(fmaxf(c[i + 1], 0.0f), 15.0f);
-        unpair(add_pair(add_pair(pair(c[i], c[i + 1]), pair(kMagic, kMagic)), pair(-kMagic, -kMagic)), c[i], c[i + 1]);
+    for (int i = 0; i < kLaneValues; i += 2) unpair(mul_pair(add_pair(pair(x[i], x[i + 1]), base2), inverse2), c[i], c[i + 1]);
+    if (clamp) {
+#pragma unroll
+        for (int i = 0; i < kLaneValues; ++i) c[i] = fminf(fmaxf(c[i], 0.0f), 15.0f);      // (NaN: 0)
     }
-    const float low4 = fmaf(16.0f, fmaf(16.0f, fmaf(16.0f, c[3], c[2]), c[1]), c[0]), high4 = fmaf(16.0f, fmaf(16.0f, fmaf(16.0f, c[7], c[6]), c[5]), c[4]);
-    codes = __byte_perm(__float_as_uint(low4 + kMagic), __float_as_uint(high4 + kMagic), 0x5410);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf(step, c[i], base);
+    for (int i = 0; i < kLaneValues; i += 2) unpair(add_pair(add_pair(pair(c[i], c[i + 1]), pair(kMagic, kMagic)), pair(-kMagic, -kMagic)), c[i], c[i + 1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float* d = c + 8 * h;
+        const float low4 = fmaf(16.0f, fmaf(16.0f, fmaf(16.0f, d[3], d[2]), d[1]), d[0]), high4 = fmaf(16.0f, fmaf(16.0f, fmaf(16.0f, d[7], d[6]), d[5]), d[4]);
+        codes[h] = __byte_perm(__float_as_uint(low4 + kMagic), __float_as_uint(high4 + kMagic), 0x5410);
+    }
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) x[i] = fmaf(step, c[i], base);
     params = (uint32_t)__half_as_ushort(lo_h) | ((uint32_t)__half_as_ushort(step_h) << 16);
 }
 
@@ -162,7 +195,7 @@ template <int D, typename IO, int kHeads>
 __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const CacheAppendArgs p)
 {
     using U = Unit<D>;
-    constexpr int kLanes = D / 8;
+    constexpr int kLanes = D / kLaneValues, kPairs = kLaneValues / 2;
     grid_dependency_sync();
     const int head_blocks = (p.c.kv_heads + kHeads - 1) / kHeads;
     const long long group = ((long long)blockIdx.x * kAppendThreads + threadIdx.x) / kLanes;
@@ -193,21 +226,24 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Cach
         }
     }
     const bool rotate = stored && p.c.rope_cos != nullptr;
-    float cs[4] = {1.0f, 1.0f, 1.0f, 1.0f}, sn[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float cs[kPairs], sn[kPairs];
     if (rotate) {
-        const float4 c4 = *reinterpret_cast<const float4*>(p.c.rope_cos + pos * (D / 2) + lr * 4);
-        const float4 s4 = *reinterpret_cast<const float4*>(p.c.rope_sin + pos * (D / 2) + lr * 4);
-        cs[0] = c4.x; cs[1] = c4.y; cs[2] = c4.z; cs[3] = c4.w;
-        sn[0] = s4.x; sn[1] = s4.y; sn[2] = s4.z; sn[3] = s4.w;
+#pragma unroll
+        for (int h = 0; h < kPairs / 4; ++h) {
+            const float4 c4 = reinterpret_cast<const float4*>(p.c.rope_cos + pos * (D / 2) + lr * kPairs)[h];
+            const float4 s4 = reinterpret_cast<const float4*>(p.c.rope_sin + pos * (D / 2) + lr * kPairs)[h];
+            cs[4 * h] = c4.x; cs[4 * h + 1] = c4.y; cs[4 * h + 2] = c4.z; cs[4 * h + 3] = c4.w;
+            sn[4 * h] = s4.x; sn[4 * h + 1] = s4.y; sn[4 * h + 2] = s4.z; sn[4 * h + 3] = s4.w;
+        }
     }
-    const IO* k = static_cast<const IO*>(p.k) + b * p.k_batch + i * p.k_token + lr * 8;
-    const IO* v = static_cast<const IO*>(p.v) + b * p.v_batch + i * p.v_token + lr * 8;
-    float x[2][kHeads][8];
+    const IO* k = static_cast<const IO*>(p.k) + b * p.k_batch + i * p.k_token + lr * kLaneValues;
+    const IO* v = static_cast<const IO*>(p.v) + b * p.v_batch + i * p.v_token + lr * kLaneValues;
+    float x[2][kHeads][kLaneValues];
 #pragma unroll
     for (int n = 0; n < kHeads; ++n) {
         const int h = min(h0 + n, p.c.kv_heads - 1);
-        load8(k + (size_t)h * D, p.wide, x[0][n]);
-        load8(v + (size_t)h * D, p.wide, x[1][n]);
+        load_values(k + (size_t)h * D, p.wide, x[0][n]);
+        load_values(v + (size_t)h * D, p.wide, x[1][n]);
     }
     const int slot = (int)(pos & ((1 << p.c.page_shift) - 1)), page_tokens = 1 << p.c.page_shift;
     uint8_t* unit = p.c.pages + ((size_t)page * p.c.kv_heads + h0) * p.c.unit_bytes;
@@ -217,29 +253,29 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Cach
         for (int t = 0; t < 2; ++t) {
             if (t == 0 && rotate) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
+                for (int m = 0; m < kPairs; ++m) {
                     // every operation rounded (of a packed product and sum the compiler makes one with a single rounding)
                     const float a = x[0][n][2 * m], c = x[0][n][2 * m + 1];
                     x[0][n][2 * m] = __fsub_rn(__fmul_rn(a, cs[m]), __fmul_rn(c, sn[m]));
                     x[0][n][2 * m + 1] = __fadd_rn(__fmul_rn(a, sn[m]), __fmul_rn(c, cs[m]));
                 }
             }
-            uint32_t codes, params;
-            hold8(x[t][n], codes, params);
+            uint32_t codes[2], params;
+            hold_values(x[t][n], codes, params);
             const bool mine = h0 + n < p.c.kv_heads;
             if (stored && mine) {
                 uint8_t* at = unit + n * p.c.unit_bytes;
-                *reinterpret_cast<uint32_t*>(at + (t ? U::v_codes(page_tokens) : 0) + slot * U::kRow + lr * 4) = codes;
-                if ((lr & 7) == 0)
-                    *reinterpret_cast<uint32_t*>(at + (t ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + (lr >> 3) * 4) = params;
+                *reinterpret_cast<uint2*>(at + (t ? U::v_codes(page_tokens) : 0) + slot * U::kRow + lr * 8) = make_uint2(codes[0], codes[1]);
+                if (lr % (kCacheGroup / kLaneValues) == 0)
+                    *reinterpret_cast<uint32_t*>(at + (t ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + lr / (kCacheGroup / kLaneValues) * 4) = params;
             }
             void* held = t ? p.v_held : p.k_held;
             if (held != nullptr && there && mine) {
                 if (!stored) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[t][n][e] = 0.0f;
+                    for (int e = 0; e < kLaneValues; ++e) x[t][n][e] = 0.0f;
                 }
-                store8(static_cast<IO*>(held) + ((size_t)row * p.c.kv_heads + h0 + n) * D + lr * 8, p.wide, x[t][n]);
+                store_values(static_cast<IO*>(held) + ((size_t)row * p.c.kv_heads + h0 + n) * D + lr * kLaneValues, p.wide, x[t][n]);
             }
         }
     }
@@ -1006,14 +1042,14 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 template <int D, typename IO>
 int launch_append(const CacheAppendArgs& a, cudaStream_t st)
 {
-    constexpr int kLanes = D / 8;
+    constexpr int kLanes = D / kLaneValues;
     const long long rows = (long long)a.B * a.tokens;
     auto blocks = [&](int heads) { return (rows * ((a.c.kv_heads + heads - 1) / heads) * kLanes + kAppendThreads - 1) / kAppendThreads; };
     // one head per row group while that does not fill the device
-    const bool few = blocks(4) < 148 * 2;
-    const long long grid = blocks(few ? 1 : 4);
+    const bool few = blocks(2) < 148 * 2;
+    const long long grid = blocks(few ? 1 : 2);
     if (grid > 0x7fffffffLL) { set_error("cache_append: too many rows"); return ARL2_ERR_UNSUPPORTED; }
-    const cudaError_t e = launch_kernel(few ? cache_append_kernel<D, IO, 1> : cache_append_kernel<D, IO, 4>, dim3((unsigned)grid), kAppendThreads, 0, st, a);
+    const cudaError_t e = launch_kernel(few ? cache_append_kernel<D, IO, 1> : cache_append_kernel<D, IO, 2>, dim3((unsigned)grid), kAppendThreads, 0, st, a);
     if (e != cudaSuccess) { set_error("launch of cache_append_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
     return 1;
 }
