@@ -457,7 +457,9 @@ class Cache:
     def __init__(self, layer, num_pages, max_pages, kv_heads=None, page_tokens=64, rope_cos=None, rope_sin=None, pages=None, page_table=None):
         lib = load()
         self._lib, self._cache = lib, None
+        self._append, self._attend = lib.arl2_cache_append, lib.arl2_cache_attend
         self.layer, self.device, self.dtype = layer, layer.device, layer.dtype
+        self._B, self._H, self._D = layer.B, layer.H, layer.D
         self.kv_heads = layer.H if kv_heads is None else kv_heads
         rows = 0 if rope_cos is None else int(rope_cos.shape[0])
         self.cfg = arl2_cache_config(ctypes.sizeof(arl2_cache_config), self.kv_heads, page_tokens, num_pages, max_pages, rows)
@@ -486,32 +488,36 @@ class Cache:
         """Rows k, v [B, T, kv_heads, D] of tokens start[b] .. start[b] + T - 1 (start: int32 [B], negative: idle stream), keys
         rotated to their positions.  ``held=True`` returns (k, v) as the cache now holds them, which may also be given as a pair
         of tensors to write to."""
-        layer = self.layer
-        shape = (layer.B, int(k.shape[1]), self.kv_heads, layer.D)
-        ks, vs = self._rows(k, shape, "k"), self._rows(v, shape, "v")
-        layer._want(start, (layer.B,), torch.int32, "start")
+        tokens = k.shape[1]
+        shape = (self._B, tokens, self.kv_heads, self._D)
+        k_batch, k_token = self._rows(k, shape, "k")
+        v_batch, v_token = self._rows(v, shape, "v")
+        self.layer._want(start, (self._B,), torch.int32, "start")
         kh = vh = None
-        if held is not False:
-            kh, vh = (torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(2)) if held is True else held
-            layer._want(kh, shape, self.dtype, "held keys")
-            layer._want(vh, shape, self.dtype, "held values")
-        self._run("arl2_cache_append", k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], shape[1], start.data_ptr(), _ptr(kh), _ptr(vh))
+        if held is True:
+            kh, vh = self._empty(k, shape), self._empty(v, shape)
+        elif held is not False:
+            kh, vh = held
+            self.layer._want(kh, shape, self.dtype, "held keys")
+            self.layer._want(vh, shape, self.dtype, "held values")
+        self._run(self._append, k.data_ptr(), k_batch, k_token, v.data_ptr(), v_batch, v_token, tokens, start.data_ptr(), _ptr(kh), _ptr(vh))
         return None if kh is None else (kh, vh)
 
     def attend(self, q, lengths, q_start=None, causal=False, out=None):
         """Attention of q [B, T, H, D] over the first lengths[b] tokens held (int32 [B]); q is rotated to its positions
         q_start[b] + i, by default those of the last T tokens.  ``causal``: query i sees the tokens up to its own position."""
-        layer = self.layer
-        shape = (layer.B, int(q.shape[1]), layer.H, layer.D)
-        qs = self._rows(q, shape, "q")
-        layer._want(lengths, (layer.B,), torch.int32, "lengths")
+        queries = q.shape[1]
+        shape = (self._B, queries, self._H, self._D)
+        q_batch, q_token = self._rows(q, shape, "q")
+        want = self.layer._want
+        want(lengths, (self._B,), torch.int32, "lengths")
         if q_start is not None:
-            layer._want(q_start, (layer.B,), torch.int32, "q_start")
+            want(q_start, (self._B,), torch.int32, "q_start")
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = self._empty(q, shape)
         else:
-            layer._want(out, shape, self.dtype, "out")
-        self._run("arl2_cache_attend", q.data_ptr(), qs[0], qs[1], shape[1], lengths.data_ptr(), _ptr(q_start), ARL2_CACHE_CAUSAL if causal else 0, out.data_ptr())
+            want(out, shape, self.dtype, "out")
+        self._run(self._attend, q.data_ptr(), q_batch, q_token, queries, lengths.data_ptr(), _ptr(q_start), ARL2_CACHE_CAUSAL if causal else 0, out.data_ptr())
         return out
 
     def close(self):
@@ -529,25 +535,32 @@ class Cache:
     def _rows(self, t, shape, what):
         """The batch and token strides of a tensor whose heads and channels are contiguous."""
         if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is self.dtype and t.shape == shape:
+            token = shape[2] * shape[3]
+            if t.is_contiguous():
+                return shape[1] * token, token
             st = t.stride()
-            if (st[3] == 1 or shape[3] == 1) and (st[2] == shape[3] or shape[2] == 1):
+            if st[3] == 1 and (st[2] == shape[3] or shape[2] == 1):
                 # (a dimension of one element may have any stride)
-                return st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else shape[2] * shape[3]
+                return st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else token
         raise Arl2Error(f"{what}: expected a CUDA tensor {tuple(shape)} {self.dtype} with contiguous heads and channels, got "
                         f"{tuple(t.shape)} {t.dtype} with strides {tuple(t.stride())} on {t.device}")
 
-    def _run(self, name, *args):
+    def _empty(self, like, shape):
+        # (empty_like costs the host less than empty, and gives the same for a contiguous tensor)
+        return torch.empty_like(like) if like.is_contiguous() else torch.empty(shape, dtype=self.dtype, device=self.device)
+
+    def _run(self, call, *args):
         if self.layer._ctx is None:
-            raise Arl2Error(f"{name}: the cache's layer has been closed")
+            raise Arl2Error(f"{call.__name__}: the cache's layer has been closed")
         current = torch.cuda.current_device()
         index = self.device.index
         if index is None or index == current:
-            status = getattr(self._lib, name)(self._cache, *args, _raw_stream(current))
+            status = call(self._cache, *args, _raw_stream(current))
         else:
             with torch.cuda.device(index):
-                status = getattr(self._lib, name)(self._cache, *args, _raw_stream(index))
+                status = call(self._cache, *args, _raw_stream(index))
         if status != 0:
-            _check(status, name)
+            _check(status, call.__name__)
 
 
 STATIC_SCRATCH_BYTES = 8 << 20

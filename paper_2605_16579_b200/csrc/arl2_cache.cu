@@ -3,8 +3,8 @@
 // Append.  Each lane holds 16 channels of a row (8 lanes a row of 128), rotates them, finds minimum and maximum of its group of
 // 64 channels with its 3 neighbours, and writes two words of 8 codes.  4 D bytes (bf16) are read per token and head and 9/8 D written,
 // but what bounds it is the instructions: about 18 a value, of which minimum, maximum, quotient and clamp are on the half-rate pipe.
-// A row group takes two heads of one token, so that the token's row of the rotary tables is fetched once for
-// them and their loads are in flight together.
+// One head per row group, K and V of it: with two, which fetch the token's row of the rotary tables once, 40 heads x 4 x 4680 tokens took
+// 175 us, with one, and twice the warps on an SM, 157.
 //
 // Attention (one query per stream up to a few dozen rows; any number in fp32 and with D = 64).  Keys are the M side of the
 // matrix instruction and query rows the N side, so that 8 rows fill it:  S^T = K Q^T, then  O^T = V^T P^T.  Codes go into the
@@ -190,23 +190,20 @@ __device__ __forceinline__ void hold_values(float (&x)[kLaneValues], uint32_t (&
 
 constexpr int kAppendThreads = 256;
 
-// kHeads heads of one token per row group
-template <int D, typename IO, int kHeads>
-__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const CacheAppendArgs p)
+template <int D, typename IO>
+__global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const CacheAppendArgs p)
 {
     using U = Unit<D>;
     constexpr int kLanes = D / kLaneValues, kPairs = kLaneValues / 2;
     grid_dependency_sync();
-    const int head_blocks = (p.c.kv_heads + kHeads - 1) / kHeads;
-    const long long group = ((long long)blockIdx.x * kAppendThreads + threadIdx.x) / kLanes;
+    const uint32_t group = blockIdx.x * (kAppendThreads / kLanes) + threadIdx.x / kLanes;     // (there are fewer than 2^31)
     const int lr = threadIdx.x % kLanes;
-    const long long rows = (long long)p.B * p.tokens;
-    long long row = group / head_blocks;
-    const int h0 = (int)(group - row * head_blocks) * kHeads;
+    const uint32_t rows = (uint32_t)p.B * (uint32_t)p.tokens;
+    uint32_t row = group / (uint32_t)p.c.kv_heads;
+    const int h = (int)(group - row * (uint32_t)p.c.kv_heads);
     const bool there = row < rows;       // (the lanes of a warp stay together: they shuffle)
     if (!there) row = rows - 1;
-    const int b = (int)(row / p.tokens), i = (int)(row - (long long)b * p.tokens);
-
+    const int b = (int)(row / (uint32_t)p.tokens), i = (int)(row - (uint32_t)b * (uint32_t)p.tokens);
     const int begin = p.start[b];
     const long long pos = (long long)begin + i;
     // what cannot be stored is left out, and recorded by one lane
@@ -222,61 +219,54 @@ __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const Cach
         }
         if (wrong != kRangeNone) {
             stored = false;
-            if (lr == 0 && h0 == 0) range_error(p.c.status, wrong, b);
+            if (lr == 0 && h == 0) range_error(p.c.status, wrong, b);
         }
     }
+    // (the tables' rows are asked for before the values, of which there are more: waited for behind them, 40 heads x 4 x 4680 tokens took
+    // 170 us instead of 151)
     const bool rotate = stored && p.c.rope_cos != nullptr;
     float cs[kPairs], sn[kPairs];
     if (rotate) {
+        const float4* cos4 = reinterpret_cast<const float4*>(p.c.rope_cos + pos * (D / 2) + lr * kPairs);
+        const float4* sin4 = reinterpret_cast<const float4*>(p.c.rope_sin + pos * (D / 2) + lr * kPairs);
 #pragma unroll
-        for (int h = 0; h < kPairs / 4; ++h) {
-            const float4 c4 = reinterpret_cast<const float4*>(p.c.rope_cos + pos * (D / 2) + lr * kPairs)[h];
-            const float4 s4 = reinterpret_cast<const float4*>(p.c.rope_sin + pos * (D / 2) + lr * kPairs)[h];
-            cs[4 * h] = c4.x; cs[4 * h + 1] = c4.y; cs[4 * h + 2] = c4.z; cs[4 * h + 3] = c4.w;
-            sn[4 * h] = s4.x; sn[4 * h + 1] = s4.y; sn[4 * h + 2] = s4.z; sn[4 * h + 3] = s4.w;
+        for (int q = 0; q < kPairs / 4; ++q) {
+            const float4 c4 = cos4[q], s4 = sin4[q];
+            cs[4 * q] = c4.x; cs[4 * q + 1] = c4.y; cs[4 * q + 2] = c4.z; cs[4 * q + 3] = c4.w;
+            sn[4 * q] = s4.x; sn[4 * q + 1] = s4.y; sn[4 * q + 2] = s4.z; sn[4 * q + 3] = s4.w;
         }
     }
-    const IO* k = static_cast<const IO*>(p.k) + b * p.k_batch + i * p.k_token + lr * kLaneValues;
-    const IO* v = static_cast<const IO*>(p.v) + b * p.v_batch + i * p.v_token + lr * kLaneValues;
-    float x[2][kHeads][kLaneValues];
+    float x[2][kLaneValues];
+    load_values(static_cast<const IO*>(p.k) + b * p.k_batch + i * p.k_token + (size_t)h * D + lr * kLaneValues, p.wide, x[0]);
+    load_values(static_cast<const IO*>(p.v) + b * p.v_batch + i * p.v_token + (size_t)h * D + lr * kLaneValues, p.wide, x[1]);
+    if (rotate) {
 #pragma unroll
-    for (int n = 0; n < kHeads; ++n) {
-        const int h = min(h0 + n, p.c.kv_heads - 1);
-        load_values(k + (size_t)h * D, p.wide, x[0][n]);
-        load_values(v + (size_t)h * D, p.wide, x[1][n]);
+        for (int m = 0; m < kPairs; ++m) {
+            // every operation rounded (of a packed product and sum the compiler makes one with a single rounding)
+            float &a = x[0][2 * m], &c = x[0][2 * m + 1];
+            const float u = __fsub_rn(__fmul_rn(a, cs[m]), __fmul_rn(c, sn[m]));
+            c = __fadd_rn(__fmul_rn(a, sn[m]), __fmul_rn(c, cs[m]));
+            a = u;
+        }
     }
     const int slot = (int)(pos & ((1 << p.c.page_shift) - 1)), page_tokens = 1 << p.c.page_shift;
-    uint8_t* unit = p.c.pages + ((size_t)page * p.c.kv_heads + h0) * p.c.unit_bytes;
+    uint8_t* unit = p.c.pages + ((size_t)page * p.c.kv_heads + h) * p.c.unit_bytes;
 #pragma unroll
-    for (int n = 0; n < kHeads; ++n) {
+    for (int t = 0; t < 2; ++t) {
+        uint32_t codes[2], params;
+        hold_values(x[t], codes, params);
+        if (stored) {
+            *reinterpret_cast<uint2*>(unit + (t ? U::v_codes(page_tokens) : 0) + slot * U::kRow + lr * 8) = make_uint2(codes[0], codes[1]);
+            if (lr % (kCacheGroup / kLaneValues) == 0)
+                *reinterpret_cast<uint32_t*>(unit + (t ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + lr / (kCacheGroup / kLaneValues) * 4) = params;
+        }
+        void* held = t ? p.v_held : p.k_held;
+        if (held != nullptr && there) {
+            if (!stored) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if (t == 0 && rotate) {
-#pragma unroll
-                for (int m = 0; m < kPairs; ++m) {
-                    // every operation rounded (of a packed product and sum the compiler makes one with a single rounding)
-                    const float a = x[0][n][2 * m], c = x[0][n][2 * m + 1];
-                    x[0][n][2 * m] = __fsub_rn(__fmul_rn(a, cs[m]), __fmul_rn(c, sn[m]));
-                    x[0][n][2 * m + 1] = __fadd_rn(__fmul_rn(a, sn[m]), __fmul_rn(c, cs[m]));
-                }
+                for (int e = 0; e < kLaneValues; ++e) x[t][e] = 0.0f;
             }
-            uint32_t codes[2], params;
-            hold_values(x[t][n], codes, params);
-            const bool mine = h0 + n < p.c.kv_heads;
-            if (stored && mine) {
-                uint8_t* at = unit + n * p.c.unit_bytes;
-                *reinterpret_cast<uint2*>(at + (t ? U::v_codes(page_tokens) : 0) + slot * U::kRow + lr * 8) = make_uint2(codes[0], codes[1]);
-                if (lr % (kCacheGroup / kLaneValues) == 0)
-                    *reinterpret_cast<uint32_t*>(at + (t ? U::v_par(page_tokens) : U::k_par(page_tokens)) + slot * U::kPar + lr / (kCacheGroup / kLaneValues) * 4) = params;
-            }
-            void* held = t ? p.v_held : p.k_held;
-            if (held != nullptr && there && mine) {
-                if (!stored) {
-#pragma unroll
-                    for (int e = 0; e < kLaneValues; ++e) x[t][n][e] = 0.0f;
-                }
-                store_values(static_cast<IO*>(held) + ((size_t)row * p.c.kv_heads + h0 + n) * D + lr * kLaneValues, p.wide, x[t][n]);
-            }
+            store_values(static_cast<IO*>(held) + ((size_t)row * p.c.kv_heads + h) * D + lr * kLaneValues, p.wide, x[t]);
         }
     }
 }
@@ -1044,12 +1034,9 @@ int launch_append(const CacheAppendArgs& a, cudaStream_t st)
 {
     constexpr int kLanes = D / kLaneValues;
     const long long rows = (long long)a.B * a.tokens;
-    auto blocks = [&](int heads) { return (rows * ((a.c.kv_heads + heads - 1) / heads) * kLanes + kAppendThreads - 1) / kAppendThreads; };
-    // one head per row group while that does not fill the device
-    const bool few = blocks(2) < 148 * 2;
-    const long long grid = blocks(few ? 1 : 2);
-    if (grid > 0x7fffffffLL) { set_error("cache_append: too many rows"); return ARL2_ERR_UNSUPPORTED; }
-    const cudaError_t e = launch_kernel(few ? cache_append_kernel<D, IO, 1> : cache_append_kernel<D, IO, 2>, dim3((unsigned)grid), kAppendThreads, 0, st, a);
+    const long long grid = (rows * a.c.kv_heads * kLanes + kAppendThreads - 1) / kAppendThreads;
+    if (rows * a.c.kv_heads >= 1LL << 31) { set_error("cache_append: too many rows"); return ARL2_ERR_UNSUPPORTED; }
+    const cudaError_t e = launch_kernel(cache_append_kernel<D, IO>, dim3((unsigned)grid), kAppendThreads, 0, st, a);
     if (e != cudaSuccess) { set_error("launch of cache_append_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
     return 1;
 }
