@@ -934,19 +934,24 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             static_cast<IO*>(p.out)[(((size_t)b * p.queries + i) * p.H + q_head) * D + ch] = static_cast<IO>(value);
         };
         const int part_slot = parts.slot((int)blockIdx.x);
-        for (int x = tid; x < rows * D; x += kThreads) {
-            const int r = x / D, ch = x - r * D;
-            float m = -INFINITY;
+        // an element of what the four warps have of a row
+        auto warps_row = [&](int r, int ch, float& m, float& sum, float& total) {
+            m = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) m = fmaxf(m, merge_ml[(w * kRows + r) * 2]);
             const float m_use = m == -INFINITY ? 0.0f : m;
-            float sum = 0.0f, total = 0.0f;
+            sum = total = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float f = exp2_fast(merge_ml[(w * kRows + r) * 2] - m_use);
                 sum = fmaf(merge_o[(w * kRows + r) * C::kLd + ch], f, sum);
                 total = fmaf(merge_ml[(w * kRows + r) * 2 + 1], f, total);
             }
+        };
+        for (int x = tid; x < rows * D; x += kThreads) {
+            const int r = x / D, ch = x - r * D;
+            float m, sum, total;
+            warps_row(r, ch, m, sum, total);
             if (parts.count == 1) write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
             else {
                 p.part_o[((size_t)part_slot * kRows + r) * D + ch] = sum;
@@ -965,63 +970,79 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             if (last_part) {
                 __threadfence();
                 if (tid == 0) p.tickets[parts.first] = 0;      // as it was found
-                // The common reference maximum of a row, then its parts.  With few rows each warp takes a fourth of the parts; with more, a row.
+                // Each warp takes a fourth of the rows, or, where there are fewer than warps, of the parts.  Several rows of several parts are
+                // asked for at once; the reference maximum grows as they come.
                 constexpr int kPer = D / 32;
-                const int shared_by = rows < kWarps ? kWarps : 1, lead = shared_by == 1 ? 0 : warp;
-                for (int r = shared_by == 1 ? warp : 0; r < rows; r += shared_by == 1 ? kWarps : 1) {
-                    float m = -INFINITY;
-                    for (int w = lane; w < parts.count; w += 32) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)parts.slot(parts.first + w) * kRows + r) * 2));
+                constexpr int kRowsAtOnce = kRows / kWarps > 4 ? 4 : kRows / kWarps, kBatch = 16 / kRowsAtOnce;
+                const bool by_part = rows < kWarps;
+                const int row_step = by_part ? 1 : kWarps, part_step = by_part ? kWarps : 1;
+                for (int r0 = by_part ? 0 : warp; r0 < rows; r0 += row_step * kRowsAtOnce) {
+                    float sum[kRowsAtOnce][kPer], total[kRowsAtOnce], m[kRowsAtOnce];
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                    if (m == -INFINITY) m = 0.0f;
-                    float sum[kPer], total = 0.0f;
+                    for (int y = 0; y < kRowsAtOnce; ++y) {
+                        m[y] = -INFINITY;
+                        total[y] = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
-                    constexpr int kBatch = 8;       // parts asked for at once
-                    for (int w0 = lead; w0 < parts.count; w0 += kBatch * shared_by) {
-                        float2 ml[kBatch];
-                        float x[kBatch][kPer];
+                        for (int e = 0; e < kPer; ++e) sum[y][e] = 0.0f;
+                    }
+                    for (int w0 = by_part ? warp : 0; w0 < parts.count; w0 += kBatch * part_step) {
+                        float2 ml[kBatch][kRowsAtOnce];
+                        float x[kBatch][kRowsAtOnce][kPer];
 #pragma unroll
-                        for (int k = 0; k < kBatch; ++k) {
-                            const int w = min(w0 + k * shared_by, parts.count - 1);
-                            const size_t s = (size_t)parts.slot(parts.first + w) * kRows + r;
-                            ml[k] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + s * 2));
-                            if constexpr (kPer == 4) {
-                                const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + s * D) + lane);
-                                x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
-                            } else {
-                                const float2 v = __ldcg(reinterpret_cast<const float2*>(p.part_o + s * D) + lane);
-                                x[k][0] = v.x; x[k][1] = v.y;
+                        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+                            for (int y = 0; y < kRowsAtOnce; ++y) {
+                                // (a row or part beyond the last: the last again)
+                                const size_t s = (size_t)parts.slot(parts.first + min(w0 + k * part_step, parts.count - 1)) * kRows + min(r0 + y * row_step, rows - 1);
+                                ml[k][y] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + s * 2));
+                                if constexpr (kPer == 4) {
+                                    const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + s * D) + lane);
+                                    x[k][y][0] = v.x; x[k][y][1] = v.y; x[k][y][2] = v.z; x[k][y][3] = v.w;
+                                } else {
+                                    const float2 v = __ldcg(reinterpret_cast<const float2*>(p.part_o + s * D) + lane);
+                                    x[k][y][0] = v.x; x[k][y][1] = v.y;
+                                }
+                            }
+#pragma unroll
+                        for (int y = 0; y < kRowsAtOnce; ++y) {
+                            float m_new = m[y];
+#pragma unroll
+                            for (int k = 0; k < kBatch; ++k) m_new = fmaxf(m_new, ml[k][y].x);
+                            const float m_use = m_new == -INFINITY ? 0.0f : m_new, f = exp2_fast(m[y] - m_use);
+                            m[y] = m_new;
+                            total[y] *= f;
+#pragma unroll
+                            for (int e = 0; e < kPer; ++e) sum[y][e] *= f;
+#pragma unroll
+                            for (int k = 0; k < kBatch; ++k) {
+                                if (w0 + k * part_step >= parts.count) break;
+                                const float g = exp2_fast(ml[k][y].x - m_use);
+                                total[y] = fmaf(ml[k][y].y, g, total[y]);
+#pragma unroll
+                                for (int e = 0; e < kPer; ++e) sum[y][e] = fmaf(x[k][y][e], g, sum[y][e]);
                             }
                         }
+                    }
 #pragma unroll
-                        for (int k = 0; k < kBatch; ++k) {
-                            if (w0 + k * shared_by >= parts.count) break;
-                            const float f = exp2_fast(ml[k].x - m);
-                            total = fmaf(ml[k].y, f, total);
+                    for (int y = 0; y < kRowsAtOnce; ++y) {
+                        const int r = r0 + y * row_step;
+                        if (r >= rows) break;
+                        if (!by_part) {
 #pragma unroll
-                            for (int e = 0; e < kPer; ++e) sum[e] = fmaf(x[k][e], f, sum[e]);
+                            for (int e = 0; e < kPer; ++e) write_row(r, lane * kPer + e, total[y] == 0.0f ? 0.0f : sum[y][e] / total[y]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < kPer; ++e) merge_o[(warp * kRows + r) * C::kLd + lane * kPer + e] = sum[y][e];
+                            if (lane == 0) *reinterpret_cast<float2*>(merge_ml + (warp * kRows + r) * 2) = make_float2(m[y], total[y]);
                         }
                     }
-                    if (shared_by == 1) {
-#pragma unroll
-                        for (int e = 0; e < kPer; ++e) write_row(r, lane * kPer + e, total == 0.0f ? 0.0f : sum[e] / total);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < kPer; ++e) merge_o[(warp * kRows + r) * C::kLd + lane * kPer + e] = sum[e];
-                        if (lane == 0) merge_ml[(warp * kRows + r) * 2 + 1] = total;
-                    }
                 }
-                if (shared_by == 1) continue;
+                if (!by_part) continue;
                 __syncthreads();
                 for (int x = tid; x < rows * D; x += kThreads) {
                     const int r = x / D, ch = x - r * D;
-                    float sum = 0.0f, total = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        sum += merge_o[(w * kRows + r) * C::kLd + ch];
-                        total += merge_ml[(w * kRows + r) * 2 + 1];
-                    }
+                    float m, sum, total;
+                    warps_row(r, ch, m, sum, total);
                     write_row(r, ch, total == 0.0f ? 0.0f : sum / total);
                 }
             }
@@ -1093,9 +1114,14 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
     return dtype == ARL2_FP32 ? launch_append<64, float>(a, st) : launch_append<64, __nv_bfloat16>(a, st);
 }
 
+// Rows per key head up to which this file's kernel is the faster one, with tcgen05 or without.  us with it and with tcgen05: 2 x 12
+// heads, 24 rows over 9360 keys 49 and 62; 12 heads, 32 over 600 15.4 and 18.3, 64 over 600 15.9 and 19.6; 2 heads, 32 over 20000 39 and
+// 35; 2 x 12 heads, 48 over 9360 (an earlier state of both) 66 and 59.
+constexpr int kFewRows = 32;
+
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)
 {
-    if (a.tensor_cores && a.queries * a.rep > 16) return tc_cache_attend(a, st);
+    if (a.tensor_cores && a.queries * a.rep > kFewRows) return tc_cache_attend(a, st);
     return a.D == 128 ? attend_any<128>(a, dtype, st) : attend_any<64>(a, dtype, st);
 }
 

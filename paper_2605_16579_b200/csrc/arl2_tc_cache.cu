@@ -233,7 +233,7 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
 // beside the tiles unpacked ahead (first: place_tiles)
 template <bool kUnpacked>
 __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* smem, uint32_t bars, uint32_t tmem_base, const Abort& ab,
-                                             const volatile uint32_t* marks, const int* first, ItemWalk walk, const Cut& cut, int t, int r, int warp_in_group)
+                                             const volatile uint32_t* marks, const int* first, ItemWalk walk, const Cut& cut, bool mine, int t, int r, int warp_in_group)
 {
     const uint32_t lane_base = tmem_base + ((uint32_t)(warp_in_group * 32) << 16);
     const uint32_t s_addr = lane_base + (uint32_t)(t * kTile);
@@ -411,7 +411,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         }
         tc_fence_before();
     }
-    if (t == 0 && r == 0) p.part_items[blockIdx.x] = begun;
+    if (mine && t == 0 && r == 0) p.part_items[blockIdx.x] = begun;     // (of the two kernels that may be there, one has done the work)
 }
 
 // ---- two warps that bring K, two that bring V: four threads a row of codes, 16 bytes each
@@ -621,7 +621,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kRegsSoftmax));
-        softmax_role<kUnpacked>(p, smem, bars, tmem_base, ab, marks, first, walk, cut, warp >> 2, (warp & 3) * 32 + lane, warp & 3);
+        softmax_role<kUnpacked>(p, smem, bars, tmem_base, ab, marks, first, walk, cut, mine, warp >> 2, (warp & 3) * 32 + lane, warp & 3);
     } else if constexpr (!kUnpacked) {
         if (warp < 12) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsHold));
@@ -861,25 +861,33 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
         total[x] = 0.0f;
         acc[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    for (int w = 0; w < parts.count; ++w) {
-        const size_t row = (size_t)parts.slot(cta + w) * kItemRows + r0;
-        float2 ml[kRowsEach];
-        float4 o[kRowsEach];
+    constexpr int kBatch = 3;      // parts asked for at once
+    for (int w0 = 0; w0 < parts.count; w0 += kBatch) {
+        float2 ml[kBatch][kRowsEach];
+        float4 o[kBatch][kRowsEach];
 #pragma unroll
-        for (int x = 0; x < kRowsEach; ++x) {
-            ml[x] = *reinterpret_cast<const float2*>(p.part_ml + (row + x) * 2);
-            o[x] = *reinterpret_cast<const float4*>(p.part_o + (row + x) * kD + lane * 4);
+        for (int k = 0; k < kBatch; ++k) {
+            const size_t row = (size_t)parts.slot(cta + min(w0 + k, parts.count - 1)) * kItemRows + r0;
+#pragma unroll
+            for (int x = 0; x < kRowsEach; ++x) {
+                ml[k][x] = *reinterpret_cast<const float2*>(p.part_ml + (row + x) * 2);
+                o[k][x] = *reinterpret_cast<const float4*>(p.part_o + (row + x) * kD + lane * 4);
+            }
         }
 #pragma unroll
-        for (int x = 0; x < kRowsEach; ++x) {
-            const float m_new = fmaxf(m[x], ml[x].x), m_use = m_new == -INFINITY ? 0.0f : m_new;
-            const float f = ex2_approx(m[x] - m_use), g = ex2_approx(ml[x].x - m_use);
-            m[x] = m_new;
-            total[x] = total[x] * f + ml[x].y * g;
-            acc[x].x = acc[x].x * f + o[x].x * g;
-            acc[x].y = acc[x].y * f + o[x].y * g;
-            acc[x].z = acc[x].z * f + o[x].z * g;
-            acc[x].w = acc[x].w * f + o[x].w * g;
+        for (int k = 0; k < kBatch; ++k) {
+            if (w0 + k >= parts.count) break;
+#pragma unroll
+            for (int x = 0; x < kRowsEach; ++x) {
+                const float m_new = fmaxf(m[x], ml[k][x].x), m_use = m_new == -INFINITY ? 0.0f : m_new;
+                const float f = ex2_approx(m[x] - m_use), g = ex2_approx(ml[k][x].x - m_use);
+                m[x] = m_new;
+                total[x] = total[x] * f + ml[k][x].y * g;
+                acc[x].x = acc[x].x * f + o[k][x].x * g;
+                acc[x].y = acc[x].y * f + o[k][x].y * g;
+                acc[x].z = acc[x].z * f + o[k][x].z * g;
+                acc[x].w = acc[x].w * f + o[k][x].w * g;
+            }
         }
     }
 #pragma unroll
@@ -902,9 +910,6 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
 std::mutex g_setup_mutex;
 DeviceSetup g_setup[kMaxDevices];
 
-// Rows per key head from which on unpacking ahead pays for itself.
-constexpr int kUnpackRows = 512;
-
 int launch_tc_attend(bool unpacked, const CacheAttendArgs& a, int grid, cudaStream_t st)
 {
     const cudaError_t e = unpacked ? launch_kernel(tc_cache_attend_kernel<true>, dim3((unsigned)grid), Roles<true>::kThreads, kSmemBytes, st, a)
@@ -923,13 +928,15 @@ int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
             return e == cudaSuccess ? opt_in_smem(tc_cache_attend_kernel<false>, kSmemBytes) : e;
         }, &num_sms)) return r;
     a.row_blocks = (a.queries * a.rep + kItemRows - 1) / kItemRows;
-    a.min_share = 4;
+    a.min_share = 2;
     a.max_parts = 32;
     const long long tiles = (((long long)a.c.max_pages << a.c.page_shift) + kTile - 1) / kTile;   // of a stream and head, at most
     const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * tiles;
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;
     if (grid > most) grid = most;
-    const bool ahead = a.queries * a.rep >= kUnpackRows && a.unpack_pairs > 0 && a.s_B <= kUnpackStreams;
+    // Operands are made ahead wherever there is room for them.  us with them made ahead and on the way: 12 heads, 64 rows over 600 keys 20
+    // and 34, 256 over 9360 53 and 57, 1536 over 9360 117 and 137; 2 x 12 heads, 64 over 9360 65 and 59.
+    const bool ahead = a.unpack_pairs > 0 && a.s_B <= kUnpackStreams;
     const long long pairs = (long long)a.s_B * a.c.kv_heads * (tiles + a.row_blocks);
     // where the workspace may be too small for the lengths, which only the device knows, both kernels go out, and one returns at once
     a.either = ahead && pairs > a.unpack_pairs;

@@ -101,7 +101,7 @@ struct Planner {
     }
 
     // Work of any shape: sums over the streams and blocks of rows.  All threads; `scratch`: 2 kWarps + 4 words of shared memory.
-    // (A function of its own: what calls of one length, the usual ones, do not reach should not stand in their way.)
+    // (A function of its own, 5 k clk: what most calls do not reach should not stand in their way.)
     static __device__ __noinline__ void general(const CacheAttendArgs& p, const Streams& st, int cta, int ctas, long long* scratch, Cut* out)
     {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -191,40 +191,45 @@ struct Planner {
     // This CTA's share.  All threads; st, scratch and `slow` in shared memory.
     static __device__ __forceinline__ Cut cut(const CacheAttendArgs& p, Streams& st, int cta, int ctas, long long* scratch, Cut* slow)
     {
-        // all streams alike: a few divisions (in 32 bits, where the chunks can be counted in them)
-        int have0, first0;
-        Streams::look_up(p, 0, have0, first0);
-        bool alike = !p.causal;
-        for (int b = threadIdx.x; b < p.s_B; b += kThreads) {
-            int have, first;
-            Streams::look_up(p, b, have, first);
-            if (b < kPlanStreams) {
-                st.have[b] = have;
-                st.first[b] = first;
-            }
-            alike = alike && have == have0;
-        }
-        const int each = chunks_of(have0);
-        const long long all = (long long)p.s_B * p.row_blocks * p.c.kv_heads;
-        alike = alike && all * each < (1LL << 31);
-        if (!__syncthreads_and(alike)) {
+        for (int b = threadIdx.x; b < min(p.s_B, kPlanStreams); b += kThreads) Streams::look_up(p, b, st.have[b], st.first[b]);
+        __syncthreads();
+        // Up to 32 streams whose blocks of rows all see the same keys: a lane per stream, every warp for itself.
+        const int lane = threadIdx.x & 31;
+        const bool few = p.s_B <= 32 && (!p.causal || p.row_blocks == 1);
+        int each = 0;
+        if (few && lane < p.s_B) each = unit_chunks(p, st, lane, 0);
+        const long long items = (long long)p.row_blocks * p.c.kv_heads;          // of a stream
+        if (!few || __any_sync(0xffffffffu, each * items >= 1LL << 25)) {        // (what follows counts in 32 bits)
             general(p, st, cta, ctas, scratch, slow);
             return *slow;
         }
-        const uint32_t items = (uint32_t)all, total = items * (uint32_t)each;
+        const uint32_t size = (uint32_t)each * (uint32_t)items;
+        uint32_t upto = size;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += x;
+        }
+        const uint32_t total = __shfl_sync(0xffffffffu, upto, 31), longest = (uint32_t)__reduce_max_sync(0xffffffffu, each);
         Cut c;
-        c.whole = kByHead ? (int)(items / (uint32_t)ctas) : 0;
-        const uint32_t base = (uint32_t)c.whole * (uint32_t)ctas * (uint32_t)each;
-        const uint32_t fewest = max((uint32_t)p.min_share, ((uint32_t)each + p.max_parts - 1) / p.max_parts);
+        c.whole = 0;
+        if (kByHead && __all_sync(0xffffffffu, lane >= p.s_B || each == (int)longest)) c.whole = (int)((uint32_t)(p.s_B * (uint32_t)items) / (uint32_t)ctas);
+        const uint32_t base = (uint32_t)c.whole * (uint32_t)ctas * longest;
+        const uint32_t fewest = max((uint32_t)p.min_share, (longest + (uint32_t)p.max_parts - 1) / (uint32_t)p.max_parts);
         const uint32_t share = max(fewest, (total - base + (uint32_t)ctas - 1) / (uint32_t)ctas);
         const uint32_t begin = (uint32_t)min((long long)total, (long long)base + (long long)share * cta);
         c.base = base;
         c.share = share;
         c.begin = begin;
         c.end = min(total, begin + share);
-        const uint32_t item = begin / (uint32_t)each;
+        // the stream that holds `begin`, and the item in it
+        const uint32_t here = __ballot_sync(0xffffffffu, upto - size <= begin && begin < upto);
+        const int b = here != 0 ? __ffs(here) - 1 : 0;
+        const uint32_t from = __shfl_sync(0xffffffffu, upto - size, b), in_stream = (uint32_t)max(1, __shfl_sync(0xffffffffu, each, b));
+        const uint32_t item = here != 0 ? (begin - from) / in_stream : 0;
         c.place = split(p, item);
-        c.place.item_begin = (long long)item * each;
+        c.place.b = b;
+        c.place.item_begin = (long long)from + (long long)item * in_stream;
         return c;
     }
     // item number -> stream, block of rows, head
