@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) cache_append_kernel(const C
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kKeys = 16;                  // keys of a matrix instruction
+constexpr int kShort = 64;                 // keys up to which every product's rounding is followed
 
 // What a page that the pool does not have reads as.
 __device__ uint4 g_no_page[Unit<128>::bytes(256) / 16];
@@ -730,7 +731,8 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
             for (int u = 0; u < kSteps; ++u)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) T::params(vp[u][e], step + u * T::kBytes, 1, gid + 8 * e);
-            const bool edge = key0 + kSteps * kKeys > fewest;     // some row does not see some of these keys
+            // Some row does not see some of these keys, or there are few: of many, the roundings of p * step against p * minimum average out.
+            const bool edge = key0 + kSteps * kKeys > fewest || seen <= kShort;
             if (edge) {
 #pragma unroll
                 for (int u = 0; u < kSteps; ++u)
@@ -848,8 +850,17 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                                 } else {
                                     hi = mul_half2(p2, mul_half2(__byte_perm(vp[u][e][g], 0, 0x3232), v_mul2[g]));
                                 }
-                                if (!(kMasked && hidden[2 * e])) lows[t][0][g] = fmaf(pr[2 * e], vl, lows[t][0][g]);
-                                if (!(kMasked && hidden[2 * e + 1])) lows[t][1][g] = fmaf(pr[2 * e + 1], vl, lows[t][1][g]);
+                                float w0 = pr[2 * e], w1 = pr[2 * e + 1], low = vl;
+                                if constexpr (kMasked && !kSplit) {      // the minimum's part from the rounded product itself
+                                    if (v.y != 0.0f) {
+                                        const float2 back = unpack_half(hi);
+                                        w0 = back.x;
+                                        w1 = back.y;
+                                        low = vl / (v.y * v_mul[g]);
+                                    }
+                                }
+                                if (!(kMasked && hidden[2 * e])) lows[t][0][g] = fmaf(w0, low, lows[t][0][g]);
+                                if (!(kMasked && hidden[2 * e + 1])) lows[t][1][g] = fmaf(w1, low, lows[t][1][g]);
                                 if (kMasked) {
                                     hi &= keep;
                                     lo &= keep;
@@ -1089,7 +1100,9 @@ int launch_attend(CacheAttendArgs& a, cudaStream_t st)
     a.row_blocks = (a.queries * a.rep + C::kRows - 1) / C::kRows;
     a.min_share = 2;
     a.max_parts = kTiles == 1 ? 64 : 32;
-    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * ((((long long)a.c.max_pages << a.c.page_shift) + C::kChunk - 1) / C::kChunk);
+    const long long items = (long long)a.s_B * a.row_blocks * a.c.kv_heads;
+    if (items >= 1LL << 31) { set_error("cache_attend: too many rows"); return ARL2_ERR_UNSUPPORTED; }
+    const long long most = items * ((((long long)a.c.max_pages << a.c.page_shift) + C::kChunk - 1) / C::kChunk);
     long long grid = ctas;
     if (grid > kCacheCtas) grid = kCacheCtas;
     if (grid > most) grid = most;

@@ -931,7 +931,9 @@ int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
     a.min_share = 2;
     a.max_parts = 32;
     const long long tiles = (((long long)a.c.max_pages << a.c.page_shift) + kTile - 1) / kTile;   // of a stream and head, at most
-    const long long most = (long long)a.s_B * a.row_blocks * a.c.kv_heads * tiles;
+    const long long items = (long long)a.s_B * a.row_blocks * a.c.kv_heads;
+    if (items >= 1LL << 31) { set_error("cache_attend: too many rows"); return ARL2_ERR_UNSUPPORTED; }
+    const long long most = items * tiles;
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;
     if (grid > most) grid = most;
     // Operands are made ahead wherever there is room for them.  us with them made ahead and on the way: 12 heads, 64 rows over 600 keys 20
