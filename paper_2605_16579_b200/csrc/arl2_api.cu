@@ -1092,6 +1092,9 @@ int arl2_sync_status(arl2_ctx* ctx, void* stream)
 
 namespace {
 
+// Whether a cache's attention over many rows goes to the tcgen05 kernel, which has both head dimensions.
+bool cache_tensor_cores(const arl2_config& c) { return c.io_dtype == ARL2_BF16 && !(c.flags & ARL2_FLAG_FORCE_SIMT); }
+
 // Scratch of a cache: tickets of the items that several CTAs share, their rows' statistics, their rows
 struct CacheLayout {
     size_t tickets, part_items, part_ml, part_o, marks, q_scale, unpacked, total;
@@ -1109,10 +1112,10 @@ CacheLayout cache_layout(const arl2_config& cfg, const arl2_cache_config& c)
     // operand tiles of all the keys that there may be and of a block of queries, or of as many as that is worth
     const int64_t rows = (int64_t)cfg.L * (cfg.H / c.kv_heads);
     const int64_t pairs = (((int64_t)c.max_pages * c.page_tokens + 127) / 128 + (rows + 255) / 256) * c.kv_heads * cfg.B;
-    l.unpack_pairs = !tc_supported(cfg) ? 0 : (int)(pairs < kUnpackMost ? pairs : kUnpackMost);
+    l.unpack_pairs = !cache_tensor_cores(cfg) ? 0 : (int)(pairs < kUnpackMost ? pairs : kUnpackMost);
     l.marks = off;    off += align_up((size_t)l.unpack_pairs * kUnpackMarks * sizeof(uint32_t));
     l.q_scale = off;  off += align_up((size_t)l.unpack_pairs * 256 * sizeof(float));
-    l.unpacked = off; off += (size_t)l.unpack_pairs * kUnpackPair;
+    l.unpacked = off; off += (size_t)l.unpack_pairs * unpack_pair_bytes(cfg.D);
     l.total = off;
     return l;
 }
@@ -1311,7 +1314,7 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
     a.part_o = cache->part_o; a.part_ml = cache->part_ml; a.tickets = cache->tickets;
     a.part_items = cache->part_items;
     a.unpacked = cache->unpacked; a.unpack_marks = cache->unpack_marks; a.unpack_pairs = cache->unpack_pairs; a.q_scale = cache->q_scale;
-    a.tensor_cores = cache->ctx->use_tc;
+    a.tensor_cores = cache_tensor_cores(cfg);
     a.wide = rows_are_wide(d_q, q_batch_stride, q_token_stride, elem) && rows_are_wide(d_out, 0, 0, 1);
     a.wait_limit = cache->ctx->wait_limit;
     return account(cache->ctx, cache_attend(a, cfg.io_dtype, as_stream(stream)));

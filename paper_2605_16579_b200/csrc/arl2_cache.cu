@@ -1129,7 +1129,8 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
 
 // Rows per key head up to which this file's kernel is the faster one, with tcgen05 or without.  us with it and with tcgen05: 2 x 12
 // heads, 24 rows over 9360 keys 49 and 62; 12 heads, 32 over 600 15.4 and 18.3, 64 over 600 15.9 and 19.6; 2 heads, 32 over 20000 39 and
-// 35; 2 x 12 heads, 48 over 9360 (an earlier state of both) 66 and 59.
+// 35; 2 x 12 heads, 48 over 9360 (an earlier state of both) 66 and 59.  At D = 64, 12 heads: 40 rows over 300, 600, 2000 and 9360 keys
+// 15.9, 13.6, 21.7, 32.0 and 15.6, 16.3, 19.3, 31.8; 128 rows 19.7, 19.6, 24.8, 50.5 and 17.4, 18.2, 20.4, 33.5; 1560 over 9360 353 and 95.
 constexpr int kFewRows = 32;
 
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)

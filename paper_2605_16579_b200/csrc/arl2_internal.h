@@ -215,10 +215,10 @@ constexpr int kCacheCtas = 4 * 148;        // most CTAs of the warp-level kernel
 constexpr int kCacheTcCtas = 148;          // most CTAs of the tcgen05 kernel, of 256 rows
 constexpr int kCachePartRows = 2 * kCacheTcCtas * 256;
 static_assert(2 * kCacheCtas * 32 <= kCachePartRows, "the partial rows of both kernels have the same room");
-// ... and for the operands of the tcgen05 kernel, made ahead of it: 64 KB are a K and a V tile of 128 keys of a head (from the front),
+// ... and for the operands of the tcgen05 kernel, made ahead of it: a pair is a K and a V tile of 128 keys of a head (from the front),
 // or the Q tiles of 256 query rows of a key head (from the back)
-constexpr size_t kUnpackPair = 2 * 128 * 128 * 2;
-constexpr int kUnpackMost = 4096;          // pairs at most (256 MB)
+constexpr int unpack_pair_bytes(int D) { return 2 * 128 * D * 2; }
+constexpr int kUnpackMost = 4096;          // pairs at most (256 MB at D = 128)
 constexpr int kUnpackMarks = 16;           // words beside a pair of K and V: what is special about its keys
 constexpr int kUnpackStreams = 64;         // most streams
 struct CacheAttendArgs {
@@ -245,14 +245,14 @@ struct CacheAttendArgs {
     int unpack_pairs = 0;
     int either = 0;          // the lengths decide whether the tiles are unpacked ahead (set by the launcher)
     bool wide;               // as in CacheAppendArgs, for q and out
-    bool tensor_cores;       // the context is one of the tcgen05 kernels (bf16 I/O, D = 128, not asked to do without)
+    bool tensor_cores;       // many rows may go to the tcgen05 kernel (bf16 I/O, a context not asked to do without)
     uint32_t wait_limit = 0; // as in StepArgs
 };
 int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st);
 // attention by warp-level matrix instructions: every shape and type
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st);
-// attention by tcgen05: bf16 I/O, D = 128, many rows
-int tc_cache_attend(CacheAttendArgs a, cudaStream_t st);
+// attention by tcgen05: bf16 I/O, many rows
+int tc_cache_attend(const CacheAttendArgs& a, cudaStream_t st);
 
 void set_error(const char* fmt, ...);
 

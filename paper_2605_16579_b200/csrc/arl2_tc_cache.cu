@@ -1,30 +1,31 @@
-// Attention over the paged 4-bit cache on tcgen05 / TMEM, for many query rows (bf16 I/O, D = 128).
+// Attention over the paged 4-bit cache on tcgen05 / TMEM, for many query rows (bf16 I/O, D = 64 or 128).
 //
 // One CTA per SM.  An item is two 128-row tiles of query rows of one key head against the keys that they see; the items' key
 // tiles of 128 form one sequence that is cut evenly over the CTAs (cache_common.cuh).  Roles:
 //   warps 0-3 / 4-7   softmax group of tile 0 / 1, one thread per query row
 //   two warps         MMA issuer of tile 0 / 1:  S_t = Q_t K_j^T and O_t += P_t V_j into TMEM
-// The operands are tiles of 32 KB: Q's rows, rotated in fp32, scaled by a power of two into fp16's range and rounded to fp16; K and V
+// The operands are tiles of 128 rows (32 KB at D = 128): Q's rows, rotated in fp32, scaled by a power of two into fp16's range and rounded to fp16; K and V
 // as minimum + step * code in fp16 (in which the codes are exact; its rounding, 2^-12, is an eighth of bf16's), through a ring.  They
 // are made in one of two ways:
 //     ahead       cache_unpack_kernel writes all of them to the workspace, as they stand in shared memory, and one thread copies them
 //                 in.  Costs 512 bytes per key and head written and read again, once per call.
 //     on the way  four warps read codes and parameters, one tile ahead, and write the tiles of K and V, the softmax groups those of Q:
 //                 less to move, but every item converts its keys anew, beside two softmax groups that want the same issue slots.
-// TMEM (512 columns): S_0 | S_1 | O_0 | O_1, the fp16 probabilities over the first 64 columns of S_t.
+// TMEM (512 columns): S_0 | S_1 | O_0 | O_1, 128 each, the fp16 probabilities over the first 64 columns of S_t.
 // The codes i and i + 4 of a 32-bit word come out of it as a pair, so that operand columns stand in the order 0 4 1 5 2 6 3 7 in every
 // eight: the Q operand is written in the same order, and the output's columns are put back in order when they are read.
 // Keys past the length are written as zeros and masked in the scores; a page that the pool does not have reads as zeros.
 //
 // An item that several CTAs work on leaves unnormalised fp32 rows, which cache_join_kernel puts together.
 // Every wait is bounded, as in the step kernel.
+#include <type_traits>
+
 #include "cache_common.cuh"
 #include "tc_common.cuh"
 
 namespace arl2 {
 namespace {
 
-constexpr int kD = 128;
 constexpr int kItemRows = 2 * kTile;
 constexpr int kStages = 5;
 // Warps and registers of the two ways.  setmaxnreg moves registers within what the CTA was launched with (threads x launch registers).
@@ -44,15 +45,22 @@ struct Roles<false> {
 };
 constexpr float kRescaleThreshold = 8.0f;   // log2 units of slack before O is rescaled: p <= 2^8
 
-constexpr int kOffQ = 0;
-constexpr int kOffRing = kOffQ + 2 * kTileBytes;
-constexpr int kOffBars = kOffRing + kStages * kTileBytes;
 constexpr int kSpecials = 16;               // key tiles whose marks are kept (more than are ever under way)
-constexpr int kOffMarks = kOffBars + 256;   // [kSpecials][kMarkWords]
 constexpr int kMarkWords = 9;               // whether a value is not finite; the keys of those, per group [2][4]
 static_assert(kMarkWords <= kUnpackMarks, "marks");
-constexpr int kSmemBytes = kOffMarks + kSpecials * kMarkWords * 4 + 1024;   // + alignment slack
-static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 36 * 8 + (int)sizeof(Streams) + (int)sizeof(Cut) <= 227 * 1024, "shared memory, with what the kernel declares itself");
+template <int kD>
+struct Dims {
+    static constexpr int kOperand = kTile * kD * 2;       // an operand tile: 64-column halves of kHalfBytes
+    static constexpr int kPair = 2 * kOperand;
+    // shared memory: two Q tiles, the ring, barriers, marks
+    static constexpr int kOffRing = 2 * kOperand;
+    static constexpr int kOffBars = kOffRing + kStages * kOperand;
+    static constexpr int kOffMarks = kOffBars + 256;      // [kSpecials][kMarkWords]
+    static constexpr int kSmemBytes = kOffMarks + kSpecials * kMarkWords * 4 + 1024;   // + alignment slack
+    static_assert(kSmemBytes + (kUnpackStreams + 1) * 4 + 36 * 8 + (int)sizeof(Streams) + (int)sizeof(Cut) <= 227 * 1024,
+                  "shared memory, with what the kernel declares itself");
+    static_assert(kPair == unpack_pair_bytes(kD), "a pair's room in the workspace");
+};
 
 enum Bar : int {
     kBarQ0 = 0, kBarQ1,                         // -> issuer t: its Q tile is there
@@ -147,7 +155,7 @@ __device__ __forceinline__ uint4 hold_word(uint32_t codes, __half2 low, __half2 
 // ---- the Q operand of kWarpRows rows, from row `row0` of block rb of (b, h) on: rotated in fp32, scaled by a power of two into fp16's
 // range, rounded to fp16.  `first`: the position of the stream's first query, rows: the block's.  A row at a time by the whole warp,
 // kBatch rows' loads in flight.  Lane l gets the factor of row l's scores.
-template <int kWarpRows, int kBatch>
+template <int kD, int kWarpRows, int kBatch>
 __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb, int h, int first, int rows, uint8_t* tile, int row0, int lane)
 {
     int own_e2 = 0;
@@ -164,64 +172,106 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
 #pragma unroll 1
     for (int r0 = 0; r0 < kWarpRows; r0 += kBatch) {
         // (no branch and nothing that is written among the loads: they would wait for one another)
-        float x[kBatch][4];
-        float2 cs[kBatch], sn[kBatch];
+        constexpr int kPer = kD / 32, kPairs = kPer / 2;       // channels of a lane, and rotation pairs
+        float x[kBatch][kPer], cs[kBatch][kPairs], sn[kBatch][kPairs];
+        auto src_of = [&](int k) {
+            return reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own_src), r0 + k)) + lane * kPer;
+        };
         if (p.wide) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own_src), r0 + k));
-                const uint2 v = reinterpret_cast<const uint2*>(src)[lane];
-                x[k][0] = __uint_as_float(v.x << 16);
-                x[k][1] = __uint_as_float(v.x & 0xFFFF0000u);
-                x[k][2] = __uint_as_float(v.y << 16);
-                x[k][3] = __uint_as_float(v.y & 0xFFFF0000u);
+                const __nv_bfloat16* src = src_of(k);
+                uint32_t w[2];
+                if constexpr (kPairs == 2) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(src);
+                    w[0] = v.x;
+                    w[1] = v.y;
+                } else {
+                    w[0] = *reinterpret_cast<const uint32_t*>(src);
+                }
+#pragma unroll
+                for (int m = 0; m < kPairs; ++m) {
+                    x[k][2 * m] = __uint_as_float(w[m] << 16);
+                    x[k][2 * m + 1] = __uint_as_float(w[m] & 0xFFFF0000u);
+                }
             }
         } else {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own_src), r0 + k));
+                const __nv_bfloat16* src = src_of(k);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[k][e] = __bfloat162float(src[lane * 4 + e]);
+                for (int e = 0; e < kPer; ++e) x[k][e] = __bfloat162float(src[e]);
             }
         }
         if (p.c.rope_cos != nullptr) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 const int at = __shfl_sync(0xffffffffu, (int)own_at, r0 + k);
-                cs[k] = reinterpret_cast<const float2*>(p.c.rope_cos + (size_t)at * (kD / 2))[lane];
-                sn[k] = reinterpret_cast<const float2*>(p.c.rope_sin + (size_t)at * (kD / 2))[lane];
+                const float* c = p.c.rope_cos + (size_t)at * (kD / 2) + lane * kPairs;
+                const float* s = p.c.rope_sin + (size_t)at * (kD / 2) + lane * kPairs;
+                if constexpr (kPairs == 2) {
+                    const float2 c2 = *reinterpret_cast<const float2*>(c), s2 = *reinterpret_cast<const float2*>(s);
+                    cs[k][0] = c2.x; cs[k][kPairs - 1] = c2.y;
+                    sn[k][0] = s2.x; sn[k][kPairs - 1] = s2.y;
+                } else {
+                    cs[k][0] = *c;
+                    sn[k][0] = *s;
+                }
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                cs[k] = make_float2(1.0f, 1.0f);
-                sn[k] = make_float2(0.0f, 0.0f);
-            }
+            for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+                for (int m = 0; m < kPairs; ++m) {
+                    cs[k][m] = 1.0f;
+                    sn[k][m] = 0.0f;
+                }
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const float a0 = x[k][0] * cs[k].x - x[k][1] * sn[k].x, a1 = x[k][0] * sn[k].x + x[k][1] * cs[k].x;
-            const float a2 = x[k][2] * cs[k].y - x[k][3] * sn[k].y, a3 = x[k][2] * sn[k].y + x[k][3] * cs[k].y;
-            // (as whole numbers the magnitudes are in the same order, infinities and NaN above all others)
-            uint32_t most = max(max(__float_as_uint(a0) & 0x7fffffffu, __float_as_uint(a1) & 0x7fffffffu),
-                                max(__float_as_uint(a2) & 0x7fffffffu, __float_as_uint(a3) & 0x7fffffffu));
+            float y[kPer];
+            uint32_t most = 0;
+#pragma unroll
+            for (int m = 0; m < kPairs; ++m) {
+                y[2 * m] = x[k][2 * m] * cs[k][m] - x[k][2 * m + 1] * sn[k][m];
+                y[2 * m + 1] = x[k][2 * m] * sn[k][m] + x[k][2 * m + 1] * cs[k][m];
+                // (as whole numbers the magnitudes are in the same order, infinities and NaN above all others)
+                most = max(most, max(__float_as_uint(y[2 * m]) & 0x7fffffffu, __float_as_uint(y[2 * m + 1]) & 0x7fffffffu));
+            }
             most = __reduce_max_sync(0xffffffffu, most);
             // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
             const bool finite = most < 0x7f800000u;
-            const int e2 = most == 0 ? 0 : min(137 - (int)(most >> 23), 126);
+            const int e2 = !finite || most == 0 ? 0 : min(137 - (int)(most >> 23), 126);
             const float up = __uint_as_float((uint32_t)(127 + (e2 >> 1)) << 23), up2 = __uint_as_float((uint32_t)(127 + e2 - (e2 >> 1)) << 23);
             if (lane == r0 + k) {
                 own_e2 = e2;
                 own_finite = finite;
             }
             const bool zero = !finite || row0 + r0 + k >= rows;
-            const uint32_t w0 = zero ? 0u : pack_f16(a0 * up * up2, a1 * up * up2), w1 = zero ? 0u : pack_f16(a2 * up * up2, a3 * up * up2);
-            // channels 8 c + 0 .. 3 are in even lanes, 4 .. 7 in odd ones; columns hold 0 4 1 5 | 2 6 3 7: an even lane writes the first four
-            const uint32_t give = (lane & 1) ? w0 : w1, got = __shfl_xor_sync(0xffffffffu, give, 1);
-            const uint32_t lo = (lane & 1) ? got : w0, hi = (lane & 1) ? w1 : got;     // channels m, m + 1 and m + 4, m + 5
-            const int row = (row0 & (kTile - 1)) + r0 + k, c = lane >> 1;
-            *reinterpret_cast<uint2*>(tile + (c >> 3) * kHalfBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4) + (lane & 1) * 8) =
-                make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+            uint32_t w[kPairs];
+#pragma unroll
+            for (int m = 0; m < kPairs; ++m) w[m] = zero ? 0u : pack_f16(y[2 * m] * up * up2, y[2 * m + 1] * up * up2);
+            // Columns of eight channels hold 0 4 1 5 | 2 6 3 7, eight bytes each: who has channels 4 .. 7 gives them to who has 0 .. 3.
+            const int row = (row0 & (kTile - 1)) + r0 + k;
+            uint32_t lo, hi;       // channels n, n + 1 and n + 4, n + 5
+            int chunk, part;
+            bool writes = true;
+            if constexpr (kPairs == 2) {      // even lanes have 0 .. 3, odd ones 4 .. 7; each writes eight bytes
+                const uint32_t give = (lane & 1) ? w[0] : w[kPairs - 1], got = __shfl_xor_sync(0xffffffffu, give, 1);
+                lo = (lane & 1) ? got : w[0];
+                hi = (lane & 1) ? w[kPairs - 1] : got;
+                chunk = lane >> 1;
+                part = lane & 1;
+            } else {                          // of four lanes the first two write, with what the last two give
+                lo = w[0];
+                hi = __shfl_xor_sync(0xffffffffu, w[0], 2);
+                chunk = lane >> 2;
+                part = lane & 1;
+                writes = (lane & 2) == 0;
+            }
+            if (writes)
+                *reinterpret_cast<uint2*>(tile + (chunk >> 3) * kHalfBytes + row * 128 + (((chunk & 7) ^ (row & 7)) << 4) + part * 8) =
+                    make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
         }
     }
     // (both factors have exponents that a float has)
@@ -231,7 +281,7 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
 
 // ---- one thread per query row.  marks: what is special about the key tiles, in shared memory by key tiles so far, or
 // beside the tiles unpacked ahead (first: place_tiles)
-template <bool kUnpacked>
+template <int kD, bool kUnpacked>
 __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* smem, uint32_t bars, uint32_t tmem_base, const Abort& ab,
                                              const volatile uint32_t* marks, const int* first, ItemWalk walk, const Cut& cut, bool mine, int t, int r, int warp_in_group)
 {
@@ -259,7 +309,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             c2 = p.q_scale[q_pair(p, seg.at) * kItemRows + in_item];
         } else {
             // (Every MMA that read the item before's Q has ended: its last scores have been here.)
-            c2 = write_q<32, 8>(p, seg.at.b, seg.at.rb, seg.at.h, seg.first, seg.rows, smem + kOffQ + t * kTileBytes, t * kTile + warp_in_group * 32, r & 31);
+            c2 = write_q<kD, 32, 8>(p, seg.at.b, seg.at.rb, seg.at.h, seg.first, seg.rows, smem + t * Dims<kD>::kOperand, t * kTile + warp_in_group * 32, r & 31);
             fence_proxy_async_smem();
             mbar_arrive(bars + 8 * (kBarQ0 + t));
         }
@@ -318,7 +368,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
                     // the MMA that last accumulated into O_t finished before S_t(j) was signalled, and the next one waits for
                     // this group's arrival below
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < kD / 32; ++c) {
                         uint32_t o[32];
                         tmem_ld32(o_addr + c * 32, o);
                         tmem_wait_ld();
@@ -361,7 +411,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             const size_t row = (size_t)parts.slot((int)blockIdx.x) * kItemRows + in_item;
             float* dst = p.part_o + row * kD;
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kD / 32; ++c) {
                 uint32_t o[32];
                 tmem_ld32(o_addr + c * 32, o);
                 tmem_wait_ld();
@@ -385,7 +435,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)seg.at.b * p.queries + i) * p.H + head) * kD;
             const bool wide = wide_rows(p.out);
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kD / 32; ++c) {
                 uint32_t o[32];
                 tmem_ld32(o_addr + c * 32, o);
                 tmem_wait_ld();
@@ -414,35 +464,39 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
     if (mine && t == 0 && r == 0) p.part_items[blockIdx.x] = begun;     // (of the two kernels that may be there, one has done the work)
 }
 
-// ---- two warps that bring K, two that bring V: four threads a row of codes, 16 bytes each
-constexpr int kHoldRows = 8;        // rows of a thread
+// ---- two warps that bring K, two that bring V: 16 bytes of a row of codes a thread
+template <int kD>
 struct HeldRows {
-    uint4 codes[kHoldRows];
-    uint32_t params[kHoldRows];     // fp16 (minimum, step); zero where no key is
+    static constexpr int kRows = kD / 16;       // of a thread: a row has kD / 32 threads, a tile 64
+    uint4 codes[kRows];
+    uint32_t params[kRows];     // fp16 (minimum, step); zero where no key is
 };
+
+template <int kD>
 __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* smem, uint32_t bars, const Abort& ab, uint32_t* marks, ItemWalk walk, int which, int tid)
 {
     using U = Unit<kD>;
-    const int page_tokens = 1 << p.c.page_shift, quarter = tid & 3, lane = tid & 31;
+    constexpr int kThreadsPerRow = kD / 32, kStep = 64 / kThreadsPerRow, kHoldRows = HeldRows<kD>::kRows;
+    const int page_tokens = 1 << p.c.page_shift, quarter = tid % kThreadsPerRow, lane = tid & 31;
     const int codes_at = (which ? U::v_codes(page_tokens) : 0) + quarter * 16;
     const int params_at = (which ? U::v_par(page_tokens) : U::k_par(page_tokens)) + (quarter >> 1) * 4;
-    // Rows of this thread: row0 + 16 i.  The two upper quarters take the row two further (^ 2) at the same time: with it the eight
-    // threads of a store's phase fall into eight different 16-byte columns of the swizzled tile.
-    const int row0 = (tid >> 2) ^ ((quarter & 2) ? 2 : 0);
+    // Rows of this thread: row0 + kStep i.  With four threads a row, the two upper ones take the row two further (^ 2) at the same time:
+    // with it the eight threads of a store's phase fall into eight different 16-byte columns of the swizzled tile.
+    const int row0 = (tid / kThreadsPerRow) ^ ((quarter & 2) ? 2 : 0);
     uint32_t entry = which, tile_cnt = 0;     // this role's next ring entry; key tiles so far
     bool ok = true;
 
     Segment seg;
-    // pages of this thread's rows of a key tile; -1: no key there.  (16 rows that begin at a multiple of 16 have one page.)
+    // pages of this thread's rows of a key tile; -1: no key there
     auto look_up = [&](int tile, int (&page)[kHoldRows]) {
         const int32_t* table = p.c.table + (size_t)seg.at.b * p.c.max_pages;
 #pragma unroll
         for (int i = 0; i < kHoldRows; ++i) {
-            const int key = tile * kTile + row0 + 16 * i;
+            const int key = tile * kTile + row0 + kStep * i;
             page[i] = key < seg.seen && tile < seg.c1 ? table[key >> p.c.page_shift] : -1;
         }
     };
-    auto fetch = [&](int tile, const int (&page)[kHoldRows], HeldRows& r) {
+    auto fetch = [&](int tile, const int (&page)[kHoldRows], HeldRows<kD>& r) {
         const uint8_t* head = p.c.pages + seg.at.h * p.c.unit_bytes;
         const size_t page_bytes = p.c.unit_bytes * p.c.kv_heads;
 #pragma unroll
@@ -450,7 +504,7 @@ __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* sme
             r.codes[i] = make_uint4(0, 0, 0, 0);
             r.params[i] = 0;
             if ((uint32_t)page[i] < (uint32_t)p.c.num_pages) {
-                const int slot = (tile * kTile + row0 + 16 * i) & (page_tokens - 1);
+                const int slot = (tile * kTile + row0 + kStep * i) & (page_tokens - 1);
                 const uint8_t* unit = head + (uint32_t)page[i] * page_bytes;
                 r.codes[i] = *reinterpret_cast<const uint4*>(unit + codes_at + slot * U::kRow);
                 r.params[i] = *reinterpret_cast<const uint32_t*>(unit + params_at + slot * U::kPar);
@@ -458,11 +512,11 @@ __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* sme
         }
     };
     // what softmax has to know of a tile, and the caller (rare)
-    auto mark = [&](int tile, const int (&page)[kHoldRows], HeldRows& r) {
+    auto mark = [&](int tile, const int (&page)[kHoldRows], HeldRows<kD>& r) {
         uint32_t* m = marks + (tile_cnt % kSpecials) * kMarkWords;
 #pragma unroll
         for (int i = 0; i < kHoldRows; ++i) {
-            const int row = row0 + 16 * i;
+            const int row = row0 + kStep * i;
             if (which == 0) {
                 if (tile * kTile + row < seg.seen && (uint32_t)page[i] >= (uint32_t)p.c.num_pages) range_error(p.c.status, kRangePage, seg.at.b);
             } else if (p.causal && not_finite(r.params[i])) {
@@ -473,14 +527,14 @@ __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* sme
         }
     };
     // a ring entry: out of registers, as fp16 values, into the swizzled operand tile
-    auto put = [&](const HeldRows& r) {
+    auto put = [&](const HeldRows<kD>& r) {
         const uint32_t slot = entry % kStages;
         if (entry >= (uint32_t)kStages) ok = wait_bar_warp(bars + 8 * (kBarEmpty0 + slot), ((entry / kStages) - 1) & 1, ab, 151 + which);
         if (!ok) return;
-        uint8_t* tile = smem + kOffRing + slot * kTileBytes + (quarter >> 1) * kHalfBytes;
+        uint8_t* tile = smem + Dims<kD>::kOffRing + slot * Dims<kD>::kOperand + (quarter >> 1) * kHalfBytes;
 #pragma unroll
         for (int i = 0; i < kHoldRows; ++i) {
-            const int row = row0 + 16 * i;
+            const int row = row0 + kStep * i;
             const uint32_t w[4] = {r.codes[i].x, r.codes[i].y, r.codes[i].z, r.codes[i].w};
             const __half2 both = *reinterpret_cast<const __half2*>(&r.params[i]);
             const __half2 low = __low2half2(both), step = __high2half2(both);
@@ -500,7 +554,7 @@ __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* sme
         if (tid == 0 && which == 0 && seg.opens) (void)stream_tokens(p, seg.at.b, true);
         // entries: K_0 V_0 K_1 V_1 ...; a tile's codes are fetched while the tile before is waited for and its pages looked up one earlier
         int page[kHoldRows], next_page[kHoldRows];
-        HeldRows r;
+        HeldRows<kD> r;
         look_up(seg.c0, page);
         look_up(seg.c0 + 1, next_page);
         fetch(seg.c0, page, r);
@@ -518,8 +572,11 @@ __device__ __forceinline__ void hold_role(const CacheAttendArgs& p, uint8_t* sme
 }
 
 // ---- one thread that copies the tiles made ahead, and waits for what it has sent for
+template <int kD>
 __device__ __forceinline__ void copy_role(const CacheAttendArgs& p, uint32_t smem_base, uint32_t bars, const Abort& ab, const int* first, ItemWalk walk)
 {
+    constexpr int kTileBytes = Dims<kD>::kOperand;
+    constexpr size_t kUnpackPair = Dims<kD>::kPair;
     uint32_t n = 0, q_cnt[2] = {0, 0};      // ring entries and Q tiles so far
     bool ok = true;
     Segment seg;
@@ -531,7 +588,7 @@ __device__ __forceinline__ void copy_role(const CacheAttendArgs& p, uint32_t sme
             if (!ok) break;
             const uint32_t bar = bars + 8 * (kBarQ0 + t);
             mbar_expect_tx(bar, kTileBytes);
-            bulk_load(smem_base + kOffQ + t * kTileBytes, q + t * kTileBytes, kTileBytes, bar);
+            bulk_load(smem_base + t * kTileBytes, q + t * kTileBytes, kTileBytes, bar);
             ++q_cnt[t];
         }
         // (an item without keys has one tile, of which every score is masked)
@@ -542,7 +599,7 @@ __device__ __forceinline__ void copy_role(const CacheAttendArgs& p, uint32_t sme
             const uint32_t slot = n % kStages;
             if (n >= (uint32_t)kStages) ok = wait_bar(bars + 8 * (kBarEmpty0 + slot), ((n / kStages) - 1) & 1, ab, 150);
             if (!ok) break;
-            const uint32_t bar = bars + 8 * (kBarFull0 + slot), dst = smem_base + kOffRing + slot * kTileBytes;
+            const uint32_t bar = bars + 8 * (kBarFull0 + slot), dst = smem_base + Dims<kD>::kOffRing + slot * kTileBytes;
             if (none) {
                 for (int i = 0; i < kTileBytes / 16; ++i) st_shared_zero(dst + i * 16);
                 fence_proxy_async_smem();
@@ -560,10 +617,11 @@ __device__ __forceinline__ void copy_role(const CacheAttendArgs& p, uint32_t sme
     for (uint32_t m = (n > (uint32_t)kStages ? n - kStages : 0); m < n; ++m) drain_bar(bars + 8 * (kBarFull0 + m % kStages), (m / kStages) & 1);
 }
 
-template <bool kUnpacked>
+template <int kD, bool kUnpacked>
 __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend_kernel(const __grid_constant__ CacheAttendArgs p)
 {
     using R = Roles<kUnpacked>;
+    constexpr int kTileBytes = Dims<kD>::kOperand, kOffRing = Dims<kD>::kOffRing, kOffBars = Dims<kD>::kOffBars, kOffMarks = Dims<kD>::kOffMarks;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t bars = smem_u32(smem) + kOffBars;
@@ -621,11 +679,11 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kRegsSoftmax));
-        softmax_role<kUnpacked>(p, smem, bars, tmem_base, ab, marks, first, walk, cut, mine, warp >> 2, (warp & 3) * 32 + lane, warp & 3);
+        softmax_role<kD, kUnpacked>(p, smem, bars, tmem_base, ab, marks, first, walk, cut, mine, warp >> 2, (warp & 3) * 32 + lane, warp & 3);
     } else if constexpr (!kUnpacked) {
         if (warp < 12) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsHold));
-            hold_role(p, smem, bars, ab, marks, walk, (warp - 8) >> 1, tid & 63);
+            hold_role<kD>(p, smem, bars, ab, marks, walk, (warp - 8) >> 1, tid & 63);
         } else {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsOther));
         }
@@ -633,7 +691,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kRegsOther));
         if (warp == 8 && lane == 0) {
             grid_dependency_sync();
-            copy_role(p, smem_u32(smem), bars, ab, first, walk);
+            copy_role<kD>(p, smem_u32(smem), bars, ab, first, walk);
         }
     }
     if (warp == R::kIssuer || warp == R::kIssuer + 1) {
@@ -646,7 +704,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
         const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
         constexpr uint32_t idesc_qk = idesc_f16(kTile, kTile, 0, 0);   // A, B K-major
         constexpr uint32_t idesc_pv = idesc_f16(kTile, kD, 0, 1);      // A in TMEM, B N-contiguous
-        const uint32_t q_tile = smem_base + kOffQ + t * kTileBytes;
+        const uint32_t q_tile = smem_base + t * kTileBytes;
         const uint32_t s_col = tmem_base + t * kTile, o_col = tmem_base + 2 * kTile + t * kTile;
         const uint32_t bar_s = bars + 8 * (kBarS0 + t), bar_p = bars + 8 * (kBarP0 + t);
         const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
@@ -660,7 +718,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
         auto issue_qk = [&](uint32_t k_tile) {
             const uint32_t a_lo = (q_tile >> 4) | kLboK, b_lo = (k_tile >> 4) | kLboK;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
+            for (int ks = 0; ks < kD / 16; ++ks) {
                 const uint32_t koff = (uint32_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4);
                 mma_ss_if(lead, s_col, desc64(a_lo + koff), desc64(b_lo + koff), idesc_qk, ks > 0);
             }
@@ -740,12 +798,15 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
 // Bound by writing them: 512 bytes per key and head.  A thread takes 32 channels of a cached row at a time and writes them as two
 // whole 32-byte sectors.
 constexpr int kUnpackThreads = 256;
+template <int kD>
 __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const CacheAttendArgs p)
 {
     using U = Unit<kD>;
+    constexpr int kTileBytes = Dims<kD>::kOperand, kThreadsPerRow = kD / 32, kStep = kUnpackThreads / kThreadsPerRow, kRowsEach = kTile / kStep;
+    constexpr size_t kUnpackPair = Dims<kD>::kPair;
     __shared__ int first[kUnpackStreams + 1];
     __shared__ uint32_t marks[kUnpackMarks];
-    const int tid = threadIdx.x, quarter = tid & 3, page_tokens = 1 << p.c.page_shift;
+    const int tid = threadIdx.x, quarter = tid % kThreadsPerRow, page_tokens = 1 << p.c.page_shift;
     grid_dependency_sync();
     if (!place_tiles(p, first)) return;
     constexpr int kQParts = 4;      // of a block of query rows
@@ -762,15 +823,15 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
         Streams::look_up(p, at.b, have, position);
         constexpr int kWarpRows = kItemRows / kQParts / (kUnpackThreads / 32);
         const int row0 = (work % kQParts) * (kItemRows / kQParts) + (tid >> 5) * kWarpRows, lane = tid & 31;
-        const float scale = write_q<kWarpRows, 8>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
+        const float scale = write_q<kD, kWarpRows, 8>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
                                         p.unpacked + pair * kUnpackPair + (row0 / kTile) * kTileBytes, row0, lane);
         if (lane < kWarpRows) p.q_scale[pair * kItemRows + row0 + lane] = scale;
     }
-    // Then tiles, K (even) and V (odd) of a pair.  A thread has rows tid / 4 and 64 further of a tile; the next tile's are fetched while
+    // Then tiles, K (even) and V (odd) of a pair.  A thread has every kStep-th row of a tile; the next tile's are fetched while
     // this one's are written.
     struct Rows {
-        uint4 codes[2];
-        uint32_t params[2];
+        uint4 codes[kRowsEach];
+        uint32_t params[kRowsEach];
     };
     int fetch_b = 0;      // (tiles only grow)
     auto fetch = [&](int tile_no, Rows& r) {
@@ -779,8 +840,8 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
         const int tile = at - first[fetch_b], have = stream_tokens(p, fetch_b, false);
         const int32_t* table = p.c.table + (size_t)fetch_b * p.c.max_pages;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int key = tile * kTile + (tid >> 2) + 64 * e;
+        for (int e = 0; e < kRowsEach; ++e) {
+            const int key = tile * kTile + tid / kThreadsPerRow + kStep * e;
             r.codes[e] = make_uint4(0, 0, 0, 0);
             r.params[e] = 0;
             if (key < have) {
@@ -807,8 +868,8 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
             if (tid < kUnpackMarks) marks[tid] = 0;
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int row = (tid >> 2) + 64 * e;
+            for (int e = 0; e < kRowsEach; ++e) {
+                const int row = tid / kThreadsPerRow + kStep * e;
                 if (!not_finite(cur.params[e])) continue;
                 cur.params[e] = 0;
                 atomicOr(marks + 1 + (quarter >> 1) * 4 + (row >> 5), 1u << (row & 31));
@@ -819,8 +880,8 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
         }
         uint8_t* out = p.unpacked + (size_t)tile_no * kTileBytes + (quarter >> 1) * kHalfBytes;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int row = (tid >> 2) + 64 * e;
+        for (int e = 0; e < kRowsEach; ++e) {
+            const int row = tid / kThreadsPerRow + kStep * e;
             const __half2 both = *reinterpret_cast<const __half2*>(&cur.params[e]);
             const __half2 low = __low2half2(both), step = __high2half2(both);
             const uint32_t c[4] = {cur.codes[e].x, cur.codes[e].y, cur.codes[e].z, cur.codes[e].w};
@@ -841,6 +902,7 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
 // ---- rows of the items that several CTAs share.  Block x of a launch of ctas x kJoinBlocks looks after part of the item that CTA
 // x / kJoinBlocks began and did not end, if there is one: a warp per row, the parts in the order of their CTAs.
 constexpr int kJoinBlocks = 8, kJoinThreads = 256;
+template <int kD>
 __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAttendArgs p)
 {
     const int cta = (int)blockIdx.x / kJoinBlocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -854,24 +916,27 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
     const Parts parts{cta, item.x};
     // rows that are not there are computed from whatever the workspace holds, and not written
     float m[kRowsEach], total[kRowsEach];
-    float4 acc[kRowsEach];
+    constexpr int kPer = kD / 32;      // channels of a lane
+    using Vec = typename std::conditional<kPer == 4, float4, float2>::type;
+    float acc[kRowsEach][kPer];
 #pragma unroll
     for (int x = 0; x < kRowsEach; ++x) {
         m[x] = -INFINITY;
         total[x] = 0.0f;
-        acc[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[x][e] = 0.0f;
     }
     constexpr int kBatch = 3;      // parts asked for at once
     for (int w0 = 0; w0 < parts.count; w0 += kBatch) {
         float2 ml[kBatch][kRowsEach];
-        float4 o[kBatch][kRowsEach];
+        Vec o[kBatch][kRowsEach];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const size_t row = (size_t)parts.slot(cta + min(w0 + k, parts.count - 1)) * kItemRows + r0;
 #pragma unroll
             for (int x = 0; x < kRowsEach; ++x) {
                 ml[k][x] = *reinterpret_cast<const float2*>(p.part_ml + (row + x) * 2);
-                o[k][x] = *reinterpret_cast<const float4*>(p.part_o + (row + x) * kD + lane * 4);
+                o[k][x] = *reinterpret_cast<const Vec*>(p.part_o + (row + x) * kD + lane * kPer);
             }
         }
 #pragma unroll
@@ -881,12 +946,11 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
             for (int x = 0; x < kRowsEach; ++x) {
                 const float m_new = fmaxf(m[x], ml[k][x].x), m_use = m_new == -INFINITY ? 0.0f : m_new;
                 const float f = ex2_approx(m[x] - m_use), g = ex2_approx(ml[k][x].x - m_use);
+                const float* y = reinterpret_cast<const float*>(&o[k][x]);
                 m[x] = m_new;
                 total[x] = total[x] * f + ml[k][x].y * g;
-                acc[x].x = acc[x].x * f + o[k][x].x * g;
-                acc[x].y = acc[x].y * f + o[k][x].y * g;
-                acc[x].z = acc[x].z * f + o[k][x].z * g;
-                acc[x].w = acc[x].w * f + o[k][x].w * g;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) acc[x][e] = acc[x][e] * f + y[e] * g;
             }
         }
     }
@@ -895,14 +959,19 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
         if (r0 + x >= rows) break;
         const float inv = total[x] == 0.0f ? 0.0f : 1.0f / total[x];
         const int flat = item.z * kItemRows + r0 + x, i = flat / p.rep, head = item.w * p.rep + flat - i * p.rep;
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)item.y * p.queries + i) * p.H + head) * kD + lane * 4;
-        const uint32_t w0 = pack_bf16(acc[x].x * inv, acc[x].y * inv), w1 = pack_bf16(acc[x].z * inv, acc[x].w * inv);
-        if (p.wide) *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
-        else {
-            dst[0] = __ushort_as_bfloat16((unsigned short)(w0 & 0xffffu));
-            dst[1] = __ushort_as_bfloat16((unsigned short)(w0 >> 16));
-            dst[2] = __ushort_as_bfloat16((unsigned short)(w1 & 0xffffu));
-            dst[3] = __ushort_as_bfloat16((unsigned short)(w1 >> 16));
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)item.y * p.queries + i) * p.H + head) * kD + lane * kPer;
+        uint32_t w[kPer / 2];
+#pragma unroll
+        for (int e = 0; e < kPer / 2; ++e) w[e] = pack_bf16(acc[x][2 * e] * inv, acc[x][2 * e + 1] * inv);
+        if (p.wide) {
+#pragma unroll
+            for (int e = 0; e < kPer / 2; ++e) reinterpret_cast<uint32_t*>(dst)[e] = w[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer / 2; ++e) {
+                dst[2 * e] = __ushort_as_bfloat16((unsigned short)(w[e] & 0xffffu));
+                dst[2 * e + 1] = __ushort_as_bfloat16((unsigned short)(w[e] >> 16));
+            }
         }
     }
 }
@@ -910,23 +979,18 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
 std::mutex g_setup_mutex;
 DeviceSetup g_setup[kMaxDevices];
 
+template <int kD>
 int launch_tc_attend(bool unpacked, const CacheAttendArgs& a, int grid, cudaStream_t st)
 {
-    const cudaError_t e = unpacked ? launch_kernel(tc_cache_attend_kernel<true>, dim3((unsigned)grid), Roles<true>::kThreads, kSmemBytes, st, a)
-                                   : launch_kernel(tc_cache_attend_kernel<false>, dim3((unsigned)grid), Roles<false>::kThreads, kSmemBytes, st, a);
+    const cudaError_t e = unpacked ? launch_kernel(tc_cache_attend_kernel<kD, true>, dim3((unsigned)grid), Roles<true>::kThreads, Dims<kD>::kSmemBytes, st, a)
+                                   : launch_kernel(tc_cache_attend_kernel<kD, false>, dim3((unsigned)grid), Roles<false>::kThreads, Dims<kD>::kSmemBytes, st, a);
     if (e != cudaSuccess) { set_error("launch of tc_cache_attend_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
     return 1;
 }
 
-}  // namespace
-
-int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
+template <int kD>
+int launch_tc(CacheAttendArgs a, int num_sms, cudaStream_t st)
 {
-    int num_sms = 0;
-    if (int r = device_setup_once(g_setup_mutex, g_setup, [] {
-            const cudaError_t e = opt_in_smem(tc_cache_attend_kernel<true>, kSmemBytes);
-            return e == cudaSuccess ? opt_in_smem(tc_cache_attend_kernel<false>, kSmemBytes) : e;
-        }, &num_sms)) return r;
     a.row_blocks = (a.queries * a.rep + kItemRows - 1) / kItemRows;
     a.min_share = 2;
     a.max_parts = 32;
@@ -945,20 +1009,35 @@ int tc_cache_attend(CacheAttendArgs a, cudaStream_t st)
     int launched = 0;
     if (ahead) {
         const long long ctas = pairs < num_sms * 4 ? pairs : num_sms * 4;   // (all of them at once)
-        const cudaError_t e = launch_kernel(cache_unpack_kernel, dim3((unsigned)ctas), kUnpackThreads, 0, st, a);
+        const cudaError_t e = launch_kernel(cache_unpack_kernel<kD>, dim3((unsigned)ctas), kUnpackThreads, 0, st, a);
         if (e != cudaSuccess) { set_error("launch of cache_unpack_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
-        const int r = launch_tc_attend(true, a, (int)grid, st);
+        const int r = launch_tc_attend<kD>(true, a, (int)grid, st);
         if (r < 0) return r;
         launched += 1 + r;
     }
     if (!ahead || a.either) {
-        const int r = launch_tc_attend(false, a, (int)grid, st);
+        const int r = launch_tc_attend<kD>(false, a, (int)grid, st);
         if (r < 0) return r;
         launched += r;
     }
-    const cudaError_t e = launch_kernel(cache_join_kernel, dim3((unsigned)grid * kJoinBlocks), kJoinThreads, 0, st, a);
+    const cudaError_t e = launch_kernel(cache_join_kernel<kD>, dim3((unsigned)grid * kJoinBlocks), kJoinThreads, 0, st, a);
     if (e != cudaSuccess) { set_error("launch of cache_join_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
     return launched + 1;
+}
+
+}  // namespace
+
+int tc_cache_attend(const CacheAttendArgs& a, cudaStream_t st)
+{
+    int num_sms = 0;
+    if (int r = device_setup_once(g_setup_mutex, g_setup, [] {
+            cudaError_t e = opt_in_smem(tc_cache_attend_kernel<128, true>, Dims<128>::kSmemBytes);
+            if (e == cudaSuccess) e = opt_in_smem(tc_cache_attend_kernel<128, false>, Dims<128>::kSmemBytes);
+            if (e == cudaSuccess) e = opt_in_smem(tc_cache_attend_kernel<64, true>, Dims<64>::kSmemBytes);
+            if (e == cudaSuccess) e = opt_in_smem(tc_cache_attend_kernel<64, false>, Dims<64>::kSmemBytes);
+            return e;
+        }, &num_sms)) return r;
+    return a.D == 128 ? launch_tc<128>(a, num_sms, st) : launch_tc<64>(a, num_sms, st);
 }
 
 }  // namespace arl2

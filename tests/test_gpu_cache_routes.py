@@ -79,6 +79,40 @@ def test_operands_on_the_way_where_the_workspace_is_too_small():
     assert (short.float() - torch.cat(parts, 1).float()).abs().max() <= 2.0 ** -6 * short.float().abs().max()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,T,lengths,route", [(2, 150, (517, 260), 3), (1, 300, (1000,), 3), (65, 20, None, 2), (3, 40, (0, 129, 1), 3)])
+def test_many_rows_of_64_channels(B, T, lengths, route, causal):
+    """Heads of 64 channels on tcgen05: operands made ahead, on the way (many streams), empty streams and an unaligned tensor.
+    route: the launches of a call."""
+    rng = np.random.default_rng(T)
+    if lengths is None:
+        lengths = [int(x) for x in rng.integers(0, 300, B)]
+    n = max(lengths)
+    layer, cache, pool, cos, sin = make(B, 4, 2, 64, "bf16", 32, n, rope_rows=max(n, T), L=T)
+    fill_streams(pool, lengths)
+    flat, ff = draw((B * T * 4 * 64 + 1,), "bf16", 61)
+    q, qf = flat[1:].view(B, T, 4, 64), ff[1:].reshape(B, T, 4, 64)          # rows on 2 bytes
+    before = layer.launch_count
+    out = cache.attend(q, start_of(lengths), causal=causal)
+    assert layer.launch_count - before == route
+    layer.sync_status()
+    check(out, *reference(qf, pool, lengths, causal, cos, sin), "bf16", n)
+    assert torch.equal(out, cache.attend(q.clone(), start_of(lengths), causal=causal))
+
+
+def test_context_without_tcgen05_of_64_channels():
+    layer = arl2.Layer(1, 2, 1, 64, "bf16", device=DEV, flags=arl2.ARL2_FLAG_FORCE_SIMT)
+    pool = Pool(1, 2, 64, 32, 333, DEV)
+    cache = arl2.Cache(layer, pool.count, pool.width, page_tokens=32, pages=pool.guard.t, page_table=pool.table)
+    fill_random(pool, 333, 30)
+    q, qf = draw((1, 100, 2, 64), "bf16", 31)
+    before = layer.launch_count
+    out = cache.attend(q, start_of((333,)), causal=True)
+    assert layer.launch_count - before == 1
+    layer.sync_status()
+    check(out, *reference(qf, pool, (333,), True, None, None), "bf16", 333)
+
+
 @pytest.mark.parametrize("B,T,causal", [(33, 1, False), (70, 2, True), (40, 40, False), (66, 36, True)])
 def test_many_streams(B, T, causal):
     """More streams than a plan counts by lanes, than it keeps copies of, and than operands are made ahead for; of lengths that differ."""
