@@ -279,6 +279,29 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
     return own_finite ? p.scale_log2 * down * down2 : __int_as_float(0x7fc00000);
 }
 
+// 2^x of two x <= 8 without the special-function units: 2^n * y(f), n the whole number nearest to x, f = x - n in [-1/2, 1/2] and y the
+// cubic of least relative error there, 7.5e-5 (the probability's rounding to fp16: up to 4.9e-4).  Below 2^-125 it stays there, where
+// an exponential would go to zero: nothing next to a sum that has a term of at least 2^-8.  A NaN stays one.
+// One pair of four goes this way.  us for 12 heads, 1560 rows over 9360 keys, D = 128 and 64, and 4680 over 18720, single calls: none 129,
+// 105, 518; one of eight no better than half of it; one of four 125, 103, 491; one of two 2 to 3 % slower than none.
+constexpr int kByFmaEvery = 4;
+__device__ __forceinline__ void exp2_pair(float x0, float x1, float& p0, float& p1)
+{
+    constexpr float kShift = 12582912.0f;     // 1.5 * 2^23: a sum with it is rounded to a whole number, in its lowest bits
+    auto both = [](float v) { return pack2(v, v); };
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x0) : "f"(-125.0f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x1) : "f"(-125.0f));
+    const uint64_t x = pack2(x0, x1), shifted = add2(x, both(kShift));
+    const uint64_t f = fma2(add2(shifted, both(-kShift)), both(-1.0f), x);
+    uint64_t y = fma2(f, both(0.05517167f), both(0.24261113f));
+    y = fma2(y, f, both(0.69326097f));
+    y = fma2(y, f, both(0.99992806f));
+    float n0, n1;
+    unpack2(shifted, n0, n1);
+    const uint64_t two_n = pack2(__uint_as_float((__float_as_uint(n0) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(n1) << 23) + 0x3f800000u));
+    unpack2(fma2(y, two_n, both(0.0f)), p0, p1);
+}
+
 // ---- one thread per query row.  marks: what is special about the key tiles, in shared memory by key tiles so far, or
 // beside the tiles unpacked ahead (first: place_tiles)
 template <int kD, bool kUnpacked>
@@ -382,9 +405,14 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             const uint64_t neg_m2 = pack2(-m_use, -m_use);
 #pragma unroll
             for (int c = 0; c < 64; ++c) {
-                float x0, x1;
+                float x0, x1, p0, p1;
                 unpack2(fma2(pack2(__uint_as_float(sreg[2 * c]), __uint_as_float(sreg[2 * c + 1])), c2x2, neg_m2), x0, x1);
-                const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                if (c % kByFmaEvery == kByFmaEvery - 1) {
+                    exp2_pair(x0, x1, p0, p1);
+                } else {
+                    p0 = ex2_approx(x0);
+                    p1 = ex2_approx(x1);
+                }
                 l2 = add2(l2, pack2(p0, p1));
                 sreg[c] = pack_f16(p0, p1);
             }
