@@ -362,15 +362,24 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             (void)wait_bar(bar_s, s_cnt & 1, ab, 120 + t);   // (where it expired, the loop goes on over whatever is there)
             ++s_cnt;
             tc_fence_after();
+            const int n_valid = sees - key0;
+            if (__any_sync(0xffffffffu, n_valid < kTile)) {
+                // (in tensor memory: as another state of the registers below it cost every tile, 1 %)
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t x[32];
+                    tmem_ld32(s_addr + c * 32, x);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c * 32 + e >= n_valid) x[e] = __float_as_uint(-INFINITY);
+                    tmem_st32(s_addr + c * 32, x);
+                }
+                tmem_wait_st();
+            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sreg[c * 32]));
             tmem_wait_ld();
-            const int n_valid = sees - key0;
-            if (n_valid < kTile) {
-#pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if (c >= n_valid) sreg[c] = __float_as_uint(-INFINITY);
-            }
             if (p.causal && jj > 0) {     // (V of the tile before is there: P V has been computed)
                 if (!kUnpacked) special = mark_word(jj - 1, 0);
                 if (special != 0) poison_of(jj - 1);
@@ -407,6 +416,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             }
             const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;     // (no key seen so far)
             const uint64_t neg_m2 = pack2(-m_use, -m_use);
+            uint64_t pair = 0;
             // P V of the first half of the keys runs beside the exponentials of the second (12 heads, 1560 rows over 9360 keys: 1 %)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -420,7 +430,8 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
                         p0 = ex2_approx(x0);
                         p1 = ex2_approx(x1);
                     }
-                    l2 = add2(l2, pack2(p0, p1));
+                    if (c % 2 == 0) pair = pack2(p0, p1);
+                    else l2 = add2(l2, add2(pair, pack2(p0, p1)));      // (half the steps one after another)
                     sreg[c] = pack_f16(p0, p1);
                 }
                 tmem_st32(s_addr + half * 32, *reinterpret_cast<uint32_t(*)[32]>(&sreg[half * 32]));
