@@ -90,6 +90,11 @@ struct Cut {
 template <int kRows, int kChunk, bool kByHead, int kThreads>
 struct Planner {
     static constexpr int kWarps = kThreads / 32;
+    // Chunks more per CTA at which a CTA is given work of one item only: a second item costs it about as much as three chunks do (its
+    // rows of Q, its partial rows).  us with 0, 1 and 3, and without: 2 streams of 4 key heads, 21 rows over 3001 keys 21.0, 20.9, 21.0
+    // and 27.8; 6 rows over 300 9.9, 10.0, 10.0 and 14.3; 4 of 12, one row over 9360 24.7, 22.9, 22.7 and 24.5; 12 heads, 64 rows over 9360
+    // (tcgen05) 39.4, 38.0, 38.1 and 39.1; where items end with CTAs anyway the search costs 0.2.
+    static constexpr uint32_t kSlack = 3;
 
     // Chunks of (stream, block of rows); never none, so that rows without keys are written too.
     static __device__ __forceinline__ int chunks_of(int seen) { return max(1, (seen + kChunk - 1) / kChunk); }
@@ -193,11 +198,12 @@ struct Planner {
     {
         for (int b = threadIdx.x; b < min(p.s_B, kPlanStreams); b += kThreads) Streams::look_up(p, b, st.have[b], st.first[b]);
         __syncthreads();
-        // Up to 32 streams whose blocks of rows all see the same keys: a lane per stream, every warp for itself.
+        // Up to 32 streams whose blocks of rows see the same keys, or nearly: a lane per stream, every warp for itself.
         const int lane = threadIdx.x & 31;
-        const bool few = p.s_B <= 32 && (!p.causal || p.row_blocks == 1);
-        int each = 0;
-        if (few && lane < p.s_B) each = unit_chunks(p, st, lane, 0);
+        const bool even = !p.causal || p.row_blocks == 1;
+        const bool few = p.s_B <= 32 && (even || (!kByHead && p.row_blocks * kRows <= kChunk));
+        int each = 0;      // (the last block of rows sees the most)
+        if (few && lane < p.s_B) each = unit_chunks(p, st, lane, p.row_blocks - 1);
         const long long items = (long long)p.row_blocks * p.c.kv_heads;          // of a stream
         if (!few || __any_sync(0xffffffffu, each * items >= 1LL << 25)) {        // (what follows counts in 32 bits)
             general(p, st, cta, ctas, scratch, slow);
@@ -213,10 +219,40 @@ struct Planner {
         const uint32_t total = __shfl_sync(0xffffffffu, upto, 31), longest = (uint32_t)__reduce_max_sync(0xffffffffu, each);
         Cut c;
         c.whole = 0;
-        if (kByHead && __all_sync(0xffffffffu, lane >= p.s_B || each == (int)longest)) c.whole = (int)((uint32_t)(p.s_B * (uint32_t)items) / (uint32_t)ctas);
+        if (kByHead && even && __all_sync(0xffffffffu, lane >= p.s_B || each == (int)longest)) c.whole = (int)((uint32_t)(p.s_B * (uint32_t)items) / (uint32_t)ctas);
         const uint32_t base = (uint32_t)c.whole * (uint32_t)ctas * longest;
         const uint32_t fewest = max((uint32_t)p.min_share, (longest + (uint32_t)p.max_parts - 1) / (uint32_t)p.max_parts);
         const uint32_t share = max(fewest, (total - base + (uint32_t)ctas - 1) / (uint32_t)ctas);
+        // Where it costs at most kSlack chunks more, every CTA has work of one item only: part by part of an item, then the next item's.
+        if (c.whole == 0) {
+            for (uint32_t alone = share; alone <= share + kSlack; ++alone) {
+                const uint32_t parts = ((uint32_t)each + alone - 1) / alone, ctas_of = parts * (uint32_t)items;     // of an item, and of a stream
+                uint32_t until = ctas_of;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const uint32_t x = __shfl_up_sync(0xffffffffu, until, d);
+                    if (lane >= d) until += x;
+                }
+                if (__shfl_sync(0xffffffffu, until, 31) > (uint32_t)ctas) continue;
+                const uint32_t here = __ballot_sync(0xffffffffu, until - ctas_of <= (uint32_t)cta && (uint32_t)cta < until);
+                const int b = here != 0 ? __ffs(here) - 1 : 0;
+                const uint32_t from = __shfl_sync(0xffffffffu, until - ctas_of, b), of = max(1u, __shfl_sync(0xffffffffu, parts, b));
+                const uint32_t item = here != 0 ? ((uint32_t)cta - from) / of : 0;
+                c.base = 0;
+                c.share = alone;
+                c.place = split(p, item);
+                c.place.b = b;
+                c.place.item_begin = (long long)(from + item * of) * alone;
+                c.begin = (long long)alone * cta;
+                const int chunks = even ? __shfl_sync(0xffffffffu, each, b) : unit_chunks(p, st, b, c.place.rb);
+                c.end = here != 0 ? max(c.begin, min(c.begin + alone, c.place.item_begin + chunks)) : c.begin;
+                return c;
+            }
+        }
+        if (!even) {
+            general(p, st, cta, ctas, scratch, slow);
+            return *slow;
+        }
         const uint32_t begin = (uint32_t)min((long long)total, (long long)base + (long long)share * cta);
         c.base = base;
         c.share = share;
