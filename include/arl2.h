@@ -304,7 +304,9 @@ size_t arl2_cache_workspace_bytes(const arl2_config* cfg, const arl2_cache_confi
  *   d_pages       [num_pages, arl2_cache_page_bytes] bytes, 128-byte aligned; not cleared
  *   d_page_table  [B, max_pages] int32, may be rewritten between calls in stream order
  *   d_rope_cos, d_rope_sin  [rope_rows, D/2] fp32, 16-byte aligned; both NULL where rope_rows is 0
- *   d_workspace   private to this cache until arl2_cache_destroy
+ *   d_workspace   private to this cache until arl2_cache_destroy.  Partial rows, and with bf16 I/O operand tiles: room for all
+ *                 tokens of all streams as fp16 and for a block of L queries, as far as 256 MB (D = 128; 128 MB at D = 64) go.
+ *                 A call that needs more of it converts on the way and is slower, no more.
  * All stay the caller's.  Launches one small kernel on `stream`.  Calls on one cache are ordered by the caller (one stream, or
  * events between streams): they share the workspace.  Calls may be captured and replayed.
  */
@@ -337,6 +339,8 @@ int arl2_cache_append(arl2_cache* cache, const void* d_k, int64_t k_batch_stride
  * rotary tables counts as the last there is, a page that the pool does not have reads as zeros, and arl2_sync_status reports
  * ARL2_ERR_RANGE.  bf16 I/O: fp16 operands on tensor cores, fp32 softmax and sums; fp32 I/O: each
  * fp32 operand as two fp16 numbers (the codes are exact), to fp32's accuracy.  Bitwise reproducible.
+ * More than 32 rows (queries * H / kv_heads) with bf16 I/O go to tcgen05 kernels, three or four launches; all else, and every call
+ * of an ARL2_FLAG_FORCE_SIMT context, to one kernel of warp-level matrix instructions.  `queries` need not be L.
  */
 #define ARL2_CACHE_CAUSAL 1u
 int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride, int64_t q_token_stride, int32_t queries,

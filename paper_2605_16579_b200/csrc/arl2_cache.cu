@@ -4,9 +4,10 @@
 // 64 channels with its 3 neighbours, and writes two words of 8 codes.  4 D bytes (bf16) are read per token and head and 9/8 D written,
 // but what bounds it is the instructions: about 18 a value, of which minimum, maximum, quotient and clamp are on the half-rate pipe.
 // One head per row group, K and V of it: with two, which fetch the token's row of the rotary tables once, 40 heads x 4 x 4680 tokens took
-// 175 us, with one, and twice the warps on an SM, 157.
+// 175 us, with one, and twice the warps on an SM, 157.  Now 152 in a row: 877 MB at 5.8 TB/s, 0.88 of the rate of a copy; 183 where
+// other work has emptied L2 in between.  One token of each stream: 6 us, of which the kernel has about 2.
 //
-// Attention (one query per stream up to a few dozen rows; any number in fp32 and with D = 64).  Keys are the M side of the
+// Attention (one query per stream up to a few dozen rows; any number in fp32).  Keys are the M side of the
 // matrix instruction and query rows the N side, so that 8 rows fill it:  S^T = K Q^T, then  O^T = V^T P^T.  Codes go into the
 // instruction as they are: four bits of a word, masked out where they stand, are the fp16 denormal code * 2^-24 (bits 0-3 of a
 // half) or code * 2^-20 (bits 4-7), both exact.  With minimum lo and step st per key and group g of channels,
@@ -16,6 +17,11 @@
 // grows like the softmax's reference maximum.  fp32 I/O: q and p st as two fp16 numbers each, twice the instructions, and codes
 // less 8 as whole numbers (an addition per pair): with unsigned ones the sums of 64 products, from which the minimum's part is
 // subtracted, lost five bits (errors of 3e-6 to 9e-6 of the output, now 1e-7).
+// What bounds it over long caches is the instructions of a warp, about 264 per 16 keys and 8 rows (two products, the scores' factors, the
+// exponentials), which wait for one another: issue slots 55 %, tensor pipe 25 %, DRAM 51 % busy.  Over short ones, what a CTA does once:
+// plan, rows of Q, first keys, its four warps' rows put together, and the item's parts (a part more costs about 0.4 us at 16 rows).  us in
+// a row: one query in each of 4 streams of 12 heads over 74880 tokens 103 (518 MB, 5.0 TB/s, 0.77 of a copy's rate); 8 streams of 40
+// heads on 8 over 9360 32; 12 heads over 500 9.7; fp32, 2 heads, 256 rows over 768 14.6.
 #include <cuda_bf16.h>
 
 #include <atomic>

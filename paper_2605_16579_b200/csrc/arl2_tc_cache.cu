@@ -4,9 +4,9 @@
 // tiles of 128 form one sequence that is cut evenly over the CTAs (cache_common.cuh).  Roles:
 //   warps 0-3 / 4-7   softmax group of tile 0 / 1, one thread per query row
 //   two warps         MMA issuer of tile 0 / 1:  S_t = Q_t K_j^T and O_t += P_t V_j into TMEM
-// The operands are tiles of 128 rows (32 KB at D = 128): Q's rows, rotated in fp32, scaled by a power of two into fp16's range and rounded to fp16; K and V
-// as minimum + step * code in fp16 (in which the codes are exact; its rounding, 2^-12, is an eighth of bf16's), through a ring.  They
-// are made in one of two ways:
+// The operands are tiles of 128 rows (32 KB at D = 128): Q's rows, rotated in fp32, scaled by a power of two into fp16's range and
+// rounded to fp16; K and V as minimum + step * code in fp16 (in which the codes are exact; its rounding, 2^-12, is an eighth of
+// bf16's), through a ring.  They are made in one of two ways:
 //     ahead       cache_unpack_kernel writes all of them to the workspace, as they stand in shared memory, and one thread copies them
 //                 in.  Costs 512 bytes per key and head written and read again, once per call.
 //     on the way  four warps read codes and parameters, one tile ahead, and write the tiles of K and V, the softmax groups those of Q:
@@ -18,6 +18,13 @@
 //
 // An item that several CTAs work on leaves unnormalised fp32 rows, which cache_join_kernel puts together.
 // Every wait is bounded, as in the step kernel.
+//
+// What bounds it: of a key tile's 3800 clk, the tensor pipe works 2048 (D = 128), the special-function units 1536; the rest is a
+// group's own chain - scores, maximum, exponentials, P V, the next scores - of which the other group hides only a part.  Two threads per
+// row (registers spilled: 141 us for 113), scores of 64 keys at a time, two sets of them (131), and issuers that do not take turns (131)
+// were slower.  12 heads, D = 128, us in a row: 1560 rows over 9360 keys 111, of which the unpacking has 17 (26 MB read, 67 MB written)
+// and the joining 8 (28 MB of partial rows), 810 TFLOP/s in all, 0.49 of a large matrix product's rate; 4680 over 18720 485 alone
+// (1110 TFLOP/s, 0.67), 528 under the power limit.  At D = 64 1560 over 9360 take 90.
 #include <type_traits>
 
 #include "cache_common.cuh"
