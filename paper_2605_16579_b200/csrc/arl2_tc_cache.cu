@@ -160,130 +160,95 @@ __device__ __forceinline__ uint4 hold_word(uint32_t codes, __half2 low, __half2 
 }
 
 // ---- the Q operand of kWarpRows rows, from row `row0` of block rb of (b, h) on: rotated in fp32, scaled by a power of two into fp16's
-// range, rounded to fp16.  `first`: the position of the stream's first query, rows: the block's.  A row at a time by the whole warp,
-// kBatch rows' loads in flight.  Lane l gets the factor of row l's scores.
+// range, rounded to fp16.  `first`: the position of the stream's first query, rows: the block's.  A lane has eight channels of a row, a
+// warp two or four rows at a time; kBatch such steps' loads are in flight.  Lane l gets the factor of row l's scores.
 template <int kD, int kWarpRows, int kBatch>
 __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb, int h, int first, int rows, uint8_t* tile, int row0, int lane)
 {
-    int own_e2 = 0;
-    bool own_finite = true;
-    // lane l: where row l's channels are, and its row of the rotary tables
-    const int own_flat = rb * kItemRows + min(row0 + (lane & (kWarpRows - 1)), rows - 1);
-    const int own_i = own_flat / p.rep, own_head = h * p.rep + own_flat - own_i * p.rep;
-    const __nv_bfloat16* own_src = static_cast<const __nv_bfloat16*>(p.q) + b * p.q_batch + own_i * p.q_token + (size_t)own_head * kD;
-    long long own_at = max((long long)first + own_i, 0LL);
-    if (p.c.rope_cos != nullptr && own_at >= p.c.rope_rows) {
-        range_error(p.c.status, kRangePosition, b);
-        own_at = p.c.rope_rows - 1;
-    }
+    constexpr int kLanes = kD / 8, kAtOnce = 32 / kLanes;      // lanes of a row, rows of a step
+    static_assert(kWarpRows % (kAtOnce * kBatch) == 0, "whole batches");
+    const int within = lane / kLanes, chunk = lane % kLanes;
+    float own = 0.0f;
 #pragma unroll 1
-    for (int r0 = 0; r0 < kWarpRows; r0 += kBatch) {
+    for (int r0 = 0; r0 < kWarpRows; r0 += kAtOnce * kBatch) {
         // (no branch and nothing that is written among the loads: they would wait for one another)
-        constexpr int kPer = kD / 32, kPairs = kPer / 2;       // channels of a lane, and rotation pairs
-        float x[kBatch][kPer], cs[kBatch][kPairs], sn[kBatch][kPairs];
-        auto src_of = [&](int k) {
-            return reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own_src), r0 + k)) + lane * kPer;
-        };
+        const __nv_bfloat16* src[kBatch];
+        int at[kBatch];
+        bool past = false;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int flat = rb * kItemRows + min(row0 + r0 + k * kAtOnce + within, rows - 1), i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
+            src[k] = static_cast<const __nv_bfloat16*>(p.q) + b * p.q_batch + i * p.q_token + (size_t)head * kD + chunk * 8;
+            const long long t = max((long long)first + i, 0LL);
+            past |= t >= p.c.rope_rows;
+            at[k] = (int)min(t, (long long)max(p.c.rope_rows, 1) - 1);
+        }
+        float x[kBatch][8], cs[kBatch][4], sn[kBatch][4];
         if (p.wide) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const __nv_bfloat16* src = src_of(k);
-                uint32_t w[2];
-                if constexpr (kPairs == 2) {
-                    const uint2 v = *reinterpret_cast<const uint2*>(src);
-                    w[0] = v.x;
-                    w[1] = v.y;
-                } else {
-                    w[0] = *reinterpret_cast<const uint32_t*>(src);
-                }
+                const uint4 v = *reinterpret_cast<const uint4*>(src[k]);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int m = 0; m < kPairs; ++m) {
+                for (int m = 0; m < 4; ++m) {
                     x[k][2 * m] = __uint_as_float(w[m] << 16);
                     x[k][2 * m + 1] = __uint_as_float(w[m] & 0xFFFF0000u);
                 }
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                const __nv_bfloat16* src = src_of(k);
+            for (int k = 0; k < kBatch; ++k)
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) x[k][e] = __bfloat162float(src[e]);
-            }
+                for (int e = 0; e < 8; ++e) x[k][e] = __bfloat162float(src[k][e]);
         }
         if (p.c.rope_cos != nullptr) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const int at = __shfl_sync(0xffffffffu, (int)own_at, r0 + k);
-                const float* c = p.c.rope_cos + (size_t)at * (kD / 2) + lane * kPairs;
-                const float* s = p.c.rope_sin + (size_t)at * (kD / 2) + lane * kPairs;
-                if constexpr (kPairs == 2) {
-                    const float2 c2 = *reinterpret_cast<const float2*>(c), s2 = *reinterpret_cast<const float2*>(s);
-                    cs[k][0] = c2.x; cs[k][kPairs - 1] = c2.y;
-                    sn[k][0] = s2.x; sn[k][kPairs - 1] = s2.y;
-                } else {
-                    cs[k][0] = *c;
-                    sn[k][0] = *s;
-                }
+                const float4 c = *reinterpret_cast<const float4*>(p.c.rope_cos + (size_t)at[k] * (kD / 2) + chunk * 4);
+                const float4 s = *reinterpret_cast<const float4*>(p.c.rope_sin + (size_t)at[k] * (kD / 2) + chunk * 4);
+                cs[k][0] = c.x; cs[k][1] = c.y; cs[k][2] = c.z; cs[k][3] = c.w;
+                sn[k][0] = s.x; sn[k][1] = s.y; sn[k][2] = s.z; sn[k][3] = s.w;
             }
+            if (past) range_error(p.c.status, kRangePosition, b);
         } else {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k)
 #pragma unroll
-                for (int m = 0; m < kPairs; ++m) {
+                for (int m = 0; m < 4; ++m) {
                     cs[k][m] = 1.0f;
                     sn[k][m] = 0.0f;
                 }
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            float y[kPer];
+            float y[8];
             uint32_t most = 0;
 #pragma unroll
-            for (int m = 0; m < kPairs; ++m) {
+            for (int m = 0; m < 4; ++m) {
                 y[2 * m] = x[k][2 * m] * cs[k][m] - x[k][2 * m + 1] * sn[k][m];
                 y[2 * m + 1] = x[k][2 * m] * sn[k][m] + x[k][2 * m + 1] * cs[k][m];
                 // (as whole numbers the magnitudes are in the same order, infinities and NaN above all others)
                 most = max(most, max(__float_as_uint(y[2 * m]) & 0x7fffffffu, __float_as_uint(y[2 * m + 1]) & 0x7fffffffu));
             }
-            most = __reduce_max_sync(0xffffffffu, most);
-            // 2^e with 1024 <= most * 2^e < 2048; a row with an infinity or a NaN has no finite scores: its factor is NaN
+#pragma unroll
+            for (int d = 1; d < kLanes; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+            // 2^e with 1024 <= most * 2^e < 2048, -117 <= e <= 126; a row with an infinity or a NaN has no finite scores: its factor is NaN
             const bool finite = most < 0x7f800000u;
             const int e2 = !finite || most == 0 ? 0 : min(137 - (int)(most >> 23), 126);
-            const float up = __uint_as_float((uint32_t)(127 + (e2 >> 1)) << 23), up2 = __uint_as_float((uint32_t)(127 + e2 - (e2 >> 1)) << 23);
-            if (lane == r0 + k) {
-                own_e2 = e2;
-                own_finite = finite;
-            }
-            const bool zero = !finite || row0 + r0 + k >= rows;
-            uint32_t w[kPairs];
+            const int row = r0 + k * kAtOnce + within;
+            const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
+            const float factor = finite ? p.scale_log2 * __uint_as_float((uint32_t)(127 - e2) << 23) : __int_as_float(0x7fc00000);
+            const float given = __shfl_sync(0xffffffffu, factor, (lane % kAtOnce) * kLanes);
+            if (lane / kAtOnce == (r0 / kAtOnce) + k) own = given;
+            const bool zero = !finite || row0 + row >= rows;
+            uint32_t w[4];      // columns 0 4 1 5 2 6 3 7 of the eight channels
 #pragma unroll
-            for (int m = 0; m < kPairs; ++m) w[m] = zero ? 0u : pack_f16(y[2 * m] * up * up2, y[2 * m + 1] * up * up2);
-            // Columns of eight channels hold 0 4 1 5 | 2 6 3 7, eight bytes each: who has channels 4 .. 7 gives them to who has 0 .. 3.
-            const int row = (row0 & (kTile - 1)) + r0 + k;
-            uint32_t lo, hi;       // channels n, n + 1 and n + 4, n + 5
-            int chunk, part;
-            bool writes = true;
-            if constexpr (kPairs == 2) {      // even lanes have 0 .. 3, odd ones 4 .. 7; each writes eight bytes
-                const uint32_t give = (lane & 1) ? w[0] : w[kPairs - 1], got = __shfl_xor_sync(0xffffffffu, give, 1);
-                lo = (lane & 1) ? got : w[0];
-                hi = (lane & 1) ? w[kPairs - 1] : got;
-                chunk = lane >> 1;
-                part = lane & 1;
-            } else {                          // of four lanes the first two write, with what the last two give
-                lo = w[0];
-                hi = __shfl_xor_sync(0xffffffffu, w[0], 2);
-                chunk = lane >> 2;
-                part = lane & 1;
-                writes = (lane & 2) == 0;
-            }
-            if (writes)
-                *reinterpret_cast<uint2*>(tile + (chunk >> 3) * kHalfBytes + row * 128 + (((chunk & 7) ^ (row & 7)) << 4) + part * 8) =
-                    make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+            for (int m = 0; m < 4; ++m) w[m] = zero ? 0u : pack_f16(y[m] * up, y[m + 4] * up);
+            const int in_tile = (row0 & (kTile - 1)) + row;
+            *reinterpret_cast<uint4*>(tile + (chunk >> 3) * kHalfBytes + in_tile * 128 + (((chunk & 7) ^ (in_tile & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    // (both factors have exponents that a float has)
-    const float down = __uint_as_float((uint32_t)(127 - (own_e2 >> 1)) << 23), down2 = __uint_as_float((uint32_t)(127 - own_e2 + (own_e2 >> 1)) << 23);
-    return own_finite ? p.scale_log2 * down * down2 : __int_as_float(0x7fc00000);
+    return own;
 }
 
 // 2^x of two x <= 8 without the special-function units: 2^n * y(f), n the whole number nearest to x, f = x - n in [-1/2, 1/2] and y the
@@ -339,7 +304,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             c2 = p.q_scale[q_pair(p, seg.at) * kItemRows + in_item];
         } else {
             // (Every MMA that read the item before's Q has ended: its last scores have been here.)
-            c2 = write_q<kD, 32, 8>(p, seg.at.b, seg.at.rb, seg.at.h, seg.first, seg.rows, smem + t * Dims<kD>::kOperand, t * kTile + warp_in_group * 32, r & 31);
+            c2 = write_q<kD, 32, 4>(p, seg.at.b, seg.at.rb, seg.at.h, seg.first, seg.rows, smem + t * Dims<kD>::kOperand, t * kTile + warp_in_group * 32, r & 31);
             fence_proxy_async_smem();
             mbar_arrive(bars + 8 * (kBarQ0 + t));
         }
@@ -867,9 +832,12 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
     grid_dependency_sync();
     if (!place_tiles(p, first)) return;
     constexpr int kQParts = 4;      // of a block of query rows
-    const int pairs = first[p.s_B] * p.c.kv_heads, q_works = p.s_B * p.c.kv_heads * p.row_blocks * kQParts;
-    int work = (int)blockIdx.x;
-    for (; work < q_works; work += (int)gridDim.x) {
+    const int tiles = 2 * first[p.s_B] * p.c.kv_heads, q_works = p.s_B * p.c.kv_heads * p.row_blocks * kQParts;
+    // Some CTAs make rows of Q, 64 of which take them about as long as two tiles do the others: so that one's loads are waited for beside
+    // the other's work (12 heads, 1560 rows over 9360 keys 112.7 -> 111.1 us in a row, 64 over 600 18.2 -> 17.8).
+    const int ctas = (int)gridDim.x;      // (at least two)
+    const int q_ctas = tiles == 0 ? ctas : min(ctas - 1, max(1, (int)(ctas * (2LL * q_works) / (2LL * q_works + tiles))));
+    for (int work = (int)blockIdx.x; (int)blockIdx.x < q_ctas && work < q_works; work += q_ctas) {
         const int block = work / kQParts, bh = block / p.row_blocks;
         Place at;
         at.rb = block - bh * p.row_blocks;
@@ -880,11 +848,12 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
         Streams::look_up(p, at.b, have, position);
         constexpr int kWarpRows = kItemRows / kQParts / (kUnpackThreads / 32);
         const int row0 = (work % kQParts) * (kItemRows / kQParts) + (tid >> 5) * kWarpRows, lane = tid & 31;
-        const float scale = write_q<kD, kWarpRows, 8>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
+        const float scale = write_q<kD, kWarpRows, 2>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
                                         p.unpacked + pair * kUnpackPair + (row0 / kTile) * kTileBytes, row0, lane);
         if (lane < kWarpRows) p.q_scale[pair * kItemRows + row0 + lane] = scale;
     }
-    // Then tiles, K (even) and V (odd) of a pair.  A thread has every kStep-th row of a tile; the next tile's are fetched while
+    if ((int)blockIdx.x < q_ctas) return;
+    // Tiles, K (even) and V (odd) of a pair.  A thread has every kStep-th row of a tile; the next tile's are fetched while
     // this one's are written.
     struct Rows {
         uint4 codes[kRowsEach];
@@ -914,12 +883,13 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
             }
         }
     };
-    int tile_no = work - q_works;
+    const int step = ctas - q_ctas;
+    int tile_no = (int)blockIdx.x - q_ctas;
     Rows next;
-    if (tile_no < 2 * pairs) fetch(tile_no, next);
-    for (; tile_no < 2 * pairs; tile_no += (int)gridDim.x) {
+    if (tile_no < tiles) fetch(tile_no, next);
+    for (; tile_no < tiles; tile_no += step) {
         Rows cur = next;
-        if (tile_no + (int)gridDim.x < 2 * pairs) fetch(tile_no + (int)gridDim.x, next);
+        if (tile_no + step < tiles) fetch(tile_no + step, next);
         if (p.causal && (tile_no & 1)) {      // values that are not finite are taken out, and softmax told
             __syncthreads();
             if (tid < kUnpackMarks) marks[tid] = 0;

@@ -224,9 +224,10 @@ struct Planner {
         const uint32_t fewest = max((uint32_t)p.min_share, (longest + (uint32_t)p.max_parts - 1) / (uint32_t)p.max_parts);
         const uint32_t share = max(fewest, (total - base + (uint32_t)ctas - 1) / (uint32_t)ctas);
         // Where it costs at most kSlack chunks more, every CTA has work of one item only: part by part of an item, then the next item's.
-        if (c.whole == 0) {
+        auto parts_of = [&](uint32_t alone) { return ((uint32_t)each + alone - 1) / alone; };      // of an item
+        if (c.whole == 0 && __reduce_add_sync(0xffffffffu, parts_of(share + kSlack) * (uint32_t)items) <= (uint32_t)ctas) {
             for (uint32_t alone = share; alone <= share + kSlack; ++alone) {
-                const uint32_t parts = ((uint32_t)each + alone - 1) / alone, ctas_of = parts * (uint32_t)items;     // of an item, and of a stream
+                const uint32_t parts = parts_of(alone), ctas_of = parts * (uint32_t)items;     // of an item, and of a stream
                 uint32_t until = ctas_of;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
