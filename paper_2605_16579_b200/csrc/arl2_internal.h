@@ -235,7 +235,7 @@ struct CacheAttendArgs {
     int causal;
     float scale_log2;
     void* out;
-    float* part_o;           // [kCachePartRows, D] unnormalised rows
+    float* part_o;           // [kCachePartRows, D] unnormalised rows (by eight channels where tcgen05 makes them)
     float* part_ml;          // [kCachePartRows, 2] reference maximum (log2 units), row sum
     uint32_t* tickets;       // [kCacheCtas], zero between calls
     int4* part_items;        // [kCacheTcCtas] the item that a CTA of the tcgen05 kernel began and others went on with: parts, stream, block of rows, key head

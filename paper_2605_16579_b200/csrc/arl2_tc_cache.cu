@@ -25,8 +25,6 @@
 // were slower.  12 heads, D = 128, us in a row: 1560 rows over 9360 keys 111, of which the unpacking has 17 (26 MB read, 67 MB written)
 // and the joining 8 (28 MB of partial rows), 810 TFLOP/s in all, 0.49 of a large matrix product's rate; 4680 over 18720 485 alone
 // (1110 TFLOP/s, 0.67), 528 under the power limit.  At D = 64 1560 over 9360 take 90.
-#include <type_traits>
-
 #include "cache_common.cuh"
 #include "tc_common.cuh"
 
@@ -425,58 +423,54 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
         const Parts parts = item_parts(cut, seg);
         if (parts.count > 1 && parts.first == (int)blockIdx.x) begun = make_int4(parts.count, seg.at.b, seg.at.rb, seg.at.h);
         const float nan = __int_as_float(0x7fc00000);
-        if (parts.count > 1) {
-            const size_t row = (size_t)parts.slot((int)blockIdx.x) * kItemRows + in_item;
-            float* dst = p.part_o + row * kD;
+        const size_t slot = (size_t)parts.slot((int)blockIdx.x);
+        const float inv_l = l_sum == 0.0f ? 0.0f : 1.0f / l_sum;
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)seg.at.b * p.queries + i) * p.H + head) * kD;
+        const bool wide = wide_rows(p.out);
 #pragma unroll 1
-            for (int c = 0; c < kD / 32; ++c) {
-                uint32_t o[32];
-                tmem_ld32(o_addr + c * 32, o);
-                tmem_wait_ld();
-                if (poison & (c < 2 ? 1u : 2u)) {
+        for (int g = 0; g < kD / kCacheGroup; ++g) {
+            uint32_t* o = sreg;
+            tmem_ld32(o_addr + g * 64, *reinterpret_cast<uint32_t(*)[32]>(&sreg[0]));
+            tmem_ld32(o_addr + g * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&sreg[32]));
+            tmem_wait_ld();
+            if (parts.count > 1) {
+                // [eight channels][row]: a warp's stores are of whole lines
+                float* part = p.part_o + ((slot * (kD / 8) + g * 8) * kItemRows + in_item) * 8;
+                if (poison & (1u << g)) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(nan);
+                    for (int e = 0; e < 64; ++e) o[e] = __float_as_uint(nan);
                 }
+                if (valid) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) w[k] = o[column_of(e * 8 + k)];
+                        store_row32(part + (size_t)e * kItemRows * 8, w);
+                    }
+                }
+            } else {
+                const float f = (poison & (1u << g)) ? nan : inv_l;
                 if (valid) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         uint32_t w[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) w[k] = o[column_of(e * 8 + k)];
-                        store_row32(dst + c * 32 + e * 8, w);
-                    }
-                }
-            }
-            if (valid) *reinterpret_cast<float2*>(p.part_ml + row * 2) = make_float2(m_ref, l_sum);
-        } else {
-            const float inv_l = l_sum == 0.0f ? 0.0f : 1.0f / l_sum;
-            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)seg.at.b * p.queries + i) * p.H + head) * kD;
-            const bool wide = wide_rows(p.out);
-#pragma unroll 1
-            for (int c = 0; c < kD / 32; ++c) {
-                uint32_t o[32];
-                tmem_ld32(o_addr + c * 32, o);
-                tmem_wait_ld();
-                const float f = (poison & (c < 2 ? 1u : 2u)) ? nan : inv_l;
-                if (valid) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t w[8];
-#pragma unroll
                         for (int k = 0; k < 8; ++k)
                             w[k] = pack_bf16(__uint_as_float(o[column_of(e * 16 + 2 * k)]) * f, __uint_as_float(o[column_of(e * 16 + 2 * k + 1)]) * f);
-                        if (wide) store_row32(dst + c * 32 + e * 16, w);
+                        if (wide) store_row32(dst + g * 64 + e * 16, w);
                         else {
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                dst[c * 32 + e * 16 + 2 * k] = __ushort_as_bfloat16((unsigned short)(w[k] & 0xffffu));
-                                dst[c * 32 + e * 16 + 2 * k + 1] = __ushort_as_bfloat16((unsigned short)(w[k] >> 16));
+                                dst[g * 64 + e * 16 + 2 * k] = __ushort_as_bfloat16((unsigned short)(w[k] & 0xffffu));
+                                dst[g * 64 + e * 16 + 2 * k + 1] = __ushort_as_bfloat16((unsigned short)(w[k] >> 16));
                             }
                         }
                     }
                 }
             }
         }
+        if (parts.count > 1 && valid) *reinterpret_cast<float2*>(p.part_ml + (slot * kItemRows + in_item) * 2) = make_float2(m_ref, l_sum);
         tc_fence_before();
     }
     if (mine && t == 0 && r == 0) p.part_items[blockIdx.x] = begun;     // (of the two kernels that may be there, one has done the work)
@@ -927,8 +921,8 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
 }
 
 // ---- rows of the items that several CTAs share.  Block x of a launch of ctas x kJoinBlocks looks after part of the item that CTA
-// x / kJoinBlocks began and did not end, if there is one: a warp per row, the parts in the order of their CTAs.
-constexpr int kJoinBlocks = 8, kJoinThreads = 256;
+// x / kJoinBlocks began and did not end, if there is one: a lane per row, a warp per 8 or 16 channels, the parts in the order of their CTAs.
+constexpr int kJoinBlocks = kItemRows / 32, kJoinThreads = 256;
 template <int kD>
 __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAttendArgs p)
 {
@@ -936,68 +930,60 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const CacheAtt
     grid_dependency_sync();
     const int4 item = p.part_items[cta];       // parts, stream, block of rows, key head
     if (item.x < 2 || p.c.status[kStatusError] != 0u) return;
-    constexpr int kRowsEach = kItemRows / kJoinBlocks / (kJoinThreads / 32);
-    const int rows = min(kItemRows, p.queries * p.rep - item.z * kItemRows);
-    const int r0 = ((int)blockIdx.x % kJoinBlocks) * (kItemRows / kJoinBlocks) + warp * kRowsEach;
-    if (r0 >= rows) return;
+    constexpr int kEights = kD / 8 / (kJoinThreads / 32);      // of channels, of a warp
+    const int row = ((int)blockIdx.x % kJoinBlocks) * 32 + lane;
+    if (row >= min(kItemRows, p.queries * p.rep - item.z * kItemRows)) return;
     const Parts parts{cta, item.x};
-    // rows that are not there are computed from whatever the workspace holds, and not written
-    float m[kRowsEach], total[kRowsEach];
-    constexpr int kPer = kD / 32;      // channels of a lane
-    using Vec = typename std::conditional<kPer == 4, float4, float2>::type;
-    float acc[kRowsEach][kPer];
+    float m = -INFINITY, total = 0.0f, acc[kEights][8];
 #pragma unroll
-    for (int x = 0; x < kRowsEach; ++x) {
-        m[x] = -INFINITY;
-        total[x] = 0.0f;
+    for (int c = 0; c < kEights; ++c)
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[x][e] = 0.0f;
-    }
+        for (int e = 0; e < 8; ++e) acc[c][e] = 0.0f;
     constexpr int kBatch = 3;      // parts asked for at once
     for (int w0 = 0; w0 < parts.count; w0 += kBatch) {
-        float2 ml[kBatch][kRowsEach];
-        Vec o[kBatch][kRowsEach];
+        float2 ml[kBatch];
+        float4 o[kBatch][kEights][2];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const size_t row = (size_t)parts.slot(cta + min(w0 + k, parts.count - 1)) * kItemRows + r0;
+            const size_t slot = (size_t)parts.slot(cta + min(w0 + k, parts.count - 1));
+            ml[k] = *reinterpret_cast<const float2*>(p.part_ml + (slot * kItemRows + row) * 2);
+            const float4* src = reinterpret_cast<const float4*>(p.part_o + slot * kItemRows * kD + ((size_t)warp * kEights * kItemRows + row) * 8);
 #pragma unroll
-            for (int x = 0; x < kRowsEach; ++x) {
-                ml[k][x] = *reinterpret_cast<const float2*>(p.part_ml + (row + x) * 2);
-                o[k][x] = *reinterpret_cast<const Vec*>(p.part_o + (row + x) * kD + lane * kPer);
+            for (int c = 0; c < kEights; ++c) {
+                o[k][c][0] = src[(size_t)c * kItemRows * 2];
+                o[k][c][1] = src[(size_t)c * kItemRows * 2 + 1];
             }
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             if (w0 + k >= parts.count) break;
+            const float m_new = fmaxf(m, ml[k].x), m_use = m_new == -INFINITY ? 0.0f : m_new;
+            const float f = ex2_approx(m - m_use), g = ex2_approx(ml[k].x - m_use);
+            m = m_new;
+            total = total * f + ml[k].y * g;
 #pragma unroll
-            for (int x = 0; x < kRowsEach; ++x) {
-                const float m_new = fmaxf(m[x], ml[k][x].x), m_use = m_new == -INFINITY ? 0.0f : m_new;
-                const float f = ex2_approx(m[x] - m_use), g = ex2_approx(ml[k][x].x - m_use);
-                const float* y = reinterpret_cast<const float*>(&o[k][x]);
-                m[x] = m_new;
-                total[x] = total[x] * f + ml[k][x].y * g;
+            for (int c = 0; c < kEights; ++c) {
+                const float* y = reinterpret_cast<const float*>(&o[k][c][0]);
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) acc[x][e] = acc[x][e] * f + y[e] * g;
+                for (int e = 0; e < 8; ++e) acc[c][e] = acc[c][e] * f + y[e] * g;
             }
         }
     }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const int flat = item.z * kItemRows + row, i = flat / p.rep, head = item.w * p.rep + flat - i * p.rep;
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)item.y * p.queries + i) * p.H + head) * kD + warp * kEights * 8;
 #pragma unroll
-    for (int x = 0; x < kRowsEach; ++x) {
-        if (r0 + x >= rows) break;
-        const float inv = total[x] == 0.0f ? 0.0f : 1.0f / total[x];
-        const int flat = item.z * kItemRows + r0 + x, i = flat / p.rep, head = item.w * p.rep + flat - i * p.rep;
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (((size_t)item.y * p.queries + i) * p.H + head) * kD + lane * kPer;
-        uint32_t w[kPer / 2];
+    for (int c = 0; c < kEights; ++c) {
+        uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < kPer / 2; ++e) w[e] = pack_bf16(acc[x][2 * e] * inv, acc[x][2 * e + 1] * inv);
+        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(acc[c][2 * e] * inv, acc[c][2 * e + 1] * inv);
         if (p.wide) {
-#pragma unroll
-            for (int e = 0; e < kPer / 2; ++e) reinterpret_cast<uint32_t*>(dst)[e] = w[e];
+            *reinterpret_cast<uint4*>(dst + c * 8) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
 #pragma unroll
-            for (int e = 0; e < kPer / 2; ++e) {
-                dst[2 * e] = __ushort_as_bfloat16((unsigned short)(w[e] & 0xffffu));
-                dst[2 * e + 1] = __ushort_as_bfloat16((unsigned short)(w[e] >> 16));
+            for (int e = 0; e < 4; ++e) {
+                dst[c * 8 + 2 * e] = __ushort_as_bfloat16((unsigned short)(w[e] & 0xffffu));
+                dst[c * 8 + 2 * e + 1] = __ushort_as_bfloat16((unsigned short)(w[e] >> 16));
             }
         }
     }
