@@ -4,8 +4,8 @@
 // 64 channels with its 3 neighbours, and writes two words of 8 codes.  4 D bytes (bf16) are read per token and head and 9/8 D written,
 // but what bounds it is the instructions: about 18 a value, of which minimum, maximum, quotient and clamp are on the half-rate pipe.
 // One head per row group, K and V of it: with two, which fetch the token's row of the rotary tables once, 40 heads x 4 x 4680 tokens took
-// 175 us, with one, and twice the warps on an SM, 157.  Now 152 in a row: 877 MB at 5.8 TB/s, 0.88 of the rate of a copy; 183 where
-// other work has emptied L2 in between.  One token of each stream: 6 us, of which the kernel has about 2.
+// 175 us, with one, and twice the warps on an SM, 157.  Now 151 in a row: 877 MB at 5.8 TB/s, 0.89 of the rate of a copy; 181 where
+// other work has emptied L2 in between.  One token of each stream: 2.8 us.
 //
 // Attention (one query per stream up to a few dozen rows; any number in fp32).  Keys are the M side of the
 // matrix instruction and query rows the N side, so that 8 rows fill it:  S^T = K Q^T, then  O^T = V^T P^T.  Codes go into the
@@ -20,8 +20,8 @@
 // What bounds it over long caches is the instructions of a warp, about 264 per 16 keys and 8 rows (two products, the scores' factors, the
 // exponentials), which wait for one another: issue slots 55 %, tensor pipe 25 %, DRAM 51 % busy.  Over short ones, what a CTA does once:
 // plan, rows of Q, first keys, its four warps' rows put together, and the item's parts (a part more costs about 0.4 us at 16 rows).  us in
-// a row: one query in each of 4 streams of 12 heads over 74880 tokens 103 (518 MB, 5.0 TB/s, 0.77 of a copy's rate); 8 streams of 40
-// heads on 8 over 9360 32; 12 heads over 500 9.7; fp32, 2 heads, 256 rows over 768 14.6.
+// a row: one query in each of 4 streams of 12 heads over 74880 tokens 103 to 107 (518 MB, 5.0 TB/s, 0.77 of a copy's rate); 8 streams of
+// 40 heads on 8 over 9360 32; 12 heads over 500 9.5; fp32, 2 heads, 256 rows over 768 14.7, 12 heads, 700 over 1400 97.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -1133,10 +1133,11 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
     return dtype == ARL2_FP32 ? launch_append<64, float>(a, st) : launch_append<64, __nv_bfloat16>(a, st);
 }
 
-// Rows per key head up to which this file's kernel is the faster one, with tcgen05 or without.  us with it and with tcgen05: 2 x 12
-// heads, 24 rows over 9360 keys 49 and 62; 12 heads, 32 over 600 15.4 and 18.3, 64 over 600 15.9 and 19.6; 2 heads, 32 over 20000 39 and
-// 35; 2 x 12 heads, 48 over 9360 (an earlier state of both) 66 and 59.  At D = 64, 12 heads: 40 rows over 300, 600, 2000 and 9360 keys
-// 15.9, 13.6, 21.7, 32.0 and 15.6, 16.3, 19.3, 31.8; 128 rows 19.7, 19.6, 24.8, 50.5 and 17.4, 18.2, 20.4, 33.5; 1560 over 9360 353 and 95.
+// Rows per key head up to which this file's kernel is the faster one where both can do it.  us with it and with tcgen05: 32 rows of 12
+// heads over 300, 1000, 9360 keys 13.8, 17.0, 32.6 and 16.0, 17.1, 37.0, of 2 x 12 15.1, 18.3, 44 and 17.5, 19.8, 59, of 2 heads 13.8, 15.4,
+// 29.0 and 14.0, 15.0, 26.1; 48 rows of 8 x 8 17, 34, 122 and 22, 27, 128 (now 119); 64 rows of 2 x 12 15.6, 20.7, 66 and 17.7, 20.8, 60 (now
+// 52).  At D = 64, 12 heads: 32 rows 11.3, 14.8, 26.4 and 12.7, 14.2, 28.4, 64 rows 12.1, 15.1, 31.8 and 12.8, 14.4, 28.7; 1560 over 9360 353
+// and 88.
 constexpr int kFewRows = 32;
 
 int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st)

@@ -22,9 +22,10 @@
 // What bounds it: of a key tile's 3800 clk, the tensor pipe works 2048 (D = 128), the special-function units 1536; the rest is a
 // group's own chain - scores, maximum, exponentials, P V, the next scores - of which the other group hides only a part.  Two threads per
 // row (registers spilled: 141 us for 113), scores of 64 keys at a time, two sets of them (131), and issuers that do not take turns (131)
-// were slower.  12 heads, D = 128, us in a row: 1560 rows over 9360 keys 111, of which the unpacking has 17 (26 MB read, 67 MB written)
-// and the joining 8 (28 MB of partial rows), 810 TFLOP/s in all, 0.49 of a large matrix product's rate; 4680 over 18720 485 alone
-// (1110 TFLOP/s, 0.67), 528 under the power limit.  At D = 64 1560 over 9360 take 90.
+// were slower.  12 heads, D = 128, us in a row: 1560 rows over 9360 keys 110, of which the unpacking has 16 (26 MB read, 67 MB written)
+// and the joining 8 (28 MB of partial rows), 815 TFLOP/s in all, 0.50 of a large matrix product's rate; 4680 over 18720 482 alone
+// (1115 TFLOP/s, 0.68), 525 under the power limit; 4 streams of 701 rows over 1399 keys, causal, 63 (14, 41, 8).  At D = 64 1560 over
+// 9360 take 88.
 #include "cache_common.cuh"
 #include "tc_common.cuh"
 
@@ -1013,9 +1014,11 @@ int launch_tc(CacheAttendArgs a, int num_sms, cudaStream_t st)
     const long long most = items * tiles;
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;
     if (grid > most) grid = most;
-    // Operands are made ahead wherever there is room for them.  us with them made ahead and on the way: 12 heads, 64 rows over 600 keys 20
-    // and 34, 256 over 9360 53 and 57, 1536 over 9360 117 and 137; 2 x 12 heads, 64 over 9360 65 and 59.
-    const bool ahead = a.unpack_pairs > 0 && a.s_B <= kUnpackStreams;
+    // Operands are made ahead where there is room for them and several items read them, or where there are so few that the launch is
+    // what counts.  us with them made ahead and on the way: 12 heads, 1536 rows over 9360 keys 111 and 124, 512 rows 58 and 62; 2 x 12
+    // heads, 256 rows over 9360 75 and 62; 64 rows of 12 heads over 300, 1000, 4000, 9360 16.4, 17.6, 27.2, 38.0 and 18.4, 19.6, 26.5, 37.4,
+    // of 2 x 12 17.5, 20.8, 33.7, 60.4 and 18.5, 21.2, 33.5, 52.1, of 8 x 8 22.3, 27.8, 68.0, 129 and 20.5, 25.8, 58.2, 119.
+    const bool ahead = a.unpack_pairs > 0 && a.s_B <= kUnpackStreams && (a.row_blocks > 1 || most <= 2LL * num_sms);
     const long long pairs = (long long)a.s_B * a.c.kv_heads * (tiles + a.row_blocks);
     // where the workspace may be too small for the lengths, which only the device knows, both kernels go out, and one returns at once
     a.either = ahead && pairs > a.unpack_pairs;

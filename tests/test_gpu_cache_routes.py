@@ -79,6 +79,44 @@ def test_operands_on_the_way_where_the_workspace_is_too_small():
     assert (short.float() - torch.cat(parts, 1).float()).abs().max() <= 2.0 ** -6 * short.float().abs().max()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_operands_of_several_items_where_the_workspace_is_too_small(D):
+    """Rows of several items over more cached tokens than there is room for operand tiles: both kernels go out, and the converting one
+    does the work; over fewer tokens the other one."""
+    B, H, T, page, n = 1, 2, 300, 256, 4096 * 128 // 2 + 3000
+    layer = arl2.Layer(B, H, T, D, "bf16", device=DEV)
+    width = -(-n // page)
+    cache = arl2.Cache(layer, width, width, page_tokens=page)
+    cache.page_table.copy_(torch.randperm(width, device=DEV).to(torch.int32).view(1, width))
+    k, v = (torch.randn(1, 8192, H, D, device=DEV).to(torch.bfloat16) for _ in range(2))
+    for first in range(0, n, 8192):
+        m = min(8192, n - first)
+        cache.append(k[:, :m] * 1.5, v[:, :m], start_of((first,)))
+    q, _ = draw((B, T, H, D), "bf16", 21)
+    for tokens in (n, 500):
+        before = layer.launch_count
+        out = cache.attend(q, start_of((tokens,)))
+        assert layer.launch_count - before == 4
+        parts = [cache.attend(q[:, i:i + 20].contiguous(), start_of((tokens,)), q_start=start_of((tokens - T + i,))) for i in range(0, T, 20)]
+        layer.sync_status()
+        far = (out.float() - torch.cat(parts, 1).float()).abs().max() / out.float().abs().max()
+        assert far <= 2.0 ** -6, (tokens, far)
+
+
+@pytest.mark.parametrize("B,H,T,n", [(3, 12, 40, 1500), (1, 6, 130, 9000)])
+def test_one_item_per_head_converts_on_the_way(B, H, T, n):
+    """More than two key tiles per SM for one item per key head: no operands are made ahead."""
+    layer, cache, pool, cos, sin = make(B, H, H, 128, "bf16", 64, n, rope_rows=n, L=T)
+    lengths = [n - 37 * b for b in range(B)]
+    fill_streams(pool, lengths)
+    q, qf = draw((B, T, H, 128), "bf16", 63)
+    before = layer.launch_count
+    out = cache.attend(q, start_of(lengths))
+    assert layer.launch_count - before == 2
+    layer.sync_status()
+    check(out, *reference(qf, pool, lengths, False, cos, sin), "bf16", n)
+
+
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("B,T,lengths,route", [(2, 150, (517, 260), 3), (1, 300, (1000,), 3), (65, 20, None, 2), (3, 40, (0, 129, 1), 3)])
 def test_many_rows_of_64_channels(B, T, lengths, route, causal):
