@@ -79,6 +79,17 @@ def test_operands_on_the_way_where_the_workspace_is_too_small():
     assert (short.float() - torch.cat(parts, 1).float()).abs().max() <= 2.0 ** -6 * short.float().abs().max()
 
 
+@pytest.mark.parametrize("H,kv,page,T,lengths,seed", [(2, 2, 64, 7, (11,), 292), (4, 2, 256, 16, (58, 44), 256), (6, 3, 16, 16, (19, 1, 65, 65, 25), 350)])
+def test_one_of_few_keys_has_nearly_all_the_weight(H, kv, page, T, lengths, seed):
+    """... and a value near zero, as minimum + 8 steps: what the other keys add is not to be cut off beside the two parts."""
+    layer, cache, pool, _, _ = make(len(lengths), H, kv, 128, "bf16", page, max(lengths))
+    fill_streams(pool, lengths, seed=seed)
+    q, qf = draw((len(lengths), T, H, 128), "bf16", seed)
+    out = cache.attend(q, start_of(lengths))
+    layer.sync_status()
+    check(out, *reference(qf, pool, lengths, False, None, None), "bf16", max(lengths))
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_operands_of_several_items_where_the_workspace_is_too_small(D):
     """Rows of several items over more cached tokens than there is room for operand tiles: both kernels go out, and the converting one
