@@ -339,7 +339,7 @@ int arl2_cache_append(arl2_cache* cache, const void* d_k, int64_t k_batch_stride
  * rotary tables counts as the last there is, a page that the pool does not have reads as zeros, and arl2_sync_status reports
  * ARL2_ERR_RANGE.  bf16 I/O: fp16 operands on tensor cores, fp32 softmax and sums; fp32 I/O: each
  * fp32 operand as two fp16 numbers (the codes are exact), to fp32's accuracy.  Bitwise reproducible.
- * More than 32 rows (queries * H / kv_heads) with bf16 I/O go to tcgen05 kernels, three or four launches; all else, and every call
+ * More than 32 rows (queries * H / kv_heads) with bf16 I/O go to tcgen05 kernels, two to four launches; all else, and every call
  * of an ARL2_FLAG_FORCE_SIMT context, to one kernel of warp-level matrix instructions.  `queries` need not be L.
  */
 #define ARL2_CACHE_CAUSAL 1u

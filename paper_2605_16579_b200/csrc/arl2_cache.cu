@@ -5,7 +5,7 @@
 // but what bounds it is the instructions: about 18 a value, of which minimum, maximum, quotient and clamp are on the half-rate pipe.
 // One head per row group, K and V of it: with two, which fetch the token's row of the rotary tables once, 40 heads x 4 x 4680 tokens took
 // 175 us, with one, and twice the warps on an SM, 157.  Now 151 in a row: 877 MB at 5.8 TB/s, 0.89 of the rate of a copy; 181 where
-// other work has emptied L2 in between.  One token of each stream: 2.8 us.
+// other sets of inputs have been in L2 in between.  One token of each stream: 2.8 us.
 //
 // Attention (one query per stream up to a few dozen rows; any number in fp32).  Keys are the M side of the
 // matrix instruction and query rows the N side, so that 8 rows fill it:  S^T = K Q^T, then  O^T = V^T P^T.  Codes go into the
@@ -845,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                         }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const uint32_t p2 = kSplit ? 0u : pack_half(pr[2 * e], pr[2 * e + 1]);
+                            [[maybe_unused]] const uint32_t p2 = kSplit ? 0u : pack_half(pr[2 * e], pr[2 * e + 1]);
                             // a NaN or an infinity that a row does not see is not to reach it as 0 * NaN
                             const uint32_t keep = (hidden[2 * e] ? 0u : 0xffffu) | (hidden[2 * e + 1] ? 0u : 0xffff0000u);
 #pragma unroll
