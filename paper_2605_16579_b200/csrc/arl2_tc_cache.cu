@@ -746,18 +746,22 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
         auto wait_full = [&](uint32_t entry, int site) {
             return wait_bar_warp(bars + 8 * (kBarFull0 + entry % kStages), (entry / kStages) & 1, ab, site);
         };
-        // both issuers release every entry; one that works alone does it for the other, too
-        auto release = [&](uint32_t entry, bool alone) {
-            mma_commit_if(lead, bars + 8 * (kBarEmpty0 + entry % kStages));
-            if (alone) mma_commit_if(lead, bars + 8 * (kBarEmpty0 + entry % kStages));
-        };
+        // both issuers release every entry, when their MMAs have read it
+        auto release = [&](uint32_t entry) { mma_commit_if(lead, bars + 8 * (kBarEmpty0 + entry % kStages)); };
         uint32_t cons = 0, p_cnt = 0, q_cnt = 0, turn = 0;
         bool ok = true;
         Segment seg;
         while (ok && walk.next(p, seg)) {
             const int n = seg.c1 - seg.c0;
             const bool alone = seg.rows <= kTile;
-            if (alone && t == 1) { cons += 2 * n; continue; }
+            if (alone && t == 1) {
+                // (entry by entry, too: the ring's phases have one bit, and who skipped more than the ring would take an old one for its own)
+                for (int e = 0; e < 2 * n && ok; ++e, ++cons) {
+                    ok = wait_full(cons, 168);
+                    if (ok) mbar_arrive_if(lead, bars + 8 * (kBarEmpty0 + cons % kStages));
+                }
+                continue;
+            }
             ok = wait_bar_warp(bars + 8 * (kBarQ0 + t), q_cnt & 1, ab, 161);
             ++q_cnt;
             if (ok) ok = wait_full(cons, 162);
@@ -765,7 +769,7 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
             tc_fence_after();
             issue_qk(slot_addr(cons));
             mma_commit_if(lead, bar_s);
-            release(cons, alone);
+            release(cons);
             if (kUnpacked && n == 1) mma_commit_if(lead, bars + 8 * (kBarQFree0 + t));
             for (int j = 0; j < n; ++j) {
                 const uint32_t e_v = cons + 2 * j + 1, e_k = e_v + 1;
@@ -793,8 +797,8 @@ __global__ void __launch_bounds__(Roles<kUnpacked>::kThreads, 1) tc_cache_attend
                     mma_commit_if(lead, bars + 8 * (kBarO0 + t));
                 }
                 if (!alone) mbar_arrive_if(lead, bars + 8 * (kBarTurn0 + (t ^ 1)));
-                release(e_v, alone);
-                if (!last) release(e_k, alone);
+                release(e_v);
+                if (!last) release(e_k);
             }
             cons += 2 * n;
         }

@@ -79,6 +79,25 @@ def test_operands_on_the_way_where_the_workspace_is_too_small():
     assert (short.float() - torch.cat(parts, 1).float()).abs().max() <= 2.0 ** -6 * short.float().abs().max()
 
 
+@pytest.mark.parametrize("B,H,kv,T,n", [(70, 24, 3, 33, 300), (66, 2, 1, 130, 700), (12, 12, 12, 264, 900)])
+def test_items_of_both_tiles_after_items_of_one(B, H, kv, T, n):
+    """Items whose second tile of rows is empty among others: whoever has nothing to do in one keeps step with the ring."""
+    layer, cache, pool, _, _ = make(B, H, kv, 128, "bf16", 64, n, L=T)
+    lengths = [n] * B
+    fill_streams(pool, lengths[:1])
+    pool.table[1:] = pool.table[:1]          # all streams over the same pages
+    q, qf = draw((1, T, H, 128), "bf16", 64)
+    q = q.expand(B, T, H, 128).contiguous()
+    outs = [cache.attend(q, start_of(lengths)) for _ in range(3)]
+    layer.sync_status()
+    one = Pool.__new__(Pool)
+    one.__dict__ = dict(pool.__dict__, B=1, order=pool.order[:1])
+    ref = reference(qf, one, lengths[:1], False, None, None)
+    for b in (0, B // 2, B - 1):
+        check(outs[0][b:b + 1], *ref, "bf16", n)
+    assert all(torch.equal(x, outs[0]) for x in outs)
+
+
 @pytest.mark.parametrize("H,kv,page,T,lengths,seed", [(2, 2, 64, 7, (11,), 292), (4, 2, 256, 16, (58, 44), 256), (6, 3, 16, 16, (19, 1, 65, 65, 25), 350)])
 def test_one_of_few_keys_has_nearly_all_the_weight(H, kv, page, T, lengths, seed):
     """... and a value near zero, as minimum + 8 steps: what the other keys add is not to be cut off beside the two parts."""
