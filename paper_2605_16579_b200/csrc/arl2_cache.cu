@@ -147,9 +147,9 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
 
 // 16 of a group's 64 channels -> two words of codes and the group's (minimum, step); x becomes what these stand for.  Every
 // operation is a single fp32 one, so that the codes are those of the formula whoever evaluates it.
-// (Magnitudes above the limit need no clamp of their own: their codes are the ends' anyway.  Rounding to whole numbers is an addition
-// of 1.5 * 2^23, and codes come together as digits of a whole number in fp32: conversions and rint have a quarter of the rate.
-// The quotients are clamped only where the roundings of minimum and step let the ends' fall outside.)
+// (Rounding to whole numbers is an addition of 1.5 * 2^23, and codes come together as digits of a whole number in fp32: conversions and
+// rint have a quarter of the rate.  The quotients are clamped only where a group of the warp has one outside of the codes, by the
+// roundings of minimum and step, or beyond the limit: as digits they would change their neighbours.)
 __device__ __forceinline__ void hold_values(float (&x)[kLaneValues], uint32_t (&codes)[2], uint32_t& params)
 {
     float lo = min_nan(x[0], x[1]), hi = max_nan(x[0], x[1]);
@@ -163,14 +163,14 @@ __device__ __forceinline__ void hold_values(float (&x)[kLaneValues], uint32_t (&
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
+    const float first = lo, last = hi;
     lo = max_nan(min_nan(lo, kHoldLimit), -kHoldLimit);
-    const float end = hi;
     hi = max_nan(min_nan(hi, kHoldLimit), -kHoldLimit);
     const __half step_h = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), lo_h = __float2half_rn(lo);
     const float step = __half2float(step_h), base = __half2float(lo_h);
     const float inverse = step > 0.0f ? __frcp_rn(step) : 0.0f;
-    // the ends' quotients, between which the others' are (of an infinity or a NaN among the values: not so)
-    const bool inside = __fmul_rn(__fsub_rn(lo, base), inverse) >= -0.5f && __fmul_rn(__fsub_rn(end, base), inverse) < 15.5f && end >= lo;
+    // the quotients of the least and the greatest value as they are, not as they are held: the others' are between them (a NaN: not so)
+    const bool inside = __fmul_rn(__fsub_rn(first, base), inverse) >= -0.5f && __fmul_rn(__fsub_rn(last, base), inverse) < 15.5f;
     const bool clamp = !__all_sync(0xffffffffu, inside);
     const uint64_t base2 = pair(-base, -base), inverse2 = pair(inverse, inverse);
     constexpr float kMagic = 12582912.0f;
