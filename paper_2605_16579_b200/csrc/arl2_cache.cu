@@ -804,9 +804,18 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                     }
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    const uint32_t most = __reduce_max_sync(0xffffffffu, v_most[g]) >> 16;
+                    // the largest finite step (in a group that is not finite, which some rows may not see, there is nothing to keep in range)
+                    uint32_t largest = 0;
+#pragma unroll
+                    for (int u = 0; u < kSteps; ++u)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t step = vp[u][e][g] >> 16;
+                            if (step < 0x7c00u) largest = max(largest, step);
+                        }
+                    const uint32_t most = __reduce_max_sync(0xffffffffu, largest);
                     float shrink = 1.0f;
-                    if (most > (v_limit[g] >> 16) && most < 0x7c00u) {
+                    if (most > (v_limit[g] >> 16)) {
                         // kPlace over the next power of two above the step, as far as fp16 goes
                         const float step = __half2float(__ushort_as_half((unsigned short)most));
                         const float above = __uint_as_float(__float_as_uint(2.0f * step) & 0x7f800000u);

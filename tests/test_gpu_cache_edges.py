@@ -42,3 +42,29 @@ def test_append_of_one_outlier(dtype, D):
         pages.append(pool.guard.t.clone())
     assert torch.equal(pages[0], pages[1])
     assert np.isfinite(values).all()
+
+
+# ---------------------------------------------------------------------------------------------- attention
+def fill_streams(pool, k, v):
+    pool.fill(k.astype(np.float32), v.astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype,D,H,kv,queries", [("bf16", 128, 2, 2, 1), ("bf16", 64, 2, 2, 1), ("bf16", 128, 6, 2, 4), ("bf16", 64, 2, 2, 12),
+                                                  ("fp32", 128, 2, 2, 1), ("fp32", 64, 4, 2, 6), ("bf16", 128, 2, 2, 70)])
+@pytest.mark.parametrize("first", [3, 11, 150])
+def test_values_not_finite_beside_wide_ones(dtype, D, H, kv, queries, first):
+    """Tokens whose values are NaN, hidden from some rows by causality, in the same tile of keys as visible values of a wide range."""
+    n = first + queries + 9
+    layer, cache, pool, _, _ = make(1, H, kv, D, dtype, 16, n)
+    rng = np.random.default_rng(first)
+    k, v = rng.standard_normal((1, n, kv, D)), 200.0 * rng.standard_normal((1, n, kv, D))
+    v[0, first + 1:first + 3] = np.nan             # seen by the third and later rows (the second sees one of them)
+    fill_streams(pool, k, v)
+    q, qf = draw((1, queries, H, D), dtype, 41)
+    out = cache.attend(q, start_of((n,)), q_start=start_of((first,)), causal=True)
+    layer.sync_status()
+    ref, weight_v, reach = attend64(qf, pool, (n,), (first,), True)
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got[0, 0]).all() and np.isnan(got[0, 1:]).all()
+    room = tolerance(ref, weight_v, reach, dtype, n)
+    assert (np.abs(got - ref)[0, 0] <= room[0, 0]).all()
