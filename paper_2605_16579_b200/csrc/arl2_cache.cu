@@ -750,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int key = key0 + u * kKeys + gid + 8 * e;
-                        if (key >= have) {                   // nothing is there: whatever the memory holds stays out of the sums
+                        if (key >= seen) {      // nothing is there, or no row sees it: it stays out of the sums, and out of p * step's scale
 #pragma unroll
                             for (int g = 0; g < G; ++g) vp[u][e][g] = 0;
                         }

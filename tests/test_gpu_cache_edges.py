@@ -68,3 +68,19 @@ def test_values_not_finite_beside_wide_ones(dtype, D, H, kv, queries, first):
     assert np.isfinite(got[0, 0]).all() and np.isnan(got[0, 1:]).all()
     room = tolerance(ref, weight_v, reach, dtype, n)
     assert (np.abs(got - ref)[0, 0] <= room[0, 0]).all()
+
+
+@pytest.mark.parametrize("dtype,D,H,kv", [("bf16", 128, 2, 2), ("bf16", 64, 10, 2), ("fp32", 128, 2, 2), ("fp32", 64, 4, 1)])
+@pytest.mark.parametrize("first", [3, 11, 300])
+def test_wide_values_that_no_row_sees(dtype, D, H, kv, first):
+    """A token's queries before later tokens whose values have a range 2^29 times as wide: nothing of the visible values' accuracy is lost."""
+    n = first + 20
+    layer, cache, pool, _, _ = make(1, H, kv, D, dtype, 16, n)
+    rng = np.random.default_rng(first)
+    k, v = rng.standard_normal((1, n, kv, D)), 1e-4 * rng.standard_normal((1, n, kv, D))
+    v[0, first + 1:] = 6e4 * np.sign(v[0, first + 1:])
+    fill_streams(pool, k, v)
+    q, qf = draw((1, 1, H, D), dtype, 41)
+    out = cache.attend(q, start_of((n,)), q_start=start_of((first,)), causal=True)
+    layer.sync_status()
+    check(out, *attend64(qf, pool, (n,), (first,), True), dtype, n)
