@@ -308,6 +308,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             mbar_arrive(bars + 8 * (kBarQ0 + t));
         }
 
+        if (sees <= 0) c2 = 1.0f;      // (the factor of a row that is not finite is NaN; a row that sees no key is zero all the same)
         const uint64_t c2x2 = pack2(c2, c2);
         float m_ref = -INFINITY;
         uint64_t l2 = pack2(0.0f, 0.0f);

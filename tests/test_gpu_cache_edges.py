@@ -84,3 +84,37 @@ def test_wide_values_that_no_row_sees(dtype, D, H, kv, first):
     out = cache.attend(q, start_of((n,)), q_start=start_of((first,)), causal=True)
     layer.sync_status()
     check(out, *attend64(qf, pool, (n,), (first,), True), dtype, n)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,T,n,route", [(1, 3, 290, 1), (1, 300, 290, 3), (2, 40, 500, 3), (65, 40, 290, 2), (1, 260, 40000, 3)])
+def test_not_finite_queries_that_see_no_key(B, T, n, route, D):
+    """Rows of infinities and NaN before the first key, and in streams without keys, are zero as all rows that see none are; the others
+    are as without them.  Items of one CTA and of several, operands made ahead and on the way.  route: the launches of a call."""
+    layer, cache, pool, _, _ = make(B, 2, 2, D, "bf16", 64, n, L=T)
+    rng = np.random.default_rng(T)
+    k, v = (rng.standard_normal((B, min(n, 300), 2, D)) for _ in range(2))
+    fill_streams(pool, k, v)
+    if n > 300:
+        pool.table[:] = pool.table[:, :4].repeat(1, -(-pool.width // 4))[:, :pool.width]      # the same four pages over and over
+    hidden = 2                                      # rows before the first key
+    lengths, first = [n] * B, [-hidden] * B
+    if B > 1:
+        lengths[B - 1] = 0
+    if n > T:
+        first = [f + n - T for f in first]
+        first[0] = -hidden
+    q, _ = draw((B, T, 2, D), "bf16", 61)
+    call = lambda x: cache.attend(x, start_of(lengths), q_start=start_of(first), causal=True)  # noqa: E731
+    before = layer.launch_count
+    plain = call(q)
+    assert layer.launch_count - before == route
+    bad = q.clone()
+    bad[0, 0, :, 3], bad[0, 1, 0, D - 1] = float("nan"), float("-inf")
+    if B > 1:
+        bad[B - 1] = float("nan")
+        bad[B - 1, 5, 1] = float("inf")
+    out = call(bad)
+    layer.sync_status()
+    assert (plain[0, :hidden] == 0).all() and torch.isfinite(plain).all()
+    assert torch.equal(out, plain)
