@@ -464,9 +464,11 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
     using C = RowsConfig<D, kTiles, kSplit>;
     using T = Tile<D>;
     constexpr int G = C::G, kRows = C::kRows, kParts = C::kParts, kSteps = C::kSteps, kChunk = C::kChunk;
-    // The place of p * step in fp16's range: at most 2^14.  The reference maximum follows every larger score, so that the largest p is
-    // exactly 1: its p * step then has no rounding against its p * minimum, which it nearly cancels with where the value is small.
-    constexpr float kPlace = 16384.0f;
+    // The weights p are 2^7 for the reference maximum, which follows every larger score: the lowest fp16 number is 2^-31 of it (with p = 1
+    // weights below 2^-25 were lost, however many there were, while the row's sum had them).  The largest p is 2^7 exactly: its p * step
+    // then has no rounding against its p * minimum, which it nearly cancels with where the value is small.
+    // The place of p * step in fp16's range: at most 2^14.
+    constexpr float kLift = 7.0f, kPlace = 16384.0f / 128.0f, kMostMul = 32768.0f / 128.0f;
     extern __shared__ __align__(128) uint8_t smem[];
     __half* q_frag = reinterpret_cast<__half*>(smem);          // [part][tile][group][k-step][lane][4]
     float* merge_o = reinterpret_cast<float*>(smem);           // [warp][row][kLd]
@@ -642,15 +644,15 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
         if (p.causal) fewest = min(have, max(0, (int)max(-1LL, min((long long)have, (long long)first + (rb * kRows) / p.rep)) + 1));   // the first row's
 
         float o[G][4][kTiles][4];     // [group][channel tile][row tile]
-        // reference maximum: in the scores' own units, and times the row's factor
-        float top[kTiles][2], m_ref[kTiles][2], l[kTiles][2], lows[kTiles][2][G];
+        // reference maximum, in the scores' own units; the same, and zero where no key was seen
+        float top[kTiles][2], base[kTiles][2], l[kTiles][2], lows[kTiles][2][G];
         // what p * step is multiplied by per group, as a pair of fp16 (bf16 I/O), and the parameters above which it has to shrink
         float v_mul[G];
         uint32_t v_mul2[G], v_limit[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            v_mul[g] = 32768.0f;
-            v_mul2[g] = 0x78007800u;
+            v_mul[g] = kMostMul;
+            v_mul2[g] = 0x5c005c00u;
             v_limit[g] = 0x0000ffffu;      // a step of zero; then the power of two below which steps are
 #pragma unroll
             for (int m = 0; m < 4; ++m)
@@ -664,7 +666,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 top[t][e] = -INFINITY;
-                m_ref[t][e] = l[t][e] = 0.0f;
+                base[t][e] = l[t][e] = 0.0f;
 #pragma unroll
                 for (int g = 0; g < G; ++g) lows[t][e][g] = 0.0f;
             }
@@ -793,10 +795,8 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                         for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                         down[t][f] = 1.0f;
                         if (mx > top[t][f]) {
-                            const float m_new = __fmul_rn(mx, scale[t][f]);
-                            down[t][f] = top[t][f] == -INFINITY ? 0.0f : exp2_fast(m_ref[t][f] - m_new);
-                            top[t][f] = mx;
-                            m_ref[t][f] = m_new;
+                            down[t][f] = top[t][f] == -INFINITY ? 0.0f : exp2_fast(__fmul_rn(__fsub_rn(top[t][f], mx), scale[t][f]));
+                            top[t][f] = base[t][f] = mx;
                         }
                         l[t][f] *= down[t][f];
 #pragma unroll
@@ -819,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                         // kPlace over the next power of two above the step, as far as fp16 goes
                         const float step = __half2float(__ushort_as_half((unsigned short)most));
                         const float above = __uint_as_float(__float_as_uint(2.0f * step) & 0x7f800000u);
-                        const float mul = fminf(kPlace / above, 32768.0f);
+                        const float mul = fminf(kPlace / above, kMostMul);
                         v_limit[g] = ((uint32_t)__half_as_ushort(__float2half_rn(above)) << 16) | 0xffffu;
                         shrink = mul / v_mul[g];
                         v_mul[g] = mul;
@@ -846,8 +846,8 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
                         bool hidden[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            // (with a fused product the largest would not be 1)
-                            pr[e] = exp2_fast(__fsub_rn(__fmul_rn(x[u][t][e], scale[t][e & 1]), m_ref[t][e & 1]));
+                            // (in this order the largest score's exponent is exactly kLift)
+                            pr[e] = exp2_fast(__fmaf_rn(__fsub_rn(x[u][t][e], base[t][e & 1]), scale[t][e & 1], kLift));
                             hidden[e] = kMasked && x[u][t][e] == -INFINITY;
                             if (kMasked && hidden[e]) pr[e] = 0.0f;          // (its factor may be NaN)
                             l[t][e & 1] += pr[e];
@@ -958,7 +958,7 @@ __global__ void __launch_bounds__(kThreads, RowsConfig<D, kTiles, sizeof(IO) == 
 #pragma unroll
                     for (int f = 0; f < 2; ++f) {
                         const int r = 8 * t + 2 * tig + f;
-                        merge_ml[(warp * kRows + r) * 2] = top[t][f] == -INFINITY ? -INFINITY : m_ref[t][f];
+                        merge_ml[(warp * kRows + r) * 2] = top[t][f] == -INFINITY ? -INFINITY : __fmul_rn(top[t][f], scale[t][f]);
                         merge_ml[(warp * kRows + r) * 2 + 1] = l[t][f];
                     }
             }

@@ -49,7 +49,10 @@ struct Roles<false> {
     static constexpr int kRegsSoftmax = 192, kRegsHold = 88, kRegsOther = 40;
     static_assert(256 * kRegsSoftmax + 128 * kRegsHold + 128 * kRegsOther <= kThreads * 128, "register pool");
 };
-constexpr float kRescaleThreshold = 8.0f;   // log2 units of slack before O is rescaled: p <= 2^8
+constexpr float kRescaleThreshold = 8.0f;   // log2 units of slack before O is rescaled
+// Weights are 2^7 for the reference maximum, at most 2^15: the lowest fp16 number is then 2^-31 of it.  (With 1 for the maximum a weight
+// below 2^-25 of it was lost, however many there were, while the row's sum had them.)
+constexpr float kLift = 7.0f;
 
 constexpr int kSpecials = 16;               // key tiles whose marks are kept (more than are ever under way)
 constexpr int kMarkWords = 9;               // whether a value is not finite; the keys of those, per group [2][4]
@@ -250,9 +253,9 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
     return own;
 }
 
-// 2^x of two x <= 8 without the special-function units: 2^n * y(f), n the whole number nearest to x, f = x - n in [-1/2, 1/2] and y the
+// 2^x of two x <= 15 without the special-function units: 2^n * y(f), n the whole number nearest to x, f = x - n in [-1/2, 1/2] and y the
 // cubic of least relative error there, 7.5e-5 (the probability's rounding to fp16: up to 4.9e-4).  Below 2^-125 it stays there, where
-// an exponential would go to zero: nothing next to a sum that has a term of at least 2^-8.  A NaN stays one.
+// an exponential would go to zero: nothing next to a sum that has a term of 2^7.  A NaN stays one.
 // One pair of four goes this way.  us for 12 heads, 1560 rows over 9360 keys, D = 128 and 64, and 4680 over 18720, single calls: none 129,
 // 105, 518; one of eight no better than half of it; one of four 125, 103, 491; one of two 2 to 3 % slower than none.
 constexpr int kByFmaEvery = 4;
@@ -386,7 +389,7 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
                     }
                 }
             }
-            const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;     // (no key seen so far)
+            const float m_use = m_ref == -INFINITY ? 0.0f : m_ref - kLift;     // (no key seen so far)
             const uint64_t neg_m2 = pack2(-m_use, -m_use);
             uint64_t pair = 0;
             // P V of the first half of the keys runs beside the exponentials of the second (12 heads, 1560 rows over 9360 keys: 1 %)

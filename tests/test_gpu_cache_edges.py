@@ -118,3 +118,30 @@ def test_not_finite_queries_that_see_no_key(B, T, n, route, D):
     layer.sync_status()
     assert (plain[0, :hidden] == 0).all() and torch.isfinite(plain).all()
     assert torch.equal(out, plain)
+
+
+@pytest.mark.parametrize("D,queries,n", [(128, 1, 120), (128, 1, 4000), (64, 12, 1000), (128, 300, 1000), (64, 50, 700)])
+def test_small_weights_beside_large_ones(D, queries, n):
+    """Weights of about 2^-26 of the largest, which alone bring values: every 16 keys one takes nearly all the weight, and its value is zero.
+
+    Beyond `tolerance`: weights are fp16 numbers of up to 2^7 (few rows) or 2^15 (many) for the largest, so that one is rounded to a
+    multiple of at least 2^-31 of it: off by at most 2^-32.
+    """
+    H = 2
+    layer, cache, pool, _, _ = make(1, H, H, D, "bf16", 64, n, L=queries)
+    rng = np.random.default_rng(n)
+    sign = np.where(rng.random(D) < 0.5, -1.0, 1.0)
+    k, v = 0.3 * rng.standard_normal((1, n, H, D)), 0.5 + rng.random((1, n, H, D))
+    large = np.arange(n) % 16 == 5
+    # <q, k> scale = 26 log 2 for q = sign
+    k[0, large] = sign * 26 * np.log(2.0) / D ** 0.5
+    v[0, large] = 0.0
+    fill_streams(pool, k, v)
+    qf = np.broadcast_to(sign, (1, queries, H, D)).astype(np.float32)
+    q = torch.from_numpy(qf.copy()).to(torch.bfloat16).to(DEV)
+    out = cache.attend(q, start_of((n,)))
+    layer.sync_status()
+    ref, weight_v, reach = attend64(qf, pool, (n,), None, False)
+    values = np.abs(pool.values(0, n)[1]).sum(1)             # [H, D]
+    room = tolerance(ref, weight_v, reach, "bf16", n) + 2.0 ** -32 * values / large.sum()
+    assert (ref > 1e-7).all() and (np.abs(out.double().cpu().numpy() - ref) <= room).all()
