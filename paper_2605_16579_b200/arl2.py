@@ -198,6 +198,9 @@ class Layer:
         self.B, self.H, self.L, self.D = B, H, L, D
         self.flags = flags
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.dtype = torch.bfloat16 if self.cfg.io_dtype == ARL2_BF16 else torch.float32
         self._lib = lib
         self.workspace_bytes = arl2_workspace_bytes(self.cfg)
@@ -207,9 +210,9 @@ class Layer:
             if workspace is None:
                 workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
             self._want(state, (B, H, D, D), torch.float32, "state")
-            if not (workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+            if not (workspace.get_device() == self._index and workspace.dtype == torch.uint8 and workspace.is_contiguous()
                     and workspace.numel() >= self.workspace_bytes):
-                raise Arl2Error(f"workspace: expected >= {self.workspace_bytes} contiguous CUDA bytes")
+                raise Arl2Error(f"workspace: expected >= {self.workspace_bytes} contiguous bytes on {self.device}")
             self.state, self.workspace = state, workspace
             ctx = ctypes.c_void_p()
             _check(lib.arl2_create(ctypes.byref(self.cfg), _ptr(self.state), _ptr(self.workspace),
@@ -438,11 +441,12 @@ class Layer:
             _check(status, name)
 
     def _want(self, t, shape, dtype, what):
-        if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous() and isinstance(t, torch.Tensor):
+        # (get_device: the GPU's number, -1 on the host; a kernel on one GPU is not to be given another's memory)
+        if t.shape == shape and t.dtype is dtype and t.get_device() == self._index and t.is_contiguous() and isinstance(t, torch.Tensor):
             return
-        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()
+        if not (isinstance(t, torch.Tensor) and t.get_device() == self._index and t.is_contiguous()
                 and tuple(t.shape) == tuple(shape) and t.dtype == dtype):
-            raise Arl2Error(f"{what}: expected a contiguous CUDA tensor {tuple(shape)} {dtype}, got "
+            raise Arl2Error(f"{what}: expected a contiguous tensor {tuple(shape)} {dtype} on {self.device}, got "
                             f"{tuple(t.shape)} {t.dtype} on {t.device}")
 
 
@@ -458,7 +462,7 @@ class Cache:
         lib = load()
         self._lib, self._cache = lib, None
         self._append, self._attend = lib.arl2_cache_append, lib.arl2_cache_attend
-        self.layer, self.device, self.dtype = layer, layer.device, layer.dtype
+        self.layer, self.device, self.dtype, self._index = layer, layer.device, layer.dtype, layer._index
         self._B, self._H, self._D = layer.B, layer.H, layer.D
         self.kv_heads = layer.H if kv_heads is None else kv_heads
         rows = 0 if rope_cos is None else int(rope_cos.shape[0])
@@ -534,7 +538,7 @@ class Cache:
     # -- helpers -----------------------------------------------------------------------
     def _rows(self, t, shape, what):
         """The batch and token strides of a tensor whose heads and channels are contiguous."""
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is self.dtype and t.shape == shape:
+        if isinstance(t, torch.Tensor) and t.get_device() == self._index and t.dtype is self.dtype and t.shape == shape:
             token = shape[2] * shape[3]
             if t.is_contiguous():
                 return shape[1] * token, token
@@ -542,7 +546,7 @@ class Cache:
             if st[3] == 1 and (st[2] == shape[3] or shape[2] == 1):
                 # (a dimension of one element may have any stride)
                 return st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else token
-        raise Arl2Error(f"{what}: expected a CUDA tensor {tuple(shape)} {self.dtype} with contiguous heads and channels, got "
+        raise Arl2Error(f"{what}: expected a tensor {tuple(shape)} {self.dtype} on {self.device} with contiguous heads and channels, got "
                         f"{tuple(t.shape)} {t.dtype} with strides {tuple(t.stride())} on {t.device}")
 
     def _empty(self, like, shape):
