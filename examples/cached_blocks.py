@@ -5,7 +5,8 @@
 At every denoising step the block's keys and values are written to their places in the cache (over those of the step before), rotated
 to their positions on the way, and the block's queries read all tokens so far; the clean pass writes them for good.  Then a few
 tokens are generated one by one over the same cache.  Beside it runs the same layer over a contiguous bf16 cache
-(``Layer.teacher_step``): the outputs' distance is what 4 bits cost, and both caches' sizes are printed.
+(``Layer.teacher_step``): the outputs' distance is what 4 bits cost, and both caches' sizes are printed, with the scratch that the 4-bit
+cache's calls need: one for all caches whose calls follow one another, here those of the blocks and of the single tokens.
 """
 import argparse
 import os
@@ -69,7 +70,8 @@ def main(argv=None):
 
     # tokens one by one over the same cache
     single = arl2.Layer(1, H, 1, D, "bf16", device=dev)
-    follow = arl2.Cache(single, cache.cfg.num_pages, width, page_tokens=a.page, rope_cos=cos, rope_sin=sin, pages=cache.pages, page_table=cache.page_table)
+    follow = arl2.Cache(single, cache.cfg.num_pages, width, page_tokens=a.page, rope_cos=cos, rope_sin=sin, pages=cache.pages, page_table=cache.page_table,
+                        workspace=cache.workspace)
     for i in range(8):
         start.fill_(a.blocks * L + i)
         lengths.fill_(a.blocks * L + i + 1)
@@ -79,8 +81,10 @@ def main(argv=None):
     layer.sync_status()
     single.sync_status()
     held, wide = int(width * cache.page_bytes), width * a.page * H * D * 4       # (of the same number of tokens)
-    print(f"cache: {held / 1e6:.1f} MB in 4 bits, {wide / 1e6:.1f} MB in bf16 ({wide / held:.2f} times); outputs at most {worst:.3f} apart")
-    return {"worst": worst, "held": held, "wide": wide, "last": out}
+    scratch = cache.workspace.numel()
+    print(f"cache: {held / 1e6:.1f} MB in 4 bits, {wide / 1e6:.1f} MB in bf16 ({wide / held:.2f} times), and {scratch / 1e6:.1f} MB of scratch for "
+          f"all layers that run one after the other; outputs at most {worst:.3f} apart")
+    return {"worst": worst, "held": held, "wide": wide, "scratch": scratch, "last": out}
 
 
 if __name__ == "__main__":

@@ -296,23 +296,37 @@ typedef struct {
     int32_t rope_rows;
 } arl2_cache_config;
 
-/* Bytes of one page, and of the scratch that a cache needs (256-byte aligned base).  0 for an invalid configuration. */
+/*
+ * Bytes of one page; of the scratch (256-byte aligned base) with which every call of a cache is as fast as it can be; and of the
+ * least scratch that arl2_cache_set_workspace takes.  0 for an invalid configuration.
+ * The scratch is partial rows (39 MB at D = 128, 20 MB at D = 64) and, with bf16 I/O, operand tiles: room for all tokens of all streams
+ * as fp16 and for a block of L queries, as far as 256 MB (D = 128; 128 MB at D = 64) go.  With less of it calls give results of the same
+ * accuracy: without room for its operand tiles a call converts on the way; and the least, 7.5 MB at D = 128, 3.8 at D = 64, is all that
+ * calls of up to 32 rows per key head use, while one of more rows works on 28 SMs.  Nothing in it outlives a call.
+ */
 size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg);
 size_t arl2_cache_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg);
+size_t arl2_cache_least_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg);
 
 /*
  *   d_pages       [num_pages, arl2_cache_page_bytes] bytes, 128-byte aligned; not cleared
  *   d_page_table  [B, max_pages] int32, may be rewritten between calls in stream order
  *   d_rope_cos, d_rope_sin  [rope_rows, D/2] fp32, 16-byte aligned; both NULL where rope_rows is 0
- *   d_workspace   private to this cache until arl2_cache_destroy.  Partial rows, and with bf16 I/O operand tiles: room for all
- *                 tokens of all streams as fp16 and for a block of L queries, as far as 256 MB (D = 128; 128 MB at D = 64) go.
- *                 A call that needs more of it converts on the way and is slower, no more.
- * All stay the caller's.  Launches one small kernel on `stream`.  Calls on one cache are ordered by the caller (one stream, or
- * events between streams): they share the workspace.  Calls may be captured and replayed.
+ *   d_workspace   >= arl2_cache_workspace_bytes; or NULL with workspace_bytes 0: arl2_cache_set_workspace gives it before the first
+ *                 arl2_cache_attend
+ * All stay the caller's.  Launches one small kernel on `stream` (without a workspace none).  Calls on one cache are ordered by the
+ * caller (one stream, or events between streams): they share the workspace.  Calls may be captured and replayed.
  */
 int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d_pages, const int32_t* d_page_table,
                       const float* d_rope_cos, const float* d_rope_sin, void* d_workspace, size_t workspace_bytes,
                       void* stream, arl2_cache** out);
+
+/*
+ * The scratch of a cache's later calls: `bytes` >= arl2_cache_least_workspace_bytes.  Several caches, of one context or of several, may
+ * have the same one, as the layers of a stack that run one after the other do, if the caller orders the calls of all of them as it
+ * orders those of one.  Launches one small kernel on `stream`, after the calls before it.  What was captured before keeps what it had.
+ */
+int arl2_cache_set_workspace(arl2_cache* cache, void* d_workspace, size_t bytes, void* stream);
 
 /*
  * Tokens start[b] .. start[b] + tokens - 1 of each stream, written to their places (over whatever is there, as a block is

@@ -33,7 +33,8 @@ EXPORTS = (
     "arl2_set_profile_events", "arl2_commit_static_scratch", "arl2_commit_delta", "arl2_commit_tokens", "arl2_teacher_step", "arl2_commit_decay_tokens",
     "arl2_step_kernel_name", "arl2_destroy", "arl2_last_error", "arl2_version", "arl2_debug_set_wait_limit", "arl2_debug_set_walk_wait_limit", "arl2_clean_pass", "arl2_denoise_step_token_level",
     "arl2_projection_workspace_bytes", "arl2_set_projections", "arl2_project_in", "arl2_project_out",
-    "arl2_cache_page_bytes", "arl2_cache_workspace_bytes", "arl2_cache_create", "arl2_cache_append", "arl2_cache_attend", "arl2_cache_destroy",
+    "arl2_cache_page_bytes", "arl2_cache_workspace_bytes", "arl2_cache_least_workspace_bytes", "arl2_cache_create", "arl2_cache_set_workspace",
+    "arl2_cache_append", "arl2_cache_attend", "arl2_cache_destroy",
 )
 
 
@@ -129,6 +130,10 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.arl2_cache_page_bytes.argtypes = [cp, ccp]
     lib.arl2_cache_workspace_bytes.restype = ctypes.c_size_t
     lib.arl2_cache_workspace_bytes.argtypes = [cp, ccp]
+    lib.arl2_cache_least_workspace_bytes.restype = ctypes.c_size_t
+    lib.arl2_cache_least_workspace_bytes.argtypes = [cp, ccp]
+    lib.arl2_cache_set_workspace.restype = ctypes.c_int
+    lib.arl2_cache_set_workspace.argtypes = [vp, vp, ctypes.c_size_t, vp]
     lib.arl2_cache_create.restype = ctypes.c_int
     lib.arl2_cache_create.argtypes = [vp, ccp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]
     lib.arl2_cache_append.restype = ctypes.c_int
@@ -456,9 +461,14 @@ class Cache:
     ``page_table`` ([B, max_pages] int32) says which pages of the pool hold a stream's tokens, in order; the caller hands them
     out.  ``pages`` (uint8 [num_pages, page_bytes], uncleared) and ``page_table`` (filled with -1) are made here unless they
     are handed in.  Rotary tables: [positions, D/2] fp32, both or neither.  Calls on one cache are for one stream at a time.
+
+    ``workspace``: scratch (uint8, at least ``workspace_range(...)[0]`` bytes) that this cache uses beside others whose calls do not
+    overlap with its own, as in a stack whose layers run one after the other: ``Cache(..., workspace=first.workspace)``.  By default
+    ``workspace_range(...)[1]`` bytes of its own, with which no call waits for room.
     """
 
-    def __init__(self, layer, num_pages, max_pages, kv_heads=None, page_tokens=64, rope_cos=None, rope_sin=None, pages=None, page_table=None):
+    def __init__(self, layer, num_pages, max_pages, kv_heads=None, page_tokens=64, rope_cos=None, rope_sin=None, pages=None, page_table=None,
+                 workspace=None):
         lib = load()
         self._lib, self._cache = lib, None
         self._append, self._attend = lib.arl2_cache_append, lib.arl2_cache_attend
@@ -470,7 +480,6 @@ class Cache:
         self.page_bytes = lib.arl2_cache_page_bytes(ctypes.byref(layer.cfg), ctypes.byref(self.cfg))
         if self.page_bytes == 0:
             raise Arl2Error("arl2_cache_page_bytes: " + lib.arl2_last_error().decode())
-        n = lib.arl2_cache_workspace_bytes(ctypes.byref(layer.cfg), ctypes.byref(self.cfg))
         for t in (rope_cos, rope_sin):
             if t is not None:
                 layer._want(t, (rows, layer.D // 2), torch.float32, "rope table")
@@ -482,11 +491,36 @@ class Cache:
             layer._want(pages, (num_pages, self.page_bytes), torch.uint8, "pages")
             layer._want(page_table, (layer.B, max_pages), torch.int32, "page_table")
             self.pages, self.page_table, self._rope = pages, page_table, (rope_cos, rope_sin)
-            self._workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
             handle = ctypes.c_void_p()
             _check(lib.arl2_cache_create(layer._ctx, ctypes.byref(self.cfg), _ptr(pages), _ptr(page_table), _ptr(rope_cos), _ptr(rope_sin),
-                                         _ptr(self._workspace), n, _stream(), ctypes.byref(handle)), "arl2_cache_create")
-        self._cache = handle
+                                         None, 0, _stream(), ctypes.byref(handle)), "arl2_cache_create")
+            self._cache = handle
+            if workspace is None:
+                n = lib.arl2_cache_workspace_bytes(ctypes.byref(layer.cfg), ctypes.byref(self.cfg))
+                workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self.set_workspace(workspace)
+
+    @staticmethod
+    def workspace_range(layer, num_pages, max_pages, kv_heads=None, page_tokens=64):
+        """Bytes of scratch of such a cache: the least that it works with, and those with which every call is as fast as it can be."""
+        lib = load()
+        cfg = arl2_cache_config(ctypes.sizeof(arl2_cache_config), layer.H if kv_heads is None else kv_heads, page_tokens, num_pages, max_pages, 0)
+        sizes = tuple(f(ctypes.byref(layer.cfg), ctypes.byref(cfg)) for f in (lib.arl2_cache_least_workspace_bytes, lib.arl2_cache_workspace_bytes))
+        if 0 in sizes:
+            raise Arl2Error("arl2_cache_workspace_bytes: " + lib.arl2_last_error().decode())
+        return sizes
+
+    @property
+    def workspace(self):
+        return self._workspace
+
+    def set_workspace(self, workspace):
+        """Scratch of later calls (arl2_cache_set_workspace); what was captured before keeps the scratch that it was captured with."""
+        if not (isinstance(workspace, torch.Tensor) and workspace.get_device() == self._index and workspace.dtype == torch.uint8
+                and workspace.is_contiguous()):
+            raise Arl2Error(f"workspace: expected contiguous uint8 on {self.device}")
+        self._run(self._lib.arl2_cache_set_workspace, workspace.data_ptr(), workspace.numel())
+        self._workspace = workspace
 
     def append(self, k, v, start, held=False):
         """Rows k, v [B, T, kv_heads, D] of tokens start[b] .. start[b] + T - 1 (start: int32 [B], negative: idle stream), keys

@@ -1098,26 +1098,44 @@ bool cache_tensor_cores(const arl2_config& c) { return c.io_dtype == ARL2_BF16 &
 // Scratch of a cache: tickets of the items that several CTAs share, their rows' statistics, their rows
 struct CacheLayout {
     size_t tickets, part_items, part_ml, part_o, marks, q_scale, unpacked, total;
-    int unpack_pairs;
+    int part_rows, unpack_pairs;
 };
-CacheLayout cache_layout(const arl2_config& cfg, const arl2_cache_config& c)
+CacheLayout cache_layout(const arl2_config& cfg, int part_rows, int unpack_pairs)
 {
     CacheLayout l;
-    const int D = cfg.D;
     size_t off = 0;
+    l.part_rows = part_rows;
+    l.unpack_pairs = unpack_pairs;
+    // (tickets first: they are at zero between calls, wherever caches that share a scratch have the rest)
     l.tickets = off; off += align_up((size_t)kCacheCtas * sizeof(uint32_t));
     l.part_items = off; off += align_up((size_t)kCacheTcCtas * sizeof(int4));
-    l.part_ml = off; off += align_up((size_t)kCachePartRows * 2 * sizeof(float));
-    l.part_o = off;  off += align_up((size_t)kCachePartRows * D * sizeof(float));
-    // operand tiles of all the keys that there may be and of a block of queries, or of as many as that is worth
-    const int64_t rows = (int64_t)cfg.L * (cfg.H / c.kv_heads);
-    const int64_t pairs = (((int64_t)c.max_pages * c.page_tokens + 127) / 128 + (rows + 255) / 256) * c.kv_heads * cfg.B;
-    l.unpack_pairs = !cache_tensor_cores(cfg) ? 0 : (int)(pairs < kUnpackMost ? pairs : kUnpackMost);
-    l.marks = off;    off += align_up((size_t)l.unpack_pairs * kUnpackMarks * sizeof(uint32_t));
-    l.q_scale = off;  off += align_up((size_t)l.unpack_pairs * 256 * sizeof(float));
-    l.unpacked = off; off += (size_t)l.unpack_pairs * unpack_pair_bytes(cfg.D);
+    l.part_ml = off; off += align_up((size_t)part_rows * 2 * sizeof(float));
+    l.part_o = off;  off += align_up((size_t)part_rows * cfg.D * sizeof(float));
+    l.marks = off;    off += align_up((size_t)unpack_pairs * kUnpackMarks * sizeof(uint32_t));
+    l.q_scale = off;  off += align_up((size_t)unpack_pairs * 256 * sizeof(float));
+    l.unpacked = off; off += (size_t)unpack_pairs * unpack_pair_bytes(cfg.D);
     l.total = off;
     return l;
+}
+// ... with room for all partial rows, and for operand tiles of all the keys that there may be and of a block of queries, or of as many
+// as that is worth
+CacheLayout full_cache_layout(const arl2_config& cfg, const arl2_cache_config& c)
+{
+    const int64_t rows = (int64_t)cfg.L * (cfg.H / c.kv_heads);
+    const int64_t pairs = (((int64_t)c.max_pages * c.page_tokens + 127) / 128 + (rows + 255) / 256) * c.kv_heads * cfg.B;
+    return cache_layout(cfg, kCachePartRows, !cache_tensor_cores(cfg) ? 0 : (int)(pairs < kUnpackMost ? pairs : kUnpackMost));
+}
+CacheLayout least_cache_layout(const arl2_config& cfg) { return cache_layout(cfg, kCacheLeastPartRows, 0); }
+// ... within `bytes`, at least those of the least: partial rows first, then operand tiles
+CacheLayout cache_layout_within(const arl2_config& cfg, const arl2_cache_config& c, size_t bytes)
+{
+    const CacheLayout full = full_cache_layout(cfg, c);
+    if (full.total <= bytes) return full;
+    const size_t rows = (bytes - full.part_ml) / ((size_t)kCachePartStep * (2 + cfg.D) * sizeof(float)) * kCachePartStep;
+    if (rows < (size_t)kCachePartRows) return cache_layout(cfg, (int)rows, 0);
+    const size_t left = bytes - full.marks, each = (size_t)unpack_pair_bytes(cfg.D) + (kUnpackMarks + 256) * 4;
+    const size_t pairs = left < kAlign ? 0 : (left - kAlign) / each;     // (the marks end anywhere)
+    return cache_layout(cfg, kCachePartRows, pairs < (size_t)full.unpack_pairs ? (int)pairs : full.unpack_pairs);
 }
 
 bool valid_cache_config(const arl2_config* cfg, const arl2_cache_config* c)
@@ -1169,14 +1187,15 @@ struct arl2_cache {
     arl2_ctx* ctx;
     arl2_cache_config cfg;
     CacheView view;
-    float* part_o;
-    float* part_ml;
-    uint32_t* tickets;
-    int4* part_items;
-    uint8_t* unpacked;
-    uint32_t* unpack_marks;
-    float* q_scale;
-    int unpack_pairs;
+    // the scratch; nullptr: none yet
+    float* part_o = nullptr;
+    float* part_ml = nullptr;
+    uint32_t* tickets = nullptr;
+    int4* part_items = nullptr;
+    uint8_t* unpacked = nullptr;
+    uint32_t* unpack_marks = nullptr;
+    float* q_scale = nullptr;
+    int part_rows = 0, unpack_pairs = 0;
 };
 
 size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
@@ -1188,7 +1207,39 @@ size_t arl2_cache_page_bytes(const arl2_config* cfg, const arl2_cache_config* ca
 size_t arl2_cache_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
 {
     if (!valid_cache_config(cfg, cache_cfg)) return 0;
-    return cache_layout(*cfg, *cache_cfg).total;
+    return full_cache_layout(*cfg, *cache_cfg).total;
+}
+
+size_t arl2_cache_least_workspace_bytes(const arl2_config* cfg, const arl2_cache_config* cache_cfg)
+{
+    if (!valid_cache_config(cfg, cache_cfg)) return 0;
+    return least_cache_layout(*cfg).total;
+}
+
+int arl2_cache_set_workspace(arl2_cache* cache, void* d_workspace, size_t bytes, void* stream)
+{
+    if (cache == nullptr) { set_error("cache is NULL"); return ARL2_ERR_INVALID_ARG; }
+    if (d_workspace == nullptr) { set_error("cache_set_workspace: the workspace must not be NULL"); return ARL2_ERR_INVALID_ARG; }
+    const arl2_config& cfg = cache->ctx->cfg;
+    const size_t least = least_cache_layout(cfg).total;
+    if (bytes < least || reinterpret_cast<uintptr_t>(d_workspace) % kAlign != 0) {
+        set_error("cache_set_workspace: the workspace needs %zu bytes at least, 256-byte aligned (got %zu)", least, bytes);
+        return ARL2_ERR_WORKSPACE;
+    }
+    const CacheLayout lay = cache_layout_within(cfg, cache->cfg, bytes);
+    uint8_t* ws = static_cast<uint8_t*>(d_workspace);
+    const int r = account(cache->ctx, fill_zero(ws + lay.tickets, kCacheCtas * sizeof(uint32_t), as_stream(stream)));
+    if (r != ARL2_OK) return r;
+    cache->tickets = reinterpret_cast<uint32_t*>(ws + lay.tickets);
+    cache->part_items = reinterpret_cast<int4*>(ws + lay.part_items);
+    cache->part_ml = reinterpret_cast<float*>(ws + lay.part_ml);
+    cache->part_o = reinterpret_cast<float*>(ws + lay.part_o);
+    cache->unpacked = ws + lay.unpacked;
+    cache->unpack_marks = reinterpret_cast<uint32_t*>(ws + lay.marks);
+    cache->q_scale = reinterpret_cast<float*>(ws + lay.q_scale);
+    cache->part_rows = lay.part_rows;
+    cache->unpack_pairs = lay.unpack_pairs;
+    return ARL2_OK;
 }
 
 int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d_pages, const int32_t* d_page_table,
@@ -1198,8 +1249,9 @@ int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d
     if (out == nullptr) { set_error("out is NULL"); return ARL2_ERR_INVALID_ARG; }
     *out = nullptr;
     if (!check_ctx(ctx) || !valid_cache_config(&ctx->cfg, cache_cfg)) return ARL2_ERR_INVALID_ARG;
-    if (d_pages == nullptr || d_page_table == nullptr || d_workspace == nullptr) {
-        set_error("cache_create: pages, page_table and workspace must not be NULL");
+    const bool later = d_workspace == nullptr && workspace_bytes == 0;
+    if (d_pages == nullptr || d_page_table == nullptr || (d_workspace == nullptr && !later)) {
+        set_error("cache_create: pages, page_table and a workspace of any size must not be NULL");
         return ARL2_ERR_INVALID_ARG;
     }
     if ((d_rope_cos != nullptr) != (cache_cfg->rope_rows > 0) || (d_rope_sin != nullptr) != (cache_cfg->rope_rows > 0)) {
@@ -1211,14 +1263,13 @@ int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d
         set_error("cache_create: pages must be 128-byte, rotary tables 16-byte and the page table 4-byte aligned");
         return ARL2_ERR_INVALID_ARG;
     }
-    const CacheLayout lay = cache_layout(ctx->cfg, *cache_cfg);
-    if (workspace_bytes < lay.total || reinterpret_cast<uintptr_t>(d_workspace) % kAlign != 0) {
-        set_error("cache_create: the workspace needs %zu bytes, 256-byte aligned (got %zu)", lay.total, workspace_bytes);
+    const size_t full = full_cache_layout(ctx->cfg, *cache_cfg).total;
+    if (!later && (workspace_bytes < full || reinterpret_cast<uintptr_t>(d_workspace) % kAlign != 0)) {
+        set_error("cache_create: the workspace needs %zu bytes, 256-byte aligned (got %zu)", full, workspace_bytes);
         return ARL2_ERR_WORKSPACE;
     }
     arl2_cache* c = new (std::nothrow) arl2_cache();
     if (c == nullptr) { set_error("out of host memory"); return ARL2_ERR_INVALID_ARG; }
-    uint8_t* ws = static_cast<uint8_t*>(d_workspace);
     c->ctx = ctx;
     c->cfg = *cache_cfg;
     c->view.pages = static_cast<uint8_t*>(d_pages);
@@ -1233,15 +1284,7 @@ int arl2_cache_create(arl2_ctx* ctx, const arl2_cache_config* cache_cfg, void* d
     c->view.rope_sin = d_rope_sin;
     c->view.rope_rows = cache_cfg->rope_rows;
     c->view.status = reinterpret_cast<uint32_t*>(ctx->ws + ctx->lay.status);
-    c->tickets = reinterpret_cast<uint32_t*>(ws + lay.tickets);
-    c->part_items = reinterpret_cast<int4*>(ws + lay.part_items);
-    c->part_ml = reinterpret_cast<float*>(ws + lay.part_ml);
-    c->part_o = reinterpret_cast<float*>(ws + lay.part_o);
-    c->unpacked = ws + lay.unpacked;
-    c->unpack_marks = reinterpret_cast<uint32_t*>(ws + lay.marks);
-    c->q_scale = reinterpret_cast<float*>(ws + lay.q_scale);
-    c->unpack_pairs = lay.unpack_pairs;
-    const int r = account(ctx, fill_zero(c->tickets, kCacheCtas * sizeof(uint32_t), as_stream(stream)));
+    const int r = later ? ARL2_OK : arl2_cache_set_workspace(c, d_workspace, workspace_bytes, stream);
     if (r != ARL2_OK) { delete c; return r; }
     *out = c;
     return ARL2_OK;
@@ -1287,6 +1330,7 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
     if (cache == nullptr) { set_error("cache is NULL"); return ARL2_ERR_INVALID_ARG; }
     const arl2_config& cfg = cache->ctx->cfg;
     if (!d_q || !d_lengths || !d_out) { set_error("cache_attend: q, lengths and out must not be NULL"); return ARL2_ERR_INVALID_ARG; }
+    if (cache->tickets == nullptr) { set_error("cache_attend: the cache has been given no workspace"); return ARL2_ERR_WORKSPACE; }
     if (d_out == d_q) { set_error("cache_attend: out must not alias q"); return ARL2_ERR_INVALID_ARG; }
     if (queries < 1 || (int64_t)queries * (cfg.H / cache->cfg.kv_heads) > ((int64_t)1 << 30)) {
         set_error("cache_attend: queries must be >= 1, and at most 2^30 rows per key head (got %d)", queries);
@@ -1311,7 +1355,7 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
     a.causal = (flags & ARL2_CACHE_CAUSAL) ? 1 : 0;
     a.scale_log2 = cache->ctx->shape.scale_log2;
     a.out = d_out;
-    a.part_o = cache->part_o; a.part_ml = cache->part_ml; a.tickets = cache->tickets;
+    a.part_rows = cache->part_rows; a.part_o = cache->part_o; a.part_ml = cache->part_ml; a.tickets = cache->tickets;
     a.part_items = cache->part_items;
     a.unpacked = cache->unpacked; a.unpack_marks = cache->unpack_marks; a.unpack_pairs = cache->unpack_pairs; a.q_scale = cache->q_scale;
     a.tensor_cores = cache_tensor_cores(cfg);

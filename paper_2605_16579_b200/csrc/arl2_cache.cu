@@ -1130,6 +1130,7 @@ int launch_attend(CacheAttendArgs& a, cudaStream_t st)
     const long long most = items * ((((long long)a.c.max_pages << a.c.page_shift) + C::kChunk - 1) / C::kChunk);
     long long grid = ctas;
     if (grid > kCacheCtas) grid = kCacheCtas;
+    if (grid > a.part_rows / (2 * C::kRows)) grid = a.part_rows / (2 * C::kRows);
     if (grid > most) grid = most;
     e = launch_kernel(kernel, dim3((unsigned)grid), kThreads, C::kBytes, st, a);
     if (e != cudaSuccess) { set_error("launch of cache_attend_kernel failed: %s", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }

@@ -215,6 +215,11 @@ constexpr int kCacheCtas = 4 * 148;        // most CTAs of the warp-level kernel
 constexpr int kCacheTcCtas = 148;          // most CTAs of the tcgen05 kernel, of 256 rows
 constexpr int kCachePartRows = 2 * kCacheTcCtas * 256;
 static_assert(2 * kCacheCtas * 32 <= kCachePartRows, "the partial rows of both kernels have the same room");
+// Rows by which that room may be smaller (where it is, the launchers take fewer CTAs), and the least: all CTAs of the warp-level kernel
+// that are there at once (four per SM of 8 rows, or three of 16).
+constexpr int kCachePartStep = 2 * 256;
+constexpr int kCacheLeastPartRows = 28 * kCachePartStep;
+static_assert(kCacheLeastPartRows >= 2 * 3 * 148 * 16 && kCacheLeastPartRows >= 2 * kCacheCtas * 8 && kCachePartRows % kCachePartStep == 0, "partial rows");
 // ... and for the operands of the tcgen05 kernel, made ahead of it: a pair is a K and a V tile of 128 keys of a head (from the front),
 // or the Q tiles of 256 query rows of a key head (from the back)
 constexpr int unpack_pair_bytes(int D) { return 2 * 128 * D * 2; }
@@ -235,8 +240,9 @@ struct CacheAttendArgs {
     int causal;
     float scale_log2;
     void* out;
-    float* part_o;           // [kCachePartRows, D] unnormalised rows (by eight channels where tcgen05 makes them)
-    float* part_ml;          // [kCachePartRows, 2] reference maximum (log2 units), row sum
+    int part_rows;           // partial rows that there is room for, at most kCachePartRows
+    float* part_o;           // [part_rows, D] unnormalised rows (by eight channels where tcgen05 makes them)
+    float* part_ml;          // [part_rows, 2] reference maximum (log2 units), row sum
     uint32_t* tickets;       // [kCacheCtas], zero between calls
     int4* part_items;        // [kCacheTcCtas] the item that a CTA of the tcgen05 kernel began and others went on with: parts, stream, block of rows, key head
     uint8_t* unpacked = nullptr;       // [unpack_pairs] pairs of operand tiles, and

@@ -1021,12 +1021,13 @@ int launch_tc(CacheAttendArgs a, int num_sms, cudaStream_t st)
     if (items >= 1LL << 31) { set_error("cache_attend: too many rows"); return ARL2_ERR_UNSUPPORTED; }
     const long long most = items * tiles;
     long long grid = num_sms < kCacheTcCtas ? num_sms : kCacheTcCtas;
+    if (grid > a.part_rows / (2 * kItemRows)) grid = a.part_rows / (2 * kItemRows);
     if (grid > most) grid = most;
     // Operands are made ahead where there is room for them and several items read them, or where there are so few that the launch is
     // what counts.  us with them made ahead and on the way: 12 heads, 1536 rows over 9360 keys 111 and 124, 512 rows 58 and 62; 2 x 12
     // heads, 256 rows over 9360 75 and 62; 64 rows of 12 heads over 300, 1000, 4000, 9360 16.4, 17.6, 27.2, 38.0 and 18.4, 19.6, 26.5, 37.4,
     // of 2 x 12 17.5, 20.8, 33.7, 60.4 and 18.5, 21.2, 33.5, 52.1, of 8 x 8 22.3, 27.8, 68.0, 129 and 20.5, 25.8, 58.2, 119.
-    const bool ahead = a.unpack_pairs > 0 && a.s_B <= kUnpackStreams && (a.row_blocks > 1 || most <= 2LL * num_sms);
+    const bool ahead = items < a.unpack_pairs && a.s_B <= kUnpackStreams && (a.row_blocks > 1 || most <= 2LL * num_sms);
     const long long pairs = (long long)a.s_B * a.c.kv_heads * (tiles + a.row_blocks);
     // where the workspace may be too small for the lengths, which only the device knows, both kernels go out, and one returns at once
     a.either = ahead && pairs > a.unpack_pairs;

@@ -68,3 +68,18 @@ def test_struct_size_and_null_are_refused(lib):
     assert lib.arl2_cache_append(None, None, 0, 0, None, 0, 0, 1, None, None, None, None) == -1
     assert lib.arl2_cache_attend(None, None, 0, 0, 1, None, None, 0, None, None) == -1
     lib.arl2_cache_destroy(None)
+
+
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "bf16"), (64, "fp32"), (128, "fp32")])
+def test_least_workspace(lib, D, dtype):
+    """The least scratch: 14336 partial rows (28 SMs' of 256, two each) beside two small tables, whatever the capacity."""
+    cfg = layer_config(D=D, dtype=dtype)
+    sizes = [lib.arl2_cache_least_workspace_bytes(ctypes.byref(cfg), ctypes.byref(config(max_pages=n))) for n in (1, 100, 1 << 20)]
+    assert len(set(sizes)) == 1 and sizes[0] % 256 == 0
+    assert 0 <= sizes[0] - 14336 * 4 * (D + 2) <= 8192
+    assert sizes[0] < lib.arl2_cache_workspace_bytes(ctypes.byref(cfg), ctypes.byref(config(max_pages=1)))
+    assert lib.arl2_cache_least_workspace_bytes(ctypes.byref(cfg), ctypes.byref(config(kv_heads=5))) == 0
+
+
+def test_set_workspace_of_no_cache(lib):
+    assert lib.arl2_cache_set_workspace(None, None, 0, None) == -1
