@@ -162,10 +162,10 @@ __device__ __forceinline__ uint4 hold_word(uint32_t codes, __half2 low, __half2 
 }
 
 // ---- the Q operand of kWarpRows rows, from row `row0` of block rb of (b, h) on: rotated in fp32, scaled by a power of two into fp16's
-// range, rounded to fp16.  `first`: the position of the stream's first query, rows: the block's.  A lane has eight channels of a row, a
+// range, rounded to fp16.  have: the stream's keys, first: the position of its first query, rows: the block's.  A lane has eight channels of a row, a
 // warp two or four rows at a time; kBatch such steps' loads are in flight.  Lane l gets the factor of row l's scores.
 template <int kD, int kWarpRows, int kBatch>
-__device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb, int h, int first, int rows, uint8_t* tile, int row0, int lane)
+__device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb, int h, int have, int first, int rows, uint8_t* tile, int row0, int lane)
 {
     constexpr int kLanes = kD / 8, kAtOnce = 32 / kLanes;      // lanes of a row, rows of a step
     static_assert(kWarpRows % (kAtOnce * kBatch) == 0, "whole batches");
@@ -177,11 +177,13 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
         const __nv_bfloat16* src[kBatch];
         int at[kBatch];
         bool past = false;
+        uint32_t blind = have > 0 ? 0u : ~0u;      // steps whose row sees no key
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int flat = rb * kItemRows + min(row0 + r0 + k * kAtOnce + within, rows - 1), i = flat / p.rep, head = h * p.rep + flat - i * p.rep;
             src[k] = static_cast<const __nv_bfloat16*>(p.q) + b * p.q_batch + i * p.q_token + (size_t)head * kD + chunk * 8;
-            const long long t = max((long long)first + i, 0LL);
+            const long long pos = (long long)first + i, t = max(pos, 0LL);
+            if (p.causal && pos < 0) blind |= 1u << k;
             past |= t >= p.c.rope_rows;
             at[k] = (int)min(t, (long long)max(p.c.rope_rows, 1) - 1);
         }
@@ -235,11 +237,12 @@ __device__ __forceinline__ float write_q(const CacheAttendArgs& p, int b, int rb
 #pragma unroll
             for (int d = 1; d < kLanes; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
             // 2^e with 1024 <= most * 2^e < 2048, -117 <= e <= 126; a row with an infinity or a NaN has no finite scores: its factor is NaN
+            // (but a row that sees no key is zero whatever it holds)
             const bool finite = most < 0x7f800000u;
             const int e2 = !finite || most == 0 ? 0 : min(137 - (int)(most >> 23), 126);
             const int row = r0 + k * kAtOnce + within;
             const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
-            const float factor = finite ? p.scale_log2 * __uint_as_float((uint32_t)(127 - e2) << 23) : __int_as_float(0x7fc00000);
+            const float factor = finite ? p.scale_log2 * __uint_as_float((uint32_t)(127 - e2) << 23) : (blind >> k) & 1u ? 1.0f : __int_as_float(0x7fc00000);
             const float given = __shfl_sync(0xffffffffu, factor, (lane % kAtOnce) * kLanes);
             if (lane / kAtOnce == (r0 / kAtOnce) + k) own = given;
             const bool zero = !finite || row0 + row >= rows;
@@ -306,12 +309,11 @@ __device__ __forceinline__ void softmax_role(const CacheAttendArgs& p, uint8_t* 
             c2 = p.q_scale[q_pair(p, seg.at) * kItemRows + in_item];
         } else {
             // (Every MMA that read the item before's Q has ended: its last scores have been here.)
-            c2 = write_q<kD, 32, 4>(p, seg.at.b, seg.at.rb, seg.at.h, seg.first, seg.rows, smem + t * Dims<kD>::kOperand, t * kTile + warp_in_group * 32, r & 31);
+            c2 = write_q<kD, 32, 4>(p, seg.at.b, seg.at.rb, seg.at.h, seg.have, seg.first, seg.rows, smem + t * Dims<kD>::kOperand, t * kTile + warp_in_group * 32, r & 31);
             fence_proxy_async_smem();
             mbar_arrive(bars + 8 * (kBarQ0 + t));
         }
 
-        if (sees <= 0) c2 = 1.0f;      // (the factor of a row that is not finite is NaN; a row that sees no key is zero all the same)
         const uint64_t c2x2 = pack2(c2, c2);
         float m_ref = -INFINITY;
         uint64_t l2 = pack2(0.0f, 0.0f);
@@ -851,7 +853,7 @@ __global__ void __launch_bounds__(kUnpackThreads, 4) cache_unpack_kernel(const C
         Streams::look_up(p, at.b, have, position);
         constexpr int kWarpRows = kItemRows / kQParts / (kUnpackThreads / 32);
         const int row0 = (work % kQParts) * (kItemRows / kQParts) + (tid >> 5) * kWarpRows, lane = tid & 31;
-        const float scale = write_q<kD, kWarpRows, 2>(p, at.b, at.rb, at.h, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
+        const float scale = write_q<kD, kWarpRows, 2>(p, at.b, at.rb, at.h, have, position, min(kItemRows, p.queries * p.rep - at.rb * kItemRows),
                                         p.unpacked + pair * kUnpackPair + (row0 / kTile) * kTileBytes, row0, lane);
         if (lane < kWarpRows) p.q_scale[pair * kItemRows + row0 + lane] = scale;
     }
