@@ -352,7 +352,9 @@ int arl2_cache_append(arl2_cache* cache, const void* d_k, int64_t k_batch_stride
  * Positions before the first row of the rotary tables count as the first row.  A length past the table or a position past the
  * rotary tables counts as the last there is, a page that the pool does not have reads as zeros, and arl2_sync_status reports
  * ARL2_ERR_RANGE.  bf16 I/O: fp16 operands on tensor cores, fp32 softmax and sums; fp32 I/O: each
- * fp32 operand as two fp16 numbers (the codes are exact), to fp32's accuracy.  Bitwise reproducible.
+ * fp32 operand as two fp16 numbers (the codes are exact), to fp32's accuracy.  Bitwise reproducible (with a scratch of the same
+ * size: a smaller one may cut the work elsewhere).  Weights below 2^-32 of a row's largest count in its sum only (bf16 I/O); where value
+ * ranges of visible tokens differ by more than 2^20 in a group of 64 channels, the narrow ones lose bits (up to 32 rows, and fp32).
  * More than 32 rows (queries * H / kv_heads) with bf16 I/O go to tcgen05 kernels, two to four launches; all else, and every call
  * of an ARL2_FLAG_FORCE_SIMT context, to one kernel of warp-level matrix instructions.  `queries` need not be L.
  */

@@ -4,8 +4,8 @@
 // 64 channels with its 3 neighbours, and writes two words of 8 codes.  4 D bytes (bf16) are read per token and head and 9/8 D written,
 // but what bounds it is the instructions: about 18 a value, of which minimum, maximum, quotient and clamp are on the half-rate pipe.
 // One head per row group, K and V of it: with two, which fetch the token's row of the rotary tables once, 40 heads x 4 x 4680 tokens took
-// 175 us, with one, and twice the warps on an SM, 157.  Now 151 in a row: 877 MB at 5.8 TB/s, 0.89 of the rate of a copy; 181 where
-// other sets of inputs have been in L2 in between.  One token of each stream: 2.8 us.
+// 175 us, with one, and twice the warps on an SM, 157.  Now 150 in a row: 877 MB at 5.8 TB/s, 0.89 of the rate of a copy (118 where the
+// held values are not asked for); 175 to 181 where other sets of inputs have been in L2 in between.  One token of each stream: 2.8 us.
 //
 // Attention (one query per stream up to a few dozen rows; any number in fp32).  Keys are the M side of the
 // matrix instruction and query rows the N side, so that 8 rows fill it:  S^T = K Q^T, then  O^T = V^T P^T.  Codes go into the
@@ -14,14 +14,17 @@
 //   s_j = sum_g  st_jg (sum_c q_c code_jc) + lo_jg (sum_c q_c),        o_c = sum_j (p_j st_jg) code_jc + sum_j p_j lo_jg,
 // so a key costs a few fp32 operations per group and its 256 values cost one AND each pair, and nothing of a value is rounded.
 // Rows of q are scaled by a power of two into fp16's range (1024 <= max < 2048), p st by a power of two per group, which
-// grows like the softmax's reference maximum.  fp32 I/O: q and p st as two fp16 numbers each, twice the instructions, and codes
-// less 8 as whole numbers (an addition per pair): with unsigned ones the sums of 64 products, from which the minimum's part is
-// subtracted, lost five bits (errors of 3e-6 to 9e-6 of the output, now 1e-7).
+// grows like the softmax's reference maximum: with the largest finite step among the keys that some row sees.  (Where that is more than
+// 2^20 times another key's step, the latter's products get into fp16's denormals and lose bits, however small the larger one's weight
+// is.)  fp32 I/O: q and p st as two fp16 numbers each, twice the instructions, and codes less 8 as whole numbers (an addition per pair):
+// with unsigned ones the sums of 64 products, from which the minimum's part is subtracted, lost five bits (errors of 3e-6 to 9e-6 of the
+// output, now 1e-7).
 // What bounds it over long caches is the instructions of a warp, about 264 per 16 keys and 8 rows (two products, the scores' factors, the
 // exponentials), which wait for one another: issue slots 55 %, tensor pipe 25 %, DRAM 51 % busy.  Over short ones, what a CTA does once:
 // plan, rows of Q, first keys, its four warps' rows put together, and the item's parts (a part more costs about 0.4 us at 16 rows).  us in
-// a row: one query in each of 4 streams of 12 heads over 74880 tokens 103 to 107 (518 MB, 5.0 TB/s, 0.77 of a copy's rate); 8 streams of
-// 40 heads on 8 over 9360 32; 12 heads over 500 9.5; fp32, 2 heads, 256 rows over 768 14.7, 12 heads, 700 over 1400 97.
+// a row: one query in each of 4 streams of 12 heads over 74880 tokens 104 to 110 (518 MB, 4.7 to 5.0 TB/s, 0.72 to 0.76 of a copy's rate),
+// of 64 channels 68, in fp32 176; 8 streams of 40 heads on 8 over 9360 33; 12 heads over 500 9.7; fp32, 2 heads, 256 rows over 768 14.7, 12
+// heads, 700 over 1400 97.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -1156,7 +1159,7 @@ int cache_append(const CacheAppendArgs& a, int dtype, cudaStream_t st)
 // Rows per key head up to which this file's kernel is the faster one where both can do it.  us with it and with tcgen05: 32 rows of 12
 // heads over 300, 1000, 9360 keys 13.8, 17.0, 32.6 and 16.0, 17.1, 37.0, of 2 x 12 15.1, 18.3, 44 and 17.5, 19.8, 59, of 2 heads 13.8, 15.4,
 // 29.0 and 14.0, 15.0, 26.1; 48 rows of 8 x 8 17, 34, 122 and 22, 27, 128 (now 119); 64 rows of 2 x 12 15.6, 20.7, 66 and 17.7, 20.8, 60 (now
-// 52).  At D = 64, 12 heads: 32 rows 11.3, 14.8, 26.4 and 12.7, 14.2, 28.4, 64 rows 12.1, 15.1, 31.8 and 12.8, 14.4, 28.7; 1560 over 9360 353
+// 52).  (33 to 64 rows over a few hundred keys lose by this rule.  The host does not know the lengths.)  At D = 64, 12 heads: 32 rows 11.3, 14.8, 26.4 and 12.7, 14.2, 28.4, 64 rows 12.1, 15.1, 31.8 and 12.8, 14.4, 28.7; 1560 over 9360 353
 // and 88.
 constexpr int kFewRows = 32;
 

@@ -22,10 +22,10 @@
 // What bounds it: of a key tile's 3800 clk, the tensor pipe works 2048 (D = 128), the special-function units 1536; the rest is a
 // group's own chain - scores, maximum, exponentials, P V, the next scores - of which the other group hides only a part.  Two threads per
 // row (registers spilled: 141 us for 113), scores of 64 keys at a time, two sets of them (125), and issuers that do not take turns (131)
-// were slower.  12 heads, D = 128, us in a row: 1560 rows over 9360 keys 110, of which the unpacking has 16 (26 MB read, 67 MB written)
+// were slower.  12 heads, D = 128, us in a row: 1560 rows over 9360 keys 110 (120 under the power limit), of which the unpacking has 16 (26 MB read, 67 MB written)
 // and the joining 8 (28 MB of partial rows), 815 TFLOP/s in all, 0.50 of a large matrix product's rate; 4680 over 18720 482 alone
 // (1115 TFLOP/s, 0.68), 525 under the power limit; 4 streams of 701 rows over 1399 keys, causal, 63 (14, 41, 8).  At D = 64 1560 over
-// 9360 take 88.
+// 9360 take 86.
 #include "cache_common.cuh"
 #include "tc_common.cuh"
 
