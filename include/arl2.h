@@ -365,6 +365,100 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
 /* Frees the host object only; no device buffer is touched and nothing is synchronised. */
 void arl2_cache_destroy(arl2_cache* cache);
 
+/*
+ * What stands around the core in a block of the model.  Three operators with their backward passes; `tokens` per stream is given
+ * with each call and need not be L, B, H, D and the I/O type are the context's.  Their calls read and write no state of the context (its status
+ * word and launch counter are all they share), may be captured and replayed, and are bitwise reproducible.
+ *
+ * Rows of a tensor that need not be contiguous: `data` [B, rows, ...] with the innermost dimensions contiguous and the strides of the
+ * others in elements (0 repeats a row).  All tensors and strides are multiples of 16 bytes.
+ */
+typedef struct {
+    const void* data;      /* NULL: none */
+    int64_t batch_stride;
+    int64_t row_stride;
+} arl2_rows;
+
+typedef enum {
+    ARL2_NORM_NONE = 0,
+    ARL2_NORM_LAYER = 1,   /* (x - mean) / sqrt(variance + eps) over the row                     */
+    ARL2_NORM_RMS = 2,     /* x / sqrt(mean x^2 + eps) over the row                              */
+    ARL2_NORM_TOKEN = 3,   /* rotation: x / sqrt(mean x^2 + eps) over all heads of a token       */
+    ARL2_NORM_HEAD = 4,    /* rotation: the same over the D channels of a head                   */
+    ARL2_NORM_LENGTH = 5   /* rotation: x / sqrt(sum x^2 + eps) over a head, the layer's L2Norm  */
+} arl2_norm;
+
+/*
+ * Modulation: the end of one block part and the beginning of the next in one pass over the residual stream, rows of d = H * D
+ * (at most 8192) channels:
+ *   r = x + gate_f * P(y) * w_post,   n = N(r) * w * (1 + scale_f) + shift_f,   f = token / frame_tokens
+ * x, r [B, tokens, d]: the stream, of the I/O type, or fp32 with ARL2_MODULATION_FP32_RESIDUAL; n is made from r as it is stored.
+ * y, n [B, tokens, d] of the I/O type.  gate, scale, shift: fp32, a row of d per frame, ceil(tokens / frame_tokens) per stream.
+ *   y NULL: nothing is added, r must be NULL and n comes from x.  n NULL: no norm.  gate (1), scale (0), shift (0), weight and post_weight
+ *   (fp32 [d], 1) may be NULL, the three arl2_rows also as pointers.  r may be x, and n may be y.
+ * 16-byte aligned contiguous tensors.
+ */
+#define ARL2_MODULATION_FP32_RESIDUAL 1u
+typedef struct {
+    uint32_t struct_size;
+    int32_t frame_tokens;  /* >= 1 */
+    int32_t norm;          /* N: ARL2_NORM_LAYER or ARL2_NORM_RMS */
+    int32_t post_norm;     /* P: the same, or ARL2_NORM_NONE: P(y) = y, and no post_weight */
+    float eps;             /* 0 -> 1e-6 */
+    uint32_t flags;        /* ARL2_MODULATION_* */
+} arl2_modulation_config;
+int arl2_modulate(arl2_ctx* ctx, const arl2_modulation_config* cfg, int32_t tokens, const void* d_x, const void* d_y,
+                  const arl2_rows* gate, const arl2_rows* scale, const arl2_rows* shift, const float* d_weight,
+                  const float* d_post_weight, void* d_r, void* d_n, void* stream);
+
+/*
+ * Its backward pass: from dr and dn, the gradients of r (through all else that reads it) and n, either may be NULL:
+ *   d_r   what arl2_modulate wrote (its x, where there was no y);  d_y as there, or NULL
+ *   d_dx  gradient of x, of the stream's type;  d_dy of y (NULL exactly where y is)
+ *   d_dgate, d_dscale, d_dshift  fp32 [B, ceil(tokens / frame_tokens), d], contiguous;  d_dweight, d_dpost_weight  fp32 [d]; each may be NULL
+ * dx may be dr, and dy may be y or dn.  The workspace (arl2_modulation_workspace_bytes, 256-byte aligned) holds nothing between calls.
+ */
+size_t arl2_modulation_workspace_bytes(const arl2_config* cfg, const arl2_modulation_config* modulation_cfg, int32_t tokens);
+int arl2_modulate_backward(arl2_ctx* ctx, const arl2_modulation_config* cfg, int32_t tokens, const void* d_r, const void* d_dn,
+                           const void* d_dr, const void* d_y, const arl2_rows* gate, const arl2_rows* scale, const float* d_weight,
+                           const float* d_post_weight, void* d_dx, void* d_dy, float* d_dgate, float* d_dscale, float* d_dshift,
+                           float* d_dweight, float* d_dpost_weight, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotation: queries [B, tokens, H, D] and keys [B, tokens, kv_heads, D] (data NULL: queries alone) on their way to the attention,
+ *   out = R_pos(w * x / length),
+ * the norm by cfg.norm (weights fp32, [heads * D] with ARL2_NORM_TOKEN, [D] with ARL2_NORM_HEAD, else NULL; NULL: 1), then pair
+ * (2m, 2m+1) of each head turned by the angle whose cos and sin stand in column m of the tables, in the row of the token's position
+ * along the pair's axis: the first axis_pairs[0] pairs go by the first position, the next axis_pairs[1] by the second, the next
+ * axis_pairs[2] by the third, and what is left does not turn.  Positions: d_positions [B, tokens, 3], or NULL and
+ *   (start[b] + l / (grid_rows * grid_columns),  l / grid_columns % grid_rows,  l % grid_columns)   of token l; d_start [B] or NULL: 0.
+ * A position before the tables counts as their first row; one behind them as the last, and arl2_sync_status reports ARL2_ERR_RANGE.
+ * Outputs are contiguous and 16-byte aligned; one may be its own input where that is contiguous.  (H + kv_heads) * D <= 16384.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t kv_heads;      /* >= 1 */
+    int32_t rope_rows;     /* rows of the tables, >= 1 */
+    int32_t axis_pairs[3]; /* >= 0, at most D / 2 together */
+    int32_t grid_rows, grid_columns;   /* >= 1 */
+    int32_t norm;          /* ARL2_NORM_NONE, _TOKEN, _HEAD or _LENGTH */
+    float eps;             /* 0 -> 1e-6 */
+} arl2_rotation_config;
+int arl2_rotate(arl2_ctx* ctx, const arl2_rotation_config* cfg, const float* d_rope_cos, const float* d_rope_sin, int32_t tokens,
+                const arl2_rows* q, const arl2_rows* k, const int32_t* d_start, const int32_t* d_positions, const float* d_q_weight,
+                const float* d_k_weight, void* d_q_out, void* d_k_out, void* stream);
+
+/*
+ * Its backward pass: dq_out, dk_out [B, tokens, heads, D] contiguous (dk_out NULL: queries alone), q and k as there (looked at only where
+ * there is a norm).  d_dq, d_dk contiguous, each may be the gradient it is made from; d_dq_weight, d_dk_weight fp32, shaped like the weights (given or
+ * not), each may be NULL.  Workspace as above.
+ */
+size_t arl2_rotation_workspace_bytes(const arl2_config* cfg, const arl2_rotation_config* rotation_cfg, int32_t tokens);
+int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* cfg, const float* d_rope_cos, const float* d_rope_sin, int32_t tokens,
+                         const void* d_dq_out, const void* d_dk_out, const arl2_rows* q, const arl2_rows* k, const int32_t* d_start,
+                         const int32_t* d_positions, const float* d_q_weight, const float* d_k_weight, void* d_dq, void* d_dk,
+                         float* d_dq_weight, float* d_dk_weight, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* S <- 0 for stream `stream_index` (0..B-1) or all streams (-1): Algorithm 1, first line. */
 int arl2_reset(arl2_ctx* ctx, int32_t stream_index, void* stream);
 

@@ -22,6 +22,8 @@ ARL2_FLAG_GATE_SCALAR = 4
 ARL2_FLAG_GATE_ELEMENTWISE = 8
 ARL2_FLAG_DELTA_DECAYED_PREDICTION = 32
 ARL2_CACHE_CAUSAL = 1
+ARL2_NORM_NONE, ARL2_NORM_LAYER, ARL2_NORM_RMS, ARL2_NORM_TOKEN, ARL2_NORM_HEAD, ARL2_NORM_LENGTH = range(6)
+ARL2_MODULATION_FP32_RESIDUAL = 1
 
 
 def ARL2_FLAG_DEBUG_WAIT_LIMIT(polls: int) -> int:
@@ -35,6 +37,7 @@ EXPORTS = (
     "arl2_projection_workspace_bytes", "arl2_set_projections", "arl2_project_in", "arl2_project_out",
     "arl2_cache_page_bytes", "arl2_cache_workspace_bytes", "arl2_cache_least_workspace_bytes", "arl2_cache_create", "arl2_cache_set_workspace",
     "arl2_cache_append", "arl2_cache_attend", "arl2_cache_destroy",
+    "arl2_modulate", "arl2_modulate_backward", "arl2_modulation_workspace_bytes", "arl2_rotate", "arl2_rotate_backward", "arl2_rotation_workspace_bytes",
 )
 
 
@@ -57,6 +60,24 @@ class arl2_cache_config(ctypes.Structure):
         ("struct_size", ctypes.c_uint32),
         ("kv_heads", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("num_pages", ctypes.c_int32),
         ("max_pages", ctypes.c_int32), ("rope_rows", ctypes.c_int32),
+    ]
+
+
+class arl2_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class arl2_modulation_config(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("frame_tokens", ctypes.c_int32), ("norm", ctypes.c_int32), ("post_norm", ctypes.c_int32),
+        ("eps", ctypes.c_float), ("flags", ctypes.c_uint32),
+    ]
+
+
+class arl2_rotation_config(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("kv_heads", ctypes.c_int32), ("rope_rows", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * 3),
+        ("grid_rows", ctypes.c_int32), ("grid_columns", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
     ]
 
 
@@ -142,6 +163,19 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.arl2_cache_attend.argtypes = [vp, vp, i64, i64, i32, vp, vp, u32, vp, vp]
     lib.arl2_cache_destroy.restype = None
     lib.arl2_cache_destroy.argtypes = [vp]
+    rp, mp, tp = ctypes.POINTER(arl2_rows), ctypes.POINTER(arl2_modulation_config), ctypes.POINTER(arl2_rotation_config)
+    lib.arl2_modulation_workspace_bytes.restype = ctypes.c_size_t
+    lib.arl2_modulation_workspace_bytes.argtypes = [cp, mp, i32]
+    lib.arl2_modulate.restype = ctypes.c_int
+    lib.arl2_modulate.argtypes = [vp, mp, i32, vp, vp, rp, rp, rp, vp, vp, vp, vp, vp]
+    lib.arl2_modulate_backward.restype = ctypes.c_int
+    lib.arl2_modulate_backward.argtypes = [vp, mp, i32, vp, vp, vp, vp, rp, rp] + [vp] * 10 + [ctypes.c_size_t, vp]
+    lib.arl2_rotation_workspace_bytes.restype = ctypes.c_size_t
+    lib.arl2_rotation_workspace_bytes.argtypes = [cp, tp, i32]
+    lib.arl2_rotate.restype = ctypes.c_int
+    lib.arl2_rotate.argtypes = [vp, tp, vp, vp, i32, rp, rp, vp, vp, vp, vp, vp, vp, vp]
+    lib.arl2_rotate_backward.restype = ctypes.c_int
+    lib.arl2_rotate_backward.argtypes = [vp, tp, vp, vp, i32, vp, vp, rp, rp] + [vp] * 9 + [ctypes.c_size_t, vp]
     lib.arl2_launch_count.restype = ctypes.c_uint64
     lib.arl2_launch_count.argtypes = [vp]
     lib.arl2_step_kernel_name.restype = ctypes.c_char_p
@@ -599,6 +633,240 @@ class Cache:
                 status = call(self._cache, *args, _raw_stream(index))
         if status != 0:
             _check(status, call.__name__)
+
+
+
+class _BlockOp:
+    """What stands around a layer's core shares its context: B, H, D, dtype, device."""
+
+    def __init__(self, layer):
+        self.layer = layer
+        self.device, self.dtype = layer.device, layer.dtype
+        self._lib, self._index = layer._lib, layer.device.index
+        self._B, self._H, self._D = layer.B, layer.H, layer.D
+        self._width = layer.H * layer.D
+
+    def _run(self, call, *args):
+        ctx = self.layer._ctx
+        if ctx is None:
+            raise Arl2Error(f"{call.__name__}: the layer has been closed")
+        current = torch.cuda.current_device()
+        index = self._index
+        if index is None or index == current:
+            status = call(ctx, *args, _raw_stream(current))
+        else:
+            with torch.cuda.device(index):
+                status = call(ctx, *args, _raw_stream(index))
+        if status != 0:
+            _check(status, call.__name__)
+
+    def _strided(self, t, shape, dtype, what, inner):
+        """arl2_rows of a tensor [B, rows, ...] whose dimensions from `inner` on are contiguous."""
+        if isinstance(t, torch.Tensor) and t.get_device() == self._index and t.dtype is dtype and t.shape == shape:
+            st, row = t.stride(), 1
+            for n, s in zip(reversed(shape[inner:]), reversed(st[inner:])):
+                if n != 1 and s != row:
+                    break
+                row *= n
+            else:
+                # (a dimension of one element may have any stride)
+                return arl2_rows(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else row)
+        raise Arl2Error(f"{what}: expected a tensor {tuple(shape)} {dtype} on {self.device} with contiguous rows, got "
+                        + (f"{tuple(t.shape)} {t.dtype} with strides {tuple(t.stride())} on {t.device}" if isinstance(t, torch.Tensor) else f"{t!r}"))
+
+    def _tokens(self, t, what, dims):
+        if not isinstance(t, torch.Tensor) or t.dim() != dims:
+            raise Arl2Error(f"{what}: expected a tensor of {dims} dimensions")
+        return t.shape[1]
+
+    def _scratch(self, n, given):
+        """Scratch of one call: the caller's, or memory that torch hands out for the current stream (or the graph being captured)."""
+        if given is None:
+            return torch.empty(n, dtype=torch.uint8, device=self.device)
+        if not (isinstance(given, torch.Tensor) and given.get_device() == self._index and given.dtype == torch.uint8 and given.is_contiguous()):
+            raise Arl2Error(f"workspace: expected contiguous uint8 on {self.device}")
+        return given
+
+
+class Modulation(_BlockOp):
+    """The end of one block part and the beginning of the next (arl2_modulate): r = x + gate P(y), n = N(r) weight (1 + scale) + shift.
+
+    ``frame_tokens`` tokens share a row of gate, scale and shift.  ``norm`` (N) is "layer" or "rms", ``post`` (P) one of them or None.
+    ``residual``: the type of x and r, the layer's or torch.float32.
+    """
+
+    def __init__(self, layer, frame_tokens, norm="layer", post=None, eps=0.0, residual=None):
+        super().__init__(layer)
+        self.frame_tokens = frame_tokens
+        self.residual = self.dtype if residual is None else residual
+        if self.residual not in (self.dtype, torch.float32):
+            raise Arl2Error(f"residual: expected {self.dtype} or {torch.float32}, got {residual}")
+        names = {None: ARL2_NORM_NONE, "layer": ARL2_NORM_LAYER, "rms": ARL2_NORM_RMS}
+        if norm not in names or post not in names:
+            raise Arl2Error(f"norm, post: expected one of {list(names)}, got {norm!r} and {post!r}")
+        flags = ARL2_MODULATION_FP32_RESIDUAL if self.residual is not self.dtype else 0
+        self.cfg = arl2_modulation_config(ctypes.sizeof(arl2_modulation_config), frame_tokens, names[norm], names[post], eps, flags)
+        self._cfg = ctypes.byref(self.cfg)
+        self.workspace_bytes(1)     # (what the library refuses is refused here)
+
+    def workspace_bytes(self, tokens):
+        n = self._lib.arl2_modulation_workspace_bytes(ctypes.byref(self.layer.cfg), self._cfg, tokens)
+        if n == 0:
+            raise Arl2Error("arl2_modulation_workspace_bytes: " + self._lib.arl2_last_error().decode())
+        return n
+
+    def _frames(self, tokens):
+        return -(-tokens // self.frame_tokens)
+
+    def _modulation(self, t, tokens, what):
+        if t is None:
+            return None
+        return self._strided(t, (self._B, self._frames(tokens), self._width), torch.float32, what, 2)
+
+    def _weight(self, t, what):
+        if t is not None:
+            self.layer._want(t, (self._width,), torch.float32, what)
+        return _ptr(t)
+
+    def forward(self, x, y=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, normed=True, r=None, n=None):
+        """x, y [B, T, H * D]; gate, scale, shift fp32 [B, ceil(T / frame_tokens), H * D] with contiguous rows (others may be strided or
+        expanded); weights fp32 [H * D].  Returns (r, n): r is x itself where there is no y, n is None with ``normed=False``.  ``r`` may
+        be given as x, and ``n`` as y: in place."""
+        tokens = self._tokens(x, "x", 3)
+        shape, want = (self._B, tokens, self._width), self.layer._want
+        want(x, shape, self.residual, "x")
+        if y is None:
+            if r is not None:
+                raise Arl2Error("r: nothing is written without y")
+        else:
+            want(y, shape, self.dtype, "y")
+            if r is None:
+                r = torch.empty_like(x)
+            else:
+                want(r, shape, self.residual, "r")
+        if not normed:
+            if n is not None:
+                raise Arl2Error("n: nothing is written with normed=False")
+        elif n is None:
+            n = torch.empty(shape, dtype=self.dtype, device=self.device)
+        else:
+            want(n, shape, self.dtype, "n")
+        self._run(self._lib.arl2_modulate, self._cfg, tokens, x.data_ptr(), _ptr(y), self._modulation(gate, tokens, "gate"),
+                  self._modulation(scale, tokens, "scale"), self._modulation(shift, tokens, "shift"), self._weight(weight, "weight"),
+                  self._weight(post_weight, "post_weight"), _ptr(r), _ptr(n))
+        return (x if r is None else r), n
+
+    def backward(self, r, dn=None, dr=None, y=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, workspace=None):
+        """Gradients (dx, dy, dgate, dscale, dshift, dweight, dpost_weight) from dn and dr, those of n and r (either may be None); None for
+        what forward was called without.  ``r`` is what forward returned; ``shift`` is not looked at beyond whether there is one."""
+        tokens = self._tokens(dn if dr is None else dr, "dn or dr", 3)
+        shape, want = (self._B, tokens, self._width), self.layer._want
+        if r is not None or dn is not None:
+            want(r, shape, self.residual, "r") if isinstance(r, torch.Tensor) else self._tokens(r, "r", 3)
+        for t, kind, what in ((dn, self.dtype, "dn"), (dr, self.residual, "dr"), (y, self.dtype, "y")):
+            if t is not None:
+                want(t, shape, kind, what)
+        rows = (self._B, self._frames(tokens), self._width)
+        empty = lambda given, shape: None if given is None else torch.empty(shape, dtype=torch.float32, device=self.device)  # noqa: E731
+        dx = torch.empty(shape, dtype=self.residual, device=self.device)
+        dy = None if y is None else torch.empty_like(y)
+        dgate, dscale, dshift = empty(gate, rows), None if dn is None else empty(scale, rows), None if dn is None else empty(shift, rows)
+        dweight, dpost = None if dn is None else empty(weight, (self._width,)), empty(post_weight, (self._width,))
+        ws = self._scratch(self.workspace_bytes(tokens), workspace)
+        self._run(self._lib.arl2_modulate_backward, self._cfg, tokens, _ptr(r), _ptr(dn), _ptr(dr), _ptr(y), self._modulation(gate, tokens, "gate"),
+                  self._modulation(scale, tokens, "scale"), self._weight(weight, "weight"), self._weight(post_weight, "post_weight"),
+                  dx.data_ptr(), _ptr(dy), _ptr(dgate), _ptr(dscale), _ptr(dshift), _ptr(dweight), _ptr(dpost), ws.data_ptr(), ws.numel())
+        return dx, dy, dgate, dscale, dshift, dweight, dpost
+
+
+class Rotation(_BlockOp):
+    """Queries and keys on their way to the attention (arl2_rotate): a norm, then the rotation of adjacent channels by positions along up
+    to three axes.
+
+    ``rope_cos``, ``rope_sin`` fp32 [positions, D / 2]; ``axes``: pairs that turn with the first, second and third position (the rest do not turn).
+    Positions of token l: (start + l // (rows * columns), l // columns % rows, l % columns) for ``grid`` = (rows, columns).
+    ``norm``: None, "token" (RMS over all heads), "head" (RMS over one) or "l2" (rows of length one, the layer's L2Norm).
+    """
+
+    def __init__(self, layer, rope_cos, rope_sin, axes, grid=(1, 1), norm=None, kv_heads=None, eps=0.0):
+        super().__init__(layer)
+        self.kv_heads = layer.H if kv_heads is None else kv_heads
+        names = {None: ARL2_NORM_NONE, "token": ARL2_NORM_TOKEN, "head": ARL2_NORM_HEAD, "l2": ARL2_NORM_LENGTH}
+        if norm not in names:
+            raise Arl2Error(f"norm: expected one of {list(names)}, got {norm!r}")
+        self.norm = norm
+        self._tokens(rope_cos, "rope table", 2)
+        rows = rope_cos.shape[0]
+        for t in (rope_cos, rope_sin):
+            layer._want(t, (rows, self._D // 2), torch.float32, "rope table")
+        axes = tuple(axes) + (0,) * (3 - len(axes))
+        if len(axes) != 3:
+            raise Arl2Error(f"axes: expected at most three, got {axes}")
+        self._rope = (rope_cos, rope_sin)
+        self._tables = (rope_cos.data_ptr(), rope_sin.data_ptr())
+        self.cfg = arl2_rotation_config(ctypes.sizeof(arl2_rotation_config), self.kv_heads, rows, axes, grid[0], grid[1], names[norm], eps)
+        self._cfg = ctypes.byref(self.cfg)
+        self.workspace_bytes(1)
+
+    def workspace_bytes(self, tokens):
+        n = self._lib.arl2_rotation_workspace_bytes(ctypes.byref(self.layer.cfg), self._cfg, tokens)
+        if n == 0:
+            raise Arl2Error("arl2_rotation_workspace_bytes: " + self._lib.arl2_last_error().decode())
+        return n
+
+    def _where(self, start, positions, tokens):
+        if start is not None:
+            self.layer._want(start, (self._B,), torch.int32, "start")
+        if positions is not None:
+            self.layer._want(positions, (self._B, tokens, 3), torch.int32, "positions")
+        return _ptr(start), _ptr(positions)
+
+    def _weight(self, t, heads, what):
+        if t is not None:
+            self.layer._want(t, (heads * self._D if self.norm == "token" else self._D,), torch.float32, what)
+        return _ptr(t)
+
+    def forward(self, q, k=None, start=None, positions=None, q_weight=None, k_weight=None, q_out=None, k_out=None):
+        """q [B, T, H, D], k [B, T, kv_heads, D] (heads and channels contiguous) -> the same, rotated, contiguous; (q, None) without k.
+        ``start`` int32 [B] (first position along the first axis), or ``positions`` int32 [B, T, 3].  An output given as its own
+        contiguous input is written in place."""
+        tokens = self._tokens(q, "q", 4)
+        q_shape, k_shape = (self._B, tokens, self._H, self._D), (self._B, tokens, self.kv_heads, self._D)
+        q_rows = self._strided(q, q_shape, self.dtype, "q", 2)
+        k_rows = None if k is None else self._strided(k, k_shape, self.dtype, "k", 2)
+        if q_out is None:
+            q_out = torch.empty(q_shape, dtype=self.dtype, device=self.device)
+        else:
+            self.layer._want(q_out, q_shape, self.dtype, "q_out")
+        if k_out is not None:
+            self.layer._want(k_out, k_shape, self.dtype, "k_out")
+        elif k is not None:
+            k_out = torch.empty(k_shape, dtype=self.dtype, device=self.device)
+        self._run(self._lib.arl2_rotate, self._cfg, *self._tables, tokens, q_rows, k_rows, *self._where(start, positions, tokens),
+                  self._weight(q_weight, self._H, "q_weight"), self._weight(k_weight, self.kv_heads, "k_weight"), q_out.data_ptr(), _ptr(k_out))
+        return q_out, k_out
+
+    def backward(self, dq_out, dk_out=None, q=None, k=None, start=None, positions=None, q_weight=None, k_weight=None, workspace=None):
+        """Gradients (dq, dk, dq_weight, dk_weight) from those of the outputs; q and k are the inputs (needed only with a norm).
+        None for what forward was called without."""
+        tokens = self._tokens(dq_out, "dq_out", 4)
+        q_shape, k_shape = (self._B, tokens, self._H, self._D), (self._B, tokens, self.kv_heads, self._D)
+        self.layer._want(dq_out, q_shape, self.dtype, "dq_out")
+        if dk_out is not None:
+            self.layer._want(dk_out, k_shape, self.dtype, "dk_out")
+        q_rows = None if q is None else self._strided(q, q_shape, self.dtype, "q", 2)
+        k_rows = None if k is None else self._strided(k, k_shape, self.dtype, "k", 2)
+        dq, dk = torch.empty_like(dq_out), None if dk_out is None else torch.empty_like(dk_out)
+        q_w, k_w = self._weight(q_weight, self._H, "q_weight"), self._weight(k_weight, self.kv_heads, "k_weight")
+        dq_weight = None if q_weight is None else torch.empty_like(q_weight)
+        dk_weight = None if k_weight is None or dk_out is None else torch.empty_like(k_weight)
+        ws = None
+        if dq_weight is not None or dk_weight is not None or workspace is not None:
+            ws = self._scratch(self.workspace_bytes(tokens), workspace)
+        self._run(self._lib.arl2_rotate_backward, self._cfg, *self._tables, tokens, dq_out.data_ptr(), _ptr(dk_out), q_rows, k_rows,
+                  *self._where(start, positions, tokens), q_w, k_w, dq.data_ptr(), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight), _ptr(ws),
+                  0 if ws is None else ws.numel())
+        return dq, dk, dq_weight, dk_weight
 
 
 STATIC_SCRATCH_BYTES = 8 << 20

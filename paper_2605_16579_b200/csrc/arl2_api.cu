@@ -7,6 +7,7 @@
 
 #include <cuda.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <new>
 
@@ -1082,7 +1083,7 @@ int arl2_sync_status(arl2_ctx* ctx, void* stream)
     if (words[kStatusRange] != 0) {
         static const char* const what[] = {"", "a length or token outside of the page table", "a page that the pool does not have",
                                            "a position outside of the rotary tables"};
-        set_error("a cache call met %s (stream %u)", what[words[kStatusRange] & 3u], words[kStatusRangeWhere]);
+        set_error("a call met %s (stream %u)", what[words[kStatusRange] & 3u], words[kStatusRangeWhere]);
         int r = account(ctx, fill_zero(ctx->ws + ctx->lay.status, kStatusWords * sizeof(uint32_t), st));
         if (r != ARL2_OK) return r;
         return ARL2_ERR_RANGE;
@@ -1365,6 +1366,326 @@ int arl2_cache_attend(arl2_cache* cache, const void* d_q, int64_t q_batch_stride
 }
 
 void arl2_cache_destroy(arl2_cache* cache) { delete cache; }
+
+// ---- what stands around the core in a block: modulation and rotation ------------------------------------
+namespace {
+
+bool aligned16(std::initializer_list<const void*> ps)
+{
+    uintptr_t all = 0;
+    for (const void* p : ps) all |= reinterpret_cast<uintptr_t>(p);
+    return all % 16 == 0;
+}
+
+bool check_tokens(const char* who, const arl2_config& cfg, int32_t tokens)
+{
+    if (tokens >= 1 && (int64_t)tokens * cfg.B < ((int64_t)1 << 31)) return true;
+    set_error("%s: tokens must be >= 1, and fewer than 2^31 over the streams (got %d for each of %d)", who, tokens, cfg.B);
+    return false;
+}
+
+// Strided rows of `elem` bytes an element; nullptr is as good as no data.
+bool check_rows(const char* who, const arl2_rows* r, int elem)
+{
+    if (r == nullptr || r->data == nullptr) return true;
+    const int64_t most = (int64_t)1 << 40;
+    if (r->batch_stride < 0 || r->row_stride < 0 || r->batch_stride >= most || r->row_stride >= most) {
+        set_error("%s: strides must be in [0, 2^40) (got %lld and %lld)", who, (long long)r->batch_stride, (long long)r->row_stride);
+        return false;
+    }
+    if (!rows_are_wide(r->data, r->batch_stride, r->row_stride, elem)) {
+        set_error("%s: tensors and strides must be multiples of 16 bytes", who);
+        return false;
+    }
+    return true;
+}
+
+bool check_workspace(const char* who, const void* ws, size_t bytes, size_t need)
+{
+    if (need == 0 || (ws != nullptr && bytes >= need && reinterpret_cast<uintptr_t>(ws) % kAlign == 0)) return true;
+    set_error("%s: the workspace needs %zu bytes, 256-byte aligned (got %zu)", who, need, bytes);
+    return false;
+}
+
+// Whether two of the outputs are the same memory (NULL: no output).
+bool outputs_meet(const char* who, std::initializer_list<const void*> out)
+{
+    for (auto a = out.begin(); a != out.end(); ++a)
+        for (auto b = a + 1; b != out.end(); ++b)
+            if (*a != nullptr && *a == *b) { set_error("%s: two outputs are the same memory", who); return true; }
+    return false;
+}
+
+bool valid_modulation(const arl2_config* cfg, const arl2_modulation_config* c)
+{
+    if (c == nullptr) { set_error("modulation config is NULL"); return false; }
+    if (c->struct_size != sizeof(arl2_modulation_config)) {
+        set_error("modulation config.struct_size is %u, this library expects %zu", c->struct_size, sizeof(arl2_modulation_config));
+        return false;
+    }
+    if (c->frame_tokens < 1) { set_error("frame_tokens must be >= 1 (got %d)", c->frame_tokens); return false; }
+    if ((c->norm != ARL2_NORM_LAYER && c->norm != ARL2_NORM_RMS) ||
+        (c->post_norm != ARL2_NORM_NONE && c->post_norm != ARL2_NORM_LAYER && c->post_norm != ARL2_NORM_RMS)) {
+        set_error("norm must be ARL2_NORM_LAYER or ARL2_NORM_RMS, post_norm one of them or ARL2_NORM_NONE (got %d and %d)", c->norm, c->post_norm);
+        return false;
+    }
+    if (!(c->eps >= 0.0f) || isinf(c->eps)) { set_error("eps must be finite and >= 0"); return false; }
+    if ((c->flags & ~ARL2_MODULATION_FP32_RESIDUAL) != 0) { set_error("unknown modulation flags 0x%x", c->flags); return false; }
+    if ((int64_t)cfg->H * cfg->D > kBlockMostChannels) { set_error("modulation: H * D must be at most %d (got %lld)", kBlockMostChannels, (long long)cfg->H * cfg->D); return false; }
+    return true;
+}
+
+struct ModulationLayout { size_t parts, weight_parts, total; };
+ModulationLayout modulation_layout(const arl2_config& cfg, int32_t tokens)
+{
+    const int d = cfg.H * cfg.D;
+    const int64_t rows = (int64_t)cfg.B * tokens, most = block_runs(d / 8), runs = rows < most ? rows : most;
+    ModulationLayout l;
+    size_t off = 0;
+    l.parts = off;        off += align_up((size_t)runs * 2 * 3 * d * sizeof(float));
+    l.weight_parts = off; off += align_up((size_t)runs * 2 * d * sizeof(float));
+    l.total = off;
+    return l;
+}
+
+FrameRows frame_rows(const arl2_rows* r)
+{
+    return r == nullptr ? FrameRows{nullptr, 0, 0} : FrameRows{static_cast<const float*>(r->data), r->batch_stride, r->row_stride};
+}
+
+ModulateArgs modulate_args(const arl2_config& cfg, const arl2_modulation_config& c, int32_t tokens, const void* y, const arl2_rows* gate,
+                           const arl2_rows* scale, const float* weight, const float* post_weight)
+{
+    ModulateArgs a = {};
+    a.B = cfg.B; a.T = tokens; a.d = cfg.H * cfg.D; a.rows = cfg.B * tokens;
+    a.frame = c.frame_tokens < tokens ? c.frame_tokens : tokens;
+    a.norm = c.norm; a.post_norm = c.post_norm;
+    a.eps = c.eps > 0.0f ? c.eps : 1e-6f;
+    a.y = y;
+    a.gate = frame_rows(gate); a.scale = frame_rows(scale);
+    a.weight = weight; a.post_weight = post_weight;
+    return a;
+}
+
+bool valid_rotation(const arl2_config* cfg, const arl2_rotation_config* c)
+{
+    if (c == nullptr) { set_error("rotation config is NULL"); return false; }
+    if (c->struct_size != sizeof(arl2_rotation_config)) {
+        set_error("rotation config.struct_size is %u, this library expects %zu", c->struct_size, sizeof(arl2_rotation_config));
+        return false;
+    }
+    if (c->kv_heads < 1 || ((int64_t)cfg->H + c->kv_heads) * cfg->D > 2 * kBlockMostChannels) {
+        set_error("rotation: kv_heads must be >= 1 and (H + kv_heads) * D at most %d (got H = %d, kv_heads = %d)", 2 * kBlockMostChannels, cfg->H, c->kv_heads);
+        return false;
+    }
+    int64_t pairs = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (c->axis_pairs[i] < 0) { set_error("axis_pairs must be >= 0"); return false; }
+        pairs += c->axis_pairs[i];
+    }
+    if (pairs > cfg->D / 2) { set_error("axis_pairs are %lld together, a head has %d", (long long)pairs, cfg->D / 2); return false; }
+    if (c->rope_rows < 1) { set_error("rope_rows must be >= 1 (got %d)", c->rope_rows); return false; }
+    if (c->grid_rows < 1 || c->grid_columns < 1 || (int64_t)c->grid_rows * c->grid_columns >= ((int64_t)1 << 31)) {
+        set_error("grid_rows and grid_columns must be >= 1, their product below 2^31 (got %d and %d)", c->grid_rows, c->grid_columns);
+        return false;
+    }
+    if (c->norm != ARL2_NORM_NONE && c->norm != ARL2_NORM_TOKEN && c->norm != ARL2_NORM_HEAD && c->norm != ARL2_NORM_LENGTH) {
+        set_error("rotation: unknown norm %d", c->norm);
+        return false;
+    }
+    if (!(c->eps >= 0.0f) || isinf(c->eps)) { set_error("eps must be finite and >= 0"); return false; }
+    return true;
+}
+
+size_t rotation_workspace(const arl2_config& cfg, const arl2_rotation_config& c, int32_t tokens)
+{
+    if (c.norm != ARL2_NORM_TOKEN && c.norm != ARL2_NORM_HEAD) return 0;
+    // (with fewer vectors, of queries alone, there are more runs of fewer channels: room for either)
+    size_t most = 0;
+    for (int k = 0; k <= c.kv_heads; k += c.kv_heads) {
+        const int vecs = (cfg.H + k) * cfg.D / 8;
+        const int64_t rows = (int64_t)cfg.B * tokens, runs = rows < block_runs((vecs + 1) / 2) ? rows : block_runs((vecs + 1) / 2);
+        const size_t n = align_up((size_t)runs * vecs * 8 * sizeof(float));
+        if (n > most) most = n;
+    }
+    return most;
+}
+
+// What both directions check and fill in; false: refused.
+bool rotate_args(const char* who, arl2_ctx* ctx, const arl2_rotation_config* c, const float* cos_t, const float* sin_t, int32_t tokens, const arl2_rows* q,
+                 const arl2_rows* k, bool with_k, bool reads_x, const int32_t* start, const int32_t* positions, const float* q_weight,
+                 const float* k_weight, RotateArgs& a)
+{
+    if (!check_ctx(ctx) || !valid_rotation(&ctx->cfg, c) || !check_tokens(who, ctx->cfg, tokens)) return false;
+    const arl2_config& cfg = ctx->cfg;
+    const int elem = cfg.io_dtype == ARL2_FP32 ? 4 : 2;
+    if (cos_t == nullptr || sin_t == nullptr) { set_error("%s: the rotary tables must not be NULL", who); return false; }
+    if (reads_x && (q == nullptr || q->data == nullptr || (with_k && (k == nullptr || k->data == nullptr)))) {
+        set_error("%s: q, and k where its output or gradient is given, must not be NULL", who);
+        return false;
+    }
+    if (!check_rows(who, q, elem) || !check_rows(who, k, elem)) return false;
+    const bool weights = c->norm == ARL2_NORM_TOKEN || c->norm == ARL2_NORM_HEAD;
+    if (!weights && (q_weight != nullptr || k_weight != nullptr)) { set_error("%s: weights belong to ARL2_NORM_TOKEN and ARL2_NORM_HEAD", who); return false; }
+    if (!aligned16({cos_t, sin_t, q_weight, k_weight}) || (reinterpret_cast<uintptr_t>(start) | reinterpret_cast<uintptr_t>(positions)) % 4 != 0) {
+        set_error("%s: tables and weights must be 16-byte, positions 4-byte aligned", who);
+        return false;
+    }
+    a = RotateArgs{};
+    a.B = cfg.B; a.T = tokens; a.D = cfg.D; a.rows = cfg.B * tokens;
+    a.q_vecs = cfg.H * cfg.D / 8;
+    a.vecs = a.q_vecs + (with_k ? c->kv_heads * cfg.D / 8 : 0);
+    a.norm = c->norm;
+    a.eps = c->eps > 0.0f ? c->eps : 1e-6f;
+    a.q_over = c->norm == ARL2_NORM_LENGTH ? 1.0f : 1.0f / (float)(c->norm == ARL2_NORM_TOKEN ? cfg.H * cfg.D : cfg.D);
+    a.k_over = c->norm == ARL2_NORM_TOKEN ? 1.0f / (float)(c->kv_heads * cfg.D) : a.q_over;
+    a.cos = cos_t; a.sin = sin_t;
+    a.rope_rows = c->rope_rows;
+    for (int i = 0; i < 3; ++i) a.pairs[i] = c->axis_pairs[i];
+    a.grid_rows = c->grid_rows; a.grid_columns = c->grid_columns;
+    a.start = start; a.positions = positions;
+    if (q != nullptr) { a.q = q->data; a.q_batch = q->batch_stride; a.q_token = q->row_stride; }
+    if (k != nullptr) { a.k = k->data; a.k_batch = k->batch_stride; a.k_token = k->row_stride; }
+    a.q_weight = q_weight; a.k_weight = k_weight;
+    a.status = reinterpret_cast<uint32_t*>(ctx->ws + ctx->lay.status);
+    return true;
+}
+
+}  // namespace
+
+int arl2_modulate(arl2_ctx* ctx, const arl2_modulation_config* c, int32_t tokens, const void* d_x, const void* d_y, const arl2_rows* gate,
+                  const arl2_rows* scale, const arl2_rows* shift, const float* d_weight, const float* d_post_weight, void* d_r, void* d_n, void* stream)
+{
+    if (!check_ctx(ctx) || !valid_modulation(&ctx->cfg, c) || !check_tokens("modulate", ctx->cfg, tokens)) return ARL2_ERR_INVALID_ARG;
+    if (d_x == nullptr || (d_y == nullptr && d_n == nullptr)) { set_error("modulate: x, and one of y and n, must not be NULL"); return ARL2_ERR_INVALID_ARG; }
+    if ((d_y == nullptr) != (d_r == nullptr)) { set_error("modulate: r is written where y is added, and only there"); return ARL2_ERR_INVALID_ARG; }
+    const bool gated = gate != nullptr && gate->data != nullptr;
+    if (d_y == nullptr && (gated || d_post_weight != nullptr)) { set_error("modulate: a gate or post_weight without y"); return ARL2_ERR_INVALID_ARG; }
+    if (c->post_norm == ARL2_NORM_NONE && d_post_weight != nullptr) { set_error("modulate: post_weight without a post_norm"); return ARL2_ERR_INVALID_ARG; }
+    if (!check_rows("modulate: gate", gate, 4) || !check_rows("modulate: scale", scale, 4) || !check_rows("modulate: shift", shift, 4)) return ARL2_ERR_INVALID_ARG;
+    if (!aligned16({d_x, d_y, d_weight, d_post_weight, d_r, d_n})) { set_error("modulate: tensors must be 16-byte aligned"); return ARL2_ERR_INVALID_ARG; }
+    if (outputs_meet("modulate", {d_r, d_n})) return ARL2_ERR_INVALID_ARG;
+    if (d_r == d_y && d_r != nullptr) { set_error("modulate: r may be x, not y"); return ARL2_ERR_INVALID_ARG; }
+    if (d_n == d_x) { set_error("modulate: n may be y, not x"); return ARL2_ERR_INVALID_ARG; }
+    ModulateArgs a = modulate_args(ctx->cfg, *c, tokens, d_y, gate, scale, d_weight, d_post_weight);
+    a.x = d_x;
+    a.shift = frame_rows(shift);
+    a.r = d_r; a.n = d_n;
+    return account(ctx, modulate(a, ctx->cfg.io_dtype, (c->flags & ARL2_MODULATION_FP32_RESIDUAL) != 0, as_stream(stream)));
+}
+
+size_t arl2_modulation_workspace_bytes(const arl2_config* cfg, const arl2_modulation_config* c, int32_t tokens)
+{
+    if (!valid_config(cfg) || !valid_modulation(cfg, c) || !check_tokens("modulation_workspace_bytes", *cfg, tokens)) return 0;
+    return modulation_layout(*cfg, tokens).total;
+}
+
+int arl2_modulate_backward(arl2_ctx* ctx, const arl2_modulation_config* c, int32_t tokens, const void* d_r, const void* d_dn, const void* d_dr,
+                           const void* d_y, const arl2_rows* gate, const arl2_rows* scale, const float* d_weight, const float* d_post_weight,
+                           void* d_dx, void* d_dy, float* d_dgate, float* d_dscale, float* d_dshift, float* d_dweight, float* d_dpost_weight,
+                           void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    if (!check_ctx(ctx) || !valid_modulation(&ctx->cfg, c) || !check_tokens("modulate_backward", ctx->cfg, tokens)) return ARL2_ERR_INVALID_ARG;
+    if (d_dx == nullptr || (d_dn == nullptr && d_dr == nullptr) || (d_dn != nullptr && d_r == nullptr)) {
+        set_error("modulate_backward: dx, one of dn and dr, and with dn also r, must not be NULL");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if ((d_y == nullptr) != (d_dy == nullptr)) { set_error("modulate_backward: dy is written where there is a y, and only there"); return ARL2_ERR_INVALID_ARG; }
+    const bool gated = gate != nullptr && gate->data != nullptr;
+    if (d_y == nullptr && (gated || d_post_weight != nullptr || d_dgate != nullptr || d_dpost_weight != nullptr)) {
+        set_error("modulate_backward: a gate, post_weight or gradient of one without y");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (c->post_norm == ARL2_NORM_NONE && (d_post_weight != nullptr || d_dpost_weight != nullptr)) { set_error("modulate_backward: post_weight without a post_norm"); return ARL2_ERR_INVALID_ARG; }
+    if (d_dn == nullptr && (d_dscale != nullptr || d_dshift != nullptr || d_dweight != nullptr)) {
+        set_error("modulate_backward: gradients of scale, shift and weight come from dn");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (!check_rows("modulate_backward: gate", gate, 4) || !check_rows("modulate_backward: scale", scale, 4)) return ARL2_ERR_INVALID_ARG;
+    if (!aligned16({d_r, d_dn, d_dr, d_y, d_weight, d_post_weight, d_dx, d_dy, d_dgate, d_dscale, d_dshift, d_dweight, d_dpost_weight})) {
+        set_error("modulate_backward: tensors must be 16-byte aligned");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (outputs_meet("modulate_backward", {d_dx, d_dy, d_dgate, d_dscale, d_dshift, d_dweight, d_dpost_weight})) return ARL2_ERR_INVALID_ARG;
+    if ((d_dx == d_r && d_dx != nullptr) || d_dx == d_dn || (d_dx == d_y && d_y != nullptr) || (d_dy != nullptr && (d_dy == d_r || d_dy == d_dr))) {
+        set_error("modulate_backward: dx may be dr, and dy may be y or dn");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    const ModulationLayout lay = modulation_layout(ctx->cfg, tokens);
+    if (!check_workspace("modulate_backward", d_workspace, workspace_bytes, lay.total)) return ARL2_ERR_WORKSPACE;
+    ModulateBackArgs a = {};
+    a.m = modulate_args(ctx->cfg, *c, tokens, d_y, gate, scale, d_weight, d_post_weight);
+    a.m.r = const_cast<void*>(d_r);
+    a.frames = (tokens + a.m.frame - 1) / a.m.frame;
+    a.dn = d_dn; a.dr = d_dr; a.dx = d_dx; a.dy = d_dy;
+    a.dgate = d_dgate; a.dscale = d_dscale; a.dshift = d_dshift;
+    a.dweight = d_dweight; a.dpost_weight = d_dpost_weight;
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(d_workspace) + lay.parts);
+    a.weight_parts = reinterpret_cast<float*>(static_cast<uint8_t*>(d_workspace) + lay.weight_parts);
+    return account(ctx, modulate_backward(a, ctx->cfg.io_dtype, (c->flags & ARL2_MODULATION_FP32_RESIDUAL) != 0, as_stream(stream)));
+}
+
+int arl2_rotate(arl2_ctx* ctx, const arl2_rotation_config* c, const float* d_rope_cos, const float* d_rope_sin, int32_t tokens, const arl2_rows* q,
+                const arl2_rows* k, const int32_t* d_start, const int32_t* d_positions, const float* d_q_weight, const float* d_k_weight,
+                void* d_q_out, void* d_k_out, void* stream)
+{
+    const bool with_k = k != nullptr && k->data != nullptr;
+    RotateArgs a;
+    if (!rotate_args("rotate", ctx, c, d_rope_cos, d_rope_sin, tokens, q, k, with_k, true, d_start, d_positions, d_q_weight, d_k_weight, a)) return ARL2_ERR_INVALID_ARG;
+    if (d_q_out == nullptr || (d_k_out != nullptr) != with_k) { set_error("rotate: q_out, and with k also k_out (else not), must be given"); return ARL2_ERR_INVALID_ARG; }
+    if (!aligned16({d_q_out, d_k_out})) { set_error("rotate: outputs must be 16-byte aligned"); return ARL2_ERR_INVALID_ARG; }
+    if (outputs_meet("rotate", {d_q_out, d_k_out})) return ARL2_ERR_INVALID_ARG;
+    const int64_t q_row = (int64_t)a.q_vecs * 8, k_row = (int64_t)(a.vecs - a.q_vecs) * 8;
+    auto packed = [&](int64_t batch, int64_t token, int64_t row) { return (a.T == 1 || token == row) && (a.B == 1 || batch == row * a.T); };
+    if ((d_q_out == a.q && !packed(a.q_batch, a.q_token, q_row)) || (with_k && (d_k_out == a.q || d_q_out == a.k || (d_k_out == a.k && !packed(a.k_batch, a.k_token, k_row))))) {
+        set_error("rotate: an output may be its own input where that is contiguous, and no other");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    a.q_out = d_q_out; a.k_out = d_k_out;
+    return account(ctx, rotate(a, ctx->cfg.io_dtype, as_stream(stream)));
+}
+
+size_t arl2_rotation_workspace_bytes(const arl2_config* cfg, const arl2_rotation_config* c, int32_t tokens)
+{
+    if (!valid_config(cfg) || !valid_rotation(cfg, c) || !check_tokens("rotation_workspace_bytes", *cfg, tokens)) return 0;
+    const size_t n = rotation_workspace(*cfg, *c, tokens);
+    return n > 0 ? n : kAlign;     // (0 says that the configuration is invalid)
+}
+
+int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* c, const float* d_rope_cos, const float* d_rope_sin, int32_t tokens,
+                         const void* d_dq_out, const void* d_dk_out, const arl2_rows* q, const arl2_rows* k, const int32_t* d_start,
+                         const int32_t* d_positions, const float* d_q_weight, const float* d_k_weight, void* d_dq, void* d_dk,
+                         float* d_dq_weight, float* d_dk_weight, void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    const bool with_k = d_dk_out != nullptr;
+    RotateBackArgs a = {};
+    if (!rotate_args("rotate_backward", ctx, c, d_rope_cos, d_rope_sin, tokens, q, k, with_k, c != nullptr && c->norm != ARL2_NORM_NONE, d_start, d_positions,
+                     d_q_weight, d_k_weight, a.r))
+        return ARL2_ERR_INVALID_ARG;
+    if (d_dq_out == nullptr || d_dq == nullptr || (d_dk != nullptr) != with_k) {
+        set_error("rotate_backward: dq_out and dq, and with dk_out also dk (else not), must be given");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    const bool weights = c->norm == ARL2_NORM_TOKEN || c->norm == ARL2_NORM_HEAD;
+    if ((!weights && (d_dq_weight != nullptr || d_dk_weight != nullptr)) || (!with_k && d_dk_weight != nullptr)) {
+        set_error("rotate_backward: a gradient of weights that there are none of");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (!aligned16({d_dq_out, d_dk_out, d_dq, d_dk, d_dq_weight, d_dk_weight})) { set_error("rotate_backward: tensors must be 16-byte aligned"); return ARL2_ERR_INVALID_ARG; }
+    if (outputs_meet("rotate_backward", {d_dq, d_dk, d_dq_weight, d_dk_weight})) return ARL2_ERR_INVALID_ARG;
+    const bool reads_x = c->norm != ARL2_NORM_NONE;
+    if ((with_k && (d_dq == d_dk_out || d_dk == d_dq_out)) || (reads_x && (d_dq == a.r.q || d_dq == a.r.k || (with_k && (d_dk == a.r.q || d_dk == a.r.k))))) {
+        set_error("rotate_backward: an output may be the gradient that it is made from, and no other input");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if ((d_dq_weight != nullptr || d_dk_weight != nullptr) && !check_workspace("rotate_backward", d_workspace, workspace_bytes, rotation_workspace(ctx->cfg, *c, tokens)))
+        return ARL2_ERR_WORKSPACE;
+    a.dq_out = d_dq_out; a.dk_out = d_dk_out;
+    a.dq = d_dq; a.dk = d_dk;
+    a.dq_weight = d_dq_weight; a.dk_weight = d_dk_weight;
+    a.parts = static_cast<float*>(d_workspace);
+    return account(ctx, rotate_backward(a, ctx->cfg.io_dtype, as_stream(stream)));
+}
 
 uint64_t arl2_launch_count(const arl2_ctx* ctx) { return ctx ? ctx->launches : 0; }
 

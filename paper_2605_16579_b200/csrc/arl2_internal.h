@@ -260,6 +260,72 @@ int cache_attend(CacheAttendArgs a, int dtype, cudaStream_t st);
 // attention by tcgen05: bf16 I/O, many rows
 int tc_cache_attend(const CacheAttendArgs& a, cudaStream_t st);
 
+// ---- what stands around the core in a block (arl2_block.cu) --------------------------------
+enum RowNorm : int { kNormNone = ARL2_NORM_NONE, kNormLayer = ARL2_NORM_LAYER, kNormRms = ARL2_NORM_RMS, kNormToken = ARL2_NORM_TOKEN,
+                     kNormHead = ARL2_NORM_HEAD, kNormLength = ARL2_NORM_LENGTH };
+constexpr int kBlockMostChannels = 8192;   // of a row of the modulation; twice as many for queries and keys together
+// Runs of rows whose sums over tokens have room in a workspace: `teams` per CTA (block_teams) of at most four CTAs per SM of 148
+constexpr int block_teams(int vecs) { return (vecs + 31) / 32 >= 8 ? 1 : 8 / ((vecs + 31) / 32); }
+constexpr int block_runs(int vecs) { return 4 * 148 * block_teams(vecs); }
+struct FrameRows {           // a row of d channels per frame, fp32; nullptr: none
+    const float* p;
+    int64_t batch, frame;    // strides in elements
+};
+struct ModulateArgs {
+    int B, T, d, rows;       // rows = B * T
+    int frame;               // tokens that share a row of gate, scale and shift
+    int norm, post_norm;
+    float eps;
+    const void* x;           // [B, T, d]
+    const void* y;           // or nullptr
+    FrameRows gate, scale, shift;
+    const float* weight;     // [d] or nullptr
+    const float* post_weight;
+    void* r;                 // the residual with y added (the backward pass reads it)
+    void* n;                 // or nullptr
+    int share = 0;           // rows per run (set by the launcher)
+};
+struct ModulateBackArgs {
+    ModulateArgs m;
+    int frames;              // per stream
+    const void* dn;          // or nullptr
+    const void* dr;          // or nullptr
+    void* dx;
+    void* dy;
+    float *dgate, *dscale, *dshift;      // [B, frames, d], each may be nullptr
+    float *dweight, *dpost_weight;       // [d], each may be nullptr
+    float* parts;            // [2 * runs, 3, d]
+    float* weight_parts;     // [runs, 2, d]
+};
+struct RotateArgs {
+    int B, T, D, rows;
+    int q_vecs, vecs;        // groups of eight channels of a token's queries, and of both
+    int norm;
+    float eps, q_over, k_over;   // sums of squares are multiplied with these
+    const float *cos, *sin;  // [rope_rows, D/2]
+    int rope_rows, pairs[3];
+    int grid_rows, grid_columns;
+    const int32_t* start;    // [B] or nullptr
+    const int32_t* positions;    // [B, T, 3] or nullptr
+    const void *q, *k;
+    int64_t q_batch, q_token, k_batch, k_token;
+    const float *q_weight, *k_weight;
+    void *q_out, *k_out;
+    uint32_t* status;
+    int share = 0;
+};
+struct RotateBackArgs {
+    RotateArgs r;
+    const void *dq_out, *dk_out;
+    void *dq, *dk;
+    float *dq_weight, *dk_weight;
+    float* parts;            // [runs, vecs * 8]
+};
+int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st);
+int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st);
+int rotate(const RotateArgs& a, int dtype, cudaStream_t st);
+int rotate_backward(const RotateBackArgs& a, int dtype, cudaStream_t st);
+
 void set_error(const char* fmt, ...);
 
 // Nearly every kernel of a call goes out with programmatic stream serialisation: it may become resident while the kernel
@@ -292,11 +358,11 @@ inline size_t even_spread_smem(int need, int per_sm)
     return (size_t)(share > need ? share : need);
 }
 template <typename... P, typename... A>
-cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, A... args)
+cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int cluster, dim3 threads, size_t smem, cudaStream_t st, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
+    cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -315,7 +381,12 @@ cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int cluster, int thr
 template <typename... P, typename... A>
 cudaError_t launch_kernel(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args)
 {
-    return launch_cluster(kernel, grid, 1, threads, smem, st, args...);
+    return launch_cluster(kernel, grid, 1, dim3((unsigned)threads), smem, st, args...);
+}
+template <typename... P, typename... A>
+cudaError_t launch_block(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args)
+{
+    return launch_cluster(kernel, grid, 1, block, smem, st, args...);
 }
 
 }  // namespace arl2
