@@ -459,6 +459,39 @@ int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* cfg, const f
                          const int32_t* d_positions, const float* d_q_weight, const float* d_k_weight, void* d_dq, void* d_dk,
                          float* d_dq_weight, float* d_dk_weight, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The recurrence over the blocks of a whole sequence, its first ceil(tokens / block_tokens) blocks of block_tokens tokens each (the last may have
+ * fewer), for training the remembering branch or for going through many known blocks at once:
+ *   out[b,i,h,:] = q[b,i,h,:] S_n  for the tokens i of block n,   S_{n+1} = sigmoid(a[b,n,h]) S_n + sum over them of k^T v
+ * -- the readout and the gated-linear commit of the layer (Eq. 4, 5, 8), block after block, on features that the caller has made (ARL2_NORM_LENGTH
+ * of arl2_rotate gives rows of length one).
+ *   q, k, v  [B, tokens, H, D] of the I/O type (arl2_rows);  d_decay_logits [B, blocks, H] fp32
+ *   d_state_in   S_0, [B, H, D, D] fp32, or NULL: 0;  d_state_out the state behind the last block, or NULL; may be d_state_in.  (The
+ *                context's own state is set by arl2_set_state, not here.)
+ *   d_out    [B, tokens, H, D] contiguous, 16-byte aligned
+ * bf16 I/O: operands of the matrix products are bf16, the states as two bf16 numbers (2^-17), fp32 accumulation, fp32 states; fp32 I/O: products to
+ * 2^-21 (each operand as two TF32 numbers).  The workspace (256-byte aligned) holds nothing between calls; it has a state of 4 D^2 bytes
+ * for each block and head, and as many sums (short blocks of long sequences want much of it).
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t block_tokens;  /* >= 1 */
+} arl2_recurrence_config;
+size_t arl2_recurrence_workspace_bytes(const arl2_config* cfg, const arl2_recurrence_config* recurrence_cfg, int32_t tokens, int32_t backward);
+int arl2_recur(arl2_ctx* ctx, const arl2_recurrence_config* cfg, int32_t tokens, const arl2_rows* q, const arl2_rows* k, const arl2_rows* v,
+               const float* d_decay_logits, const float* d_state_in, void* d_out, float* d_state_out, void* d_workspace,
+               size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass, from d_dout [B, tokens, H, D] (contiguous) and d_dstate_out, the gradient of the state behind the last block (NULL: 0):
+ * d_dq, d_dk, d_dv like d_out;  d_ddecay_logits like the logits, or NULL;  d_dstate_in the gradient of S_0, or NULL; may be d_dstate_out.
+ * It makes the states again from k and v.  The workspace is that of backward != 0.
+ */
+int arl2_recur_backward(arl2_ctx* ctx, const arl2_recurrence_config* cfg, int32_t tokens, const void* d_dout, const arl2_rows* q, const arl2_rows* k,
+                        const arl2_rows* v, const float* d_decay_logits, const float* d_state_in, const float* d_dstate_out, void* d_dq,
+                        void* d_dk, void* d_dv, float* d_ddecay_logits, float* d_dstate_in, void* d_workspace, size_t workspace_bytes,
+                        void* stream);
+
 /* S <- 0 for stream `stream_index` (0..B-1) or all streams (-1): Algorithm 1, first line. */
 int arl2_reset(arl2_ctx* ctx, int32_t stream_index, void* stream);
 

@@ -38,6 +38,7 @@ EXPORTS = (
     "arl2_cache_page_bytes", "arl2_cache_workspace_bytes", "arl2_cache_least_workspace_bytes", "arl2_cache_create", "arl2_cache_set_workspace",
     "arl2_cache_append", "arl2_cache_attend", "arl2_cache_destroy",
     "arl2_modulate", "arl2_modulate_backward", "arl2_modulation_workspace_bytes", "arl2_rotate", "arl2_rotate_backward", "arl2_rotation_workspace_bytes",
+    "arl2_recurrence_workspace_bytes", "arl2_recur", "arl2_recur_backward",
 )
 
 
@@ -79,6 +80,10 @@ class arl2_rotation_config(ctypes.Structure):
         ("struct_size", ctypes.c_uint32), ("kv_heads", ctypes.c_int32), ("rope_rows", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * 3),
         ("grid_rows", ctypes.c_int32), ("grid_columns", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
     ]
+
+
+class arl2_recurrence_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("block_tokens", ctypes.c_int32)]
 
 
 _lib = None
@@ -176,6 +181,13 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.arl2_rotate.argtypes = [vp, tp, vp, vp, i32, rp, rp, vp, vp, vp, vp, vp, vp, vp]
     lib.arl2_rotate_backward.restype = ctypes.c_int
     lib.arl2_rotate_backward.argtypes = [vp, tp, vp, vp, i32, vp, vp, rp, rp] + [vp] * 9 + [ctypes.c_size_t, vp]
+    ep = ctypes.POINTER(arl2_recurrence_config)
+    lib.arl2_recurrence_workspace_bytes.restype = ctypes.c_size_t
+    lib.arl2_recurrence_workspace_bytes.argtypes = [cp, ep, i32, i32]
+    lib.arl2_recur.restype = ctypes.c_int
+    lib.arl2_recur.argtypes = [vp, ep, i32, rp, rp, rp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.arl2_recur_backward.restype = ctypes.c_int
+    lib.arl2_recur_backward.argtypes = [vp, ep, i32, vp, rp, rp, rp] + [vp] * 9 + [ctypes.c_size_t, vp]
     lib.arl2_launch_count.restype = ctypes.c_uint64
     lib.arl2_launch_count.argtypes = [vp]
     lib.arl2_step_kernel_name.restype = ctypes.c_char_p
@@ -867,6 +879,63 @@ class Rotation(_BlockOp):
                   *self._where(start, positions, tokens), q_w, k_w, dq.data_ptr(), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight), _ptr(ws),
                   0 if ws is None else ws.numel())
         return dq, dk, dq_weight, dk_weight
+
+class Recurrence(_BlockOp):
+    """The state over the blocks of a whole sequence (arl2_recur): out_i = q_i S_n for the tokens i of block n of ``block_tokens`` tokens,
+    S_{n+1} = sigmoid(a_n) S_n + K_n^T V_n.  Reads and sets no state of the layer."""
+
+    def __init__(self, layer, block_tokens):
+        super().__init__(layer)
+        self.block_tokens = block_tokens
+        self.cfg = arl2_recurrence_config(ctypes.sizeof(arl2_recurrence_config), block_tokens)
+        self._cfg = ctypes.byref(self.cfg)
+        self.workspace_bytes(1)
+
+    def workspace_bytes(self, tokens, backward=False):
+        n = self._lib.arl2_recurrence_workspace_bytes(ctypes.byref(self.layer.cfg), self._cfg, tokens, backward)
+        if n == 0:
+            raise Arl2Error("arl2_recurrence_workspace_bytes: " + self._lib.arl2_last_error().decode())
+        return n
+
+    def _inputs(self, q, k, v, decay_logits, state):
+        tokens = self._tokens(q, "q", 4)
+        shape = (self._B, tokens, self._H, self._D)
+        rows = [self._strided(t, shape, self.dtype, what, 2) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
+        self.layer._want(decay_logits, (self._B, -(-tokens // self.block_tokens), self._H), torch.float32, "decay_logits")
+        self._state(state, "state")
+        return tokens, shape, rows
+
+    def _state(self, t, what):
+        if t is not None:
+            self.layer._want(t, (self._B, self._H, self._D, self._D), torch.float32, what)
+
+    def forward(self, q, k, v, decay_logits, state=None, final=True, out=None, workspace=None):
+        """q, k, v [B, T, H, D] (heads and channels contiguous), decay_logits fp32 [B, ceil(T / block_tokens), H], state fp32 [B, H, D, D] or None
+        (zeros) -> (out [B, T, H, D], the state behind the last block, or None with ``final=False``)."""
+        tokens, shape, rows = self._inputs(q, k, v, decay_logits, state)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        else:
+            self.layer._want(out, shape, self.dtype, "out")
+        last = torch.empty(self._B, self._H, self._D, self._D, dtype=torch.float32, device=self.device) if final else None
+        ws = self._scratch(self.workspace_bytes(tokens), workspace)
+        self._run(self._lib.arl2_recur, self._cfg, tokens, *rows, decay_logits.data_ptr(), _ptr(state), out.data_ptr(), _ptr(last), ws.data_ptr(), ws.numel())
+        return out, last
+
+    def backward(self, dout, q, k, v, decay_logits, state=None, dstate=None, initial=True, workspace=None):
+        """Gradients (dq, dk, dv, ddecay_logits, the gradient of ``state``) from dout [B, T, H, D] and dstate, that of the state behind the last
+        block (None: zeros); the last is None with ``initial=False``."""
+        tokens, shape, rows = self._inputs(q, k, v, decay_logits, state)
+        self.layer._want(dout, shape, self.dtype, "dout")
+        self._state(dstate, "dstate")
+        dq, dk, dv = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout)
+        ddecay = torch.empty_like(decay_logits)
+        first = torch.empty(self._B, self._H, self._D, self._D, dtype=torch.float32, device=self.device) if initial else None
+        ws = self._scratch(self.workspace_bytes(tokens, True), workspace)
+        self._run(self._lib.arl2_recur_backward, self._cfg, tokens, dout.data_ptr(), *rows, decay_logits.data_ptr(), _ptr(state), _ptr(dstate),
+                  dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ddecay.data_ptr(), _ptr(first), ws.data_ptr(), ws.numel())
+        return dq, dk, dv, ddecay, first
+
 
 
 STATIC_SCRATCH_BYTES = 8 << 20

@@ -1687,6 +1687,144 @@ int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* c, const flo
     return account(ctx, rotate_backward(a, ctx->cfg.io_dtype, as_stream(stream)));
 }
 
+// ---- the recurrence over the blocks of a sequence -------------------------------------------------------------
+namespace {
+
+bool recur_tensor_cores(const arl2_config& c) { return c.io_dtype == ARL2_BF16 && !(c.flags & ARL2_FLAG_FORCE_SIMT); }
+
+bool valid_recurrence(const char* who, const arl2_config& cfg, const arl2_recurrence_config* c, int32_t tokens)
+{
+    if (c == nullptr) { set_error("recurrence config is NULL"); return false; }
+    if (c->struct_size != sizeof(arl2_recurrence_config)) {
+        set_error("recurrence config.struct_size is %u, this library expects %zu", c->struct_size, sizeof(arl2_recurrence_config));
+        return false;
+    }
+    if (c->block_tokens < 1) { set_error("block_tokens must be >= 1 (got %d)", c->block_tokens); return false; }
+    if (!check_tokens(who, cfg, tokens)) return false;
+    // tiles of three products, of whole blocks and of the shorter one
+    const int64_t block = c->block_tokens < tokens ? c->block_tokens : tokens, tiles = (tokens + block - 1) / block * ((block + kRecurTile - 1) / kRecurTile);
+    if (tiles * cfg.B * cfg.H * 3 >= ((int64_t)1 << 30)) { set_error("%s: too many blocks", who); return false; }
+    return true;
+}
+
+struct RecurLayout { size_t slots, states, dstates, beside, dots, total; };
+RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c, int32_t tokens, bool back)
+{
+    const bool tc = recur_tensor_cores(cfg);
+    const size_t pair = tc && cfg.D == 64 ? 2 : 1, heads = (cfg.H + pair - 1) / pair, dd = (size_t)cfg.D * cfg.D;
+    const size_t blocks = (size_t)(((int64_t)tokens + c.block_tokens - 1) / c.block_tokens), units = cfg.B * heads * blocks;
+    const size_t state = align_up(units * pair * dd * sizeof(float));      // (as two bf16 numbers it takes the same room)
+    RecurLayout l;
+    size_t off = 0;
+    l.slots = off;   off += align_up((units * (back ? 2 : 1) + kRecurCtas) * pair * dd * sizeof(float));
+    l.states = off;  off += state;
+    l.dstates = off; off += back ? state : 0;
+    l.beside = off;  off += back && tc ? state : 0;
+    l.dots = off;    off += back ? align_up((size_t)cfg.B * cfg.H * blocks * (dd / 128) * sizeof(float)) : 0;
+    l.total = off;
+    return l;
+}
+
+// What both directions check and fill in.
+int recur_args(const char* who, arl2_ctx* ctx, const arl2_recurrence_config* c, int32_t tokens, const arl2_rows* q, const arl2_rows* k, const arl2_rows* v,
+               const float* decay, const float* state_in, const void* dout, bool back, void* ws, size_t bytes, RecurArgs& a, bool& tc)
+{
+    if (!check_ctx(ctx) || !valid_recurrence(who, ctx->cfg, c, tokens)) return ARL2_ERR_INVALID_ARG;
+    const arl2_config& cfg = ctx->cfg;
+    const int elem = cfg.io_dtype == ARL2_FP32 ? 4 : 2;
+    for (const arl2_rows* r : {q, k, v})
+        if (r == nullptr || r->data == nullptr) { set_error("%s: q, k and v must not be NULL", who); return ARL2_ERR_INVALID_ARG; }
+    if (decay == nullptr) { set_error("%s: decay_logits must not be NULL", who); return ARL2_ERR_INVALID_ARG; }
+    if (!check_rows(who, q, elem) || !check_rows(who, k, elem) || !check_rows(who, v, elem)) return ARL2_ERR_INVALID_ARG;
+    if (!aligned16({state_in, dout}) || reinterpret_cast<uintptr_t>(decay) % 4 != 0) {
+        set_error("%s: tensors must be 16-byte, decay_logits 4-byte aligned", who);
+        return ARL2_ERR_INVALID_ARG;
+    }
+    const RecurLayout lay = recur_layout(cfg, *c, tokens, back);
+    if (!check_workspace(who, ws, bytes, lay.total)) return ARL2_ERR_WORKSPACE;
+    a = RecurArgs{};
+    a.B = cfg.B; a.H = cfg.H; a.D = cfg.D; a.T = tokens;
+    a.block = c->block_tokens < tokens ? c->block_tokens : tokens;
+    a.N = (tokens + a.block - 1) / a.block;
+    a.back = back;
+    auto rows = [](const arl2_rows* r) { return RecurRows{r->data, r->batch_stride, r->row_stride}; };
+    a.q = rows(q); a.k = rows(k); a.v = rows(v);
+    a.dout = RecurRows{dout, (int64_t)tokens * cfg.H * cfg.D, (int64_t)cfg.H * cfg.D};
+    a.decay = decay; a.state_in = state_in;
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    a.pair = cfg.D == 64 ? 2 : 1;
+    tc = recur_tensor_cores(cfg) && tc_recur_supported(a);
+    a.slots = reinterpret_cast<float*>(w + lay.slots);
+    if (tc) {
+        a.states_op = reinterpret_cast<__nv_bfloat16*>(w + lay.states);
+        a.dstates_op = back ? reinterpret_cast<__nv_bfloat16*>(w + lay.dstates) : nullptr;
+        a.states = back ? reinterpret_cast<float*>(w + lay.beside) : nullptr;
+    } else {
+        a.pair = 1;
+        a.states = reinterpret_cast<float*>(w + lay.states);
+        a.dstates = back ? reinterpret_cast<float*>(w + lay.dstates) : nullptr;
+    }
+    a.dots = back ? reinterpret_cast<float*>(w + lay.dots) : nullptr;
+    a.status = reinterpret_cast<uint32_t*>(ctx->ws + ctx->lay.status);
+    a.wait_limit = ctx->wait_limit;
+    return ARL2_OK;
+}
+
+}  // namespace
+
+size_t arl2_recurrence_workspace_bytes(const arl2_config* cfg, const arl2_recurrence_config* c, int32_t tokens, int32_t backward)
+{
+    if (!valid_config(cfg) || !valid_recurrence("recurrence_workspace_bytes", *cfg, c, tokens)) return 0;
+    return recur_layout(*cfg, *c, tokens, backward != 0).total;
+}
+
+int arl2_recur(arl2_ctx* ctx, const arl2_recurrence_config* c, int32_t tokens, const arl2_rows* q, const arl2_rows* k, const arl2_rows* v,
+               const float* d_decay_logits, const float* d_state_in, void* d_out, float* d_state_out, void* d_workspace, size_t workspace_bytes,
+               void* stream)
+{
+    RecurArgs a;
+    bool tc;
+    const int r = recur_args("recur", ctx, c, tokens, q, k, v, d_decay_logits, d_state_in, nullptr, false, d_workspace, workspace_bytes, a, tc);
+    if (r != ARL2_OK) return r;
+    if (d_out == nullptr || !aligned16({d_out, d_state_out})) { set_error("recur: out must be given, outputs 16-byte aligned"); return ARL2_ERR_INVALID_ARG; }
+    if (d_out == a.q.p || d_out == a.k.p || d_out == a.v.p || d_out == d_state_in || d_out == d_state_out || (d_state_out != nullptr && d_state_out == d_decay_logits)) {
+        set_error("recur: out must not alias an input or state_out");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    a.out = d_out;
+    a.state_out = d_state_out;
+    recur_plan(a);
+    return account(ctx, recur(a, ctx->cfg.io_dtype, tc, as_stream(stream)));
+}
+
+int arl2_recur_backward(arl2_ctx* ctx, const arl2_recurrence_config* c, int32_t tokens, const void* d_dout, const arl2_rows* q, const arl2_rows* k,
+                        const arl2_rows* v, const float* d_decay_logits, const float* d_state_in, const float* d_dstate_out, void* d_dq, void* d_dk,
+                        void* d_dv, float* d_ddecay_logits, float* d_dstate_in, void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    RecurArgs a;
+    bool tc;
+    const int r = recur_args("recur_backward", ctx, c, tokens, q, k, v, d_decay_logits, d_state_in, d_dout, true, d_workspace, workspace_bytes, a, tc);
+    if (r != ARL2_OK) return r;
+    if (d_dout == nullptr || d_dq == nullptr || d_dk == nullptr || d_dv == nullptr) { set_error("recur_backward: dout, dq, dk and dv must not be NULL"); return ARL2_ERR_INVALID_ARG; }
+    if (!aligned16({d_dstate_out, d_dq, d_dk, d_dv, d_dstate_in}) || reinterpret_cast<uintptr_t>(d_ddecay_logits) % 4 != 0) {
+        set_error("recur_backward: tensors must be 16-byte, ddecay_logits 4-byte aligned");
+        return ARL2_ERR_INVALID_ARG;
+    }
+    if (outputs_meet("recur_backward", {d_dq, d_dk, d_dv, d_ddecay_logits, d_dstate_in})) return ARL2_ERR_INVALID_ARG;
+    for (const void* out : {(const void*)d_dq, (const void*)d_dk, (const void*)d_dv, (const void*)d_ddecay_logits, (const void*)d_dstate_in})
+        for (const void* in : {a.q.p, a.k.p, a.v.p, d_dout, (const void*)d_decay_logits, (const void*)d_state_in, (const void*)d_dstate_out})
+            if (out != nullptr && out == in && !(out == d_dstate_in && in == d_dstate_out)) {
+                set_error("recur_backward: an output must not alias an input (dstate_in may be dstate_out)");
+                return ARL2_ERR_INVALID_ARG;
+            }
+    a.dstate_out = d_dstate_out;
+    a.dq = d_dq; a.dk = d_dk; a.dv = d_dv;
+    a.ddecay = d_ddecay_logits;
+    a.dstate_in = d_dstate_in;
+    recur_plan(a);
+    return account(ctx, recur(a, ctx->cfg.io_dtype, tc, as_stream(stream)));
+}
+
 uint64_t arl2_launch_count(const arl2_ctx* ctx) { return ctx ? ctx->launches : 0; }
 
 const char* arl2_step_kernel_name(const arl2_ctx* ctx)

@@ -326,6 +326,86 @@ int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStrea
 int rotate(const RotateArgs& a, int dtype, cudaStream_t st);
 int rotate_backward(const RotateBackArgs& a, int dtype, cudaStream_t st);
 
+// ---- the recurrence over the blocks of a sequence (arl2_recur.cu, arl2_tc_recur.cu) ------------
+// Three steps: sums over the tokens of a block (K^T V; backward also Q^T dO), the scan over the blocks, and rows times the
+// states (Q S; backward dO S^T, V D^T, K D).  The first and the last go over tiles of up to 128 tokens of a unit, which is one block of a
+// head (of two heads side by side where D = 64 and tensor cores do it).  Units of equal length are a job; the tiles of all jobs
+// of a step form one sequence, cut into equal runs, one for each CTA.
+constexpr int kRecurTile = 128;
+struct RecurJob {
+    int tile0, unit0;        // where this job's tiles and units begin in the step's sequence
+    int ntile, len;          // tiles of a unit, tokens of a unit
+    int n0, n_count;         // blocks n0 .. n0 + n_count - 1 of each head
+    int which;               // the pair of operands (sums), or the product (rows times states)
+    int part;                // 0: blocks of full length; 1: the shorter last one
+};
+constexpr int kRecurJobs = 6;
+struct RecurStep {
+    RecurJob job[kRecurJobs];
+    int jobs, tiles, units;
+    int share, ctas;         // tiles of a CTA, CTAs
+};
+struct RecurRows {           // [B, T, H, D] of the I/O type
+    const void* p;
+    int64_t batch, token;    // strides in elements
+};
+// Where tile g of a step is
+struct RecurAt { int job, unit, tile, b, head, n; };   // unit: within the step; head: the unit's first
+__device__ __forceinline__ RecurAt recur_at(const RecurStep& s, int g, int heads, int pair)
+{
+    RecurAt r;
+    r.job = 0;
+    while (r.job + 1 < s.jobs && g >= s.job[r.job + 1].tile0) ++r.job;
+    const RecurJob& j = s.job[r.job];
+    const int v = (g - j.tile0) / j.ntile;
+    r.tile = g - j.tile0 - v * j.ntile;
+    r.unit = j.unit0 + v;
+    const int bh = v / j.n_count;
+    r.n = j.n0 + v - bh * j.n_count;
+    r.b = bh / heads;
+    r.head = (bh - r.b * heads) * pair;
+    return r;
+}
+inline void recur_cut(RecurStep& s, int ctas)
+{
+    s.share = (s.tiles + ctas - 1) / ctas;
+    if (s.share < 1) s.share = 1;
+    s.ctas = (s.tiles + s.share - 1) / s.share;
+}
+struct RecurArgs {
+    int B, H, D, T;
+    int block, N;            // tokens of a block (the last may have fewer), blocks
+    int pair;                // heads of a unit
+    bool back;
+    RecurRows q, k, v, dout; // dout contiguous
+    const float* decay;      // [B, N, H] logits
+    const float* state_in;   // [B, H, D, D] or nullptr = 0
+    float* state_out;        // ... or nullptr
+    const float* dstate_out;
+    float* dstate_in;
+    void *out, *dq, *dk, *dv;
+    float* ddecay;           // [B, N, H]
+    // scratch
+    float* slots;            // [units + CTAs of the sums, pair, D, D]: the part of unit u that CTA c made is at u + c
+    float* states;           // [B, H / pair up, N, pair, D, D] fp32: state before block n
+    float* dstates;          // ... and the gradient of the state after block n
+    __nv_bfloat16* states_op;    // the same as a bf16 head and a bf16 remainder, [.., pair, 2, D, D] (tensor cores)
+    __nv_bfloat16* dstates_op;
+    float* dots;             // [B, H, N, D * D / 128]: parts of <dstate, state>
+    uint32_t* status;
+    uint32_t wait_limit;
+    RecurStep sums, rows;
+};
+__host__ __device__ inline int recur_heads(const RecurArgs& a) { return (a.H + a.pair - 1) / a.pair; }
+int recur(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st);
+// whether the tensors can be read by tiled copies
+bool tc_recur_supported(const RecurArgs& a);
+int tc_recur_sums(RecurArgs& a, cudaStream_t st);
+int tc_recur_rows(RecurArgs& a, cudaStream_t st);
+// fills in the steps' jobs; the launchers cut them into runs, the sums for at most kRecurCtas CTAs
+void recur_plan(RecurArgs& a);
+constexpr int kRecurCtas = 4 * 148;
+
 void set_error(const char* fmt, ...);
 
 // Nearly every kernel of a call goes out with programmatic stream serialisation: it may become resident while the kernel

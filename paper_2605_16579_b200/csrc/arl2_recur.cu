@@ -1,0 +1,538 @@
+// The recurrence over the blocks of a whole sequence, and its backward pass:
+//   o_i = q_i S_n for the tokens i of block n,   S_{n+1} = alpha_n S_n + K_n^T V_n,   alpha_n = sigmoid(a_n);
+//   D_N = dS_out, D_n = alpha_n D_{n+1} + Q_n^T dO_n (D_n: gradient of S_n);
+//   dq = dO S_n^T, dk = V D_{n+1}^T, dv = K D_{n+1}, da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n>, dS_in = D_0.
+// The sums over a block's tokens do not depend on the state, so only the scan over the blocks is sequential, and it is a few
+// operations per element of the states.  Three steps (arl2_internal.h): sums, scan, rows times states.
+//
+// This file has the scan, and sums and rows for fp32 I/O (and bf16 without tensor memory): warp-level matrix instructions on
+// TF32 numbers.  A fp32 operand is taken as a head of 11 bits and a remainder of 11 more, three products (remainder times remainder
+// left out): off by 2^-22 of each product; bf16 inputs are exact in the head alone.  fp32 accumulation.
+#include <algorithm>
+#include <atomic>
+
+#include "row_common.cuh"
+
+namespace arl2 {
+namespace {
+
+constexpr int kMaxDev = 64;
+constexpr int kRThreads = 256;
+
+__device__ __forceinline__ float gate_of(float logit) { return 1.0f / (1.0f + expf(-logit)); }
+
+// ---- TF32 fragments ------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t tf32_head(float x)
+{
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+    return r;
+}
+template <bool kExact> struct Tf32 { uint32_t h, l; };
+template <bool kExact>
+__device__ __forceinline__ Tf32<kExact> tf32_split(float x)
+{
+    Tf32<kExact> r;
+    if (kExact) {
+        r.h = __float_as_uint(x);
+        r.l = 0;
+    } else {
+        r.h = tf32_head(x);
+        // (an infinity has no remainder)
+        const float rem = x - __uint_as_float(r.h);
+        r.l = tf32_head(fabsf(x) <= 3.0e38f ? rem : 0.0f);
+    }
+    return r;
+}
+__device__ __forceinline__ void tf32_mma(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p)
+{
+    if (sizeof(T) == 4) return *reinterpret_cast<const float4*>(p);
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
+}
+
+// ---- sums: X^T Y over the tokens of a unit -------------------------------------------------------------
+// A warp has a block of the D x D result; 32 tokens at a time through shared memory, rows padded so that the fragments' reads
+// fall on different banks; the next tokens are on their way in registers meanwhile.
+constexpr int kSumTokens = 32;
+template <int D> constexpr int sum_smem() { return 2 * kSumTokens * (D + 8) * 4; }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_constant__ RecurArgs a)
+{
+    constexpr bool kExact = sizeof(T) == 2;
+    constexpr int kLd = D + 8, kM = D / 64, kN = D / 16;      // m16 and n8 tiles of a warp: four warps down, two across
+    constexpr int kLoads = kSumTokens * D / 4 / kRThreads;     // of four channels, per operand and thread
+    extern __shared__ float smem[];
+    float* xs = smem;
+    float* ys = smem + kSumTokens * kLd;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int m0 = (warp >> 1) * kM * 16, n0 = (warp & 1) * kN * 8;
+    const int first = blockIdx.x * a.sums.share, last = min(first + a.sums.share, a.sums.tiles);
+    grid_dependency_sync();
+
+    float acc[kM][kN][4];
+    float4 xr[kLoads], yr[kLoads];
+    RecurAt at;
+    int tokens = 0;            // of the tile
+    const T *x = nullptr, *y = nullptr;
+    int64_t x_step = 0, y_step = 0;
+    auto enter = [&](int tile) {
+        at = recur_at(a.sums, tile, recur_heads(a), a.pair);
+        const RecurJob& j = a.sums.job[at.job];
+        tokens = min(kRecurTile, j.len - at.tile * kRecurTile);
+        const RecurRows& rx = j.which == 0 ? a.k : a.q;
+        const RecurRows& ry = j.which == 0 ? a.v : a.dout;
+        const int64_t token = (int64_t)at.n * a.block + at.tile * kRecurTile;
+        x = static_cast<const T*>(rx.p) + at.b * rx.batch + token * rx.token + at.head * D;
+        y = static_cast<const T*>(ry.p) + at.b * ry.batch + token * ry.token + at.head * D;
+        x_step = rx.token;
+        y_step = ry.token;
+    };
+    auto fetch = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int e = tid + i * kRThreads, row = from + e / (D / 4), c = e % (D / 4) * 4;
+            xr[i] = yr[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (row < tokens) {
+                xr[i] = load4(x + row * x_step + c);
+                yr[i] = load4(y + row * y_step + c);
+            }
+        }
+    };
+    if (first >= last) return;
+    enter(first);
+    fetch(0);
+    bool fresh = true;
+    for (int tile = first; tile < last; ++tile) {
+        if (fresh) {
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+            fresh = false;
+        }
+        const RecurAt here = at;
+        const int steps = (tokens + kSumTokens - 1) / kSumTokens;
+        for (int s = 0; s < steps; ++s) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int e = tid + i * kRThreads, at_s = e / (D / 4) * kLd + e % (D / 4) * 4;
+                *reinterpret_cast<float4*>(xs + at_s) = xr[i];
+                *reinterpret_cast<float4*>(ys + at_s) = yr[i];
+            }
+            __syncthreads();
+            if (s + 1 < steps) {
+                fetch((s + 1) * kSumTokens);
+            } else if (tile + 1 < last) {
+                enter(tile + 1);
+                fetch(0);
+            }
+#pragma unroll
+            for (int k = 0; k < kSumTokens; k += 8) {
+                uint32_t ah[kM][4], al[kM][4];
+#pragma unroll
+                for (int i = 0; i < kM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // (channel g or g + 8, token t or t + 4)
+                        const Tf32<kExact> v = tf32_split<kExact>(xs[(k + t + (e >> 1) * 4) * kLd + m0 + i * 16 + g + (e & 1) * 8]);
+                        ah[i][e] = v.h;
+                        al[i][e] = v.l;
+                    }
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    uint32_t bh[2], bl[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const Tf32<kExact> v = tf32_split<kExact>(ys[(k + t + e * 4) * kLd + n0 + j * 8 + g]);
+                        bh[e] = v.h;
+                        bl[e] = v.l;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kM; ++i) {
+                        if (!kExact) {
+                            tf32_mma(acc[i][j], al[i], bh);
+                            tf32_mma(acc[i][j], ah[i], bl);
+                        }
+                        tf32_mma(acc[i][j], ah[i], bh);
+                    }
+                }
+            }
+        }
+        if (tile + 1 == last || at.unit != here.unit) {   // the unit's last tile, or this CTA's
+            float* to = a.slots + (size_t)(here.unit + blockIdx.x) * D * D;
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<float2*>(to + (m0 + i * 16 + g + e * 8) * D + n0 + j * 8 + 2 * t) = make_float2(acc[i][j][2 * e], acc[i][j][2 * e + 1]);
+            fresh = true;
+        }
+    }
+}
+
+// ---- rows times states: X M or X M^T -----------------------------------------------------------------
+// M (fp32, D x D) stays in shared memory while the unit lasts; 64 rows of X at a time, the next ones on their way in registers.
+constexpr int kRowTokens = 64;
+template <int D> constexpr int rows_smem() { return (D * (D + 8) + kRowTokens * (D + 4)) * 4; }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_constant__ RecurArgs a)
+{
+    constexpr bool kExact = sizeof(T) == 2;
+    constexpr int kLdX = D + 4, kN = D / 16;          // four warps of 16 rows, two across
+    constexpr int kLoads = kRowTokens * D / 4 / kRThreads;
+    extern __shared__ float smem[];
+    float* ms = smem;
+    float* xs = smem + D * (D + 8);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int m0 = (warp >> 1) * 16, n0 = (warp & 1) * kN * 8;
+    const int first = blockIdx.x * a.rows.share, last = min(first + a.rows.share, a.rows.tiles);
+    grid_dependency_sync();
+    if (first >= last) return;
+
+    float4 xr[kLoads];
+    RecurAt at;
+    int tokens = 0;
+    const T* x = nullptr;
+    int64_t x_step = 0;
+    auto enter = [&](int tile) {
+        at = recur_at(a.rows, tile, recur_heads(a), a.pair);
+        const RecurJob& j = a.rows.job[at.job];
+        tokens = min(kRecurTile, j.len - at.tile * kRecurTile);
+        const RecurRows& r = !a.back ? a.q : j.which == 0 ? a.dout : j.which == 1 ? a.v : a.k;
+        x = static_cast<const T*>(r.p) + at.b * r.batch + ((int64_t)at.n * a.block + at.tile * kRecurTile) * r.token + at.head * D;
+        x_step = r.token;
+    };
+    auto fetch = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int e = tid + i * kRThreads, row = from + e / (D / 4), c = e % (D / 4) * 4;
+            xr[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (row < tokens) xr[i] = load4(x + row * x_step + c);
+        }
+    };
+    enter(first);
+    fetch(0);
+    int unit = -1;
+    for (int tile = first; tile < last; ++tile) {
+        const RecurAt here = at;
+        const int which = a.rows.job[here.job].which, here_tokens = tokens;
+        const bool across = a.back && which < 2;      // M^T: rows of M are the result's columns
+        const int ld = across ? D + 4 : D + 8;        // (either way the fragments' reads fall on different banks)
+        const int steps = (tokens + kRowTokens - 1) / kRowTokens;
+        for (int s = 0; s < steps; ++s) {
+            __syncthreads();
+            if (unit != here.unit) {
+                unit = here.unit;
+                const float* m = (a.back && which > 0 ? a.dstates : a.states) + ((size_t)(here.b * a.H + here.head) * a.N + here.n) * D * D;
+                for (int e = tid; e < D * D / 4; e += kRThreads) *reinterpret_cast<float4*>(ms + e / (D / 4) * ld + e % (D / 4) * 4) = *reinterpret_cast<const float4*>(m + e * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int e = tid + i * kRThreads;
+                *reinterpret_cast<float4*>(xs + e / (D / 4) * kLdX + e % (D / 4) * 4) = xr[i];
+            }
+            __syncthreads();
+            if (s + 1 < steps) {
+                fetch((s + 1) * kRowTokens);
+            } else if (tile + 1 < last) {
+                enter(tile + 1);
+                fetch(0);
+            }
+            float acc[kN][4];
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
+#pragma unroll 2
+            for (int k = 0; k < D; k += 8) {
+                uint32_t ah[4], al[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const Tf32<kExact> v = tf32_split<kExact>(xs[(m0 + g + (e & 1) * 8) * kLdX + k + t + (e >> 1) * 4]);
+                    ah[e] = v.h;
+                    al[e] = v.l;
+                }
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    uint32_t bh[2], bl[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int kk = k + t + e * 4, nn = n0 + j * 8 + g;
+                        const Tf32<false> v = tf32_split<false>(ms[across ? nn * ld + kk : kk * ld + nn]);
+                        bh[e] = v.h;
+                        bl[e] = v.l;
+                    }
+                    if (!kExact) tf32_mma(acc[j], al, bh);
+                    tf32_mma(acc[j], ah, bl);
+                    tf32_mma(acc[j], ah, bh);
+                }
+            }
+            T* to = static_cast<T*>(!a.back ? a.out : which == 0 ? a.dq : which == 1 ? a.dk : a.dv);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = s * kRowTokens + m0 + g + e * 8;
+                if (row >= here_tokens) continue;
+                T* p = to + (((size_t)here.b * a.T + (size_t)here.n * a.block + here.tile * kRecurTile + row) * a.H + here.head) * D + n0 + 2 * t;
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    if (sizeof(T) == 4) *reinterpret_cast<float2*>(p + j * 8) = make_float2(acc[j][2 * e], acc[j][2 * e + 1]);
+                    else *reinterpret_cast<__nv_bfloat162*>(p + j * 8) = __floats2bfloat162_rn(acc[j][2 * e], acc[j][2 * e + 1]);
+                }
+            }
+        }
+    }
+}
+
+// ---- the scan over the blocks --------------------------------------------------------------------------
+// A thread has four elements of a head's state.  The sums of several blocks are asked for before the first is used.
+constexpr int kScanThreads = 256, kScanAhead = 4;
+
+template <int D>
+__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, size_t unit, int in_pair, int pair, int e, const float4& s)
+{
+    if (f32 != nullptr) *reinterpret_cast<float4*>(f32 + (unit * pair + in_pair) * D * D + e) = s;
+    if (op == nullptr) return;
+    // head and remainder: 2^-17 of the value together; an infinity has no remainder
+    __nv_bfloat16* h = op + ((unit * pair + in_pair) * 2) * D * D + e;
+    const float x[4] = {s.x, s.y, s.z, s.w};
+    __nv_bfloat16 hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        hi[i] = __float2bfloat16_rn(x[i]);
+        const float back = __bfloat162float(hi[i]);
+        lo[i] = __float2bfloat16_rn(fabsf(back) <= 3.3e38f ? x[i] - back : 0.0f);
+    }
+    *reinterpret_cast<uint2*>(h) = *reinterpret_cast<uint2*>(hi);
+    *reinterpret_cast<uint2*>(h + D * D) = *reinterpret_cast<uint2*>(lo);
+}
+
+// The sum of block n of operand pair `which`, as the CTAs of the first step left it.
+template <int D>
+__device__ __forceinline__ float4 scan_sum(const RecurArgs& a, int which, int b, int head, int n, int e)
+{
+    const int hu = head / a.pair, heads = recur_heads(a);
+    for (int i = 0; i < a.sums.jobs; ++i) {
+        const RecurJob& j = a.sums.job[i];
+        if (j.which != which || n < j.n0 || n >= j.n0 + j.n_count) continue;
+        const int v = (b * heads + hu) * j.n_count + n - j.n0, unit = j.unit0 + v;
+        const int c0 = (j.tile0 + v * j.ntile) / a.sums.share, c1 = (j.tile0 + v * j.ntile + j.ntile - 1) / a.sums.share;
+        const size_t size = (size_t)a.pair * D * D;
+        const float* p = a.slots + (size_t)(unit + c0) * size + (size_t)(head - hu * a.pair) * D * D + e;
+        float4 s = *reinterpret_cast<const float4*>(p);
+        for (int c = c0 + 1; c <= c1; ++c) {
+            p += size;
+            const float4 o = *reinterpret_cast<const float4*>(p);
+            s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+        }
+        return s;
+    }
+    return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_constant__ RecurArgs a)
+{
+    const int e = (blockIdx.x * kScanThreads + threadIdx.x) * 4, head = blockIdx.y, b = blockIdx.z;
+    const int hu = head / a.pair, in_pair = head - hu * a.pair;
+    const size_t unit0 = (size_t)(b * recur_heads(a) + hu) * a.N;
+    const size_t at = ((size_t)b * a.H + head) * D * D + e;
+    grid_dependency_sync();
+    const float* decay = a.decay + (size_t)b * a.N * a.H + head;
+    auto step = [](float4& s, float g, const float4& add) {
+        s.x = fmaf(g, s.x, add.x); s.y = fmaf(g, s.y, add.y); s.z = fmaf(g, s.z, add.z); s.w = fmaf(g, s.w, add.w);
+    };
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (a.state_in != nullptr) s = *reinterpret_cast<const float4*>(a.state_in + at);
+    for (int n0 = 0; n0 < a.N; n0 += kScanAhead) {
+        float4 sum[kScanAhead];
+        float g[kScanAhead];
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i)
+            if (n0 + i < a.N) {
+                sum[i] = scan_sum<D>(a, 0, b, head, n0 + i, e);
+                g[i] = gate_of(decay[(size_t)(n0 + i) * a.H]);
+            }
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i)
+            if (n0 + i < a.N) {
+                scan_store<D>(a.states, a.states_op, unit0 + n0 + i, in_pair, a.pair, e, s);
+                step(s, g[i], sum[i]);
+            }
+    }
+    if (!a.back) {
+        if (a.state_out != nullptr) *reinterpret_cast<float4*>(a.state_out + at) = s;
+        return;
+    }
+    s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (a.dstate_out != nullptr) s = *reinterpret_cast<const float4*>(a.dstate_out + at);
+    for (int n0 = a.N - 1; n0 >= 0; n0 -= kScanAhead) {
+        float4 sum[kScanAhead], before[kScanAhead];
+        float g[kScanAhead];
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i)
+            if (n0 - i >= 0) {
+                sum[i] = scan_sum<D>(a, 1, b, head, n0 - i, e);
+                g[i] = gate_of(decay[(size_t)(n0 - i) * a.H]);
+                before[i] = *reinterpret_cast<const float4*>(a.states + ((unit0 + n0 - i) * a.pair + in_pair) * D * D + e);   // (this thread's own)
+            }
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i)
+            if (n0 - i >= 0) {
+                const int n = n0 - i;
+                scan_store<D>(a.dstates, a.dstates_op, unit0 + n, in_pair, a.pair, e, s);
+                const float dot = warp_sum(s.x * before[i].x + s.y * before[i].y + s.z * before[i].z + s.w * before[i].w);
+                if ((threadIdx.x & 31) == 0) a.dots[(((size_t)b * a.H + head) * a.N + n) * (D * D / 128) + e / 128] = dot;
+                step(s, g[i], sum[i]);
+            }
+    }
+    if (a.dstate_in != nullptr) *reinterpret_cast<float4*>(a.dstate_in + at) = s;
+}
+
+// da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n>: a warp each
+template <int D>
+__global__ void __launch_bounds__(kScanThreads) recur_gates_kernel(const __grid_constant__ RecurArgs a)
+{
+    constexpr int kParts = D * D / 128;
+    grid_dependency_sync();
+    const long long u = ((long long)blockIdx.x * kScanThreads + threadIdx.x) >> 5;
+    if (u >= (long long)a.B * a.H * a.N) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kParts / 32; ++i) s += a.dots[u * kParts + i * 32 + (threadIdx.x & 31)];
+    s = warp_sum(s);
+    if ((threadIdx.x & 31) != 0) return;
+    const long long bh = u / a.N, n = u - bh * a.N, b = bh / a.H, h = bh - b * a.H, at = (b * a.N + n) * a.H + h;
+    const float x = a.decay[at];
+    // (alpha (1 - alpha) without the difference, which loses its digits near 1)
+    a.ddecay[at] = s * gate_of(x) * gate_of(-x);
+}
+
+template <typename K>
+int set_up(std::atomic<int>& resident, K kernel, int smem, const char* what)
+{
+    int ctas = resident.load(std::memory_order_relaxed);
+    if (ctas != 0) return ctas;
+    int dev = -1, sms = 0, per_sm = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kRThreads, smem);
+    if (e != cudaSuccess || sms * per_sm < 1) {
+        cudaGetLastError();
+        set_error("%s: cannot set up the kernel: %s", what, cudaGetErrorString(e));
+        return ARL2_ERR_CUDA;
+    }
+    ctas = sms * per_sm;
+    resident.store(ctas, std::memory_order_relaxed);
+    return ctas;
+}
+
+template <int D>
+int launch_scan(const RecurArgs& a, cudaStream_t st)
+{
+    int r = check_launch(launch_kernel(recur_scan_kernel<D>, dim3(D * D / (4 * kScanThreads), (unsigned)a.H, (unsigned)a.B), kScanThreads, 0, st, a), "recur_scan_kernel");
+    return r;
+}
+
+template <typename T, int D>
+int run_plain(RecurArgs& a, cudaStream_t st)
+{
+    static std::atomic<int> for_sums[kMaxDev], for_rows[kMaxDev];
+    int dev = -1;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || dev < 0 || dev >= kMaxDev) { set_error("cannot identify the current device (%s)", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    auto sums = recur_sums_kernel<T, D>;
+    auto rows = recur_rows_kernel<T, D>;
+    const int c0 = set_up(for_sums[dev], sums, sum_smem<D>(), "recurrence"), c1 = set_up(for_rows[dev], rows, rows_smem<D>(), "recurrence");
+    if (c0 < 0 || c1 < 0) return ARL2_ERR_CUDA;
+    recur_cut(a.sums, std::min(c0, kRecurCtas));
+    recur_cut(a.rows, c1);
+    int n = 0, r;
+    if (a.sums.tiles > 0) {
+        r = check_launch(launch_kernel(sums, dim3((unsigned)a.sums.ctas), kRThreads, sum_smem<D>(), st, a), "recur_sums_kernel");
+        if (r < 0) return r;
+        n += r;
+    }
+    r = launch_scan<D>(a, st);
+    if (r < 0) return r;
+    n += r;
+    r = check_launch(launch_kernel(rows, dim3((unsigned)a.rows.ctas), kRThreads, rows_smem<D>(), st, a), "recur_rows_kernel");
+    return r < 0 ? r : n + r;
+}
+
+template <int D>
+int run_any(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st)
+{
+    int n;
+    if (tensor_cores) {
+        n = 0;
+        int r = tc_recur_sums(a, st);
+        if (r < 0) return r;
+        n += r;
+        r = launch_scan<D>(a, st);
+        if (r < 0) return r;
+        n += r;
+        r = tc_recur_rows(a, st);
+        if (r < 0) return r;
+        n += r;
+    } else {
+        n = dtype == ARL2_FP32 ? run_plain<float, D>(a, st) : run_plain<__nv_bfloat16, D>(a, st);
+        if (n < 0) return n;
+    }
+    if (!a.back || a.ddecay == nullptr) return n;
+    const long long units = (long long)a.B * a.H * a.N;
+    const int r = check_launch(launch_kernel(recur_gates_kernel<D>, dim3((unsigned)((units * 32 + kScanThreads - 1) / kScanThreads)), kScanThreads, 0, st, a), "recur_gates_kernel");
+    return r < 0 ? r : n + r;
+}
+
+}  // namespace
+
+void recur_plan(RecurArgs& a)
+{
+    const int heads = a.B * recur_heads(a);
+    const int whole = a.T / a.block, rest = a.T - whole * a.block;    // blocks of full length, tokens of a shorter one
+    auto add = [&](RecurStep& s, int which, int from, int to) {       // blocks from .. to - 1
+        for (int part = 0; part < 2; ++part) {
+            const int lo = part == 0 ? from : std::max(from, whole), hi = part == 0 ? std::min(to, whole) : to;
+            if (lo >= hi) continue;
+            RecurJob& j = s.job[s.jobs++];
+            j.which = which;
+            j.part = part;
+            j.len = part == 0 ? a.block : rest;
+            j.ntile = (j.len + kRecurTile - 1) / kRecurTile;
+            j.n0 = lo;
+            j.n_count = hi - lo;
+            j.tile0 = s.tiles;
+            j.unit0 = s.units;
+            s.units += heads * j.n_count;
+            s.tiles += heads * j.n_count * j.ntile;
+        }
+    };
+    a.sums = a.rows = RecurStep{};
+    // the last block's K^T V is for the state behind it alone, the first block's Q^T dO for the gradient of the state before it
+    add(a.sums, 0, 0, a.back || a.state_out == nullptr ? a.N - 1 : a.N);
+    if (a.back) add(a.sums, 1, a.dstate_in == nullptr ? 1 : 0, a.N);
+    for (int which = 0; which < (a.back ? 3 : 1); ++which) add(a.rows, which, 0, a.N);
+}
+
+int recur(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st)
+{
+    return a.D == 128 ? run_any<128>(a, dtype, tensor_cores, st) : run_any<64>(a, dtype, tensor_cores, st);
+}
+
+}  // namespace arl2

@@ -1,0 +1,464 @@
+// The recurrence over the blocks of a sequence on tensor cores (bf16 I/O): sums over tokens, X^T Y, and rows times states,
+// X M or X M^T (arl2_recur.cu has the mathematics and the scan between the two).
+//
+// Both go over 128-token tiles of units, a unit being a block of one head, or of two heads of 64 channels side by side; the
+// tiles of all units are one sequence, cut into equal runs, one CTA (one per SM) per run.  Tiles come by TMA; the tensors are
+// seen as (channel, head, token in block, block, stream), so that what lies past a block's end reads as zeros.  Memory bounds
+// them: 64 flops per byte where the tensor cores do 250, so a ring of stages kept full is all that counts.
+//
+// tc_recur_sums_kernel:  warp 0 TMA producer, warp 1 MMA issuer, warps 2-5 store the accumulators (one of two in
+//   TMEM, so that a unit's go out beside the next one's products) to the slot of (unit, CTA).  bf16 operands, fp32
+//   accumulation: the products are exact.  Of two heads side by side the 128 x 128 product has two blocks that nobody wants:
+//   tensor time that there is plenty of.
+// tc_recur_rows_kernel:  the same with warps 2-9 writing rows; a state is a bf16 head and a bf16 remainder (2^-17 of it
+//   together, 2^-9 of the output's own rounding), two products each.  M stands in shared memory as it is in memory; M^T is the
+//   same tile read with its other dimension innermost.
+//
+// Every wait is bounded; a CTA that gives up records ARL2_ERR_TIMEOUT, drains what is in flight and frees its tensor memory.
+#include "tc_common.cuh"
+
+namespace arl2 {
+namespace {
+
+constexpr int kSStages = 3, kRStages = 3;
+constexpr int kSThreads = 192, kRThreads = 320;
+constexpr int kSOffBars = 2 * kSStages * kTileBytes;
+constexpr int kSSmemBytes = kSOffBars + 256 + 1024;
+constexpr int kMatBytes = 2 * kTileBytes;                  // a state's head and remainder (two heads of 64 channels have half of it)
+constexpr int kROffStage = 2 * kMatBytes;
+constexpr int kROffBars = kROffStage + kRStages * kTileBytes;
+constexpr int kRSmemBytes = kROffBars + 256 + 1024;
+static_assert(kRSmemBytes <= kMaxSmemPerCta && kSSmemBytes <= kMaxSmemPerCta, "shared memory");
+
+struct RecurMaps { CUtensorMap m[2][3]; };   // [part of the blocks][tensor]
+
+enum SBar : int { kSBarFull0 = 0, kSBarFree0 = kSBarFull0 + kSStages, kSBarAccFull0 = kSBarFree0 + kSStages, kSBarAccFree0 = kSBarAccFull0 + 2,
+                  kSBarDrain = kSBarAccFree0 + 2, kSNumBars };
+enum RBar : int { kRBarFull0 = 0, kRBarFree0 = kRBarFull0 + kRStages, kRBarMatFull0 = kRBarFree0 + kRStages, kRBarMatFree0 = kRBarMatFull0 + 2,
+                  kRBarAccFull0 = kRBarMatFree0 + 2, kRBarAccFree0 = kRBarAccFull0 + 2, kRBarDrain = kRBarAccFree0 + 2, kRNumBars };
+static_assert(kSNumBars * 8 + 16 <= 256 && kRNumBars * 8 + 16 <= 256, "barrier block");
+
+// rows of a TMA box for blocks of `len` tokens
+__host__ __device__ constexpr int box_rows(int len) { return len >= kTile ? kTile : (len + 15) / 16 * 16; }
+
+// a tile: two boxes of 64 columns, of one head or of two
+template <int D>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, const RecurAt& at, const RecurJob& j, int b)
+{
+    const int n = j.part == 0 ? at.n : 0, row = at.tile * kTile;
+    tma_load_5d(dst, map, bar, 0, at.head, row, n, b);
+    if (D == 128) tma_load_5d(dst + kHalfBytes, map, bar, 64, at.head, row, n, b);
+    else tma_load_5d(dst + kHalfBytes, map, bar, 0, at.head + 1, row, n, b);
+}
+
+__device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+    return d;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSThreads, 1)
+tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_constant__ RecurMaps maps_y, const __grid_constant__ RecurArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t smem_base = smem_u32(smem), bars = smem_base + kSOffBars;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kSOffBars + kSNumBars * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kSOffBars + kSNumBars * 8 + 4);
+    const Abort ab{abort_flag, a.status, a.wait_limit ? a.wait_limit - 1 : kSpinLimit};
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int first = (int)blockIdx.x * a.sums.share, count = min(a.sums.share, a.sums.tiles - first);
+    const int heads = recur_heads(a);
+
+    if (tid == 0) {
+        for (int s = 0; s < kSStages; ++s) {
+            mbar_init(bars + 8 * (kSBarFull0 + s), 1);
+            mbar_init(bars + 8 * (kSBarFree0 + s), 1);
+        }
+        for (int u = 0; u < 2; ++u) {
+            mbar_init(bars + 8 * (kSBarAccFull0 + u), 1);
+            mbar_init(bars + 8 * (kSBarAccFree0 + u), 128);
+        }
+        mbar_init(bars + 8 * kSBarDrain, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+        fence_proxy_async_smem();
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), 256);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    grid_dependency_sync();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            bool ok = true;
+            int issued = 0;
+            for (int k = 0; k < count && ok; ++k) {
+                const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
+                const RecurJob& j = a.sums.job[at.job];
+                const int s = k % kSStages;
+                if (k >= kSStages) ok = wait_bar(bars + 8 * (kSBarFree0 + s), (uint32_t)((k / kSStages) - 1) & 1u, ab, 200);
+                if (!ok) break;
+                const uint32_t bar = bars + 8 * (kSBarFull0 + s), dst = smem_base + s * 2 * kTileBytes;
+                mbar_expect_tx(bar, (uint32_t)box_rows(j.len) * 512u);
+                const RecurRows& x = j.which == 0 ? a.k : a.q;
+                const RecurRows& y = j.which == 0 ? a.v : a.dout;
+                load_tile<D>(dst, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b);
+                load_tile<D>(dst + kTileBytes, &maps_y.m[j.part][j.which], bar, at, j, y.batch == 0 ? 0 : at.b);
+                ++issued;
+            }
+            for (int m = (issued > kSStages ? issued - kSStages : 0); m < issued; ++m) drain_bar(bars + 8 * (kSBarFull0 + m % kSStages), (uint32_t)(m / kSStages) & 1u);
+        }
+    } else if (warp == 1) {
+        const uint32_t lead = elect_one();
+        const uint32_t base = __shfl_sync(0xffffffffu, smem_base, 0), ubars = base + kSOffBars, tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
+        const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
+        constexpr uint32_t kLbo = (uint32_t)(kHalfBytes >> 4) << 16;
+        constexpr uint32_t idesc = idesc_bf16(kTile, kTile, 1, 1);      // both operands token-major
+        bool ok = true;
+        int seg = 0;
+        int unit = -1;
+        for (int k = 0; k < count && ok; ++k) {
+            const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
+            const RecurJob& j = a.sums.job[at.job];
+            const bool fresh = at.unit != unit;
+            if (fresh && seg >= 2) ok = wait_bar_warp(ubars + 8 * (kSBarAccFree0 + (seg & 1)), (uint32_t)((seg >> 1) - 1) & 1u, ab, 201);
+            unit = at.unit;
+            const int s = k % kSStages;
+            if (ok) ok = wait_bar_warp(ubars + 8 * (kSBarFull0 + s), (uint32_t)(k / kSStages) & 1u, ab, 202);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t x_lo = ((base + s * 2 * kTileBytes) >> 4) | kLbo, y_lo = ((base + s * 2 * kTileBytes + kTileBytes) >> 4) | kLbo;
+            const int steps = (min(kTile, j.len - at.tile * kTile) + 15) >> 4;      // 16 tokens each
+            const uint32_t acc = tmem + (seg & 1) * kTile;
+            for (int ks = 0; ks < steps; ++ks)
+                mma_ss_if(lead, acc, desc64(x_lo + (uint32_t)(ks * (2048 >> 4)), desc_hi), desc64(y_lo + (uint32_t)(ks * (2048 >> 4)), desc_hi), idesc, (!fresh || ks > 0) ? 1u : 0u);
+            mma_commit_if(lead, ubars + 8 * (kSBarFree0 + s));
+            if (at.tile + 1 == j.ntile || k + 1 == count) {
+                mma_commit_if(lead, ubars + 8 * (kSBarAccFull0 + (seg & 1)));
+                ++seg;
+            }
+        }
+        // tensor memory is freed below: none of the MMAs may still be running
+        mma_commit_if(lead, ubars + 8 * kSBarDrain);
+        drain_bar(ubars + 8 * kSBarDrain, 0);
+    } else {
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+        int seg = 0;
+        for (int k = 0; k < count; ++k) {
+            const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
+            if (at.tile + 1 != a.sums.job[at.job].ntile && k + 1 != count) continue;
+            if (!wait_bar_warp(bars + 8 * (kSBarAccFull0 + (seg & 1)), (uint32_t)(seg >> 1) & 1u, ab, 203)) break;
+            tc_fence_after();
+            // row = channel of X; row-major [D][D], of two heads one after the other
+            float* to = a.slots + (size_t)(at.unit + blockIdx.x) * (D * kTile) + row * D;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                // (the warp's rows are all of one head)
+                tmem_ld32(lane_base + (seg & 1) * kTile + (D == 128 ? 0 : (warp & 3) >> 1 << 6) + c * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = o[e * 8 + i];
+                    store_row32(to + c * 32 + e * 8, w);
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(bars + 8 * (kSBarAccFree0 + (seg & 1)));
+            ++seg;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 256);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kRThreads, 1)
+tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_d,
+                     const __grid_constant__ RecurArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t smem_base = smem_u32(smem), bars = smem_base + kROffBars;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kROffBars + kRNumBars * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kROffBars + kRNumBars * 8 + 4);
+    const Abort ab{abort_flag, a.status, a.wait_limit ? a.wait_limit - 1 : kSpinLimit};
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int first = (int)blockIdx.x * a.rows.share, count = min(a.rows.share, a.rows.tiles - first);
+    const int heads = recur_heads(a);
+    constexpr int kMatPart = D == 128 ? kTileBytes : 64 * 64 * 2;          // bytes of a head or a remainder
+    constexpr int kParts = D == 128 ? 2 : 4;                               // ... of a unit's state
+
+    if (tid == 0) {
+        for (int s = 0; s < kRStages; ++s) {
+            mbar_init(bars + 8 * (kRBarFull0 + s), 1);
+            mbar_init(bars + 8 * (kRBarFree0 + s), 1);
+        }
+        for (int u = 0; u < 2; ++u) {
+            mbar_init(bars + 8 * (kRBarMatFull0 + u), 1);
+            mbar_init(bars + 8 * (kRBarMatFree0 + u), 1);
+            mbar_init(bars + 8 * (kRBarAccFull0 + u), 1);
+            mbar_init(bars + 8 * (kRBarAccFree0 + u), 256);
+        }
+        mbar_init(bars + 8 * kRBarDrain, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+        fence_proxy_async_smem();
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), 256);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    grid_dependency_sync();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            fence_proxy_async_global();      // the states come from the scan's stores
+            bool ok = true;
+            int issued = 0, mats = 0, unit = -1;
+            for (int k = 0; k < count && ok; ++k) {
+                const RecurAt at = recur_at(a.rows, first + k, heads, a.pair);
+                const RecurJob& j = a.rows.job[at.job];
+                if (at.unit != unit) {
+                    unit = at.unit;
+                    const int u = mats & 1;
+                    if (mats >= 2) ok = wait_bar(bars + 8 * (kRBarMatFree0 + u), (uint32_t)((mats >> 1) - 1) & 1u, ab, 210);
+                    if (!ok) break;
+                    const uint32_t bar = bars + 8 * (kRBarMatFull0 + u), dst = smem_base + u * kMatBytes;
+                    const CUtensorMap* map = a.back && j.which > 0 ? &map_d : &map_s;
+                    const int row = ((at.b * heads + at.head / a.pair) * a.N + at.n) * kParts * D;
+                    mbar_expect_tx(bar, kParts * kMatPart);
+                    for (int p = 0; p < kParts; ++p) {
+                        tma_load_2d(dst + p * kMatPart, map, bar, 0, row + p * D);
+                        if (D == 128) tma_load_2d(dst + p * kMatPart + kHalfBytes, map, bar, 64, row + p * D);
+                    }
+                    ++mats;
+                }
+                const int s = k % kRStages;
+                if (k >= kRStages) ok = wait_bar(bars + 8 * (kRBarFree0 + s), (uint32_t)((k / kRStages) - 1) & 1u, ab, 211);
+                if (!ok) break;
+                const uint32_t bar = bars + 8 * (kRBarFull0 + s);
+                mbar_expect_tx(bar, (uint32_t)box_rows(j.len) * 256u);
+                const RecurRows& x = !a.back ? a.q : j.which == 0 ? a.dout : j.which == 1 ? a.v : a.k;
+                load_tile<D>(smem_base + kROffStage + s * kTileBytes, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b);
+                ++issued;
+            }
+            for (int m = (issued > kRStages ? issued - kRStages : 0); m < issued; ++m) drain_bar(bars + 8 * (kRBarFull0 + m % kRStages), (uint32_t)(m / kRStages) & 1u);
+            for (int m = (mats > 2 ? mats - 2 : 0); m < mats; ++m) drain_bar(bars + 8 * (kRBarMatFull0 + (m & 1)), (uint32_t)(m >> 1) & 1u);
+        }
+    } else if (warp == 1) {
+        const uint32_t lead = elect_one();
+        const uint32_t base = __shfl_sync(0xffffffffu, smem_base, 0), ubars = base + kROffBars, tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
+        const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
+        constexpr uint32_t kLboK = 1u << 16, kLboMN = (uint32_t)(kHalfBytes >> 4) << 16;
+        bool ok = true;
+        int mats = 0, unit = -1;
+        for (int k = 0; k < count && ok; ++k) {
+            const RecurAt at = recur_at(a.rows, first + k, heads, a.pair);
+            const RecurJob& j = a.rows.job[at.job];
+            const int s = k % kRStages;
+            if (at.unit != unit) {
+                unit = at.unit;
+                ok = wait_bar_warp(ubars + 8 * (kRBarMatFull0 + (mats & 1)), (uint32_t)(mats >> 1) & 1u, ab, 212);
+                ++mats;
+            }
+            if (ok && k >= 2) ok = wait_bar_warp(ubars + 8 * (kRBarAccFree0 + (k & 1)), (uint32_t)((k >> 1) - 1) & 1u, ab, 213);
+            if (ok) ok = wait_bar_warp(ubars + 8 * (kRBarFull0 + s), (uint32_t)(k / kRStages) & 1u, ab, 214);
+            if (!ok) break;
+            tc_fence_after();
+            const bool across = a.back && j.which < 2;       // M^T
+            const uint32_t x_lo = ((base + kROffStage + s * kTileBytes) >> 4) | kLboK;
+            const uint32_t m_lo = ((base + ((mats - 1) & 1) * kMatBytes) >> 4) | (across ? kLboK : kLboMN);
+            const uint32_t acc = tmem + (k & 1) * kTile;
+            if (D == 128) {
+                const uint32_t idesc = across ? idesc_bf16(kTile, kTile, 0, 0) : idesc_bf16(kTile, kTile, 0, 1);
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        const uint32_t koff = (uint32_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4);
+                        mma_ss_if(lead, acc, desc64(x_lo + koff, desc_hi), desc64(m_lo + (uint32_t)(p * kTileBytes >> 4) + (across ? koff : (uint32_t)(ks * (2048 >> 4))), desc_hi),
+                                  idesc, (p > 0 || ks > 0) ? 1u : 0u);
+                    }
+            } else {
+                const uint32_t idesc = across ? idesc_bf16(kTile, 64, 0, 0) : idesc_bf16(kTile, 64, 0, 1);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+                            mma_ss_if(lead, acc + h * 64, desc64(x_lo + (uint32_t)((h * kHalfBytes + ks * 32) >> 4), desc_hi),
+                                      desc64(m_lo + (uint32_t)((h * 2 + p) * kMatPart >> 4) + (uint32_t)(ks * ((across ? 32 : 2048) >> 4)), desc_hi), idesc, (p > 0 || ks > 0) ? 1u : 0u);
+            }
+            mma_commit_if(lead, ubars + 8 * (kRBarFree0 + s));
+            mma_commit_if(lead, ubars + 8 * (kRBarAccFull0 + (k & 1)));
+            if (at.tile + 1 == j.ntile) mma_commit_if(lead, ubars + 8 * (kRBarMatFree0 + ((mats - 1) & 1)));
+        }
+        mma_commit_if(lead, ubars + 8 * kRBarDrain);
+        drain_bar(ubars + 8 * kRBarDrain, 0);
+    } else {
+        const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+        for (int k = 0; k < count; ++k) {
+            const RecurAt at = recur_at(a.rows, first + k, heads, a.pair);
+            const RecurJob& j = a.rows.job[at.job];
+            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(!a.back ? a.out : j.which == 0 ? a.dq : j.which == 1 ? a.dk : a.dv);
+            const int head = D == 128 ? at.head : at.head + half;
+            const bool mine = at.tile * kTile + row < j.len && head < a.H;
+            __nv_bfloat16* p = to + (((size_t)at.b * a.T + (size_t)at.n * a.block + at.tile * kTile + row) * a.H + head) * D + (D == 128 ? half * 64 : 0);
+            if (!wait_bar_warp(bars + 8 * (kRBarAccFull0 + (k & 1)), (uint32_t)(k >> 1) & 1u, ab, 215)) break;
+            tc_fence_after();
+            uint32_t x[64];
+            tmem_ld32(lane_base + (k & 1) * kTile + half * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+            tmem_ld32(lane_base + (k & 1) * kTile + half * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+            tmem_wait_ld();
+            tc_fence_before();
+            mbar_arrive(bars + 8 * (kRBarAccFree0 + (k & 1)));
+            if (mine) {
+                const bool wide = wide_rows(to);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = pack_bf16(__uint_as_float(x[c * 16 + 2 * i]), __uint_as_float(x[c * 16 + 2 * i + 1]));
+                    if (wide) {
+                        store_row32(p + c * 16, w);
+                    } else {
+                        *reinterpret_cast<uint4*>(p + c * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(p + c * 16 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 256);
+    }
+}
+
+// [B, T, H, D] with strides, seen as (channel, head, token in block, block, stream): the blocks of full length, or the shorter last one.
+// A stride of zero (one stream's rows for all of them) is a dimension of one.
+int make_map_blocks(CUtensorMap* m, const RecurArgs& a, const RecurRows& r, int part)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) { set_error("cuTensorMapEncodeTiled is not available from the driver"); return ARL2_ERR_CUDA; }
+    const int whole = a.T / a.block, rest = a.T - whole * a.block, len = part == 0 ? a.block : rest;
+    const __nv_bfloat16* base = static_cast<const __nv_bfloat16*>(r.p) + (part == 0 ? 0 : (int64_t)whole * a.block * r.token);
+    cuuint64_t dims[5] = {(cuuint64_t)a.D, (cuuint64_t)a.H, (cuuint64_t)len, (cuuint64_t)(part == 0 ? whole : 1), (cuuint64_t)(r.batch == 0 ? 1 : a.B)};
+    const cuuint64_t token = (cuuint64_t)r.token * 2;
+    cuuint64_t strides[4] = {(cuuint64_t)a.D * 2, token, part == 0 ? token * (cuuint64_t)a.block : token, r.batch == 0 ? token : (cuuint64_t)r.batch * 2};
+    cuuint32_t box[5] = {64, 1, (cuuint32_t)box_rows(len), 1, 1};
+    cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    const CUresult e = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<__nv_bfloat16*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (e != CUDA_SUCCESS) { set_error("cuTensorMapEncodeTiled([B,T,H,D]) failed with %d", (int)e); return ARL2_ERR_CUDA; }
+    return 0;
+}
+int make_maps(RecurMaps& m, const RecurArgs& a, int which, const RecurRows& r)
+{
+    const int whole = a.T / a.block, rest = a.T - whole * a.block;
+    if (whole > 0)
+        if (int e = make_map_blocks(&m.m[0][which], a, r, 0)) return e;
+    return rest > 0 ? make_map_blocks(&m.m[1][which], a, r, 1) : 0;
+}
+// states as operands: rows of D numbers
+int make_map_states(CUtensorMap* m, const RecurArgs& a, const __nv_bfloat16* p)
+{
+    EncodeTiledFn fn = encode_fn();
+    cuuint64_t dims[2] = {(cuuint64_t)a.D, (cuuint64_t)a.B * recur_heads(a) * a.N * a.pair * 2 * a.D};
+    cuuint64_t strides[1] = {(cuuint64_t)a.D * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)a.D};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult e = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<__nv_bfloat16*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (e != CUDA_SUCCESS) { set_error("cuTensorMapEncodeTiled(states) failed with %d", (int)e); return ARL2_ERR_CUDA; }
+    return 0;
+}
+
+std::mutex g_setup_mutex;
+DeviceSetup g_setup[kMaxDevices];
+int recur_sms(int* sms)
+{
+    return device_setup_once(g_setup_mutex, g_setup, [] {
+        cudaError_t e = opt_in_smem(tc_recur_sums_kernel<128>, kSSmemBytes);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_sums_kernel<64>, kSSmemBytes);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_rows_kernel<128>, kRSmemBytes);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_rows_kernel<64>, kRSmemBytes);
+        return e;
+    }, sms);
+}
+
+int launched(cudaError_t e, const char* what)
+{
+    if (e == cudaSuccess) return 1;
+    set_error("launch of %s failed: %s", what, cudaGetErrorString(e));
+    return ARL2_ERR_CUDA;
+}
+
+}  // namespace
+
+bool tc_recur_supported(const RecurArgs& a)
+{
+    // (a tensor map's strides are below 2^40 bytes, its coordinates 31 bits)
+    for (const RecurRows* r : {&a.q, &a.k, &a.v, &a.dout})
+        if (r->token >= ((int64_t)1 << 39) / a.block || r->batch >= ((int64_t)1 << 39)) return false;
+    return (int64_t)a.B * recur_heads(a) * a.N * a.pair * 2 * a.D < ((int64_t)1 << 31);
+}
+
+int tc_recur_sums(RecurArgs& a, cudaStream_t st)
+{
+    if (a.sums.tiles == 0) return 0;
+    int sms = 0;
+    if (int r = recur_sms(&sms)) return r;
+    recur_cut(a.sums, sms < kRecurCtas ? sms : kRecurCtas);
+    RecurMaps x, y;
+    int r = make_maps(x, a, 0, a.k);
+    if (r == 0) r = make_maps(y, a, 0, a.v);
+    if (r == 0 && a.back) r = make_maps(x, a, 1, a.q);
+    if (r == 0 && a.back) r = make_maps(y, a, 1, a.dout);
+    if (r != 0) return r;
+    return launched(a.D == 128 ? launch_kernel(tc_recur_sums_kernel<128>, dim3((unsigned)a.sums.ctas), kSThreads, kSSmemBytes, st, x, y, a)
+                               : launch_kernel(tc_recur_sums_kernel<64>, dim3((unsigned)a.sums.ctas), kSThreads, kSSmemBytes, st, x, y, a), "tc_recur_sums_kernel");
+}
+
+int tc_recur_rows(RecurArgs& a, cudaStream_t st)
+{
+    int sms = 0;
+    if (int r = recur_sms(&sms)) return r;
+    recur_cut(a.rows, sms);
+    RecurMaps x;
+    CUtensorMap s, d;
+    int r = make_maps(x, a, 0, a.back ? a.dout : a.q);
+    if (r == 0 && a.back) r = make_maps(x, a, 1, a.v);
+    if (r == 0 && a.back) r = make_maps(x, a, 2, a.k);
+    if (r == 0) r = make_map_states(&s, a, a.states_op);
+    if (r == 0) r = make_map_states(&d, a, a.back ? a.dstates_op : a.states_op);
+    if (r != 0) return r;
+    return launched(a.D == 128 ? launch_kernel(tc_recur_rows_kernel<128>, dim3((unsigned)a.rows.ctas), kRThreads, kRSmemBytes, st, x, s, d, a)
+                               : launch_kernel(tc_recur_rows_kernel<64>, dim3((unsigned)a.rows.ctas), kRThreads, kRSmemBytes, st, x, s, d, a), "tc_recur_rows_kernel");
+}
+
+}  // namespace arl2
