@@ -6,10 +6,11 @@
 // seen as (channel, head, token in block, block, stream), so that what lies past a block's end reads as zeros.  Memory bounds
 // them: 64 flops per byte where the tensor cores do 250, so a ring of stages kept full is all that counts.
 //
-// tc_recur_sums_kernel:  warp 0 TMA producer, warp 1 MMA issuer, warps 2-5 store the accumulators (one of two in
-//   TMEM, so that a unit's go out beside the next one's products) to the slot of (unit, CTA).  bf16 operands, fp32
-//   accumulation: the products are exact.  Of two heads side by side the 128 x 128 product has two blocks that nobody wants:
-//   tensor time that there is plenty of.
+// tc_recur_sums_kernel:  warp 0 TMA producer, warp 1 MMA issuer, warps 2-9 add up the accumulators (two in TMEM, by turns) in
+//   registers and store a unit's to the slot of (unit, CTA).  The products of bf16 are exact, but the tensor cores cut what does not fit
+//   when they add: 3e-6 too small at the end of 4680 tokens.  So an accumulator takes kFlush tiles, and these sums are added by
+//   rounding additions (40 heads x 14040 tokens: the state 3.1e-6 off -> 2.4e-7).  Of two heads side by side the 128 x 128 product
+//   has two blocks that nobody wants: tensor time that there is plenty of.
 // tc_recur_rows_kernel:  the same with warps 2-9 writing rows; a state is a bf16 head and a bf16 remainder (2^-17 of it
 //   together, 2^-9 of the output's own rounding), two products each.  M stands in shared memory as it is in memory; M^T is the
 //   same tile read with its other dimension innermost.
@@ -21,7 +22,8 @@ namespace arl2 {
 namespace {
 
 constexpr int kSStages = 3, kRStages = 3;
-constexpr int kSThreads = 192, kRThreads = 320;
+constexpr int kSThreads = 320, kRThreads = 320;
+constexpr int kFlush = 2;                                  // tiles whose sums an accumulator takes
 constexpr int kSOffBars = 2 * kSStages * kTileBytes;
 constexpr int kSSmemBytes = kSOffBars + 256 + 1024;
 constexpr int kMatBytes = 2 * kTileBytes;                  // a state's head and remainder (two heads of 64 channels have half of it)
@@ -79,7 +81,7 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         }
         for (int u = 0; u < 2; ++u) {
             mbar_init(bars + 8 * (kSBarAccFull0 + u), 1);
-            mbar_init(bars + 8 * (kSBarAccFree0 + u), 128);
+            mbar_init(bars + 8 * (kSBarAccFree0 + u), 256);
         }
         mbar_init(bars + 8 * kSBarDrain, 1);
         *abort_flag = 0;
@@ -123,60 +125,67 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         constexpr uint32_t kLbo = (uint32_t)(kHalfBytes >> 4) << 16;
         constexpr uint32_t idesc = idesc_bf16(kTile, kTile, 1, 1);      // both operands token-major
         bool ok = true;
-        int seg = 0;
-        int unit = -1;
+        int turn = 0, in_turn = 0;      // accumulators so far, tiles of this one
         for (int k = 0; k < count && ok; ++k) {
             const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
             const RecurJob& j = a.sums.job[at.job];
-            const bool fresh = at.unit != unit;
-            if (fresh && seg >= 2) ok = wait_bar_warp(ubars + 8 * (kSBarAccFree0 + (seg & 1)), (uint32_t)((seg >> 1) - 1) & 1u, ab, 201);
-            unit = at.unit;
+            const bool fresh = in_turn == 0;
+            if (fresh && turn >= 2) ok = wait_bar_warp(ubars + 8 * (kSBarAccFree0 + (turn & 1)), (uint32_t)((turn >> 1) - 1) & 1u, ab, 201);
             const int s = k % kSStages;
             if (ok) ok = wait_bar_warp(ubars + 8 * (kSBarFull0 + s), (uint32_t)(k / kSStages) & 1u, ab, 202);
             if (!ok) break;
             tc_fence_after();
             const uint32_t x_lo = ((base + s * 2 * kTileBytes) >> 4) | kLbo, y_lo = ((base + s * 2 * kTileBytes + kTileBytes) >> 4) | kLbo;
             const int steps = (min(kTile, j.len - at.tile * kTile) + 15) >> 4;      // 16 tokens each
-            const uint32_t acc = tmem + (seg & 1) * kTile;
+            const uint32_t acc = tmem + (turn & 1) * kTile;
             for (int ks = 0; ks < steps; ++ks)
                 mma_ss_if(lead, acc, desc64(x_lo + (uint32_t)(ks * (2048 >> 4)), desc_hi), desc64(y_lo + (uint32_t)(ks * (2048 >> 4)), desc_hi), idesc, (!fresh || ks > 0) ? 1u : 0u);
             mma_commit_if(lead, ubars + 8 * (kSBarFree0 + s));
-            if (at.tile + 1 == j.ntile || k + 1 == count) {
-                mma_commit_if(lead, ubars + 8 * (kSBarAccFull0 + (seg & 1)));
-                ++seg;
+            if (++in_turn == kFlush || at.tile + 1 == j.ntile || k + 1 == count) {
+                mma_commit_if(lead, ubars + 8 * (kSBarAccFull0 + (turn & 1)));
+                ++turn;
+                in_turn = 0;
             }
         }
         // tensor memory is freed below: none of the MMAs may still be running
         mma_commit_if(lead, ubars + 8 * kSBarDrain);
         drain_bar(ubars + 8 * kSBarDrain, 0);
     } else {
-        const int row = (warp & 3) * 32 + lane;
-        const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-        int seg = 0;
+        // a row (channel of X) and half of its columns, of its own head where there are two
+        constexpr int kCols = D / 2;
+        const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t from = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (D == 128 ? 0 : (warp & 3) >> 1 << 6) + half * kCols;
+        float sum[kCols];
+        int turn = 0, in_turn = 0;
+        bool fresh = true;
         for (int k = 0; k < count; ++k) {
             const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
-            if (at.tile + 1 != a.sums.job[at.job].ntile && k + 1 != count) continue;
-            if (!wait_bar_warp(bars + 8 * (kSBarAccFull0 + (seg & 1)), (uint32_t)(seg >> 1) & 1u, ab, 203)) break;
+            const bool last = at.tile + 1 == a.sums.job[at.job].ntile || k + 1 == count;
+            if (++in_turn != kFlush && !last) continue;
+            in_turn = 0;
+            if (!wait_bar_warp(bars + 8 * (kSBarAccFull0 + (turn & 1)), (uint32_t)(turn >> 1) & 1u, ab, 203)) break;
             tc_fence_after();
-            // row = channel of X; row-major [D][D], of two heads one after the other
-            float* to = a.slots + (size_t)(at.unit + blockIdx.x) * (D * kTile) + row * D;
-#pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                // (the warp's rows are all of one head)
-                tmem_ld32(lane_base + (seg & 1) * kTile + (D == 128 ? 0 : (warp & 3) >> 1 << 6) + c * 32, o);
-                tmem_wait_ld();
+            uint32_t o[kCols];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = o[e * 8 + i];
-                    store_row32(to + c * 32 + e * 8, w);
-                }
-            }
+            for (int c = 0; c < kCols; c += 32) tmem_ld32(from + (turn & 1) * kTile + c, *reinterpret_cast<uint32_t(*)[32]>(&o[c]));
+            tmem_wait_ld();
             tc_fence_before();
-            mbar_arrive(bars + 8 * (kSBarAccFree0 + (seg & 1)));
-            ++seg;
+            mbar_arrive(bars + 8 * (kSBarAccFree0 + (turn & 1)));
+            ++turn;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) sum[c] = fresh ? __uint_as_float(o[c]) : sum[c] + __uint_as_float(o[c]);
+            fresh = false;
+            if (!last) continue;
+            fresh = true;
+            // row-major [D][D], of two heads one after the other
+            float* to = a.slots + (size_t)(at.unit + blockIdx.x) * (D * kTile) + row * D + half * kCols;
+#pragma unroll
+            for (int c = 0; c < kCols; c += 8) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(sum[c + i]);
+                store_row32(to + c, w);
+            }
         }
     }
     tc_fence_before();

@@ -20,7 +20,7 @@ def near(got, want, slack, what=""):
     bound = u(got.dtype) * want.abs() * 1.001 + slack + 1e-300
     off = (got64 - want).abs() / bound
     assert not torch.isnan(off).any(), what
-    worst = float(off.max())
+    worst = float(off.detach().max())
     assert worst <= 1.0, f"{what}: {worst:.3g} times the tolerance"
 
 
