@@ -433,7 +433,8 @@ int arl2_modulate_backward(arl2_ctx* ctx, const arl2_modulation_config* cfg, int
  * axis_pairs[2] by the third, and what is left does not turn.  Positions: d_positions [B, tokens, 3], or NULL and
  *   (start[b] + l / (grid_rows * grid_columns),  l / grid_columns % grid_rows,  l % grid_columns)   of token l; d_start [B] or NULL: 0.
  * A position before the tables counts as their first row; one behind them as the last, and arl2_sync_status reports ARL2_ERR_RANGE.
- * Outputs are contiguous and 16-byte aligned; one may be its own input where that is contiguous.  (H + kv_heads) * D <= 16384.
+ * Outputs are contiguous and 16-byte aligned; one may be its own input where that is contiguous.  H * D and
+ * kv_heads * D are at most 8192.
  */
 typedef struct {
     uint32_t struct_size;

@@ -1439,7 +1439,7 @@ struct ModulationLayout { size_t parts, weight_parts, total; };
 ModulationLayout modulation_layout(const arl2_config& cfg, int32_t tokens)
 {
     const int d = cfg.H * cfg.D;
-    const int64_t rows = (int64_t)cfg.B * tokens, most = block_runs(d / 8), runs = rows < most ? rows : most;
+    const int64_t rows = (int64_t)cfg.B * tokens, most = block_runs(d, modulate_back_vecs(d)), runs = rows < most ? rows : most;
     ModulationLayout l;
     size_t off = 0;
     l.parts = off;        off += align_up((size_t)runs * 2 * 3 * d * sizeof(float));
@@ -1474,8 +1474,8 @@ bool valid_rotation(const arl2_config* cfg, const arl2_rotation_config* c)
         set_error("rotation config.struct_size is %u, this library expects %zu", c->struct_size, sizeof(arl2_rotation_config));
         return false;
     }
-    if (c->kv_heads < 1 || ((int64_t)cfg->H + c->kv_heads) * cfg->D > 2 * kBlockMostChannels) {
-        set_error("rotation: kv_heads must be >= 1 and (H + kv_heads) * D at most %d (got H = %d, kv_heads = %d)", 2 * kBlockMostChannels, cfg->H, c->kv_heads);
+    if (c->kv_heads < 1 || (int64_t)cfg->H * cfg->D > kBlockMostChannels || (int64_t)c->kv_heads * cfg->D > kBlockMostChannels) {
+        set_error("rotation: kv_heads must be >= 1, and H * D and kv_heads * D at most %d (got H = %d, kv_heads = %d)", kBlockMostChannels, cfg->H, c->kv_heads);
         return false;
     }
     int64_t pairs = 0;
@@ -1500,15 +1500,10 @@ bool valid_rotation(const arl2_config* cfg, const arl2_rotation_config* c)
 size_t rotation_workspace(const arl2_config& cfg, const arl2_rotation_config& c, int32_t tokens)
 {
     if (c.norm != ARL2_NORM_TOKEN && c.norm != ARL2_NORM_HEAD) return 0;
-    // (with fewer vectors, of queries alone, there are more runs of fewer channels: room for either)
-    size_t most = 0;
-    for (int k = 0; k <= c.kv_heads; k += c.kv_heads) {
-        const int vecs = (cfg.H + k) * cfg.D / 8;
-        const int64_t rows = (int64_t)cfg.B * tokens, runs = rows < block_runs((vecs + 1) / 2) ? rows : block_runs((vecs + 1) / 2);
-        const size_t n = align_up((size_t)runs * vecs * 8 * sizeof(float));
-        if (n > most) most = n;
-    }
-    return most;
+    const int q = cfg.H * cfg.D, k = c.kv_heads * cfg.D;
+    // (queries alone may be narrower rows, of which a CTA has more)
+    const int64_t rows = (int64_t)cfg.B * tokens, most = block_runs(q, kRotateBackVecs), runs = rows < most ? rows : most;
+    return align_up((size_t)runs * (q + k) * sizeof(float));
 }
 
 // What both directions check and fill in; false: refused.
@@ -1533,8 +1528,8 @@ bool rotate_args(const char* who, arl2_ctx* ctx, const arl2_rotation_config* c, 
     }
     a = RotateArgs{};
     a.B = cfg.B; a.T = tokens; a.D = cfg.D; a.rows = cfg.B * tokens;
-    a.q_vecs = cfg.H * cfg.D / 8;
-    a.vecs = a.q_vecs + (with_k ? c->kv_heads * cfg.D / 8 : 0);
+    a.q_width = cfg.H * cfg.D;
+    a.k_width = with_k ? c->kv_heads * cfg.D : 0;
     a.norm = c->norm;
     a.eps = c->eps > 0.0f ? c->eps : 1e-6f;
     a.q_over = c->norm == ARL2_NORM_LENGTH ? 1.0f : 1.0f / (float)(c->norm == ARL2_NORM_TOKEN ? cfg.H * cfg.D : cfg.D);
@@ -1635,7 +1630,7 @@ int arl2_rotate(arl2_ctx* ctx, const arl2_rotation_config* c, const float* d_rop
     if (d_q_out == nullptr || (d_k_out != nullptr) != with_k) { set_error("rotate: q_out, and with k also k_out (else not), must be given"); return ARL2_ERR_INVALID_ARG; }
     if (!aligned16({d_q_out, d_k_out})) { set_error("rotate: outputs must be 16-byte aligned"); return ARL2_ERR_INVALID_ARG; }
     if (outputs_meet("rotate", {d_q_out, d_k_out})) return ARL2_ERR_INVALID_ARG;
-    const int64_t q_row = (int64_t)a.q_vecs * 8, k_row = (int64_t)(a.vecs - a.q_vecs) * 8;
+    const int64_t q_row = a.q_width, k_row = a.k_width;
     auto packed = [&](int64_t batch, int64_t token, int64_t row) { return (a.T == 1 || token == row) && (a.B == 1 || batch == row * a.T); };
     if ((d_q_out == a.q && !packed(a.q_batch, a.q_token, q_row)) || (with_k && (d_k_out == a.q || d_q_out == a.k || (d_k_out == a.k && !packed(a.k_batch, a.k_token, k_row))))) {
         set_error("rotate: an output may be its own input where that is contiguous, and no other");

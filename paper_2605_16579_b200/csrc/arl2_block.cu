@@ -20,170 +20,249 @@ namespace {
 
 constexpr int kMaxDev = 64;
 
-__device__ __forceinline__ int team_channels(int d, int w) { return min(256, d - 256 * w); }   // of warp w of a team, eight a lane
+// Threads of a CTA at most, with that many vectors a lane: rows of 8192 channels
+__host__ __device__ constexpr int row_threads(int vecs) { return vecs >= 4 ? 256 : vecs == 3 ? 352 : 512; }
 
-// Mean and one over the deviation of a row from what its warps know: the mean of each one's channels and the sum of squares
-// about it (zero mean for an RMS norm).  Joined with their differences, so that no digits are lost where the mean is large.
-struct RowStats { float mean, inverse; };
-
-template <bool kDots>
-struct RowSums {
-    RowStats s;
-    float g, gx;   // kDots: sum of g, and of g * (x - mean)
-};
-
-// x, g: this lane's eight channels (zeros where it has none).
-template <bool kDots>
-__device__ __forceinline__ RowSums<kDots> row_sums(Team<4>& team, const float (&x)[8], const float (&g)[8], bool layer, bool active, int d, float eps)
+// Rows in flight, and the one in work: as many as there is room for with CTAs of this many threads, four at most.  `pieces` of 16 bytes that
+// a lane has of a row, `beside`: bytes that it has besides.
+__host__ __device__ constexpr int row_stages(int pieces, int threads, int beside)
 {
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    float mean_w = 0.0f;
-    if (layer) {
-        float s = 0.0f;
+    const int n = ((kMaxSmemPerCta - 2048) / threads - beside) / (16 * pieces);
+    return n < 1 ? 1 : n > 4 ? 4 : n;
+}
+
+// What a lane has of a row: vectors of eight channels, blockDim.x * 8 channels apart.  kFull: every lane has all of them.
+template <int kVecs, bool kFull>
+struct LaneChannels {
+    int c0, d;
+    __device__ __forceinline__ LaneChannels(int width) : c0((int)threadIdx.x * 8), d(width) {}
+    __device__ __forceinline__ int step() const { return (int)blockDim.x * 8; }
+    __device__ __forceinline__ int at(int i) const { return c0 + i * step(); }
+    __device__ __forceinline__ bool has(int i) const { return kFull || at(i) < d; }
+    __device__ __forceinline__ float warp_channels(int warp) const       // that warp `warp` of the team has
+    {
+        if (kFull) return (float)(256 * kVecs);
+        int n = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += x[i];
-        mean_w = warp_sum(s) / (float)team_channels(d, w);
+        for (int i = 0; i < kVecs; ++i) n += max(0, min(256, d - i * step() - warp * 256));
+        return (float)n;
     }
-    float m2 = 0.0f, sg = 0.0f, sgx = 0.0f;
-    if (active) {
+};
+template <int kVecs>
+__device__ __forceinline__ void clear(f2 (&v)[kVecs][4])
+{
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = x[i] - mean_w;
-            m2 = fmaf(c, c, m2);
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = 0;
+}
+
+// Mean of a row and one over its deviation, and (kDots) the sums of g and of g * (x - mean), from what the team's warps know: the
+// mean of each one's channels and the sum of squares about it (about zero for an RMS norm).  Joined with the means' differences, so
+// that no digits are lost where the mean is large.  Channels that a lane does not have are zeros in x and g.
+struct RowSums { float mean, inverse, g, gx; };
+
+template <bool kDots, int kVecs, bool kFull>
+__device__ __forceinline__ RowSums row_sums(Team<4>& team, const f2 (&x)[kVecs][4], const f2 (&g)[kVecs][4], bool layer,
+                                            const LaneChannels<kVecs, kFull>& ch, float over, float eps)
+{
+    float mine[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (layer) {
+        f2 s = 0;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = add2(s, x[i][e]);
+        mine[0] = warp_sum(lo_plus_hi(s)) / ch.warp_channels(threadIdx.x >> 5);
+    }
+    f2 m2 = 0, sg = 0, sgx = 0;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const f2 m = both(ch.has(i) ? -mine[0] : 0.0f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f2 c = add2(x[i][e], m);
+            m2 = fma2(c, c, m2);
             if (kDots) {
-                sg += g[i];
-                sgx = fmaf(g[i], c, sgx);
+                sg = add2(sg, g[i][e]);
+                sgx = fma2(g[i][e], c, sgx);
             }
         }
     }
-    m2 = warp_sum(m2);
+    mine[1] = warp_sum(lo_plus_hi(m2));
     if (kDots) {
-        sg = warp_sum(sg);
-        sgx = warp_sum(sgx);
+        if (layer) mine[2] = warp_sum(lo_plus_hi(sg));
+        mine[3] = warp_sum(lo_plus_hi(sgx));
     }
-    const float mine[4] = {mean_w, m2, sg, sgx};
+    RowSums r;
+    if (team.warps == 1) {
+        r.mean = mine[0];
+        r.inverse = rsqrtf(mine[1] * over + eps);
+        r.g = mine[2];
+        r.gx = mine[3];
+        return r;
+    }
     float of[4];
     team.exchange(mine, of);
-    RowSums<kDots> r;
-    float mean = 0.0f;
+    r.mean = r.g = 0.0f;
     if (layer) {
-        const float n = lane < team.warps ? (float)team_channels(d, lane) : 0.0f;
-        mean = warp_sum(n * of[0]) / (float)d;
-        const float apart = of[0] - mean;
+        const int w = threadIdx.x & (kTeamWarps - 1);
+        const float n = w < team.warps ? ch.warp_channels(w) : 0.0f;
+        r.mean = team_sum(n * of[0]) * over;
+        const float apart = of[0] - r.mean;
         of[1] = fmaf(n * apart, apart, of[1]);
-        if (kDots) of[3] = fmaf(apart, of[2], of[3]);
+        if (kDots) {
+            of[3] = fmaf(apart, of[2], of[3]);
+            r.g = team_sum(of[2]);
+        }
     }
-    r.s.mean = mean;
-    r.s.inverse = rsqrtf(warp_sum(of[1]) / (float)d + eps);
-    if (kDots) {
-        r.g = warp_sum(of[2]);
-        r.gx = warp_sum(of[3]);
-    }
+    r.inverse = rsqrtf(team_sum(of[1]) * over + eps);
+    if (kDots) r.gx = team_sum(of[3]);
     return r;
 }
 
 // ---- modulation ------------------------------------------------------------------------------------------
 __device__ __forceinline__ const float* frame_row(const FrameRows& f, int b, int frame, int c) { return f.p + b * f.batch + frame * f.frame + c; }
 
-// factor[i] = (p ? p[i] (+ 1) : 1) * (w ? w[i] : 1)
-__device__ __forceinline__ void load_factor(float (&out)[8], const FrameRows& f, int b, int frame, int c, float add, const float* weight)
+// (p ? p (+ 1) : 1) * (w ? w : 1)
+__device__ __forceinline__ void load_factor(f2 (&out)[4], const FrameRows& f, int b, int frame, int c, float add, const float* weight)
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = 1.0f;
+    for (int i = 0; i < 4; ++i) out[i] = both(1.0f);
     if (f.p != nullptr) {
         load_kept(frame_row(f, b, frame, c), out);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] += add;
+        for (int i = 0; i < 4; ++i) out[i] = add2(out[i], both(add));
     }
     if (weight != nullptr) {
-        float w[8];
+        f2 w[4];
         load_kept(weight + c, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] *= w[i];
+        for (int i = 0; i < 4; ++i) out[i] = mul2(out[i], w[i]);
     }
 }
 
-// r = x + gate P(y), n = N(r) w (1 + scale) + shift.  Four units of memory: x and y in, r and n out.
-template <typename T, typename R, int kThreads>
-__global__ void __launch_bounds__(kThreads) modulate_kernel(const ModulateArgs a)
-{
-    __shared__ float place[2][kTeamWarps][4];
-    const int team_id = threadIdx.y, warps = blockDim.x >> 5;
-    Team<4> team{place, team_id * warps, warps, team_id, 0};
-    const int c = threadIdx.x * 8, d = a.d;
-    const bool active = c < d;
-    const long long first = ((long long)blockIdx.x * blockDim.y + team_id) * a.share;
-    const long long last = min(first + a.share, (long long)a.rows);
-    grid_dependency_sync();
-    if (first >= last) return;
-    const T* y = static_cast<const T*>(a.y);
-    const R* x = static_cast<const R*>(a.x);
-    R* r_out = static_cast<R*>(a.r);
-    T* n_out = static_cast<T*>(a.n);
-    const bool has_y = a.y != nullptr, has_n = a.n != nullptr;
-
-    int b = (int)(first / a.T), t = (int)(first - (long long)b * a.T), frame = t / a.frame, left = 0;
-    float gate[8], scale[8], shift[8];
-    Eight<R> xr;
-    Eight<T> yr;
-    xr.zero();
-    yr.zero();
-    if (active) {
-        xr.load(x + first * d + c);
-        if (has_y) yr.load(y + first * d + c);
-    }
-    for (long long row = first; row < last; ++row) {
-        float v[8], u[8];
-        xr.get(v);
-        yr.get(u);
-        if (active && row + 1 < last) {
-            xr.load(x + (row + 1) * d + c);
-            if (has_y) yr.load(y + (row + 1) * d + c);
+// The frame that a run of rows is in: a step per row.
+struct FrameWalk {
+    int b, t, frame, left;        // left: rows of this frame from here on, 0 before the first row and behind a frame's last
+    __device__ __forceinline__ FrameWalk(const ModulateArgs& a, long long row) : b((int)(row / a.T)), t((int)(row - (long long)b * a.T)), frame(t / a.frame), left(0) {}
+    __device__ __forceinline__ void enter(const ModulateArgs& a) { left = min((frame + 1) * a.frame, a.T) - t; }
+    __device__ __forceinline__ void next(const ModulateArgs& a)
+    {
+        if (--left == 0) ++frame;
+        if (++t == a.T) {
+            t = frame = 0;
+            ++b;
         }
-        if (left == 0) {   // the first row of this team, or of a frame
-            left = min((frame + 1) * a.frame, a.T) - t;
-            if (active) {
-                load_factor(gate, a.gate, b, frame, c, 0.0f, a.post_weight);
-                load_factor(scale, a.scale, b, frame, c, 1.0f, a.weight);
-                if (a.shift.p != nullptr) load_kept(frame_row(a.shift, b, frame, c), shift);
-            }
-            if (a.shift.p == nullptr || !active) {
+    }
+};
+
+// r = x + gate P(y), n = N(r) w (1 + scale) + shift.  Four units of memory: x and y in, r and n out.
+template <typename T, typename R> constexpr int kModulatePieces = kPieces<R> + kPieces<T>;
+template <typename T, typename R, int kVecs, bool kFull>
+__global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __grid_constant__ ModulateArgs a)
+{
+    __shared__ __align__(16) float place[2 * kTeamWarps * 4];
+    constexpr int kPer = kModulatePieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
+    extern __shared__ uint4 ring_smem[];
+    RowRing<kVecs * kPer, kRowStages> ring;
+    ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
+    Team<4> team;
+    team.start(place, threadIdx.y);
+    const LaneChannels<kVecs, kFull> ch(a.d);
+    const int first = (int)min(((long long)blockIdx.x * blockDim.y + threadIdx.y) * a.share, (long long)a.rows), rows = min(a.share, a.rows - first);
+    grid_dependency_sync();
+    if (rows <= 0) return;
+    const bool has_y = a.y != nullptr, has_n = a.n != nullptr, has_shift = a.shift.p != nullptr;
+    const float over = 1.0f / (float)a.d;
+    const long long at0 = (long long)first * a.d + ch.c0;
+    const R* x = static_cast<const R*>(a.x) + at0;
+    const T* y = static_cast<const T*>(a.y) + at0;
+    R* r_out = static_cast<R*>(a.r) + at0;
+    T* n_out = static_cast<T*>(a.n) + at0;
+
+    FrameWalk walk(a, first);
+    f2 gate[kVecs][4], scale[kVecs][4], shift[kVecs][4];
+    int to_send = rows;
+    auto send = [&]() {
+        if (--to_send >= 0) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) shift[i] = 0.0f;
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) {
+                    ring.copy8(i * kPer, x + i * ch.step());
+                    if (has_y) ring.copy8(i * kPer + kPieces<R>, y + i * ch.step());
+                }
+            x += a.d;
+            y += a.d;
+        }
+        ring.sent();
+    };
+#pragma unroll
+    for (int i = 0; i + 1 < kRowStages; ++i) send();
+    for (int row = 0; row < rows; ++row) {
+        f2 v[kVecs][4], u[kVecs][4];
+        if (!kFull) {
+            clear(v);
+            clear(u);
+        }
+        send();
+        ring.landed();
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (ch.has(i)) {
+                read8<R>(ring, i * kPer, v[i]);
+                if (has_y) read8<T>(ring, i * kPer + kPieces<R>, u[i]);
+            }
+        ring.done();
+        if (walk.left == 0) {   // the first row of this team, or of a frame
+            walk.enter(a);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) shift[i][e] = 0;
+                if (!ch.has(i)) continue;
+                if (has_y) load_factor(gate[i], a.gate, walk.b, walk.frame, ch.at(i), 0.0f, a.post_weight);
+                if (has_n) load_factor(scale[i], a.scale, walk.b, walk.frame, ch.at(i), 1.0f, a.weight);
+                if (has_n && has_shift) load_kept(frame_row(a.shift, walk.b, walk.frame, ch.at(i)), shift[i]);
             }
         }
         if (has_y) {
             if (a.post_norm != 0) {
-                const RowStats s = row_sums<false>(team, u, u, a.post_norm == kNormLayer, active, d, a.eps).s;
+                const RowSums s = row_sums<false>(team, u, u, a.post_norm == kNormLayer, ch, over, a.eps);
+                const f2 m = both(-s.mean), k = both(s.inverse);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] = (u[i] - s.mean) * s.inverse;
-            }
-            if (active) {
+                for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = fmaf(gate[i], u[i], v[i]);
-                // (rounded to what the stream holds before the norm reads it: the backward pass has nothing else)
-                Eight<R> o;
-                o.set(v);
-                o.store(r_out + row * d + c);
-                o.get(v);
+                    for (int e = 0; e < 4; ++e) u[i][e] = mul2(add2(u[i][e], m), k);
             }
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[i][e] = fma2(gate[i][e], u[i][e], v[i][e]);
+                    // (rounded to what the stream holds before the norm reads it: the backward pass has nothing else)
+                    Eight<R> o;
+                    o.set(v[i]);
+                    o.store(r_out + i * ch.step());
+                    o.get(v[i]);
+                }
+            r_out += a.d;
         }
         if (has_n) {
-            const RowStats s = row_sums<false>(team, v, v, a.norm == kNormLayer, active, d, a.eps).s;
-            if (active) {
+            const RowSums s = row_sums<false>(team, v, v, a.norm == kNormLayer, ch, over, a.eps);
+            const f2 m = both(-s.mean), k = both(s.inverse);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = fmaf((v[i] - s.mean) * s.inverse, scale[i], shift[i]);
-                Eight<T> o;
-                o.set(v);
-                o.store(n_out + row * d + c);
-            }
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[i][e] = fma2(mul2(add2(v[i][e], m), k), scale[i][e], shift[i][e]);
+                    Eight<T> o;
+                    o.set(v[i]);
+                    o.store(n_out + i * ch.step());
+                }
+            n_out += a.d;
         }
-        if (--left == 0) ++frame;
-        if (++t == a.T) {
-            t = 0;
-            frame = 0;
-            ++b;
-        }
+        walk.next(a);
     }
 }
 
@@ -191,156 +270,211 @@ __global__ void __launch_bounds__(kThreads) modulate_kernel(const ModulateArgs a
 //   dx = dr + i (g - hat mean(g hat) - [LayerNorm] mean(g));   dgate = sum dx P(y), dscale = w sum dn hat, dshift = sum dn,
 //   dw = sum (1 + scale) dn hat;   dy = the same of P for the gradient dx gate w_post, dw_post = sum gate dx yhat.
 // Six units of memory: r, dn, dr and y in, dx and dy out.  The weights' sums are made from the frames' sums.
-template <typename T, typename R, int kThreads>
-__global__ void __launch_bounds__(kThreads) modulate_backward_kernel(const ModulateBackArgs a)
+template <typename T, typename R> constexpr int kModulateBackPieces = 2 * kPieces<R> + 2 * kPieces<T>;
+template <typename T, typename R, int kVecs, bool kFull>
+__global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a)
 {
-    __shared__ float place[2][kTeamWarps][4];
-    extern __shared__ float weight_sums[];     // [threads][16]: dw and dw_post of a thread's channels
-    const int team_id = threadIdx.y, warps = blockDim.x >> 5;
-    Team<4> team{place, team_id * warps, warps, team_id, 0};
-    const int c = threadIdx.x * 8, d = a.m.d;
-    const bool active = c < d;
-    const int team_at = (int)blockIdx.x * blockDim.y + team_id;
-    const long long first = (long long)team_at * a.m.share;
-    const long long last = min(first + a.m.share, (long long)a.m.rows);
+    __shared__ __align__(16) float place[2 * kTeamWarps * 4];
+    constexpr int kPer = kModulateBackPieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 64 * kVecs);
+    constexpr int kR = 0, kDr = kPieces<R>, kDn = 2 * kPieces<R>, kY = kDn + kPieces<T>;
+    extern __shared__ uint4 ring_smem[];       // the rows, then [8 kVecs][threads] pairs: dw and dw_post of a thread's channels
+    RowRing<kVecs * kPer, kRowStages> ring;
+    ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
+    Team<4> team;
+    team.start(place, threadIdx.y);
+    const LaneChannels<kVecs, kFull> ch(a.m.d);
+    const int team_at = (int)blockIdx.x * blockDim.y + threadIdx.y, first = (int)min((long long)team_at * a.m.share, (long long)a.m.rows), rows = min(a.m.share, a.m.rows - first);
     grid_dependency_sync();
-    if (first >= last) return;
-    const R* r = static_cast<const R*>(a.m.r);
-    const T* y = static_cast<const T*>(a.m.y);
-    const T* dn = static_cast<const T*>(a.dn);
-    const R* dr = static_cast<const R*>(a.dr);
-    const bool has_y = y != nullptr, has_n = dn != nullptr, has_r = dr != nullptr, has_weights = a.weight_parts != nullptr;
-    float* ws = weight_sums + (team_id * blockDim.x + threadIdx.x);   // (strided by the CTA's threads: no bank conflicts)
-    const int ws_step = blockDim.x * blockDim.y;
+    if (rows <= 0) return;
+    const int d = a.m.d;
+    const float over = 1.0f / (float)d;
+    const long long at0 = (long long)first * d + ch.c0;
+    const R* r = static_cast<const R*>(a.m.r) + at0;
+    const T* y = static_cast<const T*>(a.m.y) + at0;
+    const T* dn = static_cast<const T*>(a.dn) + at0;
+    const R* dr = static_cast<const R*>(a.dr) + at0;
+    R* dx_out = static_cast<R*>(a.dx) + at0;
+    T* dy_out = static_cast<T*>(a.dy) + at0;
+    const bool has_y = a.m.y != nullptr, has_n = a.dn != nullptr, has_r = a.dr != nullptr, has_weights = a.weight_parts != nullptr;
+    const bool layer = a.m.norm == kNormLayer;
+    const int ws_step = blockDim.x * blockDim.y;       // (strided by the CTA's threads: no bank conflicts)
+    f2* ws = reinterpret_cast<f2*>(ring_smem + kVecs * kPer * kRowStages * ws_step) + (threadIdx.y * blockDim.x + threadIdx.x);
+    if (has_weights) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) ws[i * ws_step] = 0.0f;
-
-    int b = (int)(first / a.m.T), t = (int)(first - (long long)b * a.m.T), frame = t / a.m.frame, left = 0;
+        for (int i = 0; i < 8 * kVecs; ++i) ws[i * ws_step] = 0;
+    }
+    FrameWalk walk(a.m, first);
     bool whole = false, at_first = true;
-    float gate[8], scale[8], sum_n[8], sum_hat[8], sum_y[8];
-    Eight<R> rr, drr;
-    Eight<T> yr, dnr;
-    rr.zero(); drr.zero(); yr.zero(); dnr.zero();
-    auto fetch = [&](long long row) {
-        if (!active) return;
-        const long long at = row * d + c;
-        if (has_n) {
-            rr.load(r + at);
-            dnr.load(dn + at);
-        }
-        if (has_r) drr.load(dr + at);
-        if (has_y) yr.load(y + at);
-    };
-    fetch(first);
-    for (long long row = first; row < last; ++row) {
-        float v[8], g[8], u[8], dx[8];
-        rr.get(v);
-        dnr.get(g);
-        drr.get(dx);
-        yr.get(u);
-        if (row + 1 < last) fetch(row + 1);
-        if (left == 0) {
-            left = min((frame + 1) * a.m.frame, a.m.T) - t;
-            whole = t == frame * a.m.frame && row + left <= last;
-            if (active) {
-                load_factor(gate, a.m.gate, b, frame, c, 0.0f, a.m.post_weight);
-                load_factor(scale, a.m.scale, b, frame, c, 1.0f, a.m.weight);
-            }
+    f2 gate[kVecs][4], scale[kVecs][4], sum_n[kVecs][4], sum_hat[kVecs][4], sum_y[kVecs][4];
+    int to_send = rows;
+    auto send = [&]() {
+        if (--to_send >= 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum_n[i] = sum_hat[i] = sum_y[i] = 0.0f;
-        }
-        if (has_n) {
-            float gs[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) gs[i] = active ? g[i] * scale[i] : 0.0f;
-            const RowSums<true> s = row_sums<true>(team, v, gs, a.m.norm == kNormLayer, active, d, a.m.eps);
-            const float mean_g = a.m.norm == kNormLayer ? s.g / (float)d : 0.0f;
-            const float mean_gx = s.gx * s.s.inverse / (float)d;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float hat = (v[i] - s.s.mean) * s.s.inverse;
-                sum_n[i] += g[i];
-                sum_hat[i] = fmaf(g[i], hat, sum_hat[i]);
-                dx[i] = fmaf(s.s.inverse, gs[i] - mean_g - hat * mean_gx, dx[i]);
-            }
-        }
-        if (active) {
-            Eight<R> o;
-            o.set(dx);
-            o.store(static_cast<R*>(a.dx) + row * d + c);
-        }
-        if (has_y) {
-            float dy[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dy[i] = active ? dx[i] * gate[i] : 0.0f;
-            if (a.m.post_norm != 0) {
-                const RowSums<true> s = row_sums<true>(team, u, dy, a.m.post_norm == kNormLayer, active, d, a.m.eps);
-                const float mean_g = a.m.post_norm == kNormLayer ? s.g / (float)d : 0.0f;
-                const float mean_gx = s.gx * s.s.inverse / (float)d;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    u[i] = (u[i] - s.s.mean) * s.s.inverse;
-                    dy[i] = s.s.inverse * (dy[i] - mean_g - u[i] * mean_gx);
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) {
+                    if (has_n) {
+                        ring.copy8(i * kPer + kR, r + i * ch.step());
+                        ring.copy8(i * kPer + kDn, dn + i * ch.step());
+                    }
+                    if (has_r) ring.copy8(i * kPer + kDr, dr + i * ch.step());
+                    if (has_y) ring.copy8(i * kPer + kY, y + i * ch.step());
                 }
-            }
-            if (active) {
+            r += d;
+            dn += d;
+            dr += d;
+            y += d;
+        }
+        ring.sent();
+    };
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum_y[i] = fmaf(dx[i], u[i], sum_y[i]);
+    for (int i = 0; i + 1 < kRowStages; ++i) send();
+    for (int row = 0; row < rows; ++row) {
+        f2 dx[kVecs][4], u[kVecs][4];
+        clear(dx);
+        if (!kFull) clear(u);
+        send();
+        ring.landed();
+        if (walk.left == 0) {
+            walk.enter(a.m);
+            whole = walk.t == walk.frame * a.m.frame && row + walk.left <= rows;
+            clear(sum_n);
+            clear(sum_hat);
+            clear(sum_y);
+            if (!kFull) {
+                clear(gate);
+                clear(scale);
+            }
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                if (!ch.has(i)) continue;
+                if (has_y) load_factor(gate[i], a.m.gate, walk.b, walk.frame, ch.at(i), 0.0f, a.m.post_weight);
+                if (has_n) load_factor(scale[i], a.m.scale, walk.b, walk.frame, ch.at(i), 1.0f, a.m.weight);
+            }
+        }
+        if (has_r) {
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) read8<R>(ring, i * kPer + kDr, dx[i]);
+        }
+        if (has_n) {
+            f2 v[kVecs][4], g[kVecs][4];
+            if (!kFull) {
+                clear(v);
+                clear(g);
+            }
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) {
+                    read8<R>(ring, i * kPer + kR, v[i]);
+                    read8<T>(ring, i * kPer + kDn, g[i]);
+                }
+            f2 gs[kVecs][4];
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    gs[i][e] = mul2(g[i][e], scale[i][e]);
+                    sum_n[i][e] = add2(sum_n[i][e], g[i][e]);
+                }
+            const RowSums s = row_sums<true>(team, v, gs, layer, ch, over, a.m.eps);
+            // dx = dr + i gs - i mean(g) - hat i mean(g hat)
+            const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * over * s.inverse), mean_gx = both(-s.gx * s.inverse * over * s.inverse);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f2 hat = mul2(add2(v[i][e], m), k);
+                    sum_hat[i][e] = fma2(g[i][e], hat, sum_hat[i][e]);
+                    dx[i][e] = fma2(hat, mean_gx, fma2(gs[i][e], k, add2(dx[i][e], mean_g)));
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (ch.has(i)) {
+                if (has_y) read8<T>(ring, i * kPer + kY, u[i]);
+                Eight<R> o;
+                o.set(dx[i]);
+                o.store(dx_out + i * ch.step());
+            }
+        ring.done();
+        dx_out += d;
+        if (has_y) {
+            f2 dy[kVecs][4];
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dy[i][e] = mul2(dx[i][e], gate[i][e]);
+            if (a.m.post_norm != 0) {
+                const RowSums s = row_sums<true>(team, u, dy, a.m.post_norm == kNormLayer, ch, over, a.m.eps);
+                const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * over * s.inverse), mean_gx = both(-s.gx * s.inverse * over * s.inverse);
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        u[i][e] = mul2(add2(u[i][e], m), k);
+                        dy[i][e] = fma2(u[i][e], mean_gx, fma2(dy[i][e], k, mean_g));
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum_y[i][e] = fma2(dx[i][e], u[i][e], sum_y[i][e]);
+                if (!ch.has(i)) continue;
                 Eight<T> o;
-                o.set(dy);
-                o.store(static_cast<T*>(a.dy) + row * d + c);
+                o.set(dy[i]);
+                o.store(dy_out + i * ch.step());
             }
+            dy_out += d;
         }
-        --left;
-        if ((left == 0 || row + 1 == last) && active) {   // the end of a frame, or of this team's part of it
-            if (has_weights) {
-                float f[8];
-                load_factor(f, a.m.scale, b, frame, c, 1.0f, nullptr);
+        if (walk.left == 1 || row + 1 == rows) {   // the end of a frame, or of this team's part of it
+            const long long frame_at = ((long long)walk.b * a.frames + walk.frame) * d, slot = ((long long)team_at * 2 + (at_first ? 0 : 1)) * 3 * d;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ws[i * ws_step] += f[i] * sum_hat[i];
-                load_factor(f, a.m.gate, b, frame, c, 0.0f, nullptr);
+            for (int i = 0; i < kVecs; ++i) {
+                if (!ch.has(i)) continue;
+                const int c = ch.at(i);
+                f2 f[4];
+                if (has_weights) {
+                    load_factor(f, a.m.scale, walk.b, walk.frame, c, 1.0f, nullptr);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ws[(8 + i) * ws_step] += f[i] * sum_y[i];
+                    for (int e = 0; e < 4; ++e) ws[(i * 8 + e) * ws_step] = fma2(f[e], sum_hat[i][e], ws[(i * 8 + e) * ws_step]);
+                    load_factor(f, a.m.gate, walk.b, walk.frame, c, 0.0f, nullptr);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ws[(i * 8 + 4 + e) * ws_step] = fma2(f[e], sum_y[i][e], ws[(i * 8 + 4 + e) * ws_step]);
+                }
+                const FrameRows none{nullptr, 0, 0};
+                load_factor(f, none, 0, 0, c, 0.0f, a.m.weight);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum_hat[i][e] = mul2(sum_hat[i][e], f[e]);
+                load_factor(f, none, 0, 0, c, 0.0f, a.m.post_weight);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum_y[i][e] = mul2(sum_y[i][e], f[e]);
+                Eight<float> o;
+                auto put = [&](const f2 (&s)[4], float* whole_to, int which) {
+                    o.set(s);
+                    if (!whole) o.store(a.parts + slot + (long long)which * d + c);
+                    else if (whole_to != nullptr) o.store(whole_to + frame_at + c);
+                };
+                put(sum_y[i], a.dgate, 0);
+                put(sum_hat[i], a.dscale, 1);
+                put(sum_n[i], a.dshift, 2);
             }
-            const FrameRows none{nullptr, 0, 0};
-            float f[8];
-            load_factor(f, none, 0, 0, c, 0.0f, a.m.weight);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum_hat[i] *= f[i];
-            load_factor(f, none, 0, 0, c, 0.0f, a.m.post_weight);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum_y[i] *= f[i];
-            const long long at = ((long long)b * a.frames + frame) * d + c;
-            const long long slot = ((long long)team_at * 2 + (at_first ? 0 : 1)) * 3 * d + c;
-            Eight<float> o;
-            auto put = [&](const float (&s)[8], float* whole_to, int which) {
-                o.set(s);
-                if (!whole) o.store(a.parts + slot + (long long)which * d);
-                else if (whole_to != nullptr) o.store(whole_to + at);
-            };
-            put(sum_y, a.dgate, 0);
-            put(sum_hat, a.dscale, 1);
-            put(sum_n, a.dshift, 2);
-        }
-        if (left == 0) {
-            ++frame;
             at_first = false;
         }
-        if (++t == a.m.T) {
-            t = 0;
-            frame = 0;
-            ++b;
-        }
+        walk.next(a.m);
     }
-    if (has_weights && active) {
+    if (has_weights) {
         Eight<float> o;
-        float f[8];
+        f2 f[4];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int i = 0; i < kVecs; ++i) {
+            if (!ch.has(i)) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = ws[(8 * k + i) * ws_step];
-            o.set(f);
-            o.store(a.weight_parts + ((long long)team_at * 2 + k) * d + c);
+            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = ws[(i * 8 + 4 * k + e) * ws_step];
+                o.set(f);
+                o.store(a.weight_parts + ((long long)team_at * 2 + k) * d + ch.at(i));
+            }
         }
     }
 }
@@ -374,7 +508,7 @@ __device__ __forceinline__ float4 add_parts(const float* p, long long step, int 
 }
 
 // blockIdx.x: a frame (or, where there are fewer runs than frames, the start of a run), and one more for the weights; z: which sum
-__global__ void __launch_bounds__(kAddLanes* kAddSlices) modulate_sums_kernel(const ModulateBackArgs a, const int by_frame, const int units, const int teams)
+__global__ void __launch_bounds__(kAddLanes* kAddSlices) modulate_sums_kernel(const __grid_constant__ ModulateBackArgs a, const int by_frame, const int units, const int teams)
 {
     grid_dependency_sync();
     const int c = (blockIdx.y * kAddLanes + threadIdx.x) * 4, d = a.m.d;
@@ -415,6 +549,33 @@ __global__ void __launch_bounds__(kAddLanes* kAddSlices) modulate_sums_kernel(co
 }
 
 // ---- rotation ------------------------------------------------------------------------------------------------
+// Queries and keys are runs of rows of their own: the first `q_ctas` CTAs have the queries'.
+struct RotateSide {
+    bool keys;
+    int width;           // channels of a row
+    const void* x;
+    int64_t batch, token;
+    const float* weight;
+    float over;
+    int first, rows, team;   // this team's run; its number among the tensor's
+};
+__device__ __forceinline__ RotateSide rotate_side(const RotateArgs& a)
+{
+    RotateSide s;
+    s.keys = (int)blockIdx.x >= a.q_ctas;
+    s.width = s.keys ? a.k_width : a.q_width;
+    s.x = s.keys ? a.k : a.q;
+    s.batch = s.keys ? a.k_batch : a.q_batch;
+    s.token = s.keys ? a.k_token : a.q_token;
+    s.weight = s.keys ? a.k_weight : a.q_weight;
+    s.over = s.keys ? a.k_over : a.q_over;
+    const int share = s.keys ? a.k_share : a.q_share;
+    s.team = ((int)blockIdx.x - (s.keys ? a.q_ctas : 0)) * blockDim.y + threadIdx.y;
+    s.first = (int)min((long long)s.team * share, (long long)a.rows);
+    s.rows = min(share, a.rows - s.first);
+    return s;
+}
+
 // Row of the tables for a position: the first for those before it, the last for those behind, which is reported.
 __device__ __forceinline__ int table_row(int at, const RotateArgs& a, int b)
 {
@@ -425,306 +586,388 @@ __device__ __forceinline__ int table_row(int at, const RotateArgs& a, int b)
     return max(at, 0);
 }
 
-// cos and sin of four pairs of the row's token, from pair m on; pairs past the axes do not turn.
-__device__ __forceinline__ void load_angles(const RotateArgs& a, int b, int t, long long row, int m, float (&cs)[4], float (&sn)[4])
-{
-    int at[3];
-    if (a.positions != nullptr) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) at[i] = a.positions[row * 3 + i];
-    } else {
-        const int area = a.grid_rows * a.grid_columns, frame = t / area, in = t - frame * area;
-        at[0] = (int)min((long long)(a.start != nullptr ? a.start[b] : 0) + frame, 0x7fffffffLL);
-        at[1] = in / a.grid_columns;
-        at[2] = in - at[1] * a.grid_columns;
+// The token that a run of rows is at, and its place in the grid: a step per row, without divisions.
+struct TokenWalk {
+    int b, t, frame, line, column;
+    __device__ __forceinline__ TokenWalk(const RotateArgs& a, int row) : b(row / a.T), t(row - b * a.T)
+    {
+        const int area = a.grid_rows * a.grid_columns, in = t - t / area * area;
+        frame = t / area;
+        line = in / a.grid_columns;
+        column = in - line * a.grid_columns;
     }
-    const int end0 = a.pairs[0], end1 = end0 + a.pairs[1], end2 = end1 + a.pairs[2], half = a.D / 2;
+    __device__ __forceinline__ void next(const RotateArgs& a)
+    {
+        if (++column == a.grid_columns) {
+            column = 0;
+            if (++line == a.grid_rows) {
+                line = 0;
+                ++frame;
+            }
+        }
+        if (++t == a.T) {
+            t = frame = line = column = 0;
+            ++b;
+        }
+    }
+};
+
+// cos and sin of the four pairs that a lane has of each head, pair m on.  Which axes turn them is the lane's own for all rows: most
+// lanes have one, those where an axis ends two; three or more changes within four pairs only where an axis has fewer than three pairs.
+constexpr int kNoAxis = 3;
+struct Angles {
+    int m, axis, other, split;    // pairs below `split` go by `axis`, the others by `other`
+    bool many;                    // ... unless there are more changes: then by axis_of
+    __device__ __forceinline__ static int axis_of(const RotateArgs& a, int pair)
+    {
+        return pair < a.pairs[0] ? 0 : pair < a.pairs[0] + a.pairs[1] ? 1 : pair < a.pairs[0] + a.pairs[1] + a.pairs[2] ? 2 : kNoAxis;
+    }
+    __device__ __forceinline__ Angles(const RotateArgs& a, int pair) : m(pair), split(4), many(false)
+    {
+        axis = axis_of(a, m);
+        other = axis_of(a, m + 3);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { cs[i] = 1.0f; sn[i] = 0.0f; }
+        for (int i = 3; i >= 1; --i) {
+            const int x = axis_of(a, m + i);
+            if (x != axis) split = i;
+            many |= x != axis && x != other;
+        }
+        many = __any_sync(0xffffffffu, many);
+    }
+    __device__ __forceinline__ void load(const RotateArgs& a, const TokenWalk& w, float (&cs)[4], float (&sn)[4]) const
+    {
+        int at[3];
+        if (a.positions != nullptr) {
+            const int32_t* p = a.positions + ((long long)w.b * a.T + w.t) * 3;
 #pragma unroll
-    for (int x = 0; x < 3; ++x) {
-        const int from = x == 0 ? 0 : x == 1 ? end0 : end1, to = x == 0 ? end0 : x == 1 ? end1 : end2;
-        if (m < to && m + 4 > from) {
-            const long long o = (long long)table_row(at[x], a, b) * half + m;
+            for (int i = 0; i < 3; ++i) at[i] = p[i];
+        } else {
+            at[0] = (int)min((long long)(a.start != nullptr ? a.start[w.b] : 0) + w.frame, 0x7fffffffLL);
+            at[1] = w.line;
+            at[2] = w.column;
+        }
+        auto fetch = [&](int x, float (&c)[4], float (&s)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
+            if (x == kNoAxis) return;
+            const long long o = (long long)table_row(x == 0 ? at[0] : x == 1 ? at[1] : at[2], a, w.b) * (a.D / 2) + m;
             const float4 c4 = *reinterpret_cast<const float4*>(a.cos + o), s4 = *reinterpret_cast<const float4*>(a.sin + o);
-            const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+            c[0] = c4.x; c[1] = c4.y; c[2] = c4.z; c[3] = c4.w;
+            s[0] = s4.x; s[1] = s4.y; s[2] = s4.z; s[3] = s4.w;
+        };
+        fetch(axis, cs, sn);
+        if (split < 4) {
+            float c[4], s[4];
+            fetch(other, c, s);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (m + i >= from && m + i < to) {
+            for (int i = 1; i < 4; ++i)
+                if (i >= split) {
                     cs[i] = c[i];
                     sn[i] = s[i];
                 }
         }
+        if (many) {
+#pragma unroll
+            for (int i = 1; i < 3; ++i) {
+                const int x = axis_of(a, m + i);
+                if (x == axis || x == other) continue;
+                float c[4], s[4];
+                fetch(x, c, s);
+                cs[i] = c[i];
+                sn[i] = s[i];
+            }
+        }
     }
-}
+};
 
 // The sum over the lanes that hold a head, `lanes` of them side by side.
 __device__ __forceinline__ float head_sum(float v, int lanes)
 {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    if (lanes == 16) v += __shfl_xor_sync(0xffffffffu, v, 8);
+    v += __shfl_xor_sync(0xffffffffu, v, 4);
+    v += __shfl_xor_sync(0xffffffffu, v, 2);
+    return v + __shfl_xor_sync(0xffffffffu, v, 1);
 }
 
-// Where the vectors of a lane are: queries and keys are one row of (H + kv_heads) * D channels.
-struct RotateLane {
-    bool active, is_q;
-    int c;        // channel in its tensor
-};
-__device__ __forceinline__ RotateLane rotate_lane(const RotateArgs& a, int i)
+__device__ __forceinline__ void rotate_weight(const RotateArgs& a, const RotateSide& s, int c, bool has, f2 (&w)[4])
 {
-    const int v = i * blockDim.x + threadIdx.x;
-    RotateLane l;
-    l.is_q = v < a.q_vecs;
-    l.active = v < a.vecs;
-    l.c = (l.is_q ? v : v - a.q_vecs) * 8;
-    return l;
-}
-
-__device__ __forceinline__ void rotate_weight(const RotateArgs& a, const RotateLane& l, float (&w)[8])
-{
-    const float* p = l.is_q ? a.q_weight : a.k_weight;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = 1.0f;
-    if (l.active && p != nullptr) load_kept(p + (a.norm == kNormHead ? l.c % a.D : l.c), w);
+    for (int e = 0; e < 4; ++e) w[e] = both(1.0f);
+    if (has && s.weight != nullptr) load_kept(s.weight + (a.norm == kNormHead ? c % a.D : c), w);
+}
+__device__ __forceinline__ f2 swapped(f2 v)
+{
+    float lo, hi;
+    apart(v, lo, hi);
+    return pair(hi, lo);
 }
 
-// y = R(w x / length).  Two units of memory.
-template <typename T, int kVecs, int kThreads>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a)
+// y = R(w x / length).  Two units of memory.  A pair (p, q) turned: (p, q) (c, c) + (q, p) (-s, s).
+template <typename T, int kVecs, bool kFull>
+__global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid_constant__ RotateArgs a)
 {
-    __shared__ float place[2][kTeamWarps][2];
-    const int team_id = threadIdx.y, warps = blockDim.x >> 5, lanes = a.D / 8;
-    Team<2> team{place, team_id * warps, warps, team_id, 0};
-    const long long first = ((long long)blockIdx.x * blockDim.y + team_id) * a.share;
-    const long long last = min(first + a.share, (long long)a.rows);
+    __shared__ float place[2 * kTeamWarps];
+    constexpr int kPer = kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
+    extern __shared__ uint4 ring_smem[];
+    RowRing<kVecs * kPer, kRowStages> ring;
+    ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
+    Team<1> team;
+    team.start(place, threadIdx.y);
+    const RotateSide side = rotate_side(a);
+    const LaneChannels<kVecs, kFull> ch(side.width);
+    const int lanes = a.D / 8;
     grid_dependency_sync();
-    if (first >= last) return;
-    RotateLane l[kVecs];
-    float w[kVecs][8];
-    Eight<T> raw[kVecs];
+    if (side.rows <= 0) return;
+    f2 w[kVecs][4];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        l[i] = rotate_lane(a, i);
-        rotate_weight(a, l[i], w[i]);
-        raw[i].zero();
-    }
-    auto fetch = [&](int b, int t) {
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-            if (l[i].active) raw[i].load(static_cast<const T*>(l[i].is_q ? a.q : a.k) + (l[i].is_q ? b * a.q_batch + t * a.q_token : b * a.k_batch + t * a.k_token) + l[i].c);
-    };
-    int b = (int)(first / a.T), t = (int)(first - (long long)b * a.T);
-    fetch(b, t);
-    for (long long row = first; row < last; ++row) {
-        float x[kVecs][8], cs[4], sn[4];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) raw[i].get(x[i]);
-        load_angles(a, b, t, row, (threadIdx.x % lanes) * 4, cs, sn);
-        if (++t == a.T) {
-            t = 0;
-            ++b;
-        }
-        if (row + 1 < last) fetch(b, t);
-        if (a.norm != 0) {
-            float ss[kVecs];
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                ss[i] = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss[i] = fmaf(x[i][e], x[i][e], ss[i]);
-            }
-            if (a.norm == kNormToken) {
-                float mine[2] = {0.0f, 0.0f}, of[2];
-#pragma unroll
-                for (int i = 0; i < kVecs; ++i) mine[l[i].is_q ? 0 : 1] += ss[i];
-                mine[0] = warp_sum(mine[0]);
-                mine[1] = warp_sum(mine[1]);
-                team.exchange(mine, of);
-                const float iq = rsqrtf(warp_sum(of[0]) * a.q_over + a.eps), ik = rsqrtf(warp_sum(of[1]) * a.k_over + a.eps);
-#pragma unroll
-                for (int i = 0; i < kVecs; ++i) ss[i] = l[i].is_q ? iq : ik;
-            } else {
-#pragma unroll
-                for (int i = 0; i < kVecs; ++i) ss[i] = rsqrtf(head_sum(ss[i], lanes) * a.q_over + a.eps);
-            }
+    for (int i = 0; i < kVecs; ++i) rotate_weight(a, side, ch.at(i), ch.has(i), w[i]);
+    TokenWalk walk(a, side.first);
+    const Angles angles(a, (threadIdx.x % lanes) * 4);
+    const T* x_in = static_cast<const T*>(side.x) + walk.b * side.batch + walk.t * side.token + ch.c0;
+    T* out = static_cast<T*>(side.keys ? a.k_out : a.q_out) + (long long)side.first * side.width + ch.c0;
+    const int64_t wrap = side.batch - (a.T - 1) * side.token;       // from a stream's last row to the next one's first
+    int to_send = side.rows, sent_t = walk.t;
+    auto send = [&]() {
+        if (--to_send >= 0) {
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) ring.copy8(i * kPer, x_in + i * ch.step());
+            const bool last = ++sent_t == a.T;
+            x_in += last ? wrap : side.token;
+            if (last) sent_t = 0;
+        }
+        ring.sent();
+    };
+    const bool weighted = side.weight != nullptr;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] *= ss[i] * w[i][e];
+    for (int i = 0; i + 1 < kRowStages; ++i) send();
+    for (int row = 0; row < side.rows; ++row) {
+        f2 x[kVecs][4];
+        float cs[4], sn[4];
+        if (!kFull) clear(x);
+        angles.load(a, walk, cs, sn);
+        send();
+        ring.landed();
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (ch.has(i)) read8<T>(ring, i * kPer, x[i]);
+        ring.done();
+        if (a.norm != 0) {
+            f2 ss[kVecs];
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                ss[i] = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ss[i] = fma2(x[i][e], x[i][e], ss[i]);
+            }
+            if (a.norm == kNormToken) {
+#pragma unroll
+                for (int i = 1; i < kVecs; ++i) ss[0] = add2(ss[0], ss[i]);
+                float all = warp_sum(lo_plus_hi(ss[0]));
+                if (team.warps > 1) {
+                    const float mine[1] = {all};
+                    float of[1];
+                    team.exchange(mine, of);
+                    all = team_sum(of[0]);
+                }
+                // (the length goes into the angles, once for all the lane's heads)
+                const float inverse = rsqrtf(all * side.over + a.eps);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    cs[m] *= inverse;
+                    sn[m] *= inverse;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i) {
+                    const f2 inverse = both(rsqrtf(head_sum(lo_plus_hi(ss[i]), lanes) * side.over + a.eps));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][e] = mul2(x[i][e], inverse);
+                }
+            }
+            if (weighted) {
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][e] = mul2(x[i][e], w[i][e]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-            if (!l[i].active) continue;
-            float o[8];
+            if (!ch.has(i)) continue;
+            f2 o[4];
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                o[2 * m] = x[i][2 * m] * cs[m] - x[i][2 * m + 1] * sn[m];
-                o[2 * m + 1] = x[i][2 * m] * sn[m] + x[i][2 * m + 1] * cs[m];
-            }
-            Eight<T> out;
-            out.set(o);
-            out.store(static_cast<T*>(l[i].is_q ? a.q_out : a.k_out) + row * (l[i].is_q ? a.q_vecs : a.vecs - a.q_vecs) * 8 + l[i].c);
+            for (int m = 0; m < 4; ++m) o[m] = fma2(x[i][m], both(cs[m]), mul2(swapped(x[i][m]), pair(-sn[m], sn[m])));
+            Eight<T> e8;
+            e8.set(o);
+            e8.store(out + i * ch.step());
         }
+        out += side.width;
+        walk.next(a);
     }
 }
 
 // With g = R^T dy, hat = x / length (its inverse i), G = w g:  dx = i (G - hat mean(G hat)), dw = sum g hat; the mean is a sum for
 // rows of length one.  Without a norm dx = g, and x is not looked at.  Three units of memory, or two.
-template <typename T, int kVecs, int kThreads>
-__global__ void __launch_bounds__(kThreads) rotate_backward_kernel(const RotateBackArgs a)
+template <typename T, int kVecs, bool kFull>
+__global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(const __grid_constant__ RotateBackArgs a)
 {
-    __shared__ float place[2][kTeamWarps][4];
-    const int team_id = threadIdx.y, warps = blockDim.x >> 5, lanes = a.r.D / 8;
-    Team<4> team{place, team_id * warps, warps, team_id, 0};
-    const int team_at = (int)blockIdx.x * blockDim.y + team_id;
-    const long long first = (long long)team_at * a.r.share;
-    const long long last = min(first + a.r.share, (long long)a.r.rows);
+    __shared__ __align__(16) float place[2 * kTeamWarps * 2];
+    constexpr int kPer = 2 * kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
+    extern __shared__ uint4 ring_smem[];
+    RowRing<kVecs * kPer, kRowStages> ring;
+    ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
+    Team<2> team;
+    team.start(place, threadIdx.y);
+    const RotateSide side = rotate_side(a.r);
+    const LaneChannels<kVecs, kFull> ch(side.width);
+    const int lanes = a.r.D / 8;
     grid_dependency_sync();
-    if (first >= last) return;
-    const bool normed = a.r.norm != 0;
-    RotateLane l[kVecs];
-    float w[kVecs][8], sum[kVecs][8];
-    Eight<T> xr[kVecs], gr[kVecs];
+    if (side.rows <= 0) return;
+    const bool normed = a.r.norm != 0, weighted = side.weight != nullptr;
+    f2 w[kVecs][4], sum[kVecs][4];
+    clear(sum);
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        l[i] = rotate_lane(a.r, i);
-        rotate_weight(a.r, l[i], w[i]);
-        xr[i].zero();
-        gr[i].zero();
+    for (int i = 0; i < kVecs; ++i) rotate_weight(a.r, side, ch.at(i), ch.has(i), w[i]);
+    TokenWalk walk(a.r, side.first);
+    const Angles angles(a.r, (threadIdx.x % lanes) * 4);
+    const long long at0 = (long long)side.first * side.width + ch.c0;
+    const T* g_in = static_cast<const T*>(side.keys ? a.dk_out : a.dq_out) + at0;
+    T* out = static_cast<T*>(side.keys ? a.dk : a.dq) + at0;
+    const T* x_in = static_cast<const T*>(side.x) + walk.b * side.batch + walk.t * side.token + ch.c0;
+    const int64_t wrap = side.batch - (a.r.T - 1) * side.token;
+    int to_send = side.rows, sent_t = walk.t;
+    auto send = [&]() {
+        if (--to_send >= 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[i][e] = 0.0f;
-    }
-    const int k_vecs = a.r.vecs - a.r.q_vecs;
-    auto fetch = [&](int b, int t, long long row) {
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (!l[i].active) continue;
-            gr[i].load(static_cast<const T*>(l[i].is_q ? a.dq_out : a.dk_out) + row * (l[i].is_q ? a.r.q_vecs : k_vecs) * 8 + l[i].c);
-            if (normed)
-                xr[i].load(static_cast<const T*>(l[i].is_q ? a.r.q : a.r.k) + (l[i].is_q ? b * a.r.q_batch + t * a.r.q_token : b * a.r.k_batch + t * a.r.k_token) + l[i].c);
+            for (int i = 0; i < kVecs; ++i)
+                if (ch.has(i)) {
+                    ring.copy8(i * kPer, g_in + i * ch.step());
+                    if (normed) ring.copy8(i * kPer + kPieces<T>, x_in + i * ch.step());
+                }
+            g_in += side.width;
+            const bool last = ++sent_t == a.r.T;
+            x_in += last ? wrap : side.token;
+            if (last) sent_t = 0;
         }
+        ring.sent();
     };
-    int b = (int)(first / a.r.T), t = (int)(first - (long long)b * a.r.T);
-    fetch(b, t, first);
-    for (long long row = first; row < last; ++row) {
-        float x[kVecs][8], g[kVecs][8], cs[4], sn[4];
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            xr[i].get(x[i]);
-            gr[i].get(g[i]);
+    for (int i = 0; i + 1 < kRowStages; ++i) send();
+    for (int row = 0; row < side.rows; ++row) {
+        f2 x[kVecs][4], g[kVecs][4];
+        float cs[4], sn[4];
+        if (!kFull) {
+            clear(x);
+            clear(g);
         }
-        load_angles(a.r, b, t, row, (threadIdx.x % lanes) * 4, cs, sn);
-        if (++t == a.r.T) {
-            t = 0;
-            ++b;
-        }
-        if (row + 1 < last) fetch(b, t, row + 1);
+        angles.load(a.r, walk, cs, sn);
+        send();
+        ring.landed();
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {   // turned back
-                const float p = g[i][2 * m], q = g[i][2 * m + 1];
-                g[i][2 * m] = p * cs[m] + q * sn[m];
-                g[i][2 * m + 1] = q * cs[m] - p * sn[m];
+            if (ch.has(i)) {
+                read8<T>(ring, i * kPer, g[i]);
+                if (normed) read8<T>(ring, i * kPer + kPieces<T>, x[i]);
             }
+        ring.done();
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {   // turned back
+            const f2 c = both(cs[m]), s = pair(sn[m], -sn[m]);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) g[i][m] = fma2(g[i][m], c, mul2(swapped(g[i][m]), s));
+        }
         if (normed) {
-            float inverse[kVecs], dot[kVecs];
+            f2 ss[kVecs], dot[kVecs];
 #pragma unroll
             for (int i = 0; i < kVecs; ++i) {
-                inverse[i] = dot[i] = 0.0f;
+                ss[i] = dot[i] = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    inverse[i] = fmaf(x[i][e], x[i][e], inverse[i]);
-                    dot[i] = fmaf(g[i][e] * w[i][e], x[i][e], dot[i]);
+                for (int e = 0; e < 4; ++e) {
+                    ss[i] = fma2(x[i][e], x[i][e], ss[i]);
+                    const f2 gx = mul2(g[i][e], x[i][e]);
+                    dot[i] = weighted ? fma2(gx, w[i][e], dot[i]) : add2(dot[i], gx);
                 }
             }
+            float inverse[kVecs], mean[kVecs];      // (mean: of G hat, times the inverse)
             if (a.r.norm == kNormToken) {
-                float mine[4] = {0.0f, 0.0f, 0.0f, 0.0f}, of[4];
 #pragma unroll
-                for (int i = 0; i < kVecs; ++i) {
-                    mine[0] += l[i].is_q ? inverse[i] : 0.0f;
-                    mine[1] += l[i].is_q ? 0.0f : inverse[i];
-                    mine[2] += l[i].is_q ? dot[i] : 0.0f;
-                    mine[3] += l[i].is_q ? 0.0f : dot[i];
+                for (int i = 1; i < kVecs; ++i) {
+                    ss[0] = add2(ss[0], ss[i]);
+                    dot[0] = add2(dot[0], dot[i]);
                 }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mine[k] = warp_sum(mine[k]);
-                team.exchange(mine, of);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) of[k] = warp_sum(of[k]);
-                const float iq = rsqrtf(of[0] * a.r.q_over + a.r.eps), ik = rsqrtf(of[1] * a.r.k_over + a.r.eps);
+                float mine[2] = {warp_sum(lo_plus_hi(ss[0])), warp_sum(lo_plus_hi(dot[0]))};
+                if (team.warps > 1) {
+                    float of[2];
+                    team.exchange(mine, of);
+                    mine[0] = team_sum(of[0]);
+                    mine[1] = team_sum(of[1]);
+                }
+                const float i0 = rsqrtf(mine[0] * side.over + a.r.eps);
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i) {
-                    inverse[i] = l[i].is_q ? iq : ik;
-                    dot[i] = l[i].is_q ? of[2] * a.r.q_over : of[3] * a.r.k_over;
+                    inverse[i] = i0;
+                    mean[i] = mine[1] * side.over * i0 * i0;
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i) {
-                    inverse[i] = rsqrtf(head_sum(inverse[i], lanes) * a.r.q_over + a.r.eps);
-                    dot[i] = head_sum(dot[i], lanes) * a.r.q_over;
+                    inverse[i] = rsqrtf(head_sum(lo_plus_hi(ss[i]), lanes) * side.over + a.r.eps);
+                    mean[i] = head_sum(lo_plus_hi(dot[i]), lanes) * side.over * inverse[i] * inverse[i];
                 }
             }
 #pragma unroll
             for (int i = 0; i < kVecs; ++i) {
-                const float mean = dot[i] * inverse[i];     // of G hat
+                const f2 k = both(inverse[i]), mn = both(-mean[i]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float hat = x[i][e] * inverse[i];
-                    sum[i][e] = fmaf(g[i][e], hat, sum[i][e]);
-                    g[i][e] = inverse[i] * (g[i][e] * w[i][e] - hat * mean);
+                for (int e = 0; e < 4; ++e) {
+                    const f2 hat = mul2(x[i][e], k);
+                    sum[i][e] = fma2(g[i][e], hat, sum[i][e]);
+                    if (weighted) g[i][e] = mul2(g[i][e], w[i][e]);
+                    g[i][e] = fma2(g[i][e], k, mul2(hat, mn));
                 }
             }
         }
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (!l[i].active) continue;
-            Eight<T> o;
-            o.set(g[i]);
-            o.store(static_cast<T*>(l[i].is_q ? a.dq : a.dk) + row * (l[i].is_q ? a.r.q_vecs : k_vecs) * 8 + l[i].c);
-        }
+        for (int i = 0; i < kVecs; ++i)
+            if (ch.has(i)) {
+                Eight<T> o;
+                o.set(g[i]);
+                o.store(out + i * ch.step());
+            }
+        out += side.width;
+        walk.next(a.r);
     }
-    if (a.parts != nullptr) {
+    if (a.parts == nullptr) return;
+    float* part = a.parts + (side.keys ? (long long)a.q_runs * a.r.q_width : 0) + (long long)side.team * side.width;
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (!l[i].active) continue;
+    for (int i = 0; i < kVecs; ++i)
+        if (ch.has(i)) {
             Eight<float> o;
             o.set(sum[i]);
-            o.store(a.parts + (long long)team_at * a.r.vecs * 8 + (l[i].is_q ? 0 : a.r.q_vecs * 8) + l[i].c);
+            o.store(part + ch.at(i));
         }
-    }
 }
 
 // The gradients of the weights: y = 0 for the queries', 1 for the keys'; a weight per head is shared by the heads, whose parts
-// follow one another in a team's row.
-__global__ void __launch_bounds__(kAddLanes* kAddSlices) rotate_sums_kernel(const RotateBackArgs a, const int teams)
+// follow one another in a run's row.
+__global__ void __launch_bounds__(kAddLanes* kAddSlices) rotate_sums_kernel(const __grid_constant__ RotateBackArgs a)
 {
     grid_dependency_sync();
-    const int q = a.r.q_vecs * 8, all = a.r.vecs * 8, width = blockIdx.y == 0 ? q : all - q;
-    float* to = blockIdx.y == 0 ? a.dq_weight : a.dk_weight;
+    const bool keys = blockIdx.y == 1, shared = a.r.norm == kNormHead;
+    float* to = keys ? a.dk_weight : a.dq_weight;
     if (to == nullptr) return;
+    const int width = keys ? a.r.k_width : a.r.q_width, runs = keys ? a.k_runs : a.q_runs, each = shared ? a.r.D : width;
     const int c = (blockIdx.x * kAddLanes + threadIdx.x) * 4;
-    const bool shared = a.r.norm == kNormHead;
-    const bool active = c < (shared ? a.r.D : width);
-    const float* p = a.parts + (blockIdx.y == 0 ? 0 : q) + c;
-    float4 s;
-    if (!shared) {
-        s = add_parts(p, all, teams, active);
-    } else {
-        s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int h = 0; h < width / a.r.D; ++h) {
-            if (h > 0) __syncthreads();
-            const float4 v = add_parts(p + h * a.r.D, all, teams, active);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-    }
-    if (active && threadIdx.y == 0) *reinterpret_cast<float4*>(to + c) = s;
+    if (c - (int)threadIdx.x * 4 >= each) return;
+    const float4 s = add_parts(a.parts + (keys ? (long long)a.q_runs * a.r.q_width : 0) + c, each, runs * (width / each), c < each);
+    if (c < each && threadIdx.y == 0) *reinterpret_cast<float4*>(to + c) = s;
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------
 // How the rows are cut into runs: as many teams as the device holds at once, each with the same number of rows but the last.
 struct RowPlan {
-    int warps = 0, teams = 0;      // of a team, of a CTA
+    int vecs = 0, warps = 0, teams = 0;      // of a lane, of a team, of a CTA
     int share = 0, runs = 0, ctas = 0;
 };
 
@@ -742,7 +985,8 @@ int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, co
     if (ctas != 0) return ctas;
     int sms = 0, per_sm = 0;
     e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess && smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (as much as any team width may ask for: the attribute is the kernel's, not the launch's)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmemPerCta - 2048);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
     if (e != cudaSuccess || sms * per_sm < 1) {
         cudaGetLastError();
@@ -754,11 +998,13 @@ int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, co
     return ctas;
 }
 
-RowPlan team_shape(int vecs)
+// `most`: vectors of eight channels that a lane has at most.  As few warps as that takes, and then as few vectors.
+RowPlan team_shape(int d, int most)
 {
     RowPlan p;
-    p.warps = (vecs + 31) / 32;
-    p.teams = block_teams(vecs);
+    p.warps = block_warps(d, most);
+    p.vecs = block_vecs(d, most);
+    p.teams = block_teams(d, most);
     return p;
 }
 void cut_rows(RowPlan& p, long long rows, long long most_teams)
@@ -768,35 +1014,38 @@ void cut_rows(RowPlan& p, long long rows, long long most_teams)
     p.runs = (int)((rows + p.share - 1) / p.share);
     p.ctas = (p.runs + p.teams - 1) / p.teams;
 }
+dim3 team_block(const RowPlan& p) { return dim3((unsigned)p.warps * 32, (unsigned)p.teams); }
+bool is_full(const RowPlan& p, int d) { return d == p.warps * 32 * 8 * p.vecs; }
 
-template <typename T, typename R, int kThreads>
-int launch_modulate(ModulateArgs a, cudaStream_t st)
+template <typename T, typename R, int kVecs, bool kFull>
+int launch_modulate(ModulateArgs a, RowPlan p, cudaStream_t st)
 {
     static Resident resident;
-    auto kernel = modulate_kernel<T, R, kThreads>;
-    RowPlan p = team_shape(a.d / 8);
-    const int ctas = resident_ctas(resident, kernel, p.warps, p.warps * 32 * p.teams, 0, "modulate");
+    auto kernel = modulate_kernel<T, R, kVecs, kFull>;
+    constexpr int kPer = kVecs * kModulatePieces<T, R>;
+    const int threads = p.warps * 32 * p.teams;
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
+    const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, "modulate");
     if (ctas < 0) return ctas;
     cut_rows(p, a.rows, (long long)ctas * p.teams);
     a.share = p.share;
-    return check_launch(launch_block(kernel, dim3((unsigned)p.ctas), dim3((unsigned)p.warps * 32, (unsigned)p.teams), 0, st, a), "modulate_kernel");
+    return check_launch(launch_block(kernel, dim3((unsigned)p.ctas), team_block(p), smem, st, a), "modulate_kernel");
 }
 
-template <typename T, typename R, int kThreads>
-int launch_modulate_backward(ModulateBackArgs a, cudaStream_t st)
+template <typename T, typename R, int kVecs, bool kFull>
+int launch_modulate_backward(ModulateBackArgs a, RowPlan p, cudaStream_t st)
 {
     static Resident resident;
-    auto kernel = modulate_backward_kernel<T, R, kThreads>;
-    RowPlan p = team_shape(a.m.d / 8);
+    auto kernel = modulate_backward_kernel<T, R, kVecs, kFull>;
+    constexpr int kPer = kVecs * kModulateBackPieces<T, R>;
     const int threads = p.warps * 32 * p.teams;
-    const size_t smem = (size_t)threads * 16 * sizeof(float);
+    const size_t smem = (size_t)threads * (16 * kPer * row_stages(kPer, row_threads(kVecs), 64 * kVecs) + 64 * kVecs);
     const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, "modulate_backward");
     if (ctas < 0) return ctas;
-    const long long most = (long long)ctas * p.teams;
-    cut_rows(p, a.m.rows, std::min<long long>(most, block_runs(a.m.d / 8)));
+    cut_rows(p, a.m.rows, std::min<long long>((long long)ctas * p.teams, block_runs(a.m.d, modulate_back_vecs(a.m.d))));
     a.m.share = p.share;
     if (a.dweight == nullptr && a.dpost_weight == nullptr) a.weight_parts = nullptr;
-    int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), dim3((unsigned)p.warps * 32, (unsigned)p.teams), smem, st, a), "modulate_backward_kernel");
+    int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), team_block(p), smem, st, a), "modulate_backward_kernel");
     if (r < 0) return r;
     // a frame that several runs share, or weights: their parts are added up
     const bool shared = a.m.frame > 1 && p.runs > 1 && (a.dgate != nullptr || a.dscale != nullptr || a.dshift != nullptr);
@@ -809,74 +1058,103 @@ int launch_modulate_backward(ModulateBackArgs a, cudaStream_t st)
     return r < 0 ? r : 2;
 }
 
-template <typename T, int kVecs, int kThreads>
-int launch_rotate(RotateArgs a, cudaStream_t st)
+// Runs of the queries and of the keys: CTAs for each by their share of the channels.
+void cut_rotation(RowPlan& q, RowPlan& k, const RotateArgs& r, long long ctas, long long most_runs)
 {
-    static Resident resident;
-    auto kernel = rotate_kernel<T, kVecs, kThreads>;
-    RowPlan p = team_shape((a.vecs + kVecs - 1) / kVecs);
-    const int ctas = resident_ctas(resident, kernel, p.warps, p.warps * 32 * p.teams, 0, "rotate");
-    if (ctas < 0) return ctas;
-    cut_rows(p, a.rows, (long long)ctas * p.teams);
-    a.share = p.share;
-    return check_launch(launch_block(kernel, dim3((unsigned)p.ctas), dim3((unsigned)p.warps * 32, (unsigned)p.teams), 0, st, a), "rotate_kernel");
+    long long for_k = r.k_width == 0 ? 0 : ctas * r.k_width / (r.q_width + r.k_width);
+    if (r.k_width > 0 && for_k < 1) for_k = 1;
+    const long long for_q = ctas > for_k ? ctas - for_k : 1;
+    cut_rows(q, r.rows, std::min(for_q * q.teams, most_runs));
+    k = q;
+    k.runs = k.ctas = 0;
+    if (r.k_width > 0) cut_rows(k, r.rows, std::min(for_k * q.teams, most_runs));
 }
 
-template <typename T, int kVecs, int kThreads>
-int launch_rotate_backward(RotateBackArgs a, cudaStream_t st)
+template <typename T, int kVecs, bool kFull>
+int launch_rotate(RotateArgs a, RowPlan q, cudaStream_t st)
 {
     static Resident resident;
-    auto kernel = rotate_backward_kernel<T, kVecs, kThreads>;
-    RowPlan p = team_shape((a.r.vecs + kVecs - 1) / kVecs);
-    const int ctas = resident_ctas(resident, kernel, p.warps, p.warps * 32 * p.teams, 0, "rotate_backward");
+    auto kernel = rotate_kernel<T, kVecs, kFull>;
+    constexpr int kPer = kVecs * kPieces<T>;
+    RowPlan k;
+    const int threads = q.warps * 32 * q.teams;
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
+    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, "rotate");
     if (ctas < 0) return ctas;
-    const long long most = (long long)ctas * p.teams;
-    cut_rows(p, a.r.rows, std::min<long long>(most, block_runs((a.r.vecs + kVecs - 1) / kVecs)));
-    a.r.share = p.share;
+    cut_rotation(q, k, a, ctas, 1LL << 40);
+    a.q_share = q.share;
+    a.k_share = k.share;
+    a.q_ctas = q.ctas;
+    return check_launch(launch_block(kernel, dim3((unsigned)(q.ctas + k.ctas)), team_block(q), smem, st, a), "rotate_kernel");
+}
+
+template <typename T, int kVecs, bool kFull>
+int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
+{
+    static Resident resident;
+    auto kernel = rotate_backward_kernel<T, kVecs, kFull>;
+    constexpr int kPer = 2 * kVecs * kPieces<T>;
+    RowPlan k;
+    const int threads = q.warps * 32 * q.teams;
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
+    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, "rotate_backward");
+    if (ctas < 0) return ctas;
     if (a.dq_weight == nullptr && a.dk_weight == nullptr) a.parts = nullptr;
-    int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), dim3((unsigned)p.warps * 32, (unsigned)p.teams), 0, st, a), "rotate_backward_kernel");
+    cut_rotation(q, k, a.r, ctas, a.parts != nullptr ? block_runs(std::max(a.r.q_width, a.r.k_width), kRotateBackVecs) : 1LL << 40);
+    a.r.q_share = q.share;
+    a.r.k_share = k.share;
+    a.r.q_ctas = q.ctas;
+    a.q_runs = q.runs;
+    a.k_runs = k.runs;
+    int r = check_launch(launch_block(kernel, dim3((unsigned)(q.ctas + k.ctas)), team_block(q), smem, st, a), "rotate_backward_kernel");
     if (r < 0 || a.parts == nullptr) return r;
-    const int q = a.r.q_vecs * 8, k = a.r.vecs * 8 - q, widest = a.r.norm == kNormHead ? a.r.D : q > k ? q : k;
-    r = check_launch(launch_block(rotate_sums_kernel, dim3((unsigned)((widest + 4 * kAddLanes - 1) / (4 * kAddLanes)), k > 0 ? 2 : 1), dim3(kAddLanes, kAddSlices), 0, st, a, p.runs),
+    const int widest = a.r.norm == kNormHead ? a.r.D : std::max(a.r.q_width, a.r.k_width);
+    r = check_launch(launch_block(rotate_sums_kernel, dim3((unsigned)((widest + 4 * kAddLanes - 1) / (4 * kAddLanes)), a.r.k_width > 0 ? 2 : 1), dim3(kAddLanes, kAddSlices), 0, st, a),
                      "rotate_sums_kernel");
     return r < 0 ? r : 2;
 }
 
 }  // namespace
 
-// Threads of a CTA decide how many registers there are for each: rows of up to 2048 channels, up to 5120, and wider ones.
-#define ARL2_BY_WIDTH(threads, call)                                   \
-    ((threads) <= 256 ? call(256) : (threads) <= 640 ? call(640) : call(1024))
+// The instance for the vectors of a lane, and for lanes that all have as many.
+#define ARL2_BY_VECS(p, full, call)                                                                          \
+    ((p).vecs == 1 ? ((full) ? call(1, true) : call(1, false)) : (p).vecs == 2 ? ((full) ? call(2, true) : call(2, false)) \
+     : (p).vecs == 3 ? ((full) ? call(3, true) : call(3, false)) : ((full) ? call(4, true) : call(4, false)))
+#define ARL2_UP_TO_2(p, full, call) ((p).vecs == 1 ? ((full) ? call(1, true) : call(1, false)) : ((full) ? call(2, true) : call(2, false)))
 
 int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st)
 {
-    const int threads = (a.d / 8 + 31) / 32 * 32;
-#define ARL2_CALL(n) (dtype == ARL2_FP32 ? launch_modulate<float, float, n>(a, st) : wide ? launch_modulate<__nv_bfloat16, float, n>(a, st) : launch_modulate<__nv_bfloat16, __nv_bfloat16, n>(a, st))
-    return ARL2_BY_WIDTH(threads, ARL2_CALL);
+    const RowPlan p = team_shape(a.d, kModulateVecs);
+#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_modulate<float, float, v, f>(a, p, st) : wide ? launch_modulate<__nv_bfloat16, float, v, f>(a, p, st) : launch_modulate<__nv_bfloat16, __nv_bfloat16, v, f>(a, p, st))
+    return ARL2_UP_TO_2(p, is_full(p, a.d), ARL2_CALL);
 #undef ARL2_CALL
 }
 
 int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st)
 {
-    const int threads = (a.m.d / 8 + 31) / 32 * 32;
-#define ARL2_CALL(n) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, n>(a, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, n>(a, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, n>(a, st))
-    return ARL2_BY_WIDTH(threads, ARL2_CALL);
+    const RowPlan p = team_shape(a.m.d, modulate_back_vecs(a.m.d));
+#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, v, f>(a, p, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, v, f>(a, p, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, v, f>(a, p, st))
+    return ARL2_UP_TO_2(p, is_full(p, a.m.d), ARL2_CALL);
 #undef ARL2_CALL
 }
 
 int rotate(const RotateArgs& a, int dtype, cudaStream_t st)
 {
-    const int threads = ((a.vecs + 1) / 2 + 31) / 32 * 32;
-#define ARL2_CALL(n) (dtype == ARL2_FP32 ? launch_rotate<float, 2, n>(a, st) : launch_rotate<__nv_bfloat16, 2, n>(a, st))
-    return ARL2_BY_WIDTH(threads, ARL2_CALL);
+    const int d = std::max(a.q_width, a.k_width);
+    const RowPlan p = team_shape(d, kRotateVecs);
+    const bool full = is_full(p, a.q_width) && (a.k_width == 0 || a.k_width == a.q_width);
+#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_rotate<float, v, f>(a, p, st) : launch_rotate<__nv_bfloat16, v, f>(a, p, st))
+    return ARL2_BY_VECS(p, full, ARL2_CALL);
 #undef ARL2_CALL
 }
 
 int rotate_backward(const RotateBackArgs& a, int dtype, cudaStream_t st)
 {
-    const int threads = ((a.r.vecs + 1) / 2 + 31) / 32 * 32;
-#define ARL2_CALL(n) (dtype == ARL2_FP32 ? launch_rotate_backward<float, 2, n>(a, st) : launch_rotate_backward<__nv_bfloat16, 2, n>(a, st))
-    return ARL2_BY_WIDTH(threads, ARL2_CALL);
+    const int d = std::max(a.r.q_width, a.r.k_width);
+    const RowPlan p = team_shape(d, kRotateBackVecs);
+    const bool full = is_full(p, a.r.q_width) && (a.r.k_width == 0 || a.r.k_width == a.r.q_width);
+#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_rotate_backward<float, v, f>(a, p, st) : launch_rotate_backward<__nv_bfloat16, v, f>(a, p, st))
+    return ARL2_UP_TO_2(p, full, ARL2_CALL);
 #undef ARL2_CALL
 }
 

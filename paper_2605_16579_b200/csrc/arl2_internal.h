@@ -263,10 +263,15 @@ int tc_cache_attend(const CacheAttendArgs& a, cudaStream_t st);
 // ---- what stands around the core in a block (arl2_block.cu) --------------------------------
 enum RowNorm : int { kNormNone = ARL2_NORM_NONE, kNormLayer = ARL2_NORM_LAYER, kNormRms = ARL2_NORM_RMS, kNormToken = ARL2_NORM_TOKEN,
                      kNormHead = ARL2_NORM_HEAD, kNormLength = ARL2_NORM_LENGTH };
-constexpr int kBlockMostChannels = 8192;   // of a row of the modulation; twice as many for queries and keys together
-// Runs of rows whose sums over tokens have room in a workspace: `teams` per CTA (block_teams) of at most four CTAs per SM of 148
-constexpr int block_teams(int vecs) { return (vecs + 31) / 32 >= 8 ? 1 : 8 / ((vecs + 31) / 32); }
-constexpr int block_runs(int vecs) { return 4 * 148 * block_teams(vecs); }
+constexpr int kBlockMostChannels = 8192;   // of a row: of the modulation, of queries, of keys
+// How a row of d channels is held: `warps` warps whose lanes have `vecs` groups of eight channels each, at most `most` of them; teams of
+// warps that make up a CTA; and the runs of rows whose sums over tokens have room in a workspace: those of four CTAs per SM of 148.
+constexpr int modulate_back_vecs(int d) { return d <= 4096 ? 1 : 2; }      // (512 threads with 128 registers each hold one vector)
+constexpr int kModulateVecs = 2, kRotateVecs = 4, kRotateBackVecs = 2;
+constexpr int block_warps(int d, int most) { return (d / 8 + 32 * most - 1) / (32 * most); }
+constexpr int block_vecs(int d, int most) { return (d / 8 + 32 * block_warps(d, most) - 1) / (32 * block_warps(d, most)); }
+constexpr int block_teams(int d, int most) { return block_warps(d, most) >= 8 ? 1 : 8 / block_warps(d, most); }
+constexpr int block_runs(int d, int most) { return 4 * 148 * block_teams(d, most); }
 struct FrameRows {           // a row of d channels per frame, fp32; nullptr: none
     const float* p;
     int64_t batch, frame;    // strides in elements
@@ -299,7 +304,7 @@ struct ModulateBackArgs {
 };
 struct RotateArgs {
     int B, T, D, rows;
-    int q_vecs, vecs;        // groups of eight channels of a token's queries, and of both
+    int q_width, k_width;    // channels of a token's queries and keys (0: no keys)
     int norm;
     float eps, q_over, k_over;   // sums of squares are multiplied with these
     const float *cos, *sin;  // [rope_rows, D/2]
@@ -312,14 +317,15 @@ struct RotateArgs {
     const float *q_weight, *k_weight;
     void *q_out, *k_out;
     uint32_t* status;
-    int share = 0;
+    int q_share = 0, k_share = 0, q_ctas = 0;    // rows per run, and the CTAs that have the queries' (set by the launcher)
 };
 struct RotateBackArgs {
     RotateArgs r;
     const void *dq_out, *dk_out;
     void *dq, *dk;
     float *dq_weight, *dk_weight;
-    float* parts;            // [runs, vecs * 8]
+    float* parts;            // [q_runs, q_width], [k_runs, k_width]
+    int q_runs = 0, k_runs = 0;                  // (set by the launcher)
 };
 int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st);
 int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st);

@@ -11,68 +11,148 @@
 namespace arl2 {
 namespace {
 
-// ---- eight channels of a row: what a lane loads and stores at once --------------------------------------
-// Rows pass through once, so they do not take the room in L1 that the rows per frame and the rotary tables use.
+// ---- pairs of fp32, of which an instruction makes two operations ---------------------------------------------
+typedef uint64_t f2;
+__device__ __forceinline__ f2 pair(float lo, float hi)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ f2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ void apart(f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ float lo_plus_hi(f2 v)
+{
+    float a, b;
+    apart(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// ---- eight channels of a row, four pairs: what a lane loads and stores at once ----------------------------------
+template <typename T> constexpr int kPieces = sizeof(T) / 2;      // of 16 bytes
 template <typename T> struct Eight;
 template <> struct Eight<__nv_bfloat16> {
     uint4 u;
-    __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p)
+    __device__ __forceinline__ static f2 widen(uint32_t w) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    __device__ __forceinline__ void get(f2 (&f)[4]) const
     {
-        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p) : "memory");
-    }
-    __device__ __forceinline__ void get(float (&f)[8]) const
-    {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+        f[0] = widen(u.x); f[1] = widen(u.y); f[2] = widen(u.z); f[3] = widen(u.w);
     }
     // rounded once, to the nearest
-    __device__ __forceinline__ void set(const float (&f)[8])
+    __device__ __forceinline__ static uint32_t narrow(f2 v)
     {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
-        u = make_uint4(w[0], w[1], w[2], w[3]);
+        float lo, hi;
+        apart(v, lo, hi);
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
     }
+    __device__ __forceinline__ void set(const f2 (&f)[4]) { u = make_uint4(narrow(f[0]), narrow(f[1]), narrow(f[2]), narrow(f[3])); }
     __device__ __forceinline__ void store(__nv_bfloat16* p) const
     {
         asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
     }
 };
 template <> struct Eight<float> {
-    float4 a, b;
-    __device__ __forceinline__ void zero() { a = b = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
-    __device__ __forceinline__ void load(const float* p)
+    f2 f[4];
+    __device__ __forceinline__ void get(f2 (&o)[4]) const
     {
-        asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "l"(p) : "memory");
-        asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "l"(p + 4) : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = f[i];
     }
-    __device__ __forceinline__ void get(float (&f)[8]) const
+    __device__ __forceinline__ void set(const f2 (&o)[4])
     {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-        f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    }
-    __device__ __forceinline__ void set(const float (&f)[8])
-    {
-        a = make_float4(f[0], f[1], f[2], f[3]);
-        b = make_float4(f[4], f[5], f[6], f[7]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = o[i];
     }
     __device__ __forceinline__ void store(float* p) const
     {
-        asm volatile("st.global.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w) : "memory");
-        asm volatile("st.global.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + 4), "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w) : "memory");
+        asm volatile("st.global.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(f[0]), "l"(f[1]) : "memory");
+        asm volatile("st.global.v2.b64 [%0], {%1, %2};" ::"l"(p + 4), "l"(f[2]), "l"(f[3]) : "memory");
     }
 };
+
+// ---- rows on their way -----------------------------------------------------------------------------------------
+// Each lane copies its own channels of the next rows to places of its own in shared memory and reads them there itself: nobody else
+// has to be waited for, and the ring is in flight without a register for them.  (One row ahead in registers: 40 heads' queries and
+// keys of 4680 tokens, 20 KB in flight per SM, 104 us; @RING@)
+template <int kItems, int kStages>       // pieces of 16 bytes that a lane has of a row; rows in flight and the one in work
+struct RowRing {
+    uint32_t at;         // this lane's place
+    int step;            // bytes from a piece to the next: 16 for each thread of the CTA
+    uint32_t put, get;   // stages, as offsets
+    __device__ __forceinline__ void start(const void* smem, int thread, int threads)
+    {
+        at = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + thread * 16;
+        step = threads * 16;
+        put = get = 0;
+    }
+    __device__ __forceinline__ void copy(int item, const void* p) const
+    {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + put + item * step), "l"(p) : "memory");
+    }
+    // a row's copies are all on their way (or there is no row)
+    __device__ __forceinline__ void sent()
+    {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        put = put == (uint32_t)(kStages - 1) * kItems * step ? 0 : put + kItems * step;
+    }
+    // the oldest row has landed; its pieces may be read until the next call of sent()
+    __device__ __forceinline__ void landed() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
+    __device__ __forceinline__ uint4 piece(int item) const
+    {
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + get + item * step) : "memory");
+        return v;
+    }
+    __device__ __forceinline__ void done() { get = get == (uint32_t)(kStages - 1) * kItems * step ? 0 : get + kItems * step; }
+
+    // eight channels of type T, one piece or two
+    template <typename T> __device__ __forceinline__ void copy8(int item, const T* p) const
+    {
+        copy(item, p);
+        if (sizeof(T) == 4) copy(item + 1, p + 4);
+    }
+};
+template <typename T, typename Ring>
+__device__ __forceinline__ void read8(const Ring& ring, int item, f2 (&f)[4])
+{
+    if (sizeof(T) == 2) {
+        Eight<__nv_bfloat16> e;
+        e.u = ring.piece(item);
+        e.get(f);
+    } else {
+        const uint4 u = ring.piece(item), w = ring.piece(item + 1);
+        f[0] = pair(__uint_as_float(u.x), __uint_as_float(u.y));
+        f[1] = pair(__uint_as_float(u.z), __uint_as_float(u.w));
+        f[2] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
+        f[3] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
+    }
+}
 // rows that are read again and again: through L1
-__device__ __forceinline__ void load_kept(const float* p, float (&f)[8])
+__device__ __forceinline__ void load_kept(const float* p, f2 (&f)[4])
 {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    f[0] = pair(a.x, a.y); f[1] = pair(a.z, a.w);
+    f[2] = pair(b.x, b.y); f[3] = pair(b.z, b.w);
 }
 
 // ---- sums over the warps of a team ----------------------------------------------------------------------
@@ -83,32 +163,42 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-constexpr int kTeamWarps = 32;   // warps of a CTA at most, over all its teams
+constexpr int kTeamWarps = 16;   // warps of a CTA at most, over all its teams
+__device__ __forceinline__ float team_sum(float v)      // of the lanes below kTeamWarps, in those
+{
+#pragma unroll
+    for (int o = kTeamWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
 
-// A team is `warps` warps that share a row, side by side in the CTA; warp w of the CTA's `first`th on.  What its warps have to
-// tell one another goes through shared memory, which alternates between two places so that one barrier per exchange is enough:
-// a warp that writes to a place for the second time has passed the barrier behind which everyone was done with the first.
+// A team is `warps` warps that share a row, side by side in the CTA.  What its warps have to tell one another goes through shared
+// memory, which alternates between two places so that one barrier per exchange is enough: a warp that writes to a place for the
+// second time has passed the barrier behind which everyone was done with the first.
 template <int N>
 struct Team {
-    float (*place)[kTeamWarps][N];   // [2]
-    int first, warps, id, turn;
-    // entry of warp `w` of the team, as each lane below `warps` sees its own; others get zeros
-    __device__ __forceinline__ void exchange(const float (&mine)[N], float (&out)[N])
+    float* place;        // [2][warps][N], this team's
+    int warps, id, turn;
+    __device__ __forceinline__ void start(float* smem, int team)
     {
-        const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;   // (x runs over the team)
-        if (warps == 1) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) out[i] = lane == 0 ? mine[i] : 0.0f;
-            return;
-        }
-        turn ^= 1;
+        warps = blockDim.x >> 5;       // (x runs over the team)
+        id = team;
+        place = smem + team * 2 * warps * N;
+        turn = 0;
+    }
+    // The entry of warp (lane % kTeamWarps) for each lane; zeros where there is no such warp.
+    __device__ __forceinline__ void exchange(const float (&mine)[N], float (&of)[N])
+    {
+        float* p = place + turn;
+        turn ^= warps * N;
+        const int lane = threadIdx.x & 31, w = lane & (kTeamWarps - 1);
         if (lane == 0) {
+            float* q = p + (threadIdx.x >> 5) * N;
 #pragma unroll
-            for (int i = 0; i < N; ++i) place[turn][first + w][i] = mine[i];
+            for (int i = 0; i < N; ++i) q[i] = mine[i];
         }
         asm volatile("bar.sync %0, %1;" ::"r"(1 + id), "r"(warps * 32) : "memory");
 #pragma unroll
-        for (int i = 0; i < N; ++i) out[i] = lane < warps ? place[turn][first + lane][i] : 0.0f;
+        for (int i = 0; i < N; ++i) of[i] = w < warps ? p[w * N + i] : 0.0f;
     }
 };
 
