@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
 }
 
 // ---- parts of sums over tokens, added in the order of the rows --------------------------------------------
-constexpr int kAddLanes = 32, kAddSlices = 8;   // four channels a lane; each slice a run of the parts
+constexpr int kAddLanes = 32, kAddSlices = 32;   // four channels a lane; each slice (a warp) a run of the parts
 
 // The sum of `count` rows of four channels, `step` elements apart; all threads of the CTA, the result in slice 0.
 __device__ __forceinline__ float4 add_parts(const float* p, long long step, int count, bool active)
@@ -489,7 +489,7 @@ __device__ __forceinline__ float4 add_parts(const float* p, long long step, int 
     const int per = (count + kAddSlices - 1) / kAddSlices, from = min(count, (int)threadIdx.y * per), to = min(count, from + per);
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (active) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = from; i < to; ++i) {
             const float4 v = *reinterpret_cast<const float4*>(p + i * step);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -939,32 +939,46 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
         walk.next(a.r);
     }
     if (a.parts == nullptr) return;
-    float* part = a.parts + (side.keys ? (long long)a.q_runs * a.r.q_width : 0) + (long long)side.team * side.width;
+    float* part = a.parts + (side.keys ? (long long)a.q_parts * a.q_each : 0);
+    Eight<float> o;
+    if (a.r.norm == kNormHead) {      // the heads share the weight: a warp's are added here, and a part is a warp's
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (int i = 1; i < kVecs; ++i) sum[0][e] = add2(sum[0][e], sum[i][e]);
+            for (int from = 16; from >= lanes; from >>= 1) sum[0][e] = add2(sum[0][e], __shfl_xor_sync(0xffffffffu, sum[0][e], from));
+        }
+        const int warps = min(team.warps, (side.width + 255) / 256), warp = threadIdx.x >> 5;     // that have channels
+        o.set(sum[0]);
+        if (warp < warps && (int)(threadIdx.x & 31) < lanes) o.store(part + ((long long)side.team * warps + warp) * a.r.D + (threadIdx.x & 31) * 8);
+        return;
+    }
+    part += (long long)side.team * side.width;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
         if (ch.has(i)) {
-            Eight<float> o;
             o.set(sum[i]);
             o.store(part + ch.at(i));
         }
 }
 
-// The gradients of the weights: y = 0 for the queries', 1 for the keys'; a weight per head is shared by the heads, whose parts
-// follow one another in a run's row.
+// The gradients of the weights: y = 0 for the queries', 1 for the keys'.
 __global__ void __launch_bounds__(kAddLanes* kAddSlices) rotate_sums_kernel(const __grid_constant__ RotateBackArgs a)
 {
     grid_dependency_sync();
-    const bool keys = blockIdx.y == 1, shared = a.r.norm == kNormHead;
+    const bool keys = blockIdx.y == 1;
     float* to = keys ? a.dk_weight : a.dq_weight;
     if (to == nullptr) return;
-    const int width = keys ? a.r.k_width : a.r.q_width, runs = keys ? a.k_runs : a.q_runs, each = shared ? a.r.D : width;
-    const int c = (blockIdx.x * kAddLanes + threadIdx.x) * 4;
+    const int each = keys ? a.k_each : a.q_each, c = (blockIdx.x * kAddLanes + threadIdx.x) * 4;
     if (c - (int)threadIdx.x * 4 >= each) return;
-    const float4 s = add_parts(a.parts + (keys ? (long long)a.q_runs * a.r.q_width : 0) + c, each, runs * (width / each), c < each);
+    const float4 s = add_parts(a.parts + (keys ? (long long)a.q_parts * a.q_each : 0) + c, each, keys ? a.k_parts : a.q_parts, c < each);
     if (c < each && threadIdx.y == 0) *reinterpret_cast<float4*>(to + c) = s;
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------
+// Rows of a run at least where it leaves sums behind: they are on their way together, and there are fewer parts to add.
+constexpr int kLeastRows = 4;
+
 // How the rows are cut into runs: as many teams as the device holds at once, each with the same number of rows but the last.
 struct RowPlan {
     int vecs = 0, warps = 0, teams = 0;      // of a lane, of a team, of a CTA
@@ -1007,10 +1021,10 @@ RowPlan team_shape(int d, int most)
     p.teams = block_teams(d, most);
     return p;
 }
-void cut_rows(RowPlan& p, long long rows, long long most_teams)
+void cut_rows(RowPlan& p, long long rows, long long most_teams, int least = 1)
 {
     if (most_teams < 1) most_teams = 1;
-    p.share = (int)((rows + most_teams - 1) / most_teams);
+    p.share = std::max(least, (int)((rows + most_teams - 1) / most_teams));
     p.runs = (int)((rows + p.share - 1) / p.share);
     p.ctas = (p.runs + p.teams - 1) / p.teams;
 }
@@ -1042,7 +1056,7 @@ int launch_modulate_backward(ModulateBackArgs a, RowPlan p, cudaStream_t st)
     const size_t smem = (size_t)threads * (16 * kPer * row_stages(kPer, row_threads(kVecs), 64 * kVecs) + 64 * kVecs);
     const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, "modulate_backward");
     if (ctas < 0) return ctas;
-    cut_rows(p, a.m.rows, std::min<long long>((long long)ctas * p.teams, block_runs(a.m.d, modulate_back_vecs(a.m.d))));
+    cut_rows(p, a.m.rows, std::min<long long>((long long)ctas * p.teams, block_runs(a.m.d, modulate_back_vecs(a.m.d))), kLeastRows);
     a.m.share = p.share;
     if (a.dweight == nullptr && a.dpost_weight == nullptr) a.weight_parts = nullptr;
     int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), team_block(p), smem, st, a), "modulate_backward_kernel");
@@ -1059,15 +1073,15 @@ int launch_modulate_backward(ModulateBackArgs a, RowPlan p, cudaStream_t st)
 }
 
 // Runs of the queries and of the keys: CTAs for each by their share of the channels.
-void cut_rotation(RowPlan& q, RowPlan& k, const RotateArgs& r, long long ctas, long long most_runs)
+void cut_rotation(RowPlan& q, RowPlan& k, const RotateArgs& r, long long ctas, long long most_runs, int least)
 {
     long long for_k = r.k_width == 0 ? 0 : ctas * r.k_width / (r.q_width + r.k_width);
     if (r.k_width > 0 && for_k < 1) for_k = 1;
     const long long for_q = ctas > for_k ? ctas - for_k : 1;
-    cut_rows(q, r.rows, std::min(for_q * q.teams, most_runs));
+    cut_rows(q, r.rows, std::min(for_q * q.teams, most_runs), least);
     k = q;
     k.runs = k.ctas = 0;
-    if (r.k_width > 0) cut_rows(k, r.rows, std::min(for_k * q.teams, most_runs));
+    if (r.k_width > 0) cut_rows(k, r.rows, std::min(for_k * q.teams, most_runs), least);
 }
 
 template <typename T, int kVecs, bool kFull>
@@ -1081,7 +1095,7 @@ int launch_rotate(RotateArgs a, RowPlan q, cudaStream_t st)
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
     const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, "rotate");
     if (ctas < 0) return ctas;
-    cut_rotation(q, k, a, ctas, 1LL << 40);
+    cut_rotation(q, k, a, ctas, 1LL << 40, 1);
     a.q_share = q.share;
     a.k_share = k.share;
     a.q_ctas = q.ctas;
@@ -1100,15 +1114,18 @@ int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
     const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, "rotate_backward");
     if (ctas < 0) return ctas;
     if (a.dq_weight == nullptr && a.dk_weight == nullptr) a.parts = nullptr;
-    cut_rotation(q, k, a.r, ctas, a.parts != nullptr ? block_runs(std::max(a.r.q_width, a.r.k_width), kRotateBackVecs) : 1LL << 40);
+    cut_rotation(q, k, a.r, ctas, a.parts != nullptr ? block_runs(std::max(a.r.q_width, a.r.k_width), kRotateBackVecs) : 1LL << 40, a.parts != nullptr ? kLeastRows : 1);
     a.r.q_share = q.share;
     a.r.k_share = k.share;
     a.r.q_ctas = q.ctas;
-    a.q_runs = q.runs;
-    a.k_runs = k.runs;
+    const bool head = a.r.norm == kNormHead;
+    a.q_each = head ? a.r.D : a.r.q_width;
+    a.k_each = head ? a.r.D : a.r.k_width;
+    a.q_parts = q.runs * (head ? std::min(q.warps, (a.r.q_width + 255) / 256) : 1);
+    a.k_parts = k.runs * (head ? std::min(q.warps, (a.r.k_width + 255) / 256) : 1);
     int r = check_launch(launch_block(kernel, dim3((unsigned)(q.ctas + k.ctas)), team_block(q), smem, st, a), "rotate_backward_kernel");
     if (r < 0 || a.parts == nullptr) return r;
-    const int widest = a.r.norm == kNormHead ? a.r.D : std::max(a.r.q_width, a.r.k_width);
+    const int widest = std::max(a.q_each, a.k_each);
     r = check_launch(launch_block(rotate_sums_kernel, dim3((unsigned)((widest + 4 * kAddLanes - 1) / (4 * kAddLanes)), a.r.k_width > 0 ? 2 : 1), dim3(kAddLanes, kAddSlices), 0, st, a),
                      "rotate_sums_kernel");
     return r < 0 ? r : 2;

@@ -324,8 +324,8 @@ struct RotateBackArgs {
     const void *dq_out, *dk_out;
     void *dq, *dk;
     float *dq_weight, *dk_weight;
-    float* parts;            // [q_runs, q_width], [k_runs, k_width]
-    int q_runs = 0, k_runs = 0;                  // (set by the launcher)
+    float* parts;            // [q_parts, q_each], [k_parts, k_each]: a run's, or for a weight that the heads share a warp's of a run
+    int q_parts = 0, k_parts = 0, q_each = 0, k_each = 0;    // (set by the launcher)
 };
 int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st);
 int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st);
