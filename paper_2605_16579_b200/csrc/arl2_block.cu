@@ -187,11 +187,10 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
     auto send = [&]() {
         if (--to_send >= 0) {
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) {
-                    ring.copy8(i * kPer, x + i * ch.step());
-                    if (has_y) ring.copy8(i * kPer + kPieces<R>, y + i * ch.step());
-                }
+            for (int i = 0; i < kVecs; ++i) {
+                ring.template copy8<kFull>(i * kPer, x + i * ch.step(), ch.at(i), a.d);
+                if (has_y) ring.template copy8<kFull>(i * kPer + kPieces<R>, y + i * ch.step(), ch.at(i), a.d);
+            }
             x += a.d;
             y += a.d;
         }
@@ -210,8 +209,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
             if (ch.has(i)) {
-                read8<R>(ring, i * kPer, v[i]);
-                if (has_y) read8<T>(ring, i * kPer + kPieces<R>, u[i]);
+                ring.template read8<R>(i * kPer, v[i]);
+                if (has_y) ring.template read8<T>(i * kPer + kPieces<R>, u[i]);
             }
         ring.done();
         if (walk.left == 0) {   // the first row of this team, or of a frame
@@ -310,15 +309,15 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
     auto send = [&]() {
         if (--to_send >= 0) {
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) {
-                    if (has_n) {
-                        ring.copy8(i * kPer + kR, r + i * ch.step());
-                        ring.copy8(i * kPer + kDn, dn + i * ch.step());
-                    }
-                    if (has_r) ring.copy8(i * kPer + kDr, dr + i * ch.step());
-                    if (has_y) ring.copy8(i * kPer + kY, y + i * ch.step());
+            for (int i = 0; i < kVecs; ++i) {
+                const int at = i * ch.step(), c = ch.at(i);
+                if (has_n) {
+                    ring.template copy8<kFull>(i * kPer + kR, r + at, c, d);
+                    ring.template copy8<kFull>(i * kPer + kDn, dn + at, c, d);
                 }
+                if (has_r) ring.template copy8<kFull>(i * kPer + kDr, dr + at, c, d);
+                if (has_y) ring.template copy8<kFull>(i * kPer + kY, y + at, c, d);
+            }
             r += d;
             dn += d;
             dr += d;
@@ -354,7 +353,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
         if (has_r) {
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) read8<R>(ring, i * kPer + kDr, dx[i]);
+                if (ch.has(i)) ring.template read8<R>(i * kPer + kDr, dx[i]);
         }
         if (has_n) {
             f2 v[kVecs][4], g[kVecs][4];
@@ -365,8 +364,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
                 if (ch.has(i)) {
-                    read8<R>(ring, i * kPer + kR, v[i]);
-                    read8<T>(ring, i * kPer + kDn, g[i]);
+                    ring.template read8<R>(i * kPer + kR, v[i]);
+                    ring.template read8<T>(i * kPer + kDn, g[i]);
                 }
             f2 gs[kVecs][4];
 #pragma unroll
@@ -391,7 +390,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
             if (ch.has(i)) {
-                if (has_y) read8<T>(ring, i * kPer + kY, u[i]);
+                if (has_y) ring.template read8<T>(i * kPer + kY, u[i]);
                 Eight<R> o;
                 o.set(dx[i]);
                 o.store(dx_out + i * ch.step());
@@ -730,8 +729,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
     auto send = [&]() {
         if (--to_send >= 0) {
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) ring.copy8(i * kPer, x_in + i * ch.step());
+            for (int i = 0; i < kVecs; ++i) ring.template copy8<kFull>(i * kPer, x_in + i * ch.step(), ch.at(i), side.width);
             const bool last = ++sent_t == a.T;
             x_in += last ? wrap : side.token;
             if (last) sent_t = 0;
@@ -750,7 +748,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
         ring.landed();
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
-            if (ch.has(i)) read8<T>(ring, i * kPer, x[i]);
+            if (ch.has(i)) ring.template read8<T>(i * kPer, x[i]);
         ring.done();
         if (a.norm != 0) {
             f2 ss[kVecs];
@@ -840,11 +838,10 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
     auto send = [&]() {
         if (--to_send >= 0) {
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) {
-                    ring.copy8(i * kPer, g_in + i * ch.step());
-                    if (normed) ring.copy8(i * kPer + kPieces<T>, x_in + i * ch.step());
-                }
+            for (int i = 0; i < kVecs; ++i) {
+                ring.template copy8<kFull>(i * kPer, g_in + i * ch.step(), ch.at(i), side.width);
+                if (normed) ring.template copy8<kFull>(i * kPer + kPieces<T>, x_in + i * ch.step(), ch.at(i), side.width);
+            }
             g_in += side.width;
             const bool last = ++sent_t == a.r.T;
             x_in += last ? wrap : side.token;
@@ -867,8 +864,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
             if (ch.has(i)) {
-                read8<T>(ring, i * kPer, g[i]);
-                if (normed) read8<T>(ring, i * kPer + kPieces<T>, x[i]);
+                ring.template read8<T>(i * kPer, g[i]);
+                if (normed) ring.template read8<T>(i * kPer + kPieces<T>, x[i]);
             }
         ring.done();
 #pragma unroll

@@ -83,17 +83,23 @@ template <> struct Eight<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = o[i];
     }
+    // (32 bytes a lane, whole sectors: halves of one cost twice the writes.  `p` is known to be a multiple of 16 bytes only)
     __device__ __forceinline__ void store(float* p) const
     {
-        asm volatile("st.global.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(f[0]), "l"(f[1]) : "memory");
-        asm volatile("st.global.v2.b64 [%0], {%1, %2};" ::"l"(p + 4), "l"(f[2]), "l"(f[3]) : "memory");
+        if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
+            asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(f[0]), "l"(f[1]), "l"(f[2]), "l"(f[3]) : "memory");
+        } else {
+            asm volatile("st.global.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(f[0]), "l"(f[1]) : "memory");
+            asm volatile("st.global.v2.b64 [%0], {%1, %2};" ::"l"(p + 4), "l"(f[2]), "l"(f[3]) : "memory");
+        }
     }
 };
 
 // ---- rows on their way -----------------------------------------------------------------------------------------
-// Each lane copies its own channels of the next rows to places of its own in shared memory and reads them there itself: nobody else
-// has to be waited for, and the ring is in flight without a register for them.  (One row ahead in registers: 40 heads' queries and
-// keys of 4680 tokens, 20 KB in flight per SM, 104 us; @RING@)
+// Each lane copies its part of the next rows to shared memory, so that they are in flight without a register for them: of bf16 rows its own
+// eight channels, 16 bytes.  Eight fp32 channels are two pieces; there a warp copies the 64 pieces of its lanes side by side (each
+// lane its own pair would ask for every sector twice: 40 heads' modulation with an fp32 residual, 9360 tokens, 122 us, now 102), and
+// neighbours trade places every other eight pieces, so that the lanes' reads fall on different banks.
 template <int kItems, int kStages>       // pieces of 16 bytes that a lane has of a row; rows in flight and the one in work
 struct RowRing {
     uint32_t at;         // this lane's place
@@ -105,48 +111,60 @@ struct RowRing {
         step = threads * 16;
         put = get = 0;
     }
-    __device__ __forceinline__ void copy(int item, const void* p) const
+    __device__ __forceinline__ void copy(uint32_t to, const void* p) const { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p) : "memory"); }
+    __device__ __forceinline__ uint4 piece(uint32_t from) const
     {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + put + item * step), "l"(p) : "memory");
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+        return v;
     }
-    // a row's copies are all on their way (or there is no row)
+    // A row's copies are all on their way (or there is no row).
     __device__ __forceinline__ void sent()
     {
         asm volatile("cp.async.commit_group;" ::: "memory");
         put = put == (uint32_t)(kStages - 1) * kItems * step ? 0 : put + kItems * step;
     }
-    // the oldest row has landed; its pieces may be read until the next call of sent()
-    __device__ __forceinline__ void landed() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
-    __device__ __forceinline__ uint4 piece(int item) const
+    // The oldest row has landed, for all lanes of the warp; its pieces may be read until done().
+    __device__ __forceinline__ void landed()
     {
-        uint4 v;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + get + item * step) : "memory");
-        return v;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
     }
-    __device__ __forceinline__ void done() { get = get == (uint32_t)(kStages - 1) * kItems * step ? 0 : get + kItems * step; }
-
-    // eight channels of type T, one piece or two
-    template <typename T> __device__ __forceinline__ void copy8(int item, const T* p) const
+    __device__ __forceinline__ void done()
     {
-        copy(item, p);
-        if (sizeof(T) == 4) copy(item + 1, p + 4);
+        get = get == (uint32_t)(kStages - 1) * kItems * step ? 0 : get + kItems * step;
+        __syncwarp();      // (the next copies go where other lanes have read)
     }
-};
-template <typename T, typename Ring>
-__device__ __forceinline__ void read8(const Ring& ring, int item, f2 (&f)[4])
-{
-    if (sizeof(T) == 2) {
-        Eight<__nv_bfloat16> e;
-        e.u = ring.piece(item);
-        e.get(f);
-    } else {
-        const uint4 u = ring.piece(item), w = ring.piece(item + 1);
+    // This lane's eight channels of type T, from channel c of a row of d on, at p; every lane of the warp calls it.
+    template <bool kFull, typename T> __device__ __forceinline__ void copy8(int item, const T* p, int c, int d) const
+    {
+        if (sizeof(T) == 2) {
+            if (kFull || c < d) copy(at + put + item * step, p);
+            return;
+        }
+        const int lane = threadIdx.x & 31;
+        const uint32_t to = at + put + item * step - lane * 16;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (kFull || c - lane * 4 + j * 128 < d) copy(to + j * step + (lane ^ (lane >> 3 & 1)) * 16, p - lane * 4 + j * 128);
+    }
+    template <typename T> __device__ __forceinline__ void read8(int item, f2 (&f)[4]) const
+    {
+        if (sizeof(T) == 2) {
+            Eight<__nv_bfloat16> e;
+            e.u = piece(at + get + item * step);
+            e.get(f);
+            return;
+        }
+        const int lane = threadIdx.x & 31, first = 2 * lane & 31;      // pieces 2 lane and 2 lane + 1, in the first 32 or the second
+        const uint32_t from = at + get + item * step - lane * 16 + (lane >> 4) * step;
+        const uint4 u = piece(from + (first ^ (first >> 3 & 1)) * 16), w = piece(from + ((first + 1) ^ (first >> 3 & 1)) * 16);
         f[0] = pair(__uint_as_float(u.x), __uint_as_float(u.y));
         f[1] = pair(__uint_as_float(u.z), __uint_as_float(u.w));
         f[2] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
         f[3] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
     }
-}
+};
 // rows that are read again and again: through L1
 __device__ __forceinline__ void load_kept(const float* p, f2 (&f)[4])
 {
