@@ -23,11 +23,13 @@ constexpr int kMaxDev = 64;
 // Threads of a CTA at most, with that many vectors a lane: rows of 8192 channels
 __host__ __device__ constexpr int row_threads(int vecs) { return vecs >= 4 ? 256 : vecs == 3 ? 352 : 512; }
 
+constexpr int kRowStatic = 5 * 1024;       // shared memory of a CTA besides, at most
+
 // Rows in flight, and the one in work: as many as there is room for with CTAs of this many threads, four at most.  `pieces` of 16 bytes that
 // a lane has of a row, `beside`: bytes that it has besides.
 __host__ __device__ constexpr int row_stages(int pieces, int threads, int beside)
 {
-    const int n = ((kMaxSmemPerCta - 2048) / threads - beside) / (16 * pieces);
+    const int n = ((kMaxSmemPerCta - kRowStatic) / threads - beside) / (16 * pieces);
     return n < 1 ? 1 : n > 4 ? 4 : n;
 }
 
@@ -39,13 +41,12 @@ struct LaneChannels {
     __device__ __forceinline__ int step() const { return (int)blockDim.x * 8; }
     __device__ __forceinline__ int at(int i) const { return c0 + i * step(); }
     __device__ __forceinline__ bool has(int i) const { return kFull || at(i) < d; }
-    __device__ __forceinline__ float warp_channels(int warp) const       // that warp `warp` of the team has
+    __device__ __forceinline__ int warp_channels(int warp) const       // that warp `warp` of the team has
     {
-        if (kFull) return (float)(256 * kVecs);
         int n = 0;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) n += max(0, min(256, d - i * step() - warp * 256));
-        return (float)n;
+        return warp < (int)blockDim.x / 32 ? n : 0;
     }
 };
 template <int kVecs>
@@ -57,67 +58,99 @@ __device__ __forceinline__ void clear(f2 (&v)[kVecs][4])
         for (int e = 0; e < 4; ++e) v[i][e] = 0;
 }
 
+// A team that makes the statistics of a row, with the channels of each warp and of one's own.
+struct NormTeam : Team<4> {
+    const float* counts;     // [kTeamWarps]
+    float per_channel;       // one over those of this lane's warp
+    float over, eps;         // one over the row's
+    template <int kVecs, bool kFull>
+    __device__ __forceinline__ void start(float* smem, float* channels, const LaneChannels<kVecs, kFull>& ch, float e)
+    {
+        if (threadIdx.y == 0 && threadIdx.x < kTeamWarps) channels[threadIdx.x] = (float)ch.warp_channels(threadIdx.x);
+        counts = channels;
+        per_channel = 1.0f / (float)ch.warp_channels(threadIdx.x >> 5);
+        over = 1.0f / (float)ch.d;
+        eps = e;
+        Team<4>::start(smem);
+    }
+};
+
 // Mean of a row and one over its deviation, and (kDots) the sums of g and of g * (x - mean), from what the team's warps know: the
 // mean of each one's channels and the sum of squares about it (about zero for an RMS norm).  Joined with the means' differences, so
 // that no digits are lost where the mean is large.  Channels that a lane does not have are zeros in x and g.
 struct RowSums { float mean, inverse, g, gx; };
 
 template <bool kDots, int kVecs, bool kFull>
-__device__ __forceinline__ RowSums row_sums(Team<4>& team, const f2 (&x)[kVecs][4], const f2 (&g)[kVecs][4], bool layer,
-                                            const LaneChannels<kVecs, kFull>& ch, float over, float eps)
+__device__ __forceinline__ RowSums row_sums(NormTeam& team, const f2 (&x)[kVecs][4], const f2 (&g)[kVecs][4], bool layer, const LaneChannels<kVecs, kFull>& ch)
 {
     float mine[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (layer) {
-        f2 s = 0;
+        f2 s[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = add2(s, x[i][e]);
-        mine[0] = warp_sum(lo_plus_hi(s)) / ch.warp_channels(threadIdx.x >> 5);
+            for (int e = 0; e < 4; ++e) s[e & 1] = add2(s[e & 1], x[i][e]);
+        mine[0] = warp_sum(lo_plus_hi(add2(s[0], s[1]))) * team.per_channel;
     }
-    f2 m2 = 0, sg = 0, sgx = 0;
+    f2 m2[2] = {0, 0}, sg[2] = {0, 0}, sgx[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const f2 m = both(ch.has(i) ? -mine[0] : 0.0f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const f2 c = add2(x[i][e], m);
-            m2 = fma2(c, c, m2);
+            m2[e & 1] = fma2(c, c, m2[e & 1]);
             if (kDots) {
-                sg = add2(sg, g[i][e]);
-                sgx = fma2(g[i][e], c, sgx);
+                sg[e & 1] = add2(sg[e & 1], g[i][e]);
+                sgx[e & 1] = fma2(g[i][e], c, sgx[e & 1]);
             }
         }
     }
-    mine[1] = warp_sum(lo_plus_hi(m2));
+    mine[1] = warp_sum(lo_plus_hi(add2(m2[0], m2[1])));
     if (kDots) {
-        if (layer) mine[2] = warp_sum(lo_plus_hi(sg));
-        mine[3] = warp_sum(lo_plus_hi(sgx));
+        if (layer) mine[2] = warp_sum(lo_plus_hi(add2(sg[0], sg[1])));
+        mine[3] = warp_sum(lo_plus_hi(add2(sgx[0], sgx[1])));
     }
     RowSums r;
+    r.mean = r.g = 0.0f;
     if (team.warps == 1) {
         r.mean = mine[0];
-        r.inverse = rsqrtf(mine[1] * over + eps);
         r.g = mine[2];
-        r.gx = mine[3];
-        return r;
-    }
-    float of[4];
-    team.exchange(mine, of);
-    r.mean = r.g = 0.0f;
-    if (layer) {
-        const int w = threadIdx.x & (kTeamWarps - 1);
-        const float n = w < team.warps ? ch.warp_channels(w) : 0.0f;
-        r.mean = team_sum(n * of[0]) * over;
-        const float apart = of[0] - r.mean;
-        of[1] = fmaf(n * apart, apart, of[1]);
-        if (kDots) {
-            of[3] = fmaf(apart, of[2], of[3]);
-            r.g = team_sum(of[2]);
+    } else {
+        const float* all = team.exchange(mine);
+        if (layer) {
+            for (int w = 0; w < team.warps; w += 4) {
+                const float4 n = *reinterpret_cast<const float4*>(team.counts + w), m = *reinterpret_cast<const float4*>(all + w);
+                r.mean += fmaf(n.x, m.x, n.y * m.y) + fmaf(n.z, m.z, n.w * m.w);
+            }
+            r.mean *= team.over;
+            mine[1] = mine[3] = 0.0f;
+            for (int w = 0; w < team.warps; w += 4) {
+                const float4 n4 = *reinterpret_cast<const float4*>(team.counts + w), m4 = *reinterpret_cast<const float4*>(all + w);
+                const float4 q4 = *reinterpret_cast<const float4*>(all + kTeamWarps + w);
+                const float n[4] = {n4.x, n4.y, n4.z, n4.w}, m[4] = {m4.x - r.mean, m4.y - r.mean, m4.z - r.mean, m4.w - r.mean}, q[4] = {q4.x, q4.y, q4.z, q4.w};
+                float4 g4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), x4 = g4;
+                if (kDots) {
+                    g4 = *reinterpret_cast<const float4*>(all + 2 * kTeamWarps + w);
+                    x4 = *reinterpret_cast<const float4*>(all + 3 * kTeamWarps + w);
+                }
+                const float gg[4] = {g4.x, g4.y, g4.z, g4.w}, gx[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {       // (there is no warp behind the last: no channels, and sums of zero)
+                    mine[1] += fmaf(n[i] * m[i], m[i], q[i]);
+                    if (kDots) {
+                        r.g += gg[i];
+                        mine[3] += fmaf(m[i], gg[i], gx[i]);
+                    }
+                }
+            }
+        } else {
+            mine[1] = team.sum(all + kTeamWarps);
+            if (kDots) mine[3] = team.sum(all + 3 * kTeamWarps);
         }
     }
-    r.inverse = rsqrtf(team_sum(of[1]) * over + eps);
-    if (kDots) r.gx = team_sum(of[3]);
+    r.inverse = rsqrtf(mine[1] * team.over + team.eps);
+    r.gx = mine[3];
     return r;
 }
 
@@ -162,19 +195,18 @@ template <typename T, typename R> constexpr int kModulatePieces = kPieces<R> + k
 template <typename T, typename R, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __grid_constant__ ModulateArgs a)
 {
-    __shared__ __align__(16) float place[2 * kTeamWarps * 4];
+    __shared__ __align__(16) float place[kTeamFloats<4>], channels[kTeamWarps];
     constexpr int kPer = kModulatePieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
     extern __shared__ uint4 ring_smem[];
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
-    Team<4> team;
-    team.start(place, threadIdx.y);
     const LaneChannels<kVecs, kFull> ch(a.d);
+    NormTeam team;
+    team.start(place, channels, ch, a.eps);
     const int first = (int)min(((long long)blockIdx.x * blockDim.y + threadIdx.y) * a.share, (long long)a.rows), rows = min(a.share, a.rows - first);
     grid_dependency_sync();
     if (rows <= 0) return;
     const bool has_y = a.y != nullptr, has_n = a.n != nullptr, has_shift = a.shift.p != nullptr;
-    const float over = 1.0f / (float)a.d;
     const long long at0 = (long long)first * a.d + ch.c0;
     const R* x = static_cast<const R*>(a.x) + at0;
     const T* y = static_cast<const T*>(a.y) + at0;
@@ -227,7 +259,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
         }
         if (has_y) {
             if (a.post_norm != 0) {
-                const RowSums s = row_sums<false>(team, u, u, a.post_norm == kNormLayer, ch, over, a.eps);
+                const RowSums s = row_sums<false>(team, u, u, a.post_norm == kNormLayer, ch);
                 const f2 m = both(-s.mean), k = both(s.inverse);
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i)
@@ -248,7 +280,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
             r_out += a.d;
         }
         if (has_n) {
-            const RowSums s = row_sums<false>(team, v, v, a.norm == kNormLayer, ch, over, a.eps);
+            const RowSums s = row_sums<false>(team, v, v, a.norm == kNormLayer, ch);
             const f2 m = both(-s.mean), k = both(s.inverse);
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
@@ -273,20 +305,19 @@ template <typename T, typename R> constexpr int kModulateBackPieces = 2 * kPiece
 template <typename T, typename R, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a)
 {
-    __shared__ __align__(16) float place[2 * kTeamWarps * 4];
+    __shared__ __align__(16) float place[kTeamFloats<4>], channels[kTeamWarps];
     constexpr int kPer = kModulateBackPieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 64 * kVecs);
     constexpr int kR = 0, kDr = kPieces<R>, kDn = 2 * kPieces<R>, kY = kDn + kPieces<T>;
     extern __shared__ uint4 ring_smem[];       // the rows, then [8 kVecs][threads] pairs: dw and dw_post of a thread's channels
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
-    Team<4> team;
-    team.start(place, threadIdx.y);
     const LaneChannels<kVecs, kFull> ch(a.m.d);
+    NormTeam team;
+    team.start(place, channels, ch, a.m.eps);
     const int team_at = (int)blockIdx.x * blockDim.y + threadIdx.y, first = (int)min((long long)team_at * a.m.share, (long long)a.m.rows), rows = min(a.m.share, a.m.rows - first);
     grid_dependency_sync();
     if (rows <= 0) return;
     const int d = a.m.d;
-    const float over = 1.0f / (float)d;
     const long long at0 = (long long)first * d + ch.c0;
     const R* r = static_cast<const R*>(a.m.r) + at0;
     const T* y = static_cast<const T*>(a.m.y) + at0;
@@ -375,9 +406,9 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
                     gs[i][e] = mul2(g[i][e], scale[i][e]);
                     sum_n[i][e] = add2(sum_n[i][e], g[i][e]);
                 }
-            const RowSums s = row_sums<true>(team, v, gs, layer, ch, over, a.m.eps);
+            const RowSums s = row_sums<true>(team, v, gs, layer, ch);
             // dx = dr + i gs - i mean(g) - hat i mean(g hat)
-            const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * over * s.inverse), mean_gx = both(-s.gx * s.inverse * over * s.inverse);
+            const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * team.over * s.inverse), mean_gx = both(-s.gx * s.inverse * team.over * s.inverse);
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
 #pragma unroll
@@ -404,8 +435,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) dy[i][e] = mul2(dx[i][e], gate[i][e]);
             if (a.m.post_norm != 0) {
-                const RowSums s = row_sums<true>(team, u, dy, a.m.post_norm == kNormLayer, ch, over, a.m.eps);
-                const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * over * s.inverse), mean_gx = both(-s.gx * s.inverse * over * s.inverse);
+                const RowSums s = row_sums<true>(team, u, dy, a.m.post_norm == kNormLayer, ch);
+                const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * team.over * s.inverse), mean_gx = both(-s.gx * s.inverse * team.over * s.inverse);
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i)
 #pragma unroll
@@ -575,16 +606,6 @@ __device__ __forceinline__ RotateSide rotate_side(const RotateArgs& a)
     return s;
 }
 
-// Row of the tables for a position: the first for those before it, the last for those behind, which is reported.
-__device__ __forceinline__ int table_row(int at, const RotateArgs& a, int b)
-{
-    if (at >= a.rope_rows) {
-        if (atomicCAS(a.status + kStatusRange, 0u, (uint32_t)kRangePosition) == 0u) a.status[kStatusRangeWhere] = (uint32_t)b;
-        return a.rope_rows - 1;
-    }
-    return max(at, 0);
-}
-
 // The token that a run of rows is at, and its place in the grid: a step per row, without divisions.
 struct TokenWalk {
     int b, t, frame, line, column;
@@ -612,16 +633,18 @@ struct TokenWalk {
 };
 
 // cos and sin of the four pairs that a lane has of each head, pair m on.  Which axes turn them is the lane's own for all rows: most
-// lanes have one, those where an axis ends two; three or more changes within four pairs only where an axis has fewer than three pairs.
+// lanes have one, those where an axis ends two (the others ask for the same again, without a branch); a third only where an axis
+// has fewer than three pairs.  A row's angles are asked for while the row before it is in work.
 constexpr int kNoAxis = 3;
 struct Angles {
     int m, axis, other, split;    // pairs below `split` go by `axis`, the others by `other`
-    bool many;                    // ... unless there are more changes: then by axis_of
+    bool many, none0, none1;      // ... unless an axis begins and ends within the four: then by axis_of; pairs that do not turn
+    int b, start;                 // the stream, and its first position
     __device__ __forceinline__ static int axis_of(const RotateArgs& a, int pair)
     {
         return pair < a.pairs[0] ? 0 : pair < a.pairs[0] + a.pairs[1] ? 1 : pair < a.pairs[0] + a.pairs[1] + a.pairs[2] ? 2 : kNoAxis;
     }
-    __device__ __forceinline__ Angles(const RotateArgs& a, int pair) : m(pair), split(4), many(false)
+    __device__ __forceinline__ Angles(const RotateArgs& a, int pair) : m(pair), split(4), many(false), b(-1), start(0)
     {
         axis = axis_of(a, m);
         other = axis_of(a, m + 3);
@@ -632,8 +655,12 @@ struct Angles {
             many |= x != axis && x != other;
         }
         many = __any_sync(0xffffffffu, many);
+        none0 = axis == kNoAxis;
+        none1 = other == kNoAxis;
     }
-    __device__ __forceinline__ void load(const RotateArgs& a, const TokenWalk& w, float (&cs)[4], float (&sn)[4]) const
+    // Row of the tables for a position: the first for those before it, the last for those behind.
+    __device__ __forceinline__ static long long table_at(const RotateArgs& a, int at, int m) { return (long long)max(0, min(at, a.rope_rows - 1)) * (a.D / 2) + m; }
+    __device__ __forceinline__ void load(const RotateArgs& a, const TokenWalk& w, bool reports, float (&cs)[4], float (&sn)[4])
     {
         int at[3];
         if (a.positions != nullptr) {
@@ -641,39 +668,38 @@ struct Angles {
 #pragma unroll
             for (int i = 0; i < 3; ++i) at[i] = p[i];
         } else {
-            at[0] = (int)min((long long)(a.start != nullptr ? a.start[w.b] : 0) + w.frame, 0x7fffffffLL);
+            if (w.b != b) {
+                b = w.b;
+                start = a.start != nullptr ? a.start[b] : 0;
+            }
+            at[0] = (int)min((long long)start + w.frame, 0x7fffffffLL);
             at[1] = w.line;
             at[2] = w.column;
         }
-        auto fetch = [&](int x, float (&c)[4], float (&s)[4]) {
+        if (reports) {      // one lane of the team: a position behind the tables
+            bool behind = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
-            if (x == kNoAxis) return;
-            const long long o = (long long)table_row(x == 0 ? at[0] : x == 1 ? at[1] : at[2], a, w.b) * (a.D / 2) + m;
-            const float4 c4 = *reinterpret_cast<const float4*>(a.cos + o), s4 = *reinterpret_cast<const float4*>(a.sin + o);
-            c[0] = c4.x; c[1] = c4.y; c[2] = c4.z; c[3] = c4.w;
-            s[0] = s4.x; s[1] = s4.y; s[2] = s4.z; s[3] = s4.w;
-        };
-        fetch(axis, cs, sn);
-        if (split < 4) {
-            float c[4], s[4];
-            fetch(other, c, s);
+            for (int i = 0; i < 3; ++i) behind |= a.pairs[i] > 0 && at[i] >= a.rope_rows;
+            if (behind && atomicCAS(a.status + kStatusRange, 0u, (uint32_t)kRangePosition) == 0u) a.status[kStatusRangeWhere] = (uint32_t)w.b;
+        }
+        const long long o = table_at(a, axis == 0 ? at[0] : axis == 1 ? at[1] : at[2], m), q = table_at(a, other == 0 ? at[0] : other == 1 ? at[1] : at[2], m);
+        const float4 c0 = *reinterpret_cast<const float4*>(a.cos + o), s0 = *reinterpret_cast<const float4*>(a.sin + o);
+        const float4 c1 = *reinterpret_cast<const float4*>(a.cos + q), s1 = *reinterpret_cast<const float4*>(a.sin + q);
+        const float c[2][4] = {{c0.x, c0.y, c0.z, c0.w}, {c1.x, c1.y, c1.z, c1.w}}, s[2][4] = {{s0.x, s0.y, s0.z, s0.w}, {s1.x, s1.y, s1.z, s1.w}};
 #pragma unroll
-            for (int i = 1; i < 4; ++i)
-                if (i >= split) {
-                    cs[i] = c[i];
-                    sn[i] = s[i];
-                }
+        for (int i = 0; i < 4; ++i) {
+            const bool first = i < split, none = first ? none0 : none1;
+            cs[i] = none ? 1.0f : first ? c[0][i] : c[1][i];
+            sn[i] = none ? 0.0f : first ? s[0][i] : s[1][i];
         }
         if (many) {
 #pragma unroll
             for (int i = 1; i < 3; ++i) {
                 const int x = axis_of(a, m + i);
                 if (x == axis || x == other) continue;
-                float c[4], s[4];
-                fetch(x, c, s);
-                cs[i] = c[i];
-                sn[i] = s[i];
+                const long long r = table_at(a, x == 0 ? at[0] : x == 1 ? at[1] : at[2], m + i);
+                cs[i] = a.cos[r];
+                sn[i] = a.sin[r];
             }
         }
     }
@@ -705,13 +731,13 @@ __device__ __forceinline__ f2 swapped(f2 v)
 template <typename T, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid_constant__ RotateArgs a)
 {
-    __shared__ float place[2 * kTeamWarps];
+    __shared__ __align__(16) float place[kTeamFloats<1>];
     constexpr int kPer = kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
     extern __shared__ uint4 ring_smem[];
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
     Team<1> team;
-    team.start(place, threadIdx.y);
+    team.start(place);
     const RotateSide side = rotate_side(a);
     const LaneChannels<kVecs, kFull> ch(side.width);
     const int lanes = a.D / 8;
@@ -721,7 +747,9 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) rotate_weight(a, side, ch.at(i), ch.has(i), w[i]);
     TokenWalk walk(a, side.first);
-    const Angles angles(a, (threadIdx.x % lanes) * 4);
+    Angles angles(a, (threadIdx.x % lanes) * 4);
+    float next_cs[4], next_sn[4];
+    angles.load(a, walk, threadIdx.x == 0, next_cs, next_sn);
     const T* x_in = static_cast<const T*>(side.x) + walk.b * side.batch + walk.t * side.token + ch.c0;
     T* out = static_cast<T*>(side.keys ? a.k_out : a.q_out) + (long long)side.first * side.width + ch.c0;
     const int64_t wrap = side.batch - (a.T - 1) * side.token;       // from a stream's last row to the next one's first
@@ -743,7 +771,13 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
         f2 x[kVecs][4];
         float cs[4], sn[4];
         if (!kFull) clear(x);
-        angles.load(a, walk, cs, sn);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            cs[m] = next_cs[m];
+            sn[m] = next_sn[m];
+        }
+        walk.next(a);
+        if (row + 1 < side.rows) angles.load(a, walk, threadIdx.x == 0, next_cs, next_sn);
         send();
         ring.landed();
 #pragma unroll
@@ -764,9 +798,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
                 float all = warp_sum(lo_plus_hi(ss[0]));
                 if (team.warps > 1) {
                     const float mine[1] = {all};
-                    float of[1];
-                    team.exchange(mine, of);
-                    all = team_sum(of[0]);
+                    all = team.sum(team.exchange(mine));
                 }
                 // (the length goes into the angles, once for all the lane's heads)
                 const float inverse = rsqrtf(all * side.over + a.eps);
@@ -801,7 +833,6 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
             e8.store(out + i * ch.step());
         }
         out += side.width;
-        walk.next(a);
     }
 }
 
@@ -810,13 +841,13 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
 template <typename T, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(const __grid_constant__ RotateBackArgs a)
 {
-    __shared__ __align__(16) float place[2 * kTeamWarps * 2];
+    __shared__ __align__(16) float place[kTeamFloats<2>];
     constexpr int kPer = 2 * kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
     extern __shared__ uint4 ring_smem[];
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
     Team<2> team;
-    team.start(place, threadIdx.y);
+    team.start(place);
     const RotateSide side = rotate_side(a.r);
     const LaneChannels<kVecs, kFull> ch(side.width);
     const int lanes = a.r.D / 8;
@@ -828,7 +859,9 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) rotate_weight(a.r, side, ch.at(i), ch.has(i), w[i]);
     TokenWalk walk(a.r, side.first);
-    const Angles angles(a.r, (threadIdx.x % lanes) * 4);
+    Angles angles(a.r, (threadIdx.x % lanes) * 4);
+    float next_cs[4], next_sn[4];
+    angles.load(a.r, walk, threadIdx.x == 0, next_cs, next_sn);
     const long long at0 = (long long)side.first * side.width + ch.c0;
     const T* g_in = static_cast<const T*>(side.keys ? a.dk_out : a.dq_out) + at0;
     T* out = static_cast<T*>(side.keys ? a.dk : a.dq) + at0;
@@ -858,7 +891,13 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
             clear(x);
             clear(g);
         }
-        angles.load(a.r, walk, cs, sn);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            cs[m] = next_cs[m];
+            sn[m] = next_sn[m];
+        }
+        walk.next(a.r);
+        if (row + 1 < side.rows) angles.load(a.r, walk, threadIdx.x == 0, next_cs, next_sn);
         send();
         ring.landed();
 #pragma unroll
@@ -895,10 +934,9 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
                 }
                 float mine[2] = {warp_sum(lo_plus_hi(ss[0])), warp_sum(lo_plus_hi(dot[0]))};
                 if (team.warps > 1) {
-                    float of[2];
-                    team.exchange(mine, of);
-                    mine[0] = team_sum(of[0]);
-                    mine[1] = team_sum(of[1]);
+                    const float* of = team.exchange(mine);
+                    mine[0] = team.sum(of);
+                    mine[1] = team.sum(of + kTeamWarps);
                 }
                 const float i0 = rsqrtf(mine[0] * side.over + a.r.eps);
 #pragma unroll
@@ -933,7 +971,6 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
                 o.store(out + i * ch.step());
             }
         out += side.width;
-        walk.next(a.r);
     }
     if (a.parts == nullptr) return;
     float* part = a.parts + (side.keys ? (long long)a.q_parts * a.q_each : 0);
@@ -997,7 +1034,7 @@ int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, co
     int sms = 0, per_sm = 0;
     e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     // (as much as any team width may ask for: the attribute is the kernel's, not the launch's)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmemPerCta - 2048);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmemPerCta - kRowStatic);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
     if (e != cudaSuccess || sms * per_sm < 1) {
         cudaGetLastError();

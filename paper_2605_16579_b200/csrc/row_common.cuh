@@ -181,42 +181,47 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-constexpr int kTeamWarps = 16;   // warps of a CTA at most, over all its teams
-__device__ __forceinline__ float team_sum(float v)      // of the lanes below kTeamWarps, in those
-{
-#pragma unroll
-    for (int o = kTeamWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
+constexpr int kTeamWarps = 16;   // warps of a team at most
 
 // A team is `warps` warps that share a row, side by side in the CTA.  What its warps have to tell one another goes through shared
-// memory, which alternates between two places so that one barrier per exchange is enough: a warp that writes to a place for the
-// second time has passed the barrier behind which everyone was done with the first.
+// memory, N numbers of each in rows of kTeamWarps (zeros behind the last warp's), which each lane reads four at a time: shuffles would
+// be four more steps one after the other.  Two places by turns, so that one barrier per exchange is enough: a warp that writes to a
+// place for the second time has passed the barrier behind which everyone was done with the first.
+template <int N> constexpr int kTeamFloats = 8 * 2 * N * kTeamWarps;     // for the most teams of a CTA
 template <int N>
 struct Team {
-    float* place;        // [2][warps][N], this team's
+    float* place;        // [2][N][kTeamWarps], this team's
     int warps, id, turn;
-    __device__ __forceinline__ void start(float* smem, int team)
+    // `smem` of kTeamFloats<N> numbers; every thread of the CTA calls it
+    __device__ __forceinline__ void start(float* smem)
     {
         warps = blockDim.x >> 5;       // (x runs over the team)
-        id = team;
-        place = smem + team * 2 * warps * N;
+        id = threadIdx.y;
+        place = smem + id * 2 * N * kTeamWarps;
         turn = 0;
+        for (int i = threadIdx.x; i < 2 * N * kTeamWarps; i += blockDim.x) place[i] = 0.0f;
+        __syncthreads();
     }
-    // The entry of warp (lane % kTeamWarps) for each lane; zeros where there is no such warp.
-    __device__ __forceinline__ void exchange(const float (&mine)[N], float (&of)[N])
+    __device__ __forceinline__ const float* exchange(const float (&mine)[N])
     {
         float* p = place + turn;
-        turn ^= warps * N;
-        const int lane = threadIdx.x & 31, w = lane & (kTeamWarps - 1);
-        if (lane == 0) {
-            float* q = p + (threadIdx.x >> 5) * N;
+        turn ^= N * kTeamWarps;
+        if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) q[i] = mine[i];
+            for (int i = 0; i < N; ++i) p[i * kTeamWarps + (threadIdx.x >> 5)] = mine[i];
         }
         asm volatile("bar.sync %0, %1;" ::"r"(1 + id), "r"(warps * 32) : "memory");
-#pragma unroll
-        for (int i = 0; i < N; ++i) of[i] = w < warps ? p[w * N + i] : 0.0f;
+        return p;
+    }
+    // the sum of a row of numbers
+    __device__ __forceinline__ float sum(const float* row) const
+    {
+        float4 s = *reinterpret_cast<const float4*>(row);
+        for (int w = 4; w < warps; w += 4) {
+            const float4 o = *reinterpret_cast<const float4*>(row + w);
+            s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+        }
+        return (s.x + s.y) + (s.z + s.w);
     }
 };
 
