@@ -1439,7 +1439,7 @@ struct ModulationLayout { size_t parts, weight_parts, total; };
 ModulationLayout modulation_layout(const arl2_config& cfg, int32_t tokens)
 {
     const int d = cfg.H * cfg.D;
-    const int64_t rows = (int64_t)cfg.B * tokens, most = block_runs(d, modulate_back_vecs(d)), runs = rows < most ? rows : most;
+    const int64_t rows = (int64_t)cfg.B * tokens, most = kTileRuns, runs = rows < most ? rows : most;
     ModulationLayout l;
     size_t off = 0;
     l.parts = off;        off += align_up((size_t)runs * 2 * 3 * d * sizeof(float));

@@ -297,214 +297,421 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
     }
 }
 
+// ---- backward passes: tiles of rows ---------------------------------------------------------------------------
+// What a backward pass makes of a row needs the row's sums; what it adds up over the rows needs a lane for a channel.  So a CTA takes tiles
+// of rows into shared memory (one in work, the next on its way) and goes over each twice: first a warp has a row, or with few rows in
+// the tile some warps a row, and makes its sums; then a thread has eight channels (or sixteen) of every row, or of every second one where
+// there are threads for it, makes the outputs and keeps the sums over tokens in registers.  Sums of a row thus cost a warp's
+// shuffles once, and there are two barriers a tile.  (Teams of warps that do both at once, an exchange per row, spent 470 instructions
+// of a warp on a row's 256 channels: 55 us for 9360 rows of 1536, now @MB@.)
+constexpr int kTileThreads = 384, kTileWarps = kTileThreads / 32;
+struct TileShape {
+    int rows;            // of a tile
+    int split;           // warps of a row
+    int vecs;            // of eight channels, of a thread
+    int groups;          // of threads, that share the rows of a tile
+    int buffer;          // bytes of a tile
+    int buffers;         // two, or one where rows are so wide
+};
+// Tiles of `row_bytes` a row: two in `room` bytes of shared memory, no more rows than the CTA has altogether.
+TileShape tile_shape(int d, int row_bytes, int room, int most_rows)
+{
+    TileShape s;
+    s.rows = std::max(1, std::min({room / 2 / row_bytes, most_rows, 2 * kTileWarps}));
+    const int vecs = d / 8;
+    s.split = std::max(1, std::min(kTileWarps / s.rows, (vecs + 31) / 32));
+    s.vecs = (vecs + kTileThreads - 1) / kTileThreads;
+    s.groups = std::max(1, std::min(kTileThreads / vecs, s.rows));
+    s.buffer = s.rows * row_bytes;
+    s.buffers = 2 * s.buffer <= room ? 2 : 1;
+    return s;
+}
+constexpr int kTileRoom = kMaxSmemPerCta - 13 * 1024;     // what is left of a CTA's shared memory for the tiles
+
+// What is known of a row: -mean, 1 / deviation, and what dx takes off: (mean(g) and mean(g hat)) / deviation, negative.
+struct RowKnown { float m, k, g, gx; };
+// mean, squares about it, sums of g and g (x - mean), of a warp's channels or of all
+struct RowPart { float mean, m2, g, gx; };
+__device__ __forceinline__ RowKnown known(const RowPart& p, bool layer, float over, float eps)
+{
+    RowKnown r;
+    r.m = -p.mean;
+    r.k = rsqrtf(fmaf(p.m2, over, eps));
+    r.g = layer ? -p.g * over * r.k : 0.0f;
+    r.gx = -p.gx * over * r.k * r.k;
+    return r;
+}
+
+template <typename T, typename R>
+struct ModulateTile {
+    const R* r;
+    const R* dr;
+    const T* dn;
+    const T* y;
+    __device__ __forceinline__ ModulateTile(const uint8_t* buffer, int rows, int d)
+    {
+        r = reinterpret_cast<const R*>(buffer);
+        dr = r + rows * d;
+        dn = reinterpret_cast<const T*>(dr + rows * d);
+        y = dn + rows * d;
+    }
+};
+
 // With hat = N(r) without its weight, S = w (1 + scale), g = dn S, i = 1 / deviation:
 //   dx = dr + i (g - hat mean(g hat) - [LayerNorm] mean(g));   dgate = sum dx P(y), dscale = w sum dn hat, dshift = sum dn,
 //   dw = sum (1 + scale) dn hat;   dy = the same of P for the gradient dx gate w_post, dw_post = sum gate dx yhat.
 // Six units of memory: r, dn, dr and y in, dx and dy out.  The weights' sums are made from the frames' sums.
-template <typename T, typename R> constexpr int kModulateBackPieces = 2 * kPieces<R> + 2 * kPieces<T>;
-template <typename T, typename R, int kVecs, bool kFull>
-__global__ void __launch_bounds__(row_threads(kVecs)) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a)
+// kAll: all four are there, no P and no weights (flags that are known cost nothing in the loops).
+template <typename T, typename R, int kVecs, bool kAll>
+__global__ void __launch_bounds__(kTileThreads, 1) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a, const __grid_constant__ TileShape shape)
 {
-    __shared__ __align__(16) float place[kTeamFloats<4>], channels[kTeamWarps];
-    constexpr int kPer = kModulateBackPieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 64 * kVecs);
-    constexpr int kR = 0, kDr = kPieces<R>, kDn = 2 * kPieces<R>, kY = kDn + kPieces<T>;
-    extern __shared__ uint4 ring_smem[];       // the rows, then [8 kVecs][threads] pairs: dw and dw_post of a thread's channels
-    RowRing<kVecs * kPer, kRowStages> ring;
-    ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
-    const LaneChannels<kVecs, kFull> ch(a.m.d);
-    NormTeam team;
-    team.start(place, channels, ch, a.m.eps);
-    const int team_at = (int)blockIdx.x * blockDim.y + threadIdx.y, first = (int)min((long long)team_at * a.m.share, (long long)a.m.rows), rows = min(a.m.share, a.m.rows - first);
+    extern __shared__ __align__(16) uint8_t tile_smem[];
+    __shared__ __align__(16) RowKnown rows_n[2 * kTileWarps], rows_y[2 * kTileWarps];
+    __shared__ __align__(16) RowPart part_n[2 * kTileWarps], part_y[2 * kTileWarps];     // (rows that are not there are read, too)
+    __shared__ __align__(16) f2 joined[kTileThreads / 2][4];       // sums of a group of threads, for another one
+    const int d = a.m.d, vecs = d / 8, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int first = (int)min((long long)blockIdx.x * a.m.share, (long long)a.m.rows), rows = min(a.m.share, a.m.rows - first);
+    const float over = 1.0f / (float)d, eps = a.m.eps;
+    const bool has_y = kAll || a.m.y != nullptr, has_n = kAll || a.dn != nullptr, has_r = kAll || a.dr != nullptr, has_weights = !kAll && a.weight_parts != nullptr;
+    const bool layer = a.m.norm == kNormLayer, post = !kAll && has_y && a.m.post_norm != 0, post_layer = a.m.post_norm == kNormLayer;
     grid_dependency_sync();
     if (rows <= 0) return;
-    const int d = a.m.d;
-    const long long at0 = (long long)first * d + ch.c0;
-    const R* r = static_cast<const R*>(a.m.r) + at0;
-    const T* y = static_cast<const T*>(a.m.y) + at0;
-    const T* dn = static_cast<const T*>(a.dn) + at0;
-    const R* dr = static_cast<const R*>(a.dr) + at0;
-    R* dx_out = static_cast<R*>(a.dx) + at0;
-    T* dy_out = static_cast<T*>(a.dy) + at0;
-    const bool has_y = a.m.y != nullptr, has_n = a.dn != nullptr, has_r = a.dr != nullptr, has_weights = a.weight_parts != nullptr;
-    const bool layer = a.m.norm == kNormLayer;
-    const int ws_step = blockDim.x * blockDim.y;       // (strided by the CTA's threads: no bank conflicts)
-    f2* ws = reinterpret_cast<f2*>(ring_smem + kVecs * kPer * kRowStages * ws_step) + (threadIdx.y * blockDim.x + threadIdx.x);
-    if (has_weights) {
-#pragma unroll
-        for (int i = 0; i < 8 * kVecs; ++i) ws[i * ws_step] = 0;
-    }
+
+    auto send = [&](int tile) {      // rows of a tile are one piece of memory in every tensor
+        const int from = tile * shape.rows, n = min(shape.rows, rows - from);
+        if (n > 0) {
+            const ModulateTile<T, R> t(tile_smem + (tile & (shape.buffers - 1)) * shape.buffer, shape.rows, d);
+            const long long at = (long long)(first + from) * d;
+            for (int c = tid * 4; c < n * d; c += kTileThreads * 4) {
+                if (sizeof(R) == 4) {
+                    if (has_n) copy_piece(const_cast<R*>(t.r) + c, static_cast<const R*>(a.m.r) + at + c);
+                    if (has_r) copy_piece(const_cast<R*>(t.dr) + c, static_cast<const R*>(a.dr) + at + c);
+                }
+                if (sizeof(T) == 4) {
+                    if (has_n) copy_piece(const_cast<T*>(t.dn) + c, static_cast<const T*>(a.dn) + at + c);
+                    if (has_y) copy_piece(const_cast<T*>(t.y) + c, static_cast<const T*>(a.m.y) + at + c);
+                }
+            }
+            for (int c = tid * 8; c < n * d; c += kTileThreads * 8) {
+                if (sizeof(R) == 2) {
+                    if (has_n) copy_piece(const_cast<R*>(t.r) + c, static_cast<const R*>(a.m.r) + at + c);
+                    if (has_r) copy_piece(const_cast<R*>(t.dr) + c, static_cast<const R*>(a.dr) + at + c);
+                }
+                if (sizeof(T) == 2) {
+                    if (has_n) copy_piece(const_cast<T*>(t.dn) + c, static_cast<const T*>(a.dn) + at + c);
+                    if (has_y) copy_piece(const_cast<T*>(t.y) + c, static_cast<const T*>(a.m.y) + at + c);
+                }
+            }
+        }
+        copies_sent();
+    };
+    send(0);
+
+    // a thread's channels: of rows group, group + groups, ..
+    const int per_group = (vecs + kVecs - 1) / kVecs, group = tid / per_group, column = tid - group * per_group;
+    const bool works = group < shape.groups;
+    auto channel = [&](int i) { return (column + i * per_group) * 8; };
+    auto has = [&](int i) { return works && column + i * per_group < vecs; };
+    f2 gate[kVecs][4], scale[kVecs][4], sum_n[kVecs][4], sum_hat[kVecs][4], sum_y[kVecs][4], sum_w[kVecs][4], sum_p[kVecs][4];
+    clear(sum_w);
+    clear(sum_p);
     FrameWalk walk(a.m, first);
     bool whole = false, at_first = true;
-    f2 gate[kVecs][4], scale[kVecs][4], sum_n[kVecs][4], sum_hat[kVecs][4], sum_y[kVecs][4];
-    int to_send = rows;
-    auto send = [&]() {
-        if (--to_send >= 0) {
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                const int at = i * ch.step(), c = ch.at(i);
-                if (has_n) {
-                    ring.template copy8<kFull>(i * kPer + kR, r + at, c, d);
-                    ring.template copy8<kFull>(i * kPer + kDn, dn + at, c, d);
-                }
-                if (has_r) ring.template copy8<kFull>(i * kPer + kDr, dr + at, c, d);
-                if (has_y) ring.template copy8<kFull>(i * kPer + kY, y + at, c, d);
-            }
-            r += d;
-            dn += d;
-            dr += d;
-            y += d;
+
+    const int tiles = (rows + shape.rows - 1) / shape.rows;
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int from = tile * shape.rows, n = min(shape.rows, rows - from);
+        if (shape.buffers == 2) {
+            send(tile + 1);
+            copies_landed<1>();
+        } else {
+            copies_landed<0>();
         }
-        ring.sent();
-    };
+        __syncthreads();
+        const ModulateTile<T, R> t(tile_smem + (tile & (shape.buffers - 1)) * shape.buffer, shape.rows, d);
+
+        // ---- sums of the rows
+        if (has_n || post) {
+            for (int item = warp; item < (n * shape.split + kTileWarps - 1) / kTileWarps * kTileWarps; item += kTileWarps) {
+                const int row = item / shape.split, piece = item - row * shape.split;
+                const bool mine = row < n;
+                const int v0 = vecs * piece / shape.split, v1 = vecs * (piece + 1) / shape.split;
+                const int at = first + from + row, b = at / a.m.T, frame = (at - b * a.m.T) / a.m.frame;
+                RowPart pn = {0.0f, 0.0f, 0.0f, 0.0f}, py = pn;
+                if (mine) {
+                    const R* r = t.r + row * d;
+                    const T* dn = t.dn + row * d;
+                    const T* y = t.y + row * d;
+                    const float per = 1.0f / (float)(8 * (v1 - v0));
+                    if ((has_n && layer) || (post && post_layer)) {
+                        f2 s[2] = {0, 0};
+#pragma unroll 2
+                        for (int v = v0 + lane; v < v1; v += 32) {
+                            f2 x[4];
+                            if (has_n && layer) {
+                                read_tile(r + 8 * v, x);
+                                s[0] = add2(s[0], add2(add2(x[0], x[1]), add2(x[2], x[3])));
+                            }
+                            if (post && post_layer) {
+                                read_tile(y + 8 * v, x);
+                                s[1] = add2(s[1], add2(add2(x[0], x[1]), add2(x[2], x[3])));
+                            }
+                        }
+                        if (has_n && layer) pn.mean = warp_sum(lo_plus_hi(s[0])) * per;
+                        if (post && post_layer) py.mean = warp_sum(lo_plus_hi(s[1])) * per;
+                    }
+                    const f2 mn = both(-pn.mean), my = both(-py.mean);
+                    f2 m2 = 0, g1 = 0, gx = 0, y2 = 0;
+                    const float* scale_row = a.m.scale.p == nullptr ? nullptr : frame_row(a.m.scale, b, frame, 0);
+#pragma unroll 2
+                    for (int v = v0 + lane; v < v1; v += 32) {
+                        f2 x[4], g[4], f[4];
+                        if (has_n) {
+                            read_tile(r + 8 * v, x);
+                            read_tile(dn + 8 * v, g);
+                            if (scale_row != nullptr) {
+                                load_kept(scale_row + 8 * v, f);
 #pragma unroll
-    for (int i = 0; i + 1 < kRowStages; ++i) send();
-    for (int row = 0; row < rows; ++row) {
-        f2 dx[kVecs][4], u[kVecs][4];
-        clear(dx);
-        if (!kFull) clear(u);
-        send();
-        ring.landed();
-        if (walk.left == 0) {
-            walk.enter(a.m);
-            whole = walk.t == walk.frame * a.m.frame && row + walk.left <= rows;
-            clear(sum_n);
-            clear(sum_hat);
-            clear(sum_y);
-            if (!kFull) {
-                clear(gate);
-                clear(scale);
-            }
+                                for (int e = 0; e < 4; ++e) g[e] = fma2(g[e], f[e], g[e]);
+                            }
+                            if (!kAll && a.m.weight != nullptr) {
+                                load_kept(a.m.weight + 8 * v, f);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                if (!ch.has(i)) continue;
-                if (has_y) load_factor(gate[i], a.m.gate, walk.b, walk.frame, ch.at(i), 0.0f, a.m.post_weight);
-                if (has_n) load_factor(scale[i], a.m.scale, walk.b, walk.frame, ch.at(i), 1.0f, a.m.weight);
-            }
-        }
-        if (has_r) {
+                                for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], f[e]);
+                            }
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) ring.template read8<R>(i * kPer + kDr, dx[i]);
-        }
-        if (has_n) {
-            f2 v[kVecs][4], g[kVecs][4];
-            if (!kFull) {
-                clear(v);
-                clear(g);
-            }
+                            for (int e = 0; e < 4; ++e) {
+                                const f2 c = add2(x[e], mn), gs = g[e];
+                                m2 = fma2(c, c, m2);
+                                g1 = add2(g1, gs);
+                                gx = fma2(gs, c, gx);
+                            }
+                        }
+                        if (post) {
+                            read_tile(y + 8 * v, x);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                if (ch.has(i)) {
-                    ring.template read8<R>(i * kPer + kR, v[i]);
-                    ring.template read8<T>(i * kPer + kDn, g[i]);
+                            for (int e = 0; e < 4; ++e) {
+                                const f2 c = add2(x[e], my);
+                                y2 = fma2(c, c, y2);
+                            }
+                        }
+                    }
+                    if (has_n) {
+                        pn.m2 = warp_sum(lo_plus_hi(m2));
+                        if (layer) pn.g = warp_sum(lo_plus_hi(g1));
+                        pn.gx = warp_sum(lo_plus_hi(gx));
+                    }
+                    if (post) py.m2 = warp_sum(lo_plus_hi(y2));
                 }
-            f2 gs[kVecs][4];
+                // of a row that several warps have, the parts are joined with their means' differences (no digits are lost where the mean is large)
+                auto join = [&](RowPart* parts, RowPart& p, bool with_dots) {
+                    if (lane == 0) parts[warp] = p;
+                    __syncthreads();
+                    RowPart all = {0.0f, 0.0f, 0.0f, 0.0f};
+                    const int w0 = warp - piece;
+                    for (int w = 0; w < shape.split; ++w) all.mean = fmaf((float)(8 * (vecs * (w + 1) / shape.split - vecs * w / shape.split)), parts[w0 + w].mean, all.mean);
+                    all.mean *= over;
+                    for (int w = 0; w < shape.split; ++w) {
+                        const RowPart o = parts[w0 + w];
+                        const float nn = (float)(8 * (vecs * (w + 1) / shape.split - vecs * w / shape.split)), away = o.mean - all.mean;
+                        all.m2 += fmaf(nn * away, away, o.m2);
+                        if (with_dots) {
+                            all.g += o.g;
+                            all.gx += fmaf(away, o.g, o.gx);
+                        }
+                    }
+                    p = all;
+                };
+                if (shape.split > 1 && has_n) join(part_n, pn, true);
+                const RowKnown kn = known(pn, layer, over, eps);
+                if (mine && piece == 0 && lane == 0) rows_n[row] = kn;
+                if (post) {
+                    if (shape.split > 1) join(part_y, py, false);
+                    // the gradient of P's output is dx gate w_post: dx again, as the second round makes it
+                    f2 g1 = 0, gx = 0;
+                    if (mine) {
+                        const f2 my = both(-py.mean);
+#pragma unroll 2
+                        for (int v = v0 + lane; v < v1; v += 32) {
+                            f2 x[4], g[4], f[4], dx[4] = {0, 0, 0, 0};
+                            if (has_r) read_tile(t.dr + row * d + 8 * v, dx);
+                            if (has_n) {
+                                read_tile(t.r + row * d + 8 * v, x);
+                                read_tile(t.dn + row * d + 8 * v, g);
+                                load_factor(f, a.m.scale, b, frame, 8 * v, 1.0f, a.m.weight);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i)
+                                for (int e = 0; e < 4; ++e) {
+                                    const f2 hat = mul2(add2(x[e], both(kn.m)), both(kn.k));
+                                    dx[e] = fma2(hat, both(kn.gx), fma2(mul2(g[e], f[e]), both(kn.k), add2(dx[e], both(kn.g))));
+                                }
+                            }
+                            read_tile(t.y + row * d + 8 * v, x);
+                            load_factor(f, a.m.gate, b, frame, 8 * v, 0.0f, a.m.post_weight);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    gs[i][e] = mul2(g[i][e], scale[i][e]);
-                    sum_n[i][e] = add2(sum_n[i][e], g[i][e]);
+                            for (int e = 0; e < 4; ++e) {
+                                const f2 dy = mul2(dx[e], f[e]);
+                                g1 = add2(g1, dy);
+                                gx = fma2(dy, add2(x[e], my), gx);
+                            }
+                        }
+                    }
+                    RowPart dots = {py.mean, py.m2, warp_sum(lo_plus_hi(g1)), warp_sum(lo_plus_hi(gx))};
+                    if (shape.split > 1) {     // (about the mean of the whole row: plain sums)
+                        __syncthreads();
+                        if (lane == 0) part_y[warp] = dots;
+                        __syncthreads();
+                        dots.g = dots.gx = 0.0f;
+                        for (int w = 0; w < shape.split; ++w) {
+                            dots.g += part_y[warp - piece + w].g;
+                            dots.gx += part_y[warp - piece + w].gx;
+                        }
+                    }
+                    if (mine && piece == 0 && lane == 0) rows_y[row] = known(dots, post_layer, over, eps);
                 }
-            const RowSums s = row_sums<true>(team, v, gs, layer, ch);
-            // dx = dr + i gs - i mean(g) - hat i mean(g hat)
-            const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * team.over * s.inverse), mean_gx = both(-s.gx * s.inverse * team.over * s.inverse);
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f2 hat = mul2(add2(v[i][e], m), k);
-                    sum_hat[i][e] = fma2(g[i][e], hat, sum_hat[i][e]);
-                    dx[i][e] = fma2(hat, mean_gx, fma2(gs[i][e], k, add2(dx[i][e], mean_g)));
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-            if (ch.has(i)) {
-                if (has_y) ring.template read8<T>(i * kPer + kY, u[i]);
-                Eight<R> o;
-                o.set(dx[i]);
-                o.store(dx_out + i * ch.step());
             }
-        ring.done();
-        dx_out += d;
-        if (has_y) {
-            f2 dy[kVecs][4];
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dy[i][e] = mul2(dx[i][e], gate[i][e]);
-            if (a.m.post_norm != 0) {
-                const RowSums s = row_sums<true>(team, u, dy, a.m.post_norm == kNormLayer, ch);
-                const f2 m = both(-s.mean), k = both(s.inverse), mean_g = both(-s.g * team.over * s.inverse), mean_gx = both(-s.gx * s.inverse * team.over * s.inverse);
+            __syncthreads();
+        }
+
+        // ---- outputs, and sums over the rows
+        for (int begin = 0; begin < n;) {
+            if (walk.left == 0) {      // the first row of this CTA, or of a frame
+                walk.enter(a.m);
+                whole = walk.t == walk.frame * a.m.frame && from + begin + walk.left <= rows;
+                clear(sum_n);
+                clear(sum_hat);
+                clear(sum_y);
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        u[i][e] = mul2(add2(u[i][e], m), k);
-                        dy[i][e] = fma2(u[i][e], mean_gx, fma2(dy[i][e], k, mean_g));
+                    if (has(i)) {
+                        if (has_y) load_factor(gate[i], a.m.gate, walk.b, walk.frame, channel(i), 0.0f, a.m.post_weight);
+                        if (has_n) load_factor(scale[i], a.m.scale, walk.b, walk.frame, channel(i), 1.0f, a.m.weight);
                     }
             }
+            const int end = min(n, begin + walk.left);       // rows of this frame
+            const long long row0 = (long long)(first + from) * d;
+            R* dx_out = static_cast<R*>(a.dx) + row0;
+            T* dy_out = static_cast<T*>(a.dy) + row0;
+            for (int row = begin + group; row < end; row += shape.groups) {
+                const RowKnown kn = rows_n[row];
+                const f2 nm = both(kn.m), nk = both(kn.k), ng = both(kn.g), ngx = both(kn.gx);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
+                for (int i = 0; i < kVecs; ++i) {
+                    if (!has(i)) continue;
+                    const int c = row * d + channel(i);
+                    f2 dx[4] = {0, 0, 0, 0};
+                    if (has_r) read_tile(t.dr + c, dx);
+                    if (has_n) {
+                        f2 x[4], g[4];
+                        read_tile(t.r + c, x);
+                        read_tile(t.dn + c, g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum_y[i][e] = fma2(dx[i][e], u[i][e], sum_y[i][e]);
-                if (!ch.has(i)) continue;
-                Eight<T> o;
-                o.set(dy[i]);
-                o.store(dy_out + i * ch.step());
-            }
-            dy_out += d;
-        }
-        if (walk.left == 1 || row + 1 == rows) {   // the end of a frame, or of this team's part of it
-            const long long frame_at = ((long long)walk.b * a.frames + walk.frame) * d, slot = ((long long)team_at * 2 + (at_first ? 0 : 1)) * 3 * d;
+                        for (int e = 0; e < 4; ++e) {
+                            const f2 hat = mul2(add2(x[e], nm), nk);
+                            sum_n[i][e] = add2(sum_n[i][e], g[e]);
+                            sum_hat[i][e] = fma2(g[e], hat, sum_hat[i][e]);
+                            dx[e] = fma2(hat, ngx, fma2(mul2(g[e], scale[i][e]), nk, add2(dx[e], ng)));
+                        }
+                    }
+                    Eight<R> o;
+                    o.set(dx);
+                    o.store(dx_out + c);
+                    if (has_y) {
+                        f2 u[4], dy[4];
+                        read_tile(t.y + c, u);
+                        if (post) {
+                            const RowKnown ky = rows_y[row];
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                if (!ch.has(i)) continue;
-                const int c = ch.at(i);
-                f2 f[4];
-                if (has_weights) {
-                    load_factor(f, a.m.scale, walk.b, walk.frame, c, 1.0f, nullptr);
+                            for (int e = 0; e < 4; ++e) {
+                                u[e] = mul2(add2(u[e], both(ky.m)), both(ky.k));
+                                dy[e] = fma2(u[e], both(ky.gx), fma2(mul2(dx[e], gate[i][e]), both(ky.k), both(ky.g)));
+                            }
+                        } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) ws[(i * 8 + e) * ws_step] = fma2(f[e], sum_hat[i][e], ws[(i * 8 + e) * ws_step]);
-                    load_factor(f, a.m.gate, walk.b, walk.frame, c, 0.0f, nullptr);
+                            for (int e = 0; e < 4; ++e) dy[e] = mul2(dx[e], gate[i][e]);
+                        }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) ws[(i * 8 + 4 + e) * ws_step] = fma2(f[e], sum_y[i][e], ws[(i * 8 + 4 + e) * ws_step]);
+                        for (int e = 0; e < 4; ++e) sum_y[i][e] = fma2(dx[e], u[e], sum_y[i][e]);
+                        Eight<T> p;
+                        p.set(dy);
+                        p.store(dy_out + c);
+                    }
                 }
-                const FrameRows none{nullptr, 0, 0};
-                load_factor(f, none, 0, 0, c, 0.0f, a.m.weight);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum_hat[i][e] = mul2(sum_hat[i][e], f[e]);
-                load_factor(f, none, 0, 0, c, 0.0f, a.m.post_weight);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum_y[i][e] = mul2(sum_y[i][e], f[e]);
-                Eight<float> o;
-                auto put = [&](const f2 (&s)[4], float* whole_to, int which) {
-                    o.set(s);
-                    if (!whole) o.store(a.parts + slot + (long long)which * d + c);
-                    else if (whole_to != nullptr) o.store(whole_to + frame_at + c);
-                };
-                put(sum_y[i], a.dgate, 0);
-                put(sum_hat[i], a.dscale, 1);
-                put(sum_n[i], a.dshift, 2);
             }
-            at_first = false;
+            walk.left -= end - begin;
+            if (walk.left == 0 || from + end == rows) {   // the end of a frame, or of this CTA's part of it
+                if (shape.groups > 1) {       // (then a thread has one vector) the groups' sums, in their order
+                    auto join = [&](f2 (&s)[4]) {
+                        for (int g = 1; g < shape.groups; ++g) {
+                            __syncthreads();
+                            if (group == g) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) joined[column][e] = s[e];
+                            }
+                            __syncthreads();
+                            if (group == 0) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) s[e] = add2(s[e], joined[column][e]);
+                            }
+                        }
+                    };
+                    join(sum_n[0]);
+                    join(sum_hat[0]);
+                    join(sum_y[0]);
+                }
+                const long long frame_at = ((long long)walk.b * a.frames + walk.frame) * d, slot = ((long long)blockIdx.x * 2 + (at_first ? 0 : 1)) * 3 * d;
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i) {
+                    if (!has(i) || group != 0) continue;
+                    const int c = channel(i);
+                    f2 f[4];
+                    if (has_weights) {
+                        load_factor(f, a.m.scale, walk.b, walk.frame, c, 1.0f, nullptr);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum_w[i][e] = fma2(f[e], sum_hat[i][e], sum_w[i][e]);
+                        load_factor(f, a.m.gate, walk.b, walk.frame, c, 0.0f, nullptr);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum_p[i][e] = fma2(f[e], sum_y[i][e], sum_p[i][e]);
+                    }
+                    const FrameRows none{nullptr, 0, 0};
+                    load_factor(f, none, 0, 0, c, 0.0f, a.m.weight);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum_hat[i][e] = mul2(sum_hat[i][e], f[e]);
+                    load_factor(f, none, 0, 0, c, 0.0f, a.m.post_weight);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum_y[i][e] = mul2(sum_y[i][e], f[e]);
+                    Eight<float> o;
+                    auto put = [&](const f2 (&s)[4], float* whole_to, int which) {
+                        o.set(s);
+                        if (!whole) o.store(a.parts + slot + (long long)which * d + c);
+                        else if (whole_to != nullptr) o.store(whole_to + frame_at + c);
+                    };
+                    put(sum_y[i], a.dgate, 0);
+                    put(sum_hat[i], a.dscale, 1);
+                    put(sum_n[i], a.dshift, 2);
+                }
+                at_first = false;
+            }
+            // to the next frame, or stream
+            walk.t += end - begin;
+            if (walk.left == 0) ++walk.frame;
+            if (walk.t == a.m.T) {
+                walk.t = walk.frame = 0;
+                ++walk.b;
+            }
+            begin = end;
         }
-        walk.next(a.m);
+        __syncthreads();       // the tile after the next goes where this one was
+        if (shape.buffers == 1) send(tile + 1);
     }
-    if (has_weights) {
+    if (has_weights && group == 0) {
         Eight<float> o;
-        f2 f[4];
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-            if (!ch.has(i)) continue;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = ws[(i * 8 + 4 * k + e) * ws_step];
-                o.set(f);
-                o.store(a.weight_parts + ((long long)team_at * 2 + k) * d + ch.at(i));
-            }
+            if (!has(i)) continue;
+            o.set(sum_w[i]);
+            o.store(a.weight_parts + (long long)blockIdx.x * 2 * d + channel(i));
+            o.set(sum_p[i]);
+            o.store(a.weight_parts + ((long long)blockIdx.x * 2 + 1) * d + channel(i));
         }
     }
 }
@@ -1024,7 +1231,7 @@ struct Resident {
     std::atomic<int> found[kMaxDev][kTeamWarps + 1];
 };
 template <typename K>
-int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, const char* what)
+int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, int most_smem, const char* what)
 {
     int dev = -1;
     cudaError_t e = cudaGetDevice(&dev);
@@ -1034,7 +1241,7 @@ int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, co
     int sms = 0, per_sm = 0;
     e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     // (as much as any team width may ask for: the attribute is the kernel's, not the launch's)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmemPerCta - kRowStatic);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
     if (e != cudaSuccess || sms * per_sm < 1) {
         cudaGetLastError();
@@ -1073,27 +1280,43 @@ int launch_modulate(ModulateArgs a, RowPlan p, cudaStream_t st)
     constexpr int kPer = kVecs * kModulatePieces<T, R>;
     const int threads = p.warps * 32 * p.teams;
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
-    const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, "modulate");
+    const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, kMaxSmemPerCta - kRowStatic, "modulate");
     if (ctas < 0) return ctas;
     cut_rows(p, a.rows, (long long)ctas * p.teams);
     a.share = p.share;
     return check_launch(launch_block(kernel, dim3((unsigned)p.ctas), team_block(p), smem, st, a), "modulate_kernel");
 }
 
-template <typename T, typename R, int kVecs, bool kFull>
-int launch_modulate_backward(ModulateBackArgs a, RowPlan p, cudaStream_t st)
+// SMs of the current device
+int device_sms(const char* what)
+{
+    static std::atomic<int> found[kMaxDev];
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || dev < 0 || dev >= kMaxDev) { set_error("cannot identify the current device (%s)", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    int sms = found[dev].load(std::memory_order_relaxed);
+    if (sms != 0) return sms;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess || sms < 1) { set_error("%s: cannot read the SM count (%s)", what, cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
+    found[dev].store(sms, std::memory_order_relaxed);
+    return sms;
+}
+
+template <typename T, typename R, int kVecs, bool kAll>
+int launch_modulate_backward(ModulateBackArgs a, cudaStream_t st)
 {
     static Resident resident;
-    auto kernel = modulate_backward_kernel<T, R, kVecs, kFull>;
-    constexpr int kPer = kVecs * kModulateBackPieces<T, R>;
-    const int threads = p.warps * 32 * p.teams;
-    const size_t smem = (size_t)threads * (16 * kPer * row_stages(kPer, row_threads(kVecs), 64 * kVecs) + 64 * kVecs);
-    const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, "modulate_backward");
+    auto kernel = modulate_backward_kernel<T, R, kVecs, kAll>;
+    const int row_bytes = a.m.d * 2 * (int)(sizeof(T) + sizeof(R));
+    const int ctas = resident_ctas(resident, kernel, 0, kTileThreads, kTileRoom, kTileRoom, "modulate_backward");    // (one to an SM)
     if (ctas < 0) return ctas;
-    cut_rows(p, a.m.rows, std::min<long long>((long long)ctas * p.teams, block_runs(a.m.d, modulate_back_vecs(a.m.d))), kLeastRows);
+    RowPlan p;
+    p.teams = 1;
+    cut_rows(p, a.m.rows, std::min(ctas, kTileRuns));
     a.m.share = p.share;
+    const TileShape shape = tile_shape(a.m.d, row_bytes, kTileRoom, p.share);
     if (a.dweight == nullptr && a.dpost_weight == nullptr) a.weight_parts = nullptr;
-    int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), team_block(p), smem, st, a), "modulate_backward_kernel");
+    int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), dim3(kTileThreads), shape.buffers * shape.buffer, st, a, shape), "modulate_backward_kernel");
     if (r < 0) return r;
     // a frame that several runs share, or weights: their parts are added up
     const bool shared = a.m.frame > 1 && p.runs > 1 && (a.dgate != nullptr || a.dscale != nullptr || a.dshift != nullptr);
@@ -1127,7 +1350,7 @@ int launch_rotate(RotateArgs a, RowPlan q, cudaStream_t st)
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
-    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, "rotate");
+    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic, "rotate");
     if (ctas < 0) return ctas;
     cut_rotation(q, k, a, ctas, 1LL << 40, 1);
     a.q_share = q.share;
@@ -1145,7 +1368,7 @@ int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
-    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, "rotate_backward");
+    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic, "rotate_backward");
     if (ctas < 0) return ctas;
     if (a.dq_weight == nullptr && a.dk_weight == nullptr) a.parts = nullptr;
     cut_rotation(q, k, a.r, ctas, a.parts != nullptr ? block_runs(std::max(a.r.q_width, a.r.k_width), kRotateBackVecs) : 1LL << 40, a.parts != nullptr ? kLeastRows : 1);
@@ -1183,9 +1406,11 @@ int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st)
 
 int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st)
 {
-    const RowPlan p = team_shape(a.m.d, modulate_back_vecs(a.m.d));
-#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, v, f>(a, p, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, v, f>(a, p, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, v, f>(a, p, st))
-    return ARL2_UP_TO_2(p, is_full(p, a.m.d), ARL2_CALL);
+    const int vecs = (a.m.d / 8 + kTileThreads - 1) / kTileThreads;
+    const bool all = a.dn != nullptr && a.dr != nullptr && a.m.y != nullptr && a.m.post_norm == kNormNone && a.m.weight == nullptr;
+#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, v, f>(a, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, v, f>(a, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, v, f>(a, st))
+    if (all) return vecs == 1 ? ARL2_CALL(1, true) : vecs == 2 ? ARL2_CALL(2, true) : ARL2_CALL(3, true);
+    return vecs == 1 ? ARL2_CALL(1, false) : vecs == 2 ? ARL2_CALL(2, false) : ARL2_CALL(3, false);
 #undef ARL2_CALL
 }
 

@@ -266,7 +266,7 @@ enum RowNorm : int { kNormNone = ARL2_NORM_NONE, kNormLayer = ARL2_NORM_LAYER, k
 constexpr int kBlockMostChannels = 8192;   // of a row: of the modulation, of queries, of keys
 // How a row of d channels is held: `warps` warps whose lanes have `vecs` groups of eight channels each, at most `most` of them; teams of
 // warps that make up a CTA; and the runs of rows whose sums over tokens have room in a workspace: those of four CTAs per SM of 148.
-constexpr int modulate_back_vecs(int d) { return d <= 4096 ? 1 : 2; }      // (512 threads with 128 registers each hold one vector)
+constexpr int kTileRuns = 4 * 148;           // runs of the modulation's backward pass
 constexpr int kModulateVecs = 2, kRotateVecs = 4, kRotateBackVecs = 2;
 constexpr int block_warps(int d, int most) { return (d / 8 + 32 * most - 1) / (32 * most); }
 constexpr int block_vecs(int d, int most) { return (d / 8 + 32 * block_warps(d, most) - 1) / (32 * block_warps(d, most)); }

@@ -165,6 +165,27 @@ struct RowRing {
         f[3] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
     }
 };
+// Eight channels from shared memory; of fp32 the halves in another order every four lanes, so that they fall on different banks.
+__device__ __forceinline__ void read_tile(const __nv_bfloat16* p, f2 (&f)[4])
+{
+    Eight<__nv_bfloat16> e;
+    e.u = *reinterpret_cast<const uint4*>(p);
+    e.get(f);
+}
+__device__ __forceinline__ void read_tile(const float* p, f2 (&f)[4])
+{
+    const int odd = threadIdx.x >> 2 & 1;
+    const ulonglong2 u = *reinterpret_cast<const ulonglong2*>(p + 4 * odd), w = *reinterpret_cast<const ulonglong2*>(p + 4 * (1 - odd));
+    f[0] = odd ? w.x : u.x; f[1] = odd ? w.y : u.y;
+    f[2] = odd ? u.x : w.x; f[3] = odd ? u.y : w.y;
+}
+__device__ __forceinline__ void copy_piece(void* to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kNewer> __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(kNewer) : "memory"); }
+
 // rows that are read again and again: through L1
 __device__ __forceinline__ void load_kept(const float* p, f2 (&f)[4])
 {
