@@ -304,7 +304,11 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
 // there are threads for it, makes the outputs and keeps the sums over tokens in registers.  Sums of a row thus cost a warp's
 // shuffles once, and there are two barriers a tile.  (Teams of warps that do both at once, an exchange per row, spent 470 instructions
 // of a warp on a row's 256 channels: 55 us for 9360 rows of 1536, now @MB@.)
-constexpr int kTileThreads = 384, kTileWarps = kTileThreads / 32;
+// Threads of a CTA, and CTAs of an SM at least: small ones for rows of up to 1536 channels, so that some of them fit beside one another
+// and work while others wait.
+constexpr int kFewCtas = 2;
+constexpr int kTileFew = 192, kTileMany = 384, kTileWarps = kTileMany / 32;
+constexpr int tile_ctas(int threads) { return threads == kTileFew ? kFewCtas : 1; }
 struct TileShape {
     int rows;            // of a tile
     int split;           // warps of a row
@@ -314,19 +318,20 @@ struct TileShape {
     int buffers;         // two, or one where rows are so wide
 };
 // Tiles of `row_bytes` a row: two in `room` bytes of shared memory, no more rows than the CTA has altogether.
-TileShape tile_shape(int d, int row_bytes, int room, int most_rows)
+TileShape tile_shape(int d, int row_bytes, int room, int most_rows, int threads)
 {
     TileShape s;
     s.rows = std::max(1, std::min({room / 2 / row_bytes, most_rows, 2 * kTileWarps}));
     const int vecs = d / 8;
-    s.split = std::max(1, std::min(kTileWarps / s.rows, (vecs + 31) / 32));
-    s.vecs = (vecs + kTileThreads - 1) / kTileThreads;
-    s.groups = std::max(1, std::min(kTileThreads / vecs, s.rows));
+    s.split = std::max(1, std::min(threads / 32 / s.rows, (vecs + 31) / 32));
+    s.vecs = (vecs + threads - 1) / threads;
+    s.groups = std::max(1, std::min(threads / vecs, s.rows));
     s.buffer = s.rows * row_bytes;
     s.buffers = 2 * s.buffer <= room ? 2 : 1;
     return s;
 }
-constexpr int kTileRoom = kMaxSmemPerCta - 13 * 1024;     // what is left of a CTA's shared memory for the tiles
+// What is left of a CTA's shared memory for the tiles
+constexpr int tile_room(int threads) { return ((kMaxSmemPerCta + 1024) / tile_ctas(threads) - 1024 - threads * 16 - 3 * 1024) / 128 * 128; }
 
 // What is known of a row: -mean, 1 / deviation, and what dx takes off: (mean(g) and mean(g hat)) / deviation, negative.
 struct RowKnown { float m, k, g, gx; };
@@ -362,9 +367,10 @@ struct ModulateTile {
 //   dw = sum (1 + scale) dn hat;   dy = the same of P for the gradient dx gate w_post, dw_post = sum gate dx yhat.
 // Six units of memory: r, dn, dr and y in, dx and dy out.  The weights' sums are made from the frames' sums.
 // kAll: all four are there, no P and no weights (flags that are known cost nothing in the loops).
-template <typename T, typename R, int kVecs, bool kAll>
-__global__ void __launch_bounds__(kTileThreads, 1) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a, const __grid_constant__ TileShape shape)
+template <typename T, typename R, int kTileThreads, int kVecs, bool kAll>
+__global__ void __launch_bounds__(kTileThreads, tile_ctas(kTileThreads)) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a, const __grid_constant__ TileShape shape)
 {
+    constexpr int kTileWarps = kTileThreads / 32;
     extern __shared__ __align__(16) uint8_t tile_smem[];
     __shared__ __align__(16) RowKnown rows_n[2 * kTileWarps], rows_y[2 * kTileWarps];
     __shared__ __align__(16) RowPart part_n[2 * kTileWarps], part_y[2 * kTileWarps];     // (rows that are not there are read, too)
@@ -1302,19 +1308,20 @@ int device_sms(const char* what)
     return sms;
 }
 
-template <typename T, typename R, int kVecs, bool kAll>
+template <typename T, typename R, int kTileThreads, int kVecs, bool kAll>
 int launch_modulate_backward(ModulateBackArgs a, cudaStream_t st)
 {
     static Resident resident;
-    auto kernel = modulate_backward_kernel<T, R, kVecs, kAll>;
+    auto kernel = modulate_backward_kernel<T, R, kTileThreads, kVecs, kAll>;
+    constexpr int kRoom = tile_room(kTileThreads);
     const int row_bytes = a.m.d * 2 * (int)(sizeof(T) + sizeof(R));
-    const int ctas = resident_ctas(resident, kernel, 0, kTileThreads, kTileRoom, kTileRoom, "modulate_backward");    // (one to an SM)
+    const int ctas = resident_ctas(resident, kernel, 0, kTileThreads, kRoom, kRoom, "modulate_backward");
     if (ctas < 0) return ctas;
     RowPlan p;
     p.teams = 1;
     cut_rows(p, a.m.rows, std::min(ctas, kTileRuns));
     a.m.share = p.share;
-    const TileShape shape = tile_shape(a.m.d, row_bytes, kTileRoom, p.share);
+    const TileShape shape = tile_shape(a.m.d, row_bytes, kRoom, p.share, kTileThreads);
     if (a.dweight == nullptr && a.dpost_weight == nullptr) a.weight_parts = nullptr;
     int r = check_launch(launch_block(kernel, dim3((unsigned)p.ctas), dim3(kTileThreads), shape.buffers * shape.buffer, st, a, shape), "modulate_backward_kernel");
     if (r < 0) return r;
@@ -1406,11 +1413,12 @@ int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st)
 
 int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st)
 {
-    const int vecs = (a.m.d / 8 + kTileThreads - 1) / kTileThreads;
+    const int vecs = a.m.d / 8, each = (vecs + kTileMany - 1) / kTileMany;
     const bool all = a.dn != nullptr && a.dr != nullptr && a.m.y != nullptr && a.m.post_norm == kNormNone && a.m.weight == nullptr;
-#define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, v, f>(a, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, v, f>(a, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, v, f>(a, st))
-    if (all) return vecs == 1 ? ARL2_CALL(1, true) : vecs == 2 ? ARL2_CALL(2, true) : ARL2_CALL(3, true);
-    return vecs == 1 ? ARL2_CALL(1, false) : vecs == 2 ? ARL2_CALL(2, false) : ARL2_CALL(3, false);
+#define ARL2_CALL(n, v, f) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, n, v, f>(a, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, n, v, f>(a, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, n, v, f>(a, st))
+    if (vecs <= kTileFew) return all ? ARL2_CALL(kTileFew, 1, true) : ARL2_CALL(kTileFew, 1, false);
+    if (all) return each == 1 ? ARL2_CALL(kTileMany, 1, true) : each == 2 ? ARL2_CALL(kTileMany, 2, true) : ARL2_CALL(kTileMany, 3, true);
+    return each == 1 ? ARL2_CALL(kTileMany, 1, false) : each == 2 ? ARL2_CALL(kTileMany, 2, false) : ARL2_CALL(kTileMany, 3, false);
 #undef ARL2_CALL
 }
 
