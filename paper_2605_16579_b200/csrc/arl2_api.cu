@@ -1715,7 +1715,7 @@ RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c
     l.states = off;  off += state;
     l.dstates = off; off += back ? state : 0;
     l.beside = off;  off += back && tc ? state : 0;
-    l.dots = off;    off += back ? align_up((size_t)cfg.B * cfg.H * blocks * (dd / 128) * sizeof(float)) : 0;
+    l.dots = off;    off += back ? align_up((size_t)cfg.B * cfg.H * blocks * (dd / 32) * sizeof(float)) : 0;
     l.total = off;
     return l;
 }

@@ -397,12 +397,29 @@ struct RecurArgs {
     float* dstates;          // ... and the gradient of the state after block n
     __nv_bfloat16* states_op;    // the same as a bf16 head and a bf16 remainder, [.., pair, 2, D, D] (tensor cores)
     __nv_bfloat16* dstates_op;
-    float* dots;             // [B, H, N, D * D / 128]: parts of <dstate, state>
+    float* dots;             // [B, H, N, dot_parts]: parts of <dstate, state>
+    int dot_parts;           // D * D / 128, or D * D / 32 (set by the launcher)
     uint32_t* status;
     uint32_t wait_limit;
     RecurStep sums, rows;
 };
 __host__ __device__ inline int recur_heads(const RecurArgs& a) { return (a.H + a.pair - 1) / a.pair; }
+__device__ __forceinline__ float gate_of(float logit) { return 1.0f / (1.0f + expf(-logit)); }
+// da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n> for blocks of heads u, u + step, ..: a warp each, in the kernel behind the scan
+__device__ __forceinline__ void recur_gates(const RecurArgs& a, int u, int step)
+{
+    if (!a.back || a.ddecay == nullptr) return;
+    for (; u < a.B * a.H * a.N; u += step) {
+        float s = 0.0f;
+        for (int i = threadIdx.x & 31; i < a.dot_parts; i += 32) s += a.dots[(size_t)u * a.dot_parts + i];
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        const int bh = u / a.N, n = u - bh * a.N, b = bh / a.H;
+        const size_t at = ((size_t)b * a.N + n) * a.H + bh - b * a.H;
+        const float x = a.decay[at];
+        // (alpha (1 - alpha) without the difference, which loses its digits near 1)
+        if ((threadIdx.x & 31) == 0) a.ddecay[at] = s * gate_of(x) * gate_of(-x);
+    }
+}
 int recur(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st);
 // whether the tensors can be read by tiled copies
 bool tc_recur_supported(const RecurArgs& a);

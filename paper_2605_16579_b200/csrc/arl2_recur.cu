@@ -19,8 +19,6 @@ namespace {
 constexpr int kMaxDev = 64;
 constexpr int kRThreads = 256;
 
-__device__ __forceinline__ float gate_of(float logit) { return 1.0f / (1.0f + expf(-logit)); }
-
 // ---- TF32 fragments ------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t tf32_head(float x)
 {
@@ -202,6 +200,7 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
     const int m0 = (warp >> 1) * 16, n0 = (warp & 1) * kN * 8;
     const int first = blockIdx.x * a.rows.share, last = min(first + a.rows.share, a.rows.tiles);
     grid_dependency_sync();
+    recur_gates(a, blockIdx.x * (kRThreads / 32) + warp, gridDim.x * (kRThreads / 32));
     if (first >= last) return;
 
     float4 xr[kLoads];
@@ -299,127 +298,150 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
 }
 
 // ---- the scan over the blocks --------------------------------------------------------------------------
-// A thread has four elements of a head's state.  The sums of several blocks are asked for before the first is used.
-constexpr int kScanThreads = 256, kScanAhead = 4;
+// A thread has kEach elements of a head's state, four, or one where the heads are few: what it takes is latencies.  Where a
+// block's sums are and how it is gated is found for many blocks at once, a thread each; the sums of kScanAhead blocks are asked for
+// before the first is used.
+constexpr int kScanThreads = 256, kScanAhead = 8;
 
-template <int D>
-__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, size_t unit, int in_pair, int pair, int e, const float4& s)
+template <int kEach> struct ScanValue;
+template <> struct ScanValue<1> {
+    float v[1];
+    __device__ __forceinline__ void load(const float* p) { v[0] = *p; }
+    __device__ __forceinline__ void store(float* p) const { *p = v[0]; }
+};
+template <> struct ScanValue<4> {
+    float v[4];
+    __device__ __forceinline__ void load(const float* p)
+    {
+        const float4 f = *reinterpret_cast<const float4*>(p);
+        v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+    }
+    __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+};
+
+template <int D, int kEach>
+__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, size_t unit, int in_pair, int pair, int e, const ScanValue<kEach>& s)
 {
-    if (f32 != nullptr) *reinterpret_cast<float4*>(f32 + (unit * pair + in_pair) * D * D + e) = s;
+    if (f32 != nullptr) s.store(f32 + (unit * pair + in_pair) * D * D + e);
     if (op == nullptr) return;
     // head and remainder: 2^-17 of the value together; an infinity has no remainder
     __nv_bfloat16* h = op + ((unit * pair + in_pair) * 2) * D * D + e;
-    const float x[4] = {s.x, s.y, s.z, s.w};
-    __nv_bfloat16 hi[4], lo[4];
+    __nv_bfloat16 hi[kEach], lo[kEach];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        hi[i] = __float2bfloat16_rn(x[i]);
+    for (int i = 0; i < kEach; ++i) {
+        hi[i] = __float2bfloat16_rn(s.v[i]);
         const float back = __bfloat162float(hi[i]);
-        lo[i] = __float2bfloat16_rn(fabsf(back) <= 3.3e38f ? x[i] - back : 0.0f);
+        lo[i] = __float2bfloat16_rn(fabsf(back) <= 3.3e38f ? s.v[i] - back : 0.0f);
     }
-    *reinterpret_cast<uint2*>(h) = *reinterpret_cast<uint2*>(hi);
-    *reinterpret_cast<uint2*>(h + D * D) = *reinterpret_cast<uint2*>(lo);
+    if (kEach == 4) {
+        *reinterpret_cast<uint2*>(h) = *reinterpret_cast<uint2*>(hi);
+        *reinterpret_cast<uint2*>(h + D * D) = *reinterpret_cast<uint2*>(lo);
+    } else {
+        *h = hi[0];
+        h[D * D] = lo[0];
+    }
 }
 
-// The sum of block n of operand pair `which`, as the CTAs of the first step left it.
-template <int D>
-__device__ __forceinline__ float4 scan_sum(const RecurArgs& a, int which, int b, int head, int n, int e)
+// The parts of a block's sum: `count` slots from `first` on, or none; and the block's gate.
+struct ScanBlock { int first, count; float gate; };
+__device__ __forceinline__ ScanBlock scan_block(const RecurArgs& a, int which, int b, int head, int n)
 {
-    const int hu = head / a.pair, heads = recur_heads(a);
+    ScanBlock r = {0, 0, gate_of(a.decay[((size_t)b * a.N + n) * a.H + head])};
     for (int i = 0; i < a.sums.jobs; ++i) {
         const RecurJob& j = a.sums.job[i];
         if (j.which != which || n < j.n0 || n >= j.n0 + j.n_count) continue;
-        const int v = (b * heads + hu) * j.n_count + n - j.n0, unit = j.unit0 + v;
-        const int c0 = (j.tile0 + v * j.ntile) / a.sums.share, c1 = (j.tile0 + v * j.ntile + j.ntile - 1) / a.sums.share;
-        const size_t size = (size_t)a.pair * D * D;
-        const float* p = a.slots + (size_t)(unit + c0) * size + (size_t)(head - hu * a.pair) * D * D + e;
-        float4 s = *reinterpret_cast<const float4*>(p);
-        for (int c = c0 + 1; c <= c1; ++c) {
-            p += size;
-            const float4 o = *reinterpret_cast<const float4*>(p);
-            s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
-        }
-        return s;
+        const int v = (b * recur_heads(a) + head / a.pair) * j.n_count + n - j.n0, tile = j.tile0 + v * j.ntile;
+        const int c0 = tile / a.sums.share, c1 = (tile + j.ntile - 1) / a.sums.share;
+        r.first = j.unit0 + v + c0;
+        r.count = c1 - c0 + 1;
     }
-    return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    return r;
 }
 
-template <int D>
+template <int D, int kEach>
 __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_constant__ RecurArgs a)
 {
-    const int e = (blockIdx.x * kScanThreads + threadIdx.x) * 4, head = blockIdx.y, b = blockIdx.z;
+    __shared__ ScanBlock blocks[kScanThreads];
+    const int tid = threadIdx.x, e = (blockIdx.x * kScanThreads + tid) * kEach, head = blockIdx.y, b = blockIdx.z;
     const int hu = head / a.pair, in_pair = head - hu * a.pair;
-    const size_t unit0 = (size_t)(b * recur_heads(a) + hu) * a.N;
-    const size_t at = ((size_t)b * a.H + head) * D * D + e;
+    const size_t unit0 = (size_t)(b * recur_heads(a) + hu) * a.N, at = ((size_t)b * a.H + head) * D * D + e, size = (size_t)a.pair * D * D;
+    const float* slots = a.slots + (size_t)in_pair * D * D + e;
+    using Value = ScanValue<kEach>;
     grid_dependency_sync();
-    const float* decay = a.decay + (size_t)b * a.N * a.H + head;
-    auto step = [](float4& s, float g, const float4& add) {
-        s.x = fmaf(g, s.x, add.x); s.y = fmaf(g, s.y, add.y); s.z = fmaf(g, s.z, add.z); s.w = fmaf(g, s.w, add.w);
+    // the sums of blocks n, n + way, ..: all their first parts before any other
+    auto fetch = [&](Value (&sum)[kScanAhead], int i0, int way, int count) {
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) sum[i].v[k] = 0.0f;
+            if (i < count && blocks[i0 + i * way].count > 0) sum[i].load(slots + (size_t)blocks[i0 + i * way].first * size);
+        }
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i)
+            if (i < count)
+                for (int c = 1; c < blocks[i0 + i * way].count; ++c) {
+                    Value o;
+                    o.load(slots + (size_t)(blocks[i0 + i * way].first + c) * size);
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) sum[i].v[k] += o.v[k];
+                }
     };
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (a.state_in != nullptr) s = *reinterpret_cast<const float4*>(a.state_in + at);
-    for (int n0 = 0; n0 < a.N; n0 += kScanAhead) {
-        float4 sum[kScanAhead];
-        float g[kScanAhead];
+    Value s;
 #pragma unroll
-        for (int i = 0; i < kScanAhead; ++i)
-            if (n0 + i < a.N) {
-                sum[i] = scan_sum<D>(a, 0, b, head, n0 + i, e);
-                g[i] = gate_of(decay[(size_t)(n0 + i) * a.H]);
-            }
+    for (int k = 0; k < kEach; ++k) s.v[k] = 0.0f;
+    if (a.state_in != nullptr) s.load(a.state_in + at);
+    for (int base = 0; base < a.N; base += kScanThreads) {
+        const int here = min(kScanThreads, a.N - base);
+        __syncthreads();
+        if (tid < here) blocks[tid] = scan_block(a, 0, b, head, base + tid);
+        __syncthreads();
+        for (int i0 = 0; i0 < here; i0 += kScanAhead) {
+            Value sum[kScanAhead];
+            fetch(sum, i0, 1, here - i0);
 #pragma unroll
-        for (int i = 0; i < kScanAhead; ++i)
-            if (n0 + i < a.N) {
-                scan_store<D>(a.states, a.states_op, unit0 + n0 + i, in_pair, a.pair, e, s);
-                step(s, g[i], sum[i]);
-            }
+            for (int i = 0; i < kScanAhead; ++i)
+                if (i0 + i < here) {
+                    scan_store<D>(a.states, a.states_op, unit0 + base + i0 + i, in_pair, a.pair, e, s);
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) s.v[k] = fmaf(blocks[i0 + i].gate, s.v[k], sum[i].v[k]);
+                }
+        }
     }
     if (!a.back) {
-        if (a.state_out != nullptr) *reinterpret_cast<float4*>(a.state_out + at) = s;
+        if (a.state_out != nullptr) s.store(a.state_out + at);
         return;
     }
-    s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (a.dstate_out != nullptr) s = *reinterpret_cast<const float4*>(a.dstate_out + at);
-    for (int n0 = a.N - 1; n0 >= 0; n0 -= kScanAhead) {
-        float4 sum[kScanAhead], before[kScanAhead];
-        float g[kScanAhead];
 #pragma unroll
-        for (int i = 0; i < kScanAhead; ++i)
-            if (n0 - i >= 0) {
-                sum[i] = scan_sum<D>(a, 1, b, head, n0 - i, e);
-                g[i] = gate_of(decay[(size_t)(n0 - i) * a.H]);
-                before[i] = *reinterpret_cast<const float4*>(a.states + ((unit0 + n0 - i) * a.pair + in_pair) * D * D + e);   // (this thread's own)
-            }
+    for (int k = 0; k < kEach; ++k) s.v[k] = 0.0f;
+    if (a.dstate_out != nullptr) s.load(a.dstate_out + at);
+    float* dots = a.dots + ((size_t)b * a.H + head) * a.N * (D * D / (32 * kEach)) + e / (32 * kEach);
+    for (int base = (a.N - 1) / kScanThreads * kScanThreads; base >= 0; base -= kScanThreads) {
+        const int here = min(kScanThreads, a.N - base);
+        __syncthreads();
+        if (tid < here) blocks[tid] = scan_block(a, 1, b, head, base + tid);
+        __syncthreads();
+        for (int i0 = here - 1; i0 >= 0; i0 -= kScanAhead) {
+            Value sum[kScanAhead], before[kScanAhead];
 #pragma unroll
-        for (int i = 0; i < kScanAhead; ++i)
-            if (n0 - i >= 0) {
-                const int n = n0 - i;
-                scan_store<D>(a.dstates, a.dstates_op, unit0 + n, in_pair, a.pair, e, s);
-                const float dot = warp_sum(s.x * before[i].x + s.y * before[i].y + s.z * before[i].z + s.w * before[i].w);
-                if ((threadIdx.x & 31) == 0) a.dots[(((size_t)b * a.H + head) * a.N + n) * (D * D / 128) + e / 128] = dot;
-                step(s, g[i], sum[i]);
-            }
+            for (int i = 0; i < kScanAhead; ++i)
+                if (i0 - i >= 0) before[i].load(a.states + ((unit0 + base + i0 - i) * a.pair + in_pair) * D * D + e);   // (this thread's own)
+            fetch(sum, i0, -1, i0 + 1);
+#pragma unroll
+            for (int i = 0; i < kScanAhead; ++i)
+                if (i0 - i >= 0) {
+                    const int n = base + i0 - i;
+                    scan_store<D>(a.dstates, a.dstates_op, unit0 + n, in_pair, a.pair, e, s);
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) dot = fmaf(s.v[k], before[i].v[k], dot);
+                    dot = warp_sum(dot);
+                    if ((tid & 31) == 0) dots[(size_t)n * (D * D / (32 * kEach))] = dot;
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) s.v[k] = fmaf(blocks[i0 - i].gate, s.v[k], sum[i].v[k]);
+                }
+        }
     }
-    if (a.dstate_in != nullptr) *reinterpret_cast<float4*>(a.dstate_in + at) = s;
-}
-
-// da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n>: a warp each
-template <int D>
-__global__ void __launch_bounds__(kScanThreads) recur_gates_kernel(const __grid_constant__ RecurArgs a)
-{
-    constexpr int kParts = D * D / 128;
-    grid_dependency_sync();
-    const long long u = ((long long)blockIdx.x * kScanThreads + threadIdx.x) >> 5;
-    if (u >= (long long)a.B * a.H * a.N) return;
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kParts / 32; ++i) s += a.dots[u * kParts + i * 32 + (threadIdx.x & 31)];
-    s = warp_sum(s);
-    if ((threadIdx.x & 31) != 0) return;
-    const long long bh = u / a.N, n = u - bh * a.N, b = bh / a.H, h = bh - b * a.H, at = (b * a.N + n) * a.H + h;
-    const float x = a.decay[at];
-    // (alpha (1 - alpha) without the difference, which loses its digits near 1)
-    a.ddecay[at] = s * gate_of(x) * gate_of(-x);
+    if (a.dstate_in != nullptr) s.store(a.dstate_in + at);
 }
 
 template <typename K>
@@ -442,11 +464,18 @@ int set_up(std::atomic<int>& resident, K kernel, int smem, const char* what)
     return ctas;
 }
 
+// Elements of a thread: one where with four there would be CTAs for fewer than half of 148 SMs (us of a backward scan over 21 blocks of
+// 2 x 5 heads of 64 channels, 40 CTAs with four: @S1@; over 7 blocks of 12 heads of 128, 192 CTAs: 23 with four, 37 with one).
+int scan_each(const RecurArgs& a) { return (long long)a.B * a.H * a.D * a.D / (4 * kScanThreads) < 148 / 2 ? 1 : 4; }
+
 template <int D>
-int launch_scan(const RecurArgs& a, cudaStream_t st)
+int launch_scan(RecurArgs& a, cudaStream_t st)
 {
-    int r = check_launch(launch_kernel(recur_scan_kernel<D>, dim3(D * D / (4 * kScanThreads), (unsigned)a.H, (unsigned)a.B), kScanThreads, 0, st, a), "recur_scan_kernel");
-    return r;
+    const int each = scan_each(a);
+    const dim3 grid((unsigned)(D * D / (each * kScanThreads)), (unsigned)a.H, (unsigned)a.B);
+    a.dot_parts = D * D / (32 * each);
+    return check_launch(each == 1 ? launch_kernel(recur_scan_kernel<D, 1>, grid, kScanThreads, 0, st, a) : launch_kernel(recur_scan_kernel<D, 4>, grid, kScanThreads, 0, st, a),
+                        "recur_scan_kernel");
 }
 
 template <typename T, int D>
@@ -494,10 +523,7 @@ int run_any(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st)
         n = dtype == ARL2_FP32 ? run_plain<float, D>(a, st) : run_plain<__nv_bfloat16, D>(a, st);
         if (n < 0) return n;
     }
-    if (!a.back || a.ddecay == nullptr) return n;
-    const long long units = (long long)a.B * a.H * a.N;
-    const int r = check_launch(launch_kernel(recur_gates_kernel<D>, dim3((unsigned)((units * 32 + kScanThreads - 1) / kScanThreads)), kScanThreads, 0, st, a), "recur_gates_kernel");
-    return r < 0 ? r : n + r;
+    return n;
 }
 
 }  // namespace

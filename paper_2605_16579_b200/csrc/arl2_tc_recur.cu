@@ -326,6 +326,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         mma_commit_if(lead, ubars + 8 * kRBarDrain);
         drain_bar(ubars + 8 * kRBarDrain, 0);
     } else {
+        recur_gates(a, blockIdx.x * 8 + warp - 2, gridDim.x * 8);      // (while the first tiles are on their way)
         const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
         for (int k = 0; k < count; ++k) {
