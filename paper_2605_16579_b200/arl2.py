@@ -657,6 +657,7 @@ class _BlockOp:
         self._lib, self._index = layer._lib, layer.device.index
         self._B, self._H, self._D = layer.B, layer.H, layer.D
         self._width = layer.H * layer.D
+        self._sizes = {}
 
     def _run(self, call, *args):
         ctx = self.layer._ctx
@@ -674,17 +675,35 @@ class _BlockOp:
 
     def _strided(self, t, shape, dtype, what, inner):
         """arl2_rows of a tensor [B, rows, ...] whose dimensions from `inner` on are contiguous."""
-        if isinstance(t, torch.Tensor) and t.get_device() == self._index and t.dtype is dtype and t.shape == shape:
+        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self._index and t.shape == shape:
+            if t.is_contiguous():
+                row = shape[2] if inner + 1 == len(shape) else shape[2] * shape[3]
+                return arl2_rows(t.data_ptr(), shape[1] * row, row)
             st, row = t.stride(), 1
-            for n, s in zip(reversed(shape[inner:]), reversed(st[inner:])):
-                if n != 1 and s != row:
+            for i in range(len(shape) - 1, inner - 1, -1):
+                if shape[i] != 1 and st[i] != row:
                     break
-                row *= n
+                row *= shape[i]
             else:
                 # (a dimension of one element may have any stride)
                 return arl2_rows(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else row)
         raise Arl2Error(f"{what}: expected a tensor {tuple(shape)} {dtype} on {self.device} with contiguous rows, got "
                         + (f"{tuple(t.shape)} {t.dtype} with strides {tuple(t.stride())} on {t.device}" if isinstance(t, torch.Tensor) else f"{t!r}"))
+
+    def _fp32(self, like):
+        """A contiguous fp32 tensor of another's shape, or None."""
+        return None if like is None else torch.empty_like(like, memory_format=torch.contiguous_format)
+
+    def _bytes(self, call, *key):
+        """What a size query of the library says: a function of the configurations and the tokens alone, asked once."""
+        n = self._sizes.get(key)
+        if n is None:
+            n = call(ctypes.byref(self.layer.cfg), self._cfg, *key)
+            if n == 0:
+                raise Arl2Error(f"{call.__name__}: " + self._lib.arl2_last_error().decode())
+            if len(self._sizes) < 256:
+                self._sizes[key] = n
+        return n
 
     def _tokens(self, t, what, dims):
         if not isinstance(t, torch.Tensor) or t.dim() != dims:
@@ -722,10 +741,7 @@ class Modulation(_BlockOp):
         self.workspace_bytes(1)     # (what the library refuses is refused here)
 
     def workspace_bytes(self, tokens):
-        n = self._lib.arl2_modulation_workspace_bytes(ctypes.byref(self.layer.cfg), self._cfg, tokens)
-        if n == 0:
-            raise Arl2Error("arl2_modulation_workspace_bytes: " + self._lib.arl2_last_error().decode())
-        return n
+        return self._bytes(self._lib.arl2_modulation_workspace_bytes, tokens)
 
     def _frames(self, tokens):
         return -(-tokens // self.frame_tokens)
@@ -760,7 +776,7 @@ class Modulation(_BlockOp):
             if n is not None:
                 raise Arl2Error("n: nothing is written with normed=False")
         elif n is None:
-            n = torch.empty(shape, dtype=self.dtype, device=self.device)
+            n = torch.empty_like(y) if y is not None else torch.empty(shape, dtype=self.dtype, device=self.device)
         else:
             want(n, shape, self.dtype, "n")
         self._run(self._lib.arl2_modulate, self._cfg, tokens, x.data_ptr(), _ptr(y), self._modulation(gate, tokens, "gate"),
@@ -770,7 +786,7 @@ class Modulation(_BlockOp):
 
     def backward(self, r, dn=None, dr=None, y=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, workspace=None):
         """Gradients (dx, dy, dgate, dscale, dshift, dweight, dpost_weight) from dn and dr, those of n and r (either may be None); None for
-        what forward was called without.  ``r`` is what forward returned; ``shift`` is not looked at beyond whether there is one."""
+        what forward was called without.  ``r`` is what forward returned; ``shift`` is not read."""
         tokens = self._tokens(dn if dr is None else dr, "dn or dr", 3)
         shape, want = (self._B, tokens, self._width), self.layer._want
         if r is not None or dn is not None:
@@ -778,15 +794,17 @@ class Modulation(_BlockOp):
         for t, kind, what in ((dn, self.dtype, "dn"), (dr, self.residual, "dr"), (y, self.dtype, "y")):
             if t is not None:
                 want(t, shape, kind, what)
-        rows = (self._B, self._frames(tokens), self._width)
-        empty = lambda given, shape: None if given is None else torch.empty(shape, dtype=torch.float32, device=self.device)  # noqa: E731
-        dx = torch.empty(shape, dtype=self.residual, device=self.device)
+        gate_rows, scale_rows = self._modulation(gate, tokens, "gate"), self._modulation(scale, tokens, "scale")
+        if shift is not None:
+            self._modulation(shift, tokens, "shift")
+        w, pw = self._weight(weight, "weight"), self._weight(post_weight, "post_weight")
+        dx = torch.empty_like(r if r is not None else dr)
         dy = None if y is None else torch.empty_like(y)
-        dgate, dscale, dshift = empty(gate, rows), None if dn is None else empty(scale, rows), None if dn is None else empty(shift, rows)
-        dweight, dpost = None if dn is None else empty(weight, (self._width,)), empty(post_weight, (self._width,))
+        normed = dn is not None
+        dgate, dscale, dshift = self._fp32(gate), self._fp32(scale) if normed else None, self._fp32(shift) if normed else None
+        dweight, dpost = self._fp32(weight) if normed else None, self._fp32(post_weight)
         ws = self._scratch(self.workspace_bytes(tokens), workspace)
-        self._run(self._lib.arl2_modulate_backward, self._cfg, tokens, _ptr(r), _ptr(dn), _ptr(dr), _ptr(y), self._modulation(gate, tokens, "gate"),
-                  self._modulation(scale, tokens, "scale"), self._weight(weight, "weight"), self._weight(post_weight, "post_weight"),
+        self._run(self._lib.arl2_modulate_backward, self._cfg, tokens, _ptr(r), _ptr(dn), _ptr(dr), _ptr(y), gate_rows, scale_rows, w, pw,
                   dx.data_ptr(), _ptr(dy), _ptr(dgate), _ptr(dscale), _ptr(dshift), _ptr(dweight), _ptr(dpost), ws.data_ptr(), ws.numel())
         return dx, dy, dgate, dscale, dshift, dweight, dpost
 
@@ -821,10 +839,7 @@ class Rotation(_BlockOp):
         self.workspace_bytes(1)
 
     def workspace_bytes(self, tokens):
-        n = self._lib.arl2_rotation_workspace_bytes(ctypes.byref(self.layer.cfg), self._cfg, tokens)
-        if n == 0:
-            raise Arl2Error("arl2_rotation_workspace_bytes: " + self._lib.arl2_last_error().decode())
-        return n
+        return self._bytes(self._lib.arl2_rotation_workspace_bytes, tokens)
 
     def _where(self, start, positions, tokens):
         if start is not None:
@@ -847,13 +862,13 @@ class Rotation(_BlockOp):
         q_rows = self._strided(q, q_shape, self.dtype, "q", 2)
         k_rows = None if k is None else self._strided(k, k_shape, self.dtype, "k", 2)
         if q_out is None:
-            q_out = torch.empty(q_shape, dtype=self.dtype, device=self.device)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             self.layer._want(q_out, q_shape, self.dtype, "q_out")
         if k_out is not None:
             self.layer._want(k_out, k_shape, self.dtype, "k_out")
         elif k is not None:
-            k_out = torch.empty(k_shape, dtype=self.dtype, device=self.device)
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         self._run(self._lib.arl2_rotate, self._cfg, *self._tables, tokens, q_rows, k_rows, *self._where(start, positions, tokens),
                   self._weight(q_weight, self._H, "q_weight"), self._weight(k_weight, self.kv_heads, "k_weight"), q_out.data_ptr(), _ptr(k_out))
         return q_out, k_out
@@ -892,10 +907,7 @@ class Recurrence(_BlockOp):
         self.workspace_bytes(1)
 
     def workspace_bytes(self, tokens, backward=False):
-        n = self._lib.arl2_recurrence_workspace_bytes(ctypes.byref(self.layer.cfg), self._cfg, tokens, backward)
-        if n == 0:
-            raise Arl2Error("arl2_recurrence_workspace_bytes: " + self._lib.arl2_last_error().decode())
-        return n
+        return self._bytes(self._lib.arl2_recurrence_workspace_bytes, tokens, int(backward))
 
     def _inputs(self, q, k, v, decay_logits, state):
         tokens = self._tokens(q, "q", 4)
@@ -914,10 +926,12 @@ class Recurrence(_BlockOp):
         (zeros) -> (out [B, T, H, D], the state behind the last block, or None with ``final=False``)."""
         tokens, shape, rows = self._inputs(q, k, v, decay_logits, state)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             self.layer._want(out, shape, self.dtype, "out")
-        last = torch.empty(self._B, self._H, self._D, self._D, dtype=torch.float32, device=self.device) if final else None
+        last = None
+        if final:
+            last = torch.empty((self._B, self._H, self._D, self._D), dtype=torch.float32, device=self.device) if state is None else torch.empty_like(state)
         ws = self._scratch(self.workspace_bytes(tokens), workspace)
         self._run(self._lib.arl2_recur, self._cfg, tokens, *rows, decay_logits.data_ptr(), _ptr(state), out.data_ptr(), _ptr(last), ws.data_ptr(), ws.numel())
         return out, last

@@ -1402,6 +1402,7 @@ int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
     ((p).vecs == 1 ? ((full) ? call(1, true) : call(1, false)) : (p).vecs == 2 ? ((full) ? call(2, true) : call(2, false)) \
      : (p).vecs == 3 ? ((full) ? call(3, true) : call(3, false)) : ((full) ? call(4, true) : call(4, false)))
 #define ARL2_UP_TO_2(p, full, call) ((p).vecs == 1 ? ((full) ? call(1, true) : call(1, false)) : ((full) ? call(2, true) : call(2, false)))
+#define ARL2_UP_TO_3(p, full, call) ((p).vecs == 3 ? ((full) ? call(3, true) : call(3, false)) : ARL2_UP_TO_2(p, full, call))
 
 int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st)
 {
@@ -1438,7 +1439,7 @@ int rotate_backward(const RotateBackArgs& a, int dtype, cudaStream_t st)
     const RowPlan p = team_shape(d, kRotateBackVecs);
     const bool full = is_full(p, a.r.q_width) && (a.r.k_width == 0 || a.r.k_width == a.r.q_width);
 #define ARL2_CALL(v, f) (dtype == ARL2_FP32 ? launch_rotate_backward<float, v, f>(a, p, st) : launch_rotate_backward<__nv_bfloat16, v, f>(a, p, st))
-    return ARL2_UP_TO_2(p, full, ARL2_CALL);
+    return ARL2_UP_TO_3(p, full, ARL2_CALL);
 #undef ARL2_CALL
 }
 

@@ -222,3 +222,11 @@ def test_wrong_tensors_are_refused():
             pytest.fail(f"call {i} was not refused")
     r.forward(q, k)
     r.layer.sync_status()
+
+
+@pytest.mark.parametrize("H,kv,norm", [(64, 8, "token"), (64, 1, "head"), (3, 40, "token"), (40, 3, "head"), (1, 64, None)])
+def test_queries_and_keys_of_very_different_widths(H, kv, norm):
+    """A thread's share of a row goes by the wider of the two."""
+    case = (1, 333, H, kv, 128, torch.bfloat16, norm, (22, 21, 21), (7, 9))
+    test_forward(case, False)
+    test_backward(case)
