@@ -368,23 +368,28 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
     const float* slots = a.slots + (size_t)in_pair * D * D + e;
     using Value = ScanValue<kEach>;
     grid_dependency_sync();
-    // the sums of blocks n, n + way, ..: all their first parts before any other
+    // the sums of blocks n, n + way, ..: a part of each at a time
     auto fetch = [&](Value (&sum)[kScanAhead], int i0, int way, int count) {
+        int most = 0;
 #pragma unroll
         for (int i = 0; i < kScanAhead; ++i) {
 #pragma unroll
             for (int k = 0; k < kEach; ++k) sum[i].v[k] = 0.0f;
-            if (i < count && blocks[i0 + i * way].count > 0) sum[i].load(slots + (size_t)blocks[i0 + i * way].first * size);
+            if (i < count) most = max(most, blocks[i0 + i * way].count);
         }
+        for (int c = 0; c < most; ++c) {
+            Value o[kScanAhead];
 #pragma unroll
-        for (int i = 0; i < kScanAhead; ++i)
-            if (i < count)
-                for (int c = 1; c < blocks[i0 + i * way].count; ++c) {
-                    Value o;
-                    o.load(slots + (size_t)(blocks[i0 + i * way].first + c) * size);
+            for (int i = 0; i < kScanAhead; ++i) {
 #pragma unroll
-                    for (int k = 0; k < kEach; ++k) sum[i].v[k] += o.v[k];
-                }
+                for (int k = 0; k < kEach; ++k) o[i].v[k] = 0.0f;
+                if (i < count && c < blocks[i0 + i * way].count) o[i].load(slots + (size_t)(blocks[i0 + i * way].first + c) * size);
+            }
+#pragma unroll
+            for (int i = 0; i < kScanAhead; ++i)
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) sum[i].v[k] += o[i].v[k];
+        }
     };
     Value s;
 #pragma unroll
