@@ -1711,7 +1711,10 @@ RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c
     const size_t state = align_up(units * pair * dd * sizeof(float));      // (as two bf16 numbers it takes the same room)
     RecurLayout l;
     size_t off = 0;
-    l.slots = off;   off += align_up((units * (back ? 2 : 1) + kRecurCtas) * pair * dd * sizeof(float));
+    // (a slice holds a tile at least, and of each job's slices there are at most as many as CTAs: two jobs, each with its shorter blocks)
+    const size_t block = c.block_tokens < tokens ? c.block_tokens : tokens, tiles = units * (back ? 2 : 1) * ((block + kRecurTile - 1) / kRecurTile);
+    const size_t slices = (size_t)kRecurCtas * (back ? 4 : 2);
+    l.slots = off;   off += align_up((units * (back ? 2 : 1) + (tiles < slices ? tiles : slices)) * pair * dd * sizeof(float));
     l.states = off;  off += state;
     l.dstates = off; off += back ? state : 0;
     l.beside = off;  off += back && tc ? state : 0;

@@ -335,37 +335,75 @@ int rotate_backward(const RotateBackArgs& a, int dtype, cudaStream_t st);
 // ---- the recurrence over the blocks of a sequence (arl2_recur.cu, arl2_tc_recur.cu) ------------
 // Three steps: sums over the tokens of a block (K^T V; backward also Q^T dO), the scan over the blocks, and rows times the
 // states (Q S; backward dO S^T, V D^T, K D).  The first and the last go over tiles of up to 128 tokens of a unit, which is one block of a
-// head (of two heads side by side where D = 64 and tensor cores do it).  Units of equal length are a job; the tiles of all jobs
-// of a step form one sequence, cut into equal runs, one for each CTA.
+// head (of two heads side by side where D = 64 and tensor cores do it).  Units of equal length are a job, whose tiles are cut into equal
+// slices for the CTAs; a CTA has a slice of every job, one after the other (where there are fewer slices than CTAs, the next job
+// begins at the CTA behind).  So in the backward pass all read dO last in the first step and first, from the end, in the last step:
+// what the L2 still holds of it is not read from memory again.
 constexpr int kRecurTile = 128;
 struct RecurJob {
-    int tile0, unit0;        // where this job's tiles and units begin in the step's sequence
-    int ntile, len;          // tiles of a unit, tokens of a unit
+    int units, ntile, len;   // units, tiles of a unit, tokens of a unit
     int n0, n_count;         // blocks n0 .. n0 + n_count - 1 of each head
     int which;               // the pair of operands (sums), or the product (rows times states)
     int part;                // 0: blocks of full length; 1: the shorter last one
+    // set by recur_cut
+    int share, slices;       // tiles of a slice; slices
+    int start;               // CTA of the first slice
+    int slot0;               // sums: the part of unit u that slice i makes is slot slot0 + u + i
 };
 constexpr int kRecurJobs = 6;
 struct RecurStep {
     RecurJob job[kRecurJobs];
-    int jobs, tiles, units;
-    int share, ctas;         // tiles of a CTA, CTAs
+    int jobs, wrap, ctas;    // CTAs that there may be, and that there are
+    bool backwards;          // the tiles of a slice from the last to the first
 };
 struct RecurRows {           // [B, T, H, D] of the I/O type
     const void* p;
     int64_t batch, token;    // strides in elements
 };
-// Where tile g of a step is
-struct RecurAt { int job, unit, tile, b, head, n; };   // unit: within the step; head: the unit's first
-__device__ __forceinline__ RecurAt recur_at(const RecurStep& s, int g, int heads, int pair)
+// The slices of a CTA, and tile k of them.
+struct RecurRun { int from[kRecurJobs], upto[kRecurJobs], slice[kRecurJobs]; int count; };
+struct RecurAt { int job, unit, slot, tile, b, head, n; bool ends; };   // head: the unit's first; unit: unlike the tile's before in another unit; ends: the unit, or the slice
+__device__ __forceinline__ RecurRun recur_run(const RecurStep& s, int cta)
+{
+    RecurRun r;
+    r.count = 0;
+#pragma unroll
+    for (int j = 0; j < kRecurJobs; ++j) {
+        r.from[j] = r.slice[j] = 0;
+        if (j < s.jobs) {
+            const RecurJob& job = s.job[j];
+            int i = cta - job.start;
+            if (i < 0) i += s.wrap;
+            if (i < job.slices) {
+                r.slice[j] = i;
+                r.from[j] = i * job.share;
+                r.count += min(job.share, job.units * job.ntile - i * job.share);
+            }
+        }
+        r.upto[j] = r.count;
+    }
+    return r;
+}
+__device__ __forceinline__ RecurAt recur_at(const RecurStep& s, const RecurRun& run, int k, int heads, int pair)
 {
     RecurAt r;
+    int from = 0, before = 0, n = 0, slice = 0;
     r.job = 0;
-    while (r.job + 1 < s.jobs && g >= s.job[r.job + 1].tile0) ++r.job;
+#pragma unroll
+    for (int j = kRecurJobs - 1; j >= 0; --j)
+        if (k < run.upto[j]) {
+            r.job = j;
+            from = run.from[j];
+            slice = run.slice[j];
+            before = j > 0 ? run.upto[j > 0 ? j - 1 : 0] : 0;
+            n = run.upto[j] - before;
+        }
     const RecurJob& j = s.job[r.job];
-    const int v = (g - j.tile0) / j.ntile;
-    r.tile = g - j.tile0 - v * j.ntile;
-    r.unit = j.unit0 + v;
+    const int at = k - before, g = from + (s.backwards ? n - 1 - at : at), v = g / j.ntile;
+    r.tile = g - v * j.ntile;
+    r.unit = r.job << 28 ^ v;
+    r.slot = j.slot0 + v + slice;
+    r.ends = at + 1 == n || r.tile == (s.backwards ? 0 : j.ntile - 1);
     const int bh = v / j.n_count;
     r.n = j.n0 + v - bh * j.n_count;
     r.b = bh / heads;
@@ -374,9 +412,20 @@ __device__ __forceinline__ RecurAt recur_at(const RecurStep& s, int g, int heads
 }
 inline void recur_cut(RecurStep& s, int ctas)
 {
-    s.share = (s.tiles + ctas - 1) / ctas;
-    if (s.share < 1) s.share = 1;
-    s.ctas = (s.tiles + s.share - 1) / s.share;
+    int start = 0, slot = 0, slices = 0;
+    for (int i = 0; i < s.jobs; ++i) {
+        RecurJob& j = s.job[i];
+        const int tiles = j.units * j.ntile;
+        j.share = (tiles + ctas - 1) / ctas;
+        j.slices = (tiles + j.share - 1) / j.share;
+        j.start = start;
+        j.slot0 = slot;
+        start = (start + j.slices) % ctas;
+        slot += j.units + j.slices;
+        slices += j.slices;
+    }
+    s.wrap = ctas;
+    s.ctas = slices < ctas ? slices : ctas;
 }
 struct RecurArgs {
     int B, H, D, T;
@@ -392,7 +441,7 @@ struct RecurArgs {
     void *out, *dq, *dk, *dv;
     float* ddecay;           // [B, N, H]
     // scratch
-    float* slots;            // [units + CTAs of the sums, pair, D, D]: the part of unit u that CTA c made is at u + c
+    float* slots;            // [units + slices of the sums, pair, D, D]
     float* states;           // [B, H / pair up, N, pair, D, D] fp32: state before block n
     float* dstates;          // ... and the gradient of the state after block n
     __nv_bfloat16* states_op;    // the same as a bf16 head and a bf16 remainder, [.., pair, 2, D, D] (tensor cores)
@@ -425,9 +474,9 @@ int recur(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st);
 bool tc_recur_supported(const RecurArgs& a);
 int tc_recur_sums(RecurArgs& a, cudaStream_t st);
 int tc_recur_rows(RecurArgs& a, cudaStream_t st);
-// fills in the steps' jobs; the launchers cut them into runs, the sums for at most kRecurCtas CTAs
+// fills in the steps' jobs; the launchers cut them into slices, the sums for at most kRecurCtas CTAs
 void recur_plan(RecurArgs& a);
-constexpr int kRecurCtas = 4 * 148;
+constexpr int kRecurCtas = 2 * 148;
 
 void set_error(const char* fmt, ...);
 

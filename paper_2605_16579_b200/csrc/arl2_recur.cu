@@ -74,7 +74,8 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
     float* ys = smem + kSumTokens * kLd;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int m0 = (warp >> 1) * kM * 16, n0 = (warp & 1) * kN * 8;
-    const int first = blockIdx.x * a.sums.share, last = min(first + a.sums.share, a.sums.tiles);
+    const RecurRun run = recur_run(a.sums, blockIdx.x);
+    const int first = 0, last = run.count;
     grid_dependency_sync();
 
     float acc[kM][kN][4];
@@ -84,7 +85,7 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
     const T *x = nullptr, *y = nullptr;
     int64_t x_step = 0, y_step = 0;
     auto enter = [&](int tile) {
-        at = recur_at(a.sums, tile, recur_heads(a), a.pair);
+        at = recur_at(a.sums, run, tile, recur_heads(a), a.pair);
         const RecurJob& j = a.sums.job[at.job];
         tokens = min(kRecurTile, j.len - at.tile * kRecurTile);
         const RecurRows& rx = j.which == 0 ? a.k : a.q;
@@ -168,8 +169,8 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
                 }
             }
         }
-        if (tile + 1 == last || at.unit != here.unit) {   // the unit's last tile, or this CTA's
-            float* to = a.slots + (size_t)(here.unit + blockIdx.x) * D * D;
+        if (here.ends) {
+            float* to = a.slots + (size_t)here.slot * D * D;
 #pragma unroll
             for (int i = 0; i < kM; ++i)
 #pragma unroll
@@ -198,7 +199,8 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
     float* xs = smem + D * (D + 8);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int m0 = (warp >> 1) * 16, n0 = (warp & 1) * kN * 8;
-    const int first = blockIdx.x * a.rows.share, last = min(first + a.rows.share, a.rows.tiles);
+    const RecurRun run = recur_run(a.rows, blockIdx.x);
+    const int first = 0, last = run.count;
     grid_dependency_sync();
     recur_gates(a, blockIdx.x * (kRThreads / 32) + warp, gridDim.x * (kRThreads / 32));
     if (first >= last) return;
@@ -209,7 +211,7 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
     const T* x = nullptr;
     int64_t x_step = 0;
     auto enter = [&](int tile) {
-        at = recur_at(a.rows, tile, recur_heads(a), a.pair);
+        at = recur_at(a.rows, run, tile, recur_heads(a), a.pair);
         const RecurJob& j = a.rows.job[at.job];
         tokens = min(kRecurTile, j.len - at.tile * kRecurTile);
         const RecurRows& r = !a.back ? a.q : j.which == 0 ? a.dout : j.which == 1 ? a.v : a.k;
@@ -350,9 +352,9 @@ __device__ __forceinline__ ScanBlock scan_block(const RecurArgs& a, int which, i
     for (int i = 0; i < a.sums.jobs; ++i) {
         const RecurJob& j = a.sums.job[i];
         if (j.which != which || n < j.n0 || n >= j.n0 + j.n_count) continue;
-        const int v = (b * recur_heads(a) + head / a.pair) * j.n_count + n - j.n0, tile = j.tile0 + v * j.ntile;
-        const int c0 = tile / a.sums.share, c1 = (tile + j.ntile - 1) / a.sums.share;
-        r.first = j.unit0 + v + c0;
+        const int v = (b * recur_heads(a) + head / a.pair) * j.n_count + n - j.n0;
+        const int c0 = v * j.ntile / j.share, c1 = (v * j.ntile + j.ntile - 1) / j.share;
+        r.first = j.slot0 + v + c0;
         r.count = c1 - c0 + 1;
     }
     return r;
@@ -497,7 +499,7 @@ int run_plain(RecurArgs& a, cudaStream_t st)
     recur_cut(a.sums, std::min(c0, kRecurCtas));
     recur_cut(a.rows, c1);
     int n = 0, r;
-    if (a.sums.tiles > 0) {
+    if (a.sums.jobs > 0) {
         r = check_launch(launch_kernel(sums, dim3((unsigned)a.sums.ctas), kRThreads, sum_smem<D>(), st, a), "recur_sums_kernel");
         if (r < 0) return r;
         n += r;
@@ -548,13 +550,11 @@ void recur_plan(RecurArgs& a)
             j.ntile = (j.len + kRecurTile - 1) / kRecurTile;
             j.n0 = lo;
             j.n_count = hi - lo;
-            j.tile0 = s.tiles;
-            j.unit0 = s.units;
-            s.units += heads * j.n_count;
-            s.tiles += heads * j.n_count * j.ntile;
+            j.units = heads * j.n_count;
         }
     };
     a.sums = a.rows = RecurStep{};
+    a.rows.backwards = a.back;
     // the last block's K^T V is for the state behind it alone, the first block's Q^T dO for the gradient of the state before it
     add(a.sums, 0, 0, a.back || a.state_out == nullptr ? a.N - 1 : a.N);
     if (a.back) add(a.sums, 1, a.dstate_in == nullptr ? 1 : 0, a.N);

@@ -1,13 +1,13 @@
 // The recurrence over the blocks of a sequence on tensor cores (bf16 I/O): sums over tokens, X^T Y, and rows times states,
 // X M or X M^T (arl2_recur.cu has the mathematics and the scan between the two).
 //
-// Both go over 128-token tiles of units, a unit being a block of one head, or of two heads of 64 channels side by side; the
-// tiles of all units are one sequence, cut into equal runs, one CTA (one per SM) per run.  Tiles come by TMA; the tensors are
+// Both go over 128-token tiles of units, a unit being a block of one head, or of two heads of 64 channels side by side; one CTA per
+// SM has a slice of each job's tiles.  Tiles come by TMA; the tensors are
 // seen as (channel, head, token in block, block, stream), so that what lies past a block's end reads as zeros.  Memory bounds
 // them: 64 flops per byte where the tensor cores do 250, so a ring of stages kept full is all that counts.
 //
 // tc_recur_sums_kernel:  warp 0 TMA producer, warp 1 MMA issuer, warps 2-9 add up the accumulators (two in TMEM, by turns) in
-//   registers and store a unit's to the slot of (unit, CTA).  The products of bf16 are exact, but the tensor cores cut what does not fit
+//   registers and store a unit's to the slot of (unit, slice).  The products of bf16 are exact, but the tensor cores cut what does not fit
 //   when they add: 3e-6 too small at the end of 4680 tokens.  So an accumulator takes kFlush tiles, and these sums are added by
 //   rounding additions (40 heads x 14040 tokens: the state 3.1e-6 off -> 2.4e-7).  Of two heads side by side the 128 x 128 product
 //   has two blocks that nobody wants: tensor time that there is plenty of.
@@ -71,7 +71,8 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kSOffBars + kSNumBars * 8 + 4);
     const Abort ab{abort_flag, a.status, a.wait_limit ? a.wait_limit - 1 : kSpinLimit};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int first = (int)blockIdx.x * a.sums.share, count = min(a.sums.share, a.sums.tiles - first);
+    const RecurRun run = recur_run(a.sums, blockIdx.x);
+    const int count = run.count;
     const int heads = recur_heads(a);
 
     if (tid == 0) {
@@ -103,7 +104,7 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
             bool ok = true;
             int issued = 0;
             for (int k = 0; k < count && ok; ++k) {
-                const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
+                const RecurAt at = recur_at(a.sums, run, k, heads, a.pair);
                 const RecurJob& j = a.sums.job[at.job];
                 const int s = k % kSStages;
                 if (k >= kSStages) ok = wait_bar(bars + 8 * (kSBarFree0 + s), (uint32_t)((k / kSStages) - 1) & 1u, ab, 200);
@@ -127,7 +128,7 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         bool ok = true;
         int turn = 0, in_turn = 0;      // accumulators so far, tiles of this one
         for (int k = 0; k < count && ok; ++k) {
-            const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
+            const RecurAt at = recur_at(a.sums, run, k, heads, a.pair);
             const RecurJob& j = a.sums.job[at.job];
             const bool fresh = in_turn == 0;
             if (fresh && turn >= 2) ok = wait_bar_warp(ubars + 8 * (kSBarAccFree0 + (turn & 1)), (uint32_t)((turn >> 1) - 1) & 1u, ab, 201);
@@ -141,7 +142,7 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
             for (int ks = 0; ks < steps; ++ks)
                 mma_ss_if(lead, acc, desc64(x_lo + (uint32_t)(ks * (2048 >> 4)), desc_hi), desc64(y_lo + (uint32_t)(ks * (2048 >> 4)), desc_hi), idesc, (!fresh || ks > 0) ? 1u : 0u);
             mma_commit_if(lead, ubars + 8 * (kSBarFree0 + s));
-            if (++in_turn == kFlush || at.tile + 1 == j.ntile || k + 1 == count) {
+            if (++in_turn == kFlush || at.ends) {
                 mma_commit_if(lead, ubars + 8 * (kSBarAccFull0 + (turn & 1)));
                 ++turn;
                 in_turn = 0;
@@ -159,8 +160,8 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         int turn = 0, in_turn = 0;
         bool fresh = true;
         for (int k = 0; k < count; ++k) {
-            const RecurAt at = recur_at(a.sums, first + k, heads, a.pair);
-            const bool last = at.tile + 1 == a.sums.job[at.job].ntile || k + 1 == count;
+            const RecurAt at = recur_at(a.sums, run, k, heads, a.pair);
+            const bool last = at.ends;
             if (++in_turn != kFlush && !last) continue;
             in_turn = 0;
             if (!wait_bar_warp(bars + 8 * (kSBarAccFull0 + (turn & 1)), (uint32_t)(turn >> 1) & 1u, ab, 203)) break;
@@ -178,7 +179,7 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
             if (!last) continue;
             fresh = true;
             // row-major [D][D], of two heads one after the other
-            float* to = a.slots + (size_t)(at.unit + blockIdx.x) * (D * kTile) + row * D + half * kCols;
+            float* to = a.slots + (size_t)at.slot * (D * kTile) + row * D + half * kCols;
 #pragma unroll
             for (int c = 0; c < kCols; c += 8) {
                 uint32_t w[8];
@@ -208,7 +209,8 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kROffBars + kRNumBars * 8 + 4);
     const Abort ab{abort_flag, a.status, a.wait_limit ? a.wait_limit - 1 : kSpinLimit};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int first = (int)blockIdx.x * a.rows.share, count = min(a.rows.share, a.rows.tiles - first);
+    const RecurRun run = recur_run(a.rows, blockIdx.x);
+    const int count = run.count;
     const int heads = recur_heads(a);
     constexpr int kMatPart = D == 128 ? kTileBytes : 64 * 64 * 2;          // bytes of a head or a remainder
     constexpr int kParts = D == 128 ? 2 : 4;                               // ... of a unit's state
@@ -245,7 +247,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
             bool ok = true;
             int issued = 0, mats = 0, unit = -1;
             for (int k = 0; k < count && ok; ++k) {
-                const RecurAt at = recur_at(a.rows, first + k, heads, a.pair);
+                const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
                 const RecurJob& j = a.rows.job[at.job];
                 if (at.unit != unit) {
                     unit = at.unit;
@@ -282,7 +284,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         bool ok = true;
         int mats = 0, unit = -1;
         for (int k = 0; k < count && ok; ++k) {
-            const RecurAt at = recur_at(a.rows, first + k, heads, a.pair);
+            const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
             const RecurJob& j = a.rows.job[at.job];
             const int s = k % kRStages;
             if (at.unit != unit) {
@@ -321,7 +323,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
             }
             mma_commit_if(lead, ubars + 8 * (kRBarFree0 + s));
             mma_commit_if(lead, ubars + 8 * (kRBarAccFull0 + (k & 1)));
-            if (at.tile + 1 == j.ntile) mma_commit_if(lead, ubars + 8 * (kRBarMatFree0 + ((mats - 1) & 1)));
+            if (at.ends) mma_commit_if(lead, ubars + 8 * (kRBarMatFree0 + ((mats - 1) & 1)));
         }
         mma_commit_if(lead, ubars + 8 * kRBarDrain);
         drain_bar(ubars + 8 * kRBarDrain, 0);
@@ -330,7 +332,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
         for (int k = 0; k < count; ++k) {
-            const RecurAt at = recur_at(a.rows, first + k, heads, a.pair);
+            const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
             const RecurJob& j = a.rows.job[at.job];
             __nv_bfloat16* to = static_cast<__nv_bfloat16*>(!a.back ? a.out : j.which == 0 ? a.dq : j.which == 1 ? a.dk : a.dv);
             const int head = D == 128 ? at.head : at.head + half;
@@ -440,7 +442,7 @@ bool tc_recur_supported(const RecurArgs& a)
 
 int tc_recur_sums(RecurArgs& a, cudaStream_t st)
 {
-    if (a.sums.tiles == 0) return 0;
+    if (a.sums.jobs == 0) return 0;
     int sms = 0;
     if (int r = recur_sms(&sms)) return r;
     recur_cut(a.sums, sms < kRecurCtas ? sms : kRecurCtas);
