@@ -43,14 +43,18 @@ static_assert(kSNumBars * 8 + 16 <= 256 && kRNumBars * 8 + 16 <= 256, "barrier b
 // rows of a TMA box for blocks of `len` tokens
 __host__ __device__ constexpr int box_rows(int len) { return len >= kTile ? kTile : (len + 15) / 16 * 16; }
 
+// Forward every tensor passes through once, and makes room in the L2 for the states (40 heads x 14040 tokens 121.3 -> 119.1 us); backward the
+// last step reads K, V and dO again, and finds some of them (let go of first, or Q or the outputs alone: 196 -> 198 to 206 us).
+__device__ __forceinline__ uint64_t tile_policy(const RecurArgs& a) { return a.back ? policy_evict_normal() : policy_evict_first(); }
+
 // a tile: two boxes of 64 columns, of one head or of two
 template <int D>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, const RecurAt& at, const RecurJob& j, int b)
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, const RecurAt& at, const RecurJob& j, int b, uint64_t policy)
 {
     const int n = j.part == 0 ? at.n : 0, row = at.tile * kTile;
-    tma_load_5d(dst, map, bar, 0, at.head, row, n, b);
-    if (D == 128) tma_load_5d(dst + kHalfBytes, map, bar, 64, at.head, row, n, b);
-    else tma_load_5d(dst + kHalfBytes, map, bar, 0, at.head + 1, row, n, b);
+    tma_load_5d(dst, map, bar, 0, at.head, row, n, b, policy);
+    if (D == 128) tma_load_5d(dst + kHalfBytes, map, bar, 64, at.head, row, n, b, policy);
+    else tma_load_5d(dst + kHalfBytes, map, bar, 0, at.head + 1, row, n, b, policy);
 }
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi)
@@ -101,6 +105,7 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
 
     if (warp == 0) {
         if (lane == 0) {
+            const uint64_t policy = tile_policy(a);
             bool ok = true;
             int issued = 0;
             for (int k = 0; k < count && ok; ++k) {
@@ -113,8 +118,8 @@ tc_recur_sums_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
                 mbar_expect_tx(bar, (uint32_t)box_rows(j.len) * 512u);
                 const RecurRows& x = j.which == 0 ? a.k : a.q;
                 const RecurRows& y = j.which == 0 ? a.v : a.dout;
-                load_tile<D>(dst, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b);
-                load_tile<D>(dst + kTileBytes, &maps_y.m[j.part][j.which], bar, at, j, y.batch == 0 ? 0 : at.b);
+                load_tile<D>(dst, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b, policy);
+                load_tile<D>(dst + kTileBytes, &maps_y.m[j.part][j.which], bar, at, j, y.batch == 0 ? 0 : at.b, policy);
                 ++issued;
             }
             for (int m = (issued > kSStages ? issued - kSStages : 0); m < issued; ++m) drain_bar(bars + 8 * (kSBarFull0 + m % kSStages), (uint32_t)(m / kSStages) & 1u);
@@ -243,6 +248,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
 
     if (warp == 0) {
         if (lane == 0) {
+            const uint64_t policy = tile_policy(a);
             fence_proxy_async_global();      // the states come from the scan's stores
             bool ok = true;
             int issued = 0, mats = 0, unit = -1;
@@ -270,7 +276,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
                 const uint32_t bar = bars + 8 * (kRBarFull0 + s);
                 mbar_expect_tx(bar, (uint32_t)box_rows(j.len) * 256u);
                 const RecurRows& x = !a.back ? a.q : j.which == 0 ? a.dout : j.which == 1 ? a.v : a.k;
-                load_tile<D>(smem_base + kROffStage + s * kTileBytes, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b);
+                load_tile<D>(smem_base + kROffStage + s * kTileBytes, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b, policy);
                 ++issued;
             }
             for (int m = (issued > kRStages ? issued - kRStages : 0); m < issued; ++m) drain_bar(bars + 8 * (kRBarFull0 + m % kRStages), (uint32_t)(m / kRStages) & 1u);
@@ -331,6 +337,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         recur_gates(a, blockIdx.x * 8 + warp - 2, gridDim.x * 8);      // (while the first tiles are on their way)
         const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint64_t policy = tile_policy(a);
         for (int k = 0; k < count; ++k) {
             const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
             const RecurJob& j = a.rows.job[at.job];
@@ -354,7 +361,9 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
 #pragma unroll
                     for (int i = 0; i < 8; ++i) w[i] = pack_bf16(__uint_as_float(x[c * 16 + 2 * i]), __uint_as_float(x[c * 16 + 2 * i + 1]));
                     if (wide) {
-                        store_row32(p + c * 16, w);
+                        asm volatile("st.global.L2::cache_hint.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;" ::"l"(p + c * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                                     "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(policy)
+                                     : "memory");
                     } else {
                         *reinterpret_cast<uint4*>(p + c * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                         *reinterpret_cast<uint4*>(p + c * 16 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
