@@ -7,7 +7,9 @@
 //
 // This file has the scan, and sums and rows for fp32 I/O (and bf16 without tensor memory): warp-level matrix instructions on
 // TF32 numbers.  A fp32 operand is taken as a head of 11 bits and a remainder of 11 more, three products (remainder times remainder
-// left out): off by 2^-22 of each product; bf16 inputs are exact in the head alone.  fp32 accumulation.
+// left out): off by 2^-22 of each product; bf16 inputs are exact in the head alone.  The tensor cores cut what does not fit when they
+// add, always to the same side, so a sum stays with them for 32 terms only and is then added to the others by a rounding addition
+// (6 heads of 128 fp32, 3 x 2800 tokens: 1.5e-6 off without that, 3.4e-7 with it).
 #include <algorithm>
 #include <atomic>
 
@@ -78,7 +80,7 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
     const int first = 0, last = run.count;
     grid_dependency_sync();
 
-    float acc[kM][kN][4];
+    float sum[kM][kN][4];
     float4 xr[kLoads], yr[kLoads];
     RecurAt at;
     int tokens = 0;            // of the tile
@@ -118,7 +120,7 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
 #pragma unroll
                 for (int j = 0; j < kN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+                    for (int e = 0; e < 4; ++e) sum[i][j][e] = 0.0f;
             fresh = false;
         }
         const RecurAt here = at;
@@ -138,6 +140,13 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
                 enter(tile + 1);
                 fetch(0);
             }
+            float acc[kM][kN][4];
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
 #pragma unroll
             for (int k = 0; k < kSumTokens; k += 8) {
                 uint32_t ah[kM][4], al[kM][4];
@@ -168,6 +177,12 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
                     }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[i][j][e] += acc[i][j][e];
         }
         if (here.ends) {
             float* to = a.slots + (size_t)here.slot * D * D;
@@ -177,7 +192,7 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
                 for (int j = 0; j < kN; ++j)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        *reinterpret_cast<float2*>(to + (m0 + i * 16 + g + e * 8) * D + n0 + j * 8 + 2 * t) = make_float2(acc[i][j][2 * e], acc[i][j][2 * e + 1]);
+                        *reinterpret_cast<float2*>(to + (m0 + i * 16 + g + e * 8) * D + n0 + j * 8 + 2 * t) = make_float2(sum[i][j][2 * e], sum[i][j][2 * e + 1]);
             fresh = true;
         }
     }
@@ -254,13 +269,19 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
                 enter(tile + 1);
                 fetch(0);
             }
-            float acc[kN][4];
+            float sum[kN][4], acc[kN][4], low[kN][4];       // low: the products with a remainder, 2^-11 of the others
 #pragma unroll
             for (int j = 0; j < kN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
-#pragma unroll 2
+                for (int e = 0; e < 4; ++e) sum[j][e] = low[j][e] = 0.0f;
+#pragma unroll 4
             for (int k = 0; k < D; k += 8) {
+                if (k % 32 == 0) {
+#pragma unroll
+                    for (int j = 0; j < kN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
+                }
                 uint32_t ah[4], al[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -278,11 +299,21 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
                         bh[e] = v.h;
                         bl[e] = v.l;
                     }
-                    if (!kExact) tf32_mma(acc[j], al, bh);
-                    tf32_mma(acc[j], ah, bl);
+                    if (!kExact) tf32_mma(low[j], al, bh);
+                    tf32_mma(low[j], ah, bl);
                     tf32_mma(acc[j], ah, bh);
                 }
+                if (k % 32 == 24) {
+#pragma unroll
+                    for (int j = 0; j < kN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[j][e] += acc[j][e];
+                }
             }
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] = sum[j][e] + low[j][e];
             T* to = static_cast<T*>(!a.back ? a.out : which == 0 ? a.dq : which == 1 ? a.dk : a.dv);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -471,8 +502,8 @@ int set_up(std::atomic<int>& resident, K kernel, int smem, const char* what)
     return ctas;
 }
 
-// Elements of a thread: one where with four there would be CTAs for fewer than half of 148 SMs (us of a backward scan over 21 blocks of
-// 2 x 5 heads of 64 channels, 40 CTAs with four: @S1@; over 7 blocks of 12 heads of 128, 192 CTAs: 23 with four, 37 with one).
+// Elements of a thread: one where with four there would be CTAs for fewer than half of 148 SMs (us of a scan over 16 blocks
+// of 2 x 2 heads of 64 channels, 16 CTAs with four: 17 with four, 7 with one; a backward one over 7 blocks of 12 heads of 128, 192 CTAs: 23 and 37).
 int scan_each(const RecurArgs& a) { return (long long)a.B * a.H * a.D * a.D / (4 * kScanThreads) < 148 / 2 ? 1 : 4; }
 
 template <int D>
