@@ -23,7 +23,7 @@ constexpr int kMaxDev = 64;
 // Threads of a CTA at most, with that many vectors a lane: rows of 8192 channels
 __host__ __device__ constexpr int row_threads(int vecs) { return vecs >= 4 ? 256 : vecs == 3 ? 352 : 512; }
 
-constexpr int kRowStatic = 5 * 1024;       // shared memory of a CTA besides, at most
+constexpr int kRowStatic = 14 * 1024;       // shared memory of a CTA besides, at most
 
 // Rows in flight, and the one in work: as many as there is room for with CTAs of this many threads, four at most.  `pieces` of 16 bytes that
 // a lane has of a row, `beside`: bytes that it has besides.
@@ -845,78 +845,101 @@ struct TokenWalk {
     }
 };
 
-// cos and sin of the four pairs that a lane has of each head, pair m on.  Which axes turn them is the lane's own for all rows: most
-// lanes have one, those where an axis ends two (the others ask for the same again, without a branch); a third only where an axis
-// has fewer than three pairs.  A row's angles are asked for while the row before it is in work.
-constexpr int kNoAxis = 3;
+// The angles of a team's rows, cos and then sin of all pairs of a head, in three places by turns: the warps of the team take
+// turns at finding those of the row after the next, each lane a pair or two, and leave them in shared memory when their own part of the row
+// in work is done.  Between that and the row's use lies a barrier of the team.  (Found by every lane for its own pairs: 40 heads'
+// queries and keys of 4680 tokens 40 us, now 36.)
+constexpr int kAngleRows = 3;
+constexpr int kAngleFloats = 8 * kAngleRows * 128;       // of a CTA: eight teams of one warp, or fewer
 struct Angles {
-    int m, axis, other, split;    // pairs below `split` go by `axis`, the others by `other`
-    bool many, none0, none1;      // ... unless an axis begins and ends within the four: then by axis_of; pairs that do not turn
-    int b, start;                 // the stream, and its first position
+    float* place;            // [kAngleRows][D]
+    TokenWalk ahead;         // the row whose angles are found next
+    int turn, left, warps;   // rows until it is this warp's turn; rows that there are from `ahead` on
+    int put, get;            // places
+    int pair[2], axis[2];    // of this lane
+    float cos[2], sin[2];    // on their way
+    bool due;
     __device__ __forceinline__ static int axis_of(const RotateArgs& a, int pair)
     {
-        return pair < a.pairs[0] ? 0 : pair < a.pairs[0] + a.pairs[1] ? 1 : pair < a.pairs[0] + a.pairs[1] + a.pairs[2] ? 2 : kNoAxis;
+        return pair < a.pairs[0] ? 0 : pair < a.pairs[0] + a.pairs[1] ? 1 : pair < a.pairs[0] + a.pairs[1] + a.pairs[2] ? 2 : 3;
     }
-    __device__ __forceinline__ Angles(const RotateArgs& a, int pair) : m(pair), split(4), many(false), b(-1), start(0)
+    __device__ __forceinline__ Angles(const RotateArgs& a, float* smem, int first, int rows) : ahead(a, first), left(rows), put(0), get(0), due(false)
     {
-        axis = axis_of(a, m);
-        other = axis_of(a, m + 3);
+        warps = blockDim.x >> 5;
+        turn = threadIdx.x >> 5;
+        place = smem + threadIdx.y * kAngleRows * a.D;
 #pragma unroll
-        for (int i = 3; i >= 1; --i) {
-            const int x = axis_of(a, m + i);
-            if (x != axis) split = i;
-            many |= x != axis && x != other;
+        for (int i = 0; i < 2; ++i) {
+            pair[i] = (threadIdx.x & 31) + 32 * i;
+            axis[i] = axis_of(a, pair[i]);
         }
-        many = __any_sync(0xffffffffu, many);
-        none0 = axis == kNoAxis;
-        none1 = other == kNoAxis;
     }
-    // Row of the tables for a position: the first for those before it, the last for those behind.
-    __device__ __forceinline__ static long long table_at(const RotateArgs& a, int at, int m) { return (long long)max(0, min(at, a.rope_rows - 1)) * (a.D / 2) + m; }
-    __device__ __forceinline__ void load(const RotateArgs& a, const TokenWalk& w, bool reports, float (&cs)[4], float (&sn)[4])
+    // asks for the next row's angles where it is this warp's turn
+    __device__ __forceinline__ void ask(const RotateArgs& a)
     {
-        int at[3];
-        if (a.positions != nullptr) {
-            const int32_t* p = a.positions + ((long long)w.b * a.T + w.t) * 3;
+        due = turn == 0 && left > 0;
+        if (due) {
+            int at[4];
+            if (a.positions != nullptr) {
+                const int32_t* p = a.positions + ((long long)ahead.b * a.T + ahead.t) * 3;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) at[i] = p[i];
-        } else {
-            if (w.b != b) {
-                b = w.b;
-                start = a.start != nullptr ? a.start[b] : 0;
+                for (int i = 0; i < 3; ++i) at[i] = p[i];
+            } else {
+                at[0] = (int)min((long long)(a.start != nullptr ? a.start[ahead.b] : 0) + ahead.frame, 0x7fffffffLL);
+                at[1] = ahead.line;
+                at[2] = ahead.column;
             }
-            at[0] = (int)min((long long)start + w.frame, 0x7fffffffLL);
-            at[1] = w.line;
-            at[2] = w.column;
-        }
-        if (reports) {      // one lane of the team: a position behind the tables
-            bool behind = false;
+            if ((threadIdx.x & 31) == 0) {      // a position behind the tables is reported
+                bool behind = false;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) behind |= a.pairs[i] > 0 && at[i] >= a.rope_rows;
-            if (behind && atomicCAS(a.status + kStatusRange, 0u, (uint32_t)kRangePosition) == 0u) a.status[kStatusRangeWhere] = (uint32_t)w.b;
-        }
-        const long long o = table_at(a, axis == 0 ? at[0] : axis == 1 ? at[1] : at[2], m), q = table_at(a, other == 0 ? at[0] : other == 1 ? at[1] : at[2], m);
-        const float4 c0 = *reinterpret_cast<const float4*>(a.cos + o), s0 = *reinterpret_cast<const float4*>(a.sin + o);
-        const float4 c1 = *reinterpret_cast<const float4*>(a.cos + q), s1 = *reinterpret_cast<const float4*>(a.sin + q);
-        const float c[2][4] = {{c0.x, c0.y, c0.z, c0.w}, {c1.x, c1.y, c1.z, c1.w}}, s[2][4] = {{s0.x, s0.y, s0.z, s0.w}, {s1.x, s1.y, s1.z, s1.w}};
+                for (int i = 0; i < 3; ++i) behind |= a.pairs[i] > 0 && at[i] >= a.rope_rows;
+                if (behind && atomicCAS(a.status + kStatusRange, 0u, (uint32_t)kRangePosition) == 0u) a.status[kStatusRangeWhere] = (uint32_t)ahead.b;
+            }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool first = i < split, none = first ? none0 : none1;
-            cs[i] = none ? 1.0f : first ? c[0][i] : c[1][i];
-            sn[i] = none ? 0.0f : first ? s[0][i] : s[1][i];
-        }
-        if (many) {
-#pragma unroll
-            for (int i = 1; i < 3; ++i) {
-                const int x = axis_of(a, m + i);
-                if (x == axis || x == other) continue;
-                const long long r = table_at(a, x == 0 ? at[0] : x == 1 ? at[1] : at[2], m + i);
-                cs[i] = a.cos[r];
-                sn[i] = a.sin[r];
+            for (int i = 0; i < 2; ++i) {
+                cos[i] = 1.0f;
+                sin[i] = 0.0f;
+                if (axis[i] == 3 || pair[i] >= a.D / 2) continue;      // (pairs that do not turn)
+                // the first row of the tables for positions before them, the last for those behind
+                const int row = axis[i] == 0 ? at[0] : axis[i] == 1 ? at[1] : at[2];
+                const long long o = (long long)max(0, min(row, a.rope_rows - 1)) * (a.D / 2) + pair[i];
+                cos[i] = a.cos[o];
+                sin[i] = a.sin[o];
             }
         }
+        turn = turn == 0 ? warps - 1 : turn - 1;
+        --left;
+        ahead.next(a);
+    }
+    __device__ __forceinline__ void leave(const RotateArgs& a)
+    {
+        if (due) {
+            float* to = place + put * a.D;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (pair[i] < a.D / 2) {
+                    to[pair[i]] = cos[i];
+                    to[a.D / 2 + pair[i]] = sin[i];
+                }
+        }
+        put = put == kAngleRows - 1 ? 0 : put + 1;
+    }
+    // the four pairs from pair m on of the row in work
+    __device__ __forceinline__ void take(const RotateArgs& a, int m, float (&c)[4], float (&s)[4])
+    {
+        const float* from = place + get * a.D + m;
+        const float4 c4 = *reinterpret_cast<const float4*>(from), s4 = *reinterpret_cast<const float4*>(from + a.D / 2);
+        c[0] = c4.x; c[1] = c4.y; c[2] = c4.z; c[3] = c4.w;
+        s[0] = s4.x; s[1] = s4.y; s[2] = s4.z; s[3] = s4.w;
+        get = get == kAngleRows - 1 ? 0 : get + 1;
     }
 };
+template <int N>
+__device__ __forceinline__ void team_barrier(const Team<N>& team)
+{
+    if (team.warps == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + team.id), "r"(team.warps * 32) : "memory");
+}
 
 // The sum over the lanes that hold a head, `lanes` of them side by side.
 __device__ __forceinline__ float head_sum(float v, int lanes)
@@ -933,14 +956,7 @@ __device__ __forceinline__ void rotate_weight(const RotateArgs& a, const RotateS
     for (int e = 0; e < 4; ++e) w[e] = both(1.0f);
     if (has && s.weight != nullptr) load_kept(s.weight + (a.norm == kNormHead ? c % a.D : c), w);
 }
-__device__ __forceinline__ f2 swapped(f2 v)
-{
-    float lo, hi;
-    apart(v, lo, hi);
-    return pair(hi, lo);
-}
-
-// y = R(w x / length).  Two units of memory.  A pair (p, q) turned: (p, q) (c, c) + (q, p) (-s, s).
+// y = R(w x / length).  Two units of memory.
 template <typename T, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid_constant__ RotateArgs a)
 {
@@ -960,9 +976,15 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) rotate_weight(a, side, ch.at(i), ch.has(i), w[i]);
     TokenWalk walk(a, side.first);
-    Angles angles(a, (threadIdx.x % lanes) * 4);
-    float next_cs[4], next_sn[4];
-    angles.load(a, walk, threadIdx.x == 0, next_cs, next_sn);
+    __shared__ __align__(16) float angle_places[kAngleFloats];
+    Angles angles(a, angle_places, side.first, side.rows);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        angles.ask(a);
+        angles.leave(a);
+    }
+    team_barrier(team);
+    const int pair0 = (threadIdx.x & (lanes - 1)) * 4;      // (D is 64 or 128)
     const T* x_in = static_cast<const T*>(side.x) + walk.b * side.batch + walk.t * side.token + ch.c0;
     T* out = static_cast<T*>(side.keys ? a.k_out : a.q_out) + (long long)side.first * side.width + ch.c0;
     const int64_t wrap = side.batch - (a.T - 1) * side.token;       // from a stream's last row to the next one's first
@@ -984,13 +1006,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
         f2 x[kVecs][4];
         float cs[4], sn[4];
         if (!kFull) clear(x);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            cs[m] = next_cs[m];
-            sn[m] = next_sn[m];
-        }
-        walk.next(a);
-        if (row + 1 < side.rows) angles.load(a, walk, threadIdx.x == 0, next_cs, next_sn);
+        angles.take(a, pair0, cs, sn);
+        angles.ask(a);
         send();
         ring.landed();
 #pragma unroll
@@ -1040,12 +1057,18 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
             if (!ch.has(i)) continue;
             f2 o[4];
 #pragma unroll
-            for (int m = 0; m < 4; ++m) o[m] = fma2(x[i][m], both(cs[m]), mul2(swapped(x[i][m]), pair(-sn[m], sn[m])));
+            for (int m = 0; m < 4; ++m) {
+                float p, q;
+                apart(x[i][m], p, q);
+                o[m] = pair(p * cs[m] - q * sn[m], p * sn[m] + q * cs[m]);
+            }
             Eight<T> e8;
             e8.set(o);
             e8.store(out + i * ch.step());
         }
         out += side.width;
+        angles.leave(a);
+        if (a.norm != kNormToken || team.warps == 1) team_barrier(team);      // (else the next row's exchange is one)
     }
 }
 
@@ -1072,9 +1095,15 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) rotate_weight(a.r, side, ch.at(i), ch.has(i), w[i]);
     TokenWalk walk(a.r, side.first);
-    Angles angles(a.r, (threadIdx.x % lanes) * 4);
-    float next_cs[4], next_sn[4];
-    angles.load(a.r, walk, threadIdx.x == 0, next_cs, next_sn);
+    __shared__ __align__(16) float angle_places[kAngleFloats];
+    Angles angles(a.r, angle_places, side.first, side.rows);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        angles.ask(a.r);
+        angles.leave(a.r);
+    }
+    team_barrier(team);
+    const int pair0 = (threadIdx.x & (lanes - 1)) * 4;      // (D is 64 or 128)
     const long long at0 = (long long)side.first * side.width + ch.c0;
     const T* g_in = static_cast<const T*>(side.keys ? a.dk_out : a.dq_out) + at0;
     T* out = static_cast<T*>(side.keys ? a.dk : a.dq) + at0;
@@ -1104,13 +1133,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
             clear(x);
             clear(g);
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            cs[m] = next_cs[m];
-            sn[m] = next_sn[m];
-        }
-        walk.next(a.r);
-        if (row + 1 < side.rows) angles.load(a.r, walk, threadIdx.x == 0, next_cs, next_sn);
+        angles.take(a.r, pair0, cs, sn);
+        angles.ask(a.r);
         send();
         ring.landed();
 #pragma unroll
@@ -1122,9 +1146,12 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
         ring.done();
 #pragma unroll
         for (int m = 0; m < 4; ++m) {   // turned back
-            const f2 c = both(cs[m]), s = pair(sn[m], -sn[m]);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) g[i][m] = fma2(g[i][m], c, mul2(swapped(g[i][m]), s));
+            for (int i = 0; i < kVecs; ++i) {
+                float p, q;
+                apart(g[i][m], p, q);
+                g[i][m] = pair(p * cs[m] + q * sn[m], q * cs[m] - p * sn[m]);
+            }
         }
         if (normed) {
             f2 ss[kVecs], dot[kVecs];
@@ -1184,6 +1211,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
                 o.store(out + i * ch.step());
             }
         out += side.width;
+        angles.leave(a.r);
+        if (a.r.norm != kNormToken || team.warps == 1) team_barrier(team);      // (else the next row's exchange is one)
     }
     if (a.parts == nullptr) return;
     float* part = a.parts + (side.keys ? (long long)a.q_parts * a.q_each : 0);
