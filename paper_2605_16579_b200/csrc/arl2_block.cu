@@ -23,7 +23,8 @@ constexpr int kMaxDev = 64;
 // Threads of a CTA at most, with that many vectors a lane: rows of 8192 channels
 __host__ __device__ constexpr int row_threads(int vecs) { return vecs >= 4 ? 256 : vecs == 3 ? 352 : 512; }
 
-constexpr int kRowStatic = 14 * 1024;       // shared memory of a CTA besides, at most
+constexpr int kRowStatic = 9 * 1024;        // shared memory of a CTA besides, at most, and what of it is angles
+constexpr int kAngleMost = 6 * 1024;
 
 // Rows in flight, and the one in work: as many as there is room for with CTAs of this many threads, four at most.  `pieces` of 16 bytes that
 // a lane has of a row, `beside`: bytes that it has besides.
@@ -850,7 +851,7 @@ struct TokenWalk {
 // in work is done.  Between that and the row's use lies a barrier of the team.  (Found by every lane for its own pairs: 40 heads'
 // queries and keys of 4680 tokens 40 us, now 36.)
 constexpr int kAngleRows = 3;
-constexpr int kAngleFloats = 8 * kAngleRows * 128;       // of a CTA: eight teams of one warp, or fewer
+inline int angle_bytes(int teams, int D) { return teams * kAngleRows * D * (int)sizeof(float); }      // of a CTA, behind its rows
 struct Angles {
     float* place;            // [kAngleRows][D]
     TokenWalk ahead;         // the row whose angles are found next
@@ -976,8 +977,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) rotate_weight(a, side, ch.at(i), ch.has(i), w[i]);
     TokenWalk walk(a, side.first);
-    __shared__ __align__(16) float angle_places[kAngleFloats];
-    Angles angles(a, angle_places, side.first, side.rows);
+    Angles angles(a, reinterpret_cast<float*>(ring_smem + kVecs * kPer * kRowStages * blockDim.x * blockDim.y), side.first, side.rows);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         angles.ask(a);
@@ -1095,8 +1095,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(con
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) rotate_weight(a.r, side, ch.at(i), ch.has(i), w[i]);
     TokenWalk walk(a.r, side.first);
-    __shared__ __align__(16) float angle_places[kAngleFloats];
-    Angles angles(a.r, angle_places, side.first, side.rows);
+    Angles angles(a.r, reinterpret_cast<float*>(ring_smem + kVecs * kPer * kRowStages * blockDim.x * blockDim.y), side.first, side.rows);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         angles.ask(a.r);
@@ -1385,8 +1384,8 @@ int launch_rotate(RotateArgs a, RowPlan q, cudaStream_t st)
     constexpr int kPer = kVecs * kPieces<T>;
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
-    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
-    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic, "rotate");
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0) + angle_bytes(q.teams, a.D);
+    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate");
     if (ctas < 0) return ctas;
     cut_rotation(q, k, a, ctas, 1LL << 40, 1);
     a.q_share = q.share;
@@ -1403,8 +1402,8 @@ int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
     constexpr int kPer = 2 * kVecs * kPieces<T>;
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
-    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
-    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic, "rotate_backward");
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0) + angle_bytes(q.teams, a.r.D);
+    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate_backward");
     if (ctas < 0) return ctas;
     if (a.dq_weight == nullptr && a.dk_weight == nullptr) a.parts = nullptr;
     cut_rotation(q, k, a.r, ctas, a.parts != nullptr ? block_runs(std::max(a.r.q_width, a.r.k_width), kRotateBackVecs) : 1LL << 40, a.parts != nullptr ? kLeastRows : 1);

@@ -265,13 +265,13 @@ enum RowNorm : int { kNormNone = ARL2_NORM_NONE, kNormLayer = ARL2_NORM_LAYER, k
                      kNormHead = ARL2_NORM_HEAD, kNormLength = ARL2_NORM_LENGTH };
 constexpr int kBlockMostChannels = 8192;   // of a row: of the modulation, of queries, of keys
 // How a row of d channels is held: `warps` warps whose lanes have `vecs` groups of eight channels each, at most `most` of them; teams of
-// warps that make up a CTA; and the runs of rows whose sums over tokens have room in a workspace: those of four CTAs per SM of 148.
+// warps that make up a CTA; and the runs of rows whose sums over tokens have room in a workspace: those of eight CTAs per SM of 148.
 constexpr int kTileRuns = 4 * 148;           // runs of the modulation's backward pass
 constexpr int kModulateVecs = 2, kRotateVecs = 4, kRotateBackVecs = 3;
 constexpr int block_warps(int d, int most) { return (d / 8 + 32 * most - 1) / (32 * most); }
 constexpr int block_vecs(int d, int most) { return (d / 8 + 32 * block_warps(d, most) - 1) / (32 * block_warps(d, most)); }
-constexpr int block_teams(int d, int most) { return block_warps(d, most) >= 8 ? 1 : 8 / block_warps(d, most); }
-constexpr int block_runs(int d, int most) { return 4 * 148 * block_teams(d, most); }
+constexpr int block_teams(int d, int most) { return block_warps(d, most) > 1 ? 1 : 4; }
+constexpr int block_runs(int d, int most) { return 8 * 148 * block_teams(d, most); }
 struct FrameRows {           // a row of d channels per frame, fp32; nullptr: none
     const float* p;
     int64_t batch, frame;    // strides in elements

@@ -208,7 +208,7 @@ constexpr int kTeamWarps = 16;   // warps of a team at most
 // memory, N numbers of each in rows of kTeamWarps (zeros behind the last warp's), which each lane reads four at a time: shuffles would
 // be four more steps one after the other.  Two places by turns, so that one barrier per exchange is enough: a warp that writes to a
 // place for the second time has passed the barrier behind which everyone was done with the first.
-template <int N> constexpr int kTeamFloats = 8 * 2 * N * kTeamWarps;     // for the most teams of a CTA
+template <int N> constexpr int kTeamFloats = 4 * 2 * N * kTeamWarps;     // for the most teams of a CTA
 template <int N>
 struct Team {
     float* place;        // [2][N][kTeamWarps], this team's
