@@ -663,8 +663,7 @@ class _BlockOp:
         ctx = self.layer._ctx
         if ctx is None:
             raise Arl2Error(f"{call.__name__}: the layer has been closed")
-        current = torch.cuda.current_device()
-        index = self._index
+        current, index = torch.cuda.current_device(), self._index
         if index is None or index == current:
             status = call(ctx, *args, _raw_stream(current))
         else:
@@ -738,18 +737,20 @@ class Modulation(_BlockOp):
         flags = ARL2_MODULATION_FP32_RESIDUAL if self.residual is not self.dtype else 0
         self.cfg = arl2_modulation_config(ctypes.sizeof(arl2_modulation_config), frame_tokens, names[norm], names[post], eps, flags)
         self._cfg = ctypes.byref(self.cfg)
+        self._modulate = self._lib.arl2_modulate
         self.workspace_bytes(1)     # (what the library refuses is refused here)
 
     def workspace_bytes(self, tokens):
         return self._bytes(self._lib.arl2_modulation_workspace_bytes, tokens)
 
-    def _frames(self, tokens):
-        return -(-tokens // self.frame_tokens)
-
-    def _modulation(self, t, tokens, what):
+    def _modulation(self, t, shape, what):
         if t is None:
             return None
-        return self._strided(t, (self._B, self._frames(tokens), self._width), torch.float32, what, 2)
+        if isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.get_device() == self._index and t.shape == shape:
+            batch, frame, channel = t.stride()
+            if channel == 1:
+                return arl2_rows(t.data_ptr(), batch if shape[0] > 1 else 0, frame if shape[1] > 1 else 0)
+        return self._strided(t, shape, torch.float32, what, 2)
 
     def _weight(self, t, what):
         if t is not None:
@@ -779,9 +780,10 @@ class Modulation(_BlockOp):
             n = torch.empty_like(y) if y is not None else torch.empty(shape, dtype=self.dtype, device=self.device)
         else:
             want(n, shape, self.dtype, "n")
-        self._run(self._lib.arl2_modulate, self._cfg, tokens, x.data_ptr(), _ptr(y), self._modulation(gate, tokens, "gate"),
-                  self._modulation(scale, tokens, "scale"), self._modulation(shift, tokens, "shift"), self._weight(weight, "weight"),
-                  self._weight(post_weight, "post_weight"), _ptr(r), _ptr(n))
+        rows = (shape[0], -(-tokens // self.frame_tokens), shape[2])
+        self._run(self._modulate, self._cfg, tokens, x.data_ptr(), _ptr(y), self._modulation(gate, rows, "gate"), self._modulation(scale, rows, "scale"),
+                  self._modulation(shift, rows, "shift"), None if weight is None else self._weight(weight, "weight"),
+                  None if post_weight is None else self._weight(post_weight, "post_weight"), _ptr(r), _ptr(n))
         return (x if r is None else r), n
 
     def backward(self, r, dn=None, dr=None, y=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, workspace=None):
@@ -794,9 +796,9 @@ class Modulation(_BlockOp):
         for t, kind, what in ((dn, self.dtype, "dn"), (dr, self.residual, "dr"), (y, self.dtype, "y")):
             if t is not None:
                 want(t, shape, kind, what)
-        gate_rows, scale_rows = self._modulation(gate, tokens, "gate"), self._modulation(scale, tokens, "scale")
-        if shift is not None:
-            self._modulation(shift, tokens, "shift")
+        rows = (shape[0], -(-tokens // self.frame_tokens), shape[2])
+        gate_rows, scale_rows = self._modulation(gate, rows, "gate"), self._modulation(scale, rows, "scale")
+        self._modulation(shift, rows, "shift")
         w, pw = self._weight(weight, "weight"), self._weight(post_weight, "post_weight")
         dx = torch.empty_like(r if r is not None else dr)
         dy = None if y is None else torch.empty_like(y)

@@ -1698,7 +1698,7 @@ bool valid_recurrence(const char* who, const arl2_config& cfg, const arl2_recurr
     if (!check_tokens(who, cfg, tokens)) return false;
     // tiles of three products, of whole blocks and of the shorter one
     const int64_t block = c->block_tokens < tokens ? c->block_tokens : tokens, tiles = (tokens + block - 1) / block * ((block + kRecurTile - 1) / kRecurTile);
-    if (tiles * cfg.B * cfg.H * 3 >= ((int64_t)1 << 30)) { set_error("%s: too many blocks", who); return false; }
+    if (tiles * cfg.B * cfg.H * 3 >= ((int64_t)1 << 28)) { set_error("%s: too many blocks", who); return false; }
     return true;
 }
 

@@ -443,9 +443,9 @@ int launched(cudaError_t e, const char* what)
 
 bool tc_recur_supported(const RecurArgs& a)
 {
-    // (a tensor map's strides are below 2^40 bytes, its coordinates 31 bits)
+    // (a tensor map's strides are below 2^40 bytes and not zero, its coordinates 31 bits; dO is there backward only, and contiguous)
     for (const RecurRows* r : {&a.q, &a.k, &a.v, &a.dout})
-        if (r->token >= ((int64_t)1 << 39) / a.block || r->batch >= ((int64_t)1 << 39)) return false;
+        if (r->token < 1 || r->token >= ((int64_t)1 << 39) / a.block || r->batch >= ((int64_t)1 << 39)) return false;
     return (int64_t)a.B * recur_heads(a) * a.N * a.pair * 2 * a.D < ((int64_t)1 << 31);
 }
 

@@ -177,6 +177,31 @@ def test_in_place_and_expanded_rows():
     assert r is x and n is y and torch.equal(x, want[0]) and torch.equal(y, want[1])
 
 
+def test_backward_in_place():
+    """The C call: dx may be dr, and dy may be y or dn."""
+    import ctypes
+
+    B, T, frame, H, D = 2, 333, 50, 12, 128
+    arl2, m = op(B, H, D, torch.bfloat16, frame)
+    x, y, gate, scale, shift, weight, _, randn = inputs(B, T, frame, H * D, torch.bfloat16, False, 10)
+    dn, dr = randn(*x.shape).to(x.dtype), randn(*x.shape).to(x.dtype)
+    want = m.backward(x, dn, dr, y, gate=gate, scale=scale)
+    ws = torch.empty(m.workspace_bytes(T), dtype=torch.uint8, device="cuda")
+    rows = [ctypes.byref(arl2.arl2_rows(t.data_ptr(), t.stride(0), t.stride(1))) for t in (gate, scale)]
+
+    def call(dn, dr, y, dx, dy):
+        return arl2.load().arl2_modulate_backward(m.layer._ctx, ctypes.byref(m.cfg), T, x.data_ptr(), dn.data_ptr(), dr.data_ptr(), y.data_ptr(), *rows, None, None,
+                                                  dx.data_ptr(), dy.data_ptr(), *[None] * 5, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+
+    for over in ("y", "dn"):
+        t = {"dn": dn.clone(), "dr": dr.clone(), "y": y.clone()}
+        assert call(t["dn"], t["dr"], t["y"], t["dr"], t[over]) == 0
+        assert torch.equal(t["dr"], want[0]) and torch.equal(t[over], want[1])
+    assert call(dn, dr, y, dn, torch.empty_like(y)) == -1 and call(dn, dr, y, torch.empty_like(x), dr) == -1
+    other = torch.empty_like(x)
+    assert call(dn, dr, y, other, other) == -1
+
+
 def test_a_large_mean_keeps_its_digits():
     """Rows of mean 1000 and deviation 1: each input is off by its own rounding alone, which the definition sees too."""
     B, T, H, D = 1, 40, 12, 128

@@ -136,6 +136,44 @@ def test_one_stream_for_all():
     got = r.forward(*one, decay)
     want = r.forward(*(t.contiguous() for t in one), decay)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # ... or over the tokens, which tiled copies cannot do: the plain kernels take them, off by as much
+    one[1] = k[:, :1].expand(-1, T, -1, -1)
+    case = (B, T, block, H, D, BF, False)
+    out, last = r.forward(*one, decay)
+    x = [t.double() for t in one]
+    want, want_last = recur64(*x, torch.sigmoid(decay.double()), zeros_like_state(q), block)
+    mag, mag_last = recur64(*(t.abs() for t in x), torch.sigmoid(decay.double()), zeros_like_state(q), block)
+    near(out, want, parts_of(case)[0] * mag, "out")
+    near(last, want_last, parts_of(case)[1] * mag_last, "state")
+    do = v.contiguous()
+    for a, b in zip(r.backward(do, *one, decay), r.backward(do, *(t.contiguous() for t in one), decay)):
+        assert float((a.double() - b.double()).abs().max()) <= 2.0 ** -7 * float(b.double().abs().max())
+
+
+def test_states_in_place():
+    """The C calls: a state may be replaced by the one behind the last block, and its gradient by that of the one before the first."""
+    import ctypes
+
+    B, T, block, H, D = 2, 50, 20, 3, 64
+    arl2, r = op(B, H, D, BF, block)
+    q, k, v, decay, state, randn = inputs((B, T, block, H, D, BF, True), 9)
+    want, want_last = r.forward(q, k, v, decay, state=state)
+    do, dstate = randn(B, T, H, D).to(BF), randn(B, H, D, D)
+    grads = r.backward(do, q, k, v, decay, state=state, dstate=dstate)
+    lib, stream = arl2.load(), torch.cuda.current_stream().cuda_stream
+    rows = [ctypes.byref(arl2.arl2_rows(t.data_ptr(), T * H * D, H * D)) for t in (q, k, v)]
+    ws = torch.empty(r.workspace_bytes(T, True), dtype=torch.uint8, device="cuda")
+    s, ds, out = state.clone(), dstate.clone(), [torch.empty_like(q) for _ in range(4)]
+    args = (r.layer._ctx, ctypes.byref(r.cfg), T)
+    assert lib.arl2_recur(*args, *rows, decay.data_ptr(), s.data_ptr(), out[0].data_ptr(), s.data_ptr(), ws.data_ptr(), ws.numel(), stream) == 0
+    assert torch.equal(out[0], want) and torch.equal(s, want_last)
+    assert lib.arl2_recur_backward(*args, do.data_ptr(), *rows, decay.data_ptr(), state.data_ptr(), ds.data_ptr(), *(t.data_ptr() for t in out[1:]), None,
+                                   ds.data_ptr(), ws.data_ptr(), ws.numel(), stream) == 0
+    assert torch.equal(ds, grads[4]) and all(torch.equal(a, b) for a, b in zip(out[1:], grads[:3]))
+    # and what may not be the same memory
+    assert lib.arl2_recur(*args, *rows, decay.data_ptr(), None, q.data_ptr(), None, ws.data_ptr(), ws.numel(), stream) == -1
+    assert lib.arl2_recur_backward(*args, do.data_ptr(), *rows, decay.data_ptr(), None, None, do.data_ptr(), out[1].data_ptr(), out[2].data_ptr(), None, None,
+                                   ws.data_ptr(), ws.numel(), stream) == -1
 
 
 def test_block_after_block_is_the_layer():
