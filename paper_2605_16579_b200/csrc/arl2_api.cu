@@ -1702,7 +1702,7 @@ bool valid_recurrence(const char* who, const arl2_config& cfg, const arl2_recurr
     return true;
 }
 
-struct RecurLayout { size_t slots, states, dstates, beside, dots, total; };
+struct RecurLayout { size_t slots, states, dstates, beside, dbeside, dots, total; };
 RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c, int32_t tokens, bool back)
 {
     const bool tc = recur_tensor_cores(cfg);
@@ -1718,6 +1718,7 @@ RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c
     l.states = off;  off += state;
     l.dstates = off; off += back ? state : 0;
     l.beside = off;  off += back && tc ? state : 0;
+    l.dbeside = off; off += back && tc && cfg.B * cfg.H * blocks <= kRecurApart ? state : 0;
     l.dots = off;    off += back ? align_up((size_t)cfg.B * cfg.H * blocks * (dd / 32) * sizeof(float)) : 0;
     l.total = off;
     return l;
@@ -1757,6 +1758,7 @@ int recur_args(const char* who, arl2_ctx* ctx, const arl2_recurrence_config* c, 
         a.states_op = reinterpret_cast<__nv_bfloat16*>(w + lay.states);
         a.dstates_op = back ? reinterpret_cast<__nv_bfloat16*>(w + lay.dstates) : nullptr;
         a.states = back ? reinterpret_cast<float*>(w + lay.beside) : nullptr;
+        a.dstates = back && cfg.B * cfg.H * (size_t)a.N <= kRecurApart ? reinterpret_cast<float*>(w + lay.dbeside) : nullptr;
     } else {
         a.pair = 1;
         a.states = reinterpret_cast<float*>(w + lay.states);

@@ -448,26 +448,58 @@ struct RecurArgs {
     __nv_bfloat16* dstates_op;
     float* dots;             // [B, H, N, dot_parts]: parts of <dstate, state>
     int dot_parts;           // D * D / 128, or D * D / 32 (set by the launcher)
+    bool apart;              // the scan's directions at once; no dots (set by the launcher)
     uint32_t* status;
     uint32_t wait_limit;
     RecurStep sums, rows;
 };
 __host__ __device__ inline int recur_heads(const RecurArgs& a) { return (a.H + a.pair - 1) / a.pair; }
 __device__ __forceinline__ float gate_of(float logit) { return 1.0f / (1.0f + expf(-logit)); }
-// da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n> for blocks of heads u, u + step, ..: a warp each, in the kernel behind the scan
-__device__ __forceinline__ void recur_gates(const RecurArgs& a, int u, int step)
+// da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n>, in the kernel behind the scan, by kThreads threads of each CTA (`thread`: which of them):
+// from the scan's parts a warp for each block of a head, or from the states themselves all of them.  `smem`: a number for each warp.
+constexpr int kRecurApart = 4 * 148;       // blocks of all heads up to which the scan leaves that to them
+template <int kThreads>
+__device__ __forceinline__ void recur_gates(const RecurArgs& a, int thread, float* smem)
 {
     if (!a.back || a.ddecay == nullptr) return;
-    for (; u < a.B * a.H * a.N; u += step) {
-        float s = 0.0f;
-        for (int i = threadIdx.x & 31; i < a.dot_parts; i += 32) s += a.dots[(size_t)u * a.dot_parts + i];
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    constexpr int kWarps = kThreads / 32;
+    const int warp = thread >> 5, lane = thread & 31, units = a.B * a.H * a.N, dd = a.D * a.D;
+    auto write = [&](int u, float s) {
         const int bh = u / a.N, n = u - bh * a.N, b = bh / a.H;
         const size_t at = ((size_t)b * a.N + n) * a.H + bh - b * a.H;
         const float x = a.decay[at];
         // (alpha (1 - alpha) without the difference, which loses its digits near 1)
-        if ((threadIdx.x & 31) == 0) a.ddecay[at] = s * gate_of(x) * gate_of(-x);
+        a.ddecay[at] = s * gate_of(x) * gate_of(-x);
+    };
+    if (!a.apart) {
+        for (int u = blockIdx.x * kWarps + warp; u < units; u += gridDim.x * kWarps) {
+            float s = 0.0f;
+            for (int i = lane; i < a.dot_parts; i += 32) s += a.dots[(size_t)u * a.dot_parts + i];
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane == 0) write(u, s);
+        }
+        return;
     }
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        const int bh = u / a.N, n = u - bh * a.N, b = bh / a.H, h = bh - b * a.H, hu = h / a.pair;
+        const size_t at = (((size_t)(b * recur_heads(a) + hu) * a.N + n) * a.pair + h - hu * a.pair) * dd;
+        float s = 0.0f;
+#pragma unroll 4
+        for (int e = thread * 4; e < dd; e += kThreads * 4) {
+            const float4 x = *reinterpret_cast<const float4*>(a.states + at + e), y = *reinterpret_cast<const float4*>(a.dstates + at + e);
+            s += fmaf(x.x, y.x, x.y * y.y) + fmaf(x.z, y.z, x.w * y.w);
+        }
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
+        if (lane == 0) smem[warp] = s;
+        asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
+        if (thread == 0) {
+            s = 0.0f;
+            for (int w = 0; w < kWarps; ++w) s += smem[w];
+            write(u, s);
+        }
+    }
+    asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");      // (what `smem` is next, nobody reads any more)
 }
 int recur(RecurArgs& a, int dtype, bool tensor_cores, cudaStream_t st);
 // whether the tensors can be read by tiled copies

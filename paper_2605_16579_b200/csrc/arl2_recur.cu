@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
     const RecurRun run = recur_run(a.rows, blockIdx.x);
     const int first = 0, last = run.count;
     grid_dependency_sync();
-    recur_gates(a, blockIdx.x * (kRThreads / 32) + warp, gridDim.x * (kRThreads / 32));
+    recur_gates<kRThreads>(a, tid, smem);
     if (first >= last) return;
 
     float4 xr[kLoads];
@@ -392,7 +392,9 @@ template <int D, int kEach>
 __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_constant__ RecurArgs a)
 {
     __shared__ ScanBlock blocks[kScanThreads];
-    const int tid = threadIdx.x, e = (blockIdx.x * kScanThreads + tid) * kEach, head = blockIdx.y, b = blockIdx.z;
+    // apart: the two directions are different CTAs' work, and <D, S> is left to the step behind
+    const int tid = threadIdx.x, e = (blockIdx.x * kScanThreads + tid) * kEach, head = blockIdx.y, b = a.apart ? blockIdx.z >> 1 : blockIdx.z;
+    const bool forward = !a.apart || (blockIdx.z & 1) == 0, backward = a.back && (!a.apart || (blockIdx.z & 1) != 0);
     const int hu = head / a.pair, in_pair = head - hu * a.pair;
     const size_t unit0 = (size_t)(b * recur_heads(a) + hu) * a.N, at = ((size_t)b * a.H + head) * D * D + e, size = (size_t)a.pair * D * D;
     const float* slots = a.slots + (size_t)in_pair * D * D + e;
@@ -424,8 +426,8 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
     Value s;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) s.v[k] = 0.0f;
-    if (a.state_in != nullptr) s.load(a.state_in + at);
-    for (int base = 0; base < a.N; base += kScanThreads) {
+    if (forward && a.state_in != nullptr) s.load(a.state_in + at);
+    for (int base = 0; forward && base < a.N; base += kScanThreads) {
         const int here = min(kScanThreads, a.N - base);
         __syncthreads();
         if (tid < here) blocks[tid] = scan_block(a, 0, b, head, base + tid);
@@ -442,13 +444,12 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
                 }
         }
     }
-    if (!a.back) {
-        if (a.state_out != nullptr) s.store(a.state_out + at);
-        return;
-    }
+    if (!a.back && a.state_out != nullptr) s.store(a.state_out + at);
+    if (!backward) return;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) s.v[k] = 0.0f;
     if (a.dstate_out != nullptr) s.load(a.dstate_out + at);
+    const bool with_dots = !a.apart;
     float* dots = a.dots + ((size_t)b * a.H + head) * a.N * (D * D / (32 * kEach)) + e / (32 * kEach);
     for (int base = (a.N - 1) / kScanThreads * kScanThreads; base >= 0; base -= kScanThreads) {
         const int here = min(kScanThreads, a.N - base);
@@ -459,18 +460,20 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
             Value sum[kScanAhead], before[kScanAhead];
 #pragma unroll
             for (int i = 0; i < kScanAhead; ++i)
-                if (i0 - i >= 0) before[i].load(a.states + ((unit0 + base + i0 - i) * a.pair + in_pair) * D * D + e);   // (this thread's own)
+                if (with_dots && i0 - i >= 0) before[i].load(a.states + ((unit0 + base + i0 - i) * a.pair + in_pair) * D * D + e);   // (this thread's own)
             fetch(sum, i0, -1, i0 + 1);
 #pragma unroll
             for (int i = 0; i < kScanAhead; ++i)
                 if (i0 - i >= 0) {
                     const int n = base + i0 - i;
                     scan_store<D>(a.dstates, a.dstates_op, unit0 + n, in_pair, a.pair, e, s);
-                    float dot = 0.0f;
+                    if (with_dots) {
+                        float dot = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < kEach; ++k) dot = fmaf(s.v[k], before[i].v[k], dot);
-                    dot = warp_sum(dot);
-                    if ((tid & 31) == 0) dots[(size_t)n * (D * D / (32 * kEach))] = dot;
+                        for (int k = 0; k < kEach; ++k) dot = fmaf(s.v[k], before[i].v[k], dot);
+                        dot = warp_sum(dot);
+                        if ((tid & 31) == 0) dots[(size_t)n * (D * D / (32 * kEach))] = dot;
+                    }
 #pragma unroll
                     for (int k = 0; k < kEach; ++k) s.v[k] = fmaf(blocks[i0 - i].gate, s.v[k], sum[i].v[k]);
                 }
@@ -507,7 +510,10 @@ template <int D>
 int launch_scan(RecurArgs& a, cudaStream_t st)
 {
     const int each = scan_each(a);
-    const dim3 grid((unsigned)(D * D / (each * kScanThreads)), (unsigned)a.H, (unsigned)a.B);
+    // both directions at once where the states are few: their products are read again then (us of a backward scan and the step behind
+    // it over 21 blocks of 2 x 5 heads of 64 channels: 18 and 10 one after the other, 13 and 12 so)
+    a.apart = a.back && (long long)a.B * a.H * a.N <= kRecurApart;
+    const dim3 grid((unsigned)(D * D / (each * kScanThreads)), (unsigned)a.H, (unsigned)(a.apart ? 2 * a.B : a.B));
     a.dot_parts = D * D / (32 * each);
     return check_launch(each == 1 ? launch_kernel(recur_scan_kernel<D, 1>, grid, kScanThreads, 0, st, a) : launch_kernel(recur_scan_kernel<D, 4>, grid, kScanThreads, 0, st, a),
                         "recur_scan_kernel");

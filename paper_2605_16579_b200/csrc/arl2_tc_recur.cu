@@ -38,7 +38,7 @@ enum SBar : int { kSBarFull0 = 0, kSBarFree0 = kSBarFull0 + kSStages, kSBarAccFu
                   kSBarDrain = kSBarAccFree0 + 2, kSNumBars };
 enum RBar : int { kRBarFull0 = 0, kRBarFree0 = kRBarFull0 + kRStages, kRBarMatFull0 = kRBarFree0 + kRStages, kRBarMatFree0 = kRBarMatFull0 + 2,
                   kRBarAccFull0 = kRBarMatFree0 + 2, kRBarAccFree0 = kRBarAccFull0 + 2, kRBarDrain = kRBarAccFree0 + 2, kRNumBars };
-static_assert(kSNumBars * 8 + 16 <= 256 && kRNumBars * 8 + 16 <= 256, "barrier block");
+static_assert(kSNumBars * 8 + 16 <= 256 && kRNumBars * 8 + 16 + 8 * 4 <= 256, "barrier block");
 
 // rows of a TMA box for blocks of `len` tokens
 __host__ __device__ constexpr int box_rows(int len) { return len >= kTile ? kTile : (len + 15) / 16 * 16; }
@@ -334,7 +334,7 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         mma_commit_if(lead, ubars + 8 * kRBarDrain);
         drain_bar(ubars + 8 * kRBarDrain, 0);
     } else {
-        recur_gates(a, blockIdx.x * 8 + warp - 2, gridDim.x * 8);      // (while the first tiles are on their way)
+        recur_gates<256>(a, tid - 64, reinterpret_cast<float*>(smem + kROffBars + kRNumBars * 8 + 16));      // (while the first tiles are on their way)
         const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
         const uint64_t policy = tile_policy(a);
