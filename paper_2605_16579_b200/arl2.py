@@ -658,6 +658,7 @@ class _BlockOp:
         self._B, self._H, self._D = layer.B, layer.H, layer.D
         self._width = layer.H * layer.D
         self._sizes = {}
+        self._byte = torch.empty(1, dtype=torch.uint8, device=self.device) if self.device.type == "cuda" and self._lib is not None else None
 
     def _run(self, call, *args):
         ctx = self.layer._ctx
@@ -674,10 +675,7 @@ class _BlockOp:
 
     def _strided(self, t, shape, dtype, what, inner):
         """arl2_rows of a tensor [B, rows, ...] whose dimensions from `inner` on are contiguous."""
-        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self._index and t.shape == shape:
-            if t.is_contiguous():
-                row = shape[2] if inner + 1 == len(shape) else shape[2] * shape[3]
-                return arl2_rows(t.data_ptr(), shape[1] * row, row)
+        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == self._index:
             st, row = t.stride(), 1
             for i in range(len(shape) - 1, inner - 1, -1):
                 if shape[i] != 1 and st[i] != row:
@@ -688,6 +686,14 @@ class _BlockOp:
                 return arl2_rows(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else row)
         raise Arl2Error(f"{what}: expected a tensor {tuple(shape)} {dtype} on {self.device} with contiguous rows, got "
                         + (f"{tuple(t.shape)} {t.dtype} with strides {tuple(t.stride())} on {t.device}" if isinstance(t, torch.Tensor) else f"{t!r}"))
+
+    def _heads(self, t, shape, what):
+        """The same of [B, T, heads, D] of the layer's type, whose heads and channels are contiguous."""
+        if isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.shape == shape and t.get_device() == self._index:
+            batch, token, head, channel = t.stride()
+            if channel == 1 and (head == shape[3] or shape[2] == 1):
+                return arl2_rows(t.data_ptr(), batch if shape[0] > 1 else 0, token if shape[1] > 1 else shape[2] * shape[3])
+        return self._strided(t, shape, self.dtype, what, 2)
 
     def _fp32(self, like):
         """A contiguous fp32 tensor of another's shape, or None."""
@@ -705,14 +711,15 @@ class _BlockOp:
         return n
 
     def _tokens(self, t, what, dims):
-        if not isinstance(t, torch.Tensor) or t.dim() != dims:
+        shape = t.shape if isinstance(t, torch.Tensor) else ()
+        if len(shape) != dims:
             raise Arl2Error(f"{what}: expected a tensor of {dims} dimensions")
-        return t.shape[1]
+        return shape[1]
 
     def _scratch(self, n, given):
         """Scratch of one call: the caller's, or memory that torch hands out for the current stream (or the graph being captured)."""
         if given is None:
-            return torch.empty(n, dtype=torch.uint8, device=self.device)
+            return self._byte.new_empty(n)      # (costs the host less than torch.empty)
         if not (isinstance(given, torch.Tensor) and given.get_device() == self._index and given.dtype == torch.uint8 and given.is_contiguous()):
             raise Arl2Error(f"workspace: expected contiguous uint8 on {self.device}")
         return given
@@ -861,8 +868,8 @@ class Rotation(_BlockOp):
         contiguous input is written in place."""
         tokens = self._tokens(q, "q", 4)
         q_shape, k_shape = (self._B, tokens, self._H, self._D), (self._B, tokens, self.kv_heads, self._D)
-        q_rows = self._strided(q, q_shape, self.dtype, "q", 2)
-        k_rows = None if k is None else self._strided(k, k_shape, self.dtype, "k", 2)
+        q_rows = self._heads(q, q_shape, "q")
+        k_rows = None if k is None else self._heads(k, k_shape, "k")
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
@@ -883,8 +890,8 @@ class Rotation(_BlockOp):
         self.layer._want(dq_out, q_shape, self.dtype, "dq_out")
         if dk_out is not None:
             self.layer._want(dk_out, k_shape, self.dtype, "dk_out")
-        q_rows = None if q is None else self._strided(q, q_shape, self.dtype, "q", 2)
-        k_rows = None if k is None else self._strided(k, k_shape, self.dtype, "k", 2)
+        q_rows = None if q is None else self._heads(q, q_shape, "q")
+        k_rows = None if k is None else self._heads(k, k_shape, "k")
         dq, dk = torch.empty_like(dq_out), None if dk_out is None else torch.empty_like(dk_out)
         q_w, k_w = self._weight(q_weight, self._H, "q_weight"), self._weight(k_weight, self.kv_heads, "k_weight")
         dq_weight = None if q_weight is None else torch.empty_like(q_weight)
@@ -904,6 +911,7 @@ class Recurrence(_BlockOp):
     def __init__(self, layer, block_tokens):
         super().__init__(layer)
         self.block_tokens = block_tokens
+        self._states = (layer.B, layer.H, layer.D, layer.D)
         self.cfg = arl2_recurrence_config(ctypes.sizeof(arl2_recurrence_config), block_tokens)
         self._cfg = ctypes.byref(self.cfg)
         self.workspace_bytes(1)
@@ -913,15 +921,18 @@ class Recurrence(_BlockOp):
 
     def _inputs(self, q, k, v, decay_logits, state):
         tokens = self._tokens(q, "q", 4)
-        shape = (self._B, tokens, self._H, self._D)
-        rows = [self._strided(t, shape, self.dtype, what, 2) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
+        shape, heads = (self._B, tokens, self._H, self._D), self._heads
+        rows = heads(q, shape, "q"), heads(k, shape, "k"), heads(v, shape, "v")
         self.layer._want(decay_logits, (self._B, -(-tokens // self.block_tokens), self._H), torch.float32, "decay_logits")
-        self._state(state, "state")
+        if state is not None:
+            self._state(state, "state")
         return tokens, shape, rows
 
     def _state(self, t, what):
-        if t is not None:
-            self.layer._want(t, (self._B, self._H, self._D, self._D), torch.float32, what)
+        self.layer._want(t, self._states, torch.float32, what)
+
+    def _new_state(self, like):
+        return torch.empty(self._states, dtype=torch.float32, device=self.device) if like is None else torch.empty_like(like)
 
     def forward(self, q, k, v, decay_logits, state=None, final=True, out=None, workspace=None):
         """q, k, v [B, T, H, D] (heads and channels contiguous), decay_logits fp32 [B, ceil(T / block_tokens), H], state fp32 [B, H, D, D] or None
@@ -931,9 +942,7 @@ class Recurrence(_BlockOp):
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             self.layer._want(out, shape, self.dtype, "out")
-        last = None
-        if final:
-            last = torch.empty((self._B, self._H, self._D, self._D), dtype=torch.float32, device=self.device) if state is None else torch.empty_like(state)
+        last = self._new_state(state) if final else None
         ws = self._scratch(self.workspace_bytes(tokens), workspace)
         self._run(self._lib.arl2_recur, self._cfg, tokens, *rows, decay_logits.data_ptr(), _ptr(state), out.data_ptr(), _ptr(last), ws.data_ptr(), ws.numel())
         return out, last
@@ -943,10 +952,11 @@ class Recurrence(_BlockOp):
         block (None: zeros); the last is None with ``initial=False``."""
         tokens, shape, rows = self._inputs(q, k, v, decay_logits, state)
         self.layer._want(dout, shape, self.dtype, "dout")
-        self._state(dstate, "dstate")
+        if dstate is not None:
+            self._state(dstate, "dstate")
         dq, dk, dv = torch.empty_like(dout), torch.empty_like(dout), torch.empty_like(dout)
         ddecay = torch.empty_like(decay_logits)
-        first = torch.empty(self._B, self._H, self._D, self._D, dtype=torch.float32, device=self.device) if initial else None
+        first = self._new_state(dstate if state is None else state) if initial else None
         ws = self._scratch(self.workspace_bytes(tokens, True), workspace)
         self._run(self._lib.arl2_recur_backward, self._cfg, tokens, dout.data_ptr(), *rows, decay_logits.data_ptr(), _ptr(state), _ptr(dstate),
                   dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ddecay.data_ptr(), _ptr(first), ws.data_ptr(), ws.numel())
