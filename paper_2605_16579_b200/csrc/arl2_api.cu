@@ -1685,7 +1685,7 @@ int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* c, const flo
 // ---- the recurrence over the blocks of a sequence -------------------------------------------------------------
 namespace {
 
-bool recur_tensor_cores(const arl2_config& c) { return c.io_dtype == ARL2_BF16 && !(c.flags & ARL2_FLAG_FORCE_SIMT); }
+bool recur_tensor_cores(const arl2_config& c) { return !(c.flags & ARL2_FLAG_FORCE_SIMT); }
 
 bool valid_recurrence(const char* who, const arl2_config& cfg, const arl2_recurrence_config* c, int32_t tokens)
 {
@@ -1708,15 +1708,16 @@ RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c
     const bool tc = recur_tensor_cores(cfg);
     const size_t pair = tc && cfg.D == 64 ? 2 : 1, heads = (cfg.H + pair - 1) / pair, dd = (size_t)cfg.D * cfg.D;
     const size_t blocks = (size_t)(((int64_t)tokens + c.block_tokens - 1) / c.block_tokens), units = cfg.B * heads * blocks;
-    const size_t state = align_up(units * pair * dd * sizeof(float));      // (as two bf16 numbers it takes the same room)
+    const size_t state = align_up(units * pair * dd * sizeof(float));      // (as two bf16 numbers it takes the same room, as three half as much again)
+    const size_t operand = tc && cfg.io_dtype == ARL2_FP32 ? align_up(units * pair * dd * 6) : state;
     RecurLayout l;
     size_t off = 0;
     // (a slice holds a tile at least, and of each job's slices there are at most as many as CTAs: two jobs, each with its shorter blocks)
     const size_t block = c.block_tokens < tokens ? c.block_tokens : tokens, tiles = units * (back ? 2 : 1) * ((block + kRecurTile - 1) / kRecurTile);
     const size_t slices = (size_t)kRecurCtas * (back ? 4 : 2);
     l.slots = off;   off += align_up((units * (back ? 2 : 1) + (tiles < slices ? tiles : slices)) * pair * dd * sizeof(float));
-    l.states = off;  off += state;
-    l.dstates = off; off += back ? state : 0;
+    l.states = off;  off += operand;
+    l.dstates = off; off += back ? operand : 0;
     l.beside = off;  off += back && tc ? state : 0;
     l.dbeside = off; off += back && tc && cfg.B * cfg.H * blocks <= kRecurApart ? state : 0;
     l.dots = off;    off += back ? align_up((size_t)cfg.B * cfg.H * blocks * (dd / 32) * sizeof(float)) : 0;
@@ -1752,6 +1753,7 @@ int recur_args(const char* who, arl2_ctx* ctx, const arl2_recurrence_config* c, 
     a.decay = decay; a.state_in = state_in;
     uint8_t* w = static_cast<uint8_t*>(ws);
     a.pair = cfg.D == 64 ? 2 : 1;
+    a.op_parts = cfg.io_dtype == ARL2_FP32 ? 3 : 2;
     tc = recur_tensor_cores(cfg) && tc_recur_supported(a);
     a.slots = reinterpret_cast<float*>(w + lay.slots);
     if (tc) {

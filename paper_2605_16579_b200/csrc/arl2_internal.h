@@ -444,8 +444,9 @@ struct RecurArgs {
     float* slots;            // [units + slices of the sums, pair, D, D]
     float* states;           // [B, H / pair up, N, pair, D, D] fp32: state before block n
     float* dstates;          // ... and the gradient of the state after block n
-    __nv_bfloat16* states_op;    // the same as a bf16 head and a bf16 remainder, [.., pair, 2, D, D] (tensor cores)
+    __nv_bfloat16* states_op;    // the same as bf16 numbers that add up to them, [.., pair, op_parts, D, D] (tensor cores)
     __nv_bfloat16* dstates_op;
+    int op_parts;            // two: head and remainder, 2^-17 off (bf16 I/O); or three (fp32)
     float* dots;             // [B, H, N, dot_parts]: parts of <dstate, state>
     int dot_parts;           // D * D / 128, or D * D / 32 (set by the launcher)
     bool apart;              // the scan's directions at once; no dots (set by the launcher)

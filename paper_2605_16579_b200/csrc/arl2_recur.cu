@@ -5,8 +5,8 @@
 // The sums over a block's tokens do not depend on the state, so only the scan over the blocks is sequential, and it is a few
 // operations per element of the states.  Three steps (arl2_internal.h): sums, scan, rows times states.
 //
-// This file has the scan, and sums and rows for fp32 I/O (and bf16 without tensor memory): warp-level matrix instructions on
-// TF32 numbers.  A fp32 operand is taken as a head of 11 bits and a remainder of 11 more, three products (remainder times remainder
+// This file has the scan, and sums and rows without tensor memory (contexts that ask for it, rows that a stride of zero repeats):
+// warp-level matrix instructions on TF32 numbers.  A fp32 operand is taken as a head of 11 bits and a remainder of 11 more, three products (remainder times remainder
 // left out): off by 2^-22 of each product; bf16 inputs are exact in the head alone.  The tensor cores cut what does not fit when they
 // add, always to the same side, so a sum stays with them for 32 terms only and is then added to the others by a rounding addition
 // (6 heads of 128 fp32, 3 x 2800 tokens: 1.5e-6 off without that, 3.4e-7 with it).
@@ -350,25 +350,27 @@ template <> struct ScanValue<4> {
 };
 
 template <int D, int kEach>
-__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, size_t unit, int in_pair, int pair, int e, const ScanValue<kEach>& s)
+__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, int op_parts, size_t unit, int in_pair, int pair, int e, const ScanValue<kEach>& s)
 {
     if (f32 != nullptr) s.store(f32 + (unit * pair + in_pair) * D * D + e);
     if (op == nullptr) return;
-    // head and remainder: 2^-17 of the value together; an infinity has no remainder
-    __nv_bfloat16* h = op + ((unit * pair + in_pair) * 2) * D * D + e;
-    __nv_bfloat16 hi[kEach], lo[kEach];
+    // a bf16 number, and again of what is left; nothing is left of an infinity
+    __nv_bfloat16* to = op + ((unit * pair + in_pair) * op_parts) * D * D + e;
+    float rest[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        hi[i] = __float2bfloat16_rn(s.v[i]);
-        const float back = __bfloat162float(hi[i]);
-        lo[i] = __float2bfloat16_rn(fabsf(back) <= 3.3e38f ? s.v[i] - back : 0.0f);
-    }
-    if (kEach == 4) {
-        *reinterpret_cast<uint2*>(h) = *reinterpret_cast<uint2*>(hi);
-        *reinterpret_cast<uint2*>(h + D * D) = *reinterpret_cast<uint2*>(lo);
-    } else {
-        *h = hi[0];
-        h[D * D] = lo[0];
+    for (int i = 0; i < kEach; ++i) rest[i] = s.v[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        if (p == op_parts) break;
+        __nv_bfloat16 part[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            part[i] = __float2bfloat16_rn(rest[i]);
+            const float back = __bfloat162float(part[i]);
+            rest[i] = fabsf(back) <= 3.3e38f ? rest[i] - back : 0.0f;
+        }
+        if (kEach == 4) *reinterpret_cast<uint2*>(to + p * D * D) = *reinterpret_cast<uint2*>(part);
+        else to[p * D * D] = part[0];
     }
 }
 
@@ -438,7 +440,7 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
 #pragma unroll
             for (int i = 0; i < kScanAhead; ++i)
                 if (i0 + i < here) {
-                    scan_store<D>(a.states, a.states_op, unit0 + base + i0 + i, in_pair, a.pair, e, s);
+                    scan_store<D>(a.states, a.states_op, a.op_parts, unit0 + base + i0 + i, in_pair, a.pair, e, s);
 #pragma unroll
                     for (int k = 0; k < kEach; ++k) s.v[k] = fmaf(blocks[i0 + i].gate, s.v[k], sum[i].v[k]);
                 }
@@ -466,7 +468,7 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
             for (int i = 0; i < kScanAhead; ++i)
                 if (i0 - i >= 0) {
                     const int n = base + i0 - i;
-                    scan_store<D>(a.dstates, a.dstates_op, unit0 + n, in_pair, a.pair, e, s);
+                    scan_store<D>(a.dstates, a.dstates_op, a.op_parts, unit0 + n, in_pair, a.pair, e, s);
                     if (with_dots) {
                         float dot = 0.0f;
 #pragma unroll

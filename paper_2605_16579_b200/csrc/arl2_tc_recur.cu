@@ -1,4 +1,4 @@
-// The recurrence over the blocks of a sequence on tensor cores (bf16 I/O): sums over tokens, X^T Y, and rows times states,
+// The recurrence over the blocks of a sequence on tensor cores: sums over tokens, X^T Y, and rows times states,
 // X M or X M^T (arl2_recur.cu has the mathematics and the scan between the two).
 //
 // Both go over 128-token tiles of units, a unit being a block of one head, or of two heads of 64 channels side by side; one CTA per
@@ -14,6 +14,12 @@
 // tc_recur_rows_kernel:  the same with warps 2-9 writing rows; a state is a bf16 head and a bf16 remainder (2^-17 of it
 //   together, 2^-9 of the output's own rounding), two products each.  M stands in shared memory as it is in memory; M^T is the
 //   same tile read with its other dimension innermost.
+//
+// fp32 I/O (the kernels with 32 in their names): each number is three of bf16, 24 bits, and a product six of its parts' (what is left out is
+// 2^-24 of it on average, 2^-21 at most), the smallest first, so that the tensor cores cut little when they add.  Eight warps load the rows, take them apart
+// into operand tiles of 64 tokens (sums) or 64 channels (rows), two of them by turns, and later add up or store what the tensor cores have
+// made of the tile before; the states come apart from the scan.  (8 heads of 128, 14000 tokens: sums 81 -> 43 us, rows 75 -> 34 against
+// pairs of TF32 numbers on warp-level instructions, of which an SM does 240 multiplications a clock.)
 //
 // Every wait is bounded; a CTA that gives up records ARL2_ERR_TIMEOUT, drains what is in flight and frees its tensor memory.
 #include "tc_common.cuh"
@@ -380,6 +386,418 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
     }
 }
 
+// ---- fp32: three bf16 numbers for each ---------------------------------------------------------------------------
+constexpr int k32Workers = 256, k32Threads = 384;          // 2 warpgroups that load, split and store; {MMA issuer, states, 2 idle}
+constexpr int k32RegsWorker = 216, k32RegsOther = 72;
+// (setmaxnreg.inc waits without a bound for registers of the CTA's own launch allocation)
+static_assert(k32Workers * k32RegsWorker + (k32Threads - k32Workers) * k32RegsOther <= k32Threads * ((65536 / k32Threads) / 8 * 8), "register pool");
+constexpr int k32Tokens = 64;                              // of an operand tile of the sums
+constexpr int k32Part = 16 * 1024;                         // a part of an operand tile: 64 tokens x 128 channels, or 128 x 64
+constexpr int k32SumOffBars = 2 * 6 * k32Part;
+constexpr int k32SumSmem = k32SumOffBars + 256 + 1024;
+constexpr int k32MatBytes = 3 * kTileBytes;
+constexpr int k32RowOffStage = k32MatBytes;
+constexpr int k32RowOffBars = k32RowOffStage + 2 * 3 * k32Part;
+constexpr int k32RowSmem = k32RowOffBars + 256 + 1024;
+enum B32 : int { k32Full0 = 0, k32Free0 = 2, k32AccFull0 = 4, k32AccFree0 = 6, k32Drain = 8, k32MatFull0 = 9, k32MatFree0 = 11, k32NumBars = 13 };
+static_assert(k32SumSmem <= kMaxSmemPerCta && k32RowSmem <= kMaxSmemPerCta && k32NumBars * 8 + 16 + 32 <= 256, "shared memory");
+
+// x = h + m + l for two numbers, 8 bits each, cut: exact.  (Nothing is made of an infinity's rest: it becomes NaN, as infinity times the
+// other factor's m or l would, where those are 0.)
+__device__ __forceinline__ uint32_t highs(float x0, float x1) { return __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632); }
+__device__ __forceinline__ float below(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+__device__ __forceinline__ void split3(float x0, float x1, uint32_t (&part)[3])
+{
+    part[0] = highs(x0, x1);
+    x0 = below(x0);
+    x1 = below(x1);
+    part[1] = highs(x0, x1);
+    part[2] = highs(below(x0), below(x1));
+}
+// four channels of a row of an operand tile, at `to` in its first part
+__device__ __forceinline__ void put3(uint8_t* to, const float4& v)
+{
+    uint32_t a[3], b[3];
+    split3(v.x, v.y, a);
+    split3(v.z, v.w, b);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(to + p * k32Part) = make_uint2(a[p], b[p]);
+}
+// the products of parts (of the first factor, of the second) that are taken, the smallest first
+__device__ constexpr int k32First[6] = {1, 0, 2, 0, 1, 0}, k32Second[6] = {1, 2, 0, 1, 0, 0};
+
+constexpr int k32Issuer = 8, k32States = 9;                // warps
+struct Smem32 {
+    uint8_t* base;
+    uint32_t addr, bars, tmem;
+};
+// barriers and tensor memory, by all threads; the first kernel of the two has no barriers for matrices
+template <int kOffBars, int kCols>
+__device__ __forceinline__ Smem32 start32(uint8_t* raw)
+{
+    Smem32 m;
+    m.base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    m.addr = smem_u32(m.base);
+    m.bars = m.addr + kOffBars;
+    uint32_t* slot = reinterpret_cast<uint32_t*>(m.base + kOffBars + k32NumBars * 8);
+    if (threadIdx.x == 0) {
+        for (int u = 0; u < 2; ++u) {
+            mbar_init(m.bars + 8 * (k32Full0 + u), k32Workers);
+            mbar_init(m.bars + 8 * (k32Free0 + u), 1);
+            mbar_init(m.bars + 8 * (k32AccFull0 + u), 1);
+            mbar_init(m.bars + 8 * (k32AccFree0 + u), k32Workers);
+            mbar_init(m.bars + 8 * (k32MatFull0 + u), 1);
+            mbar_init(m.bars + 8 * (k32MatFree0 + u), 1);
+        }
+        mbar_init(m.bars + 8 * k32Drain, 1);
+        slot[1] = 0;       // the flag of those that give up
+        fence_barrier_init();
+        fence_proxy_async_smem();
+    }
+    if (threadIdx.x >> 5 == k32Issuer) {
+        tmem_alloc(smem_u32(slot), kCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    m.tmem = *slot;
+    grid_dependency_sync();
+    return m;
+}
+template <int kOffBars>
+__device__ __forceinline__ Abort abort32(const Smem32& m, const RecurArgs& a)
+{
+    return Abort{reinterpret_cast<volatile int*>(m.base + kOffBars + k32NumBars * 8 + 4), a.status, a.wait_limit ? a.wait_limit - 1 : kSpinLimit};
+}
+
+template <int D>
+__global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __grid_constant__ RecurArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const Smem32 sm = start32<k32SumOffBars, 256>(smem_raw);
+    const Abort ab = abort32<k32SumOffBars>(sm, a);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const RecurRun run = recur_run(a.sums, blockIdx.x);
+    const int heads = recur_heads(a);
+
+    if (warp >= k32Issuer) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32RegsOther));
+        if (warp == k32Issuer) {
+            const uint32_t lead = elect_one();
+            const uint32_t base = __shfl_sync(0xffffffffu, sm.addr, 0), ubars = base + k32SumOffBars, tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
+            const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
+            constexpr uint32_t kLbo = (uint32_t)(k32Tokens * 128 >> 4) << 16;
+            constexpr uint32_t idesc = idesc_bf16(kTile, kTile, 1, 1);
+            bool ok = true;
+            int i = 0;
+            for (int k = 0; k < run.count && ok; ++k) {
+                const RecurAt at = recur_at(a.sums, run, k, heads, a.pair);
+                const int tokens = min(kTile, a.sums.job[at.job].len - at.tile * kTile);
+                for (int from = 0; from < tokens; from += k32Tokens, ++i) {
+                    const int s = i & 1;
+                    if (i >= 2) ok = wait_bar_warp(ubars + 8 * (k32AccFree0 + s), (uint32_t)((i >> 1) - 1) & 1u, ab, 221);
+                    if (ok) ok = wait_bar_warp(ubars + 8 * (k32Full0 + s), (uint32_t)(i >> 1) & 1u, ab, 222);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t x_lo = ((base + s * 6 * k32Part) >> 4) | kLbo, y_lo = ((base + (s * 6 + 3) * k32Part) >> 4) | kLbo;
+                    const int steps = (min(k32Tokens, tokens - from) + 15) >> 4;
+#pragma unroll
+                    for (int p = 0; p < 6; ++p)
+                        for (int ks = 0; ks < steps; ++ks)
+                            mma_ss_if(lead, tmem + s * kTile, desc64(x_lo + (uint32_t)((k32First[p] * k32Part + ks * 2048) >> 4), desc_hi),
+                                      desc64(y_lo + (uint32_t)((k32Second[p] * k32Part + ks * 2048) >> 4), desc_hi), idesc, (p > 0 || ks > 0) ? 1u : 0u);
+                    mma_commit_if(lead, ubars + 8 * (k32Free0 + s));
+                    mma_commit_if(lead, ubars + 8 * (k32AccFull0 + s));
+                }
+            }
+            mma_commit_if(lead, ubars + 8 * k32Drain);      // tensor memory is freed below
+            drain_bar(ubars + 8 * k32Drain, 0);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(k32RegsWorker));
+        // a warp loads rows warp, warp + 8, ..., a lane four channels of each
+        constexpr int kCols = D / 2, kRows = k32Tokens / 8;
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane;      // of the accumulators: a row, half of its head's columns
+        const uint32_t acc_at = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16) + (D == 128 ? 0 : (warp & 3) >> 1 << 6) + half * kCols;
+        float4 xr[kRows], yr[kRows];
+        float sum[kCols];
+        bool ok = true, fresh = true;
+        // the tile that is loaded, and the one whose products are added up
+        RecurAt next = {}, at = {};
+        int k = -1, from = 0, tokens = 0;
+        auto step = [&]() {        // to the next operand tile; false: there is none
+            from += k32Tokens;
+            if (k < 0 || from >= tokens) {
+                if (++k >= run.count) return false;
+                next = recur_at(a.sums, run, k, heads, a.pair);
+                tokens = min(kTile, a.sums.job[next.job].len - next.tile * kTile);
+                from = 0;
+            }
+            return true;
+        };
+        auto fetch = [&]() {
+            const int which = a.sums.job[next.job].which;
+            const RecurRows& rx = which == 0 ? a.k : a.q;
+            const RecurRows& ry = which == 0 ? a.v : a.dout;
+            const int64_t token = (int64_t)next.n * a.block + next.tile * kTile + from;
+            const float* x = static_cast<const float*>(rx.p) + next.b * rx.batch + token * rx.token + next.head * D + lane * 4;
+            const float* y = static_cast<const float*>(ry.p) + next.b * ry.batch + token * ry.token + next.head * D + lane * 4;
+            const bool there = D == 128 || next.head + (lane >> 4) < a.H;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int r = i * 8 + warp;
+                xr[i] = yr[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (there && from + r < tokens) {
+                    xr[i] = *reinterpret_cast<const float4*>(x + r * rx.token);
+                    yr[i] = *reinterpret_cast<const float4*>(y + r * ry.token);
+                }
+            }
+        };
+        auto add = [&](int i) {       // what the tensor cores made of tile i
+            const int s = i & 1;
+            if (!wait_bar_warp(sm.bars + 8 * (k32AccFull0 + s), (uint32_t)(i >> 1) & 1u, ab, 223)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < kCols; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(acc_at + s * kTile + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[c + e] = fresh ? __uint_as_float(o[e]) : sum[c + e] + __uint_as_float(o[e]);
+            }
+            tc_fence_before();
+            mbar_arrive(sm.bars + 8 * (k32AccFree0 + s));
+            fresh = false;
+            return true;
+        };
+        auto leave = [&]() {          // the sums of a unit, or of this CTA's part of it
+            float* to = a.slots + (size_t)at.slot * (D * kTile) + row * D + half * kCols;
+#pragma unroll
+            for (int c = 0; c < kCols; c += 8) {
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(sum[c + e]);
+                store_row32(to + c, w);
+            }
+            fresh = true;
+        };
+        bool more = step(), last = false;
+        if (more) fetch();
+        int i = 0;
+        for (; more && ok; ++i) {
+            const int s = i & 1;
+            if (i >= 2) ok = wait_bar_warp(sm.bars + 8 * (k32Free0 + s), (uint32_t)((i >> 1) - 1) & 1u, ab, 224);
+            if (!ok) break;
+            uint8_t* x_to = sm.base + s * 6 * k32Part;
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                const int r = j * 8 + warp, place = (lane >> 4) * k32Tokens * 128 + r * 128 + (((lane & 15) >> 1) ^ (r & 7)) * 16 + (lane & 1) * 8;
+                put3(x_to + place, xr[j]);
+                put3(x_to + 3 * k32Part + place, yr[j]);
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(sm.bars + 8 * (k32Full0 + s));
+            const RecurAt here = next;
+            const bool ends = here.ends && from + k32Tokens >= tokens;
+            more = step();
+            if (more) fetch();
+            if (i > 0) {
+                ok = add(i - 1);
+                if (ok && last) leave();
+            }
+            at = here;
+            last = ends;
+        }
+        if (ok && i > 0 && add(i - 1) && last) leave();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == k32Issuer) {
+        tc_fence_after();
+        tmem_dealloc(sm.tmem, 256);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(k32Threads, 1)
+tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ RecurArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const Smem32 sm = start32<k32RowOffBars, 512>(smem_raw);
+    const Abort ab = abort32<k32RowOffBars>(sm, a);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const RecurRun run = recur_run(a.rows, blockIdx.x);
+    const int heads = recur_heads(a);
+    constexpr int kMatPart = D == 128 ? kTileBytes : 64 * 64 * 2;
+    constexpr int kParts = D == 128 ? 3 : 6;
+    constexpr int kMats = D == 128 ? 1 : 2;             // units whose states there is room for
+
+    if (warp >= k32Issuer) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32RegsOther));
+        if (warp == k32States) {
+            if (lane == 0) {
+                fence_proxy_async_global();      // the states come from the scan's stores
+                bool ok = true;
+                int mats = 0, unit = -1;
+                for (int k = 0; k < run.count && ok; ++k) {
+                    const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
+                    if (at.unit == unit) continue;
+                    unit = at.unit;
+                    const int u = mats % kMats;
+                    if (mats >= kMats) ok = wait_bar(sm.bars + 8 * (k32MatFree0 + u), (uint32_t)(mats / kMats - 1) & 1u, ab, 230);
+                    if (!ok) break;
+                    const uint32_t bar = sm.bars + 8 * (k32MatFull0 + u), dst = sm.addr + u * kParts * kMatPart;
+                    const CUtensorMap* map = a.back && a.rows.job[at.job].which > 0 ? &map_d : &map_s;
+                    const int row = ((at.b * heads + at.head / a.pair) * a.N + at.n) * kParts * D;
+                    mbar_expect_tx(bar, kParts * kMatPart);
+                    for (int p = 0; p < kParts; ++p) {
+                        tma_load_2d(dst + p * kMatPart, map, bar, 0, row + p * D);
+                        if (D == 128) tma_load_2d(dst + p * kMatPart + kHalfBytes, map, bar, 64, row + p * D);
+                    }
+                    ++mats;
+                }
+                for (int m = mats > kMats ? mats - kMats : 0; m < mats; ++m) drain_bar(sm.bars + 8 * (k32MatFull0 + m % kMats), (uint32_t)(m / kMats) & 1u);
+            }
+        } else if (warp == k32Issuer) {
+            const uint32_t lead = elect_one();
+            const uint32_t base = __shfl_sync(0xffffffffu, sm.addr, 0), ubars = base + k32RowOffBars, tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
+            const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
+            constexpr uint32_t kLboK = 1u << 16, kLboMN = (uint32_t)(kHalfBytes >> 4) << 16;
+            bool ok = true;
+            int used = 0, unit = -1;
+            for (int k = 0; k < run.count && ok; ++k) {
+                const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
+                const bool across = a.back && a.rows.job[at.job].which < 2;       // M^T
+                if (at.unit != unit) {
+                    unit = at.unit;
+                    ok = wait_bar_warp(ubars + 8 * (k32MatFull0 + used % kMats), (uint32_t)(used / kMats) & 1u, ab, 231);
+                    ++used;
+                }
+                if (ok && k >= 2) ok = wait_bar_warp(ubars + 8 * (k32AccFree0 + (k & 1)), (uint32_t)((k >> 1) - 1) & 1u, ab, 232);
+                for (int h = 0; h < 2 && ok; ++h) {      // 64 channels of the rows: half of a head's, or one head's
+                    ok = wait_bar_warp(ubars + 8 * (k32Full0 + h), (uint32_t)k & 1u, ab, 233);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t x_lo = ((base + k32RowOffStage + h * 3 * k32Part) >> 4) | kLboK;
+                    const uint32_t m_lo = ((base + (used - 1) % kMats * kParts * kMatPart) >> 4) | (across ? kLboK : kLboMN);
+                    const uint32_t acc = tmem + (k & 1) * 2 * kTile + h * kTile;
+                    const uint32_t idesc = across ? idesc_bf16(kTile, D, 0, 0) : idesc_bf16(kTile, D, 0, 1);
+#pragma unroll
+                    for (int p = 0; p < 6; ++p)
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks) {
+                            const int part = (D == 128 ? k32Second[p] : h * 3 + k32Second[p]) * kMatPart;
+                            const int in = D == 128 ? (across ? h * kHalfBytes + ks * 32 : h * 8192 + ks * 2048) : (across ? ks * 32 : ks * 2048);
+                            mma_ss_if(lead, acc, desc64(x_lo + (uint32_t)((k32First[p] * k32Part + ks * 32) >> 4), desc_hi), desc64(m_lo + (uint32_t)((part + in) >> 4), desc_hi),
+                                      idesc, (p > 0 || ks > 0) ? 1u : 0u);
+                        }
+                    mma_commit_if(lead, ubars + 8 * (k32Free0 + h));
+                }
+                if (!ok) break;
+                mma_commit_if(lead, ubars + 8 * (k32AccFull0 + (k & 1)));
+                if (at.ends) mma_commit_if(lead, ubars + 8 * (k32MatFree0 + (used - 1) % kMats));
+            }
+            mma_commit_if(lead, ubars + 8 * k32Drain);      // tensor memory is freed below
+            drain_bar(ubars + 8 * k32Drain, 0);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(k32RegsWorker));
+        // half a warp loads rows 2 warp + (0 or 1), + 16, .., a lane four of 64 channels
+        constexpr int kRows = kTile / 16;
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+        // (a head of 128: 64 of its channels, of the sum of two accumulators; of 64: one of the two)
+        const uint32_t acc_at = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * (D == 128 ? 64 : kTile);
+        float4 xr[2][kRows];
+        RecurAt next = {}, at = {};
+        auto fetch = [&](int h) {
+            const int which = a.rows.job[next.job].which, tokens = a.rows.job[next.job].len - next.tile * kTile;
+            const RecurRows& r = !a.back ? a.q : which == 0 ? a.dout : which == 1 ? a.v : a.k;
+            const float* x = static_cast<const float*>(r.p) + next.b * r.batch + ((int64_t)next.n * a.block + next.tile * kTile) * r.token + next.head * D + h * 64 + (lane & 15) * 4;
+            const bool there = D == 128 || next.head + h < a.H;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int t = i * 16 + 2 * warp + (lane >> 4);
+                xr[h][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (there && t < tokens) xr[h][i] = *reinterpret_cast<const float4*>(x + t * r.token);
+            }
+        };
+        auto store = [&](int k) {      // tile k's rows
+            if (!wait_bar_warp(sm.bars + 8 * (k32AccFull0 + (k & 1)), (uint32_t)(k >> 1) & 1u, ab, 234)) return false;
+            tc_fence_after();
+            const RecurJob& j = a.rows.job[at.job];
+            float* to = static_cast<float*>(!a.back ? a.out : j.which == 0 ? a.dq : j.which == 1 ? a.dk : a.dv);
+            const int head = D == 128 ? at.head : at.head + half;
+            const bool mine = at.tile * kTile + row < j.len && head < a.H, wide = wide_rows(to);
+            float* p = to + (((size_t)at.b * a.T + (size_t)at.n * a.block + at.tile * kTile + row) * a.H + head) * D + (D == 128 ? half * 64 : 0);
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(acc_at + (k & 1) * 2 * kTile + c, o);
+                if (D == 128) {
+                    uint32_t o1[32];
+                    tmem_ld32(acc_at + (k & 1) * 2 * kTile + kTile + c, o1);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float(o1[e]));
+                } else {
+                    tmem_wait_ld();
+                }
+                if (mine) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        const uint32_t w[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
+                        if (wide) {
+                            store_row32(p + c + e, w);
+                        } else {
+                            *reinterpret_cast<uint4*>(p + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(p + c + e + 4) = make_uint4(w[4], w[5], w[6], w[7]);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(sm.bars + 8 * (k32AccFree0 + (k & 1)));
+            return true;
+        };
+        bool ok = true;
+        if (run.count > 0) {
+            next = recur_at(a.rows, run, 0, heads, a.pair);
+            fetch(0);
+            fetch(1);
+        }
+        recur_gates<k32Workers>(a, tid, reinterpret_cast<float*>(sm.base + k32RowOffBars + k32NumBars * 8 + 16));
+        for (int k = 0; k < run.count && ok; ++k) {
+            const RecurAt here = next;
+            const bool more = k + 1 < run.count;
+            if (more) next = recur_at(a.rows, run, k + 1, heads, a.pair);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (ok && k >= 1) ok = wait_bar_warp(sm.bars + 8 * (k32Free0 + h), (uint32_t)(k - 1) & 1u, ab, 235);
+                if (!ok) break;
+                uint8_t* x_to = sm.base + k32RowOffStage + h * 3 * k32Part;
+#pragma unroll
+                for (int j = 0; j < kRows; ++j) {
+                    const int r = j * 16 + 2 * warp + (lane >> 4);
+                    put3(x_to + r * 128 + (((lane & 15) >> 1) ^ (r & 7)) * 16 + (lane & 1) * 8, xr[h][j]);
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(sm.bars + 8 * (k32Full0 + h));
+                if (more) fetch(h);
+            }
+            if (ok && k > 0) ok = store(k - 1);
+            at = here;
+        }
+        if (ok && run.count > 0) store(run.count - 1);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == k32Issuer) {
+        tc_fence_after();
+        tmem_dealloc(sm.tmem, 512);
+    }
+}
+
 // [B, T, H, D] with strides, seen as (channel, head, token in block, block, stream): the blocks of full length, or the shorter last one.
 // A stride of zero (one stream's rows for all of them) is a dimension of one.
 int make_map_blocks(CUtensorMap* m, const RecurArgs& a, const RecurRows& r, int part)
@@ -409,7 +827,8 @@ int make_maps(RecurMaps& m, const RecurArgs& a, int which, const RecurRows& r)
 int make_map_states(CUtensorMap* m, const RecurArgs& a, const __nv_bfloat16* p)
 {
     EncodeTiledFn fn = encode_fn();
-    cuuint64_t dims[2] = {(cuuint64_t)a.D, (cuuint64_t)a.B * recur_heads(a) * a.N * a.pair * 2 * a.D};
+    if (fn == nullptr) { set_error("cuTensorMapEncodeTiled is not available from the driver"); return ARL2_ERR_CUDA; }
+    cuuint64_t dims[2] = {(cuuint64_t)a.D, (cuuint64_t)a.B * recur_heads(a) * a.N * a.pair * a.op_parts * a.D};
     cuuint64_t strides[1] = {(cuuint64_t)a.D * 2};
     cuuint32_t box[2] = {64, (cuuint32_t)a.D};
     cuuint32_t estr[2] = {1, 1};
@@ -428,6 +847,10 @@ int recur_sms(int* sms)
         if (e == cudaSuccess) e = opt_in_smem(tc_recur_sums_kernel<64>, kSSmemBytes);
         if (e == cudaSuccess) e = opt_in_smem(tc_recur_rows_kernel<128>, kRSmemBytes);
         if (e == cudaSuccess) e = opt_in_smem(tc_recur_rows_kernel<64>, kRSmemBytes);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_sums32_kernel<128>, k32SumSmem);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_sums32_kernel<64>, k32SumSmem);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_rows32_kernel<128>, k32RowSmem);
+        if (e == cudaSuccess) e = opt_in_smem(tc_recur_rows32_kernel<64>, k32RowSmem);
         return e;
     }, sms);
 }
@@ -446,7 +869,7 @@ bool tc_recur_supported(const RecurArgs& a)
     // (a tensor map's strides are below 2^40 bytes and not zero, its coordinates 31 bits; dO is there backward only, and contiguous)
     for (const RecurRows* r : {&a.q, &a.k, &a.v, &a.dout})
         if (r->token < 1 || r->token >= ((int64_t)1 << 39) / a.block || r->batch >= ((int64_t)1 << 39)) return false;
-    return (int64_t)a.B * recur_heads(a) * a.N * a.pair * 2 * a.D < ((int64_t)1 << 31);
+    return (int64_t)a.B * recur_heads(a) * a.N * a.pair * a.op_parts * a.D < ((int64_t)1 << 31);
 }
 
 int tc_recur_sums(RecurArgs& a, cudaStream_t st)
@@ -455,6 +878,9 @@ int tc_recur_sums(RecurArgs& a, cudaStream_t st)
     int sms = 0;
     if (int r = recur_sms(&sms)) return r;
     recur_cut(a.sums, sms < kRecurCtas ? sms : kRecurCtas);
+    if (a.op_parts == 3)
+        return launched(a.D == 128 ? launch_kernel(tc_recur_sums32_kernel<128>, dim3((unsigned)a.sums.ctas), k32Threads, k32SumSmem, st, a)
+                                   : launch_kernel(tc_recur_sums32_kernel<64>, dim3((unsigned)a.sums.ctas), k32Threads, k32SumSmem, st, a), "tc_recur_sums32_kernel");
     RecurMaps x, y;
     int r = make_maps(x, a, 0, a.k);
     if (r == 0) r = make_maps(y, a, 0, a.v);
@@ -472,11 +898,15 @@ int tc_recur_rows(RecurArgs& a, cudaStream_t st)
     recur_cut(a.rows, sms);
     RecurMaps x;
     CUtensorMap s, d;
-    int r = make_maps(x, a, 0, a.back ? a.dout : a.q);
+    int r = make_map_states(&s, a, a.states_op);
+    if (r == 0) r = make_map_states(&d, a, a.back ? a.dstates_op : a.states_op);
+    if (r != 0) return r;
+    if (a.op_parts == 3)
+        return launched(a.D == 128 ? launch_kernel(tc_recur_rows32_kernel<128>, dim3((unsigned)a.rows.ctas), k32Threads, k32RowSmem, st, s, d, a)
+                                   : launch_kernel(tc_recur_rows32_kernel<64>, dim3((unsigned)a.rows.ctas), k32Threads, k32RowSmem, st, s, d, a), "tc_recur_rows32_kernel");
+    r = make_maps(x, a, 0, a.back ? a.dout : a.q);
     if (r == 0 && a.back) r = make_maps(x, a, 1, a.v);
     if (r == 0 && a.back) r = make_maps(x, a, 2, a.k);
-    if (r == 0) r = make_map_states(&s, a, a.states_op);
-    if (r == 0) r = make_map_states(&d, a, a.back ? a.dstates_op : a.states_op);
     if (r != 0) return r;
     return launched(a.D == 128 ? launch_kernel(tc_recur_rows_kernel<128>, dim3((unsigned)a.rows.ctas), kRThreads, kRSmemBytes, st, x, s, d, a)
                                : launch_kernel(tc_recur_rows_kernel<64>, dim3((unsigned)a.rows.ctas), kRThreads, kRSmemBytes, st, x, s, d, a), "tc_recur_rows_kernel");

@@ -122,6 +122,25 @@ def test_plain_kernels_with_bf16(case):
     check(case, flags=arl2.ARL2_FLAG_FORCE_SIMT)
 
 
+@pytest.mark.parametrize("case", [CASES[3], CASES[8], CASES[14]])
+def test_plain_kernels_with_fp32(case):
+    from paper_2605_16579_b200 import arl2
+
+    check(case, flags=arl2.ARL2_FLAG_FORCE_SIMT)
+
+
+@pytest.mark.parametrize("case", [
+    (1, 4000, 40, 5, 64, FP, True),       # several units for each CTA, a head without a neighbour
+    (2, 6000, 131, 4, 128, FP, True),     # ... and a tile that has three rows
+    (1, 3000, 1500, 3, 64, FP, False),
+    (1, 2000, 2000, 1, 128, FP, True),
+    (3, 65, 33, 1, 64, FP, True),
+])
+@pytest.mark.parametrize("strided", [False, True])
+def test_fp32_rows(case, strided):
+    check(case, strided=strided)
+
+
 @pytest.mark.parametrize("case", [CASES[5], CASES[8], CASES[9]])
 def test_strided_rows(case):
     check(case, strided=True)
@@ -280,6 +299,23 @@ def test_a_wait_that_expires_is_reported():
         r.layer.sync_status()
     r.layer.debug_set_wait_limit(-1)
     got = r.forward(q, k, v, decay)
+    r.layer.sync_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_wait_that_expires_is_reported_fp32(D):
+    arl2, r = op(1, 3, D, FP, 100)
+    q, k, v, decay, _, randn = inputs((1, 950, 100, 3, D, FP, False), 7)
+    do = randn(1, 950, 3, D)
+    want = r.forward(q, k, v, decay)[0], *r.backward(do, q, k, v, decay)[:4]
+    for call in (lambda: r.forward(q, k, v, decay), lambda: r.backward(do, q, k, v, decay)):
+        r.layer.debug_set_wait_limit(0)
+        call()
+        with pytest.raises(arl2.Arl2Error, match="expired"):
+            r.layer.sync_status()
+        r.layer.debug_set_wait_limit(-1)
+    got = r.forward(q, k, v, decay)[0], *r.backward(do, q, k, v, decay)[:4]
     r.layer.sync_status()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
