@@ -329,9 +329,10 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
 
 // ---- the scan over the blocks --------------------------------------------------------------------------
 // A thread has kEach elements of a head's state, four, or one where the heads are few: what it takes is latencies.  Where a
-// block's sums are and how it is gated is found for many blocks at once, a thread each; the sums of kScanAhead blocks are asked for
-// before the first is used.
-constexpr int kScanThreads = 256, kScanAhead = 8;
+// block's sums are and how it is gated is found for many blocks at once, a thread each, and the parts of their sums make a list; kAhead
+// of them are asked for before the first is used, of however many blocks they are.
+constexpr int kScanThreads = 256;
+constexpr int kScanParts = kScanThreads + 2 * kRecurCtas;     // of kScanThreads blocks: one each, and one for each slice of a job
 
 template <int kEach> struct ScanValue;
 template <> struct ScanValue<1> {
@@ -349,19 +350,18 @@ template <> struct ScanValue<4> {
     __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 };
 
-template <int D, int kEach>
-__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, int op_parts, size_t unit, int in_pair, int pair, int e, const ScanValue<kEach>& s)
+template <int D, int kParts, int kEach>
+__device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, size_t unit, int in_pair, int pair, int e, const ScanValue<kEach>& s)
 {
     if (f32 != nullptr) s.store(f32 + (unit * pair + in_pair) * D * D + e);
-    if (op == nullptr) return;
+    if (kParts == 0) return;
     // a bf16 number, and again of what is left; nothing is left of an infinity
-    __nv_bfloat16* to = op + ((unit * pair + in_pair) * op_parts) * D * D + e;
+    __nv_bfloat16* to = op + ((unit * pair + in_pair) * kParts) * D * D + e;
     float rest[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) rest[i] = s.v[i];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-        if (p == op_parts) break;
+    for (int p = 0; p < kParts; ++p) {
         __nv_bfloat16 part[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -374,26 +374,52 @@ __device__ __forceinline__ void scan_store(float* f32, __nv_bfloat16* op, int op
     }
 }
 
-// The parts of a block's sum: `count` slots from `first` on, or none; and the block's gate.
-struct ScanBlock { int first, count; float gate; };
-__device__ __forceinline__ ScanBlock scan_block(const RecurArgs& a, int which, int b, int head, int n)
+// A part of a block's sum: its slot (-1: nothing); with a block's last part, which block it is, otherwise -1.
+struct ScanPart { int slot, block; float gate; };
+// The list for blocks base .. base + here - 1, or from the last of them to the first; its length.  By all threads.
+__device__ __forceinline__ int scan_list(const RecurArgs& a, int which, int b, int head, int base, int here, bool down, ScanPart* parts, int* warp_sums)
 {
-    ScanBlock r = {0, 0, gate_of(a.decay[((size_t)b * a.N + n) * a.H + head])};
-    for (int i = 0; i < a.sums.jobs; ++i) {
-        const RecurJob& j = a.sums.job[i];
-        if (j.which != which || n < j.n0 || n >= j.n0 + j.n_count) continue;
-        const int v = (b * recur_heads(a) + head / a.pair) * j.n_count + n - j.n0;
-        const int c0 = v * j.ntile / j.share, c1 = (v * j.ntile + j.ntile - 1) / j.share;
-        r.first = j.slot0 + v + c0;
-        r.count = c1 - c0 + 1;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, block = base + (down ? here - 1 - tid : tid);
+    int first = -1, count = 0, need = 0;
+    float gate = 0.0f;
+    if (tid < here) {
+        gate = gate_of(a.decay[((size_t)b * a.N + block) * a.H + head]);
+        for (int i = 0; i < a.sums.jobs; ++i) {
+            const RecurJob& j = a.sums.job[i];
+            if (j.which != which || block < j.n0 || block >= j.n0 + j.n_count) continue;
+            const int v = (b * recur_heads(a) + head / a.pair) * j.n_count + block - j.n0;
+            const int c0 = v * j.ntile / j.share, c1 = (v * j.ntile + j.ntile - 1) / j.share;
+            first = j.slot0 + v + c0;
+            count = c1 - c0 + 1;
+        }
+        need = max(count, 1);
     }
-    return r;
+    int upto = need;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int below = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += below;
+    }
+    __syncthreads();        // (the list before this one has been read)
+    if (lane == 31) warp_sums[warp] = upto;
+    __syncthreads();
+    int total = 0, at = upto - need;
+#pragma unroll
+    for (int w = 0; w < kScanThreads / 32; ++w) {
+        at += w < warp ? warp_sums[w] : 0;
+        total += warp_sums[w];
+    }
+    for (int c = 0; c < need; ++c) parts[at + c] = {c < count ? first + c : -1, c + 1 == need ? block : -1, gate};
+    __syncthreads();
+    return total;
 }
 
-template <int D, int kEach>
-__global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_constant__ RecurArgs a)
+template <int D, int kParts, int kEach>
+__global__ void __launch_bounds__(kScanThreads, 2) recur_scan_kernel(const __grid_constant__ RecurArgs a)
 {
-    __shared__ ScanBlock blocks[kScanThreads];
+    constexpr int kAhead = kEach == 1 ? 12 : 8;
+    __shared__ ScanPart parts[kScanParts];
+    __shared__ int warp_sums[kScanThreads / 32];
     // apart: the two directions are different CTAs' work, and <D, S> is left to the step behind
     const int tid = threadIdx.x, e = (blockIdx.x * kScanThreads + tid) * kEach, head = blockIdx.y, b = a.apart ? blockIdx.z >> 1 : blockIdx.z;
     const bool forward = !a.apart || (blockIdx.z & 1) == 0, backward = a.back && (!a.apart || (blockIdx.z & 1) != 0);
@@ -402,48 +428,43 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
     const float* slots = a.slots + (size_t)in_pair * D * D + e;
     using Value = ScanValue<kEach>;
     grid_dependency_sync();
-    // the sums of blocks n, n + way, ..: a part of each at a time
-    auto fetch = [&](Value (&sum)[kScanAhead], int i0, int way, int count) {
-        int most = 0;
+    auto fetch = [&](Value& v, int slot) {
 #pragma unroll
-        for (int i = 0; i < kScanAhead; ++i) {
-#pragma unroll
-            for (int k = 0; k < kEach; ++k) sum[i].v[k] = 0.0f;
-            if (i < count) most = max(most, blocks[i0 + i * way].count);
-        }
-        for (int c = 0; c < most; ++c) {
-            Value o[kScanAhead];
-#pragma unroll
-            for (int i = 0; i < kScanAhead; ++i) {
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) o[i].v[k] = 0.0f;
-                if (i < count && c < blocks[i0 + i * way].count) o[i].load(slots + (size_t)(blocks[i0 + i * way].first + c) * size);
-            }
-#pragma unroll
-            for (int i = 0; i < kScanAhead; ++i)
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) sum[i].v[k] += o[i].v[k];
-        }
+        for (int k = 0; k < kEach; ++k) v.v[k] = 0.0f;
+        if (slot >= 0) v.load(slots + (size_t)slot * size);
     };
-    Value s;
+    auto part = [&](int i, int count) { return i < count ? parts[i] : ScanPart{-1, -1, 0.0f}; };
+    Value s, sum;
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) s.v[k] = 0.0f;
+    for (int k = 0; k < kEach; ++k) s.v[k] = sum.v[k] = 0.0f;
     if (forward && a.state_in != nullptr) s.load(a.state_in + at);
     for (int base = 0; forward && base < a.N; base += kScanThreads) {
-        const int here = min(kScanThreads, a.N - base);
-        __syncthreads();
-        if (tid < here) blocks[tid] = scan_block(a, 0, b, head, base + tid);
-        __syncthreads();
-        for (int i0 = 0; i0 < here; i0 += kScanAhead) {
-            Value sum[kScanAhead];
-            fetch(sum, i0, 1, here - i0);
+        const int count = scan_list(a, 0, b, head, base, min(kScanThreads, a.N - base), false, parts, warp_sums);
+        Value o[kAhead];
 #pragma unroll
-            for (int i = 0; i < kScanAhead; ++i)
-                if (i0 + i < here) {
-                    scan_store<D>(a.states, a.states_op, a.op_parts, unit0 + base + i0 + i, in_pair, a.pair, e, s);
+        for (int i = 0; i < kAhead; ++i) fetch(o[i], part(i, count).slot);
+        for (int i0 = 0; i0 < count; i0 += kAhead) {
+            ScanPart now[kAhead];
+            int next[kAhead];
 #pragma unroll
-                    for (int k = 0; k < kEach; ++k) s.v[k] = fmaf(blocks[i0 + i].gate, s.v[k], sum[i].v[k]);
+            for (int i = 0; i < kAhead; ++i) {
+                now[i] = part(i0 + i, count);
+                next[i] = part(i0 + i + kAhead, count).slot;
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const ScanPart p = now[i];
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) sum.v[k] += o[i].v[k];
+                fetch(o[i], next[i]);
+                if (p.block < 0) continue;
+                scan_store<D, kParts>(a.states, a.states_op, unit0 + p.block, in_pair, a.pair, e, s);
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) {
+                    s.v[k] = fmaf(p.gate, s.v[k], sum.v[k]);
+                    sum.v[k] = 0.0f;
                 }
+            }
         }
     }
     if (!a.back && a.state_out != nullptr) s.store(a.state_out + at);
@@ -454,31 +475,43 @@ __global__ void __launch_bounds__(kScanThreads) recur_scan_kernel(const __grid_c
     const bool with_dots = !a.apart;
     float* dots = a.dots + ((size_t)b * a.H + head) * a.N * (D * D / (32 * kEach)) + e / (32 * kEach);
     for (int base = (a.N - 1) / kScanThreads * kScanThreads; base >= 0; base -= kScanThreads) {
-        const int here = min(kScanThreads, a.N - base);
-        __syncthreads();
-        if (tid < here) blocks[tid] = scan_block(a, 1, b, head, base + tid);
-        __syncthreads();
-        for (int i0 = here - 1; i0 >= 0; i0 -= kScanAhead) {
-            Value sum[kScanAhead], before[kScanAhead];
+        const int count = scan_list(a, 1, b, head, base, min(kScanThreads, a.N - base), true, parts, warp_sums);
+        Value o[kAhead], before[kAhead];
+        auto ask = [&](int i, const ScanPart& p) {
+            fetch(o[i], p.slot);
+            if (with_dots && p.block >= 0) before[i].load(a.states + ((unit0 + p.block) * a.pair + in_pair) * D * D + e);   // (this thread's own)
+        };
 #pragma unroll
-            for (int i = 0; i < kScanAhead; ++i)
-                if (with_dots && i0 - i >= 0) before[i].load(a.states + ((unit0 + base + i0 - i) * a.pair + in_pair) * D * D + e);   // (this thread's own)
-            fetch(sum, i0, -1, i0 + 1);
+        for (int i = 0; i < kAhead; ++i) ask(i, part(i, count));
+        for (int i0 = 0; i0 < count; i0 += kAhead) {
+            ScanPart now[kAhead], next[kAhead];
 #pragma unroll
-            for (int i = 0; i < kScanAhead; ++i)
-                if (i0 - i >= 0) {
-                    const int n = base + i0 - i;
-                    scan_store<D>(a.dstates, a.dstates_op, a.op_parts, unit0 + n, in_pair, a.pair, e, s);
+            for (int i = 0; i < kAhead; ++i) {
+                now[i] = part(i0 + i, count);
+                next[i] = part(i0 + i + kAhead, count);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const ScanPart p = now[i];
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) sum.v[k] += o[i].v[k];
+                if (p.block >= 0) {
+                    scan_store<D, kParts>(a.dstates, a.dstates_op, unit0 + p.block, in_pair, a.pair, e, s);
                     if (with_dots) {
                         float dot = 0.0f;
 #pragma unroll
                         for (int k = 0; k < kEach; ++k) dot = fmaf(s.v[k], before[i].v[k], dot);
                         dot = warp_sum(dot);
-                        if ((tid & 31) == 0) dots[(size_t)n * (D * D / (32 * kEach))] = dot;
+                        if ((tid & 31) == 0) dots[(size_t)p.block * (D * D / (32 * kEach))] = dot;
                     }
 #pragma unroll
-                    for (int k = 0; k < kEach; ++k) s.v[k] = fmaf(blocks[i0 - i].gate, s.v[k], sum[i].v[k]);
+                    for (int k = 0; k < kEach; ++k) {
+                        s.v[k] = fmaf(p.gate, s.v[k], sum.v[k]);
+                        sum.v[k] = 0.0f;
+                    }
                 }
+                ask(i, next[i]);
+            }
         }
     }
     if (a.dstate_in != nullptr) s.store(a.dstate_in + at);
@@ -517,8 +550,10 @@ int launch_scan(RecurArgs& a, cudaStream_t st)
     a.apart = a.back && (long long)a.B * a.H * a.N <= kRecurApart;
     const dim3 grid((unsigned)(D * D / (each * kScanThreads)), (unsigned)a.H, (unsigned)(a.apart ? 2 * a.B : a.B));
     a.dot_parts = D * D / (32 * each);
-    return check_launch(each == 1 ? launch_kernel(recur_scan_kernel<D, 1>, grid, kScanThreads, 0, st, a) : launch_kernel(recur_scan_kernel<D, 4>, grid, kScanThreads, 0, st, a),
-                        "recur_scan_kernel");
+    auto kernel = a.states_op == nullptr ? (each == 1 ? recur_scan_kernel<D, 0, 1> : recur_scan_kernel<D, 0, 4>)
+                  : a.op_parts == 2     ? (each == 1 ? recur_scan_kernel<D, 2, 1> : recur_scan_kernel<D, 2, 4>)
+                                        : (each == 1 ? recur_scan_kernel<D, 3, 1> : recur_scan_kernel<D, 3, 4>);
+    return check_launch(launch_kernel(kernel, grid, kScanThreads, 0, st, a), "recur_scan_kernel");
 }
 
 template <typename T, int D>
