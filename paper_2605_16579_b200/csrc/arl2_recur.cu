@@ -12,6 +12,7 @@
 // (6 heads of 128 fp32, 3 x 2800 tokens: 1.5e-6 off without that, 3.4e-7 with it).
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "row_common.cuh"
 
@@ -414,15 +415,15 @@ __device__ __forceinline__ int scan_list(const RecurArgs& a, int which, int b, i
     return total;
 }
 
-template <int D, int kParts, int kEach>
-__global__ void __launch_bounds__(kScanThreads, 2) recur_scan_kernel(const __grid_constant__ RecurArgs a)
+template <int D, int kParts, int kEach, bool kBack>
+__global__ void __launch_bounds__(kScanThreads, kEach == 1 ? 2 : 4 - kBack - (kParts == 3)) recur_scan_kernel(const __grid_constant__ RecurArgs a)
 {
-    constexpr int kAhead = kEach == 1 ? 12 : 8;
+    constexpr int kAhead = kEach == 1 ? 12 : 6;
     __shared__ ScanPart parts[kScanParts];
     __shared__ int warp_sums[kScanThreads / 32];
     // apart: the two directions are different CTAs' work, and <D, S> is left to the step behind
-    const int tid = threadIdx.x, e = (blockIdx.x * kScanThreads + tid) * kEach, head = blockIdx.y, b = a.apart ? blockIdx.z >> 1 : blockIdx.z;
-    const bool forward = !a.apart || (blockIdx.z & 1) == 0, backward = a.back && (!a.apart || (blockIdx.z & 1) != 0);
+    const int tid = threadIdx.x, e = (blockIdx.x * kScanThreads + tid) * kEach, head = blockIdx.y, b = kBack && a.apart ? blockIdx.z >> 1 : blockIdx.z;
+    const bool forward = !kBack || !a.apart || (blockIdx.z & 1) == 0, backward = kBack && (!a.apart || (blockIdx.z & 1) != 0);
     const int hu = head / a.pair, in_pair = head - hu * a.pair;
     const size_t unit0 = (size_t)(b * recur_heads(a) + hu) * a.N, at = ((size_t)b * a.H + head) * D * D + e, size = (size_t)a.pair * D * D;
     const float* slots = a.slots + (size_t)in_pair * D * D + e;
@@ -467,7 +468,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) recur_scan_kernel(const __gri
             }
         }
     }
-    if (!a.back && a.state_out != nullptr) s.store(a.state_out + at);
+    if (!kBack && a.state_out != nullptr) s.store(a.state_out + at);
     if (!backward) return;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) s.v[k] = 0.0f;
@@ -550,9 +551,12 @@ int launch_scan(RecurArgs& a, cudaStream_t st)
     a.apart = a.back && (long long)a.B * a.H * a.N <= kRecurApart;
     const dim3 grid((unsigned)(D * D / (each * kScanThreads)), (unsigned)a.H, (unsigned)(a.apart ? 2 * a.B : a.B));
     a.dot_parts = D * D / (32 * each);
-    auto kernel = a.states_op == nullptr ? (each == 1 ? recur_scan_kernel<D, 0, 1> : recur_scan_kernel<D, 0, 4>)
-                  : a.op_parts == 2     ? (each == 1 ? recur_scan_kernel<D, 2, 1> : recur_scan_kernel<D, 2, 4>)
-                                        : (each == 1 ? recur_scan_kernel<D, 3, 1> : recur_scan_kernel<D, 3, 4>);
+    auto pick = [&](auto parts) {
+        constexpr int kParts = decltype(parts)::value;
+        return a.back ? (each == 1 ? recur_scan_kernel<D, kParts, 1, true> : recur_scan_kernel<D, kParts, 4, true>)
+                      : (each == 1 ? recur_scan_kernel<D, kParts, 1, false> : recur_scan_kernel<D, kParts, 4, false>);
+    };
+    auto kernel = a.states_op == nullptr ? pick(std::integral_constant<int, 0>{}) : a.op_parts == 2 ? pick(std::integral_constant<int, 2>{}) : pick(std::integral_constant<int, 3>{});
     return check_launch(launch_kernel(kernel, grid, kScanThreads, 0, st, a), "recur_scan_kernel");
 }
 
