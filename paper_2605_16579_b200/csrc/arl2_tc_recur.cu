@@ -522,7 +522,12 @@ __global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __
         const uint32_t acc_at = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16) + (D == 128 ? 0 : (warp & 3) >> 1 << 6) + half * kCols;
         float4 xr[kRows], yr[kRows];
         float sum[kCols];
-        bool ok = true, fresh = true;
+        bool ok = true;
+        auto clear = [&]() {
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) sum[c] = 0.0f;
+        };
+        clear();
         // the tile that is loaded, and the one whose products are added up
         RecurAt next = {}, at = {};
         int k = -1, from = 0, tokens = 0;
@@ -540,17 +545,25 @@ __global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __
             const int which = a.sums.job[next.job].which;
             const RecurRows& rx = which == 0 ? a.k : a.q;
             const RecurRows& ry = which == 0 ? a.v : a.dout;
-            const int64_t token = (int64_t)next.n * a.block + next.tile * kTile + from;
+            const int64_t token = (int64_t)next.n * a.block + next.tile * kTile + from + warp;
             const float* x = static_cast<const float*>(rx.p) + next.b * rx.batch + token * rx.token + next.head * D + lane * 4;
             const float* y = static_cast<const float*>(ry.p) + next.b * ry.batch + token * ry.token + next.head * D + lane * 4;
+            const int64_t x_step = 8 * rx.token, y_step = 8 * ry.token;
+            if (from + k32Tokens <= tokens && (D == 128 || next.head + 1 < a.H)) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i, x += x_step, y += y_step) {
+                    xr[i] = *reinterpret_cast<const float4*>(x);
+                    yr[i] = *reinterpret_cast<const float4*>(y);
+                }
+                return;
+            }
             const bool there = D == 128 || next.head + (lane >> 4) < a.H;
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int r = i * 8 + warp;
+            for (int i = 0; i < kRows; ++i, x += x_step, y += y_step) {
                 xr[i] = yr[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (there && from + r < tokens) {
-                    xr[i] = *reinterpret_cast<const float4*>(x + r * rx.token);
-                    yr[i] = *reinterpret_cast<const float4*>(y + r * ry.token);
+                if (there && from + i * 8 + warp < tokens) {
+                    xr[i] = *reinterpret_cast<const float4*>(x);
+                    yr[i] = *reinterpret_cast<const float4*>(y);
                 }
             }
         };
@@ -564,11 +577,10 @@ __global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __
                 tmem_ld32(acc_at + s * kTile + c, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) sum[c + e] = fresh ? __uint_as_float(o[e]) : sum[c + e] + __uint_as_float(o[e]);
+                for (int e = 0; e < 32; ++e) sum[c + e] += __uint_as_float(o[e]);
             }
             tc_fence_before();
             mbar_arrive(sm.bars + 8 * (k32AccFree0 + s));
-            fresh = false;
             return true;
         };
         auto leave = [&]() {          // the sums of a unit, or of this CTA's part of it
@@ -580,7 +592,7 @@ __global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __
                 for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(sum[c + e]);
                 store_row32(to + c, w);
             }
-            fresh = true;
+            clear();
         };
         bool more = step(), last = false;
         if (more) fetch();
@@ -713,13 +725,19 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
         auto fetch = [&](int h) {
             const int which = a.rows.job[next.job].which, tokens = a.rows.job[next.job].len - next.tile * kTile;
             const RecurRows& r = !a.back ? a.q : which == 0 ? a.dout : which == 1 ? a.v : a.k;
-            const float* x = static_cast<const float*>(r.p) + next.b * r.batch + ((int64_t)next.n * a.block + next.tile * kTile) * r.token + next.head * D + h * 64 + (lane & 15) * 4;
+            const int first = 2 * warp + (lane >> 4);
+            const float* x = static_cast<const float*>(r.p) + next.b * r.batch + ((int64_t)next.n * a.block + next.tile * kTile + first) * r.token + next.head * D + h * 64 + (lane & 15) * 4;
+            const int64_t step = 16 * r.token;
             const bool there = D == 128 || next.head + h < a.H;
+            if (there && tokens >= kTile) {
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int t = i * 16 + 2 * warp + (lane >> 4);
+                for (int i = 0; i < kRows; ++i, x += step) xr[h][i] = *reinterpret_cast<const float4*>(x);
+                return;
+            }
+#pragma unroll
+            for (int i = 0; i < kRows; ++i, x += step) {
                 xr[h][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (there && t < tokens) xr[h][i] = *reinterpret_cast<const float4*>(x + t * r.token);
+                if (there && i * 16 + first < tokens) xr[h][i] = *reinterpret_cast<const float4*>(x);
             }
         };
         auto store = [&](int k) {      // tile k's rows
