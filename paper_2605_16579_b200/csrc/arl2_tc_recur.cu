@@ -16,10 +16,11 @@
 //   same tile read with its other dimension innermost.
 //
 // fp32 I/O (the kernels with 32 in their names): each number is three of bf16, 24 bits, and a product six of its parts' (what is left out is
-// 2^-24 of it on average, 2^-21 at most), the smallest first, so that the tensor cores cut little when they add.  Eight warps load the rows, take them apart
-// into operand tiles of 64 tokens (sums) or 64 channels (rows), two of them by turns, and later add up or store what the tensor cores have
-// made of the tile before; the states come apart from the scan.  (8 heads of 128, 14000 tokens: sums 81 -> 43 us, rows 75 -> 34 against
-// pairs of TF32 numbers on warp-level instructions, of which an SM does 240 multiplications a clock.)
+// 2^-24 of it on average, 2^-21 at most), the smallest first, so that the tensor cores cut little when they add.  Eight warps load the rows and
+// take them apart into operand tiles of 64 tokens (sums) or 64 channels (rows), two of them by turns; the states come apart from the
+// scan.  (8 heads of 128, 14000 tokens: sums 81 -> 38 us, rows 75 -> 34 against pairs of TF32 numbers on warp-level instructions, of which an
+// SM does 240 multiplications a clock.  The tensor cores are busy for a third of it: what is left is the way from memory through registers to an
+// operand tile, which has room for two.)
 //
 // Every wait is bounded; a CTA that gives up records ARL2_ERR_TIMEOUT, drains what is in flight and frees its tensor memory.
 #include "tc_common.cuh"
@@ -387,10 +388,16 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
 }
 
 // ---- fp32: three bf16 numbers for each ---------------------------------------------------------------------------
-constexpr int k32Workers = 256, k32Threads = 384;          // 2 warpgroups that load, split and store; {MMA issuer, states, 2 idle}
-constexpr int k32RegsWorker = 216, k32RegsOther = 72;
-// (setmaxnreg.inc waits without a bound for registers of the CTA's own launch allocation)
-static_assert(k32Workers * k32RegsWorker + (k32Threads - k32Workers) * k32RegsOther <= k32Threads * ((65536 / k32Threads) / 8 * 8), "register pool");
+// Warps and registers.  setmaxnreg moves registers within what the CTA was launched with (and waits for them without a bound).
+// Sums: 2 warpgroups that load, split and add up; {issuer, 3 idle}.
+constexpr int k32Workers = 256, k32SumThreads = 384, k32SumIssuer = 8;
+constexpr int k32SumRegs = 216, k32SumRegsOther = 72;
+static_assert(256 * k32SumRegs + 128 * k32SumRegsOther <= k32SumThreads * ((65536 / k32SumThreads) / 8 * 8), "register pool");
+// Rows: 2 warpgroups that load and split; one that stores, with the registers that it starts with; {issuer, states, 2 idle}.  (Us at 12 heads of
+// 128, 14000 tokens backward with the same warps for all three: 151; so: 142; with two that store, or rows put together in shared memory: 150, 177.)
+constexpr int k32RowThreads = 512, k32RowStore = 8, k32RowIssuer = 12, k32RowStates = 13;
+constexpr int k32RowRegs = 160, k32RowRegsOther = 64, k32RowRegsStart = 65536 / k32RowThreads;
+static_assert(256 * k32RowRegs + 128 * k32RowRegsStart + 128 * k32RowRegsOther <= k32RowThreads * k32RowRegsStart, "register pool");
 constexpr int k32Tokens = 64;                              // of an operand tile of the sums
 constexpr int k32Part = 16 * 1024;                         // a part of an operand tile: 64 tokens x 128 channels, or 128 x 64
 constexpr int k32SumOffBars = 2 * 6 * k32Part;
@@ -426,13 +433,12 @@ __device__ __forceinline__ void put3(uint8_t* to, const float4& v)
 // the products of parts (of the first factor, of the second) that are taken, the smallest first
 __device__ constexpr int k32First[6] = {1, 0, 2, 0, 1, 0}, k32Second[6] = {1, 2, 0, 1, 0, 0};
 
-constexpr int k32Issuer = 8, k32States = 9;                // warps
 struct Smem32 {
     uint8_t* base;
     uint32_t addr, bars, tmem;
 };
-// barriers and tensor memory, by all threads; the first kernel of the two has no barriers for matrices
-template <int kOffBars, int kCols>
+// barriers and tensor memory, by all threads; kReaders of the accumulators
+template <int kOffBars, int kCols, int kIssuer, int kReaders>
 __device__ __forceinline__ Smem32 start32(uint8_t* raw)
 {
     Smem32 m;
@@ -445,7 +451,7 @@ __device__ __forceinline__ Smem32 start32(uint8_t* raw)
             mbar_init(m.bars + 8 * (k32Full0 + u), k32Workers);
             mbar_init(m.bars + 8 * (k32Free0 + u), 1);
             mbar_init(m.bars + 8 * (k32AccFull0 + u), 1);
-            mbar_init(m.bars + 8 * (k32AccFree0 + u), k32Workers);
+            mbar_init(m.bars + 8 * (k32AccFree0 + u), kReaders);
             mbar_init(m.bars + 8 * (k32MatFull0 + u), 1);
             mbar_init(m.bars + 8 * (k32MatFree0 + u), 1);
         }
@@ -454,7 +460,7 @@ __device__ __forceinline__ Smem32 start32(uint8_t* raw)
         fence_barrier_init();
         fence_proxy_async_smem();
     }
-    if (threadIdx.x >> 5 == k32Issuer) {
+    if (threadIdx.x >> 5 == kIssuer) {
         tmem_alloc(smem_u32(slot), kCols);
         tmem_relinquish();
     }
@@ -472,18 +478,18 @@ __device__ __forceinline__ Abort abort32(const Smem32& m, const RecurArgs& a)
 }
 
 template <int D>
-__global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __grid_constant__ RecurArgs a)
+__global__ void __launch_bounds__(k32SumThreads, 1) tc_recur_sums32_kernel(const __grid_constant__ RecurArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
-    const Smem32 sm = start32<k32SumOffBars, 256>(smem_raw);
+    const Smem32 sm = start32<k32SumOffBars, 256, k32SumIssuer, k32Workers>(smem_raw);
     const Abort ab = abort32<k32SumOffBars>(sm, a);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const RecurRun run = recur_run(a.sums, blockIdx.x);
     const int heads = recur_heads(a);
 
-    if (warp >= k32Issuer) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32RegsOther));
-        if (warp == k32Issuer) {
+    if (warp >= k32SumIssuer) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32SumRegsOther));
+        if (warp == k32SumIssuer) {
             const uint32_t lead = elect_one();
             const uint32_t base = __shfl_sync(0xffffffffu, sm.addr, 0), ubars = base + k32SumOffBars, tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
             const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
@@ -515,7 +521,7 @@ __global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __
             drain_bar(ubars + 8 * k32Drain, 0);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(k32RegsWorker));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(k32SumRegs));
         // a warp loads rows warp, warp + 8, ..., a lane four channels of each
         constexpr int kCols = D / 2, kRows = k32Tokens / 8;
         const int half = warp >> 2, row = (warp & 3) * 32 + lane;      // of the accumulators: a row, half of its head's columns
@@ -625,18 +631,18 @@ __global__ void __launch_bounds__(k32Threads, 1) tc_recur_sums32_kernel(const __
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == k32Issuer) {
+    if (warp == k32SumIssuer) {
         tc_fence_after();
         tmem_dealloc(sm.tmem, 256);
     }
 }
 
 template <int D>
-__global__ void __launch_bounds__(k32Threads, 1)
+__global__ void __launch_bounds__(k32RowThreads, 1)
 tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_d, const __grid_constant__ RecurArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
-    const Smem32 sm = start32<k32RowOffBars, 512>(smem_raw);
+    const Smem32 sm = start32<k32RowOffBars, 512, k32RowIssuer, 128>(smem_raw);
     const Abort ab = abort32<k32RowOffBars>(sm, a);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const RecurRun run = recur_run(a.rows, blockIdx.x);
@@ -645,9 +651,9 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
     constexpr int kParts = D == 128 ? 3 : 6;
     constexpr int kMats = D == 128 ? 1 : 2;             // units whose states there is room for
 
-    if (warp >= k32Issuer) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32RegsOther));
-        if (warp == k32States) {
+    if (warp >= k32RowIssuer) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32RowRegsOther));
+        if (warp == k32RowStates) {
             if (lane == 0) {
                 fence_proxy_async_global();      // the states come from the scan's stores
                 bool ok = true;
@@ -671,7 +677,7 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
                 }
                 for (int m = mats > kMats ? mats - kMats : 0; m < mats; ++m) drain_bar(sm.bars + 8 * (k32MatFull0 + m % kMats), (uint32_t)(m / kMats) & 1u);
             }
-        } else if (warp == k32Issuer) {
+        } else if (warp == k32RowIssuer) {
             const uint32_t lead = elect_one();
             const uint32_t base = __shfl_sync(0xffffffffu, sm.addr, 0), ubars = base + k32RowOffBars, tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
             const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0) >> 32);
@@ -713,15 +719,54 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
             mma_commit_if(lead, ubars + 8 * k32Drain);      // tensor memory is freed below
             drain_bar(ubars + 8 * k32Drain, 0);
         }
+    } else if (warp >= k32RowStore) {
+        recur_gates<128>(a, tid - k32RowStore * 32, reinterpret_cast<float*>(sm.base + k32RowOffBars + k32NumBars * 8 + 16));
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t acc_at = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        for (int k = 0; k < run.count; ++k) {
+            const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
+            const RecurJob& j = a.rows.job[at.job];
+            float* to = static_cast<float*>(!a.back ? a.out : j.which == 0 ? a.dq : j.which == 1 ? a.dk : a.dv);
+            const bool inside = at.tile * kTile + row < j.len, wide = wide_rows(to);
+            float* p = to + (((size_t)at.b * a.T + (size_t)at.n * a.block + at.tile * kTile + row) * a.H + at.head) * D;
+            if (!wait_bar_warp(sm.bars + 8 * (k32AccFull0 + (k & 1)), (uint32_t)(k >> 1) & 1u, ab, 234)) break;
+            tc_fence_after();
+            const uint32_t acc = acc_at + (k & 1) * 2 * kTile;
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) {      // a head of 128 channels: the sum of two accumulators; two heads of 64: one each
+                uint32_t o[32];
+                tmem_ld32(acc + (D == 128 ? c : (c >> 6) * kTile + (c & 32)), o);
+                if (D == 128) {
+                    uint32_t o1[32];
+                    tmem_ld32(acc + kTile + c, o1);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float(o1[e]));
+                } else {
+                    tmem_wait_ld();
+                }
+                if (inside && (D == 128 || at.head + (c >> 6) < a.H)) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        const uint32_t w[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
+                        if (wide) {
+                            store_row32(p + c + e, w);
+                        } else {
+                            *reinterpret_cast<uint4*>(p + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(p + c + e + 4) = make_uint4(w[4], w[5], w[6], w[7]);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(sm.bars + 8 * (k32AccFree0 + (k & 1)));
+        }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(k32RegsWorker));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(k32RowRegs));
         // half a warp loads rows 2 warp + (0 or 1), + 16, .., a lane four of 64 channels
         constexpr int kRows = kTile / 16;
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
-        // (a head of 128: 64 of its channels, of the sum of two accumulators; of 64: one of the two)
-        const uint32_t acc_at = sm.tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * (D == 128 ? 64 : kTile);
         float4 xr[2][kRows];
-        RecurAt next = {}, at = {};
+        RecurAt next = {};
         auto fetch = [&](int h) {
             const int which = a.rows.job[next.job].which, tokens = a.rows.job[next.job].len - next.tile * kTile;
             const RecurRows& r = !a.back ? a.q : which == 0 ? a.dout : which == 1 ? a.v : a.k;
@@ -740,53 +785,13 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
                 if (there && i * 16 + first < tokens) xr[h][i] = *reinterpret_cast<const float4*>(x);
             }
         };
-        auto store = [&](int k) {      // tile k's rows
-            if (!wait_bar_warp(sm.bars + 8 * (k32AccFull0 + (k & 1)), (uint32_t)(k >> 1) & 1u, ab, 234)) return false;
-            tc_fence_after();
-            const RecurJob& j = a.rows.job[at.job];
-            float* to = static_cast<float*>(!a.back ? a.out : j.which == 0 ? a.dq : j.which == 1 ? a.dk : a.dv);
-            const int head = D == 128 ? at.head : at.head + half;
-            const bool mine = at.tile * kTile + row < j.len && head < a.H, wide = wide_rows(to);
-            float* p = to + (((size_t)at.b * a.T + (size_t)at.n * a.block + at.tile * kTile + row) * a.H + head) * D + (D == 128 ? half * 64 : 0);
-#pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t o[32];
-                tmem_ld32(acc_at + (k & 1) * 2 * kTile + c, o);
-                if (D == 128) {
-                    uint32_t o1[32];
-                    tmem_ld32(acc_at + (k & 1) * 2 * kTile + kTile + c, o1);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float(o1[e]));
-                } else {
-                    tmem_wait_ld();
-                }
-                if (mine) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        const uint32_t w[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
-                        if (wide) {
-                            store_row32(p + c + e, w);
-                        } else {
-                            *reinterpret_cast<uint4*>(p + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                            *reinterpret_cast<uint4*>(p + c + e + 4) = make_uint4(w[4], w[5], w[6], w[7]);
-                        }
-                    }
-                }
-            }
-            tc_fence_before();
-            mbar_arrive(sm.bars + 8 * (k32AccFree0 + (k & 1)));
-            return true;
-        };
         bool ok = true;
         if (run.count > 0) {
             next = recur_at(a.rows, run, 0, heads, a.pair);
             fetch(0);
             fetch(1);
         }
-        recur_gates<k32Workers>(a, tid, reinterpret_cast<float*>(sm.base + k32RowOffBars + k32NumBars * 8 + 16));
         for (int k = 0; k < run.count && ok; ++k) {
-            const RecurAt here = next;
             const bool more = k + 1 < run.count;
             if (more) next = recur_at(a.rows, run, k + 1, heads, a.pair);
 #pragma unroll
@@ -803,14 +808,11 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
                 mbar_arrive(sm.bars + 8 * (k32Full0 + h));
                 if (more) fetch(h);
             }
-            if (ok && k > 0) ok = store(k - 1);
-            at = here;
         }
-        if (ok && run.count > 0) store(run.count - 1);
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == k32Issuer) {
+    if (warp == k32RowIssuer) {
         tc_fence_after();
         tmem_dealloc(sm.tmem, 512);
     }
@@ -897,8 +899,8 @@ int tc_recur_sums(RecurArgs& a, cudaStream_t st)
     if (int r = recur_sms(&sms)) return r;
     recur_cut(a.sums, sms < kRecurCtas ? sms : kRecurCtas);
     if (a.op_parts == 3)
-        return launched(a.D == 128 ? launch_kernel(tc_recur_sums32_kernel<128>, dim3((unsigned)a.sums.ctas), k32Threads, k32SumSmem, st, a)
-                                   : launch_kernel(tc_recur_sums32_kernel<64>, dim3((unsigned)a.sums.ctas), k32Threads, k32SumSmem, st, a), "tc_recur_sums32_kernel");
+        return launched(a.D == 128 ? launch_kernel(tc_recur_sums32_kernel<128>, dim3((unsigned)a.sums.ctas), k32SumThreads, k32SumSmem, st, a)
+                                   : launch_kernel(tc_recur_sums32_kernel<64>, dim3((unsigned)a.sums.ctas), k32SumThreads, k32SumSmem, st, a), "tc_recur_sums32_kernel");
     RecurMaps x, y;
     int r = make_maps(x, a, 0, a.k);
     if (r == 0) r = make_maps(y, a, 0, a.v);
@@ -920,8 +922,8 @@ int tc_recur_rows(RecurArgs& a, cudaStream_t st)
     if (r == 0) r = make_map_states(&d, a, a.back ? a.dstates_op : a.states_op);
     if (r != 0) return r;
     if (a.op_parts == 3)
-        return launched(a.D == 128 ? launch_kernel(tc_recur_rows32_kernel<128>, dim3((unsigned)a.rows.ctas), k32Threads, k32RowSmem, st, s, d, a)
-                                   : launch_kernel(tc_recur_rows32_kernel<64>, dim3((unsigned)a.rows.ctas), k32Threads, k32RowSmem, st, s, d, a), "tc_recur_rows32_kernel");
+        return launched(a.D == 128 ? launch_kernel(tc_recur_rows32_kernel<128>, dim3((unsigned)a.rows.ctas), k32RowThreads, k32RowSmem, st, s, d, a)
+                                   : launch_kernel(tc_recur_rows32_kernel<64>, dim3((unsigned)a.rows.ctas), k32RowThreads, k32RowSmem, st, s, d, a), "tc_recur_rows32_kernel");
     r = make_maps(x, a, 0, a.back ? a.dout : a.q);
     if (r == 0 && a.back) r = make_maps(x, a, 1, a.v);
     if (r == 0 && a.back) r = make_maps(x, a, 2, a.k);
