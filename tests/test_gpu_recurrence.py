@@ -133,6 +133,7 @@ def test_plain_kernels_with_fp32(case):
     (1, 4000, 40, 5, 64, FP, True),       # several units for each CTA, a head without a neighbour
     (2, 6000, 131, 4, 128, FP, True),     # ... and a tile that has three rows
     (1, 3000, 1500, 3, 64, FP, False),
+    (2, 3000, 1433, 3, 64, FP, True),
     (1, 2000, 2000, 1, 128, FP, True),
     (3, 65, 33, 1, 64, FP, True),
 ])
@@ -306,8 +307,8 @@ def test_a_wait_that_expires_is_reported():
 @pytest.mark.parametrize("D", [64, 128])
 def test_a_wait_that_expires_is_reported_fp32(D):
     arl2, r = op(1, 3, D, FP, 100)
-    q, k, v, decay, _, randn = inputs((1, 950, 100, 3, D, FP, False), 7)
-    do = randn(1, 950, 3, D)
+    q, k, v, decay, _, randn = inputs((1, 2950, 100, 3, D, FP, False), 7)
+    do = randn(1, 2950, 3, D)
     want = r.forward(q, k, v, decay)[0], *r.backward(do, q, k, v, decay)[:4]
     for call in (lambda: r.forward(q, k, v, decay), lambda: r.backward(do, q, k, v, decay)):
         r.layer.debug_set_wait_limit(0)
