@@ -472,7 +472,7 @@ int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* cfg, const f
  *   d_out    [B, tokens, H, D] contiguous, 16-byte aligned
  * bf16 I/O: operands of the matrix products are bf16, the states as two bf16 numbers (2^-17), fp32 accumulation, fp32 states; fp32 I/O: products to
  * 2^-21 (each operand as three bf16 numbers).  The workspace (256-byte aligned) holds nothing between calls; it has a state of 4 D^2 bytes
- * for each block and head, and as many sums (short blocks of long sequences want much of it).
+ * (fp32 I/O: 6 D^2) for each block and head, and as many sums (short blocks of long sequences want much of it).
  */
 typedef struct {
     uint32_t struct_size;

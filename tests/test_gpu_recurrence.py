@@ -147,6 +147,18 @@ def test_strided_rows(case):
     check(case, strided=True)
 
 
+@pytest.mark.parametrize("case", [
+    (1, 900, 3, 2, 64, BF, True),
+    (1, 512, 2, 1, 128, BF, False),
+    (1, 1300, 5, 2, 64, FP, True),
+    (2, 257, 1, 1, 64, FP, True),
+    (1, 1541, 6, 1, 128, FP, False),
+])
+def test_hundreds_of_blocks(case):
+    """More than a list of the scan has."""
+    check(case)
+
+
 def test_one_stream_for_all():
     """Rows that a stride of zero repeats over the streams."""
     B, T, block, H, D = 3, 300, 130, 2, 128
