@@ -251,14 +251,26 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+
+    const uint64_t policy = tile_policy(a);
+    auto load = [&](int k, const RecurAt& at) {
+        const RecurJob& j = a.rows.job[at.job];
+        const uint32_t bar = bars + 8 * (kRBarFull0 + k % kRStages);
+        mbar_expect_tx(bar, (uint32_t)box_rows(j.len) * 256u);
+        const RecurRows& x = !a.back ? a.q : j.which == 0 ? a.dout : j.which == 1 ? a.v : a.k;
+        load_tile<D>(smem_base + kROffStage + (k % kRStages) * kTileBytes, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b, policy);
+    };
+    // the caller's tensors have been there since before the scan: the first tiles are asked for while it runs
+    const int early = min(count, kRStages);
+    if (tid == 0)
+        for (int k = 0; k < early; ++k) load(k, recur_at(a.rows, run, k, heads, a.pair));
     grid_dependency_sync();
 
     if (warp == 0) {
         if (lane == 0) {
-            const uint64_t policy = tile_policy(a);
             fence_proxy_async_global();      // the states come from the scan's stores
             bool ok = true;
-            int issued = 0, mats = 0, unit = -1;
+            int issued = early, mats = 0, unit = -1;
             for (int k = 0; k < count && ok; ++k) {
                 const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
                 const RecurJob& j = a.rows.job[at.job];
@@ -277,13 +289,10 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
                     }
                     ++mats;
                 }
-                const int s = k % kRStages;
-                if (k >= kRStages) ok = wait_bar(bars + 8 * (kRBarFree0 + s), (uint32_t)((k / kRStages) - 1) & 1u, ab, 211);
+                if (k < early) continue;
+                ok = wait_bar(bars + 8 * (kRBarFree0 + k % kRStages), (uint32_t)((k / kRStages) - 1) & 1u, ab, 211);
                 if (!ok) break;
-                const uint32_t bar = bars + 8 * (kRBarFull0 + s);
-                mbar_expect_tx(bar, (uint32_t)box_rows(j.len) * 256u);
-                const RecurRows& x = !a.back ? a.q : j.which == 0 ? a.dout : j.which == 1 ? a.v : a.k;
-                load_tile<D>(smem_base + kROffStage + s * kTileBytes, &maps_x.m[j.part][j.which], bar, at, j, x.batch == 0 ? 0 : at.b, policy);
+                load(k, at);
                 ++issued;
             }
             for (int m = (issued > kRStages ? issued - kRStages : 0); m < issued; ++m) drain_bar(bars + 8 * (kRBarFull0 + m % kRStages), (uint32_t)(m / kRStages) & 1u);
@@ -344,7 +353,6 @@ tc_recur_rows_kernel(const __grid_constant__ RecurMaps maps_x, const __grid_cons
         recur_gates<256>(a, tid - 64, reinterpret_cast<float*>(smem + kROffBars + kRNumBars * 8 + 16));      // (while the first tiles are on their way)
         const int half = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint64_t policy = tile_policy(a);
         for (int k = 0; k < count; ++k) {
             const RecurAt at = recur_at(a.rows, run, k, heads, a.pair);
             const RecurJob& j = a.rows.job[at.job];
@@ -468,7 +476,6 @@ __device__ __forceinline__ Smem32 start32(uint8_t* raw)
     __syncthreads();
     tc_fence_after();
     m.tmem = *slot;
-    grid_dependency_sync();
     return m;
 }
 template <int kOffBars>
@@ -482,6 +489,7 @@ __global__ void __launch_bounds__(k32SumThreads, 1) tc_recur_sums32_kernel(const
 {
     extern __shared__ uint8_t smem_raw[];
     const Smem32 sm = start32<k32SumOffBars, 256, k32SumIssuer, k32Workers>(smem_raw);
+    grid_dependency_sync();
     const Abort ab = abort32<k32SumOffBars>(sm, a);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const RecurRun run = recur_run(a.sums, blockIdx.x);
@@ -651,6 +659,8 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
     constexpr int kParts = D == 128 ? 3 : 6;
     constexpr int kMats = D == 128 ? 1 : 2;             // units whose states there is room for
 
+    // (loads of the caller's tensors need not wait for the scan)
+    if (warp >= k32RowStore) grid_dependency_sync();
     if (warp >= k32RowIssuer) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(k32RowRegsOther));
         if (warp == k32RowStates) {
@@ -791,6 +801,7 @@ tc_recur_rows32_kernel(const __grid_constant__ CUtensorMap map_s, const __grid_c
             fetch(0);
             fetch(1);
         }
+        grid_dependency_sync();
         for (int k = 0; k < run.count && ok; ++k) {
             const bool more = k + 1 < run.count;
             if (more) next = recur_at(a.rows, run, k + 1, heads, a.pair);
