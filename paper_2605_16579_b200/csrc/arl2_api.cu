@@ -1754,9 +1754,9 @@ int recur_args(const char* who, arl2_ctx* ctx, const arl2_recurrence_config* c, 
     uint8_t* w = static_cast<uint8_t*>(ws);
     a.pair = cfg.D == 64 ? 2 : 1;
     a.op_parts = cfg.io_dtype == ARL2_FP32 ? 3 : 2;
-    // fp32 heads of 64 channels with tiles for less than half of 148 SMs: the kernels that split each number have more to do before their first
-    // product (us forward of 2 x 2 heads, 1000 tokens in blocks of 64: 18.3 there, 13.4 with the plain ones; of 3 heads, 1560 in blocks of 128:
-    // 20.2 and 17.7; of 4 heads, 4680 in blocks of 1560: 21.8 and 27.6.  Heads of 128: 15 and 21 with one tile each)
+    // fp32 heads of 64 channels with tiles for at most half of 148 SMs: the kernels that split each number have more to do before their first
+    // product (us forward, these and the plain ones: 2 x 2 heads, 1000 tokens in blocks of 64: 15.9 and 12.1; 3 heads, 1560 in blocks of 128:
+    // 17.8 and 16.3; 4 heads, 4680 in blocks of 1560: 20.0 and 26.2.  Heads of 128 with a tile each: 14 and 20)
     const bool few = cfg.io_dtype == ARL2_FP32 && cfg.D == 64 && (int64_t)a.B * a.H * a.N * ((a.block + kRecurTile - 1) / kRecurTile) <= 148 / 2;
     tc = recur_tensor_cores(cfg) && !few && tc_recur_supported(a);
     a.slots = reinterpret_cast<float*>(w + lay.slots);
