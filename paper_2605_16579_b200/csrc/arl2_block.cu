@@ -308,7 +308,8 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
 // Threads of a CTA, and CTAs of an SM at least: small ones for rows of up to 1536 channels, so that some of them fit beside one another
 // and work while others wait.
 constexpr int kFewCtas = 2;
-constexpr int kTileFew = 192, kTileMany = 384, kTileWarps = kTileMany / 32;
+constexpr int kTileFew = 192, kTileMany = 384;
+constexpr int kTileRows = 24;      // of a tile at most: what is known of a row has a place in arrays of so many, whatever the threads
 constexpr int tile_ctas(int threads) { return threads == kTileFew ? kFewCtas : 1; }
 struct TileShape {
     int rows;            // of a tile
@@ -322,7 +323,7 @@ struct TileShape {
 TileShape tile_shape(int d, int row_bytes, int room, int most_rows, int threads)
 {
     TileShape s;
-    s.rows = std::max(1, std::min({room / 2 / row_bytes, most_rows, 2 * kTileWarps}));
+    s.rows = std::max(1, std::min({room / 2 / row_bytes, most_rows, kTileRows}));
     const int vecs = d / 8;
     s.split = std::max(1, std::min(threads / 32 / s.rows, (vecs + 31) / 32));
     s.vecs = (vecs + threads - 1) / threads;
@@ -371,10 +372,12 @@ struct ModulateTile {
 template <typename T, typename R, int kTileThreads, int kVecs, bool kAll>
 __global__ void __launch_bounds__(kTileThreads, tile_ctas(kTileThreads)) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a, const __grid_constant__ TileShape shape)
 {
-    constexpr int kTileWarps = kTileThreads / 32;
+    constexpr int kWarps = kTileThreads / 32;
+    static_assert(2 * kWarps <= kTileRows, "a warp's part, and the parts behind it that make up a row");
+    static_assert(kTileRows * 2 * (sizeof(RowKnown) + sizeof(RowPart)) <= 3 * 1024, "what tile_room leaves for the arrays");
     extern __shared__ __align__(16) uint8_t tile_smem[];
-    __shared__ __align__(16) RowKnown rows_n[2 * kTileWarps], rows_y[2 * kTileWarps];
-    __shared__ __align__(16) RowPart part_n[2 * kTileWarps], part_y[2 * kTileWarps];     // (rows that are not there are read, too)
+    __shared__ __align__(16) RowKnown rows_n[kTileRows], rows_y[kTileRows];
+    __shared__ __align__(16) RowPart part_n[kTileRows], part_y[kTileRows];     // (rows that are not there are read, too)
     __shared__ __align__(16) f2 joined[kTileThreads / 2][4];       // sums of a group of threads, for another one
     const int d = a.m.d, vecs = d / 8, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int first = (int)min((long long)blockIdx.x * a.m.share, (long long)a.m.rows), rows = min(a.m.share, a.m.rows - first);
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(kTileThreads, tile_ctas(kTileThreads)) modulat
 
         // ---- sums of the rows
         if (has_n || post) {
-            for (int item = warp; item < (n * shape.split + kTileWarps - 1) / kTileWarps * kTileWarps; item += kTileWarps) {
+            for (int item = warp; item < (n * shape.split + kWarps - 1) / kWarps * kWarps; item += kWarps) {
                 const int row = item / shape.split, piece = item - row * shape.split;
                 const bool mine = row < n;
                 const int v0 = vecs * piece / shape.split, v1 = vecs * (piece + 1) / shape.split;
