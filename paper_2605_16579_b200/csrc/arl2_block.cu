@@ -368,7 +368,7 @@ struct ModulateTile {
 //   dx = dr + i (g - hat mean(g hat) - [LayerNorm] mean(g));   dgate = sum dx P(y), dscale = w sum dn hat, dshift = sum dn,
 //   dw = sum (1 + scale) dn hat;   dy = the same of P for the gradient dx gate w_post, dw_post = sum gate dx yhat.
 // Six units of memory: r, dn, dr and y in, dx and dy out.  The weights' sums are made from the frames' sums.
-// kAll: all four are there, no P and no weights (flags that are known cost nothing in the loops).
+// kAll: all four are there, no P, no weights and no gradients of them (flags that are known cost nothing in the loops).
 template <typename T, typename R, int kTileThreads, int kVecs, bool kAll>
 __global__ void __launch_bounds__(kTileThreads, tile_ctas(kTileThreads)) modulate_backward_kernel(const __grid_constant__ ModulateBackArgs a, const __grid_constant__ TileShape shape)
 {
@@ -1446,7 +1446,7 @@ int modulate(const ModulateArgs& a, int dtype, bool wide, cudaStream_t st)
 int modulate_backward(const ModulateBackArgs& a, int dtype, bool wide, cudaStream_t st)
 {
     const int vecs = a.m.d / 8, each = (vecs + kTileMany - 1) / kTileMany;
-    const bool all = a.dn != nullptr && a.dr != nullptr && a.m.y != nullptr && a.m.post_norm == kNormNone && a.m.weight == nullptr;
+    const bool all = a.dn != nullptr && a.dr != nullptr && a.m.y != nullptr && a.m.post_norm == kNormNone && a.m.weight == nullptr && a.dweight == nullptr;
 #define ARL2_CALL(n, v, f) (dtype == ARL2_FP32 ? launch_modulate_backward<float, float, n, v, f>(a, st) : wide ? launch_modulate_backward<__nv_bfloat16, float, n, v, f>(a, st) : launch_modulate_backward<__nv_bfloat16, __nv_bfloat16, n, v, f>(a, st))
     if (vecs <= kTileFew) return all ? ARL2_CALL(kTileFew, 1, true) : ARL2_CALL(kTileFew, 1, false);
     if (all) return each == 1 ? ARL2_CALL(kTileMany, 1, true) : each == 2 ? ARL2_CALL(kTileMany, 2, true) : ARL2_CALL(kTileMany, 3, true);
