@@ -36,9 +36,9 @@ __device__ __forceinline__ Tf32<kExact> tf32_split(float x)
         r.l = 0;
     } else {
         r.h = tf32_head(x);
-        // (an infinity has no remainder)
+        // (A NaN's head may be any number, the sum carries out of its mantissa; its remainder is NaN.  An infinity has no remainder.)
         const float rem = x - __uint_as_float(r.h);
-        r.l = __float_as_uint(fabsf(x) <= 3.0e38f ? rem : 0.0f);
+        r.l = __float_as_uint(fabsf(x) > 3.4e38f ? 0.0f : rem);
     }
     return r;
 }
