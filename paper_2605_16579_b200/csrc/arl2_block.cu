@@ -1263,17 +1263,18 @@ struct RowPlan {
     int share = 0, runs = 0, ctas = 0;
 };
 
-// CTAs of a kernel that the device holds at once; found once per device, kernel and team width (whoever finds it finds the same).
+// CTAs of a kernel that the device holds at once; found once per device, kernel, team width and size of the head's tables, all that
+// `threads` and `smem` depend on: whoever finds it finds the same, whatever was called before.
 struct Resident {
-    std::atomic<int> found[kMaxDev][kTeamWarps + 1];
+    std::atomic<int> found[kMaxDev][kTeamWarps + 1][2];
 };
 template <typename K>
-int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, int most_smem, const char* what)
+int resident_ctas(Resident& r, K kernel, int warps, bool wide_head, int threads, size_t smem, int most_smem, const char* what)
 {
     int dev = -1;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || dev < 0 || dev >= kMaxDev) { set_error("cannot identify the current device (%s)", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
-    int ctas = r.found[dev][warps].load(std::memory_order_relaxed);
+    int ctas = r.found[dev][warps][wide_head].load(std::memory_order_relaxed);
     if (ctas != 0) return ctas;
     int sms = 0, per_sm = 0;
     e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -1286,7 +1287,7 @@ int resident_ctas(Resident& r, K kernel, int warps, int threads, size_t smem, in
         return ARL2_ERR_CUDA;
     }
     ctas = sms * per_sm;
-    r.found[dev][warps].store(ctas, std::memory_order_relaxed);
+    r.found[dev][warps][wide_head].store(ctas, std::memory_order_relaxed);
     return ctas;
 }
 
@@ -1317,7 +1318,7 @@ int launch_modulate(ModulateArgs a, RowPlan p, cudaStream_t st)
     constexpr int kPer = kVecs * kModulatePieces<T, R>;
     const int threads = p.warps * 32 * p.teams;
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
-    const int ctas = resident_ctas(resident, kernel, p.warps, threads, smem, kMaxSmemPerCta - kRowStatic, "modulate");
+    const int ctas = resident_ctas(resident, kernel, p.warps, false, threads, smem, kMaxSmemPerCta - kRowStatic, "modulate");
     if (ctas < 0) return ctas;
     cut_rows(p, a.rows, (long long)ctas * p.teams);
     a.share = p.share;
@@ -1346,7 +1347,7 @@ int launch_modulate_backward(ModulateBackArgs a, cudaStream_t st)
     auto kernel = modulate_backward_kernel<T, R, kTileThreads, kVecs, kAll>;
     constexpr int kRoom = tile_room(kTileThreads);
     const int row_bytes = a.m.d * 2 * (int)(sizeof(T) + sizeof(R));
-    const int ctas = resident_ctas(resident, kernel, 0, kTileThreads, kRoom, kRoom, "modulate_backward");
+    const int ctas = resident_ctas(resident, kernel, 0, false, kTileThreads, kRoom, kRoom, "modulate_backward");
     if (ctas < 0) return ctas;
     RowPlan p;
     p.teams = 1;
@@ -1388,7 +1389,7 @@ int launch_rotate(RotateArgs a, RowPlan q, cudaStream_t st)
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0) + angle_bytes(q.teams, a.D);
-    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate");
+    const int ctas = resident_ctas(resident, kernel, q.warps, a.D == 128, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate");
     if (ctas < 0) return ctas;
     cut_rotation(q, k, a, ctas, 1LL << 40, 1);
     a.q_share = q.share;
@@ -1406,7 +1407,7 @@ int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
     const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0) + angle_bytes(q.teams, a.r.D);
-    const int ctas = resident_ctas(resident, kernel, q.warps, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate_backward");
+    const int ctas = resident_ctas(resident, kernel, q.warps, a.r.D == 128, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate_backward");
     if (ctas < 0) return ctas;
     if (a.dq_weight == nullptr && a.dk_weight == nullptr) a.parts = nullptr;
     cut_rotation(q, k, a.r, ctas, a.parts != nullptr ? block_runs(std::max(a.r.q_width, a.r.k_width), kRotateBackVecs) : 1LL << 40, a.parts != nullptr ? kLeastRows : 1);
