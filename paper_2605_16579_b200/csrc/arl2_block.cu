@@ -176,11 +176,20 @@ __device__ __forceinline__ void load_factor(f2 (&out)[4], const FrameRows& f, in
     }
 }
 
+// Rows of a frame from token t of a stream on.  (frame * size is a token; the frame behind the last one may begin past 31 bits.)
+__host__ __device__ constexpr int frame_left(int frame, int size, int tokens, int t)
+{
+    const int from = frame * size, rest = tokens - from;
+    return (rest < size ? rest : size) - (t - from);
+}
+static_assert(frame_left(0, 7, 20, 3) == 4 && frame_left(2, 7, 20, 14) == 6 && frame_left(2, 7, 20, 19) == 1 &&
+              frame_left(0, 1100000000, 1200000000, 5) == 1099999995 && frame_left(1, 1100000000, 1200000000, 1150000000) == 50000000, "frame_left");
+
 // The frame that a run of rows is in: a step per row.
 struct FrameWalk {
     int b, t, frame, left;        // left: rows of this frame from here on, 0 before the first row and behind a frame's last
     __device__ __forceinline__ FrameWalk(const ModulateArgs& a, long long row) : b((int)(row / a.T)), t((int)(row - (long long)b * a.T)), frame(t / a.frame), left(0) {}
-    __device__ __forceinline__ void enter(const ModulateArgs& a) { left = min((frame + 1) * a.frame, a.T) - t; }
+    __device__ __forceinline__ void enter(const ModulateArgs& a) { left = frame_left(frame, a.frame, a.T, t); }
     __device__ __forceinline__ void next(const ModulateArgs& a)
     {
         if (--left == 0) ++frame;
