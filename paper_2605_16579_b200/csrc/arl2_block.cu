@@ -2,14 +2,14 @@
 // and rotation (norm of queries and keys, positions along several axes), each with its backward pass.
 //
 // All of them go over rows of channels once: what bounds them is memory, a few operations per byte.  A row is held by a team of
-// warps, eight channels a lane (sixteen where queries and keys are one row), so that sums over the row are shuffles and one
-// exchange through shared memory.  A team has a run of consecutive rows; it asks for the next row before it works on this one,
-// and keeps the rows per frame (gate, scale, shift) in registers while the frame lasts.  Sums, means and
-// statistics are fp32; each output is rounded once.
+// warps, up to four vectors of eight channels a lane, so that sums over the row are shuffles and one exchange through shared memory.
+// A team has a run of consecutive rows; the next ones are on their way to shared memory while it works on this one, and the rows per
+// frame (gate, scale, shift) stay in registers while the frame lasts.  (The modulation's backward pass goes over tiles of rows
+// instead.)  Sums, means and statistics are fp32; each output is rounded once.
 //
-// Sums over tokens (gradients of gate, scale, shift and weights) are held in registers over a team's run.  A frame inside
-// one run is written as it is; of one that several runs share each team leaves its part in the workspace, and a second small kernel
-// adds the parts in the order of the rows: bitwise reproducible, no atomics.
+// Sums over tokens (gradients of gate, scale, shift and weights) are held in registers over a run of rows, a team's or (the modulation's)
+// a CTA's.  A frame inside one run is written as it is; of one that several runs share each leaves its part in the workspace, and a second
+// small kernel adds the parts in the order of the rows: bitwise reproducible, no atomics.
 #include <algorithm>
 #include <atomic>
 
@@ -27,10 +27,10 @@ constexpr int kRowStatic = 9 * 1024;        // shared memory of a CTA besides, a
 constexpr int kAngleMost = 6 * 1024;
 
 // Rows in flight, and the one in work: as many as there is room for with CTAs of this many threads, four at most.  `pieces` of 16 bytes that
-// a lane has of a row, `beside`: bytes that it has besides.
-__host__ __device__ constexpr int row_stages(int pieces, int threads, int beside)
+// a lane has of a row.
+__host__ __device__ constexpr int row_stages(int pieces, int threads)
 {
-    const int n = ((kMaxSmemPerCta - kRowStatic) / threads - beside) / (16 * pieces);
+    const int n = (kMaxSmemPerCta - kRowStatic) / threads / (16 * pieces);
     return n < 1 ? 1 : n > 4 ? 4 : n;
 }
 
@@ -60,7 +60,7 @@ __device__ __forceinline__ void clear(f2 (&v)[kVecs][4])
 }
 
 // A team that makes the statistics of a row, with the channels of each warp and of one's own.
-struct NormTeam : Team<4> {
+struct NormTeam : Team<2> {
     const float* counts;     // [kTeamWarps]
     float per_channel;       // one over those of this lane's warp
     float over, eps;         // one over the row's
@@ -72,19 +72,19 @@ struct NormTeam : Team<4> {
         per_channel = 1.0f / (float)ch.warp_channels(threadIdx.x >> 5);
         over = 1.0f / (float)ch.d;
         eps = e;
-        Team<4>::start(smem);
+        Team<2>::start(smem);
     }
 };
 
-// Mean of a row and one over its deviation, and (kDots) the sums of g and of g * (x - mean), from what the team's warps know: the
-// mean of each one's channels and the sum of squares about it (about zero for an RMS norm).  Joined with the means' differences, so
-// that no digits are lost where the mean is large.  Channels that a lane does not have are zeros in x and g.
-struct RowSums { float mean, inverse, g, gx; };
+// Mean of a row and one over its deviation, from what the team's warps know: the mean of each one's channels and the sum of squares about
+// it (about zero for an RMS norm).  Joined with the means' differences, so that no digits are lost where the mean is large.  Channels
+// that a lane does not have are zeros in x.
+struct RowSums { float mean, inverse; };
 
-template <bool kDots, int kVecs, bool kFull>
-__device__ __forceinline__ RowSums row_sums(NormTeam& team, const f2 (&x)[kVecs][4], const f2 (&g)[kVecs][4], bool layer, const LaneChannels<kVecs, kFull>& ch)
+template <int kVecs, bool kFull>
+__device__ __forceinline__ RowSums row_sums(NormTeam& team, const f2 (&x)[kVecs][4], bool layer, const LaneChannels<kVecs, kFull>& ch)
 {
-    float mine[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float mine[2] = {0.0f, 0.0f};
     if (layer) {
         f2 s[2] = {0, 0};
 #pragma unroll
@@ -93,7 +93,7 @@ __device__ __forceinline__ RowSums row_sums(NormTeam& team, const f2 (&x)[kVecs]
             for (int e = 0; e < 4; ++e) s[e & 1] = add2(s[e & 1], x[i][e]);
         mine[0] = warp_sum(lo_plus_hi(add2(s[0], s[1]))) * team.per_channel;
     }
-    f2 m2[2] = {0, 0}, sg[2] = {0, 0}, sgx[2] = {0, 0};
+    f2 m2[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const f2 m = both(ch.has(i) ? -mine[0] : 0.0f);
@@ -101,22 +101,13 @@ __device__ __forceinline__ RowSums row_sums(NormTeam& team, const f2 (&x)[kVecs]
         for (int e = 0; e < 4; ++e) {
             const f2 c = add2(x[i][e], m);
             m2[e & 1] = fma2(c, c, m2[e & 1]);
-            if (kDots) {
-                sg[e & 1] = add2(sg[e & 1], g[i][e]);
-                sgx[e & 1] = fma2(g[i][e], c, sgx[e & 1]);
-            }
         }
     }
     mine[1] = warp_sum(lo_plus_hi(add2(m2[0], m2[1])));
-    if (kDots) {
-        if (layer) mine[2] = warp_sum(lo_plus_hi(add2(sg[0], sg[1])));
-        mine[3] = warp_sum(lo_plus_hi(add2(sgx[0], sgx[1])));
-    }
     RowSums r;
-    r.mean = r.g = 0.0f;
+    r.mean = 0.0f;
     if (team.warps == 1) {
         r.mean = mine[0];
-        r.g = mine[2];
     } else {
         const float* all = team.exchange(mine);
         if (layer) {
@@ -125,33 +116,19 @@ __device__ __forceinline__ RowSums row_sums(NormTeam& team, const f2 (&x)[kVecs]
                 r.mean += fmaf(n.x, m.x, n.y * m.y) + fmaf(n.z, m.z, n.w * m.w);
             }
             r.mean *= team.over;
-            mine[1] = mine[3] = 0.0f;
+            mine[1] = 0.0f;
             for (int w = 0; w < team.warps; w += 4) {
                 const float4 n4 = *reinterpret_cast<const float4*>(team.counts + w), m4 = *reinterpret_cast<const float4*>(all + w);
                 const float4 q4 = *reinterpret_cast<const float4*>(all + kTeamWarps + w);
                 const float n[4] = {n4.x, n4.y, n4.z, n4.w}, m[4] = {m4.x - r.mean, m4.y - r.mean, m4.z - r.mean, m4.w - r.mean}, q[4] = {q4.x, q4.y, q4.z, q4.w};
-                float4 g4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), x4 = g4;
-                if (kDots) {
-                    g4 = *reinterpret_cast<const float4*>(all + 2 * kTeamWarps + w);
-                    x4 = *reinterpret_cast<const float4*>(all + 3 * kTeamWarps + w);
-                }
-                const float gg[4] = {g4.x, g4.y, g4.z, g4.w}, gx[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {       // (there is no warp behind the last: no channels, and sums of zero)
-                    mine[1] += fmaf(n[i] * m[i], m[i], q[i]);
-                    if (kDots) {
-                        r.g += gg[i];
-                        mine[3] += fmaf(m[i], gg[i], gx[i]);
-                    }
-                }
+                for (int i = 0; i < 4; ++i) mine[1] += fmaf(n[i] * m[i], m[i], q[i]);     // (there is no warp behind the last: no channels, and a sum of zero)
             }
         } else {
             mine[1] = team.sum(all + kTeamWarps);
-            if (kDots) mine[3] = team.sum(all + 3 * kTeamWarps);
         }
     }
     r.inverse = rsqrtf(mine[1] * team.over + team.eps);
-    r.gx = mine[3];
     return r;
 }
 
@@ -205,8 +182,8 @@ template <typename T, typename R> constexpr int kModulatePieces = kPieces<R> + k
 template <typename T, typename R, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __grid_constant__ ModulateArgs a)
 {
-    __shared__ __align__(16) float place[kTeamFloats<4>], channels[kTeamWarps];
-    constexpr int kPer = kModulatePieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
+    __shared__ __align__(16) float place[kTeamFloats<2>], channels[kTeamWarps];
+    constexpr int kPer = kModulatePieces<T, R>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs));
     extern __shared__ uint4 ring_smem[];
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
@@ -269,7 +246,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
         }
         if (has_y) {
             if (a.post_norm != 0) {
-                const RowSums s = row_sums<false>(team, u, u, a.post_norm == kNormLayer, ch);
+                const RowSums s = row_sums(team, u, a.post_norm == kNormLayer, ch);
                 const f2 m = both(-s.mean), k = both(s.inverse);
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i)
@@ -290,7 +267,7 @@ __global__ void __launch_bounds__(row_threads(kVecs)) modulate_kernel(const __gr
             r_out += a.d;
         }
         if (has_n) {
-            const RowSums s = row_sums<false>(team, v, v, a.norm == kNormLayer, ch);
+            const RowSums s = row_sums(team, v, a.norm == kNormLayer, ch);
             const f2 m = both(-s.mean), k = both(s.inverse);
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
@@ -974,7 +951,7 @@ template <typename T, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) rotate_kernel(const __grid_constant__ RotateArgs a)
 {
     __shared__ __align__(16) float place[kTeamFloats<1>];
-    constexpr int kPer = kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
+    constexpr int kPer = kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs));
     extern __shared__ uint4 ring_smem[];
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
@@ -1090,7 +1067,7 @@ template <typename T, int kVecs, bool kFull>
 __global__ void __launch_bounds__(row_threads(kVecs)) rotate_backward_kernel(const __grid_constant__ RotateBackArgs a)
 {
     __shared__ __align__(16) float place[kTeamFloats<2>];
-    constexpr int kPer = 2 * kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs), 0);
+    constexpr int kPer = 2 * kPieces<T>, kRowStages = row_stages(kVecs * kPer, row_threads(kVecs));
     extern __shared__ uint4 ring_smem[];
     RowRing<kVecs * kPer, kRowStages> ring;
     ring.start(ring_smem, threadIdx.y * blockDim.x + threadIdx.x, blockDim.x * blockDim.y);
@@ -1326,27 +1303,12 @@ int launch_modulate(ModulateArgs a, RowPlan p, cudaStream_t st)
     auto kernel = modulate_kernel<T, R, kVecs, kFull>;
     constexpr int kPer = kVecs * kModulatePieces<T, R>;
     const int threads = p.warps * 32 * p.teams;
-    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0);
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs));
     const int ctas = resident_ctas(resident, kernel, p.warps, false, threads, smem, kMaxSmemPerCta - kRowStatic, "modulate");
     if (ctas < 0) return ctas;
     cut_rows(p, a.rows, (long long)ctas * p.teams);
     a.share = p.share;
     return check_launch(launch_block(kernel, dim3((unsigned)p.ctas), team_block(p), smem, st, a), "modulate_kernel");
-}
-
-// SMs of the current device
-int device_sms(const char* what)
-{
-    static std::atomic<int> found[kMaxDev];
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess || dev < 0 || dev >= kMaxDev) { set_error("cannot identify the current device (%s)", cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
-    int sms = found[dev].load(std::memory_order_relaxed);
-    if (sms != 0) return sms;
-    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess || sms < 1) { set_error("%s: cannot read the SM count (%s)", what, cudaGetErrorString(e)); return ARL2_ERR_CUDA; }
-    found[dev].store(sms, std::memory_order_relaxed);
-    return sms;
 }
 
 template <typename T, typename R, int kTileThreads, int kVecs, bool kAll>
@@ -1397,7 +1359,7 @@ int launch_rotate(RotateArgs a, RowPlan q, cudaStream_t st)
     constexpr int kPer = kVecs * kPieces<T>;
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
-    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0) + angle_bytes(q.teams, a.D);
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs)) + angle_bytes(q.teams, a.D);
     const int ctas = resident_ctas(resident, kernel, q.warps, a.D == 128, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate");
     if (ctas < 0) return ctas;
     cut_rotation(q, k, a, ctas, 1LL << 40, 1);
@@ -1415,7 +1377,7 @@ int launch_rotate_backward(RotateBackArgs a, RowPlan q, cudaStream_t st)
     constexpr int kPer = 2 * kVecs * kPieces<T>;
     RowPlan k;
     const int threads = q.warps * 32 * q.teams;
-    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs), 0) + angle_bytes(q.teams, a.r.D);
+    const size_t smem = (size_t)threads * 16 * kPer * row_stages(kPer, row_threads(kVecs)) + angle_bytes(q.teams, a.r.D);
     const int ctas = resident_ctas(resident, kernel, q.warps, a.r.D == 128, threads, smem, kMaxSmemPerCta - kRowStatic + kAngleMost, "rotate_backward");
     if (ctas < 0) return ctas;
     if (a.dq_weight == nullptr && a.dk_weight == nullptr) a.parts = nullptr;

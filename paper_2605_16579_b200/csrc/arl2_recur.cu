@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int m0 = (warp >> 2) * kM * 16, n0 = (warp & 3) * kN * 8;
     const RecurRun run = recur_run(a.sums, blockIdx.x);
-    const int first = 0, last = run.count;
+    const int last = run.count;
     grid_dependency_sync();
 
     float sum[kM][kN][4];
@@ -107,11 +107,11 @@ __global__ void __launch_bounds__(kRThreads) recur_sums_kernel(const __grid_cons
             }
         }
     };
-    if (first >= last) return;
-    enter(first);
+    if (last == 0) return;
+    enter(0);
     fetch(0);
     bool fresh = true;
-    for (int tile = first; tile < last; ++tile) {
+    for (int tile = 0; tile < last; ++tile) {
         if (fresh) {
 #pragma unroll
             for (int i = 0; i < kM; ++i)
@@ -213,10 +213,10 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int m0 = (warp >> 2) * 16, n0 = (warp & 3) * kN * 8;
     const RecurRun run = recur_run(a.rows, blockIdx.x);
-    const int first = 0, last = run.count;
+    const int last = run.count;
     grid_dependency_sync();
     recur_gates<kRThreads>(a, tid, smem);
-    if (first >= last) return;
+    if (last == 0) return;
 
     float4 xr[kLoads];
     RecurAt at;
@@ -239,10 +239,10 @@ __global__ void __launch_bounds__(kRThreads) recur_rows_kernel(const __grid_cons
             if (row < tokens) xr[i] = load4(x + row * x_step + c);
         }
     };
-    enter(first);
+    enter(0);
     fetch(0);
     int unit = -1;
-    for (int tile = first; tile < last; ++tile) {
+    for (int tile = 0; tile < last; ++tile) {
         const RecurAt here = at;
         const int which = a.rows.job[here.job].which, here_tokens = tokens;
         const bool across = a.back && which < 2;      // M^T: rows of M are the result's columns
