@@ -1754,10 +1754,12 @@ int recur_args(const char* who, arl2_ctx* ctx, const arl2_recurrence_config* c, 
     uint8_t* w = static_cast<uint8_t*>(ws);
     a.pair = cfg.D == 64 ? 2 : 1;
     a.op_parts = cfg.io_dtype == ARL2_FP32 ? 3 : 2;
-    // fp32 heads of 64 channels with tiles for at most half of 148 SMs: the kernels that split each number have more to do before their first
-    // product (us forward, these and the plain ones: 2 x 2 heads, 1000 tokens in blocks of 64: 15.9 and 12.1; 3 heads, 1560 in blocks of 128:
-    // 17.8 and 16.3; 4 heads, 4680 in blocks of 1560: 20.0 and 26.2.  Heads of 128 with a tile each: 14 and 20)
-    const bool few = cfg.io_dtype == ARL2_FP32 && cfg.D == 64 && (int64_t)a.B * a.H * a.N * ((a.block + kRecurTile - 1) / kRecurTile) <= 148 / 2;
+    // fp32 heads of 64 channels with tiles for at most half of 148 SMs (a third backward, where there are five products of them and not two): the
+    // kernels that split each number have more to do before their first product.  Us as graph replays, these and the plain ones, forward: 2 heads, 74
+    // blocks of 64 tokens 18.4 and 14.5, 100 blocks 19.5 and 15.9; 3 heads, 24 blocks of 128 18.5 and 17.4, 42 blocks 21.4 and 22.9; 8 heads, 8 blocks of
+    // 256 18.5 and 18.5, 10 blocks 19.8 and 26.7.  Backward: 24 blocks of 64 19.6 and 15.9, 74 blocks 23.7 and 22.6; 16 blocks of 128 23.1 and 20.0,
+    // 24 blocks 24.1 and 27.7; 3 blocks of 256 21.6 and 19.7, 4 blocks 22.2 and 25.7.  (Heads of 128 with a tile each forward: 14 and 20.)
+    const bool few = cfg.io_dtype == ARL2_FP32 && cfg.D == 64 && (int64_t)a.B * a.H * a.N * ((a.block + kRecurTile - 1) / kRecurTile) <= (back ? 148 / 3 : 148 / 2);
     tc = recur_tensor_cores(cfg) && !few && tc_recur_supported(a);
     a.slots = reinterpret_cast<float*>(w + lay.slots);
     if (tc) {
