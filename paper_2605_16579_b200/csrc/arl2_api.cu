@@ -1719,7 +1719,7 @@ RecurLayout recur_layout(const arl2_config& cfg, const arl2_recurrence_config& c
     l.states = off;  off += operand;
     l.dstates = off; off += back ? operand : 0;
     l.beside = off;  off += back && tc ? state : 0;
-    l.dbeside = off; off += back && tc && cfg.B * cfg.H * blocks <= kRecurApart ? state : 0;
+    l.dbeside = off; off += back && tc && recur_apart(cfg.B, cfg.H, cfg.D, (int64_t)blocks) ? state : 0;
     l.dots = off;    off += back ? align_up((size_t)cfg.B * cfg.H * blocks * (dd / 32) * sizeof(float)) : 0;
     l.total = off;
     return l;
@@ -1766,7 +1766,7 @@ int recur_args(const char* who, arl2_ctx* ctx, const arl2_recurrence_config* c, 
         a.states_op = reinterpret_cast<__nv_bfloat16*>(w + lay.states);
         a.dstates_op = back ? reinterpret_cast<__nv_bfloat16*>(w + lay.dstates) : nullptr;
         a.states = back ? reinterpret_cast<float*>(w + lay.beside) : nullptr;
-        a.dstates = back && cfg.B * cfg.H * (size_t)a.N <= kRecurApart ? reinterpret_cast<float*>(w + lay.dbeside) : nullptr;
+        a.dstates = back && recur_apart(cfg.B, cfg.H, cfg.D, a.N) ? reinterpret_cast<float*>(w + lay.dbeside) : nullptr;
     } else {
         a.pair = 1;
         a.states = reinterpret_cast<float*>(w + lay.states);

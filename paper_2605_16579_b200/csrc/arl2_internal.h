@@ -456,9 +456,21 @@ struct RecurArgs {
 };
 __host__ __device__ inline int recur_heads(const RecurArgs& a) { return (a.H + a.pair - 1) / a.pair; }
 __device__ __forceinline__ float gate_of(float logit) { return 1.0f / (1.0f + expf(-logit)); }
+// Backward, the scan's two directions go at once and leave <D, S> to the step behind, which reads both states for it again, where the
+// states are so few that one direction does not fill the SMs: a CTA has 1024 elements, and 3 of both directions fit on an SM of 148.  (Us
+// of a backward pass, bf16, as graph replays, one direction after the other and so: 2 heads of 64, 100 blocks of 64 tokens 30 and 22, 592 blocks
+// 152 and 85; 2 heads of 128, 592 blocks of 256 238 and 184; 12 heads of 128, 8 blocks of 64 28.7 and 26.7; 16 heads of 128 and more, by the CTAs of
+// a direction: 160 and 192 CTAs 0.91 times the time, 256 1.02, 320 1.08, 384 1.11.  fp32: 160 CTAs 0.98, 256 1.00, 320 1.04.  Heads of 64: 160
+// CTAs 0.91, 224 0.99, 288 1.02.)  The number of blocks does not matter for the time, as far as that goes; it bounds the workspace, which has the
+// second states in fp32 then.
+constexpr int kRecurApart = 4 * 148;       // blocks of all heads at most
+constexpr int kRecurApartStates = 148 * 3 / 2 * 1024;      // elements of all heads' states at most
+inline bool recur_apart(int B, int H, int D, int64_t blocks)
+{
+    return B * H * blocks <= kRecurApart && (int64_t)B * H * D * D <= kRecurApartStates;
+}
 // da_n = alpha_n (1 - alpha_n) <D_{n+1}, S_n>, in the kernel behind the scan, by kThreads threads of each CTA (`thread`: which of them):
 // from the scan's parts a warp for each block of a head, or from the states themselves all of them.  `smem`: a number for each warp.
-constexpr int kRecurApart = 4 * 148;       // blocks of all heads up to which the scan leaves that to them
 template <int kThreads>
 __device__ __forceinline__ void recur_gates(const RecurArgs& a, int thread, float* smem)
 {

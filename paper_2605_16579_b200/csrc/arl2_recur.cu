@@ -557,9 +557,7 @@ template <int D>
 int launch_scan(RecurArgs& a, cudaStream_t st)
 {
     const int each = scan_each(a);
-    // both directions at once where the states are few: their products are read again then (us of a backward scan and the step behind
-    // it over 21 blocks of 2 x 5 heads of 64 channels: 18 and 10 one after the other, 13 and 12 so)
-    a.apart = a.back && (long long)a.B * a.H * a.N <= kRecurApart;
+    a.apart = a.back && recur_apart(a.B, a.H, D, a.N);
     const dim3 grid((unsigned)(D * D / (each * kScanThreads)), (unsigned)a.H, (unsigned)(a.apart ? 2 * a.B : a.B));
     a.dot_parts = D * D / (32 * each);
     auto pick = [&](auto parts) {
