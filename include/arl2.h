@@ -471,7 +471,10 @@ int arl2_rotate_backward(arl2_ctx* ctx, const arl2_rotation_config* cfg, const f
  *                context's own state is set by arl2_set_state, not here.)
  *   d_out    [B, tokens, H, D] contiguous, 16-byte aligned
  * bf16 I/O: operands of the matrix products are bf16, the states as two bf16 numbers (2^-17), fp32 accumulation, fp32 states; fp32 I/O: products to
- * 2^-21 (each operand as three bf16 numbers).  The workspace (256-byte aligned) holds nothing between calls; it has a state of 4 D^2 bytes
+ * 2^-21, each operand as three bf16 numbers.  Calls of few tokens (fp32, heads of 64), contexts with ARL2_FLAG_FORCE_SIMT and rows that a stride of
+ * zero repeats over the tokens take pairs of TF32 numbers instead, of fp32 operands and of all states: below 2^-19.  What a NaN or an infinity enters is not
+ * finite, and nothing else is changed by it; since products are made of parts, it may be NaN where the formula has an infinity.
+ * The workspace (256-byte aligned) holds nothing between calls; it has a state of 4 D^2 bytes
  * (fp32 I/O: 6 D^2) for each block and head, and as many sums (short blocks of long sequences want much of it).
  */
 typedef struct {

@@ -649,7 +649,10 @@ class Cache:
 
 
 class _BlockOp:
-    """What stands around a layer's core shares its context: B, H, D, dtype, device."""
+    """What stands around a layer's core shares its context: B, H, D, dtype, device.
+
+    The calls record nothing for autograd, whatever requires a gradient: ``backward`` is called with what ``forward`` was given, by hand or from an
+    autograd function (examples/train_memory.py has three)."""
 
     def __init__(self, layer):
         self.layer = layer

@@ -7,7 +7,7 @@
 //
 // This file has the scan, and sums and rows without tensor memory (contexts that ask for it, rows that a stride of zero repeats):
 // warp-level matrix instructions on TF32 numbers.  A fp32 operand is taken as a head of 11 bits and a remainder of 11 more, three products (remainder times remainder
-// left out): off by 2^-22 of each product; bf16 inputs are exact in the head alone.  The tensor cores cut what does not fit when they
+// left out): off by some 2^-22 of each product, below 2^-19 always; bf16 inputs are exact in the head alone.  The tensor cores cut what does not fit when they
 // add, always to the same side, so a sum stays with them for 32 terms only and is then added to the others by a rounding addition
 // (6 heads of 128 fp32, 3 x 2800 tokens: 1.5e-6 off without that, 3.4e-7 with it).
 #include <algorithm>
